@@ -59,9 +59,11 @@ enum {
   MLS_STATUS_BAD_TARGET = 1, /* some target was >= V; that token was treated as ignored */
   MLS_STATUS_TIMEOUT = 2,    /* a pipeline wait exceeded its bound; outputs are invalid */
   MLS_STATUS_CHECK = 4,      /* checked build only: an internal invariant failed */
-  MLS_STATUS_DRAIN = 8       /* after a timeout, a kernel's bounded shutdown wait for its own
+  MLS_STATUS_DRAIN = 8,      /* after a timeout, a kernel's bounded shutdown wait for its own
                                 copies or MMAs also ran out: some may still have been in flight
                                 when it exited, so the CUDA context should not be trusted */
+  MLS_STATUS_BAD_SEQ = 16    /* mls_policy_loss: seq_start is not sorted or leaves [0, T]; the
+                                outputs of the tokens concerned mean nothing */
 };
 
 /* Maximum number of sub-models per call. */
@@ -217,6 +219,139 @@ int mls_spec_verify(const mls_spec_problem* p, const void* H_draft, const void* 
                     const void* H_verify, const void* W_verify, const int32_t* draft_tokens,
                     const float* uniforms, int32_t* n_accepted, int32_t* next_token, void* ws,
                     size_t ws_bytes, mls_stream_t stream);
+
+/*
+ * Log-probabilities of given tokens through the heads, with the backward of a
+ * gradient per token (what a loss on log-probabilities needs, where
+ * mls_head_loss_* has its own).  Per sub-model m and token t with target y:
+ *   z = H_m[t] W_m^T,  lse = logsumexp(z / tau),  logp = z_y / tau - lse
+ * Backward, with dlogp = dL/dlogp:
+ *   dL/dz = (dlogp / tau) (e_y - softmax(z / tau)),  dH_m = dL/dz W_m,  dW_m = dL/dz^T H_m
+ * The [T, V] logits are recomputed, never stored; dL/dz is rounded to bf16 before the
+ * last products, as in mls_head_loss_bwd.  teacher, alpha and w of `p` are not used,
+ * in_dtype is MLS_BF16 (MLS_ERR_UNSUPPORTED otherwise: products of fp32 storage would
+ * go through tf32, whose errors a ratio exp(logp - old_logp) turns into gradients).
+ *   targets    device, int32 [T]; outside [0, V): logp 0, no gradient (>= V also
+ *              raises MLS_STATUS_BAD_TARGET), and its dlogp is not used
+ *   logp, lse  device, fp32 [M, T]; the backward needs lse
+ *   dlogp      device, fp32 [M, T]
+ *   dH[m], dW[m]  device, bf16 [T, d_m] and [V, d_m], 16-byte aligned, overwritten (dW zeros
+ *              when T = 0); sums are fp32, rounded once
+ *   ws         device workspace of mls_logp_workspace_size(p) bytes
+ */
+size_t mls_logp_workspace_size(const mls_problem* p);
+int mls_head_logp_fwd(const mls_problem* p, const void* const* H, const void* const* W,
+                      const int32_t* targets, float* logp, float* lse, void* ws, size_t ws_bytes,
+                      mls_stream_t stream);
+int mls_head_logp_bwd(const mls_problem* p, const void* const* H, const void* const* W,
+                      const int32_t* targets, const float* lse, const float* dlogp,
+                      void* const* dH, void* const* dW, void* ws, size_t ws_bytes,
+                      mls_stream_t stream);
+
+/*
+ * Layer norm of T rows of d values, the norm in front of a head:
+ *   mu = mean x,  r = 1 / sqrt(mean (x - mu)^2 + eps),  xh = (x - mu) r,  y = xh gain + bias
+ *   x, y        device [T, d] in_dtype (MLS_BF16 or MLS_FP32), row-major, 16-byte aligned,
+ *               rows a multiple of 16 bytes; y may be the buffer x
+ *   gain, bias  device [d] in_dtype, 16-byte aligned; NULL: 1 and 0
+ *   mean, rstd  device, fp32 [T]: mu and r, which the backward needs; or NULL (both)
+ * Backward, with dy = dL/dy and h = dy gain:
+ *   dx = r (h - mean h - xh mean(h xh))    device [T, d] in_dtype; may be the buffer dy
+ *   dgain = sum over rows of dy xh, dbias = sum over rows of dy
+ *                                          device, fp32 [d], overwritten (zeros when T = 0);
+ *                                          each may be NULL
+ *   ws          device workspace of mls_layer_norm_workspace_size(T, d) bytes, 256-byte
+ *               aligned; not used, and may be NULL, when dgain and dbias are NULL
+ * Sums are fp32.  Outputs overlap inputs only where said.  Asynchronous on `stream`;
+ * returns 0 or a negative MLS_ERR_* code (nothing launched).  T = 0 reads no row.
+ */
+int mls_layer_norm_fwd(int64_t T, int32_t d, int32_t in_dtype, float eps, const void* x,
+                       const void* gain, const void* bias, void* y, float* mean, float* rstd,
+                       mls_stream_t stream);
+size_t mls_layer_norm_workspace_size(int64_t T, int32_t d);
+int mls_layer_norm_bwd(int64_t T, int32_t d, int32_t in_dtype, const void* x, const void* gain,
+                       const void* dy, const float* mean, const float* rstd, void* dx,
+                       float* dgain, float* dbias, void* ws, size_t ws_bytes, mls_stream_t stream);
+
+/*
+ * Clipped policy loss with a KL term, and its gradient in the log-probabilities,
+ * for reinforcement fine-tuning of a suite (the paper stops before it).  Per
+ * sub-model m and token t that counts:
+ *   r = exp(logp - old_logp),  A = adv,  x = ref_logp - logp
+ *   P = -min(r A, clamp(r, 1 - clip_low, 1 + clip_high) A)    (0 when A = 0)
+ *   K = exp(x) - x - 1
+ *   L = P + beta K,   dL/dlogp = (0 where the clamp decides the minimum, else -r A)
+ *                                - beta (exp(x) - 1)
+ *   loss = sum_m w_m sum_t weight_t L_m[t]
+ *   weight_t: MLS_AGG_TOKEN_MEAN 1 / N, N the tokens that count (loss 0 when none does);
+ *             MLS_AGG_SEQ_MEAN 1 / (B n_b), n_b those of t's sequence (a sequence with
+ *             none adds 0 and stays in the mean); MLS_AGG_SUM 1
+ * A token counts when its target lies in [0, V) and it belongs to a sequence.
+ * Nothing but the target and the sequence of one that does not is read, so the
+ * other inputs may hold anything there.
+ *   logp, old_logp  device, fp32 [M, T]
+ *   ref_logp        device, fp32 [M, T]; NULL only when beta = 0 (with beta = 0 it only
+ *                   serves the reported K)
+ *   adv             device, fp32 [B] if adv_per_seq, else [T]
+ *   targets         device, int32 [T]
+ *   seq_start       device, int32 [B + 1], sorted, within [0, T]: sequence b is the tokens
+ *                   [seq_start[b], seq_start[b + 1]), which may be none; NULL: all tokens
+ *                   belong (MLS_AGG_SEQ_MEAN and adv_per_seq need sequences).  An array that
+ *                   is not sorted or leaves [0, T] raises MLS_STATUS_BAD_SEQ.
+ *   loss            device, fp32 [1]
+ *   tok_loss        device, fp32 [M, T] or NULL: L (0 for a token that does not count)
+ *   diag            device, fp32 [3, M] or NULL: sums of weight_t P, weight_t K, and
+ *                   weight_t over the tokens whose ratio the clamp stopped
+ *   dlogp           device, fp32 [M, T] or NULL: grad_scale dloss/dlogp, every entry
+ *                   written (0 for a token that does not count).  May be the buffer logp.
+ *   ws              device workspace of mls_policy_workspace_size(p) bytes, 256-byte aligned
+ * A ratio is compared with its bound as if in 64 bits (the fp32 inputs taken as
+ * exact, the bounds 1 - clip_low and 1 + clip_high as their fp32 parameters say);
+ * one exactly on a bound is not stopped.
+ * Asynchronous; returns 0 or a negative MLS_ERR_* code (nothing launched).
+ */
+enum { MLS_AGG_TOKEN_MEAN = 0, MLS_AGG_SEQ_MEAN = 1, MLS_AGG_SUM = 2 };
+typedef struct {
+  int32_t M;            /* sub-models, 1..MLS_MAX_MODELS */
+  int64_t T;            /* tokens, 0 .. 2^31 - 1 */
+  int64_t V;            /* vocabulary, 1 .. 2^31 - 1 */
+  int32_t B;            /* sequences, >= 0; >= 1 for MLS_AGG_SEQ_MEAN or adv_per_seq when T > 0 */
+  float clip_low;       /* >= 0; from 1 on the ratio has no lower bound */
+  float clip_high;      /* >= 0; infinite: no upper bound */
+  float beta;           /* weight of the KL term, >= 0 */
+  int32_t agg;          /* MLS_AGG_* */
+  int32_t adv_per_seq;  /* non-zero: one advantage per sequence */
+  const float* w;       /* host array [M] of loss weights, or NULL for all 1 */
+} mls_policy_problem;
+
+size_t mls_policy_workspace_size(const mls_policy_problem* p);
+int mls_policy_loss(const mls_policy_problem* p, const float* logp, const float* old_logp,
+                    const float* ref_logp, const float* adv, const int32_t* targets,
+                    const int32_t* seq_start, float grad_scale, float* loss, float* tok_loss,
+                    float* diag, float* dlogp, void* ws, size_t ws_bytes, mls_stream_t stream);
+
+/*
+ * Global norm of the gradients of n tensors, and clipping in place:
+ *   norm = sqrt(sum of all squares),  c = min(1, max_norm / (norm + 1e-6)),  g *= c
+ *   g      host array [n] of device pointers, aligned to their element; each tensor dense.
+ *          The tensors do not overlap (MLS_ERR_ARG).
+ *   numel  host array [n]: values of each tensor, >= 0 (a tensor of none may be NULL)
+ *   dtype  host array [n]: MLS_BF16 or MLS_FP32
+ *   max_norm  > 0; infinite: only the norm is computed
+ *   stats  device, fp32 [2]: norm and c
+ *   ws     device workspace of mls_grad_clip_workspace_size(n) bytes, 256-byte aligned
+ * The sum is taken in 64 bits (fp32 over 32 values at a time where that loses
+ * nothing): no square overflows or vanishes, and c and g are right even where norm
+ * itself is past the largest fp32 value and reads as infinite.  A NaN among the gradients makes norm,
+ * c and so every gradient NaN; an infinity among them makes norm infinite, c 0, and itself NaN.
+ * The arrays g, numel and dtype are read during the call only.  At most
+ * MLS_CLIP_MAX_TENSORS tensors (MLS_ERR_UNSUPPORTED).
+ * Asynchronous; returns 0 or a negative MLS_ERR_* code (nothing launched).
+ */
+#define MLS_CLIP_MAX_TENSORS 16384
+size_t mls_grad_clip_workspace_size(int32_t n);
+int mls_grad_clip(int32_t n, void* const* g, const int64_t* numel, const int32_t* dtype,
+                  float max_norm, float* stats, void* ws, size_t ws_bytes, mls_stream_t stream);
 
 /*
  * Synchronises `stream`, then returns the status bits (MLS_STATUS_*) recorded by

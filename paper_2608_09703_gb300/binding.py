@@ -24,6 +24,9 @@ MLS_OK = 0
 MLS_ERR_ARG, MLS_ERR_ALIGN, MLS_ERR_UNSUPPORTED = -1, -2, -3
 MLS_ERR_WORKSPACE, MLS_ERR_CUDA, MLS_ERR_DEVICE = -4, -5, -6
 MLS_STATUS_BAD_TARGET, MLS_STATUS_TIMEOUT, MLS_STATUS_CHECK, MLS_STATUS_DRAIN = 1, 2, 4, 8
+MLS_STATUS_BAD_SEQ = 16
+MLS_AGG_TOKEN_MEAN, MLS_AGG_SEQ_MEAN, MLS_AGG_SUM = 0, 1, 2
+MLS_CLIP_MAX_TENSORS = 16384
 MLS_MAX_MODELS = 4
 
 
@@ -59,6 +62,21 @@ class mls_spec_problem(ctypes.Structure):
         ("top_p", ctypes.c_float),
         ("greedy", ctypes.c_int32),
         ("in_dtype", ctypes.c_int32),
+    ]
+
+
+class mls_policy_problem(ctypes.Structure):
+    _fields_ = [
+        ("M", ctypes.c_int32),
+        ("T", ctypes.c_int64),
+        ("V", ctypes.c_int64),
+        ("B", ctypes.c_int32),
+        ("clip_low", ctypes.c_float),
+        ("clip_high", ctypes.c_float),
+        ("beta", ctypes.c_float),
+        ("agg", ctypes.c_int32),
+        ("adv_per_seq", ctypes.c_int32),
+        ("w", ctypes.POINTER(ctypes.c_float)),
     ]
 
 
@@ -107,6 +125,28 @@ def lib():
         L.mls_spec_workspace_size.restype = ctypes.c_size_t
         L.mls_spec_verify.argtypes = [SP, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
         L.mls_spec_verify.restype = ctypes.c_int
+        f32, sz = ctypes.c_float, ctypes.c_size_t
+        L.mls_logp_workspace_size.argtypes = [P]
+        L.mls_logp_workspace_size.restype = sz
+        L.mls_head_logp_fwd.argtypes = [P, vpp, vpp, vp, vp, vp, vp, sz, vp]
+        L.mls_head_logp_fwd.restype = ctypes.c_int
+        L.mls_head_logp_bwd.argtypes = [P, vpp, vpp, vp, vp, vp, vpp, vpp, vp, sz, vp]
+        L.mls_head_logp_bwd.restype = ctypes.c_int
+        L.mls_layer_norm_fwd.argtypes = [i64, i32, i32, f32, vp, vp, vp, vp, vp, vp, vp]
+        L.mls_layer_norm_fwd.restype = ctypes.c_int
+        L.mls_layer_norm_workspace_size.argtypes = [i64, i32]
+        L.mls_layer_norm_workspace_size.restype = sz
+        L.mls_layer_norm_bwd.argtypes = [i64, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.mls_layer_norm_bwd.restype = ctypes.c_int
+        PP = ctypes.POINTER(mls_policy_problem)
+        L.mls_policy_workspace_size.argtypes = [PP]
+        L.mls_policy_workspace_size.restype = sz
+        L.mls_policy_loss.argtypes = [PP, vp, vp, vp, vp, vp, vp, f32, vp, vp, vp, vp, vp, sz, vp]
+        L.mls_policy_loss.restype = ctypes.c_int
+        L.mls_grad_clip_workspace_size.argtypes = [i32]
+        L.mls_grad_clip_workspace_size.restype = sz
+        L.mls_grad_clip.argtypes = [i32, vp, vp, vp, f32, vp, vp, sz, vp]
+        L.mls_grad_clip.restype = ctypes.c_int
         L.mls_profile_enable.argtypes = [ctypes.c_int]
         L.mls_profile_enable.restype = ctypes.c_int
         L.mls_profile_read.argtypes = [ctypes.POINTER(mls_kernel_time), ctypes.c_int]
@@ -244,6 +284,195 @@ def mls_spec_verify(p: mls_spec_problem, H_draft, W_draft, H_verify, W_verify, d
     _check(rc, "mls_spec_verify")
 
 
+# The operators below check what a data pointer alone cannot say.
+def _expect(name: str, t: Optional[torch.Tensor], dtype, shape, like: int = -2) -> int:
+    """Raises unless t is a dense CUDA tensor of this type and shape on the current
+    device (and on device `like`, if given); returns its device."""
+    if t.dtype is not dtype:
+        raise TypeError(f"{name}: {t.dtype}, expected {dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: not contiguous")
+    dev = t.get_device()
+    if dev != like:
+        if like != -2:
+            raise ValueError(f"{name}: on device {t.device}, not with the other tensors")
+        if dev < 0:
+            raise ValueError(f"{name}: on {t.device}, expected a CUDA device")
+        if dev != (_get_device() if _get_device is not None else torch.cuda.current_device()):
+            raise ValueError(f"{name}: on {t.device}, which is not the current device")
+    return dev
+
+
+def _ws_args(ws: Optional[torch.Tensor], like: int):
+    if ws is None:
+        return None, 0
+    if not ws.is_contiguous() or ws.get_device() != like:
+        raise ValueError("ws: not contiguous or on another device")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def _expect_heads(prob: "Problem", H, W, targets) -> int:
+    c = prob.c
+    if len(H) != c.M or len(W) != c.M:
+        raise ValueError(f"{len(H)} hidden states and {len(W)} heads for {c.M} sub-models")
+    dev = _expect("targets", targets, torch.int32, (c.T,))
+    dt = torch.bfloat16 if c.in_dtype == MLS_BF16 else torch.float32
+    for m in range(c.M):
+        _expect(f"H[{m}]", H[m], dt, (c.T, c.d[m]), dev)
+        _expect(f"W[{m}]", W[m], dt, (c.V, c.d[m]), dev)
+    return dev
+
+
+def mls_logp_workspace_size(prob: "Problem") -> int:
+    return int(lib().mls_logp_workspace_size(prob.ref()))
+
+
+def mls_head_logp_fwd(prob: "Problem", H, W, targets, logp, lse, ws, stream=None) -> None:
+    """Log-probabilities of the targets through every head (see include/mls.h)."""
+    dev = _expect_heads(prob, H, W, targets)
+    rows = (prob.c.M, prob.c.T)
+    _expect("logp", logp, torch.float32, rows, dev)
+    _expect("lse", lse, torch.float32, rows, dev)
+    wsp, wsn = _ws_args(ws, dev)
+    rc = lib().mls_head_logp_fwd(prob.ref(), _ptrs(H), _ptrs(W), _ptr(targets), _ptr(logp), _ptr(lse),
+                                 wsp, wsn, _stream(stream))
+    _check(rc, "mls_head_logp_fwd")
+
+
+def mls_head_logp_bwd(prob: "Problem", H, W, targets, lse, dlogp, dH, dW, ws, stream=None) -> None:
+    dev = _expect_heads(prob, H, W, targets)
+    c = prob.c
+    _expect("lse", lse, torch.float32, (c.M, c.T), dev)
+    _expect("dlogp", dlogp, torch.float32, (c.M, c.T), dev)
+    if len(dH) != c.M or len(dW) != c.M:
+        raise ValueError(f"{len(dH)} and {len(dW)} gradients for {c.M} sub-models")
+    for m in range(c.M):
+        _expect(f"dH[{m}]", dH[m], H[m].dtype, (c.T, c.d[m]), dev)
+        _expect(f"dW[{m}]", dW[m], H[m].dtype, (c.V, c.d[m]), dev)
+    wsp, wsn = _ws_args(ws, dev)
+    rc = lib().mls_head_logp_bwd(prob.ref(), _ptrs(H), _ptrs(W), _ptr(targets), _ptr(lse), _ptr(dlogp),
+                                 _ptrs(dH), _ptrs(dW), wsp, wsn, _stream(stream))
+    _check(rc, "mls_head_logp_bwd")
+
+
+def mls_layer_norm_fwd(x, gain, bias, eps: float, y, mean=None, rstd=None, stream=None) -> None:
+    """y = (x - mean) rstd gain + bias per row of x [T, d] (see include/mls.h)."""
+    T, d = x.shape
+    code = _dtype_code(x)
+    dev = _expect("x", x, x.dtype, (T, d))
+    _expect("y", y, x.dtype, (T, d), dev)
+    for name, t in (("gain", gain), ("bias", bias)):
+        if t is not None:
+            _expect(name, t, x.dtype, (d,), dev)
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        if t is not None:
+            _expect(name, t, torch.float32, (T,), dev)
+    rc = lib().mls_layer_norm_fwd(T, d, code, float(eps), _ptr(x), _ptr(gain), _ptr(bias), _ptr(y),
+                                  _ptr(mean), _ptr(rstd), _stream(stream))
+    _check(rc, "mls_layer_norm_fwd")
+
+
+def mls_layer_norm_workspace_size(T: int, d: int) -> int:
+    return int(lib().mls_layer_norm_workspace_size(int(T), int(d)))
+
+
+def mls_layer_norm_bwd(x, gain, dy, mean, rstd, dx, dgain, dbias, ws, stream=None) -> None:
+    T, d = x.shape
+    code = _dtype_code(x)
+    dev = _expect("x", x, x.dtype, (T, d))
+    _expect("dy", dy, x.dtype, (T, d), dev)
+    _expect("dx", dx, x.dtype, (T, d), dev)
+    _expect("mean", mean, torch.float32, (T,), dev)
+    _expect("rstd", rstd, torch.float32, (T,), dev)
+    if gain is not None:
+        _expect("gain", gain, x.dtype, (d,), dev)
+    for name, t in (("dgain", dgain), ("dbias", dbias)):
+        if t is not None:
+            _expect(name, t, torch.float32, (d,), dev)
+    wsp, wsn = _ws_args(ws, dev)
+    rc = lib().mls_layer_norm_bwd(T, d, code, _ptr(x), _ptr(gain), _ptr(dy), _ptr(mean), _ptr(rstd),
+                                  _ptr(dx), _ptr(dgain), _ptr(dbias), wsp, wsn, _stream(stream))
+    _check(rc, "mls_layer_norm_bwd")
+
+
+_AGG = {"token": MLS_AGG_TOKEN_MEAN, "seq": MLS_AGG_SEQ_MEAN, "sum": MLS_AGG_SUM}
+
+
+class PolicyProblem:
+    """Owns an mls_policy_problem and the host array it points to.  agg: "token",
+    "seq" or "sum"."""
+
+    def __init__(self, T: int, V: int, M: int = 1, B: int = 0, clip_low: float = 0.2,
+                 clip_high: float = 0.2, beta: float = 0.0, agg: str = "token",
+                 adv_per_seq: bool = False, w: Optional[Sequence[float]] = None):
+        if w is not None and len(w) != M:
+            raise ValueError(f"w: {len(w)} weights for {M} sub-models")
+        self.w = None if w is None else (ctypes.c_float * M)(*[float(x) for x in w])
+        self.c = mls_policy_problem(int(M), int(T), int(V), int(B), float(clip_low), float(clip_high),
+                                    float(beta), _AGG[agg], int(bool(adv_per_seq)), self.w)
+
+    def ref(self):
+        return ctypes.byref(self.c)
+
+
+def mls_policy_workspace_size(prob: PolicyProblem) -> int:
+    return int(lib().mls_policy_workspace_size(prob.ref()))
+
+
+def mls_policy_loss(prob: PolicyProblem, logp, old_logp, ref_logp, adv, targets, seq_start,
+                    grad_scale: float, loss, tok_loss, diag, dlogp, ws, stream=None) -> None:
+    """Clipped policy loss with a KL term and its gradient (see include/mls.h)."""
+    c = prob.c
+    f32, i32, rows = torch.float32, torch.int32, (c.M, c.T)
+    dev = _expect("logp", logp, f32, rows)
+    _expect("old_logp", old_logp, f32, rows, dev)
+    _expect("adv", adv, f32, (c.B if c.adv_per_seq else c.T,), dev)
+    _expect("targets", targets, i32, (c.T,), dev)
+    _expect("loss", loss, f32, (1,), dev)
+    if seq_start is not None:
+        _expect("seq_start", seq_start, i32, (c.B + 1,), dev)
+    for name, t, shape in (("ref_logp", ref_logp, rows), ("tok_loss", tok_loss, rows),
+                           ("diag", diag, (3, c.M)), ("dlogp", dlogp, rows)):
+        if t is not None:
+            _expect(name, t, f32, shape, dev)
+    wsp, wsn = _ws_args(ws, dev)
+    rc = lib().mls_policy_loss(prob.ref(), _ptr(logp), _ptr(old_logp), _ptr(ref_logp), _ptr(adv),
+                               _ptr(targets), _ptr(seq_start), float(grad_scale), _ptr(loss),
+                               _ptr(tok_loss), _ptr(diag), _ptr(dlogp), wsp, wsn, _stream(stream))
+    _check(rc, "mls_policy_loss")
+
+
+class _ClipTable:
+    """The host arrays that describe a list of tensors to mls_grad_clip."""
+
+    def __init__(self, grads: Sequence[torch.Tensor]):
+        self.n, self.device = len(grads), None
+        for i, g in enumerate(grads):
+            dev = _expect(f"grads[{i}]", g, g.dtype, g.shape, -2 if self.device is None else self.device)
+            self.device = dev
+        self.g = (ctypes.c_void_p * self.n)(*[g.data_ptr() for g in grads])
+        self.numel = (ctypes.c_int64 * self.n)(*[g.numel() for g in grads])
+        self.dtype = (ctypes.c_int32 * self.n)(*[_dtype_code(g) for g in grads])
+
+
+def mls_grad_clip_workspace_size(n: int) -> int:
+    return int(lib().mls_grad_clip_workspace_size(int(n)))
+
+
+def mls_grad_clip(grads, max_norm: float, stats, ws, stream=None) -> None:
+    """Global norm of a list of tensors, and clipping in place (see include/mls.h)."""
+    t = grads if isinstance(grads, _ClipTable) else _ClipTable(grads)
+    dev = _expect("stats", stats, torch.float32, (2,))
+    if t.device is not None and t.device != dev:
+        raise ValueError("stats: not with the gradients")
+    wsp, wsn = _ws_args(ws, dev)
+    rc = lib().mls_grad_clip(t.n, t.g, t.numel, t.dtype, float(max_norm), _ptr(stats), wsp, wsn,
+                             _stream(stream))
+    _check(rc, "mls_grad_clip")
+
+
 def mls_head_loss_fwd_noalloc(prob: Problem, H, W, targets, loss, tok_loss, tok_diag, argmax,
                               stats, stream=None) -> None:
     """Forward with the library's built-in scratch instead of a workspace, for
@@ -354,3 +583,111 @@ class SpecVerify:
         mls_spec_verify(self.p, H_draft, W_draft, H_verify, W_verify, draft_tokens, uniforms,
                         self.n_accepted, self.next_token, self.ws, stream)
         return self.n_accepted, self.next_token
+
+
+class HeadLogp:
+    """Log-probabilities of given tokens through a suite's heads, and the backward
+    of a gradient per token, with outputs and workspace allocated once.  H[m]:
+    [T, d_m], W[m]: [V, d_m] bf16; targets int32 [T]; dlogp fp32 [M, T]; dH and dW
+    bf16."""
+
+    def __init__(self, d, T, V, tau=1.0, device="cuda", vocab_group=0):
+        self.prob = Problem(d, T, V, tau=tau, vocab_group=vocab_group)
+        M, dev = len(d), torch.device(device)
+        self.logp = torch.empty(M, T, dtype=torch.float32, device=dev)
+        self.lse = torch.empty(M, T, dtype=torch.float32, device=dev)
+        self.dH = [torch.empty(T, dm, dtype=torch.bfloat16, device=dev) for dm in d]
+        self.dW = [torch.empty(V, dm, dtype=torch.bfloat16, device=dev) for dm in d]
+        self.ws = torch.empty(max(mls_logp_workspace_size(self.prob), 1), dtype=torch.uint8, device=dev)
+
+    def forward(self, H, W, targets, stream=None):
+        mls_head_logp_fwd(self.prob, H, W, targets, self.logp, self.lse, self.ws, stream)
+        return self.logp
+
+    def backward(self, H, W, targets, dlogp, stream=None):
+        """Gradients for the tokens of the last forward; returns (dH, dW)."""
+        mls_head_logp_bwd(self.prob, H, W, targets, self.lse, dlogp, self.dH, self.dW, self.ws, stream)
+        return self.dH, self.dW
+
+
+class LayerNorm:
+    """Layer norm of x [T, d] (bf16 or fp32) with its outputs and workspace
+    allocated once: y, the row statistics mean and rstd, and, with `backward`, dx
+    and the fp32 gradients dgain (if gain) and dbias (if bias)."""
+
+    def __init__(self, T, d, eps=1e-5, gain=True, bias=True, dtype=torch.bfloat16, device="cuda",
+                 backward=True):
+        self.eps, self.gain, self.bias = eps, gain, bias
+        dev = torch.device(device)
+        self.y = torch.empty(T, d, dtype=dtype, device=dev)
+        self.mean = self.rstd = self.dx = self.dgain = self.dbias = self.ws = None
+        if backward:
+            self.mean = torch.empty(T, dtype=torch.float32, device=dev)
+            self.rstd = torch.empty(T, dtype=torch.float32, device=dev)
+            self.dx = torch.empty(T, d, dtype=dtype, device=dev)
+            self.dgain = torch.empty(d, dtype=torch.float32, device=dev) if gain else None
+            self.dbias = torch.empty(d, dtype=torch.float32, device=dev) if bias else None
+            if gain or bias:
+                self.ws = torch.empty(max(mls_layer_norm_workspace_size(T, d), 1), dtype=torch.uint8,
+                                      device=dev)
+
+    def _gain(self, name, t, has):
+        if (t is not None) != has:
+            raise ValueError(f"{name}: " + ("missing" if has else "given to a norm made without one"))
+
+    def forward(self, x, gain=None, bias=None, stream=None):
+        self._gain("gain", gain, self.gain)
+        self._gain("bias", bias, self.bias)
+        mls_layer_norm_fwd(x, gain, bias, self.eps, self.y, self.mean, self.rstd, stream)
+        return self.y
+
+    def backward(self, x, dy, gain=None, stream=None):
+        """Gradients for the rows of the last forward; returns (dx, dgain, dbias)."""
+        self._gain("gain", gain, self.gain)
+        if self.dx is None:
+            raise ValueError("made with backward=False")
+        mls_layer_norm_bwd(x, gain, dy, self.mean, self.rstd, self.dx, self.dgain, self.dbias, self.ws,
+                           stream)
+        return self.dx, self.dgain, self.dbias
+
+
+class PolicyLoss:
+    """Clipped policy loss with a KL term over [M, T] log-probabilities, and its
+    gradient dlogp, in one call; outputs and workspace allocated once.  adv: [B]
+    with adv_per_seq, else [T]; targets int32 [T] (outside [0, V): left out);
+    seq_start int32 [B + 1] when B > 0."""
+
+    def __init__(self, T, V, M=1, B=0, clip_low=0.2, clip_high=0.2, beta=0.0, agg="token",
+                 adv_per_seq=False, w=None, device="cuda"):
+        self.prob = PolicyProblem(T, V, M, B, clip_low, clip_high, beta, agg, adv_per_seq, w)
+        dev = torch.device(device)
+        self.loss = torch.zeros(1, dtype=torch.float32, device=dev)
+        self.tok_loss = torch.empty(M, T, dtype=torch.float32, device=dev)
+        self.diag = torch.empty(3, M, dtype=torch.float32, device=dev)
+        self.dlogp = torch.empty(M, T, dtype=torch.float32, device=dev)
+        self.ws = torch.empty(max(mls_policy_workspace_size(self.prob), 1), dtype=torch.uint8, device=dev)
+
+    def __call__(self, logp, old_logp, adv, targets, ref_logp=None, seq_start=None, grad_scale=1.0,
+                 stream=None):
+        mls_policy_loss(self.prob, logp, old_logp, ref_logp, adv, targets, seq_start, grad_scale,
+                        self.loss, self.tok_loss, self.diag, self.dlogp, self.ws, stream)
+        return self.loss
+
+
+class GradClip:
+    """Global norm of a fixed list of gradient buffers (bf16 or fp32, as HeadLoss
+    and the others keep them from step to step) and clipping in place.  Returns
+    fp32 [2]: the norm and the factor applied."""
+
+    def __init__(self, grads: Sequence[torch.Tensor]):
+        self.grads = list(grads)  # keeps the buffers alive
+        if not self.grads:
+            raise ValueError("grads: empty")
+        self.table = _ClipTable(self.grads)
+        dev = self.grads[0].device
+        self.stats = torch.empty(2, dtype=torch.float32, device=dev)
+        self.ws = torch.empty(mls_grad_clip_workspace_size(len(self.grads)), dtype=torch.uint8, device=dev)
+
+    def __call__(self, max_norm, stream=None):
+        mls_grad_clip(self.table, max_norm, self.stats, self.ws, stream)
+        return self.stats

@@ -3,6 +3,7 @@
 // forward and backward passes.  Nothing here allocates device memory.
 #include <cudaTypedefs.h>
 
+#include <algorithm>
 #include <climits>
 #include <cmath>
 #include <cstdio>
@@ -473,6 +474,7 @@ GroupPlan plan_group(const mls_problem* p, const Plan& pl, long long g, int pair
 }
 
 bool aligned16(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 15u) == 0; }
+bool aligned4(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 3u) == 0; }
 
 // 2-D row-major tensor [rows, cols] of `elt`-byte elements (128-byte swizzle
 // unless told otherwise).
@@ -587,6 +589,104 @@ int timed(const char* name, cudaStream_t s, F&& launch) {
   return rc;
 }
 
+// The vocabulary groups of a backward pass: `launch_grad(group)` launches the head
+// kernel that leaves dL/dz of the group's columns in G (`hp` is completed for it
+// here), then one GEMM launch forms that group's dW and adds its share of dH, both
+// fp32.
+template <class F>
+int backward_groups(const mls_problem* p, const Plan& pl, const DeviceState& dev, const void* const* H,
+                    const void* const* W, HeadParams& hp, void* G, float* const* dH, float* const* dW,
+                    float* split_ws, cudaStream_t s, F&& launch_grad) {
+  int rc;
+  const bool tf32 = pl.elt == 4;
+  const int KE = 128 / pl.elt;
+  // dW reads A = G viewed M-major and B = H viewed N-major, dH reads A = G
+  // K-major and B = W viewed N-major, all in place.
+  GemmParams gw, gh, gb;
+  std::memset(&gw, 0, sizeof gw);
+  std::memset(&gh, 0, sizeof gh);
+  const CUtensorMapSwizzle mn_swizzle =
+      tf32 ? CU_TENSOR_MAP_SWIZZLE_128B_ATOM_32B : CU_TENSOR_MAP_SWIZZLE_128B;
+  for (int m = 0; m < p->M; ++m) {
+    const void* Gm = static_cast<const char*>(G) + static_cast<size_t>(pl.elt) * p->T * pl.group * m;
+    // the backward head kernel's TMA stores of dL/dz
+    if (encode(&hp.mapG[m], Gm, pl.elt, pl.group, p->T, pl.group, KE / 2, 32, CU_TENSOR_MAP_SWIZZLE_64B))
+      return MLS_ERR_CUDA;
+    if (encode(&gh.mapA[m], Gm, pl.elt, pl.group, p->T, pl.group, KE, kGemmBM) ||
+        encode(&gw.mapA[m], Gm, pl.elt, pl.group, p->T, pl.group, KE, KE, mn_swizzle) ||
+        encode(&gw.mapB[m], H[m], pl.elt, p->d[m], p->T, p->d[m], KE, KE, mn_swizzle) ||
+        encode(&gh.mapB[m], W[m], pl.elt, p->d[m], p->V, p->d[m], KE, KE, mn_swizzle))
+      return MLS_ERR_CUDA;
+  }
+
+  for (long long g = 0; g < pl.ngroups; ++g) {
+    const GroupPlan gp = plan_group(p, pl, g, dev.head_pairs, dev.gemm_pairs);
+    const long long c0 = gp.c0, gc = gp.cols;
+    hp.split = gp.split;
+    hp.g_col0 = c0;
+    if ((rc = launch_grad(g))) return rc;
+    // dW and dH of every sub-model in one persistent launch, the class with the
+    // longer reduction (dH: the group's columns, dW: T) first.
+    const int pairs = dev.gemm_pairs, M = p->M;
+    const GemmCut& cut = gp.cut;
+    SplitSumParams sum;
+    std::memset(&sum, 0, sizeof sum);
+    std::memset(&gb, 0, sizeof gb);
+    int units = 0, n_long = 0;
+    long long split_off = 0;
+    for (int i = 0; i < 2 * M; ++i) {
+      const int m = i % M;
+      const bool is_long = i < M, dh = is_long == cut.dh_long;
+      gb.mapA[i] = dh ? gh.mapA[m] : gw.mapA[m];
+      gb.mapB[i] = dh ? gh.mapB[m] : gw.mapB[m];
+      GemmProblem& q = gb.prob[i];
+      q.Mrows = static_cast<int>(dh ? p->T : gc);
+      q.Ncols = p->d[m];
+      q.K = static_cast<int>(dh ? gc : p->T);
+      q.a_map = q.b_map = i;
+      q.b_k0 = dh ? static_cast<int>(c0) : 0;
+      float* out = dh ? dH[m] : dW[m] + c0 * p->d[m];
+      q.accumulate = dh && g > 0 ? 1 : 0;
+      q.a_mn = dh ? 0 : 1;
+      q.tiles_m = static_cast<int>(ceil_div(q.Mrows, 2 * kGemmBM));
+      q.tiles_n = static_cast<int>(ceil_div(p->d[m], kGemmBN));
+      q.wide = cut.wide && dh ? 1 : 0;
+      q.tile_begin = units;
+      units += q.tiles_m * (q.wide ? (q.tiles_n + 1) / 2 : q.tiles_n) * (is_long ? cut.ksplit : 1);
+      if (is_long && cut.ksplit > 1) {  // the units write their own sums, added up below
+        q.ksplit = cut.ksplit;
+        q.kb_split = cut.kb_split;
+        sum.out[m] = out;
+        sum.n4[m] = static_cast<long long>(q.Mrows) * p->d[m] / 4;
+        sum.accumulate = q.accumulate;
+        out = split_ws + split_off;
+        q.accumulate = 0;
+        sum.part[m] = out;
+        split_off += static_cast<long long>(q.Mrows) * p->d[m];
+      }
+      if (encode_out(&gb.mapC[i], out, p->d[m], q.Mrows, q.ksplit > 1 ? q.ksplit : 1,
+                     q.ksplit > 1 ? cut.part_floats / cut.ksplit : static_cast<long long>(q.Mrows) * p->d[m]))
+        return MLS_ERR_CUDA;
+      if (i == M - 1) n_long = units;
+    }
+    gb.nprob = 2 * M;
+    gb.total_tiles = units;
+    gb.status = dev.status;
+    gb.chained = cut.chained ? 1 : 0;
+    // persistent: one CTA pair per resident pair slot, never more pairs than units
+    const int grid = 2 * (units < pairs ? units : pairs);
+    schedule_two_class(gb, grid / 2, n_long, cut.cost_long, units - n_long, cut.cost_short);
+    if ((rc = timed("gemm_bwd", s, [&] { return launch_gemm_mixed(gb, tf32, grid, s); }))) return rc;
+    if (cut.ksplit > 1) {
+      sum.nprob = M;
+      sum.nsplit = cut.ksplit;
+      sum.stride = cut.part_floats / cut.ksplit;
+      if ((rc = timed("split_sum", s, [&] { return launch_split_sum(sum, s); }))) return rc;
+    }
+  }
+  return MLS_OK;
+}
+
 }  // namespace
 }  // namespace mls
 
@@ -698,7 +798,6 @@ extern "C" int mls_head_loss_bwd(const mls_problem* p, const void* const* H, con
   if ((rc = check_ws(pl, ws, ws_bytes, pl.total))) return rc;
   char* wsb = static_cast<char*>(ws);
   const bool tf32 = pl.elt == 4;
-  const int KE = 128 / pl.elt;
   float* inv_n = reinterpret_cast<float*>(wsb + pl.off_invn);
   void* G = wsb + pl.off_G;
 
@@ -714,92 +813,142 @@ extern "C" int mls_head_loss_bwd(const mls_problem* p, const void* const* H, con
   hp.one_minus_alpha = 1.0f - p->alpha;
   hp.alpha_over_tau = p->alpha / p->tau;
 
-  // dW reads A = G viewed M-major and B = H viewed N-major, dH reads A = G
-  // K-major and B = W viewed N-major, all in place.
-  GemmParams gw, gh, gb;
-  std::memset(&gw, 0, sizeof gw);
-  std::memset(&gh, 0, sizeof gh);
-  const CUtensorMapSwizzle mn_swizzle =
-      tf32 ? CU_TENSOR_MAP_SWIZZLE_128B_ATOM_32B : CU_TENSOR_MAP_SWIZZLE_128B;
-  for (int m = 0; m < p->M; ++m) {
-    const void* Gm = static_cast<const char*>(G) + static_cast<size_t>(pl.elt) * p->T * pl.group * m;
-    // the backward head kernel's TMA stores of dL/dz
-    if (encode(&hp.mapG[m], Gm, pl.elt, pl.group, p->T, pl.group, KE / 2, 32, CU_TENSOR_MAP_SWIZZLE_64B))
-      return MLS_ERR_CUDA;
-    if (encode(&gh.mapA[m], Gm, pl.elt, pl.group, p->T, pl.group, KE, kGemmBM) ||
-        encode(&gw.mapA[m], Gm, pl.elt, pl.group, p->T, pl.group, KE, KE, mn_swizzle) ||
-        encode(&gw.mapB[m], H[m], pl.elt, p->d[m], p->T, p->d[m], KE, KE, mn_swizzle) ||
-        encode(&gh.mapB[m], W[m], pl.elt, p->d[m], p->V, p->d[m], KE, KE, mn_swizzle))
-      return MLS_ERR_CUDA;
-  }
+  return backward_groups(
+      p, pl, *dev, H, W, hp, G, dH, dW, reinterpret_cast<float*>(wsb + pl.off_split), s,
+      [&](long long) { return timed("head_bwd", s, [&] { return launch_head_bwd(hp, tf32, p->tau == 1.0f, s); }); });
+}
 
-  for (long long g = 0; g < pl.ngroups; ++g) {
-    const GroupPlan gp = plan_group(p, pl, g, dev->head_pairs, dev->gemm_pairs);
-    const long long c0 = gp.c0, gc = gp.cols;
-    hp.split = gp.split;
-    hp.g_col0 = c0;
-    if ((rc = timed("head_bwd", s, [&] { return launch_head_bwd(hp, tf32, p->tau == 1.0f, s); }))) return rc;
-    // dW and dH of every sub-model in one persistent launch, the class with the
-    // longer reduction (dH: the group's columns, dW: T) first.
-    const int pairs = dev->gemm_pairs, M = p->M;
-    const GemmCut& cut = gp.cut;
-    float* split_ws = reinterpret_cast<float*>(wsb + pl.off_split);
-    SplitSumParams sum;
-    std::memset(&sum, 0, sizeof sum);
-    std::memset(&gb, 0, sizeof gb);
-    int units = 0, n_long = 0;
-    long long split_off = 0;
-    for (int i = 0; i < 2 * M; ++i) {
-      const int m = i % M;
-      const bool is_long = i < M, dh = is_long == cut.dh_long;
-      gb.mapA[i] = dh ? gh.mapA[m] : gw.mapA[m];
-      gb.mapB[i] = dh ? gh.mapB[m] : gw.mapB[m];
-      GemmProblem& q = gb.prob[i];
-      q.Mrows = static_cast<int>(dh ? p->T : gc);
-      q.Ncols = p->d[m];
-      q.K = static_cast<int>(dh ? gc : p->T);
-      q.a_map = q.b_map = i;
-      q.b_k0 = dh ? static_cast<int>(c0) : 0;
-      float* out = dh ? dH[m] : dW[m] + c0 * p->d[m];
-      q.accumulate = dh && g > 0 ? 1 : 0;
-      q.a_mn = dh ? 0 : 1;
-      q.tiles_m = static_cast<int>(ceil_div(q.Mrows, 2 * kGemmBM));
-      q.tiles_n = static_cast<int>(ceil_div(p->d[m], kGemmBN));
-      q.wide = cut.wide && dh ? 1 : 0;
-      q.tile_begin = units;
-      units += q.tiles_m * (q.wide ? (q.tiles_n + 1) / 2 : q.tiles_n) * (is_long ? cut.ksplit : 1);
-      if (is_long && cut.ksplit > 1) {  // the units write their own sums, added up below
-        q.ksplit = cut.ksplit;
-        q.kb_split = cut.kb_split;
-        sum.out[m] = out;
-        sum.n4[m] = static_cast<long long>(q.Mrows) * p->d[m] / 4;
-        sum.accumulate = q.accumulate;
-        out = split_ws + split_off;
-        q.accumulate = 0;
-        sum.part[m] = out;
-        split_off += static_cast<long long>(q.Mrows) * p->d[m];
-      }
-      if (encode_out(&gb.mapC[i], out, p->d[m], q.Mrows, q.ksplit > 1 ? q.ksplit : 1,
-                     q.ksplit > 1 ? cut.part_floats / cut.ksplit : static_cast<long long>(q.Mrows) * p->d[m]))
-        return MLS_ERR_CUDA;
-      if (i == M - 1) n_long = units;
-    }
-    gb.nprob = 2 * M;
-    gb.total_tiles = units;
-    gb.status = dev->status;
-    gb.chained = cut.chained ? 1 : 0;
-    // persistent: one CTA pair per resident pair slot, never more pairs than units
-    const int grid = 2 * (units < pairs ? units : pairs);
-    schedule_two_class(gb, grid / 2, n_long, cut.cost_long, units - n_long, cut.cost_short);
-    if ((rc = timed("gemm_bwd", s, [&] { return launch_gemm_mixed(gb, tf32, grid, s); }))) return rc;
-    if (cut.ksplit > 1) {
-      sum.nprob = M;
-      sum.nsplit = cut.ksplit;
-      sum.stride = cut.part_floats / cut.ksplit;
-      if ((rc = timed("split_sum", s, [&] { return launch_split_sum(sum, s); }))) return rc;
-    }
+// ------------------------------------------------------------------ log-probabilities
+namespace {
+// Workspace of the log-probability calls: the forward's partial states, or the backward's
+// dL/dz of a vocabulary group, the splits' copies, and dH and dW in fp32.
+struct LogpPlan {
+  Plan head;
+  size_t off_acc = 0, total = 0;
+};
+LogpPlan logp_plan(const mls_problem* p, int pairs, int gemm_pairs) {
+  LogpPlan lp;
+  lp.head = make_plan(p, pairs, gemm_pairs);
+  size_t sum_d = 0;
+  for (int m = 0; m < p->M; ++m) sum_d += p->d[m];
+  lp.off_acc = align_up(lp.head.bwd_bytes);
+  lp.total = align_up(lp.off_acc + sizeof(float) * sum_d * static_cast<size_t>(p->T + p->V));
+  const size_t fwd = sizeof(float) * static_cast<size_t>(lp.head.nparts) * kLogpFields * p->M * p->T;
+  if (fwd > lp.total) lp.total = align_up(fwd);
+  return lp;
+}
+int logp_validate(const mls_problem* p) {
+  const int rc = validate(p);
+  if (rc) return rc;
+  return p->in_dtype == MLS_BF16 ? MLS_OK : MLS_ERR_UNSUPPORTED;
+}
+}  // namespace
+
+extern "C" size_t mls_logp_workspace_size(const mls_problem* p) {
+  if (logp_validate(p) != MLS_OK) return 0;
+  int head = 0, gemm = 0;
+  current_pairs(head, gemm);
+  return logp_plan(p, head, gemm).total;
+}
+
+extern "C" int mls_head_logp_fwd(const mls_problem* p, const void* const* H, const void* const* W,
+                                 const int32_t* targets, float* logp, float* lse, void* ws,
+                                 size_t ws_bytes, mls_stream_t stream) {
+  int rc = logp_validate(p);
+  if (rc) return rc;
+  if (!H || !W || (p->T > 0 && (!targets || !logp || !lse))) return MLS_ERR_ARG;
+  for (int m = 0; m < p->M; ++m) {
+    if ((p->T > 0 && !H[m]) || !W[m]) return MLS_ERR_ARG;
+    if (!aligned16(H[m]) || !aligned16(W[m])) return MLS_ERR_ALIGN;
   }
-  return MLS_OK;
+  if (!aligned4(targets) || !aligned4(logp) || !aligned4(lse)) return MLS_ERR_ALIGN;
+  DeviceState* dev = nullptr;
+  if ((rc = device_state(&dev))) return rc;
+  if (p->T == 0) return MLS_OK;
+  const LogpPlan lp = logp_plan(p, dev->head_pairs, dev->gemm_pairs);
+  const Plan& pl = lp.head;
+  if ((rc = check_ws(pl, ws, ws_bytes, lp.total))) return rc;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  HeadParams hp;
+  std::memset(&hp, 0, sizeof hp);
+  fill_head_common(hp, p, pl, targets, dev->status);
+  for (int m = 0; m < p->M; ++m) hp.order[m] = m;
+  if ((rc = encode_head_maps(hp, p, pl, H, W))) return rc;
+  hp.split = pl.split;
+  hp.part = static_cast<float*>(ws);
+  if ((rc = timed("logp_fwd", s, [&] { return launch_logp_fwd(hp, s); }))) return rc;
+  LogpMergeParams mp;
+  std::memset(&mp, 0, sizeof mp);
+  mp.part = hp.part;
+  mp.nparts = pl.nparts;
+  mp.M = p->M;
+  mp.T = p->T;
+  mp.V = p->V;
+  mp.Ltau = hp.Ltau;
+  mp.inv_tau = static_cast<float>(1.0 / static_cast<double>(p->tau));
+  mp.y = targets;
+  mp.logp = logp;
+  mp.lse = lse;
+  mp.status = dev->status;
+  return timed("logp_merge", s, [&] { return launch_logp_merge(mp, s); });
+}
+
+extern "C" int mls_head_logp_bwd(const mls_problem* p, const void* const* H, const void* const* W,
+                                 const int32_t* targets, const float* lse, const float* dlogp,
+                                 void* const* dH, void* const* dW, void* ws, size_t ws_bytes,
+                                 mls_stream_t stream) {
+  int rc = logp_validate(p);
+  if (rc) return rc;
+  if (!H || !W || !dH || !dW || (p->T > 0 && (!targets || !lse || !dlogp))) return MLS_ERR_ARG;
+  for (int m = 0; m < p->M; ++m) {
+    if ((p->T > 0 && (!H[m] || !dH[m])) || !W[m] || !dW[m]) return MLS_ERR_ARG;
+    if (!aligned16(H[m]) || !aligned16(W[m]) || !aligned16(dW[m]) || !aligned16(dH[m]))
+      return MLS_ERR_ALIGN;
+  }
+  if (!aligned4(targets) || !aligned4(lse) || !aligned4(dlogp)) return MLS_ERR_ALIGN;
+  DeviceState* dev = nullptr;
+  if ((rc = device_state(&dev))) return rc;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  if (p->T == 0) {
+    for (int m = 0; m < p->M; ++m)
+      if ((rc = launch_ok(cudaMemsetAsync(dW[m], 0, 2 * static_cast<size_t>(p->V) * p->d[m], s)))) return rc;
+    return MLS_OK;
+  }
+  const LogpPlan lp = logp_plan(p, dev->head_pairs, dev->gemm_pairs);
+  const Plan& pl = lp.head;
+  if ((rc = check_ws(pl, ws, ws_bytes, lp.total))) return rc;
+  char* wsb = static_cast<char*>(ws);
+  HeadParams hp;
+  std::memset(&hp, 0, sizeof hp);
+  fill_head_common(hp, p, pl, targets, dev->status);
+  for (int m = 0; m < p->M; ++m) hp.order[m] = m;
+  if ((rc = encode_head_maps(hp, p, pl, H, W))) return rc;
+  hp.stats = lse;
+  hp.dlogp = dlogp;
+  hp.neg_inv_tau = static_cast<float>(-1.0 / static_cast<double>(p->tau));
+  float* acc = reinterpret_cast<float*>(wsb + lp.off_acc);
+  float *aH[kMaxModels], *aW[kMaxModels];
+  SplitSumParams th, tw;
+  std::memset(&th, 0, sizeof th);
+  std::memset(&tw, 0, sizeof tw);
+  th.nprob = tw.nprob = p->M;
+  for (int m = 0; m < p->M; ++m) {
+    th.part[m] = aH[m] = acc;
+    th.out[m] = static_cast<float*>(dH[m]);
+    th.n4[m] = p->T * p->d[m] / 4;
+    acc += p->T * p->d[m];
+    tw.part[m] = aW[m] = acc;
+    tw.out[m] = static_cast<float*>(dW[m]);
+    tw.n4[m] = p->V * p->d[m] / 4;
+    acc += p->V * p->d[m];
+  }
+  rc = backward_groups(p, pl, *dev, H, W, hp, wsb + pl.off_G, aH, aW,
+                       reinterpret_cast<float*>(wsb + pl.off_split), s, [&](long long g) {
+                         return timed("logp_bwd", s, [&] { return launch_logp_bwd(hp, g > 0, s); });
+                       });
+  if (rc) return rc;
+  if ((rc = timed("to_bf16", s, [&] { return launch_to_bf16(th, s); }))) return rc;
+  return timed("to_bf16", s, [&] { return launch_to_bf16(tw, s); });
 }
 
 extern "C" int mls_get_status(mls_stream_t stream) {
@@ -830,11 +979,12 @@ extern "C" const char* mls_strerror(int code) {
     case MLS_STATUS_TIMEOUT: return "a pipeline wait timed out; outputs are invalid";
     case MLS_STATUS_BAD_TARGET | MLS_STATUS_TIMEOUT: return "target >= V and a pipeline timeout";
     case MLS_STATUS_CHECK: return "an internal invariant failed (checked build)";
+    case MLS_STATUS_BAD_SEQ: return "sequence offsets not sorted or outside the tokens";
     case MLS_STATUS_DRAIN:
     case MLS_STATUS_TIMEOUT | MLS_STATUS_DRAIN:
       return "a pipeline timeout, and a shutdown wait ran out: the CUDA context is unreliable";
     default:
-      return code > 0 && code < 16 ? "several status bits are set (MLS_STATUS_* in mls.h)" : "unknown code";
+      return code > 0 && code < 32 ? "several status bits are set (MLS_STATUS_* in mls.h)" : "unknown code";
   }
 }
 
@@ -1083,6 +1233,300 @@ extern "C" int mls_junction_bwd(int64_t T, int32_t d_prev, int32_t d_next, int32
                     dev->sms};
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   return timed("junction_bwd", s, [&] { return launch_junction_bwd(jp, in_dtype == MLS_FP32, s); });
+}
+
+// ------------------------------------------------------------------ layer norm
+namespace {
+int norm_check(long long T, int d, int dtype, const void* const* ptrs, int n) {
+  if (T < 0 || T > INT_MAX || d < 1) return MLS_ERR_ARG;
+  if (dtype != MLS_BF16 && dtype != MLS_FP32) return MLS_ERR_ARG;
+  if ((static_cast<long long>(d) * (dtype == MLS_BF16 ? 2 : 4)) % 16) return MLS_ERR_UNSUPPORTED;
+  for (int i = 0; i < n; ++i) {
+    if (T > 0 && !ptrs[i]) return MLS_ERR_ARG;
+    if (!aligned16(ptrs[i])) return MLS_ERR_ALIGN;
+  }
+  return MLS_OK;
+}
+int current_sms() {
+  DeviceState* dev = nullptr;
+  if (device_state(&dev) == MLS_OK) return dev->sms;
+  cudaGetLastError();
+  return 152;
+}
+}  // namespace
+
+extern "C" int mls_layer_norm_fwd(int64_t T, int32_t d, int32_t in_dtype, float eps, const void* x,
+                                  const void* gain, const void* bias, void* y, float* mean,
+                                  float* rstd, mls_stream_t stream) {
+  const void* ptrs[2] = {x, y};
+  int rc = norm_check(T, d, in_dtype, ptrs, 2);
+  if (rc) return rc;
+  if (!(eps >= 0.f) || !std::isfinite(eps) || !mean != !rstd) return MLS_ERR_ARG;
+  if (!aligned16(gain) || !aligned16(bias) || !aligned4(mean) || !aligned4(rstd)) return MLS_ERR_ALIGN;
+  DeviceState* dev = nullptr;
+  if ((rc = device_state(&dev))) return rc;
+  NormParams np;
+  std::memset(&np, 0, sizeof np);
+  np.T = T;
+  np.d = d;
+  np.eps = eps;
+  np.x = x;
+  np.gain = gain;
+  np.bias = bias;
+  np.y = y;
+  np.mean = mean;
+  np.rstd = rstd;
+  np.sms = dev->sms;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  return timed("norm_fwd", s, [&] { return launch_norm_fwd(np, in_dtype == MLS_FP32, s); });
+}
+
+extern "C" size_t mls_layer_norm_workspace_size(int64_t T, int32_t d) {
+  if (T < 0 || T > INT_MAX || d < 1) return 0;
+  return align_up(sizeof(float) * 2 * static_cast<size_t>(d) * norm_splits(T, d, current_sms()));
+}
+
+extern "C" int mls_layer_norm_bwd(int64_t T, int32_t d, int32_t in_dtype, const void* x,
+                                  const void* gain, const void* dy, const float* mean,
+                                  const float* rstd, void* dx, float* dgain, float* dbias, void* ws,
+                                  size_t ws_bytes, mls_stream_t stream) {
+  const void* ptrs[3] = {x, dy, dx};
+  int rc = norm_check(T, d, in_dtype, ptrs, 3);
+  if (rc) return rc;
+  if (T > 0 && (!mean || !rstd)) return MLS_ERR_ARG;
+  if (!aligned16(gain) || !aligned4(mean) || !aligned4(rstd) || !aligned4(dgain) || !aligned4(dbias))
+    return MLS_ERR_ALIGN;
+  DeviceState* dev = nullptr;
+  if ((rc = device_state(&dev))) return rc;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  if (T == 0) {
+    for (float* out : {dgain, dbias})
+      if (out && (rc = launch_ok(cudaMemsetAsync(out, 0, sizeof(float) * d, s)))) return rc;
+    return MLS_OK;
+  }
+  NormParams np;
+  std::memset(&np, 0, sizeof np);
+  np.T = T;
+  np.d = d;
+  np.x = x;
+  np.gain = gain;
+  np.dy = dy;
+  np.mean = const_cast<float*>(mean);
+  np.rstd = const_cast<float*>(rstd);
+  np.dx = dx;
+  np.dgain = dgain;
+  np.dbias = dbias;
+  np.sms = dev->sms;
+  np.splits = norm_splits(T, d, dev->sms);
+  if (dgain || dbias) {
+    if (!ws || (reinterpret_cast<uintptr_t>(ws) % kAlign) != 0 ||
+        ws_bytes < align_up(sizeof(float) * 2 * static_cast<size_t>(d) * np.splits))
+      return MLS_ERR_WORKSPACE;
+    np.part = static_cast<float*>(ws);
+  }
+  return timed("norm_bwd", s, [&] { return launch_norm_bwd(np, in_dtype == MLS_FP32, s); });
+}
+
+// ------------------------------------------------------------------ clipped policy loss
+namespace {
+int policy_validate(const mls_policy_problem* p) {
+  if (!p || p->M < 1 || p->M > MLS_MAX_MODELS || p->T < 0 || p->T > INT_MAX || p->V < 1 || p->V > INT_MAX ||
+      p->B < 0 || p->B == INT_MAX)
+    return MLS_ERR_ARG;
+  if (p->agg != MLS_AGG_TOKEN_MEAN && p->agg != MLS_AGG_SEQ_MEAN && p->agg != MLS_AGG_SUM) return MLS_ERR_ARG;
+  if (!(p->clip_low >= 0.f) || !(p->clip_high >= 0.f)) return MLS_ERR_ARG;
+  if (!(p->beta >= 0.f) || !std::isfinite(p->beta)) return MLS_ERR_ARG;
+  if (p->T > 0 && p->B == 0 && (p->agg == MLS_AGG_SEQ_MEAN || p->adv_per_seq)) return MLS_ERR_ARG;
+  if (p->w)
+    for (int m = 0; m < p->M; ++m)
+      if (!std::isfinite(p->w[m])) return MLS_ERR_ARG;
+  return MLS_OK;
+}
+
+struct PolicyPlan {
+  int chunks = 0;
+  long long count_tokens = 0;
+  size_t off_part = 0, total = 0;
+};
+// Counts per chunk of tokens, at most 4096 of them, so that a block can add all.
+PolicyPlan policy_plan(const mls_policy_problem* p) {
+  PolicyPlan pl;
+  const long long blocks = policy_blocks(p->T);
+  pl.count_tokens = kPolicyTokens * (blocks > 4096 ? ceil_div(blocks, 4096) : 1);
+  if (blocks > 1 && p->agg != MLS_AGG_SUM) pl.chunks = static_cast<int>(ceil_div(p->T, pl.count_tokens));
+  pl.off_part = align_up(sizeof(int) * static_cast<size_t>(pl.chunks));
+  pl.total = align_up(pl.off_part + sizeof(double) * 3 * p->M * static_cast<size_t>(blocks));
+  return pl;
+}
+
+// v as the sum of two floats.
+void two_words(double v, float (&out)[2]) {
+  out[0] = static_cast<float>(v);
+  out[1] = std::isfinite(v) ? static_cast<float>(v - static_cast<double>(out[0])) : 0.f;
+}
+}  // namespace
+
+extern "C" size_t mls_policy_workspace_size(const mls_policy_problem* p) {
+  if (policy_validate(p)) return 0;
+  return policy_plan(p).total;
+}
+
+extern "C" int mls_policy_loss(const mls_policy_problem* p, const float* logp, const float* old_logp,
+                               const float* ref_logp, const float* adv, const int32_t* targets,
+                               const int32_t* seq_start, float grad_scale, float* loss,
+                               float* tok_loss, float* diag, float* dlogp, void* ws, size_t ws_bytes,
+                               mls_stream_t stream) {
+  int rc = policy_validate(p);
+  if (rc) return rc;
+  if (!loss || !std::isfinite(grad_scale)) return MLS_ERR_ARG;
+  if (p->T > 0) {
+    if (!logp || !old_logp || !adv || !targets || (p->beta > 0.f && !ref_logp)) return MLS_ERR_ARG;
+    if (!seq_start && (p->B > 0 || p->agg == MLS_AGG_SEQ_MEAN || p->adv_per_seq)) return MLS_ERR_ARG;
+    if (seq_start && p->B == 0) return MLS_ERR_ARG;
+  }
+  for (const void* ptr : {static_cast<const void*>(logp), static_cast<const void*>(old_logp),
+                          static_cast<const void*>(ref_logp), static_cast<const void*>(adv),
+                          static_cast<const void*>(targets), static_cast<const void*>(seq_start),
+                          static_cast<const void*>(loss), static_cast<const void*>(tok_loss),
+                          static_cast<const void*>(diag), static_cast<const void*>(dlogp)})
+    if (!aligned4(ptr)) return MLS_ERR_ALIGN;
+  DeviceState* dev = nullptr;
+  if ((rc = device_state(&dev))) return rc;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  if (p->T == 0) {
+    if ((rc = launch_ok(cudaMemsetAsync(loss, 0, sizeof(float), s)))) return rc;
+    return diag ? launch_ok(cudaMemsetAsync(diag, 0, sizeof(float) * 3 * p->M, s)) : MLS_OK;
+  }
+  const PolicyPlan pl = policy_plan(p);
+  if (!ws || (reinterpret_cast<uintptr_t>(ws) % kAlign) != 0 || ws_bytes < pl.total) return MLS_ERR_WORKSPACE;
+  PolicyParams pp;
+  std::memset(&pp, 0, sizeof pp);
+  pp.T = p->T;
+  pp.V = p->V;
+  pp.M = p->M;
+  pp.B = p->B;
+  pp.agg = p->agg;
+  pp.adv_per_seq = p->adv_per_seq ? 1 : 0;
+  pp.beta = p->beta;
+  pp.grad_scale = grad_scale;
+  for (int m = 0; m < p->M; ++m) pp.w[m] = p->w ? p->w[m] : 1.0f;
+  const double lo = 1.0 - static_cast<double>(p->clip_low), hi = 1.0 + static_cast<double>(p->clip_high);
+  two_words(std::log(hi), pp.high);
+  two_words(lo > 0.0 ? std::log(lo) : -INFINITY, pp.low);
+  pp.ratio_high = static_cast<float>(hi);
+  pp.ratio_low = static_cast<float>(lo);
+  pp.logp = logp;
+  pp.old_logp = old_logp;
+  pp.ref_logp = ref_logp;
+  pp.adv = adv;
+  pp.y = targets;
+  pp.seq_start = seq_start;
+  pp.loss = loss;
+  pp.tok_loss = tok_loss;
+  pp.diag = diag;
+  pp.dlogp = dlogp;
+  pp.chunks = pl.chunks;
+  pp.count_tokens = pl.count_tokens;
+  pp.chunk_count = static_cast<int*>(ws);
+  pp.part = reinterpret_cast<double*>(static_cast<char*>(ws) + pl.off_part);
+  pp.status = dev->status;
+  return timed("policy", s, [&] { return launch_policy(pp, s); });
+}
+
+// ------------------------------------------------------------------ gradient norm and clipping
+namespace {
+// Blocks of a clipping launch at most: its shares of the norm.
+constexpr int kClipBlocks = 2048;
+// Whether no two tensors share memory.  Sorted by address in place of the n^2 pairs;
+// kept off the heap, which could throw.
+bool clip_disjoint(int n, void* const* g, const int64_t* numel, const int32_t* dtype) {
+  static thread_local int order[MLS_CLIP_MAX_TENSORS];
+  int k = 0;
+  bool sorted = true;
+  auto at = [&](int i) { return reinterpret_cast<uintptr_t>(g[i]); };
+  for (int i = 0; i < n; ++i)
+    if (numel[i] > 0) {
+      sorted = sorted && (k == 0 || at(order[k - 1]) <= at(i));
+      order[k++] = i;
+    }
+  if (!sorted) std::sort(order, order + k, [&](int a, int b) { return at(a) < at(b); });
+  for (int i = 0; i + 1 < k; ++i)
+    if (at(order[i]) + static_cast<uintptr_t>(numel[order[i]]) * (dtype[order[i]] == MLS_BF16 ? 2 : 4) > at(order[i + 1]))
+      return false;
+  return true;
+}
+size_t clip_workspace(int n) {
+  return align_up(sizeof(double) * kClipBlocks * static_cast<size_t>(n > 0 ? ceil_div(n, kClipTable) : 1));
+}
+}  // namespace
+
+extern "C" size_t mls_grad_clip_workspace_size(int32_t n) {
+  return n < 0 || n > MLS_CLIP_MAX_TENSORS ? 0 : clip_workspace(n);
+}
+
+extern "C" int mls_grad_clip(int32_t n, void* const* g, const int64_t* numel, const int32_t* dtype,
+                             float max_norm, float* stats, void* ws, size_t ws_bytes,
+                             mls_stream_t stream) {
+  if (n < 0 || !stats || !(max_norm > 0.f) || (n > 0 && (!g || !numel || !dtype))) return MLS_ERR_ARG;
+  if (n > MLS_CLIP_MAX_TENSORS) return MLS_ERR_UNSUPPORTED;
+  if (!aligned4(stats)) return MLS_ERR_ALIGN;
+  long long chunks = 0;
+  for (int i = 0; i < n; ++i) {
+    if (numel[i] < 0 || (dtype[i] != MLS_BF16 && dtype[i] != MLS_FP32)) return MLS_ERR_ARG;
+    if (numel[i] == 0) continue;
+    const int elt = dtype[i] == MLS_BF16 ? 2 : 4;
+    if (!g[i] || numel[i] > INT64_MAX / 8) return MLS_ERR_ARG;
+    if (reinterpret_cast<uintptr_t>(g[i]) % elt) return MLS_ERR_ALIGN;
+    chunks += numel[i] / kClipChunk + 1;
+    if (chunks > INT_MAX) return MLS_ERR_UNSUPPORTED;
+  }
+  if (!clip_disjoint(n, g, numel, dtype)) return MLS_ERR_ARG;
+  DeviceState* dev = nullptr;
+  int rc = device_state(&dev);
+  if (rc) return rc;
+  if (!ws || (reinterpret_cast<uintptr_t>(ws) % kAlign) != 0 || ws_bytes < clip_workspace(n))
+    return MLS_ERR_WORKSPACE;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  const bool scale = !std::isinf(max_norm);
+  ClipParams<kClipTable> cp;
+  cp.max_norm = max_norm;
+  cp.part = static_cast<double*>(ws);
+  // Pass 0 sums the squares, pass 1 scales; a launch takes kClipTable tensors.
+  int nparts = 0;
+  for (int pass = 0; pass < 2; ++pass) {
+    for (int first = 0; first == 0 || first < n; first += kClipTable) {
+      const int last = n - first < kClipTable ? n : first + kClipTable;
+      cp.n = 0;
+      cp.chunks = 0;
+      for (int i = first; i < last; ++i) {
+        if (numel[i] == 0) continue;
+        const int elt = dtype[i] == MLS_BF16 ? 2 : 4;
+        long long head = (16 - reinterpret_cast<uintptr_t>(g[i]) % 16) % 16 / elt;
+        if (head > numel[i]) head = numel[i];
+        ClipTensor& t = cp.t[cp.n++];
+        t.g = g[i];
+        t.numel = numel[i];
+        t.chunk0 = cp.chunks;
+        t.head = static_cast<short>(head);
+        t.fp32 = elt == 4;
+        const long long c = ceil_div(numel[i] - head, kClipChunk);
+        cp.chunks += static_cast<int>(c > 0 ? c : 1);
+      }
+      const int most = dev->sms * 6 < kClipBlocks ? dev->sms * 6 : kClipBlocks;
+      const int grid = cp.chunks < 1 ? 1 : cp.chunks < most ? cp.chunks : most;
+      if (pass == 0) {
+        cp.part0 = nparts;
+        nparts += grid;
+        if ((rc = timed("clip_norm", s, [&] { return launch_clip_norm(cp, grid, s); }))) return rc;
+      } else {
+        cp.nparts = nparts;
+        cp.stats = first == 0 ? stats : nullptr;
+        if ((rc = timed("clip_scale", s, [&] { return launch_clip_scale(cp, scale ? grid : 1, s); }))) return rc;
+        if (!scale) break;
+      }
+    }
+  }
+  return MLS_OK;
 }
 
 // ------------------------------------------------------------------ speculative verify

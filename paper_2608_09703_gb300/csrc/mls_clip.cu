@@ -1,0 +1,180 @@
+// Global gradient norm over many tensors, and clipping in place:
+//   n = sqrt(sum over all tensors of g^2),  c = min(1, max_norm / (n + 1e-6)),  g *= c
+// A call's tensors come as a table in the kernels' parameters (kClipTable of them
+// a launch), cut into chunks of kClipChunk values that persistent blocks take in
+// turn.  Squares are summed in fp32 over the 32 values that a thread holds of a
+// chunk and in 64 bits from there on.  Where such a sum leaves the range in which
+// fp32 squares are exact to rounding (a square that overflowed, or squares so
+// small that some were flushed) those 32 values are summed again in 64 bits, so
+// the norm is right from the smallest to the largest representable gradient.
+// The blocks' shares are added in a fixed order: results do not depend on timing.
+#include "mls_device.cuh"
+#include "mls_kernels.h"
+#include "mls_vec.cuh"
+
+namespace mls {
+namespace {
+
+constexpr int kThreads = 256;
+
+// Sum over the block in thread order of a butterfly; valid in every thread.
+__device__ __forceinline__ double block_sum(double v, double* sh) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
+  __syncthreads();
+  double s = 0.0;
+#pragma unroll
+  for (int i = 0; i < kThreads / 32; ++i) s += sh[i];
+  return s;
+}
+
+// The tensor of chunk c: the last one whose first chunk is not past c.
+template <int kCap>
+__device__ __forceinline__ int tensor_of(const ClipParams<kCap>& p, int c) {
+  int lo = 0, hi = p.n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (p.t[mid].chunk0 <= c) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
+
+// Sum of the squares of a thread's values of a chunk, see above.
+template <int n>
+__device__ __forceinline__ double exact_squares(const float (&f)[n]) {
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < n; ++i) s[i & 3] = fmaf(f[i], f[i], s[i & 3]);
+  const float a = (s[0] + s[1]) + (s[2] + s[3]);
+  if (a >= 0x1p-80f && a <= 0x1p100f) return static_cast<double>(a);
+  float most = 0.f;
+#pragma unroll
+  for (int i = 0; i < n; ++i) most = fmaxf(most, fabsf(f[i]));
+  if (a == 0.f && most == 0.f) return 0.0;  // zeros: a frozen tensor, rows of unused tokens
+  double d = 0.0;
+#pragma unroll
+  for (int i = 0; i < n; ++i) d = fma(static_cast<double>(f[i]), static_cast<double>(f[i]), d);
+  return d;
+}
+
+// Chunk `local` of a tensor: whole vectors of 16 bytes where there are any, single
+// values at its end.  A tensor that starts off a 16-byte boundary has `head`
+// values before its first vector, which go with chunk 0.
+template <typename E>
+__device__ __forceinline__ double chunk_squares(const E* g, const ClipTensor& t, int local) {
+  constexpr int N = Vec<E>::N, kV = kClipChunk / kThreads / N;
+  const long long first = t.head + static_cast<long long>(local) * kClipChunk;
+  double acc = 0.0;
+  float f[kV * N];
+#pragma unroll
+  for (int v = 0; v < kV; ++v) {
+    const long long e = first + (v * kThreads + static_cast<int>(threadIdx.x)) * N;
+    float w[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = 0.f;
+    if (e + N <= t.numel) {
+      Vec<E>::unpack(ld16(g + e), w);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (e + i < t.numel) w[i] = static_cast<float>(g[e + i]);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[v * N + i] = w[i];
+  }
+  acc = exact_squares(f);
+  if (local == 0 && static_cast<int>(threadIdx.x) < t.head) {
+    const double h = static_cast<double>(static_cast<float>(g[threadIdx.x]));
+    acc = fma(h, h, acc);
+  }
+  return acc;
+}
+
+template <int kCap>
+__global__ void __launch_bounds__(kThreads) clip_norm_kernel(const __grid_constant__ ClipParams<kCap> p) {
+  __shared__ double sh[kThreads / 32];
+  double acc = 0.0;
+  for (int c = blockIdx.x; c < p.chunks; c += gridDim.x) {
+    const ClipTensor& t = p.t[tensor_of(p, c)];
+    if (t.fp32)
+      acc += chunk_squares(static_cast<const float*>(t.g), t, c - t.chunk0);
+    else
+      acc += chunk_squares(static_cast<const __nv_bfloat16*>(t.g), t, c - t.chunk0);
+  }
+  const double s = block_sum(acc, sh);
+  if (threadIdx.x == 0) p.part[p.part0 + blockIdx.x] = s;
+}
+
+template <typename E>
+__device__ __forceinline__ void chunk_scale(E* g, const ClipTensor& t, int local, float coef) {
+  constexpr int N = Vec<E>::N, kV = kClipChunk / kThreads / N;
+  const long long first = t.head + static_cast<long long>(local) * kClipChunk;
+  uint4 u[kV];
+#pragma unroll
+  for (int v = 0; v < kV; ++v) {
+    const long long e = first + (v * kThreads + static_cast<int>(threadIdx.x)) * N;
+    if (e + N <= t.numel) u[v] = ld16(g + e);
+  }
+#pragma unroll
+  for (int v = 0; v < kV; ++v) {
+    const long long e = first + (v * kThreads + static_cast<int>(threadIdx.x)) * N;
+    if (e + N <= t.numel) {
+      float w[N];
+      Vec<E>::unpack(u[v], w);
+#pragma unroll
+      for (int i = 0; i < N; ++i) w[i] *= coef;
+      st16(g + e, Vec<E>::pack(w));
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (e + i < t.numel) g[e + i] = static_cast<E>(static_cast<float>(g[e + i]) * coef);
+    }
+  }
+  if (local == 0 && static_cast<int>(threadIdx.x) < t.head)
+    g[threadIdx.x] = static_cast<E>(static_cast<float>(g[threadIdx.x]) * coef);
+}
+
+// Every block adds all shares of the norm itself, in the same order.
+template <int kCap>
+__global__ void __launch_bounds__(kThreads) clip_scale_kernel(const __grid_constant__ ClipParams<kCap> p) {
+  __shared__ double sh[kThreads / 32];
+  double a = 0.0;
+  for (int i = threadIdx.x; i < p.nparts; i += kThreads) a += p.part[i];
+  const double norm = sqrt(block_sum(a, sh));
+  const double ratio = static_cast<double>(p.max_norm) / (norm + 1e-6);
+  // NaN stays (every gradient becomes NaN); an infinite norm gives 0, as the formula says
+  const float coef = isinf(p.max_norm) || ratio >= 1.0 ? 1.f : static_cast<float>(ratio);
+  if (p.stats && blockIdx.x == 0 && threadIdx.x == 0) {
+    p.stats[0] = static_cast<float>(norm);
+    p.stats[1] = coef;
+  }
+  if (coef == 1.f) return;  // nothing to change
+  for (int i = blockIdx.x; i < p.chunks; i += gridDim.x) {
+    const int c = p.chunks - 1 - i;  // the values read last are the likeliest in L2
+    const ClipTensor& t = p.t[tensor_of(p, c)];
+    if (t.fp32)
+      chunk_scale(static_cast<float*>(t.g), t, c - t.chunk0, coef);
+    else
+      chunk_scale(static_cast<__nv_bfloat16*>(t.g), t, c - t.chunk0, coef);
+  }
+}
+
+}  // namespace
+
+template <int kCap>
+cudaError_t launch_clip_norm(const ClipParams<kCap>& p, int grid, cudaStream_t s) {
+  clip_norm_kernel<kCap><<<grid, kThreads, 0, s>>>(p);
+  return cudaGetLastError();
+}
+template <int kCap>
+cudaError_t launch_clip_scale(const ClipParams<kCap>& p, int grid, cudaStream_t s) {
+  clip_scale_kernel<kCap><<<grid, kThreads, 0, s>>>(p);
+  return cudaGetLastError();
+}
+template cudaError_t launch_clip_norm(const ClipParams<kClipTable>&, int, cudaStream_t);
+template cudaError_t launch_clip_scale(const ClipParams<kClipTable>&, int, cudaStream_t);
+
+}  // namespace mls

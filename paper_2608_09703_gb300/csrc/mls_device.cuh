@@ -16,6 +16,7 @@ constexpr int kStatusBadTarget = 1;
 constexpr int kStatusTimeout = 2;
 constexpr int kStatusCheck = 4;
 constexpr int kStatusDrain = 8;
+constexpr int kStatusBadSeq = 16;
 
 // Invariant checks of the checked build (-DMLS_CHECKED, libmls_checked.so):
 // a failed condition raises kStatusCheck in the status word and execution

@@ -30,6 +30,9 @@
 //            student  c_m [(1-alpha)(softmax(z_m) - e_y) + (alpha/tau)(softmax(z_m/tau) - q)]
 //            with q = softmax(z_t / tau) from the forward's statistics, and
 //            stores it (bf16, fp32 for fp32 inputs) for the dH / dW GEMMs.
+// Log-probabilities of given tokens run on the same tiles, every sub-model alike:
+//   forward  online sum of exp(z / tau) relative to the running maximum, and z[y]
+//   backward dL/dz = (dL/dlogp / tau) (e_y - softmax(z / tau)), a factor per token
 #include "mls_device.cuh"
 #include "mls_kernels.h"
 
@@ -38,6 +41,8 @@ namespace {
 
 constexpr int kModeFwd = 0;
 constexpr int kModeBwd = 1;
+constexpr int kModeLogpFwd = 2;
+constexpr int kModeLogpBwd = 3;
 constexpr int kStud = kMaxModels - 1;
 
 // Shared-memory map, offsets from the 1024-byte-aligned base.
@@ -653,6 +658,182 @@ __device__ __forceinline__ void bwd_epilogue(const HeadParams& p, uint32_t base,
   __syncwarp();
 }
 
+// ------------------------------------------------------------------ log-probabilities
+// One sub-model's tile: running maximum m of z, s = sum of 2^((z - m) Lt).
+template <bool kMasked>
+__device__ __forceinline__ void logp_tile(uint32_t ta, int nvalid, int yl, float Lt, float& m, float& s,
+                                          float& zy) {
+  float v[32];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    if (kMasked && c * 32 >= nvalid) break;
+    tmem_ld32(ta + c * 32, v);
+    if (kMasked) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (c * 32 + i >= nvalid) v[i] = -INFINITY;
+    }
+    float mx[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+    for (int i = 4; i < 32; ++i) mx[i & 3] = fmaxf(mx[i & 3], v[i]);
+    const float cmax = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+    if (cmax > m) {
+      s *= fast_exp2((m - cmax) * Lt);
+      m = cmax;
+    }
+    const float b = -m * Lt;
+    float s4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 32; ++i) s4[i & 3] += fast_exp2(fmaf(v[i], Lt, b));
+    s += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+    const int r = yl - c * 32;
+    if (static_cast<unsigned>(r) < 32u) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (i == r) zy = v[i];
+    }
+  }
+}
+
+__device__ __forceinline__ void logp_fwd_epilogue(const HeadParams& p, uint32_t base, uint32_t tmem,
+                                                  float* xchg, int row_base, const volatile int* tiles,
+                                                  int warp, int lane, volatile int* abort_flag) {
+  const int quad = warp & 3, half = warp >> 2;
+  const long long row = static_cast<long long>(row_base) + quad * 32 + lane;
+  const bool row_ok = row < p.T;
+  const int y = row_ok ? __ldg(p.y + row) : -1;
+  const uint32_t tl = tmem + (static_cast<uint32_t>(quad * 32) << 16) + static_cast<uint32_t>(half * 128);
+  float m[kMaxModels], s[kMaxModels], zy[kMaxModels];
+#pragma unroll
+  for (int j = 0; j < kMaxModels; ++j) {
+    m[j] = -INFINITY;
+    s[j] = zy[j] = 0.f;
+  }
+  uint32_t acc = 0, acc_par = 0;
+  bool aborted = false;
+  for (int vt = tiles[0]; !aborted && vt < tiles[1]; vt += tiles[2]) {
+    const long long col0 = static_cast<long long>(vt) * kHeadBN + half * 128;
+    const int nvalid = static_cast<int>(max(0LL, min(128LL, p.V - col0)));
+    const int yl = y >= 0 ? static_cast<int>(y - col0) : -1;
+#pragma unroll
+    for (int j = 0; j < kMaxModels; ++j) {
+      if (j < p.M && !aborted) {
+        if (!epi_acquire(p, base, acc, acc_par, abort_flag)) {
+          aborted = true;
+          break;
+        }
+        const uint32_t ta = tl + acc * kHeadBN;
+        if (nvalid == 128)
+          logp_tile<false>(ta, 128, yl, p.Ltau, m[j], s[j], zy[j]);
+        else if (nvalid > 0)
+          logp_tile<true>(ta, nvalid, yl, p.Ltau, m[j], s[j], zy[j]);
+        epi_release(base, acc, acc_par, lane);
+      }
+    }
+  }
+  // The two column halves of a token, as in the loss's forward.
+  const int r = quad * 32 + lane;
+  auto X = [&](int f, int j) -> float& { return xchg[(f * kMaxModels + j) * kHeadBM + r]; };
+  if (half == 1) {
+#pragma unroll
+    for (int j = 0; j < kMaxModels; ++j) {
+      X(kLogpMax, j) = m[j];
+      X(kLogpSum, j) = s[j];
+      X(kLogpTarget, j) = zy[j];
+    }
+  }
+  named_bar_sync(1, kHeadEpiWarps * 32);
+  if (half == 1 || !row_ok) return;
+  const long long MT = static_cast<long long>(p.M) * p.T;
+  MLS_CHECK(p.status, tiles[3] < p.split.S + p.split.extra && row < p.T);
+  float* P = p.part + static_cast<long long>(tiles[3]) * kLogpFields * MT + row;
+#pragma unroll
+  for (int j = 0; j < kMaxModels; ++j) {
+    if (j < p.M) {
+      const float m1 = X(kLogpMax, j), mm = fmaxf(m[j], m1);
+      float* Pj = P + static_cast<long long>(j) * p.T;
+      Pj[kLogpMax * MT] = mm;
+      Pj[kLogpSum * MT] = s[j] * scale_from(m[j], mm, p.Ltau) + X(kLogpSum, j) * scale_from(m1, mm, p.Ltau);
+      Pj[kLogpTarget * MT] = zy[j] + X(kLogpTarget, j);
+    }
+  }
+}
+
+// dL/dz of one tile: c (softmax(z / tau) - e_y), c = -dL/dlogp / tau, b = -logsumexp(z / tau) log2(e).
+template <bool kMasked>
+__device__ __forceinline__ void logp_grad_tile(uint32_t ta, int nvalid, int yl, float Lt, float b, float c,
+                                               const GOut& o, int gcol, int lane) {
+  float v[32], g[32];
+#pragma unroll
+  for (int ch = 0; ch < 4; ++ch) {
+    tmem_ld32(ta + ch * 32, v);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const bool ok = !kMasked || (ch * 32 + i < nvalid);
+      g[i] = ok ? c * fast_exp2(fmaf(v[i], Lt, b)) : 0.f;
+    }
+    const int r = yl - ch * 32;
+    if (static_cast<unsigned>(r) < 32u) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (i == r) g[i] -= c;
+    }
+    put_chunk<false>(o, gcol, ch, g, lane);
+  }
+}
+
+__device__ __forceinline__ void logp_bwd_epilogue(const HeadParams& p, uint32_t base, uint32_t tmem,
+                                                  int row_base, const volatile int* tiles, int warp, int lane,
+                                                  volatile int* abort_flag) {
+  const int quad = warp & 3, half = warp >> 2;
+  const long long row = static_cast<long long>(row_base) + quad * 32 + lane;
+  const bool row_ok = row < p.T;
+  const int y = row_ok ? __ldg(p.y + row) : -1;
+  const bool valid = row_ok && y >= 0 && y < p.V;
+  chain_wait();  // the GEMM of the group before has read its dL/dz
+  const uint32_t tl = tmem + (static_cast<uint32_t>(quad * 32) << 16) + static_cast<uint32_t>(half * 128);
+  uint32_t nchunks = 0;
+  const uint32_t stage = base + HeadSmem::kStage + static_cast<uint32_t>(warp) * 2 * kHeadStageChunk;
+  const int row0 = row_base + quad * 32;
+  float c[kMaxModels], b[kMaxModels];
+#pragma unroll
+  for (int j = 0; j < kMaxModels; ++j) {
+    const bool on = j < p.M && valid;
+    const long long i = static_cast<long long>(j) * p.T + row;
+    c[j] = on ? p.neg_inv_tau * p.dlogp[i] : 0.f;
+    b[j] = j < p.M && row_ok ? -__ldg(p.stats + i) * p.L1 : 0.f;
+    // A token without a gradient adds nothing, whatever its logits: 2^-inf = 0.
+    if (c[j] == 0.f) b[j] = -INFINITY;
+  }
+  uint32_t acc = 0, acc_par = 0;
+  bool aborted = false;
+  for (int vt = tiles[0]; !aborted && vt < tiles[1]; vt += tiles[2]) {
+    const long long col0 = static_cast<long long>(vt) * kHeadBN + half * 128;
+    const int nvalid = static_cast<int>(max(0LL, min(128LL, p.V - col0)));
+    const int yl = y >= 0 ? static_cast<int>(y - col0) : -1;
+    const int gcol = static_cast<int>(col0 - p.g_col0);  // column within the group buffer
+#pragma unroll
+    for (int j = 0; j < kMaxModels; ++j) {
+      if (j < p.M && !aborted) {
+        if (!epi_acquire(p, base, acc, acc_par, abort_flag)) {
+          aborted = true;
+          break;
+        }
+        const uint32_t ta = tl + acc * kHeadBN;
+        const GOut o{&p.mapG[j], stage, &nchunks, row0};
+        if (nvalid == 128)
+          logp_grad_tile<false>(ta, 128, yl, p.Ltau, b[j], c[j], o, gcol, lane);
+        else
+          logp_grad_tile<true>(ta, nvalid, yl, p.Ltau, b[j], c[j], o, gcol, lane);
+        epi_release(base, acc, acc_par, lane);
+      }
+    }
+  }
+  // Every staged store has finished before the CTA's shared memory goes away.
+  if (lane == 0) bulk_wait_all();
+  __syncwarp();
+}
+
 // ------------------------------------------------------------------ kernel
 template <int kMode, bool kTF32, bool kTauOne>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHeadThreads, 1)
@@ -725,6 +906,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHeadThreads, 1)
     if constexpr (kMode == kModeFwd)
       fwd_epilogue<kTauOne>(p, base, tmem, reinterpret_cast<float*>(gbase + HeadSmem::kStage),
                             row_base, tiles, warp, lane, abort_flag);
+    else if constexpr (kMode == kModeLogpFwd)
+      logp_fwd_epilogue(p, base, tmem, reinterpret_cast<float*>(gbase + HeadSmem::kStage), row_base, tiles,
+                        warp, lane, abort_flag);
+    else if constexpr (kMode == kModeLogpBwd)
+      logp_bwd_epilogue(p, base, tmem, row_base, tiles, warp, lane, abort_flag);
     else
       bwd_epilogue<kTauOne, kTF32>(p, base, tmem, row_base, tiles, warp, lane, abort_flag);
   }
@@ -754,9 +940,6 @@ cudaError_t launch_head(const HeadParams& p, bool tf32, bool tau_one, cudaStream
   return tau_one ? launch_mode<kMode, false, true>(p, grid, s) : launch_mode<kMode, false, false>(p, grid, s);
 }
 
-template <int kMode>
-cudaError_t setup_mode() {
-  cudaError_t e;
 #define MLS_SET(TF, TO)                                                                      \
   e = cudaFuncSetAttribute(head_kernel<kMode, TF, TO>, cudaFuncAttributeMaxDynamicSharedMemorySize, \
                            kHeadSmem);                                                       \
@@ -768,13 +951,23 @@ cudaError_t setup_mode() {
     if (fa.maxThreadsPerBlock < kHeadThreads || fa.numRegs != kHeadLaunchRegs)               \
       return cudaErrorLaunchOutOfResources;                                                  \
   }
+template <int kMode>
+cudaError_t setup_mode() {
+  cudaError_t e;
   MLS_SET(true, true)
   MLS_SET(true, false)
   MLS_SET(false, true)
   MLS_SET(false, false)
-#undef MLS_SET
   return cudaSuccess;
 }
+
+template <int kMode>
+cudaError_t setup_logp_mode() {
+  cudaError_t e;
+  MLS_SET(false, true)
+  return cudaSuccess;
+}
+#undef MLS_SET
 
 }  // namespace
 
@@ -797,10 +990,28 @@ cudaError_t launch_head_fwd(const HeadParams& p, bool tf32, bool tau_one, cudaSt
 cudaError_t launch_head_bwd(const HeadParams& p, bool tf32, bool tau_one, cudaStream_t s) {
   return launch_head<kModeBwd>(p, tf32, tau_one, s);
 }
+// The log-probability kernels serve every temperature with one exponential, so there is
+// one of each; `chained`: not the call's first kernel.
+cudaError_t launch_logp_fwd(const HeadParams& p, cudaStream_t s) {
+  const int grid = 2 * p.split.pairs();
+  if (grid <= 0) return cudaSuccess;
+  head_kernel<kModeLogpFwd, false, true><<<grid, kHeadThreads, kHeadSmem, s>>>(p);
+  return cudaGetLastError();
+}
+cudaError_t launch_logp_bwd(const HeadParams& p, bool chained, cudaStream_t s) {
+  const int grid = 2 * p.split.pairs();
+  if (grid <= 0) return cudaSuccess;
+  if (chained)
+    return launch_chained(head_kernel<kModeLogpBwd, false, true>, dim3(grid), dim3(kHeadThreads), kHeadSmem, s, p);
+  head_kernel<kModeLogpBwd, false, true><<<grid, kHeadThreads, kHeadSmem, s>>>(p);
+  return cudaGetLastError();
+}
 cudaError_t setup_head_kernels() {
   cudaError_t e = setup_mode<kModeFwd>();
   if (e != cudaSuccess) return e;
-  return setup_mode<kModeBwd>();
+  if ((e = setup_mode<kModeBwd>()) != cudaSuccess) return e;
+  if ((e = setup_logp_mode<kModeLogpFwd>()) != cudaSuccess) return e;
+  return setup_logp_mode<kModeLogpBwd>();
 }
 
 }  // namespace mls

@@ -140,7 +140,11 @@ struct HeadParams {
   float alpha_over_tau;          // alpha / tau
   CUtensorMap mapG[kMaxModels];  // G_m [T, group] bf16 (fp32), box {64 bytes, 32}, 64B swizzle (TMA store)
   long long g_col0;              // vocabulary column of the group's first column
+  // log-probabilities: `part` holds [S + extra][kLogpFields][M][T], `stats` [M][T]: logsumexp(z/tau)
+  const float* dlogp;            // [M][T]
+  float neg_inv_tau;             // -1 / tau
 };
+enum LogpField { kLogpMax = 0, kLogpSum, kLogpTarget, kLogpFields };
 
 // ------------------------------------------------------------------ GEMM kernels
 // CTA pairs: a pair owns a 256 x kGemmBN output tile; each CTA of the pair
@@ -408,6 +412,8 @@ constexpr int kEvalMergeTokens = 32;  // tokens per evaluation-merge block: one 
 // Launchers (return the cudaError_t of the launch).
 cudaError_t launch_head_fwd(const HeadParams& p, bool tf32, bool tau_one, cudaStream_t s);
 cudaError_t launch_head_bwd(const HeadParams& p, bool tf32, bool tau_one, cudaStream_t s);
+cudaError_t launch_logp_fwd(const HeadParams& p, cudaStream_t s);
+cudaError_t launch_logp_bwd(const HeadParams& p, bool chained, cudaStream_t s);
 // B MN-major, A's layout per problem (GemmProblem::a_mn): dW and dH in one launch.
 cudaError_t launch_gemm_mixed(GemmParams& p, bool tf32, int grid, cudaStream_t s);
 // Both operands K-major, with the statistics epilogues (GemmProblem::epi).
@@ -425,6 +431,19 @@ struct SplitSumParams {
   long long n4[kMaxModels];      // float4s of out_m
 };
 cudaError_t launch_split_sum(const SplitSumParams& p, cudaStream_t s);
+// logp = z_y / tau - lse, lse = logsumexp(z / tau), from the partial states.
+struct LogpMergeParams {
+  const float* part;             // [nparts][kLogpFields][M][T]
+  int nparts, M;
+  long long T, V;
+  float Ltau, inv_tau;
+  const int* y;
+  float *logp, *lse;             // [M][T]
+  int* status;
+};
+cudaError_t launch_logp_merge(const LogpMergeParams& p, cudaStream_t s);
+// out[m][i] = part[m][i] rounded to bf16, n4[m] float4s each (SplitSumParams::out as bf16).
+cudaError_t launch_to_bf16(const SplitSumParams& p, cudaStream_t s);
 cudaError_t launch_count(const int* y, long long T, long long V, float* inv_n, int* status,
                          cudaStream_t s);
 
@@ -433,6 +452,73 @@ cudaError_t launch_eval_merge(const EvalMergeParams& p, int blocks, cudaStream_t
 cudaError_t launch_eval_final(const double* block_acc, const long long* block_cnt, int nblocks,
                               int M, float* pair_stats, cudaStream_t s);
 cudaError_t setup_eval_kernels();
+
+// ------------------------------------------------------------------ layer norm
+struct NormParams {
+  long long T;
+  int d;
+  float eps;
+  const void *x, *gain, *bias;   // gain and bias may be null
+  void* y;                       // forward
+  float *mean, *rstd;            // [T]: written by the forward (may be null), read by the backward
+  const void* dy;                // backward
+  void* dx;
+  float *dgain, *dbias;          // [d] or null
+  float* part;                   // [splits][2][d]: shares of dgain and dbias
+  int splits;
+  int sms;
+};
+int norm_splits(long long T, int d, int sms);  // shares of the column sums
+cudaError_t launch_norm_fwd(const NormParams& p, bool fp32, cudaStream_t s);
+cudaError_t launch_norm_bwd(const NormParams& p, bool fp32, cudaStream_t s);
+
+// ------------------------------------------------------------------ clipped policy loss
+constexpr int kPolicyTokens = 2048;  // tokens per block
+enum PolicyAgg { kAggToken = 0, kAggSeq = 1, kAggSum = 2 };
+struct PolicyParams {
+  long long T, V;
+  int M, B, agg, adv_per_seq;
+  float beta, grad_scale;
+  float w[kMaxModels];
+  float high[2], low[2];         // log(1 + clip_high), log(1 - clip_low) as two fp32 words
+  float ratio_high, ratio_low;   // 1 + clip_high, 1 - clip_low
+  const float *logp, *old_logp, *ref_logp;  // [M][T], ref_logp may be null
+  const float* adv;              // [B] or [T]
+  const int* y;                  // [T]
+  const int* seq_start;          // [B + 1] or null
+  float *loss, *tok_loss, *diag, *dlogp;    // [1], [M][T], [3][M], [M][T]; all but loss may be null
+  int* chunk_count;              // [chunks]: counted tokens of each count_tokens tokens
+  int chunks;                    // 0: no counts needed, or one block has all tokens
+  long long count_tokens;
+  double* part;                  // [blocks][M][3]
+  int* status;
+};
+inline int policy_blocks(long long T) { return static_cast<int>((T + kPolicyTokens - 1) / kPolicyTokens); }
+cudaError_t launch_policy(const PolicyParams& p, cudaStream_t s);
+
+// ------------------------------------------------------------------ gradient norm and clipping
+constexpr int kClipChunk = 8192;     // values of a tensor per block and turn
+constexpr int kClipTable = 1024;     // tensors of a launch (24 KB of kernel parameters)
+struct ClipTensor {
+  void* g;
+  long long numel;
+  int chunk0;                    // first chunk of this tensor in the launch's numbering
+  short head;                    // values before the first 16-byte boundary
+  short fp32;
+};
+template <int kCap>
+struct ClipParams {
+  int n, chunks;
+  int part0, nparts;             // this launch's first share of the norm, all launches' shares
+  float max_norm;
+  double* part;
+  float* stats;                  // [2] or null (only one launch writes it)
+  ClipTensor t[kCap];
+};
+template <int kCap>
+cudaError_t launch_clip_norm(const ClipParams<kCap>& p, int grid, cudaStream_t s);
+template <int kCap>
+cudaError_t launch_clip_scale(const ClipParams<kCap>& p, int grid, cudaStream_t s);
 
 // One-time per-device kernel attribute setup (dynamic shared memory limits).
 cudaError_t setup_head_kernels();
