@@ -75,6 +75,8 @@ int device_state(DeviceState** out) {
       s.err = fail(MLS_ERR_CUDA, "logits kernel attributes", e);
     } else if ((e = setup_junction_kernels()) != cudaSuccess) {
       s.err = fail(MLS_ERR_CUDA, "junction kernel attributes", e);
+    } else if ((e = setup_norm_kernels()) != cudaSuccess) {
+      s.err = fail(MLS_ERR_CUDA, "norm kernel attributes", e);
     } else if ((s.gemm_pairs = gemm_max_active_pairs()) <= 0) {
       s.err = fail(MLS_ERR_CUDA, "gemm cluster occupancy");
     } else if ((s.head_pairs = head_max_active_pairs()) <= 0) {
@@ -1283,7 +1285,8 @@ extern "C" int mls_layer_norm_fwd(int64_t T, int32_t d, int32_t in_dtype, float 
 
 extern "C" size_t mls_layer_norm_workspace_size(int64_t T, int32_t d) {
   if (T < 0 || T > INT_MAX || d < 1) return 0;
-  return align_up(sizeof(float) * 2 * static_cast<size_t>(d) * norm_splits(T, d, current_sms()));
+  // fp32 rows take more warps each, so at least as many blocks as bf16 ones
+  return align_up(sizeof(float) * 2 * static_cast<size_t>(d) * norm_splits(T, d, true, current_sms()));
 }
 
 extern "C" int mls_layer_norm_bwd(int64_t T, int32_t d, int32_t in_dtype, const void* x,
@@ -1317,7 +1320,7 @@ extern "C" int mls_layer_norm_bwd(int64_t T, int32_t d, int32_t in_dtype, const 
   np.dgain = dgain;
   np.dbias = dbias;
   np.sms = dev->sms;
-  np.splits = norm_splits(T, d, dev->sms);
+  np.splits = norm_splits(T, d, in_dtype == MLS_FP32, dev->sms);
   if (dgain || dbias) {
     if (!ws || (reinterpret_cast<uintptr_t>(ws) % kAlign) != 0 ||
         ws_bytes < align_up(sizeof(float) * 2 * static_cast<size_t>(d) * np.splits))
@@ -1355,7 +1358,7 @@ PolicyPlan policy_plan(const mls_policy_problem* p) {
   pl.count_tokens = kPolicyTokens * (blocks > 4096 ? ceil_div(blocks, 4096) : 1);
   if (blocks > 1 && p->agg != MLS_AGG_SUM) pl.chunks = static_cast<int>(ceil_div(p->T, pl.count_tokens));
   pl.off_part = align_up(sizeof(int) * static_cast<size_t>(pl.chunks));
-  pl.total = align_up(pl.off_part + sizeof(double) * 3 * p->M * static_cast<size_t>(blocks));
+  pl.total = align_up(pl.off_part + sizeof(float) * 3 * p->M * static_cast<size_t>(blocks));
   return pl;
 }
 
@@ -1428,7 +1431,7 @@ extern "C" int mls_policy_loss(const mls_policy_problem* p, const float* logp, c
   pp.chunks = pl.chunks;
   pp.count_tokens = pl.count_tokens;
   pp.chunk_count = static_cast<int*>(ws);
-  pp.part = reinterpret_cast<double*>(static_cast<char*>(ws) + pl.off_part);
+  pp.part = reinterpret_cast<float*>(static_cast<char*>(ws) + pl.off_part);
   pp.status = dev->status;
   return timed("policy", s, [&] { return launch_policy(pp, s); });
 }
@@ -1512,7 +1515,8 @@ extern "C" int mls_grad_clip(int32_t n, void* const* g, const int64_t* numel, co
         const long long c = ceil_div(numel[i] - head, kClipChunk);
         cp.chunks += static_cast<int>(c > 0 ? c : 1);
       }
-      const int most = dev->sms * 6 < kClipBlocks ? dev->sms * 6 : kClipBlocks;
+      const int resident = dev->sms * (pass == 0 ? kClipNormBlocks : kClipScaleBlocks);
+      const int most = resident < kClipBlocks ? resident : kClipBlocks;
       const int grid = cp.chunks < 1 ? 1 : cp.chunks < most ? cp.chunks : most;
       if (pass == 0) {
         cp.part0 = nparts;

@@ -3,7 +3,7 @@
 // A call's tensors come as a table in the kernels' parameters (kClipTable of them
 // a launch), cut into chunks of kClipChunk values that persistent blocks take in
 // turn.  Squares are summed in fp32 over the 32 values that a thread holds of a
-// chunk and in 64 bits from there on.  Where such a sum leaves the range in which
+// chunk, in two fp32 words (Pair) over its chunks, and in 64 bits from there on.  Where such a sum leaves the range in which
 // fp32 squares are exact to rounding (a square that overflowed, or squares so
 // small that some were flushed) those 32 values are summed again in 64 bits, so
 // the norm is right from the smallest to the largest representable gradient.
@@ -17,19 +17,6 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// Sum over the block in thread order of a butterfly; valid in every thread.
-__device__ __forceinline__ double block_sum(double v, double* sh) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
-  __syncthreads();
-  double s = 0.0;
-#pragma unroll
-  for (int i = 0; i < kThreads / 32; ++i) s += sh[i];
-  return s;
-}
-
 // The tensor of chunk c: the last one whose first chunk is not past c.
 template <int kCap>
 __device__ __forceinline__ int tensor_of(const ClipParams<kCap>& p, int c) {
@@ -42,70 +29,105 @@ __device__ __forceinline__ int tensor_of(const ClipParams<kCap>& p, int c) {
   return lo;
 }
 
-// Sum of the squares of a thread's values of a chunk, see above.
+// What a thread has summed: squares in two fp32 words, and what does not fit them.
+struct Squares {
+  Pair small;
+  double rest;
+};
+
+// Adds the squares of a thread's values of a chunk, see above.
 template <int n>
-__device__ __forceinline__ double exact_squares(const float (&f)[n]) {
+__device__ __forceinline__ void add_squares(Squares& acc, const float (&f)[n]) {
   float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < n; ++i) s[i & 3] = fmaf(f[i], f[i], s[i & 3]);
   const float a = (s[0] + s[1]) + (s[2] + s[3]);
-  if (a >= 0x1p-80f && a <= 0x1p100f) return static_cast<double>(a);
+  if (a >= 0x1p-80f && a <= 0x1p90f) {
+    pair_add(acc.small, a, 0.f);
+    return;
+  }
   float most = 0.f;
 #pragma unroll
   for (int i = 0; i < n; ++i) most = fmaxf(most, fabsf(f[i]));
-  if (a == 0.f && most == 0.f) return 0.0;  // zeros: a frozen tensor, rows of unused tokens
+  if (a == 0.f && most == 0.f) return;  // zeros: a frozen tensor, rows of unused tokens
   double d = 0.0;
 #pragma unroll
   for (int i = 0; i < n; ++i) d = fma(static_cast<double>(f[i]), static_cast<double>(f[i]), d);
-  return d;
+  acc.rest += d;
 }
 
 // Chunk `local` of a tensor: whole vectors of 16 bytes where there are any, single
 // values at its end.  A tensor that starts off a 16-byte boundary has `head`
 // values before its first vector, which go with chunk 0.
 template <typename E>
-__device__ __forceinline__ double chunk_squares(const E* g, const ClipTensor& t, int local) {
+__device__ __forceinline__ void chunk_squares(const E* g, const ClipTensor& t, int local, Squares& acc) {
   constexpr int N = Vec<E>::N, kV = kClipChunk / kThreads / N;
   const long long first = t.head + static_cast<long long>(local) * kClipChunk;
-  double acc = 0.0;
   float f[kV * N];
+  if (first + kClipChunk <= t.numel) {  // every load issued before the first is used
+    uint4 u[kV];
 #pragma unroll
-  for (int v = 0; v < kV; ++v) {
-    const long long e = first + (v * kThreads + static_cast<int>(threadIdx.x)) * N;
-    float w[N];
+    for (int v = 0; v < kV; ++v) u[v] = ld16(g + first + (v * kThreads + static_cast<int>(threadIdx.x)) * N);
 #pragma unroll
-    for (int i = 0; i < N; ++i) w[i] = 0.f;
-    if (e + N <= t.numel) {
-      Vec<E>::unpack(ld16(g + e), w);
-    } else {
+    for (int v = 0; v < kV; ++v) {
+      float w[N];
+      Vec<E>::unpack(u[v], w);
 #pragma unroll
-      for (int i = 0; i < N; ++i)
-        if (e + i < t.numel) w[i] = static_cast<float>(g[e + i]);
+      for (int i = 0; i < N; ++i) f[v * N + i] = w[i];
     }
+  } else {
 #pragma unroll
-    for (int i = 0; i < N; ++i) f[v * N + i] = w[i];
+    for (int v = 0; v < kV; ++v) {
+      const long long e = first + (v * kThreads + static_cast<int>(threadIdx.x)) * N;
+      float w[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) w[i] = 0.f;
+      if (e + N <= t.numel) {
+        Vec<E>::unpack(ld16(g + e), w);
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          if (e + i < t.numel) w[i] = static_cast<float>(g[e + i]);
+      }
+#pragma unroll
+      for (int i = 0; i < N; ++i) f[v * N + i] = w[i];
+    }
   }
-  acc = exact_squares(f);
+  add_squares(acc, f);
   if (local == 0 && static_cast<int>(threadIdx.x) < t.head) {
-    const double h = static_cast<double>(static_cast<float>(g[threadIdx.x]));
-    acc = fma(h, h, acc);
+    const float h[1] = {static_cast<float>(g[threadIdx.x])};
+    add_squares(acc, h);
   }
-  return acc;
 }
 
 template <int kCap>
-__global__ void __launch_bounds__(kThreads) clip_norm_kernel(const __grid_constant__ ClipParams<kCap> p) {
-  __shared__ double sh[kThreads / 32];
-  double acc = 0.0;
+__global__ void __launch_bounds__(kThreads, kClipNormBlocks) clip_norm_kernel(const __grid_constant__ ClipParams<kCap> p) {
+  chain_trigger();
+  __shared__ Pair sh[kThreads / 32];
+  __shared__ double shr[kThreads / 32];
+  Squares acc = {{0.f, 0.f}, 0.0};
   for (int c = blockIdx.x; c < p.chunks; c += gridDim.x) {
     const ClipTensor& t = p.t[tensor_of(p, c)];
     if (t.fp32)
-      acc += chunk_squares(static_cast<const float*>(t.g), t, c - t.chunk0);
+      chunk_squares(static_cast<const float*>(t.g), t, c - t.chunk0, acc);
     else
-      acc += chunk_squares(static_cast<const __nv_bfloat16*>(t.g), t, c - t.chunk0);
+      chunk_squares(static_cast<const __nv_bfloat16*>(t.g), t, c - t.chunk0, acc);
   }
-  const double s = block_sum(acc, sh);
-  if (threadIdx.x == 0) p.part[p.part0 + blockIdx.x] = s;
+  const Pair s = warp_sum_pair(acc.small);
+  double r = acc.rest;
+  if (__any_sync(0xffffffffu, r != 0.0))  // also where it is NaN
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) r += __shfl_down_sync(0xffffffffu, r, o);
+  if ((threadIdx.x & 31) == 0) {
+    sh[threadIdx.x >> 5] = s;
+    shr[threadIdx.x >> 5] = r;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double total = 0.0;
+    for (int i = 0; i < kThreads / 32; ++i) total += pair_value(sh[i]) + shr[i];
+    p.part[p.part0 + blockIdx.x] = total;
+  }
 }
 
 template <typename E>
@@ -137,20 +159,32 @@ __device__ __forceinline__ void chunk_scale(E* g, const ClipTensor& t, int local
     g[threadIdx.x] = static_cast<E>(static_cast<float>(g[threadIdx.x]) * coef);
 }
 
-// Every block adds all shares of the norm itself, in the same order.
+// Every block adds all shares of the norm itself, in the same order: its first warp,
+// since 64-bit additions of all warps would only queue for the SM's two units.
 template <int kCap>
-__global__ void __launch_bounds__(kThreads) clip_scale_kernel(const __grid_constant__ ClipParams<kCap> p) {
-  __shared__ double sh[kThreads / 32];
-  double a = 0.0;
-  for (int i = threadIdx.x; i < p.nparts; i += kThreads) a += p.part[i];
-  const double norm = sqrt(block_sum(a, sh));
-  const double ratio = static_cast<double>(p.max_norm) / (norm + 1e-6);
-  // NaN stays (every gradient becomes NaN); an infinite norm gives 0, as the formula says
-  const float coef = isinf(p.max_norm) || ratio >= 1.0 ? 1.f : static_cast<float>(ratio);
-  if (p.stats && blockIdx.x == 0 && threadIdx.x == 0) {
-    p.stats[0] = static_cast<float>(norm);
-    p.stats[1] = coef;
+__global__ void __launch_bounds__(kThreads, kClipScaleBlocks) clip_scale_kernel(const __grid_constant__ ClipParams<kCap> p) {
+  __shared__ float sh_coef;
+  chain_trigger();
+  chain_wait();
+  if (threadIdx.x < 32) {
+    double a = 0.0;
+#pragma unroll 8
+    for (int i = threadIdx.x; i < p.nparts; i += 32) a += p.part[i];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) a += __shfl_down_sync(0xffffffffu, a, o);
+    if (threadIdx.x == 0) {
+      const double norm = sqrt(a), ratio = static_cast<double>(p.max_norm) / (norm + 1e-6);
+      // NaN stays (every gradient becomes NaN); an infinite norm gives 0, as the formula says
+      const float c = isinf(p.max_norm) || ratio >= 1.0 ? 1.f : static_cast<float>(ratio);
+      sh_coef = c;
+      if (p.stats && blockIdx.x == 0) {
+        p.stats[0] = static_cast<float>(norm);
+        p.stats[1] = c;
+      }
+    }
   }
+  __syncthreads();
+  const float coef = sh_coef;
   if (coef == 1.f) return;  // nothing to change
   for (int i = blockIdx.x; i < p.chunks; i += gridDim.x) {
     const int c = p.chunks - 1 - i;  // the values read last are the likeliest in L2
@@ -171,8 +205,7 @@ cudaError_t launch_clip_norm(const ClipParams<kCap>& p, int grid, cudaStream_t s
 }
 template <int kCap>
 cudaError_t launch_clip_scale(const ClipParams<kCap>& p, int grid, cudaStream_t s) {
-  clip_scale_kernel<kCap><<<grid, kThreads, 0, s>>>(p);
-  return cudaGetLastError();
+  return launch_chained(clip_scale_kernel<kCap>, dim3(grid), dim3(kThreads), 0, s, p);
 }
 template cudaError_t launch_clip_norm(const ClipParams<kClipTable>&, int, cudaStream_t);
 template cudaError_t launch_clip_scale(const ClipParams<kClipTable>&, int, cudaStream_t);

@@ -468,12 +468,13 @@ struct NormParams {
   int splits;
   int sms;
 };
-int norm_splits(long long T, int d, int sms);  // shares of the column sums
+int norm_splits(long long T, int d, bool fp32, int sms);  // shares of the column sums
+cudaError_t setup_norm_kernels();
 cudaError_t launch_norm_fwd(const NormParams& p, bool fp32, cudaStream_t s);
 cudaError_t launch_norm_bwd(const NormParams& p, bool fp32, cudaStream_t s);
 
 // ------------------------------------------------------------------ clipped policy loss
-constexpr int kPolicyTokens = 2048;  // tokens per block
+constexpr int kPolicyTokens = 1024;  // tokens per block
 enum PolicyAgg { kAggToken = 0, kAggSeq = 1, kAggSum = 2 };
 struct PolicyParams {
   long long T, V;
@@ -487,10 +488,11 @@ struct PolicyParams {
   const int* y;                  // [T]
   const int* seq_start;          // [B + 1] or null
   float *loss, *tok_loss, *diag, *dlogp;    // [1], [M][T], [3][M], [M][T]; all but loss may be null
-  int* chunk_count;              // [chunks]: counted tokens of each count_tokens tokens
+  int* chunk_count;              // [chunks, up to a multiple of 4]: counted tokens of each
+                                 //   count_tokens tokens
   int chunks;                    // 0: no counts needed, or one block has all tokens
   long long count_tokens;
-  double* part;                  // [blocks][M][3]
+  float* part;                   // [M][3][blocks]
   int* status;
 };
 inline int policy_blocks(long long T) { return static_cast<int>((T + kPolicyTokens - 1) / kPolicyTokens); }
@@ -499,6 +501,8 @@ cudaError_t launch_policy(const PolicyParams& p, cudaStream_t s);
 // ------------------------------------------------------------------ gradient norm and clipping
 constexpr int kClipChunk = 8192;     // values of a tensor per block and turn
 constexpr int kClipTable = 1024;     // tensors of a launch (24 KB of kernel parameters)
+// Blocks of an SM (all resident, so the last ones do not wait for a second turn).
+constexpr int kClipNormBlocks = 5, kClipScaleBlocks = 4;
 struct ClipTensor {
   void* g;
   long long numel;

@@ -5,10 +5,17 @@
 // Backward with g = dL/dy, h = g gain:
 //   dL/dx = r (h - mean h - xh mean(h xh))
 //   dL/dgain = sum over tokens of g xh,  dL/dbias = sum over tokens of g
-// One warp owns a token; the variance is the mean of the squared deviations from
-// the mean itself, so that a mean far from 0 costs no digits.  The column sums
-// are taken in two steps: a block's rows into its own copy of the two rows of
-// sums, then the copies, in order, so results do not depend on timing.
+// Bound by HBM: forward x and y, backward x, g and dx, each moved once.  The variance
+// is the mean of the squared deviations from the mean itself, so that a mean far
+// from 0 costs no digits.
+//   forward   a row's 16-byte vectors, at most 4 a lane, stay packed in the registers
+//             of its 1 to 16 warps;
+//   backward  persistent blocks of 16 warps, W of them to a row, which load the next
+//             row before they work on this one and keep their columns' sums of g xh
+//             and g in registers (in shared memory for the widest rows) over all rows
+//             of the block.  The blocks' sums are added in order by a second kernel,
+//             so results do not depend on timing;
+//   wider rows are read again from L2 instead, one warp a row.
 #include "mls_device.cuh"
 #include "mls_kernels.h"
 #include "mls_vec.cuh"
@@ -16,10 +23,301 @@
 namespace mls {
 namespace {
 
+__device__ __forceinline__ void group_sync(int id, int threads) {
+  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+
+// ------------------------------------------------------------------ forward
+// V vectors a lane, W warps a row: vector j of warp w's lane l is number (j W + w) 32 + l.
+template <int W>
+constexpr int kFwdRows = W < 4 ? 4 / W : 1;
+
+template <int W>
+__device__ __forceinline__ float row_sum(float v, float* sh, int id, int w) {
+  v = warp_sum(v);
+  if constexpr (W > 1) {
+    if ((threadIdx.x & 31) == 0) sh[w] = v;
+    group_sync(id, 32 * W);
+    v = 0.f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) v += sh[i];
+  }
+  return v;
+}
+
+template <typename E, int V, int W>
+__global__ void __launch_bounds__(32 * W * kFwdRows<W>) norm_fwd_kernel(const NormParams p) {
+  constexpr int N = Vec<E>::N;
+  __shared__ float sh[kFwdRows<W>][2][W];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = warp / W, w = warp % W;
+  const long long t = static_cast<long long>(blockIdx.x) * kFwdRows<W> + group;
+  if (t >= p.T) return;  // whole groups
+  const E* x = static_cast<const E*>(p.x) + t * p.d;
+  E* y = static_cast<E*>(p.y) + t * p.d;
+  uint4 u[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const int k = ((j * W + w) * 32 + lane) * N;
+    u[j] = k < p.d ? ld16(x + k) : make_uint4(0u, 0u, 0u, 0u);
+  }
+  const float inv_d = 1.0f / static_cast<float>(p.d);
+  float s = 0.f, q = 0.f;
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    float f[N];
+    Vec<E>::unpack(u[j], f);
+#pragma unroll
+    for (int i = 0; i < N; ++i) s += f[i];
+  }
+  const float mu = row_sum<W>(s, sh[group][0], 1 + group, w) * inv_d;
+  keep_packed(u);
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    if (((j * W + w) * 32 + lane) * N < p.d) {
+      float f[N];
+      Vec<E>::unpack(u[j], f);
+#pragma unroll
+      for (int i = 0; i < N; ++i) q = fmaf(f[i] - mu, f[i] - mu, q);
+    }
+  }
+  const float r = 1.0f / sqrtf(row_sum<W>(q, sh[group][1], 1 + group, w) * inv_d + p.eps);
+  keep_packed(u);
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const int k = ((j * W + w) * 32 + lane) * N;
+    if (k < p.d) {
+      float f[N], g[N], b[N];
+      Vec<E>::unpack(u[j], f);
+      if (p.gain) Vec<E>::unpack(ld16(static_cast<const E*>(p.gain) + k), g);
+      if (p.bias) Vec<E>::unpack(ld16(static_cast<const E*>(p.bias) + k), b);
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        f[i] = fmaf((f[i] - mu) * r, p.gain ? g[i] : 1.f, p.bias ? b[i] : 0.f);
+      st16(y + k, Vec<E>::pack(f));
+    }
+  }
+  if (w == 0 && lane == 0 && p.mean) {
+    p.mean[t] = mu;
+    p.rstd[t] = r;
+  }
+}
+
+// ------------------------------------------------------------------ backward
+constexpr int kBwdWarps = 16;
+
+// One row's vectors of a lane, and the row's statistics.
+template <int V>
+struct BwdRow {
+  uint4 x[V], g[V];
+  float mu, r;
+};
+
+template <typename E, int V, int W>
+__device__ __forceinline__ void load_row(const NormParams& p, long long t, int w, int lane, BwdRow<V>& b) {
+  constexpr int N = Vec<E>::N;
+  if (t >= p.T) return;
+  const E* x = static_cast<const E*>(p.x) + t * p.d;
+  const E* g = static_cast<const E*>(p.dy) + t * p.d;
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const int k = ((j * W + w) * 32 + lane) * N;
+    if (k < p.d) {
+      b.x[j] = ld16(x + k);
+      b.g[j] = ld16(g + k);
+    }
+  }
+  b.mu = p.mean[t];
+  b.r = p.rstd[t];
+}
+
+// kShared: the columns' sums lie in shared memory and the gain is read at each row;
+// else both stay in registers.
+template <typename E, int V, int W, bool kShared>
+__global__ void __launch_bounds__(32 * kBwdWarps, 1) norm_bwd_kernel(const NormParams p) {
+  constexpr int N = Vec<E>::N, kGroups = kBwdWarps / W;
+  extern __shared__ __align__(16) float sums[];  // [2][d]
+  __shared__ float2 sh[2][kBwdWarps];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = warp / W, w = warp % W;
+  const E* gain = static_cast<const E*>(p.gain);
+  const float inv_d = 1.0f / static_cast<float>(p.d);
+  constexpr int kR = kShared ? 1 : V;
+  uint4 gv[kR];
+  float dg[kR][N], db[kR][N];
+#pragma unroll
+  for (int j = 0; j < kR; ++j)
+#pragma unroll
+    for (int i = 0; i < N; ++i) dg[j][i] = db[j][i] = 0.f;
+  if constexpr (kShared) {
+    for (int k = threadIdx.x; k < 2 * p.d; k += 32 * kBwdWarps) sums[k] = 0.f;
+    __syncthreads();
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const int k = ((j * W + w) * 32 + lane) * N;
+      if (gain && k < p.d) gv[j] = ld16(gain + k);
+    }
+  }
+
+  const long long step = static_cast<long long>(gridDim.x) * kGroups;
+  long long t = static_cast<long long>(blockIdx.x) * kGroups + group;
+  BwdRow<V> next;
+  load_row<E, V, W>(p, t, w, lane, next);
+  for (int it = 0; t < p.T; t += step, it ^= 1) {
+    BwdRow<V> cur = next;
+    load_row<E, V, W>(p, t + step, w, lane, next);
+    float a = 0.f, b = 0.f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const int k = ((j * W + w) * 32 + lane) * N;
+      if (k < p.d) {
+        float f[N], g[N], gn[N];
+        Vec<E>::unpack(cur.x[j], f);
+        Vec<E>::unpack(cur.g[j], g);
+        if (gain) Vec<E>::unpack(kShared ? ld16(gain + k) : gv[kShared ? 0 : j], gn);
+        float sg[N], sb[N];
+        if constexpr (kShared) {
+#pragma unroll
+          for (int i = 0; i < N; i += 4) {
+            *reinterpret_cast<float4*>(sg + i) = *reinterpret_cast<const float4*>(sums + k + i);
+            *reinterpret_cast<float4*>(sb + i) = *reinterpret_cast<const float4*>(sums + p.d + k + i);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float xh = (f[i] - cur.mu) * cur.r;
+          const float h = gain ? g[i] * gn[i] : g[i];
+          a += h;
+          b = fmaf(h, xh, b);
+          if constexpr (kShared) {
+            sg[i] = fmaf(g[i], xh, sg[i]);
+            sb[i] += g[i];
+          } else {
+            dg[j][i] = fmaf(g[i], xh, dg[j][i]);
+            db[j][i] += g[i];
+          }
+        }
+        if constexpr (kShared) {
+#pragma unroll
+          for (int i = 0; i < N; i += 4) {
+            *reinterpret_cast<float4*>(sums + k + i) = *reinterpret_cast<const float4*>(sg + i);
+            *reinterpret_cast<float4*>(sums + p.d + k + i) = *reinterpret_cast<const float4*>(sb + i);
+          }
+        }
+      }
+    }
+    a = warp_sum(a);
+    b = warp_sum(b);
+    if constexpr (W > 1) {
+      // One barrier a row: the next row's words are the other half, and a warp comes back
+      // to this one only past that row's barrier, when all have read it.
+      if (lane == 0) sh[it][warp] = make_float2(a, b);
+      group_sync(1 + group, 32 * W);
+      a = b = 0.f;
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        const float2 v = sh[it][group * W + i];
+        a += v.x;
+        b += v.y;
+      }
+    }
+    a *= inv_d;
+    b *= inv_d;
+    keep_packed(cur.x);
+    keep_packed(cur.g);
+    E* dx = static_cast<E*>(p.dx) + t * p.d;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const int k = ((j * W + w) * 32 + lane) * N;
+      if (k < p.d) {
+        float f[N], g[N], gn[N];
+        Vec<E>::unpack(cur.x[j], f);
+        Vec<E>::unpack(cur.g[j], g);
+        if (gain) Vec<E>::unpack(kShared ? ld16(gain + k) : gv[kShared ? 0 : j], gn);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float xh = (f[i] - cur.mu) * cur.r, h = gain ? g[i] * gn[i] : g[i];
+          f[i] = cur.r * ((h - a) - xh * b);
+        }
+        st16(dx + k, Vec<E>::pack(f));
+      }
+    }
+  }
+  if (!p.part) return;
+
+  // ---- the block's sums: its groups' one after the other
+  float* out = p.part + 2ll * p.d * blockIdx.x;
+  if constexpr (kShared) {
+    __syncthreads();
+    for (int k = threadIdx.x; k < 2 * p.d; k += 32 * kBwdWarps) out[k] = sums[k];
+  } else {
+    for (int q = 0; q < kGroups; ++q) {
+      if (group == q) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          const int k = ((j * W + w) * 32 + lane) * N;
+          if (k < p.d) {
+            float* s = q + 1 < kGroups ? sums : out;  // the last group writes the block's share
+#pragma unroll
+            for (int i = 0; i < N; i += 4) {
+              float4 g = make_float4(dg[j][i], dg[j][i + 1], dg[j][i + 2], dg[j][i + 3]);
+              float4 b = make_float4(db[j][i], db[j][i + 1], db[j][i + 2], db[j][i + 3]);
+              if (q > 0) {
+                const float4 pg = *reinterpret_cast<const float4*>(sums + k + i);
+                const float4 pb = *reinterpret_cast<const float4*>(sums + p.d + k + i);
+                g = make_float4(g.x + pg.x, g.y + pg.y, g.z + pg.z, g.w + pg.w);
+                b = make_float4(b.x + pb.x, b.y + pb.y, b.z + pb.z, b.w + pb.w);
+              }
+              *reinterpret_cast<float4*>(s + k + i) = g;
+              *reinterpret_cast<float4*>(s + p.d + k + i) = b;
+            }
+          }
+        }
+      }
+      __syncthreads();
+    }
+  }
+}
+
+// Blocks' shares [splits][2][d] -> dgain, dbias.  A block owns 32 vectors of four columns;
+// each of its 8 warps adds every eighth share, then the first adds the warps'.
+constexpr int kColWarps = 8;
+
+__global__ void __launch_bounds__(32 * kColWarps) norm_cols_sum_kernel(const NormParams p) {
+  __shared__ float4 sh[kColWarps][32];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int c = (blockIdx.x * 32 + lane) * 4;
+  chain_trigger();
+  chain_wait();
+  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (c < 2 * p.d) {
+    const float* part = p.part + c;
+#pragma unroll 8
+    for (int s = warp; s < p.splits; s += kColWarps) {
+      const float4 b = *reinterpret_cast<const float4*>(part + 2ll * p.d * s);
+      a = make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w);
+    }
+  }
+  sh[warp][lane] = a;
+  __syncthreads();
+  if (warp > 0 || c >= 2 * p.d) return;
+  for (int i = 1; i < kColWarps; ++i) {
+    const float4 b = sh[i][lane];
+    a = make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w);
+  }
+  float* out = c < p.d ? p.dgain : p.dbias;  // d is a multiple of 4: a vector lies in one of them
+  if (!out) return;
+  const int k = c < p.d ? c : c - p.d;
+  out[k] = a.x;
+  out[k + 1] = a.y;
+  out[k + 2] = a.z;
+  out[k + 3] = a.w;
+}
+
+// ------------------------------------------------------------------ wide rows
 constexpr int kWarps = 4;
 
 template <typename E>
-__global__ void __launch_bounds__(32 * kWarps) norm_fwd_kernel(const NormParams p) {
+__global__ void __launch_bounds__(32 * kWarps) norm_fwd_wide_kernel(const NormParams p) {
   constexpr int N = Vec<E>::N;
   const long long t = static_cast<long long>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31;
@@ -61,7 +359,7 @@ __global__ void __launch_bounds__(32 * kWarps) norm_fwd_kernel(const NormParams 
 }
 
 template <typename E>
-__global__ void __launch_bounds__(32 * kWarps) norm_bwd_kernel(const NormParams p) {
+__global__ void __launch_bounds__(32 * kWarps) norm_bwd_wide_kernel(const NormParams p) {
   constexpr int N = Vec<E>::N;
   const long long t = static_cast<long long>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31;
@@ -102,7 +400,7 @@ __global__ void __launch_bounds__(32 * kWarps) norm_bwd_kernel(const NormParams 
 constexpr int kColThreads = 128;
 
 template <typename E>
-__global__ void __launch_bounds__(kColThreads) norm_cols_kernel(const NormParams p) {
+__global__ void __launch_bounds__(kColThreads) norm_cols_wide_kernel(const NormParams p) {
   const int c = blockIdx.x * kColThreads + threadIdx.x;
   if (c >= p.d) return;
   const E* x = static_cast<const E*>(p.x);
@@ -118,23 +416,63 @@ __global__ void __launch_bounds__(kColThreads) norm_cols_kernel(const NormParams
   out[p.d] = db;
 }
 
-__global__ void __launch_bounds__(kColThreads) norm_cols_sum_kernel(const NormParams p) {
-  const int c = blockIdx.x * kColThreads + threadIdx.x;
-  if (c >= p.d) return;
-  float dg = 0.f, db = 0.f;
-  for (int s = 0; s < p.splits; ++s) {
-    dg += p.part[2ll * p.d * s + c];
-    db += p.part[2ll * p.d * s + p.d + c];
-  }
-  if (p.dgain) p.dgain[c] = dg;
-  if (p.dbias) p.dbias[c] = db;
+unsigned blocks_of(long long n, int per) { return static_cast<unsigned>((n + per - 1) / per); }
+
+// Widest rows of the cached backward: 128 KB of sums in shared memory.
+constexpr int kBwdSharedMost = 16384;
+template <typename E, int V, int W>
+cudaError_t fwd(const NormParams& p, cudaStream_t s) {
+  norm_fwd_kernel<E, V, W><<<blocks_of(p.T, kFwdRows<W>), 32 * W * kFwdRows<W>, 0, s>>>(p);
+  return cudaGetLastError();
 }
 
-unsigned blocks_of(long long n, int per) { return static_cast<unsigned>((n + per - 1) / per); }
+template <typename E>
+cudaError_t fwd_any(const NormParams& p, cudaStream_t s) {
+  const int v = (p.d + 32 * Vec<E>::N - 1) / (32 * Vec<E>::N);  // vectors a lane of one warp
+  if (v <= 1) return fwd<E, 1, 1>(p, s);
+  if (v <= 2) return fwd<E, 2, 1>(p, s);
+  if (v <= 4) return fwd<E, 4, 1>(p, s);
+  if (v <= 8) return fwd<E, 4, 2>(p, s);
+  if (v <= 16) return fwd<E, 4, 4>(p, s);
+  if (v <= 32) return fwd<E, 4, 8>(p, s);
+  if (v <= 64) return fwd<E, 4, 16>(p, s);
+  norm_fwd_wide_kernel<E><<<blocks_of(p.T, kWarps), 32 * kWarps, 0, s>>>(p);
+  return cudaGetLastError();
+}
+
+template <typename E, int V, int W, bool kShared>
+cudaError_t bwd(const NormParams& p, cudaStream_t s) {
+  const size_t smem = kShared || W < kBwdWarps ? sizeof(float) * 2 * p.d : 0;
+  norm_bwd_kernel<E, V, W, kShared><<<p.splits, 32 * kBwdWarps, smem, s>>>(p);
+  return cudaGetLastError();
+}
+
+template <typename E>
+cudaError_t bwd_any(const NormParams& p, cudaStream_t s) {
+  const int v = (p.d + 32 * Vec<E>::N - 1) / (32 * Vec<E>::N);
+  if (v <= 1) return bwd<E, 1, 1, false>(p, s);
+  if (v <= 2) return bwd<E, 2, 1, false>(p, s);
+  if (v <= 4) return bwd<E, 2, 2, false>(p, s);
+  if (v <= 8) return bwd<E, 2, 4, false>(p, s);
+  if (v <= 16) return bwd<E, 2, 8, false>(p, s);
+  if (v <= 32) return bwd<E, 2, 16, false>(p, s);
+  if constexpr (Vec<E>::N == 8) return bwd<E, 4, 16, true>(p, s);  // 16384 values
+  else return v <= 64 ? bwd<E, 4, 16, true>(p, s) : bwd<E, 8, 16, true>(p, s);
+}
+
+bool bwd_cached(int d) { return d <= kBwdSharedMost; }
 
 }  // namespace
 
-int norm_splits(long long T, int d, int sms) {
+// Shares of the column sums: the cached backward's blocks, as many as its groups of
+// warps need for one row each and at most one an SM.
+int norm_splits(long long T, int d, bool fp32, int sms) {
+  if (bwd_cached(d)) {
+    const int v = (d + 32 * (fp32 ? 4 : 8) - 1) / (32 * (fp32 ? 4 : 8));
+    const int groups = kBwdWarps / (v <= 2 ? 1 : v <= 4 ? 2 : v <= 8 ? 4 : v <= 16 ? 8 : 16);
+    const long long blocks = (T + groups - 1) / groups;
+    return blocks < 1 ? 1 : blocks < sms ? static_cast<int>(blocks) : sms;
+  }
   const long long cols = (d + kColThreads - 1) / kColThreads;
   long long s = (8ll * sms + cols - 1) / cols;
   if (s > (T + 15) / 16) s = (T + 15) / 16;
@@ -143,33 +481,47 @@ int norm_splits(long long T, int d, int sms) {
 
 cudaError_t launch_norm_fwd(const NormParams& p, bool fp32, cudaStream_t s) {
   if (p.T <= 0) return cudaSuccess;
-  const unsigned grid = blocks_of(p.T, kWarps);
-  if (fp32)
-    norm_fwd_kernel<float><<<grid, 32 * kWarps, 0, s>>>(p);
-  else
-    norm_fwd_kernel<__nv_bfloat16><<<grid, 32 * kWarps, 0, s>>>(p);
-  return cudaGetLastError();
+  return fp32 ? fwd_any<float>(p, s) : fwd_any<__nv_bfloat16>(p, s);
 }
 
 cudaError_t launch_norm_bwd(const NormParams& p, bool fp32, cudaStream_t s) {
   if (p.T <= 0) return cudaSuccess;
+  const bool sums = p.dgain || p.dbias;
   cudaError_t e;
-  if (p.dgain || p.dbias) {  // before dx, which may take dy's place
+  if (bwd_cached(p.d)) {
+    e = fp32 ? bwd_any<float>(p, s) : bwd_any<__nv_bfloat16>(p, s);
+    if (e != cudaSuccess || !sums) return e;
+  } else if (sums) {  // before dx, which may take dy's place
     const dim3 cols(blocks_of(p.d, kColThreads), p.splits);
     if (fp32)
-      norm_cols_kernel<float><<<cols, kColThreads, 0, s>>>(p);
+      norm_cols_wide_kernel<float><<<cols, kColThreads, 0, s>>>(p);
     else
-      norm_cols_kernel<__nv_bfloat16><<<cols, kColThreads, 0, s>>>(p);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    norm_cols_sum_kernel<<<cols.x, kColThreads, 0, s>>>(p);
+      norm_cols_wide_kernel<__nv_bfloat16><<<cols, kColThreads, 0, s>>>(p);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
   }
+  if (sums && (e = launch_chained(norm_cols_sum_kernel, dim3(blocks_of(2 * p.d, 128)), dim3(32 * kColWarps), 0, s, p)) != cudaSuccess)
+    return e;
+  if (bwd_cached(p.d)) return cudaSuccess;
   const unsigned grid = blocks_of(p.T, kWarps);
   if (fp32)
-    norm_bwd_kernel<float><<<grid, 32 * kWarps, 0, s>>>(p);
+    norm_bwd_wide_kernel<float><<<grid, 32 * kWarps, 0, s>>>(p);
   else
-    norm_bwd_kernel<__nv_bfloat16><<<grid, 32 * kWarps, 0, s>>>(p);
+    norm_bwd_wide_kernel<__nv_bfloat16><<<grid, 32 * kWarps, 0, s>>>(p);
   return cudaGetLastError();
+}
+
+// Dynamic shared memory of the widest backward kernels (past 48 KB with the static part).
+cudaError_t setup_norm_kernels() {
+  cudaError_t e;
+#define MLS_SET(E, V, W, S)                                                                             \
+  e = cudaFuncSetAttribute(norm_bwd_kernel<E, V, W, S>, cudaFuncAttributeMaxDynamicSharedMemorySize,     \
+                           sizeof(float) * 2 * kBwdSharedMost);                                         \
+  if (e != cudaSuccess) return e;
+  MLS_SET(float, 4, 16, true)
+  MLS_SET(float, 8, 16, true)
+  MLS_SET(__nv_bfloat16, 4, 16, true)
+#undef MLS_SET
+  return cudaSuccess;
 }
 
 }  // namespace mls

@@ -34,15 +34,9 @@ __device__ __forceinline__ bool counts(const PolicyParams& p, long long t) {
   return y >= 0 && y < p.V;
 }
 
-__device__ __forceinline__ int warp_sum_int(int v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
-
 // Sum over the block, valid in every thread; sh: kThreads / 32 values.
 __device__ __forceinline__ int block_sum_int(int v, int* sh) {
-  v = warp_sum_int(v);
+  v = __reduce_add_sync(0xffffffffu, v);
   __syncthreads();
   if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
   __syncthreads();
@@ -50,12 +44,6 @@ __device__ __forceinline__ int block_sum_int(int v, int* sh) {
 #pragma unroll
   for (int i = 0; i < kThreads / 32; ++i) s += sh[i];
   return s;
-}
-
-__device__ __forceinline__ double warp_sum_double(double v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
 }
 
 // Offset b of the sequences, within [0, T] whatever the caller's array holds.
@@ -70,6 +58,22 @@ __device__ __forceinline__ int seq_of(const PolicyParams& p, long long t, int lo
     const int mid = lo + ((hi - lo + 1) >> 1);
     if (p.seq_start[mid] <= t) lo = mid;
     else hi = mid - 1;
+  }
+  return lo;
+}
+
+// The same by a whole warp, 32 candidates at a time: the search stands before
+// everything else that the block does.
+__device__ __forceinline__ int seq_of_warp(const PolicyParams& p, long long t, int hi, int lane) {
+  int lo = 0;
+  while (lo < hi) {
+    const int step = (hi - lo + 31) / 32;
+    const long long c = lo + static_cast<long long>(lane + 1) * step;  // candidates lo + step, ...
+    const unsigned below = __ballot_sync(0xffffffffu, c <= hi && p.seq_start[c] <= t);
+    // sorted offsets give a run of ones from lane 0; of others, the run before the first zero
+    const int k = __ffs(~below) == 0 ? 32 : __ffs(~below) - 1;
+    lo += k * step;
+    hi = lo + step - 1 < hi ? lo + step - 1 : hi;
   }
   return lo;
 }
@@ -90,20 +94,25 @@ __device__ int count_range(const PolicyParams& p, long long lo, long long hi, in
   return block_sum_int(n, sh);
 }
 
-__global__ void __launch_bounds__(kThreads) policy_count_kernel(const PolicyParams p) {
+// Counts of the chunks of tokens, and zeros up to a whole vector of four.
+__global__ void __launch_bounds__(kThreads) policy_count_kernel(const __grid_constant__ PolicyParams p) {
   __shared__ int sh[kThreads / 32];
+  chain_trigger();
   const long long t0 = static_cast<long long>(blockIdx.x) * p.count_tokens;
   const long long t1 = t0 + p.count_tokens < p.T ? t0 + p.count_tokens : p.T;
   // tokens outside every sequence do not count
   const long long lo = p.seq_start ? seq_at(p, 0) : 0, hi = p.seq_start ? seq_at(p, p.B) : p.T;
   int n = 0;
+#pragma unroll 4
   for (long long t = t0 + threadIdx.x; t < t1; t += kThreads) n += t >= lo && t < hi && counts(p, t);
   n = block_sum_int(n, sh);
   if (threadIdx.x == 0) p.chunk_count[blockIdx.x] = n;
+  if (blockIdx.x == 0 && threadIdx.x < 4 && p.chunks + threadIdx.x < (p.chunks + 3) / 4 * 4)
+    p.chunk_count[p.chunks + threadIdx.x] = 0;
 }
 
-// e^x - 1 - x.  Below 1/2 its Taylor series (remainder under 2^-29 of it).
-__device__ __forceinline__ float exp_excess(float x) {
+// e^x - 1 - x and e^x - 1.  Below 1/2 the Taylor series (remainder under 2^-29 of it).
+__device__ __forceinline__ void exp_excess(float x, float& excess, float& minus_one) {
   if (fabsf(x) < 0.5f) {
     float s = 1.f / 362880.f;
     s = fmaf(s, x, 1.f / 40320.f);
@@ -113,9 +122,12 @@ __device__ __forceinline__ float exp_excess(float x) {
     s = fmaf(s, x, 1.f / 24.f);
     s = fmaf(s, x, 1.f / 6.f);
     s = fmaf(s, x, 0.5f);
-    return x * x * s;
+    excess = x * x * s;
+    minus_one = x + excess;
+  } else {
+    minus_one = expf(x) - 1.f;
+    excess = minus_one - x;
   }
-  return expf(x) - 1.f - x;
 }
 
 // Sign of (d + e) - (hi + lo) for d + e an exact difference and hi + lo a bound, both
@@ -146,24 +158,67 @@ __device__ __forceinline__ Token policy_token(const PolicyParams& p, float logp,
   k.kl = 0.f;
   if (has_ref) {
     const float x = ref - logp;
-    k.kl = exp_excess(x);
-    if (p.beta != 0.f) k.grad = fmaf(-p.beta, fabsf(x) < 0.5f ? x + k.kl : expf(x) - 1.f, k.grad);
+    float e1;
+    exp_excess(x, k.kl, e1);
+    if (p.beta != 0.f) k.grad = fmaf(-p.beta, e1, k.grad);
   }
   return k;
 }
 
+// v[3 m]: sum of weight P, v[3 m + 1]: of weight K.
+__device__ __forceinline__ float total_loss(const PolicyParams& p, const double* v) {
+  double loss = 0.0;
+  for (int m = 0; m < p.M; ++m)
+    loss += static_cast<double>(p.w[m]) *
+            (p.beta != 0.f ? v[3 * m] + static_cast<double>(p.beta) * v[3 * m + 1] : v[3 * m]);
+  return static_cast<float>(loss);
+}
+
+// One token's three inputs of a sub-model, for kPer tokens of a thread.
+struct Inputs {
+  float logp[kPer], old[kPer], ref[kPer];
+};
+__device__ __forceinline__ void load_inputs(const PolicyParams& p, int m, long long t0, long long t1, Inputs& v) {
+  const long long row = static_cast<long long>(m) * p.T;
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    const long long t = t0 + threadIdx.x + j * kThreads;
+    const bool in = t < t1;
+    v.logp[j] = in ? p.logp[row + t] : 0.f;
+    v.old[j] = in ? p.old_logp[row + t] : 0.f;
+    v.ref[j] = in && p.ref_logp ? p.ref_logp[row + t] : 0.f;
+  }
+}
+
+// kOne: one block has all tokens, counts them itself and writes the sums.
+template <bool kOne>
 __global__ void __launch_bounds__(kThreads) policy_kernel(const __grid_constant__ PolicyParams p) {
   __shared__ int sh[kThreads / 32];
   __shared__ int inside[kPolicyTokens];  // counted tokens of the sequence that starts here
   __shared__ int ends[2];
-  __shared__ double shd[kThreads / 32][3 * kMaxModels];
+  __shared__ float shf[kThreads / 32][3 * kMaxModels];
+  __shared__ double shd[3 * kMaxModels];
   const long long t0 = static_cast<long long>(blockIdx.x) * kPolicyTokens;
   const long long t1 = t0 + kPolicyTokens < p.T ? t0 + kPolicyTokens : p.T;
-  const int B = p.B;
+  const int B = p.B, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (!kOne) chain_trigger();
 
+  // ---- what does not depend on the counts: the first sub-model's inputs, each
+  // token's sequence, whether it counts, its advantage
+  Inputs in;
+  load_inputs(p, 0, t0, t1, in);
+  bool on[kPer];
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    const long long t = t0 + threadIdx.x + j * kThreads;
+    on[j] = t < t1 && counts(p, t);
+  }
   if (p.agg == kAggSeq)
     for (int i = threadIdx.x; i < kPolicyTokens; i += kThreads) inside[i] = 0;
-  if (p.seq_start && threadIdx.x < 2) ends[threadIdx.x] = seq_of(p, threadIdx.x ? t1 - 1 : t0, 0, B - 1);
+  if (p.seq_start && warp < 2) {
+    const int b = seq_of_warp(p, warp ? t1 - 1 : t0, B - 1, lane);
+    if (lane == 0) ends[warp] = b;
+  }
   // The offsets have to be sorted and within [0, T].
   if (p.seq_start && blockIdx.x == 0)
     for (int b = threadIdx.x; b <= B; b += kThreads) {
@@ -172,15 +227,11 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(const __grid_constant_
     }
   __syncthreads();
   const int b0 = p.seq_start ? ends[0] : 0, b1 = p.seq_start ? ends[1] : 0;
-
-  // ---- each token's sequence, whether it counts, its advantage
-  bool on[kPer];
   int seq[kPer];
   float A[kPer], weight[kPer];
 #pragma unroll
   for (int j = 0; j < kPer; ++j) {
     const long long t = t0 + threadIdx.x + j * kThreads;
-    on[j] = t < t1 && counts(p, t);
     seq[j] = 0;
     if (p.seq_start && on[j]) {
       seq[j] = seq_of(p, t, b0, b1);
@@ -189,15 +240,21 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(const __grid_constant_
     A[j] = on[j] ? (p.adv_per_seq ? p.adv[seq[j]] : p.adv[t]) : 0.f;
     weight[j] = on[j] ? 1.f : 0.f;
   }
+  if (!kOne) chain_wait();  // the counts; and no output is written before
 
   // ---- weights
   if (p.agg == kAggToken) {
     int n = 0;
-    if (p.chunks > 0) {
-      for (int c = threadIdx.x; c < p.chunks; c += kThreads) n += p.chunk_count[c];
-    } else {  // one block has all tokens
+    if constexpr (kOne) {
 #pragma unroll
       for (int j = 0; j < kPer; ++j) n += on[j];
+    } else {
+      const int4* c = reinterpret_cast<const int4*>(p.chunk_count);
+#pragma unroll 4
+      for (int i = threadIdx.x; i < (p.chunks + 3) / 4; i += kThreads) {
+        const int4 v = c[i];
+        n += (v.x + v.y) + (v.z + v.w);
+      }
     }
     n = block_sum_int(n, sh);
     const float w = n > 0 ? 1.f / static_cast<float>(n) : 0.f;
@@ -211,101 +268,121 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(const __grid_constant_
         if (lo >= t0) atomicAdd(&inside[lo - t0], 1);
       }
     // the sequences that cross the block's ends
-    int cross[2];
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const int b = q ? b1 : b0;
-      const long long lo = seq_at(p, b), hi = seq_at(p, b + 1);
-      cross[q] = 0;
-      if (q == 1 && b0 == b1) cross[1] = cross[0];
-      else if (lo < t0 || hi > t1) cross[q] = count_range(p, lo, hi, sh);
+    int cross0 = 0, cross1 = 0;
+    if constexpr (!kOne) {
+      long long lo = seq_at(p, b0), hi = seq_at(p, b0 + 1);
+      if (lo < t0 || hi > t1) cross0 = count_range(p, lo, hi, sh);
+      cross1 = cross0;
+      if (b1 != b0) {
+        lo = seq_at(p, b1);
+        hi = seq_at(p, b1 + 1);
+        if (lo < t0 || hi > t1) cross1 = count_range(p, lo, hi, sh);
+      }
     }
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < kPer; ++j)
       if (on[j]) {
         const long long lo = seq_at(p, seq[j]), hi = seq_at(p, seq[j] + 1);
-        const int n = lo >= t0 && hi <= t1 ? inside[lo - t0] : seq[j] == b0 ? cross[0] : cross[1];
-        weight[j] = n > 0 ? static_cast<float>(1.0 / (static_cast<double>(B) * n)) : 0.f;
+        const int n = lo >= t0 && hi <= t1 ? inside[lo - t0] : seq[j] == b0 ? cross0 : cross1;
+        weight[j] = n > 0 ? 1.f / (static_cast<float>(B) * static_cast<float>(n)) : 0.f;
       }
   }
 
   // ---- loss and gradient of every sub-model
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (int m = 0; m < p.M; ++m) {
     const long long row = static_cast<long long>(m) * p.T;
     const float gw = p.grad_scale * p.w[m];
-    float sp = 0.f, sk = 0.f, sc = 0.f;
+    if (m > 0) load_inputs(p, m, t0, t1, in);
+    float s[3] = {0.f, 0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
       const long long t = t0 + threadIdx.x + j * kThreads;
       if (t >= t1) continue;
       float L = 0.f, g = 0.f;
       if (on[j]) {
-        const Token k = policy_token(p, p.logp[row + t], p.old_logp[row + t],
-                                     p.ref_logp ? p.ref_logp[row + t] : 0.f, p.ref_logp != nullptr, A[j]);
+        const Token k = policy_token(p, in.logp[j], in.old[j], in.ref[j], p.ref_logp != nullptr, A[j]);
         L = p.beta != 0.f ? fmaf(p.beta, k.kl, k.policy) : k.policy;  // beta 0: K is only reported
         g = k.grad * (weight[j] * gw);
-        sp = fmaf(k.policy, weight[j], sp);
-        sk = fmaf(k.kl, weight[j], sk);
-        sc += k.clipped ? weight[j] : 0.f;
+        s[0] = fmaf(k.policy, weight[j], s[0]);
+        s[1] = fmaf(k.kl, weight[j], s[1]);
+        s[2] += k.clipped ? weight[j] : 0.f;
       }
       if (p.tok_loss) p.tok_loss[row + t] = L;
       if (p.dlogp) p.dlogp[row + t] = g;
     }
-    const double a = warp_sum_double(sp), b = warp_sum_double(sk), c = warp_sum_double(sc);
-    if (lane == 0) {
-      shd[warp][3 * m] = a;
-      shd[warp][3 * m + 1] = b;
-      shd[warp][3 * m + 2] = c;
+#pragma unroll
+    for (int f = 0; f < 3; ++f) {
+      s[f] = warp_sum(s[f]);
+      if (lane == 0) shf[warp][3 * m + f] = s[f];
     }
   }
   __syncthreads();
   if (threadIdx.x < 3 * p.M) {
-    double s = 0.0;
-    for (int i = 0; i < kThreads / 32; ++i) s += shd[i][threadIdx.x];
-    p.part[static_cast<long long>(blockIdx.x) * 3 * p.M + threadIdx.x] = s;
+    double v = 0.0;
+    for (int i = 0; i < kThreads / 32; ++i) v += shf[i][threadIdx.x];
+    if constexpr (kOne) {
+      shd[threadIdx.x] = v;
+      if (p.diag) p.diag[threadIdx.x % 3 * p.M + threadIdx.x / 3] = static_cast<float>(v);
+    } else {
+      p.part[static_cast<long long>(threadIdx.x) * gridDim.x + blockIdx.x] = static_cast<float>(v);
+    }
+  }
+  if constexpr (kOne) {
+    __syncthreads();
+    if (threadIdx.x == 0) *p.loss = total_loss(p, shd);
   }
 }
 
-// Block shares -> diag [3][M] and the loss.  Thread i adds shares i, i + threads, ...
-// of one quantity; the threads are then added in order.
+// Block shares -> diag and the loss.  Each of the 3 M quantities has 32 / (3 M) warps;
+// a lane adds its shares in two fp32 words (Pair): 64-bit additions by every thread
+// took 25 us a sub-model, whatever the number of blocks.
 constexpr int kFinalThreads = 1024;
 
 __global__ void __launch_bounds__(kFinalThreads) policy_final_kernel(const __grid_constant__ PolicyParams p, int blocks) {
-  __shared__ double sh[kFinalThreads / 32];
-  double loss = 0.0;
-  for (int m = 0; m < p.M; ++m) {
-    double v[3];
-    for (int f = 0; f < 3; ++f) {
-      double s = 0.0;
-      for (int i = threadIdx.x; i < blocks; i += kFinalThreads) s += p.part[(static_cast<long long>(i) * p.M + m) * 3 + f];
-      s = warp_sum_double(s);
-      __syncthreads();
-      if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = s;
-      __syncthreads();
-      v[f] = 0.0;
-      for (int i = 0; i < kFinalThreads / 32; ++i) v[f] += sh[i];
-      if (p.diag && threadIdx.x == 0) p.diag[f * p.M + m] = static_cast<float>(v[f]);
-    }
-    loss += static_cast<double>(p.w[m]) * (p.beta != 0.f ? v[0] + static_cast<double>(p.beta) * v[1] : v[0]);
+  __shared__ Pair sh[kFinalThreads / 32];
+  __shared__ double shd[3 * kMaxModels];
+  const int nq = 3 * p.M, per = (kFinalThreads / 32) / nq, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int q = warp % nq, k = warp / nq;
+  chain_trigger();
+  chain_wait();
+  Pair a = {0.f, 0.f};
+  if (k < per) {
+    const float* part = p.part + static_cast<long long>(q) * blocks;
+#pragma unroll 8
+    for (int i = k * 32 + lane; i < blocks; i += per * 32) pair_add(a, part[i], 0.f);
   }
-  if (threadIdx.x == 0) *p.loss = static_cast<float>(loss);
+  a = warp_sum_pair(a);
+  if (lane == 0) sh[warp] = a;
+  __syncthreads();
+  if (threadIdx.x < nq) {
+    double v = 0.0;
+    for (int i = 0; i < per; ++i) v += pair_value(sh[i * nq + threadIdx.x]);
+    shd[threadIdx.x] = v;
+    if (p.diag) p.diag[threadIdx.x % 3 * p.M + threadIdx.x / 3] = static_cast<float>(v);
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) *p.loss = total_loss(p, shd);
 }
 
 }  // namespace
 
 cudaError_t launch_policy(const PolicyParams& p, cudaStream_t s) {
+  const int blocks = policy_blocks(p.T);
   cudaError_t e;
+  if (blocks == 1) {
+    policy_kernel<true><<<1, kThreads, 0, s>>>(p);
+    return cudaGetLastError();
+  }
   if (p.chunks > 0) {
     policy_count_kernel<<<p.chunks, kThreads, 0, s>>>(p);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    if ((e = launch_chained(policy_kernel<false>, dim3(blocks), dim3(kThreads), 0, s, p)) != cudaSuccess) return e;
+  } else {
+    policy_kernel<false><<<blocks, kThreads, 0, s>>>(p);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
   }
-  const int blocks = policy_blocks(p.T);
-  policy_kernel<<<blocks, kThreads, 0, s>>>(p);
-  if ((e = cudaGetLastError()) != cudaSuccess) return e;
-  policy_final_kernel<<<1, kFinalThreads, 0, s>>>(p, blocks);
-  return cudaGetLastError();
+  return launch_chained(policy_final_kernel, dim3(1), dim3(kFinalThreads), 0, s, p, blocks);
 }
 
 }  // namespace mls

@@ -66,4 +66,26 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
+
+// A sum in two fp32 words: what rounding the first loses goes to the second (Knuth's
+// two-sum), so a long sum keeps some 45 bits.  An SM adds two 64-bit values a clock
+// and 128 fp32 ones.  Once the first word is infinite or NaN the second means nothing.
+struct Pair {
+  float hi, lo;
+};
+__device__ __forceinline__ void pair_add(Pair& a, float hi, float lo) {
+  const float s = a.hi + hi, b = s - a.hi;
+  a.lo += ((a.hi - (s - b)) + (hi - b)) + lo;
+  a.hi = s;
+}
+__device__ __forceinline__ Pair warp_sum_pair(Pair a) {  // valid in lane 0
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1)
+    pair_add(a, __shfl_down_sync(0xffffffffu, a.hi, o), __shfl_down_sync(0xffffffffu, a.lo, o));
+  return a;
+}
+__device__ __forceinline__ double pair_value(const Pair& a) {
+  return isfinite(a.hi) ? static_cast<double>(a.hi) + static_cast<double>(a.lo) : static_cast<double>(a.hi);
+}
+
 }  // namespace mls

@@ -122,7 +122,7 @@ def check(c, data, scale=1.0):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("agg", ["token", "seq", "sum"])
-@pytest.mark.parametrize("T,n", [(1, 1), (2, 2), (31, 3), (2047, 5), (2048, 1), (2049, 40), (4096, 2),
+@pytest.mark.parametrize("T,n", [(1, 1), (2, 2), (31, 3), (1024, 9), (1025, 2), (2047, 5), (2048, 1), (2049, 40), (4096, 2),
                                  (5000, 4000), (9001, 3), (20011, 300)])
 def test_ragged_sequences(T, n, agg):
     c = config(T, B=n, agg=agg, adv_per_seq=T % 2 == 1, beta=0.07, M=1 + T % 3)
@@ -144,7 +144,7 @@ def test_without_sequences(T, agg):
 def test_sequence_borders():
     """Empty sequences in a row, sequences that end at a block's end or cross several, one that is
     all prompt, tokens before the first and behind the last sequence."""
-    lens = [0, 0, 2048, 0, 1, 2047, 4097, 0, 3, 5000, 0]
+    lens = [0, 0, 2048, 0, 1, 2047, 4097, 0, 3, 5000, 0, 1023, 1]
     T = sum(lens) + 700
     for agg in ("token", "seq", "sum"):
         c = config(T, B=len(lens), agg=agg, adv_per_seq=True, beta=0.1)
