@@ -8,12 +8,12 @@
 // Bound by HBM: forward x and y, backward x, g and dx, each moved once.  The variance
 // is the mean of the squared deviations from the mean itself, so that a mean far
 // from 0 costs no digits.
-//   forward   a row's 16-byte vectors, at most 4 a lane, stay packed in the registers
-//             of its 1 to 16 warps;
-//   backward  persistent blocks of 16 warps, W of them to a row, which load the next
-//             row before they work on this one and keep their columns' sums of g xh
-//             and g in registers (in shared memory for the widest rows) over all rows
-//             of the block.  The blocks' sums are added in order by a second kernel,
+//   forward   a row stays in the registers of its 1 to 16 warps, at most 8 16-byte
+//             vectors a lane;
+//   backward  persistent blocks of 16 warps, W of them to a row, which copy rows ahead
+//             into shared memory and keep their columns' sums of g xh and g in
+//             registers over all rows of the block (the widest rows: one row ahead in
+//             registers, the sums in shared memory).  The blocks' sums are added in order by a second kernel,
 //             so results do not depend on timing;
 //   wider rows are read again from L2 instead, one warp a row.
 #include "mls_device.cuh"
@@ -47,7 +47,7 @@ __device__ __forceinline__ float row_sum(float v, float* sh, int id, int w) {
 
 template <typename E, int V, int W>
 __global__ void __launch_bounds__(32 * W * kFwdRows<W>) norm_fwd_kernel(const NormParams p) {
-  constexpr int N = Vec<E>::N;
+  constexpr int N = Vec<E>::N, N2 = Vec2<E>::N;
   __shared__ float sh[kFwdRows<W>][2][W];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = warp / W, w = warp % W;
   const long long t = static_cast<long long>(blockIdx.x) * kFwdRows<W> + group;
@@ -61,39 +61,37 @@ __global__ void __launch_bounds__(32 * W * kFwdRows<W>) norm_fwd_kernel(const No
     u[j] = k < p.d ? ld16(x + k) : make_uint4(0u, 0u, 0u, 0u);
   }
   const float inv_d = 1.0f / static_cast<float>(p.d);
-  float s = 0.f, q = 0.f;
+  F2 f[V][N2];
+  F2 s = 0, q = 0;
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    float f[N];
-    Vec<E>::unpack(u[j], f);
+    Vec2<E>::unpack(u[j], f[j]);
 #pragma unroll
-    for (int i = 0; i < N; ++i) s += f[i];
+    for (int i = 0; i < N2; ++i) s = f2_add(s, f[j][i]);
   }
-  const float mu = row_sum<W>(s, sh[group][0], 1 + group, w) * inv_d;
-  keep_packed(u);
+  const float mu = row_sum<W>(f2_sum(s), sh[group][0], 1 + group, w) * inv_d;
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    if (((j * W + w) * 32 + lane) * N < p.d) {
-      float f[N];
-      Vec<E>::unpack(u[j], f);
+    const bool in = ((j * W + w) * 32 + lane) * N < p.d;
 #pragma unroll
-      for (int i = 0; i < N; ++i) q = fmaf(f[i] - mu, f[i] - mu, q);
+    for (int i = 0; i < N2; ++i) {
+      f[j][i] = f2_add(f[j][i], f2(in ? -mu : 0.f));
+      q = f2_fma(f[j][i], f[j][i], q);
     }
   }
-  const float r = 1.0f / sqrtf(row_sum<W>(q, sh[group][1], 1 + group, w) * inv_d + p.eps);
-  keep_packed(u);
+  const float r = 1.0f / sqrtf(row_sum<W>(f2_sum(q), sh[group][1], 1 + group, w) * inv_d + p.eps);
 #pragma unroll
   for (int j = 0; j < V; ++j) {
     const int k = ((j * W + w) * 32 + lane) * N;
     if (k < p.d) {
-      float f[N], g[N], b[N];
-      Vec<E>::unpack(u[j], f);
-      if (p.gain) Vec<E>::unpack(ld16(static_cast<const E*>(p.gain) + k), g);
-      if (p.bias) Vec<E>::unpack(ld16(static_cast<const E*>(p.bias) + k), b);
+      // no gain: ones, no bias: zeros
+      const uint32_t one = Vec2<E>::kOne;
+      F2 g[N2], b[N2];
+      Vec2<E>::unpack(p.gain ? ld16(static_cast<const E*>(p.gain) + k) : make_uint4(one, one, one, one), g);
+      Vec2<E>::unpack(p.bias ? ld16(static_cast<const E*>(p.bias) + k) : make_uint4(0u, 0u, 0u, 0u), b);
 #pragma unroll
-      for (int i = 0; i < N; ++i)
-        f[i] = fmaf((f[i] - mu) * r, p.gain ? g[i] : 1.f, p.bias ? b[i] : 0.f);
-      st16(y + k, Vec<E>::pack(f));
+      for (int i = 0; i < N2; ++i) f[j][i] = f2_fma(f2_mul(f[j][i], f2(r)), g[i], b[i]);
+      st16(y + k, Vec2<E>::pack(f[j]));
     }
   }
   if (w == 0 && lane == 0 && p.mean) {
@@ -104,6 +102,158 @@ __global__ void __launch_bounds__(32 * W * kFwdRows<W>) norm_fwd_kernel(const No
 
 // ------------------------------------------------------------------ backward
 constexpr int kBwdWarps = 16;
+
+// 16 bytes from global to shared memory without a register; a thread's copies since its
+// last commit form a group, and it waits until at most N of its groups are left.
+__device__ __forceinline__ void copy16_async(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(reinterpret_cast<uint64_t>(src)) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// S rows of every lane's own vectors in shared memory, S - 1 of them being copied there
+// (cp.async: a lane waits for and reads its own copies only, so no barrier is needed):
+// with a row ahead in registers alone, 32 KB were in flight on an SM, and 65536 x
+// 4096 bf16 values took 372 us.
+template <typename E, int V, int W, int S>
+__global__ void __launch_bounds__(32 * kBwdWarps, 1) norm_bwd_kernel(const NormParams p) {
+  constexpr int N = Vec<E>::N, N2 = Vec2<E>::N, kGroups = kBwdWarps / W, kThreads = 32 * kBwdWarps;
+  extern __shared__ __align__(16) uint4 ring[];  // [S][x, g][V][kThreads], after the loop the sums [2][d]
+  __shared__ float2 sh[2][kBwdWarps];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = warp / W, w = warp % W;
+  const E* gain = static_cast<const E*>(p.gain);
+  const float inv_d = 1.0f / static_cast<float>(p.d);
+  const uint32_t one = Vec2<E>::kOne;
+  uint4 gv[V];  // the gain; ones without one
+  F2 dg[V][N2], db[V][N2];
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const int k = ((j * W + w) * 32 + lane) * N;
+    gv[j] = gain && k < p.d ? ld16(gain + k) : make_uint4(one, one, one, one);
+#pragma unroll
+    for (int i = 0; i < N2; ++i) dg[j][i] = db[j][i] = 0;
+  }
+  const long long step = static_cast<long long>(gridDim.x) * kGroups;
+  long long t = static_cast<long long>(blockIdx.x) * kGroups + group;
+  const uint32_t mine = smem_u32(ring) + threadIdx.x * 16;
+  auto fetch = [&](long long row, int slot) {
+    if (row < p.T) {
+      const E* x = static_cast<const E*>(p.x) + row * p.d;
+      const E* g = static_cast<const E*>(p.dy) + row * p.d;
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const int k = ((j * W + w) * 32 + lane) * N;
+        if (k < p.d) {
+          copy16_async(mine + (slot * 2 * V + j) * kThreads * 16, x + k);
+          copy16_async(mine + (slot * 2 * V + V + j) * kThreads * 16, g + k);
+        }
+      }
+    }
+    copy_commit();
+  };
+#pragma unroll
+  for (int q = 0; q < S - 1; ++q) fetch(t + q * step, q);
+  float mu = 0.f, r = 0.f;
+  if (t < p.T) {
+    mu = p.mean[t];
+    r = p.rstd[t];
+  }
+  int slot = 0;
+  for (int it = 0; t < p.T; t += step, it ^= 1) {
+    fetch(t + (S - 1) * step, slot == 0 ? S - 1 : slot - 1);  // the slot read in the round before
+    copy_wait<S - 1>();
+    const F2 nmu = f2(-mu), r2 = f2(r);
+    if (t + step < p.T) {  // the next row's
+      mu = p.mean[t + step];
+      r = p.rstd[t + step];
+    }
+    F2 a2 = 0, b2 = 0, xh[V][N2], h[V][N2];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const int k = ((j * W + w) * 32 + lane) * N;
+      if (k < p.d) {
+        F2 g[N2], gn[N2];
+        Vec2<E>::unpack(ring[(slot * 2 * V + j) * kThreads + threadIdx.x], xh[j]);
+        Vec2<E>::unpack(ring[(slot * 2 * V + V + j) * kThreads + threadIdx.x], g);
+        Vec2<E>::unpack(gv[j], gn);
+#pragma unroll
+        for (int i = 0; i < N2; ++i) {
+          xh[j][i] = f2_mul(f2_add(xh[j][i], nmu), r2);
+          h[j][i] = f2_mul(g[i], gn[i]);
+          a2 = f2_add(a2, h[j][i]);
+          b2 = f2_fma(h[j][i], xh[j][i], b2);
+          dg[j][i] = f2_fma(g[i], xh[j][i], dg[j][i]);
+          db[j][i] = f2_add(db[j][i], g[i]);
+        }
+      }
+    }
+    slot = slot + 1 == S ? 0 : slot + 1;
+    float a = warp_sum(f2_sum(a2)), b = warp_sum(f2_sum(b2));
+    if constexpr (W > 1) {
+      // One barrier a row: the next row's words are the other half, and a warp comes back
+      // to this one only past that row's barrier, when all have read it.
+      if (lane == 0) sh[it][warp] = make_float2(a, b);
+      group_sync(1 + group, 32 * W);
+      a = b = 0.f;
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        const float2 v = sh[it][group * W + i];
+        a += v.x;
+        b += v.y;
+      }
+    }
+    const F2 na = f2(-a * inv_d), nb = f2(-b * inv_d);
+    E* dx = static_cast<E*>(p.dx) + t * p.d;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const int k = ((j * W + w) * 32 + lane) * N;
+      if (k < p.d) {
+#pragma unroll
+        for (int i = 0; i < N2; ++i)
+          h[j][i] = f2_mul(f2_fma(xh[j][i], nb, f2_add(h[j][i], na)), r2);
+        st16(dx + k, Vec2<E>::pack(h[j]));
+      }
+    }
+  }
+  copy_wait<0>();
+  if (!p.part) return;
+
+  // ---- the block's sums: its groups' one after the other
+  float* out = p.part + 2ll * p.d * blockIdx.x;
+  float* sums = reinterpret_cast<float*>(ring);
+  __syncthreads();
+  for (int q = 0; q < kGroups; ++q) {
+    if (group == q) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const int k = ((j * W + w) * 32 + lane) * N;
+        if (k < p.d) {
+          float* s = q + 1 < kGroups ? sums : out;  // the last group writes the block's share
+#pragma unroll
+          for (int i = 0; i < N; i += 4) {
+            float4 g, b;
+            f2_split(dg[j][i / 2], g.x, g.y);
+            f2_split(dg[j][i / 2 + 1], g.z, g.w);
+            f2_split(db[j][i / 2], b.x, b.y);
+            f2_split(db[j][i / 2 + 1], b.z, b.w);
+            if (q > 0) {
+              const float4 pg = *reinterpret_cast<const float4*>(sums + k + i);
+              const float4 pb = *reinterpret_cast<const float4*>(sums + p.d + k + i);
+              g = make_float4(g.x + pg.x, g.y + pg.y, g.z + pg.z, g.w + pg.w);
+              b = make_float4(b.x + pb.x, b.y + pb.y, b.z + pb.z, b.w + pb.w);
+            }
+            *reinterpret_cast<float4*>(s + k + i) = g;
+            *reinterpret_cast<float4*>(s + p.d + k + i) = b;
+          }
+        }
+      }
+    }
+    __syncthreads();
+  }
+}
 
 // One row's vectors of a lane, and the row's statistics.
 template <int V>
@@ -130,171 +280,112 @@ __device__ __forceinline__ void load_row(const NormParams& p, long long t, int w
   b.r = p.rstd[t];
 }
 
-// kShared: the columns' sums lie in shared memory and the gain is read at each row;
-// else both stay in registers.
-template <typename E, int V, int W, bool kShared>
-__global__ void __launch_bounds__(32 * kBwdWarps, 1) norm_bwd_kernel(const NormParams p) {
-  constexpr int N = Vec<E>::N, kGroups = kBwdWarps / W;
+// The widest rows: the columns' sums lie in shared memory and the gain is read at each
+// row, from L1 or L2.
+template <typename E, int V>
+__global__ void __launch_bounds__(32 * kBwdWarps, 1) norm_bwd_shared_kernel(const NormParams p) {
+  constexpr int N = Vec<E>::N, N2 = Vec2<E>::N, W = kBwdWarps;
   extern __shared__ __align__(16) float sums[];  // [2][d]
   __shared__ float2 sh[2][kBwdWarps];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = warp / W, w = warp % W;
+  const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const E* gain = static_cast<const E*>(p.gain);
   const float inv_d = 1.0f / static_cast<float>(p.d);
-  constexpr int kR = kShared ? 1 : V;
-  uint4 gv[kR];
-  float dg[kR][N], db[kR][N];
-#pragma unroll
-  for (int j = 0; j < kR; ++j)
-#pragma unroll
-    for (int i = 0; i < N; ++i) dg[j][i] = db[j][i] = 0.f;
-  if constexpr (kShared) {
-    for (int k = threadIdx.x; k < 2 * p.d; k += 32 * kBwdWarps) sums[k] = 0.f;
-    __syncthreads();
-  } else {
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const int k = ((j * W + w) * 32 + lane) * N;
-      if (gain && k < p.d) gv[j] = ld16(gain + k);
-    }
-  }
+  const uint32_t one = Vec2<E>::kOne;
+  for (int c = threadIdx.x; c < 2 * p.d; c += 32 * kBwdWarps) sums[c] = 0.f;
+  __syncthreads();
 
-  const long long step = static_cast<long long>(gridDim.x) * kGroups;
-  long long t = static_cast<long long>(blockIdx.x) * kGroups + group;
+  const long long step = gridDim.x;
+  long long t = blockIdx.x;
   BwdRow<V> next;
   load_row<E, V, W>(p, t, w, lane, next);
   for (int it = 0; t < p.T; t += step, it ^= 1) {
     BwdRow<V> cur = next;
     load_row<E, V, W>(p, t + step, w, lane, next);
-    float a = 0.f, b = 0.f;
+    const F2 nmu = f2(-cur.mu), r2 = f2(cur.r);
+    F2 a2 = 0, b2 = 0, xh[V][N2], h[V][N2];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       const int k = ((j * W + w) * 32 + lane) * N;
       if (k < p.d) {
-        float f[N], g[N], gn[N];
-        Vec<E>::unpack(cur.x[j], f);
-        Vec<E>::unpack(cur.g[j], g);
-        if (gain) Vec<E>::unpack(kShared ? ld16(gain + k) : gv[kShared ? 0 : j], gn);
+        F2 g[N2], gn[N2];
+        Vec2<E>::unpack(cur.x[j], xh[j]);
+        Vec2<E>::unpack(cur.g[j], g);
+        Vec2<E>::unpack(gain ? ld16(gain + k) : make_uint4(one, one, one, one), gn);
         float sg[N], sb[N];
-        if constexpr (kShared) {
 #pragma unroll
-          for (int i = 0; i < N; i += 4) {
-            *reinterpret_cast<float4*>(sg + i) = *reinterpret_cast<const float4*>(sums + k + i);
-            *reinterpret_cast<float4*>(sb + i) = *reinterpret_cast<const float4*>(sums + p.d + k + i);
-          }
+        for (int i = 0; i < N; i += 4) {
+          *reinterpret_cast<float4*>(sg + i) = *reinterpret_cast<const float4*>(sums + k + i);
+          *reinterpret_cast<float4*>(sb + i) = *reinterpret_cast<const float4*>(sums + p.d + k + i);
         }
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const float xh = (f[i] - cur.mu) * cur.r;
-          const float h = gain ? g[i] * gn[i] : g[i];
-          a += h;
-          b = fmaf(h, xh, b);
-          if constexpr (kShared) {
-            sg[i] = fmaf(g[i], xh, sg[i]);
-            sb[i] += g[i];
-          } else {
-            dg[j][i] = fmaf(g[i], xh, dg[j][i]);
-            db[j][i] += g[i];
-          }
+        for (int i = 0; i < N2; ++i) {
+          xh[j][i] = f2_mul(f2_add(xh[j][i], nmu), r2);
+          h[j][i] = f2_mul(g[i], gn[i]);
+          a2 = f2_add(a2, h[j][i]);
+          b2 = f2_fma(h[j][i], xh[j][i], b2);
+          f2_split(f2_fma(g[i], xh[j][i], f2(sg[2 * i], sg[2 * i + 1])), sg[2 * i], sg[2 * i + 1]);
+          f2_split(f2_add(g[i], f2(sb[2 * i], sb[2 * i + 1])), sb[2 * i], sb[2 * i + 1]);
         }
-        if constexpr (kShared) {
 #pragma unroll
-          for (int i = 0; i < N; i += 4) {
-            *reinterpret_cast<float4*>(sums + k + i) = *reinterpret_cast<const float4*>(sg + i);
-            *reinterpret_cast<float4*>(sums + p.d + k + i) = *reinterpret_cast<const float4*>(sb + i);
-          }
+        for (int i = 0; i < N; i += 4) {
+          *reinterpret_cast<float4*>(sums + k + i) = *reinterpret_cast<const float4*>(sg + i);
+          *reinterpret_cast<float4*>(sums + p.d + k + i) = *reinterpret_cast<const float4*>(sb + i);
         }
       }
     }
+    float a = f2_sum(a2), b = f2_sum(b2);
     a = warp_sum(a);
     b = warp_sum(b);
-    if constexpr (W > 1) {
-      // One barrier a row: the next row's words are the other half, and a warp comes back
-      // to this one only past that row's barrier, when all have read it.
-      if (lane == 0) sh[it][warp] = make_float2(a, b);
-      group_sync(1 + group, 32 * W);
-      a = b = 0.f;
+    if (lane == 0) sh[it][w] = make_float2(a, b);
+    __syncthreads();  // one a row, as above
+    a = b = 0.f;
 #pragma unroll
-      for (int i = 0; i < W; ++i) {
-        const float2 v = sh[it][group * W + i];
-        a += v.x;
-        b += v.y;
-      }
+    for (int i = 0; i < W; ++i) {
+      const float2 v = sh[it][i];
+      a += v.x;
+      b += v.y;
     }
-    a *= inv_d;
-    b *= inv_d;
-    keep_packed(cur.x);
-    keep_packed(cur.g);
+    const F2 na = f2(-a * inv_d), nb = f2(-b * inv_d);
     E* dx = static_cast<E*>(p.dx) + t * p.d;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       const int k = ((j * W + w) * 32 + lane) * N;
       if (k < p.d) {
-        float f[N], g[N], gn[N];
-        Vec<E>::unpack(cur.x[j], f);
-        Vec<E>::unpack(cur.g[j], g);
-        if (gain) Vec<E>::unpack(kShared ? ld16(gain + k) : gv[kShared ? 0 : j], gn);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const float xh = (f[i] - cur.mu) * cur.r, h = gain ? g[i] * gn[i] : g[i];
-          f[i] = cur.r * ((h - a) - xh * b);
-        }
-        st16(dx + k, Vec<E>::pack(f));
+        for (int i = 0; i < N2; ++i)
+          h[j][i] = f2_mul(f2_fma(xh[j][i], nb, f2_add(h[j][i], na)), r2);
+        st16(dx + k, Vec2<E>::pack(h[j]));
       }
     }
   }
   if (!p.part) return;
-
-  // ---- the block's sums: its groups' one after the other
   float* out = p.part + 2ll * p.d * blockIdx.x;
-  if constexpr (kShared) {
-    __syncthreads();
-    for (int k = threadIdx.x; k < 2 * p.d; k += 32 * kBwdWarps) out[k] = sums[k];
-  } else {
-    for (int q = 0; q < kGroups; ++q) {
-      if (group == q) {
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-          const int k = ((j * W + w) * 32 + lane) * N;
-          if (k < p.d) {
-            float* s = q + 1 < kGroups ? sums : out;  // the last group writes the block's share
-#pragma unroll
-            for (int i = 0; i < N; i += 4) {
-              float4 g = make_float4(dg[j][i], dg[j][i + 1], dg[j][i + 2], dg[j][i + 3]);
-              float4 b = make_float4(db[j][i], db[j][i + 1], db[j][i + 2], db[j][i + 3]);
-              if (q > 0) {
-                const float4 pg = *reinterpret_cast<const float4*>(sums + k + i);
-                const float4 pb = *reinterpret_cast<const float4*>(sums + p.d + k + i);
-                g = make_float4(g.x + pg.x, g.y + pg.y, g.z + pg.z, g.w + pg.w);
-                b = make_float4(b.x + pb.x, b.y + pb.y, b.z + pb.z, b.w + pb.w);
-              }
-              *reinterpret_cast<float4*>(s + k + i) = g;
-              *reinterpret_cast<float4*>(s + p.d + k + i) = b;
-            }
-          }
-        }
-      }
-      __syncthreads();
-    }
-  }
+  __syncthreads();
+  for (int c = threadIdx.x; c < 2 * p.d; c += 32 * kBwdWarps) out[c] = sums[c];
 }
 
 // Blocks' shares [splits][2][d] -> dgain, dbias.  A block owns 32 vectors of four columns;
-// each of its 8 warps adds every eighth share, then the first adds the warps'.
-constexpr int kColWarps = 8;
+// each of its 16 warps adds every 16th share, ten at a time (152 shares: one
+// memory latency), then the first adds the warps'.
+constexpr int kColWarps = 16, kColBatch = 10;
 
 __global__ void __launch_bounds__(32 * kColWarps) norm_cols_sum_kernel(const NormParams p) {
   __shared__ float4 sh[kColWarps][32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int c = (blockIdx.x * 32 + lane) * 4;
-  chain_trigger();
   chain_wait();
   float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
   if (c < 2 * p.d) {
     const float* part = p.part + c;
-#pragma unroll 8
-    for (int s = warp; s < p.splits; s += kColWarps) {
-      const float4 b = *reinterpret_cast<const float4*>(part + 2ll * p.d * s);
-      a = make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w);
+    for (int s0 = warp; s0 < p.splits; s0 += kColWarps * kColBatch) {
+      float4 v[kColBatch];
+#pragma unroll
+      for (int i = 0; i < kColBatch; ++i) {
+        const int s = s0 + i * kColWarps;
+        v[i] = s < p.splits ? *reinterpret_cast<const float4*>(part + 2ll * p.d * s) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+#pragma unroll
+      for (int i = 0; i < kColBatch; ++i) a = make_float4(a.x + v[i].x, a.y + v[i].y, a.z + v[i].z, a.w + v[i].w);
     }
   }
   sh[warp][lane] = a;
@@ -436,28 +527,43 @@ cudaError_t fwd_any(const NormParams& p, cudaStream_t s) {
   if (v <= 16) return fwd<E, 4, 4>(p, s);
   if (v <= 32) return fwd<E, 4, 8>(p, s);
   if (v <= 64) return fwd<E, 4, 16>(p, s);
+  if (v <= 128) return fwd<E, 8, 16>(p, s);
   norm_fwd_wide_kernel<E><<<blocks_of(p.T, kWarps), 32 * kWarps, 0, s>>>(p);
   return cudaGetLastError();
 }
 
-template <typename E, int V, int W, bool kShared>
+// Rows of a lane's vectors in the ring: as many as 160 KB hold, at most 8.
+template <int V>
+constexpr int kRows = V >= 4 ? 3 : V == 2 ? 5 : 8;
+template <int V>
+constexpr size_t kRingBytes = sizeof(uint4) * 2 * V * 32 * kBwdWarps * kRows<V>;
+
+template <typename E, int V, int W>
 cudaError_t bwd(const NormParams& p, cudaStream_t s) {
-  const size_t smem = kShared || W < kBwdWarps ? sizeof(float) * 2 * p.d : 0;
-  norm_bwd_kernel<E, V, W, kShared><<<p.splits, 32 * kBwdWarps, smem, s>>>(p);
+  static_assert(sizeof(float) * 2 * V * W * 32 * Vec<E>::N <= kRingBytes<V>, "the sums fit in the ring's memory");
+  norm_bwd_kernel<E, V, W, kRows<V>><<<p.splits, 32 * kBwdWarps, kRingBytes<V>, s>>>(p);
+  return cudaGetLastError();
+}
+template <typename E, int V>
+cudaError_t bwd_shared(const NormParams& p, cudaStream_t s) {
+  norm_bwd_shared_kernel<E, V><<<p.splits, 32 * kBwdWarps, sizeof(float) * 2 * p.d, s>>>(p);
   return cudaGetLastError();
 }
 
 template <typename E>
 cudaError_t bwd_any(const NormParams& p, cudaStream_t s) {
   const int v = (p.d + 32 * Vec<E>::N - 1) / (32 * Vec<E>::N);
-  if (v <= 1) return bwd<E, 1, 1, false>(p, s);
-  if (v <= 2) return bwd<E, 2, 1, false>(p, s);
-  if (v <= 4) return bwd<E, 2, 2, false>(p, s);
-  if (v <= 8) return bwd<E, 2, 4, false>(p, s);
-  if (v <= 16) return bwd<E, 2, 8, false>(p, s);
-  if (v <= 32) return bwd<E, 2, 16, false>(p, s);
-  if constexpr (Vec<E>::N == 8) return bwd<E, 4, 16, true>(p, s);  // 16384 values
-  else return v <= 64 ? bwd<E, 4, 16, true>(p, s) : bwd<E, 8, 16, true>(p, s);
+  if (v <= 1) return bwd<E, 1, 1>(p, s);
+  if (v <= 2) return bwd<E, 2, 1>(p, s);
+  if (v <= 4) return bwd<E, 2, 2>(p, s);
+  if (v <= 8) return bwd<E, 2, 4>(p, s);
+  if (v <= 16) return bwd<E, 2, 8>(p, s);
+  if (v <= 32) return bwd<E, 2, 16>(p, s);
+  if constexpr (Vec<E>::N == 8) {
+    return bwd_shared<E, 4>(p, s);  // 16384 values
+  } else {
+    return v <= 64 ? bwd<E, 4, 16>(p, s) : bwd_shared<E, 8>(p, s);
+  }
 }
 
 bool bwd_cached(int d) { return d <= kBwdSharedMost; }
@@ -510,16 +616,25 @@ cudaError_t launch_norm_bwd(const NormParams& p, bool fp32, cudaStream_t s) {
   return cudaGetLastError();
 }
 
-// Dynamic shared memory of the widest backward kernels (past 48 KB with the static part).
+// Dynamic shared memory beyond 48 KB.
 cudaError_t setup_norm_kernels() {
   cudaError_t e;
-#define MLS_SET(E, V, W, S)                                                                             \
-  e = cudaFuncSetAttribute(norm_bwd_kernel<E, V, W, S>, cudaFuncAttributeMaxDynamicSharedMemorySize,     \
-                           sizeof(float) * 2 * kBwdSharedMost);                                         \
+#define MLS_SET(K, BYTES)                                                                     \
+  e = cudaFuncSetAttribute(K, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(BYTES)); \
   if (e != cudaSuccess) return e;
-  MLS_SET(float, 4, 16, true)
-  MLS_SET(float, 8, 16, true)
-  MLS_SET(__nv_bfloat16, 4, 16, true)
+#define MLS_SET_RING(E, V, W) MLS_SET((norm_bwd_kernel<E, V, W, kRows<V>>), kRingBytes<V>)
+#define MLS_SET_BOTH(V, W) MLS_SET_RING(float, V, W) MLS_SET_RING(__nv_bfloat16, V, W)
+  MLS_SET_BOTH(1, 1)
+  MLS_SET_BOTH(2, 1)
+  MLS_SET_BOTH(2, 2)
+  MLS_SET_BOTH(2, 4)
+  MLS_SET_BOTH(2, 8)
+  MLS_SET_BOTH(2, 16)
+  MLS_SET_RING(float, 4, 16)
+  MLS_SET((norm_bwd_shared_kernel<float, 8>), sizeof(float) * 2 * kBwdSharedMost)
+  MLS_SET((norm_bwd_shared_kernel<__nv_bfloat16, 4>), sizeof(float) * 2 * kBwdSharedMost)
+#undef MLS_SET_BOTH
+#undef MLS_SET_RING
 #undef MLS_SET
   return cudaSuccess;
 }

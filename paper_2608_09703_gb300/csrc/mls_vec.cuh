@@ -67,6 +67,78 @@ __device__ __forceinline__ float warp_sum(float v) {
 }
 
 
+// Two fp32 values in a 64-bit register pair: one instruction works on both.
+typedef unsigned long long F2;
+__device__ __forceinline__ F2 f2(float lo, float hi) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ F2 f2(float v) { return f2(v, v); }
+__device__ __forceinline__ void f2_split(F2 v, float& lo, float& hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ float f2_sum(F2 v) {
+  float lo, hi;
+  f2_split(v, lo, hi);
+  return lo + hi;
+}
+__device__ __forceinline__ F2 f2_add(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ F2 f2_mul(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ F2 f2_fma(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+
+// The same vectors as pairs: 4 of bf16, 2 of fp32.
+template <typename E>
+struct Vec2;
+template <>
+struct Vec2<__nv_bfloat16> {
+  static constexpr int N = 4;
+  static constexpr uint32_t kOne = 0x3f803f80u;  // two ones
+  static __device__ __forceinline__ void unpack(const uint4& u, F2 (&f)[4]) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = f2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+  }
+  static __device__ __forceinline__ uint4 pack(const F2 (&f)[4]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float lo, hi;
+      f2_split(f[i], lo, hi);
+      const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+template <>
+struct Vec2<float> {
+  static constexpr int N = 2;
+  static constexpr uint32_t kOne = 0x3f800000u;
+  static __device__ __forceinline__ void unpack(const uint4& u, F2 (&f)[2]) {
+    f[0] = f2(__uint_as_float(u.x), __uint_as_float(u.y));
+    f[1] = f2(__uint_as_float(u.z), __uint_as_float(u.w));
+  }
+  static __device__ __forceinline__ uint4 pack(const F2 (&f)[2]) {
+    float a, b, c, d;
+    f2_split(f[0], a, b);
+    f2_split(f[1], c, d);
+    return make_uint4(__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d));
+  }
+};
+
 // A sum in two fp32 words: what rounding the first loses goes to the second (Knuth's
 // two-sum), so a long sum keeps some 45 bits.  An SM adds two 64-bit values a clock
 // and 128 fp32 ones.  Once the first word is infinite or NaN the second means nothing.
