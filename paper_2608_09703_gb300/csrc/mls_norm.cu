@@ -219,6 +219,7 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 1) norm_bwd_kernel(const NormP
     }
   }
   copy_wait<0>();
+  chain_trigger();  // the second kernel's launch, under the last rows
   if (!p.part) return;
 
   // ---- the block's sums: its groups' one after the other
@@ -523,7 +524,9 @@ cudaError_t fwd_any(const NormParams& p, cudaStream_t s) {
   if (v <= 1) return fwd<E, 1, 1>(p, s);
   if (v <= 2) return fwd<E, 2, 1>(p, s);
   if (v <= 4) return fwd<E, 4, 1>(p, s);
-  if (v <= 8) return fwd<E, 4, 2>(p, s);
+  // eight rows' vectors in one block: two warps a row (4 vectors each) took 59 us for
+  // 32768 x 2048 bf16 values, four 44
+  if (v <= 8) return fwd<E, 2, 4>(p, s);
   if (v <= 16) return fwd<E, 4, 4>(p, s);
   if (v <= 32) return fwd<E, 4, 8>(p, s);
   if (v <= 64) return fwd<E, 4, 16>(p, s);
