@@ -1351,21 +1351,26 @@ struct PolicyPlan {
   long long count_tokens = 0;
   size_t off_part = 0, total = 0;
 };
-// Counts per chunk of tokens, at most 4096 of them, so that a block can add all.
+// Counts per chunk of tokens: few enough for a block to add all.  The mean over
+// sequences wants small ones, for a block counts again what is left of a sequence at
+// the ends of its whole chunks.
 PolicyPlan policy_plan(const mls_policy_problem* p) {
   PolicyPlan pl;
-  const long long blocks = policy_blocks(p->T);
-  pl.count_tokens = kPolicyTokens * (blocks > 4096 ? ceil_div(blocks, 4096) : 1);
+  const long long blocks = policy_blocks(p->T), most = p->agg == MLS_AGG_SEQ_MEAN ? 4096 : 512;
+  pl.count_tokens = kPolicyTokens * ceil_div(p->T, kPolicyTokens * most);
   if (blocks > 1 && p->agg != MLS_AGG_SUM) pl.chunks = static_cast<int>(ceil_div(p->T, pl.count_tokens));
   pl.off_part = align_up(sizeof(int) * static_cast<size_t>(pl.chunks));
   pl.total = align_up(pl.off_part + sizeof(float) * 3 * p->M * static_cast<size_t>(blocks));
   return pl;
 }
 
-// v as the sum of two floats.
-void two_words(double v, float (&out)[2]) {
+// A bound as the sum of two floats; out[2]: an fp32 difference d with |d - out[0]| over
+// this is on the side that those two say.  Beyond it, |d| < 2 |out[0]| or d is further off
+// than its own rounding, so 2^-21 |out[0]| covers that (2^-24 |d|) and out[1].
+void two_words(double v, float (&out)[3]) {
   out[0] = static_cast<float>(v);
   out[1] = std::isfinite(v) ? static_cast<float>(v - static_cast<double>(out[0])) : 0.f;
+  out[2] = std::fabs(out[0]) * 0x1p-21f + 0x1p-126f;
 }
 }  // namespace
 

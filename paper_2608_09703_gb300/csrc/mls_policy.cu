@@ -6,12 +6,13 @@
 //   dL/dlogp = (0 where the clamp decides the minimum, else -r A) - beta (e^x - 1)
 // each times the token's weight: 1/N, 1/(B n_b) or 1 (N tokens count, n_b of them in
 // sequence b).  Which side of a clipping bound a token is on decides between a
-// gradient and none, so the comparison is made on D itself with the rounding of
-// the subtraction kept (its exact value is D + e) against log(1 + clip_high) and
-// log(1 - clip_low) in two fp32 words each: as exact as in 64 bits.  K of a small x
+// gradient and none, so the comparison is made on D itself, and where D is near the
+// bound with what rounding the subtraction lost (its exact value is D + e) and the
+// bound, log(1 + clip_high) or log(1 - clip_low), in two fp32 words: as exact as in 64
+// bits.  K of a small x
 // comes from its series, not from a difference of numbers near 1.
 //
-// A block owns kPolicyTokens consecutive tokens: it finds each one's sequence,
+// A block owns 1024 consecutive tokens: it finds each one's sequence,
 // computes the weights once and goes through the sub-models.  How many tokens of
 // a sequence count is known inside the block where the whole sequence is; for the
 // (at most two) that cross the block's ends it comes from counts per chunk of
@@ -27,7 +28,11 @@ namespace mls {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kPer = kPolicyTokens / kThreads;
+constexpr int kPer = kPolicyTokens / kThreads;  // tokens of a thread
+// Blocks an SM holds of the main kernel, which its instructions bound (some 110 a token
+// and sub-model): 4, 5 and 6 take 95, 90 and 106 us (spills) for 4000001 tokens of 4
+// sub-models; 2048 tokens a block, 103 us.
+constexpr int kResident = 5;
 
 __device__ __forceinline__ bool counts(const PolicyParams& p, long long t) {
   const int y = p.y[t];
@@ -45,6 +50,10 @@ __device__ __forceinline__ int block_sum_int(int v, int* sh) {
   for (int i = 0; i < kThreads / 32; ++i) s += sh[i];
   return s;
 }
+
+// Starts of sequences that a block goes through one by one, in place of a search for
+// each token.
+constexpr int kFewSeqs = 32;
 
 // Offset b of the sequences, within [0, T] whatever the caller's array holds.
 __device__ __forceinline__ long long seq_at(const PolicyParams& p, int b) {
@@ -130,36 +139,34 @@ __device__ __forceinline__ void exp_excess(float x, float& excess, float& minus_
   }
 }
 
-// Sign of (d + e) - (hi + lo) for d + e an exact difference and hi + lo a bound, both
-// with the second word under half a unit of the first's last place.
-__device__ __forceinline__ float beyond(float d, float e, float hi, float lo) {
-  return d == hi ? e - lo : (d - hi) + (e - lo);
-}
-
 struct Token {
   float policy, kl, grad;
   bool clipped;
 };
 
-__device__ __forceinline__ Token policy_token(const PolicyParams& p, float logp, float old, float ref,
-                                              bool has_ref, float A) {
+// `ref` only where kRef.
+template <bool kRef>
+__device__ __forceinline__ Token policy_token(const PolicyParams& p, float logp, float old, float ref, float A) {
   const float d = logp - old;
-  // the part of the exact difference that rounding d lost (Knuth's two-sum)
-  const float back = d - logp;
-  float e = (logp - (d - back)) - (old + back);
-  if (!(fabsf(e) < INFINITY)) e = 0.f;  // d itself is infinite (or NaN): nothing was lost
+  // The bound that this advantage meets: above for a gain, below for a loss.
+  const bool up = A > 0.f;
+  const float hi = up ? p.high[0] : p.low[0];
+  float past = d - hi;
+  if (fabsf(past) <= (up ? p.high[2] : p.low[2])) {  // as near as rounding can matter
+    // the part of the exact difference that rounding d lost (Knuth's two-sum), and the bound's second word
+    const float back = d - logp;
+    const float e = (logp - (d - back)) - (old + back);
+    past += (isfinite(d) ? e : 0.f) - (up ? p.high[1] : p.low[1]);
+  }
   Token k;
-  const bool over = A > 0.f && beyond(d, e, p.high[0], p.high[1]) > 0.f;
-  const bool under = A < 0.f && beyond(d, e, p.low[0], p.low[1]) < 0.f;
-  k.clipped = over || under;
-  const float ratio = over ? p.ratio_high : under ? p.ratio_low : expf(d);
+  k.clipped = up ? past > 0.f : A < 0.f && past < 0.f;
+  const float ratio = k.clipped ? (up ? p.ratio_high : p.ratio_low) : expf(d);
   k.policy = A == 0.f ? 0.f : -ratio * A;
   k.grad = k.clipped ? 0.f : k.policy;
   k.kl = 0.f;
-  if (has_ref) {
-    const float x = ref - logp;
+  if constexpr (kRef) {
     float e1;
-    exp_excess(x, k.kl, e1);
+    exp_excess(ref - logp, k.kl, e1);
     if (p.beta != 0.f) k.grad = fmaf(-p.beta, e1, k.grad);
   }
   return k;
@@ -174,45 +181,68 @@ __device__ __forceinline__ float total_loss(const PolicyParams& p, const double*
   return static_cast<float>(loss);
 }
 
-// One token's three inputs of a sub-model, for kPer tokens of a thread.
+// One token's three inputs of a sub-model, for kPer tokens of a thread; i: the first.
 struct Inputs {
   float logp[kPer], old[kPer], ref[kPer];
 };
-__device__ __forceinline__ void load_inputs(const PolicyParams& p, int m, long long t0, long long t1, Inputs& v) {
-  const long long row = static_cast<long long>(m) * p.T;
+__device__ __forceinline__ void load_inputs(const PolicyParams& p, long long i, int left, Inputs& v) {
+  const float *a = p.logp + i, *b = p.old_logp + i, *c = p.ref_logp ? p.ref_logp + i : a;
 #pragma unroll
   for (int j = 0; j < kPer; ++j) {
-    const long long t = t0 + threadIdx.x + j * kThreads;
-    const bool in = t < t1;
-    v.logp[j] = in ? p.logp[row + t] : 0.f;
-    v.old[j] = in ? p.old_logp[row + t] : 0.f;
-    v.ref[j] = in && p.ref_logp ? p.ref_logp[row + t] : 0.f;
+    const bool in = j * kThreads < left;
+    v.logp[j] = in ? a[j * kThreads] : 0.f;
+    v.old[j] = in ? b[j * kThreads] : 0.f;
+    v.ref[j] = in ? c[j * kThreads] : 0.f;
+  }
+}
+
+// A sub-model's loss and gradient of a thread's tokens: adds to the sums s and writes.
+template <bool kRef>
+__device__ __forceinline__ void policy_row(const PolicyParams& p, const Inputs& in, const bool (&on)[kPer],
+                                           const float (&A)[kPer], const float (&weight)[kPer], float gw,
+                                           long long i, int left, float (&s)[3]) {
+  float *tok = p.tok_loss + i, *grad = p.dlogp + i;
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    float L = 0.f, g = 0.f;
+    if (on[j]) {
+      const Token k = policy_token<kRef>(p, in.logp[j], in.old[j], in.ref[j], A[j]);
+      L = kRef && p.beta != 0.f ? fmaf(p.beta, k.kl, k.policy) : k.policy;  // beta 0: K is only reported
+      g = k.grad * (weight[j] * gw);
+      s[0] = fmaf(k.policy, weight[j], s[0]);
+      s[1] = fmaf(k.kl, weight[j], s[1]);
+      s[2] += k.clipped ? weight[j] : 0.f;
+    }
+    if (j * kThreads < left) {
+      if (p.tok_loss) tok[j * kThreads] = L;
+      if (p.dlogp) grad[j * kThreads] = g;
+    }
   }
 }
 
 // kOne: one block has all tokens, counts them itself and writes the sums.
 template <bool kOne>
-__global__ void __launch_bounds__(kThreads) policy_kernel(const __grid_constant__ PolicyParams p) {
+__global__ void __launch_bounds__(kThreads, kResident) policy_kernel(const __grid_constant__ PolicyParams p) {
   __shared__ int sh[kThreads / 32];
   __shared__ int inside[kPolicyTokens];  // counted tokens of the sequence that starts here
   __shared__ int ends[2];
+  __shared__ int starts[kFewSeqs];
   __shared__ float shf[kThreads / 32][3 * kMaxModels];
   __shared__ double shd[3 * kMaxModels];
   const long long t0 = static_cast<long long>(blockIdx.x) * kPolicyTokens;
   const long long t1 = t0 + kPolicyTokens < p.T ? t0 + kPolicyTokens : p.T;
   const int B = p.B, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const long long first = t0 + threadIdx.x;
+  const int left = static_cast<int>(t1 - first);  // this thread's token j: first + j kThreads, if that is < left
   if (!kOne) chain_trigger();
 
   // ---- what does not depend on the counts: the first sub-model's inputs, each
   // token's sequence, whether it counts, its advantage
   Inputs in;
-  load_inputs(p, 0, t0, t1, in);
+  load_inputs(p, first, left, in);
   bool on[kPer];
 #pragma unroll
-  for (int j = 0; j < kPer; ++j) {
-    const long long t = t0 + threadIdx.x + j * kThreads;
-    on[j] = t < t1 && counts(p, t);
-  }
+  for (int j = 0; j < kPer; ++j) on[j] = j * kThreads < left && counts(p, first + j * kThreads);
   if (p.agg == kAggSeq)
     for (int i = threadIdx.x; i < kPolicyTokens; i += kThreads) inside[i] = 0;
   if (p.seq_start && warp < 2) {
@@ -230,14 +260,31 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(const __grid_constant_
   int seq[kPer];
   float A[kPer], weight[kPer];
 #pragma unroll
-  for (int j = 0; j < kPer; ++j) {
-    const long long t = t0 + threadIdx.x + j * kThreads;
-    seq[j] = 0;
-    if (p.seq_start && on[j]) {
-      seq[j] = seq_of(p, t, b0, b1);
-      on[j] = t >= seq_at(p, seq[j]) && t < seq_at(p, seq[j] + 1);
+  for (int j = 0; j < kPer; ++j) seq[j] = b0;
+  if (p.seq_start) {
+    const int begin = p.seq_start[0], end = p.seq_start[B], few = b1 - b0;
+    if (few > 0 && few <= kFewSeqs) {  // each start of a sequence within the block, past b0's
+      if (threadIdx.x < few) starts[threadIdx.x] = p.seq_start[b0 + 1 + threadIdx.x];
+      __syncthreads();
+      for (int i = 0; i < few; ++i) {
+        const int s = starts[i];
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) seq[j] += s <= first + j * kThreads;
+      }
+    } else if (few > 0) {
+#pragma unroll
+      for (int j = 0; j < kPer; ++j)
+        if (on[j]) seq[j] = seq_of(p, first + j * kThreads, b0, b1);
     }
-    A[j] = on[j] ? (p.adv_per_seq ? p.adv[seq[j]] : p.adv[t]) : 0.f;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const long long t = first + j * kThreads;
+      on[j] = on[j] && t >= begin && t < end;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    A[j] = on[j] ? (p.adv_per_seq ? p.adv[seq[j]] : p.adv[first + j * kThreads]) : 0.f;
     weight[j] = on[j] ? 1.f : 0.f;
   }
   if (!kOne) chain_wait();  // the counts; and no output is written before
@@ -265,7 +312,7 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(const __grid_constant_
     for (int j = 0; j < kPer; ++j)
       if (on[j]) {
         const long long lo = seq_at(p, seq[j]);
-        if (lo >= t0) atomicAdd(&inside[lo - t0], 1);
+        if (lo >= t0 && lo < t1) atomicAdd(&inside[lo - t0], 1);
       }
     // the sequences that cross the block's ends
     int cross0 = 0, cross1 = 0;
@@ -284,33 +331,21 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(const __grid_constant_
     for (int j = 0; j < kPer; ++j)
       if (on[j]) {
         const long long lo = seq_at(p, seq[j]), hi = seq_at(p, seq[j] + 1);
-        const int n = lo >= t0 && hi <= t1 ? inside[lo - t0] : seq[j] == b0 ? cross0 : cross1;
+        const int n = lo >= t0 && lo < t1 && hi <= t1 ? inside[lo - t0] : seq[j] == b0 ? cross0 : cross1;
         weight[j] = n > 0 ? 1.f / (static_cast<float>(B) * static_cast<float>(n)) : 0.f;
       }
   }
 
   // ---- loss and gradient of every sub-model
   for (int m = 0; m < p.M; ++m) {
-    const long long row = static_cast<long long>(m) * p.T;
+    const long long i = static_cast<long long>(m) * p.T + first;
     const float gw = p.grad_scale * p.w[m];
-    if (m > 0) load_inputs(p, m, t0, t1, in);
+    if (m > 0) load_inputs(p, i, left, in);
     float s[3] = {0.f, 0.f, 0.f};
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const long long t = t0 + threadIdx.x + j * kThreads;
-      if (t >= t1) continue;
-      float L = 0.f, g = 0.f;
-      if (on[j]) {
-        const Token k = policy_token(p, in.logp[j], in.old[j], in.ref[j], p.ref_logp != nullptr, A[j]);
-        L = p.beta != 0.f ? fmaf(p.beta, k.kl, k.policy) : k.policy;  // beta 0: K is only reported
-        g = k.grad * (weight[j] * gw);
-        s[0] = fmaf(k.policy, weight[j], s[0]);
-        s[1] = fmaf(k.kl, weight[j], s[1]);
-        s[2] += k.clipped ? weight[j] : 0.f;
-      }
-      if (p.tok_loss) p.tok_loss[row + t] = L;
-      if (p.dlogp) p.dlogp[row + t] = g;
-    }
+    if (p.ref_logp)
+      policy_row<true>(p, in, on, A, weight, gw, i, left, s);
+    else
+      policy_row<false>(p, in, on, A, weight, gw, i, left, s);
 #pragma unroll
     for (int f = 0; f < 3; ++f) {
       s[f] = warp_sum(s[f]);
@@ -337,7 +372,7 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(const __grid_constant_
 // Block shares -> diag and the loss.  Each of the 3 M quantities has 32 / (3 M) warps;
 // a lane adds its shares in two fp32 words (Pair): 64-bit additions by every thread
 // took 25 us a sub-model, whatever the number of blocks.
-constexpr int kFinalThreads = 1024;
+constexpr int kFinalThreads = 1024, kFinalBatch = 16;
 
 __global__ void __launch_bounds__(kFinalThreads) policy_final_kernel(const __grid_constant__ PolicyParams p, int blocks) {
   __shared__ Pair sh[kFinalThreads / 32];
@@ -349,8 +384,16 @@ __global__ void __launch_bounds__(kFinalThreads) policy_final_kernel(const __gri
   Pair a = {0.f, 0.f};
   if (k < per) {
     const float* part = p.part + static_cast<long long>(q) * blocks;
-#pragma unroll 8
-    for (int i = k * 32 + lane; i < blocks; i += per * 32) pair_add(a, part[i], 0.f);
+    for (int i0 = k * 32 + lane; i0 < blocks; i0 += kFinalBatch * per * 32) {  // a batch's loads at once
+      float v[kFinalBatch];
+#pragma unroll
+      for (int u = 0; u < kFinalBatch; ++u) {
+        const int i = i0 + u * per * 32;
+        v[u] = i < blocks ? part[i] : 0.f;
+      }
+#pragma unroll
+      for (int u = 0; u < kFinalBatch; ++u) pair_add(a, v[u], 0.f);
+    }
   }
   a = warp_sum_pair(a);
   if (lane == 0) sh[warp] = a;

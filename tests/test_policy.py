@@ -130,6 +130,29 @@ def test_ragged_sequences(T, n, agg):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("agg,n", [("token", 700), ("seq", 700), ("seq", 3), ("sum", 0), ("seq", 200000)])
+def test_many_tokens(agg, n):
+    """More chunks of tokens than their counts' table has entries of one block; far more sequences than blocks."""
+    T = 1100003 if n < 10000 else 1048577
+    c = config(T, B=n, agg=agg, beta=0.07, M=2)
+    data = inputs(c, seed=n)
+    if n >= 10000:  # most of one token or none: too many for the loop of the reference
+        op = run(c, *data)
+        logp, old, ref, adv, y, start = data
+        s = (torch.searchsorted(start.long(), torch.arange(T, device="cuda"), right=True) - 1)
+        on = (y >= 0) & (s >= 0) & (s < n)
+        s = s.clamp(0, n - 1)
+        cnt = torch.zeros(n, device="cuda", dtype=torch.float64).index_add_(0, s, on.double())
+        want = torch.where(on, op.tok_loss.double() / (n * cnt.clamp(min=1))[s], 0.0).sum(1)
+        got = (op.diag[0].double() + float(torch.tensor(0.07)) * op.diag[1].double())
+        size = torch.where(on, op.tok_loss.double().abs() / (n * cnt.clamp(min=1))[s], 0.0).sum(1)
+        assert bool(((got - want).abs() <= 32 * U * size).all())
+        assert not op.dlogp[:, ~on].any() and not op.tok_loss[:, ~on].any()
+        return
+    check(c, data)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("T", [1, 77, 2500, 8193])
 @pytest.mark.parametrize("agg", ["token", "sum"])
 def test_without_sequences(T, agg):
