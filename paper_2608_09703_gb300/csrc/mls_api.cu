@@ -501,15 +501,15 @@ int encode(CUtensorMap* map, const void* ptr, int elt, long long cols, long long
   return MLS_OK;
 }
 
-// Row-major fp32 output [copies, rows, cols] of dense rows, `stride` floats
-// between copies, as boxes of 32 x 32 for TMA stores.
-int encode_out(CUtensorMap* map, float* ptr, long long cols, long long rows, int copies,
+// Row-major output [copies, rows, cols] of dense rows, `stride` values between copies,
+// as boxes of 128 bytes x 32 rows for TMA stores; fp32, or bf16 if elt is 2.
+int encode_out(CUtensorMap* map, void* ptr, int elt, long long cols, long long rows, int copies,
                long long stride) {
   const cuuint64_t dims[3] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows),
                               static_cast<cuuint64_t>(copies)};
-  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(cols) * 4, static_cast<cuuint64_t>(stride) * 4};
-  const cuuint32_t box[3] = {32, 32, 1}, estr[3] = {1, 1, 1};
-  const CUresult r = g_encode(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, ptr, dims, strides, box, estr,
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(cols) * elt, static_cast<cuuint64_t>(stride) * elt};
+  const cuuint32_t box[3] = {static_cast<cuuint32_t>(128 / elt), 32, 1}, estr[3] = {1, 1, 1};
+  const CUresult r = g_encode(map, elt == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, ptr, dims, strides, box, estr,
                               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? MLS_OK : fail(MLS_ERR_CUDA, "cuTensorMapEncodeTiled (output)");
@@ -593,12 +593,14 @@ int timed(const char* name, cudaStream_t s, F&& launch) {
 
 // The vocabulary groups of a backward pass: `launch_grad(group)` launches the head
 // kernel that leaves dL/dz of the group's columns in G (`hp` is completed for it
-// here), then one GEMM launch forms that group's dW and adds its share of dH, both
-// fp32.
+// here), then one GEMM launch forms that group's dW and adds its share of dH.
+// The gradients are fp32, or bf16 (`out16`, of bf16 inputs), rounded once: by the
+// GEMM, by the sum of a split reduction's copies, or, for dH over several groups, at
+// the end from the fp32 sums in `acc` (T sum of d_m floats, one sub-model after the other).
 template <class F>
 int backward_groups(const mls_problem* p, const Plan& pl, const DeviceState& dev, const void* const* H,
-                    const void* const* W, HeadParams& hp, void* G, float* const* dH, float* const* dW,
-                    float* split_ws, cudaStream_t s, F&& launch_grad) {
+                    const void* const* W, HeadParams& hp, void* G, void* const* dH, void* const* dW,
+                    bool out16, float* acc, float* split_ws, cudaStream_t s, F&& launch_grad) {
   int rc;
   const bool tf32 = pl.elt == 4;
   const int KE = 128 / pl.elt;
@@ -607,6 +609,11 @@ int backward_groups(const mls_problem* p, const Plan& pl, const DeviceState& dev
   GemmParams gw, gh, gb;
   std::memset(&gw, 0, sizeof gw);
   std::memset(&gh, 0, sizeof gh);
+  long long acc_off[kMaxModels], acc_floats = 0;
+  for (int m = 0; m < p->M; ++m) {
+    acc_off[m] = acc_floats;
+    acc_floats += p->T * p->d[m];
+  }
   const CUtensorMapSwizzle mn_swizzle =
       tf32 ? CU_TENSOR_MAP_SWIZZLE_128B_ATOM_32B : CU_TENSOR_MAP_SWIZZLE_128B;
   for (int m = 0; m < p->M; ++m) {
@@ -647,7 +654,10 @@ int backward_groups(const mls_problem* p, const Plan& pl, const DeviceState& dev
       q.K = static_cast<int>(dh ? gc : p->T);
       q.a_map = q.b_map = i;
       q.b_k0 = dh ? static_cast<int>(c0) : 0;
-      float* out = dh ? dH[m] : dW[m] + c0 * p->d[m];
+      const bool in_acc = out16 && dh && pl.ngroups > 1;
+      int elt = out16 && !in_acc ? 2 : 4;
+      char* out = static_cast<char*>(in_acc ? acc + acc_off[m] : dh ? dH[m] : dW[m]) +
+                  (dh ? 0 : static_cast<size_t>(c0) * p->d[m] * elt);
       q.accumulate = dh && g > 0 ? 1 : 0;
       q.a_mn = dh ? 0 : 1;
       q.tiles_m = static_cast<int>(ceil_div(q.Mrows, 2 * kGemmBM));
@@ -658,15 +668,19 @@ int backward_groups(const mls_problem* p, const Plan& pl, const DeviceState& dev
       if (is_long && cut.ksplit > 1) {  // the units write their own sums, added up below
         q.ksplit = cut.ksplit;
         q.kb_split = cut.kb_split;
-        sum.out[m] = out;
+        sum.out[m] = reinterpret_cast<float*>(out);
         sum.n4[m] = static_cast<long long>(q.Mrows) * p->d[m] / 4;
         sum.accumulate = q.accumulate;
-        out = split_ws + split_off;
+        sum.out16 = elt == 2;
+        sum.part[m] = split_ws + split_off;
+        out = reinterpret_cast<char*>(split_ws + split_off);
+        elt = 4;
         q.accumulate = 0;
-        sum.part[m] = out;
         split_off += static_cast<long long>(q.Mrows) * p->d[m];
       }
-      if (encode_out(&gb.mapC[i], out, p->d[m], q.Mrows, q.ksplit > 1 ? q.ksplit : 1,
+      q.out16 = elt == 2;
+      gb.any16 |= q.out16;
+      if (encode_out(&gb.mapC[i], out, elt, p->d[m], q.Mrows, q.ksplit > 1 ? q.ksplit : 1,
                      q.ksplit > 1 ? cut.part_floats / cut.ksplit : static_cast<long long>(q.Mrows) * p->d[m]))
         return MLS_ERR_CUDA;
       if (i == M - 1) n_long = units;
@@ -686,7 +700,18 @@ int backward_groups(const mls_problem* p, const Plan& pl, const DeviceState& dev
       if ((rc = timed("split_sum", s, [&] { return launch_split_sum(sum, s); }))) return rc;
     }
   }
-  return MLS_OK;
+  if (!out16 || pl.ngroups == 1) return MLS_OK;
+  SplitSumParams round;  // of one copy
+  std::memset(&round, 0, sizeof round);
+  round.nprob = p->M;
+  round.nsplit = 1;
+  round.out16 = 1;
+  for (int m = 0; m < p->M; ++m) {
+    round.part[m] = acc + acc_off[m];
+    round.out[m] = static_cast<float*>(dH[m]);
+    round.n4[m] = p->T * p->d[m] / 4;
+  }
+  return timed("round_dh", s, [&] { return launch_split_sum(round, s); });
 }
 
 }  // namespace
@@ -815,15 +840,20 @@ extern "C" int mls_head_loss_bwd(const mls_problem* p, const void* const* H, con
   hp.one_minus_alpha = 1.0f - p->alpha;
   hp.alpha_over_tau = p->alpha / p->tau;
 
+  void *oH[kMaxModels], *oW[kMaxModels];
+  for (int m = 0; m < p->M; ++m) {
+    oH[m] = dH[m];
+    oW[m] = dW[m];
+  }
   return backward_groups(
-      p, pl, *dev, H, W, hp, G, dH, dW, reinterpret_cast<float*>(wsb + pl.off_split), s,
+      p, pl, *dev, H, W, hp, G, oH, oW, false, nullptr, reinterpret_cast<float*>(wsb + pl.off_split), s,
       [&](long long) { return timed("head_bwd", s, [&] { return launch_head_bwd(hp, tf32, p->tau == 1.0f, s); }); });
 }
 
 // ------------------------------------------------------------------ log-probabilities
 namespace {
 // Workspace of the log-probability calls: the forward's partial states, or the backward's
-// dL/dz of a vocabulary group, the splits' copies, and dH and dW in fp32.
+// dL/dz of a vocabulary group, the splits' copies, and dH in fp32 while groups add to it.
 struct LogpPlan {
   Plan head;
   size_t off_acc = 0, total = 0;
@@ -834,7 +864,8 @@ LogpPlan logp_plan(const mls_problem* p, int pairs, int gemm_pairs) {
   size_t sum_d = 0;
   for (int m = 0; m < p->M; ++m) sum_d += p->d[m];
   lp.off_acc = align_up(lp.head.bwd_bytes);
-  lp.total = align_up(lp.off_acc + sizeof(float) * sum_d * static_cast<size_t>(p->T + p->V));
+  lp.total = lp.off_acc;
+  if (lp.head.ngroups > 1) lp.total = align_up(lp.off_acc + sizeof(float) * sum_d * static_cast<size_t>(p->T));
   const size_t fwd = sizeof(float) * static_cast<size_t>(lp.head.nparts) * kLogpFields * p->M * p->T;
   if (fwd > lp.total) lp.total = align_up(fwd);
   return lp;
@@ -928,29 +959,11 @@ extern "C" int mls_head_logp_bwd(const mls_problem* p, const void* const* H, con
   hp.stats = lse;
   hp.dlogp = dlogp;
   hp.neg_inv_tau = static_cast<float>(-1.0 / static_cast<double>(p->tau));
-  float* acc = reinterpret_cast<float*>(wsb + lp.off_acc);
-  float *aH[kMaxModels], *aW[kMaxModels];
-  SplitSumParams th, tw;
-  std::memset(&th, 0, sizeof th);
-  std::memset(&tw, 0, sizeof tw);
-  th.nprob = tw.nprob = p->M;
-  for (int m = 0; m < p->M; ++m) {
-    th.part[m] = aH[m] = acc;
-    th.out[m] = static_cast<float*>(dH[m]);
-    th.n4[m] = p->T * p->d[m] / 4;
-    acc += p->T * p->d[m];
-    tw.part[m] = aW[m] = acc;
-    tw.out[m] = static_cast<float*>(dW[m]);
-    tw.n4[m] = p->V * p->d[m] / 4;
-    acc += p->V * p->d[m];
-  }
-  rc = backward_groups(p, pl, *dev, H, W, hp, wsb + pl.off_G, aH, aW,
-                       reinterpret_cast<float*>(wsb + pl.off_split), s, [&](long long g) {
-                         return timed("logp_bwd", s, [&] { return launch_logp_bwd(hp, g > 0, s); });
-                       });
-  if (rc) return rc;
-  if ((rc = timed("to_bf16", s, [&] { return launch_to_bf16(th, s); }))) return rc;
-  return timed("to_bf16", s, [&] { return launch_to_bf16(tw, s); });
+  return backward_groups(p, pl, *dev, H, W, hp, wsb + pl.off_G, dH, dW, true,
+                         reinterpret_cast<float*>(wsb + lp.off_acc),
+                         reinterpret_cast<float*>(wsb + pl.off_split), s, [&](long long g) {
+                           return timed("logp_bwd", s, [&] { return launch_logp_bwd(hp, g > 0, s); });
+                         });
 }
 
 extern "C" int mls_get_status(mls_stream_t stream) {

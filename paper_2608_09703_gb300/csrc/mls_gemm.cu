@@ -476,7 +476,9 @@ __device__ __noinline__ void epilogue_stats(const GemmProblem& pr, const CUtenso
 // GEMM, whose mapC is 2-D), otherwise every one has the plain epilogue (3-D
 // mapC); with both in one kernel the training GEMMs would take the statistics
 // epilogue's 118 registers instead of 80.
-template <int kAMode, bool kStats>
+// kOut16: problems with bf16 output among them (GemmProblem::out16), rounded once from
+// the fp32 accumulators; in a kernel of their own, the others' stays as it is.
+template <int kAMode, bool kStats, bool kOut16>
 __device__ __forceinline__ void gemm_epilogue(const GemmParams& p, uint32_t base, uint32_t tmem,
                                               uint32_t rank, int warp, int lane,
                                               volatile int* abort_flag) {
@@ -512,6 +514,36 @@ __device__ __forceinline__ void gemm_epilogue(const GemmParams& p, uint32_t base
         // per 256x256 tile, more than the MMAs of a tile with K < 2500.
         float v[32];
         const int ncols = row0 < pr.Mrows ? pr.Ncols - tn * kGemmBN : 0;
+        if (kOut16 && pr.out16) {
+          // 32 x 64 bf16 values in a staging buffer: whole 128-byte lines again
+#pragma unroll 1
+          for (int c = 0; c * 64 < kGemmBN && c * 64 < ncols; ++c) {
+            uint32_t w[32];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              tmem_ld32(tl + acc * kGemmBN + c * 64 + h * 32, v);
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+                w[16 * h + i] = *reinterpret_cast<const uint32_t*>(&b);
+              }
+            }
+            const uint32_t buf = stage + (stores & 1u) * GemmSmem::kChunk;
+            if (lane == 0) bulk_wait_read<1>();  // the store that last used this buffer has read it
+            __syncwarp();
+            const uint32_t rowaddr = buf + lane * 128;
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+              st_shared_v4(rowaddr + ((q ^ (lane & 7)) << 4), w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+              tma_store_3d(&p.mapC[uc.prob], buf, tn * kGemmBN + c * 64, row0, uc.ks);
+              bulk_commit();
+            }
+            ++stores;
+          }
+        } else
 #pragma unroll 1
         for (int c = 0; c * 32 < kGemmBN && c * 32 < ncols; ++c) {
           tmem_ld32(tl + acc * kGemmBN + c * 32, v);
@@ -545,7 +577,7 @@ __device__ __forceinline__ void gemm_epilogue(const GemmParams& p, uint32_t base
   if (stores && lane == 0) bulk_wait_all();  // staging must outlive the stores reading it
 }
 
-template <bool kTF32, int kAMode, bool kBMN, bool kStats>
+template <bool kTF32, int kAMode, bool kBMN, bool kStats, bool kOut16 = false>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
     gemm_kernel(const __grid_constant__ GemmParams p) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -599,7 +631,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
     if (lane == 0 && rank == 0) gemm_mma<kTF32, kAMode, kBMN>(p, base, tmem, abort_flag);
     __syncwarp();
   } else {
-    gemm_epilogue<kAMode, kStats>(p, base, tmem, rank, warp, lane, abort_flag);
+    gemm_epilogue<kAMode, kStats, kOut16>(p, base, tmem, rank, warp, lane, abort_flag);
   }
 
   tc_fence_before();
@@ -636,6 +668,12 @@ cudaError_t launch_gemm_stats(GemmParams& p, bool tf32, int grid, cudaStream_t s
 cudaError_t launch_gemm_mixed(GemmParams& p, bool tf32, int grid, cudaStream_t s) {
   if (p.total_tiles <= 0 || grid <= 0) return cudaSuccess;
   number_units(p);
+  if (p.any16) {  // bf16 operands
+    if (p.chained)
+      return launch_chained(gemm_kernel<false, 2, true, false, true>, dim3(grid), dim3(kGemmThreads), kGemmSmem, s, p);
+    gemm_kernel<false, 2, true, false, true><<<grid, kGemmThreads, kGemmSmem, s>>>(p);
+    return cudaGetLastError();
+  }
   if (!p.chained) {
     if (tf32)
       gemm_kernel<true, 2, true, false><<<grid, kGemmThreads, kGemmSmem, s>>>(p);
@@ -664,13 +702,13 @@ int gemm_max_active_pairs() {
 
 cudaError_t setup_gemm_kernels() {
   cudaError_t e;
-#define MLS_SET(TF, AM, BM, ST)                                                                 \
-  e = cudaFuncSetAttribute(gemm_kernel<TF, AM, BM, ST>,                                         \
+#define MLS_SET(...)                                                                            \
+  e = cudaFuncSetAttribute(gemm_kernel<__VA_ARGS__>,                                            \
                            cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmem);             \
   if (e != cudaSuccess) return e;                                                               \
   {                                                                                             \
     cudaFuncAttributes fa;                                                                      \
-    e = cudaFuncGetAttributes(&fa, gemm_kernel<TF, AM, BM, ST>);                                \
+    e = cudaFuncGetAttributes(&fa, gemm_kernel<__VA_ARGS__>);                                   \
     if (e != cudaSuccess) return e;                                                             \
     if (fa.maxThreadsPerBlock < kGemmThreads) return cudaErrorLaunchOutOfResources;             \
   }
@@ -678,6 +716,7 @@ cudaError_t setup_gemm_kernels() {
   MLS_SET(false, 0, false, true)
   MLS_SET(true, 2, true, false)
   MLS_SET(false, 2, true, false)
+  MLS_SET(false, 2, true, false, true)
 #undef MLS_SET
   return cudaSuccess;
 }

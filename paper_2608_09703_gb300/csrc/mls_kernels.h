@@ -198,6 +198,7 @@ struct GemmProblem {
   float epi_scale;
   float* stats;
   long long stats_ld;
+  int out16;                     // C is bf16 (launch_gemm_mixed with some such problem, accumulate 0)
   int a_mn;                      // A is MN-major (read by launches that take the layout per problem)
   // Wide units (launch_gemm_mixed only): a unit is two adjacent column tiles
   // (tn, tn + 1) that share the A tile of each stage and take both TMEM
@@ -224,7 +225,7 @@ struct GemmParams {
   CUtensorMap mapA[kGemmMaxProblems];
   CUtensorMap mapB[kGemmMaxProblems];
   // C fp32, 128B swizzle.  kEpiPlain: [ksplit, Mrows, Ncols], box {32, 32, 1};
-  // kEpiSoftmax: [Mrows, Ncols], box {32, 32}.
+  // kEpiSoftmax: [Mrows, Ncols], box {32, 32}.  GemmProblem::out16: bf16, box {64, 32, 1}.
   CUtensorMap mapC[kGemmMaxProblems];
   int nprob;
   GemmProblem prob[kGemmMaxProblems];
@@ -241,6 +242,7 @@ struct GemmParams {
   int n_long;
   int catchup;
   int chained;                   // launch_gemm_mixed: may start before its predecessor has completed
+  int any16;                     // some problem is out16
 };
 
 // ------------------------------------------------------------------ pairwise evaluation
@@ -425,6 +427,7 @@ cudaError_t launch_final(const double* block_sum, const long long* block_cnt, in
 // every sub-model, in split order (deterministic); see GemmProblem::ksplit.
 struct SplitSumParams {
   int nprob, nsplit, accumulate;
+  int out16;                     // out_m is bf16 (accumulate 0)
   long long stride;              // floats between splits
   const float* part[kMaxModels];
   float* out[kMaxModels];
@@ -442,8 +445,6 @@ struct LogpMergeParams {
   int* status;
 };
 cudaError_t launch_logp_merge(const LogpMergeParams& p, cudaStream_t s);
-// out[m][i] = part[m][i] rounded to bf16, n4[m] float4s each (SplitSumParams::out as bf16).
-cudaError_t launch_to_bf16(const SplitSumParams& p, cudaStream_t s);
 cudaError_t launch_count(const int* y, long long T, long long V, float* inv_n, int* status,
                          cudaStream_t s);
 

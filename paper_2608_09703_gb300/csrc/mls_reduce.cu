@@ -299,7 +299,13 @@ __global__ void __launch_bounds__(kSplitSumThreads)
       a.z += b.z;
       a.w += b.w;
     }
-    out[i] = a;
+    if (p.out16) {
+      __nv_bfloat162* o = reinterpret_cast<__nv_bfloat162*>(p.out[m]) + 2 * i;
+      o[0] = __floats2bfloat162_rn(a.x, a.y);
+      o[1] = __floats2bfloat162_rn(a.z, a.w);
+    } else {
+      out[i] = a;
+    }
   }
 }
 
@@ -331,21 +337,6 @@ __global__ void __launch_bounds__(kLogpMergeThreads)
   p.lse[i] = fmaf(m, p.inv_tau, ls);
   // relative to the maximum: nothing cancels where the token has nearly all the mass
   p.logp[i] = y >= 0 && y < p.V ? (zy - m) * p.inv_tau - ls : 0.f;
-}
-
-__global__ void __launch_bounds__(kSplitSumThreads)
-    to_bf16_kernel(const __grid_constant__ SplitSumParams p) {
-  chain_trigger();
-  chain_wait();
-  const int m = blockIdx.y;
-  const float4* in = reinterpret_cast<const float4*>(p.part[m]);
-  __nv_bfloat162* out = reinterpret_cast<__nv_bfloat162*>(p.out[m]);
-  for (long long i = static_cast<long long>(blockIdx.x) * kSplitSumThreads + threadIdx.x; i < p.n4[m];
-       i += static_cast<long long>(gridDim.x) * kSplitSumThreads) {
-    const float4 a = in[i];
-    out[2 * i] = __floats2bfloat162_rn(a.x, a.y);
-    out[2 * i + 1] = __floats2bfloat162_rn(a.z, a.w);
-  }
 }
 
 constexpr int kCountThreads = 1024;
@@ -396,15 +387,6 @@ cudaError_t launch_logp_merge(const LogpMergeParams& p, cudaStream_t s) {
   if (n <= 0) return cudaSuccess;
   return launch_chained(logp_merge_kernel, dim3(static_cast<unsigned>((n + kLogpMergeThreads - 1) / kLogpMergeThreads)),
                         dim3(kLogpMergeThreads), 0, s, p);
-}
-
-cudaError_t launch_to_bf16(const SplitSumParams& p, cudaStream_t s) {
-  long long most = 0;
-  for (int m = 0; m < p.nprob; ++m) most = p.n4[m] > most ? p.n4[m] : most;
-  if (most <= 0) return cudaSuccess;
-  const long long blocks = (most + kSplitSumThreads - 1) / kSplitSumThreads;
-  const dim3 grid(static_cast<unsigned>(blocks < 4096 ? blocks : 4096), p.nprob);
-  return launch_chained(to_bf16_kernel, grid, dim3(kSplitSumThreads), 0, s, p);
 }
 
 cudaError_t launch_count(const int* y, long long T, long long V, float* inv_n, int* status,
