@@ -571,7 +571,11 @@ __device__ __forceinline__ void gemm_epilogue(const GemmParams& p, uint32_t base
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_remote(map_to_rank(GemmSmem::acce(base, acc), 0));
+      if (lane == 0) {
+        const uint32_t bar = map_to_rank(GemmSmem::acce(base, acc), 0);
+        if constexpr (kOut16) mbar_arrive_remote_light(bar);
+        else mbar_arrive_remote(bar);
+      }
     }
   }
   if (stores && lane == 0) bulk_wait_all();  // staging must outlive the stores reading it

@@ -35,6 +35,7 @@
 //   backward dL/dz = (dL/dlogp / tau) (e_y - softmax(z / tau)), a factor per token
 #include "mls_device.cuh"
 #include "mls_kernels.h"
+#include "mls_vec.cuh"
 
 namespace mls {
 namespace {
@@ -659,39 +660,54 @@ __device__ __forceinline__ void bwd_epilogue(const HeadParams& p, uint32_t base,
 }
 
 // ------------------------------------------------------------------ log-probabilities
+// Frees the accumulator that this warp has read (tmem_ld128 waits for its loads).
+__device__ __forceinline__ void logp_release(uint32_t base, uint32_t& acc, uint32_t& acc_par, int lane) {
+  tc_fence_before();
+  __syncwarp();
+  if (lane == 0) mbar_arrive_remote_light(map_to_rank(HeadSmem::acce(base, acc), 0));
+  acc ^= 1u;
+  if (acc == 0) acc_par ^= 1u;
+}
+
+// The epilogues read a thread's 128 columns of a tile at once and free the accumulator
+// before they compute: 32 columns at a time, read as they were needed, a tile took 6360
+// cycles of which the MMAs of d = 512 filled 4096.
+
 // One sub-model's tile: running maximum m of z, s = sum of 2^((z - m) Lt).
 template <bool kMasked>
-__device__ __forceinline__ void logp_tile(uint32_t ta, int nvalid, int yl, float Lt, float& m, float& s,
+__device__ __forceinline__ void logp_tile(float (&v)[128], int nvalid, int yl, float Lt, float& m, float& s,
                                           float& zy) {
-  float v[32];
+  if (kMasked) {
 #pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    if (kMasked && c * 32 >= nvalid) break;
-    tmem_ld32(ta + c * 32, v);
-    if (kMasked) {
+    for (int i = 0; i < 128; ++i)
+      if (i >= nvalid) v[i] = -INFINITY;
+  }
+  float mx[8];
 #pragma unroll
-      for (int i = 0; i < 32; ++i)
-        if (c * 32 + i >= nvalid) v[i] = -INFINITY;
-    }
-    float mx[4] = {v[0], v[1], v[2], v[3]};
+  for (int i = 0; i < 8; ++i) mx[i] = v[i];
 #pragma unroll
-    for (int i = 4; i < 32; ++i) mx[i & 3] = fmaxf(mx[i & 3], v[i]);
-    const float cmax = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-    if (cmax > m) {
-      s *= fast_exp2((m - cmax) * Lt);
-      m = cmax;
-    }
-    const float b = -m * Lt;
-    float s4[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int i = 8; i < 128; ++i) mx[i & 7] = fmaxf(mx[i & 7], v[i]);
 #pragma unroll
-    for (int i = 0; i < 32; ++i) s4[i & 3] += fast_exp2(fmaf(v[i], Lt, b));
-    s += (s4[0] + s4[1]) + (s4[2] + s4[3]);
-    const int r = yl - c * 32;
-    if (static_cast<unsigned>(r) < 32u) {
+  for (int w = 4; w > 0; w >>= 1)
 #pragma unroll
-      for (int i = 0; i < 32; ++i)
-        if (i == r) zy = v[i];
-    }
+    for (int i = 0; i < w; ++i) mx[i] = fmaxf(mx[i], mx[i + w]);
+  if (mx[0] > m) {
+    s *= fast_exp2((m - mx[0]) * Lt);
+    m = mx[0];
+  }
+  const F2 L2 = f2(Lt), b2 = f2(-m * Lt);
+  F2 acc[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < 64; ++i) {
+    float lo, hi;
+    f2_split(f2_fma(f2(v[2 * i], v[2 * i + 1]), L2, b2), lo, hi);
+    acc[i & 3] = f2_add(acc[i & 3], f2(fast_exp2(lo), fast_exp2(hi)));
+  }
+  s += f2_sum(f2_add(f2_add(acc[0], acc[1]), f2_add(acc[2], acc[3])));
+  if (static_cast<unsigned>(yl) < 128u) {
+#pragma unroll
+    for (int i = 0; i < 128; ++i)
+      if (i == yl) zy = v[i];
   }
 }
 
@@ -722,12 +738,13 @@ __device__ __forceinline__ void logp_fwd_epilogue(const HeadParams& p, uint32_t 
           aborted = true;
           break;
         }
-        const uint32_t ta = tl + acc * kHeadBN;
+        float v[128];
+        tmem_ld128(tl + acc * kHeadBN, v);
+        logp_release(base, acc, acc_par, lane);
         if (nvalid == 128)
-          logp_tile<false>(ta, 128, yl, p.Ltau, m[j], s[j], zy[j]);
+          logp_tile<false>(v, 128, yl, p.Ltau, m[j], s[j], zy[j]);
         else if (nvalid > 0)
-          logp_tile<true>(ta, nvalid, yl, p.Ltau, m[j], s[j], zy[j]);
-        epi_release(base, acc, acc_par, lane);
+          logp_tile<true>(v, nvalid, yl, p.Ltau, m[j], s[j], zy[j]);
       }
     }
   }
@@ -761,16 +778,22 @@ __device__ __forceinline__ void logp_fwd_epilogue(const HeadParams& p, uint32_t 
 
 // dL/dz of one tile: c (softmax(z / tau) - e_y), c = -dL/dlogp / tau, b = -logsumexp(z / tau) log2(e).
 template <bool kMasked>
-__device__ __forceinline__ void logp_grad_tile(uint32_t ta, int nvalid, int yl, float Lt, float b, float c,
-                                               const GOut& o, int gcol, int lane) {
-  float v[32], g[32];
+__device__ __forceinline__ void logp_grad_tile(const float (&v)[128], int nvalid, int yl, float Lt, float b,
+                                               float c, const GOut& o, int gcol, int lane) {
+  const F2 L2 = f2(Lt), b2 = f2(b), c2 = f2(c);
 #pragma unroll
   for (int ch = 0; ch < 4; ++ch) {
-    tmem_ld32(ta + ch * 32, v);
+    float g[32];
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      const bool ok = !kMasked || (ch * 32 + i < nvalid);
-      g[i] = ok ? c * fast_exp2(fmaf(v[i], Lt, b)) : 0.f;
+    for (int i = 0; i < 16; ++i) {
+      const int k = ch * 32 + 2 * i;
+      float lo, hi;
+      f2_split(f2_fma(f2(v[k], v[k + 1]), L2, b2), lo, hi);
+      f2_split(f2_mul(c2, f2(fast_exp2(lo), fast_exp2(hi))), g[2 * i], g[2 * i + 1]);
+      if (kMasked) {
+        if (k >= nvalid) g[2 * i] = 0.f;
+        if (k + 1 >= nvalid) g[2 * i + 1] = 0.f;
+      }
     }
     const int r = yl - ch * 32;
     if (static_cast<unsigned>(r) < 32u) {
@@ -819,13 +842,14 @@ __device__ __forceinline__ void logp_bwd_epilogue(const HeadParams& p, uint32_t 
           aborted = true;
           break;
         }
-        const uint32_t ta = tl + acc * kHeadBN;
         const GOut o{&p.mapG[j], stage, &nchunks, row0};
+        float v[128];
+        tmem_ld128(tl + acc * kHeadBN, v);
+        logp_release(base, acc, acc_par, lane);
         if (nvalid == 128)
-          logp_grad_tile<false>(ta, 128, yl, p.Ltau, b[j], c[j], o, gcol, lane);
+          logp_grad_tile<false>(v, 128, yl, p.Ltau, b[j], c[j], o, gcol, lane);
         else
-          logp_grad_tile<true>(ta, nvalid, yl, p.Ltau, b[j], c[j], o, gcol, lane);
-        epi_release(base, acc, acc_par, lane);
+          logp_grad_tile<true>(v, nvalid, yl, p.Ltau, b[j], c[j], o, gcol, lane);
       }
     }
   }

@@ -309,27 +309,44 @@ __global__ void __launch_bounds__(kSplitSumThreads)
   }
 }
 
-// Log-probabilities from the partial states of the log-probability forward: a
-// thread owns a (sub-model, token) and goes through its partials, consecutive
-// threads through consecutive words.
-constexpr int kLogpMergeThreads = 128;
+// Log-probabilities from the partial states of the log-probability forward.  A block
+// owns 32 (sub-model, token) rows; its eight warps take every eighth partial each (a
+// lane a row, so the lanes read consecutive words) and hand their states on
+// through shared memory, where the first warp combines them in order.
+constexpr int kLogpMergeWarps = 8;
 
-__global__ void __launch_bounds__(kLogpMergeThreads)
+__global__ void __launch_bounds__(32 * kLogpMergeWarps)
     logp_merge_kernel(const __grid_constant__ LogpMergeParams p) {
-  chain_trigger();
-  chain_wait();
+  __shared__ float sh[3][kLogpMergeWarps][32];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const long long MT = static_cast<long long>(p.M) * p.T, PS = kLogpFields * MT;
-  const long long i = static_cast<long long>(blockIdx.x) * kLogpMergeThreads + threadIdx.x;
-  if (i >= MT) return;
-  const float* P = p.part + i;
+  const long long i = static_cast<long long>(blockIdx.x) * 32 + lane;
+  chain_wait();
   float m = -INFINITY, s = 0.f, zy = 0.f;
+  if (i < MT) {
+    const float* P = p.part + i;
 #pragma unroll 4
-  for (int k = 0; k < p.nparts; ++k) m = fmaxf(m, P[k * PS + kLogpMax * MT]);
-#pragma unroll 4
-  for (int k = 0; k < p.nparts; ++k) {
-    const float mk = P[k * PS + kLogpMax * MT];
-    s += mk == -INFINITY ? 0.f : P[k * PS + kLogpSum * MT] * exp2f((mk - m) * p.Ltau);
-    zy += P[k * PS + kLogpTarget * MT];
+    for (int k = warp; k < p.nparts; k += kLogpMergeWarps) {
+      const float mk = P[k * PS + kLogpMax * MT], sk = P[k * PS + kLogpSum * MT];
+      zy += P[k * PS + kLogpTarget * MT];
+      const float mn = fmaxf(m, mk);
+      if (mn != -INFINITY) s = s * exp2f((m - mn) * p.Ltau) + sk * exp2f((mk - mn) * p.Ltau);
+      m = mn;
+    }
+  }
+  sh[0][warp][lane] = m;
+  sh[1][warp][lane] = s;
+  sh[2][warp][lane] = zy;
+  __syncthreads();
+  if (warp > 0 || i >= MT) return;
+#pragma unroll
+  for (int q = 1; q < kLogpMergeWarps; ++q) m = fmaxf(m, sh[0][q][lane]);
+  s = zy = 0.f;
+#pragma unroll
+  for (int q = 0; q < kLogpMergeWarps; ++q) {
+    const float mq = sh[0][q][lane];
+    if (mq != -INFINITY) s += sh[1][q][lane] * exp2f((mq - m) * p.Ltau);
+    zy += sh[2][q][lane];
   }
   const int y = p.y[i % p.T];
   if (y >= p.V) atomicOr(p.status, kStatusBadTarget);
@@ -385,8 +402,7 @@ cudaError_t launch_split_sum(const SplitSumParams& p, cudaStream_t s) {
 cudaError_t launch_logp_merge(const LogpMergeParams& p, cudaStream_t s) {
   const long long n = static_cast<long long>(p.M) * p.T;
   if (n <= 0) return cudaSuccess;
-  return launch_chained(logp_merge_kernel, dim3(static_cast<unsigned>((n + kLogpMergeThreads - 1) / kLogpMergeThreads)),
-                        dim3(kLogpMergeThreads), 0, s, p);
+  return launch_chained(logp_merge_kernel, dim3(static_cast<unsigned>((n + 31) / 32)), dim3(32 * kLogpMergeWarps), 0, s, p);
 }
 
 cudaError_t launch_count(const int* y, long long T, long long V, float* inv_n, int* status,
