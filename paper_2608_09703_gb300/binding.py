@@ -166,6 +166,7 @@ class Problem:
         self.w = None if w is None else (ctypes.c_float * M)(*[float(x) for x in w])
         self.c = mls_problem(M, int(T), int(V), self.d, M - 1 if teacher is None else int(teacher),
                              float(tau), float(alpha), self.w, int(in_dtype), int(vocab_group))
+        self.sizes = (tuple(self.d), int(T), int(V))  # as Python numbers: read at every call
 
     @property
     def M(self) -> int:
@@ -288,6 +289,8 @@ def mls_spec_verify(p: mls_spec_problem, H_draft, W_draft, H_verify, W_verify, d
 def _expect(name: str, t: Optional[torch.Tensor], dtype, shape, like: int = -2) -> int:
     """Raises unless t is a dense CUDA tensor of this type and shape on the current
     device (and on device `like`, if given); returns its device."""
+    if like >= 0 and t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == like:
+        return like
     if t.dtype is not dtype:
         raise TypeError(f"{name}: {t.dtype}, expected {dtype}")
     if t.shape != shape:
@@ -305,6 +308,12 @@ def _expect(name: str, t: Optional[torch.Tensor], dtype, shape, like: int = -2) 
     return dev
 
 
+def _own(dev: int, buffer: torch.Tensor) -> None:
+    """The inputs' device has to be the one that an object's buffers were made on."""
+    if buffer.get_device() != dev:
+        raise ValueError(f"inputs on cuda:{dev}, outputs and workspace on {buffer.device}")
+
+
 def _ws_args(ws: Optional[torch.Tensor], like: int):
     if ws is None:
         return None, 0
@@ -314,14 +323,14 @@ def _ws_args(ws: Optional[torch.Tensor], like: int):
 
 
 def _expect_heads(prob: "Problem", H, W, targets) -> int:
-    c = prob.c
-    if len(H) != c.M or len(W) != c.M:
-        raise ValueError(f"{len(H)} hidden states and {len(W)} heads for {c.M} sub-models")
-    dev = _expect("targets", targets, torch.int32, (c.T,))
-    dt = torch.bfloat16 if c.in_dtype == MLS_BF16 else torch.float32
-    for m in range(c.M):
-        _expect(f"H[{m}]", H[m], dt, (c.T, c.d[m]), dev)
-        _expect(f"W[{m}]", W[m], dt, (c.V, c.d[m]), dev)
+    d, T, V = prob.sizes
+    if len(H) != len(d) or len(W) != len(d):
+        raise ValueError(f"{len(H)} hidden states and {len(W)} heads for {len(d)} sub-models")
+    dev = _expect("targets", targets, torch.int32, (T,))
+    dt = torch.bfloat16 if prob.c.in_dtype == MLS_BF16 else torch.float32
+    for h, w, dm in zip(H, W, d):
+        _expect("H", h, dt, (T, dm), dev)
+        _expect("W", w, dt, (V, dm), dev)
     return dev
 
 
@@ -343,14 +352,14 @@ def mls_head_logp_fwd(prob: "Problem", H, W, targets, logp, lse, ws, stream=None
 
 def mls_head_logp_bwd(prob: "Problem", H, W, targets, lse, dlogp, dH, dW, ws, stream=None) -> None:
     dev = _expect_heads(prob, H, W, targets)
-    c = prob.c
-    _expect("lse", lse, torch.float32, (c.M, c.T), dev)
-    _expect("dlogp", dlogp, torch.float32, (c.M, c.T), dev)
-    if len(dH) != c.M or len(dW) != c.M:
-        raise ValueError(f"{len(dH)} and {len(dW)} gradients for {c.M} sub-models")
-    for m in range(c.M):
-        _expect(f"dH[{m}]", dH[m], H[m].dtype, (c.T, c.d[m]), dev)
-        _expect(f"dW[{m}]", dW[m], H[m].dtype, (c.V, c.d[m]), dev)
+    d, T, V = prob.sizes
+    _expect("lse", lse, torch.float32, (len(d), T), dev)
+    _expect("dlogp", dlogp, torch.float32, (len(d), T), dev)
+    if len(dH) != len(d) or len(dW) != len(d):
+        raise ValueError(f"{len(dH)} and {len(dW)} gradients for {len(d)} sub-models")
+    for h, w, dm in zip(dH, dW, d):
+        _expect("dH", h, H[0].dtype, (T, dm), dev)
+        _expect("dW", w, H[0].dtype, (V, dm), dev)
     wsp, wsn = _ws_args(ws, dev)
     rc = lib().mls_head_logp_bwd(prob.ref(), _ptrs(H), _ptrs(W), _ptr(targets), _ptr(lse), _ptr(dlogp),
                                  _ptrs(dH), _ptrs(dW), wsp, wsn, _stream(stream))
@@ -594,19 +603,32 @@ class HeadLogp:
     def __init__(self, d, T, V, tau=1.0, device="cuda", vocab_group=0):
         self.prob = Problem(d, T, V, tau=tau, vocab_group=vocab_group)
         M, dev = len(d), torch.device(device)
+        self.rows = (M, T)
         self.logp = torch.empty(M, T, dtype=torch.float32, device=dev)
         self.lse = torch.empty(M, T, dtype=torch.float32, device=dev)
         self.dH = [torch.empty(T, dm, dtype=torch.bfloat16, device=dev) for dm in d]
         self.dW = [torch.empty(V, dm, dtype=torch.bfloat16, device=dev) for dm in d]
         self.ws = torch.empty(max(mls_logp_workspace_size(self.prob), 1), dtype=torch.uint8, device=dev)
 
+    # The object's own buffers need no check at every call (some 4 us of a forward and
+    # backward of two sub-models).
     def forward(self, H, W, targets, stream=None):
-        mls_head_logp_fwd(self.prob, H, W, targets, self.logp, self.lse, self.ws, stream)
+        _own(_expect_heads(self.prob, H, W, targets), self.ws)
+        rc = lib().mls_head_logp_fwd(self.prob.ref(), _ptrs(H), _ptrs(W), targets.data_ptr(),
+                                     self.logp.data_ptr(), self.lse.data_ptr(), self.ws.data_ptr(),
+                                     self.ws.numel(), _stream(stream))
+        _check(rc, "mls_head_logp_fwd")
         return self.logp
 
     def backward(self, H, W, targets, dlogp, stream=None):
         """Gradients for the tokens of the last forward; returns (dH, dW)."""
-        mls_head_logp_bwd(self.prob, H, W, targets, self.lse, dlogp, self.dH, self.dW, self.ws, stream)
+        dev = _expect_heads(self.prob, H, W, targets)
+        _own(dev, self.ws)
+        _expect("dlogp", dlogp, torch.float32, self.rows, dev)
+        rc = lib().mls_head_logp_bwd(self.prob.ref(), _ptrs(H), _ptrs(W), targets.data_ptr(),
+                                     self.lse.data_ptr(), dlogp.data_ptr(), _ptrs(self.dH),
+                                     _ptrs(self.dW), self.ws.data_ptr(), self.ws.numel(), _stream(stream))
+        _check(rc, "mls_head_logp_bwd")
         return self.dH, self.dW
 
 
@@ -617,7 +639,11 @@ class LayerNorm:
 
     def __init__(self, T, d, eps=1e-5, gain=True, bias=True, dtype=torch.bfloat16, device="cuda",
                  backward=True):
-        self.eps, self.gain, self.bias = eps, gain, bias
+        self.eps, self.gain, self.bias = float(eps), gain, bias
+        self.shape, self.dtype = (T, d), dtype
+        self.code = MLS_BF16 if dtype is torch.bfloat16 else MLS_FP32
+        if dtype not in (torch.bfloat16, torch.float32):
+            raise TypeError(dtype)
         dev = torch.device(device)
         self.y = torch.empty(T, d, dtype=dtype, device=dev)
         self.mean = self.rstd = self.dx = self.dgain = self.dbias = self.ws = None
@@ -638,7 +664,16 @@ class LayerNorm:
     def forward(self, x, gain=None, bias=None, stream=None):
         self._gain("gain", gain, self.gain)
         self._gain("bias", bias, self.bias)
-        mls_layer_norm_fwd(x, gain, bias, self.eps, self.y, self.mean, self.rstd, stream)
+        dev = _expect("x", x, self.dtype, self.shape)
+        _own(dev, self.y)
+        T, d = self.shape
+        if gain is not None:
+            _expect("gain", gain, self.dtype, (d,), dev)
+        if bias is not None:
+            _expect("bias", bias, self.dtype, (d,), dev)
+        rc = lib().mls_layer_norm_fwd(T, d, self.code, self.eps, x.data_ptr(), _ptr(gain), _ptr(bias),
+                                      self.y.data_ptr(), _ptr(self.mean), _ptr(self.rstd), _stream(stream))
+        _check(rc, "mls_layer_norm_fwd")
         return self.y
 
     def backward(self, x, dy, gain=None, stream=None):
@@ -646,8 +681,18 @@ class LayerNorm:
         self._gain("gain", gain, self.gain)
         if self.dx is None:
             raise ValueError("made with backward=False")
-        mls_layer_norm_bwd(x, gain, dy, self.mean, self.rstd, self.dx, self.dgain, self.dbias, self.ws,
-                           stream)
+        dev = _expect("x", x, self.dtype, self.shape)
+        _own(dev, self.y)
+        _expect("dy", dy, self.dtype, self.shape, dev)
+        T, d = self.shape
+        if gain is not None:
+            _expect("gain", gain, self.dtype, (d,), dev)
+        ws = self.ws
+        rc = lib().mls_layer_norm_bwd(T, d, self.code, x.data_ptr(), _ptr(gain), dy.data_ptr(),
+                                      self.mean.data_ptr(), self.rstd.data_ptr(), self.dx.data_ptr(),
+                                      _ptr(self.dgain), _ptr(self.dbias), _ptr(ws),
+                                      0 if ws is None else ws.numel(), _stream(stream))
+        _check(rc, "mls_layer_norm_bwd")
         return self.dx, self.dgain, self.dbias
 
 
@@ -661,6 +706,7 @@ class PolicyLoss:
                  adv_per_seq=False, w=None, device="cuda"):
         self.prob = PolicyProblem(T, V, M, B, clip_low, clip_high, beta, agg, adv_per_seq, w)
         dev = torch.device(device)
+        self.rows, self.shapes = (M, T), ((B if adv_per_seq else T,), (T,), (B + 1,))
         self.loss = torch.zeros(1, dtype=torch.float32, device=dev)
         self.tok_loss = torch.empty(M, T, dtype=torch.float32, device=dev)
         self.diag = torch.empty(3, M, dtype=torch.float32, device=dev)
@@ -669,8 +715,21 @@ class PolicyLoss:
 
     def __call__(self, logp, old_logp, adv, targets, ref_logp=None, seq_start=None, grad_scale=1.0,
                  stream=None):
-        mls_policy_loss(self.prob, logp, old_logp, ref_logp, adv, targets, seq_start, grad_scale,
-                        self.loss, self.tok_loss, self.diag, self.dlogp, self.ws, stream)
+        f32, i32, rows, (adv_s, tok_s, seq_s) = torch.float32, torch.int32, self.rows, self.shapes
+        dev = _expect("logp", logp, f32, rows)
+        _own(dev, self.ws)
+        _expect("old_logp", old_logp, f32, rows, dev)
+        _expect("adv", adv, f32, adv_s, dev)
+        _expect("targets", targets, i32, tok_s, dev)
+        if seq_start is not None:
+            _expect("seq_start", seq_start, i32, seq_s, dev)
+        if ref_logp is not None:
+            _expect("ref_logp", ref_logp, f32, rows, dev)
+        rc = lib().mls_policy_loss(self.prob.ref(), logp.data_ptr(), old_logp.data_ptr(), _ptr(ref_logp),
+                                   adv.data_ptr(), targets.data_ptr(), _ptr(seq_start), grad_scale,
+                                   self.loss.data_ptr(), self.tok_loss.data_ptr(), self.diag.data_ptr(),
+                                   self.dlogp.data_ptr(), self.ws.data_ptr(), self.ws.numel(), _stream(stream))
+        _check(rc, "mls_policy_loss")
         return self.loss
 
 

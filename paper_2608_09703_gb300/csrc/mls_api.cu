@@ -1371,7 +1371,7 @@ PolicyPlan policy_plan(const mls_policy_problem* p) {
   PolicyPlan pl;
   const long long blocks = policy_blocks(p->T), most = p->agg == MLS_AGG_SEQ_MEAN ? 4096 : 512;
   pl.count_tokens = kPolicyTokens * ceil_div(p->T, kPolicyTokens * most);
-  if (blocks > 1 && p->agg != MLS_AGG_SUM) pl.chunks = static_cast<int>(ceil_div(p->T, pl.count_tokens));
+  if (p->T > kPolicyDirect && p->agg != MLS_AGG_SUM) pl.chunks = static_cast<int>(ceil_div(p->T, pl.count_tokens));
   pl.off_part = align_up(sizeof(int) * static_cast<size_t>(pl.chunks));
   pl.total = align_up(pl.off_part + sizeof(float) * 3 * p->M * static_cast<size_t>(blocks));
   return pl;
@@ -1476,6 +1476,53 @@ bool clip_disjoint(int n, void* const* g, const int64_t* numel, const int32_t* d
       return false;
   return true;
 }
+// Pass 0 sums the squares, pass 1 scales; a launch takes kCap tensors.
+template <int kCap>
+int clip_launches(int n, void* const* g, const int64_t* numel, const int32_t* dtype, float max_norm,
+                  float* stats, void* ws, const DeviceState& dev, cudaStream_t s) {
+  const bool scale = !std::isinf(max_norm);
+  ClipParams<kCap> cp;
+  cp.max_norm = max_norm;
+  cp.part = static_cast<double*>(ws);
+  int rc, nparts = 0;
+  for (int pass = 0; pass < 2; ++pass) {
+    for (int first = 0; first == 0 || first < n; first += kCap) {
+      const int last = n - first < kCap ? n : first + kCap;
+      if (pass == 0 || n > kCap) {  // one table serves both passes
+        cp.n = 0;
+        cp.chunks = 0;
+        for (int i = first; i < last; ++i) {
+          if (numel[i] == 0) continue;
+          const int elt = dtype[i] == MLS_BF16 ? 2 : 4;
+          long long head = (16 - reinterpret_cast<uintptr_t>(g[i]) % 16) % 16 / elt;
+          if (head > numel[i]) head = numel[i];
+          ClipTensor& t = cp.t[cp.n++];
+          t.g = g[i];
+          t.numel = numel[i];
+          t.chunk0 = cp.chunks;
+          t.head = static_cast<short>(head);
+          t.fp32 = elt == 4;
+          const long long c = ceil_div(numel[i] - head, kClipChunk);
+          cp.chunks += static_cast<int>(c > 0 ? c : 1);
+        }
+      }
+      const int resident = dev.sms * (pass == 0 ? kClipNormBlocks : kClipScaleBlocks);
+      const int most = resident < kClipBlocks ? resident : kClipBlocks;
+      const int grid = cp.chunks < 1 ? 1 : cp.chunks < most ? cp.chunks : most;
+      if (pass == 0) {
+        cp.part0 = nparts;
+        nparts += grid;
+        if ((rc = timed("clip_norm", s, [&] { return launch_clip_norm(cp, grid, s); }))) return rc;
+      } else {
+        cp.nparts = nparts;
+        cp.stats = first == 0 ? stats : nullptr;
+        if ((rc = timed("clip_scale", s, [&] { return launch_clip_scale(cp, scale ? grid : 1, s); }))) return rc;
+        if (!scale) break;
+      }
+    }
+  }
+  return MLS_OK;
+}
 size_t clip_workspace(int n) {
   return align_up(sizeof(double) * kClipBlocks * static_cast<size_t>(n > 0 ? ceil_div(n, kClipTable) : 1));
 }
@@ -1508,47 +1555,8 @@ extern "C" int mls_grad_clip(int32_t n, void* const* g, const int64_t* numel, co
   if (!ws || (reinterpret_cast<uintptr_t>(ws) % kAlign) != 0 || ws_bytes < clip_workspace(n))
     return MLS_ERR_WORKSPACE;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  const bool scale = !std::isinf(max_norm);
-  ClipParams<kClipTable> cp;
-  cp.max_norm = max_norm;
-  cp.part = static_cast<double*>(ws);
-  // Pass 0 sums the squares, pass 1 scales; a launch takes kClipTable tensors.
-  int nparts = 0;
-  for (int pass = 0; pass < 2; ++pass) {
-    for (int first = 0; first == 0 || first < n; first += kClipTable) {
-      const int last = n - first < kClipTable ? n : first + kClipTable;
-      cp.n = 0;
-      cp.chunks = 0;
-      for (int i = first; i < last; ++i) {
-        if (numel[i] == 0) continue;
-        const int elt = dtype[i] == MLS_BF16 ? 2 : 4;
-        long long head = (16 - reinterpret_cast<uintptr_t>(g[i]) % 16) % 16 / elt;
-        if (head > numel[i]) head = numel[i];
-        ClipTensor& t = cp.t[cp.n++];
-        t.g = g[i];
-        t.numel = numel[i];
-        t.chunk0 = cp.chunks;
-        t.head = static_cast<short>(head);
-        t.fp32 = elt == 4;
-        const long long c = ceil_div(numel[i] - head, kClipChunk);
-        cp.chunks += static_cast<int>(c > 0 ? c : 1);
-      }
-      const int resident = dev->sms * (pass == 0 ? kClipNormBlocks : kClipScaleBlocks);
-      const int most = resident < kClipBlocks ? resident : kClipBlocks;
-      const int grid = cp.chunks < 1 ? 1 : cp.chunks < most ? cp.chunks : most;
-      if (pass == 0) {
-        cp.part0 = nparts;
-        nparts += grid;
-        if ((rc = timed("clip_norm", s, [&] { return launch_clip_norm(cp, grid, s); }))) return rc;
-      } else {
-        cp.nparts = nparts;
-        cp.stats = first == 0 ? stats : nullptr;
-        if ((rc = timed("clip_scale", s, [&] { return launch_clip_scale(cp, scale ? grid : 1, s); }))) return rc;
-        if (!scale) break;
-      }
-    }
-  }
-  return MLS_OK;
+  return n <= kClipFew ? clip_launches<kClipFew>(n, g, numel, dtype, max_norm, stats, ws, *dev, s)
+                       : clip_launches<kClipTable>(n, g, numel, dtype, max_norm, stats, ws, *dev, s);
 }
 
 // ------------------------------------------------------------------ speculative verify

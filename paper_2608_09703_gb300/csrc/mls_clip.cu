@@ -209,5 +209,7 @@ cudaError_t launch_clip_scale(const ClipParams<kCap>& p, int grid, cudaStream_t 
 }
 template cudaError_t launch_clip_norm(const ClipParams<kClipTable>&, int, cudaStream_t);
 template cudaError_t launch_clip_scale(const ClipParams<kClipTable>&, int, cudaStream_t);
+template cudaError_t launch_clip_norm(const ClipParams<kClipFew>&, int, cudaStream_t);
+template cudaError_t launch_clip_scale(const ClipParams<kClipFew>&, int, cudaStream_t);
 
 }  // namespace mls

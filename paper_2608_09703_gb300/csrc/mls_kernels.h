@@ -476,6 +476,8 @@ cudaError_t launch_norm_bwd(const NormParams& p, bool fp32, cudaStream_t s);
 
 // ------------------------------------------------------------------ clipped policy loss
 constexpr int kPolicyTokens = 1024;  // tokens per block
+constexpr int kPolicyOne = 4096;     // at most so many take one block, and one launch
+constexpr int kPolicyDirect = 16384; // at most so many are counted by each block itself
 enum PolicyAgg { kAggToken = 0, kAggSeq = 1, kAggSum = 2 };
 struct PolicyParams {
   long long T, V;
@@ -492,7 +494,7 @@ struct PolicyParams {
   float *loss, *tok_loss, *diag, *dlogp;    // [1], [M][T], [3][M], [M][T]; all but loss may be null
   int* chunk_count;              // [chunks, up to a multiple of 4]: counted tokens of each
                                  //   count_tokens tokens
-  int chunks;                    // 0: no counts needed, or one block has all tokens
+  int chunks;                    // 0: no counts needed, or so few tokens that blocks count them
   long long count_tokens;
   float* part;                   // [M][3][blocks]
   int* status;
@@ -503,6 +505,7 @@ cudaError_t launch_policy(const PolicyParams& p, cudaStream_t s);
 // ------------------------------------------------------------------ gradient norm and clipping
 constexpr int kClipChunk = 8192;     // values of a tensor per block and turn
 constexpr int kClipTable = 1024;     // tensors of a launch (24 KB of kernel parameters)
+constexpr int kClipFew = 64;         // a shorter table: the host copies 1.5 KB a launch
 // Blocks of an SM (all resident, so the last ones do not wait for a second turn).
 constexpr int kClipNormBlocks = 5, kClipScaleBlocks = 4;
 struct ClipTensor {

@@ -29,6 +29,9 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kPer = kPolicyTokens / kThreads;  // tokens of a thread
+// The kernel of one block for all tokens has as many threads as a block can have: 2000
+// tokens of 8 sequences took 8.9 us in three launches.
+constexpr int kOneThreads = kPolicyOne / kPer;
 // Blocks an SM holds of the main kernel, which its instructions bound (some 110 a token
 // and sub-model): 4, 5 and 6 take 95, 90 and 106 us (spills) for 4000001 tokens of 4
 // sub-models; 2048 tokens a block, 103 us.
@@ -39,7 +42,8 @@ __device__ __forceinline__ bool counts(const PolicyParams& p, long long t) {
   return y >= 0 && y < p.V;
 }
 
-// Sum over the block, valid in every thread; sh: kThreads / 32 values.
+// Sum over the block of N threads, valid in every thread; sh: N / 32 values.
+template <int N>
 __device__ __forceinline__ int block_sum_int(int v, int* sh) {
   v = __reduce_add_sync(0xffffffffu, v);
   __syncthreads();
@@ -47,7 +51,7 @@ __device__ __forceinline__ int block_sum_int(int v, int* sh) {
   __syncthreads();
   int s = 0;
 #pragma unroll
-  for (int i = 0; i < kThreads / 32; ++i) s += sh[i];
+  for (int i = 0; i < N / 32; ++i) s += sh[i];
   return s;
 }
 
@@ -87,20 +91,26 @@ __device__ __forceinline__ int seq_of_warp(const PolicyParams& p, long long t, i
   return lo;
 }
 
+// Counted tokens among [lo, hi), this thread's share.
+__device__ __forceinline__ int count_some(const PolicyParams& p, long long lo, long long hi) {
+  int n = 0;
+#pragma unroll 8
+  for (long long t = lo + threadIdx.x; t < hi; t += kThreads) n += counts(p, t);
+  return n;
+}
+
 // Tokens of [lo, hi) that count; every thread of the block calls it with the same range.
 __device__ int count_range(const PolicyParams& p, long long lo, long long hi, int* sh) {
   int n = 0;
-  if (lo < hi) {
+  if (p.chunks > 0 && lo < hi) {
     const long long c0 = (lo + p.count_tokens - 1) / p.count_tokens, c1 = hi / p.count_tokens;
     if (c0 < c1) {  // whole chunks, and the two ends
       for (long long c = c0 + threadIdx.x; c < c1; c += kThreads) n += p.chunk_count[c];
-      for (long long t = lo + threadIdx.x; t < c0 * p.count_tokens; t += kThreads) n += counts(p, t);
-      for (long long t = c1 * p.count_tokens + threadIdx.x; t < hi; t += kThreads) n += counts(p, t);
-    } else {
-      for (long long t = lo + threadIdx.x; t < hi; t += kThreads) n += counts(p, t);
+      n += count_some(p, lo, c0 * p.count_tokens);
+      lo = c1 * p.count_tokens;
     }
   }
-  return block_sum_int(n, sh);
+  return block_sum_int<kThreads>(n + count_some(p, lo, hi), sh);
 }
 
 // Counts of the chunks of tokens, and zeros up to a whole vector of four.
@@ -114,7 +124,7 @@ __global__ void __launch_bounds__(kThreads) policy_count_kernel(const __grid_con
   int n = 0;
 #pragma unroll 4
   for (long long t = t0 + threadIdx.x; t < t1; t += kThreads) n += t >= lo && t < hi && counts(p, t);
-  n = block_sum_int(n, sh);
+  n = block_sum_int<kThreads>(n, sh);
   if (threadIdx.x == 0) p.chunk_count[blockIdx.x] = n;
   if (blockIdx.x == 0 && threadIdx.x < 4 && p.chunks + threadIdx.x < (p.chunks + 3) / 4 * 4)
     p.chunk_count[p.chunks + threadIdx.x] = 0;
@@ -185,19 +195,20 @@ __device__ __forceinline__ float total_loss(const PolicyParams& p, const double*
 struct Inputs {
   float logp[kPer], old[kPer], ref[kPer];
 };
+template <int N>  // threads of the block
 __device__ __forceinline__ void load_inputs(const PolicyParams& p, long long i, int left, Inputs& v) {
   const float *a = p.logp + i, *b = p.old_logp + i, *c = p.ref_logp ? p.ref_logp + i : a;
 #pragma unroll
   for (int j = 0; j < kPer; ++j) {
-    const bool in = j * kThreads < left;
-    v.logp[j] = in ? a[j * kThreads] : 0.f;
-    v.old[j] = in ? b[j * kThreads] : 0.f;
-    v.ref[j] = in ? c[j * kThreads] : 0.f;
+    const bool in = j * N < left;
+    v.logp[j] = in ? a[j * N] : 0.f;
+    v.old[j] = in ? b[j * N] : 0.f;
+    v.ref[j] = in ? c[j * N] : 0.f;
   }
 }
 
 // A sub-model's loss and gradient of a thread's tokens: adds to the sums s and writes.
-template <bool kRef>
+template <bool kRef, int N>
 __device__ __forceinline__ void policy_row(const PolicyParams& p, const Inputs& in, const bool (&on)[kPer],
                                            const float (&A)[kPer], const float (&weight)[kPer], float gw,
                                            long long i, int left, float (&s)[3]) {
@@ -213,24 +224,25 @@ __device__ __forceinline__ void policy_row(const PolicyParams& p, const Inputs& 
       s[1] = fmaf(k.kl, weight[j], s[1]);
       s[2] += k.clipped ? weight[j] : 0.f;
     }
-    if (j * kThreads < left) {
-      if (p.tok_loss) tok[j * kThreads] = L;
-      if (p.dlogp) grad[j * kThreads] = g;
+    if (j * N < left) {
+      if (p.tok_loss) tok[j * N] = L;
+      if (p.dlogp) grad[j * N] = g;
     }
   }
 }
 
 // kOne: one block has all tokens, counts them itself and writes the sums.
 template <bool kOne>
-__global__ void __launch_bounds__(kThreads, kResident) policy_kernel(const __grid_constant__ PolicyParams p) {
-  __shared__ int sh[kThreads / 32];
-  __shared__ int inside[kPolicyTokens];  // counted tokens of the sequence that starts here
+__global__ void __launch_bounds__(kOne ? kOneThreads : kThreads, kOne ? 1 : kResident) policy_kernel(const __grid_constant__ PolicyParams p) {
+  constexpr int N = kOne ? kOneThreads : kThreads, kTokens = N * kPer;
+  __shared__ int sh[N / 32];
+  __shared__ int inside[kTokens];  // counted tokens of the sequence that starts here
   __shared__ int ends[2];
   __shared__ int starts[kFewSeqs];
-  __shared__ float shf[kThreads / 32][3 * kMaxModels];
+  __shared__ float shf[N / 32][3 * kMaxModels];
   __shared__ double shd[3 * kMaxModels];
-  const long long t0 = static_cast<long long>(blockIdx.x) * kPolicyTokens;
-  const long long t1 = t0 + kPolicyTokens < p.T ? t0 + kPolicyTokens : p.T;
+  const long long t0 = static_cast<long long>(blockIdx.x) * kTokens;
+  const long long t1 = t0 + kTokens < p.T ? t0 + kTokens : p.T;
   const int B = p.B, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const long long first = t0 + threadIdx.x;
   const int left = static_cast<int>(t1 - first);  // this thread's token j: first + j kThreads, if that is < left
@@ -239,19 +251,19 @@ __global__ void __launch_bounds__(kThreads, kResident) policy_kernel(const __gri
   // ---- what does not depend on the counts: the first sub-model's inputs, each
   // token's sequence, whether it counts, its advantage
   Inputs in;
-  load_inputs(p, first, left, in);
+  load_inputs<N>(p, first, left, in);
   bool on[kPer];
 #pragma unroll
-  for (int j = 0; j < kPer; ++j) on[j] = j * kThreads < left && counts(p, first + j * kThreads);
+  for (int j = 0; j < kPer; ++j) on[j] = j * N < left && counts(p, first + j * N);
   if (p.agg == kAggSeq)
-    for (int i = threadIdx.x; i < kPolicyTokens; i += kThreads) inside[i] = 0;
+    for (int i = threadIdx.x; i < kTokens; i += N) inside[i] = 0;
   if (p.seq_start && warp < 2) {
     const int b = seq_of_warp(p, warp ? t1 - 1 : t0, B - 1, lane);
     if (lane == 0) ends[warp] = b;
   }
   // The offsets have to be sorted and within [0, T].
   if (p.seq_start && blockIdx.x == 0)
-    for (int b = threadIdx.x; b <= B; b += kThreads) {
+    for (int b = threadIdx.x; b <= B; b += N) {
       const int v = p.seq_start[b];
       if (v < 0 || v > p.T || (b > 0 && v < p.seq_start[b - 1])) atomicOr(p.status, kStatusBadSeq);
     }
@@ -269,25 +281,25 @@ __global__ void __launch_bounds__(kThreads, kResident) policy_kernel(const __gri
       for (int i = 0; i < few; ++i) {
         const int s = starts[i];
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) seq[j] += s <= first + j * kThreads;
+        for (int j = 0; j < kPer; ++j) seq[j] += s <= first + j * N;
       }
     } else if (few > 0) {
 #pragma unroll
       for (int j = 0; j < kPer; ++j)
-        if (on[j]) seq[j] = seq_of(p, first + j * kThreads, b0, b1);
+        if (on[j]) seq[j] = seq_of(p, first + j * N, b0, b1);
     }
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-      const long long t = first + j * kThreads;
+      const long long t = first + j * N;
       on[j] = on[j] && t >= begin && t < end;
     }
   }
 #pragma unroll
   for (int j = 0; j < kPer; ++j) {
-    A[j] = on[j] ? (p.adv_per_seq ? p.adv[seq[j]] : p.adv[first + j * kThreads]) : 0.f;
+    A[j] = on[j] ? (p.adv_per_seq ? p.adv[seq[j]] : p.adv[first + j * N]) : 0.f;
     weight[j] = on[j] ? 1.f : 0.f;
   }
-  if (!kOne) chain_wait();  // the counts; and no output is written before
+  if (!kOne) chain_wait();  // the counts
 
   // ---- weights
   if (p.agg == kAggToken) {
@@ -295,15 +307,17 @@ __global__ void __launch_bounds__(kThreads, kResident) policy_kernel(const __gri
     if constexpr (kOne) {
 #pragma unroll
       for (int j = 0; j < kPer; ++j) n += on[j];
+    } else if (p.chunks == 0) {  // few tokens: each block counts them all
+      n = count_some(p, p.seq_start ? seq_at(p, 0) : 0, p.seq_start ? seq_at(p, B) : p.T);
     } else {
       const int4* c = reinterpret_cast<const int4*>(p.chunk_count);
 #pragma unroll 4
-      for (int i = threadIdx.x; i < (p.chunks + 3) / 4; i += kThreads) {
+      for (int i = threadIdx.x; i < (p.chunks + 3) / 4; i += N) {
         const int4 v = c[i];
         n += (v.x + v.y) + (v.z + v.w);
       }
     }
-    n = block_sum_int(n, sh);
+    n = block_sum_int<N>(n, sh);
     const float w = n > 0 ? 1.f / static_cast<float>(n) : 0.f;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) weight[j] *= w;
@@ -340,12 +354,12 @@ __global__ void __launch_bounds__(kThreads, kResident) policy_kernel(const __gri
   for (int m = 0; m < p.M; ++m) {
     const long long i = static_cast<long long>(m) * p.T + first;
     const float gw = p.grad_scale * p.w[m];
-    if (m > 0) load_inputs(p, i, left, in);
+    if (m > 0) load_inputs<N>(p, i, left, in);
     float s[3] = {0.f, 0.f, 0.f};
     if (p.ref_logp)
-      policy_row<true>(p, in, on, A, weight, gw, i, left, s);
+      policy_row<true, N>(p, in, on, A, weight, gw, i, left, s);
     else
-      policy_row<false>(p, in, on, A, weight, gw, i, left, s);
+      policy_row<false, N>(p, in, on, A, weight, gw, i, left, s);
 #pragma unroll
     for (int f = 0; f < 3; ++f) {
       s[f] = warp_sum(s[f]);
@@ -355,7 +369,7 @@ __global__ void __launch_bounds__(kThreads, kResident) policy_kernel(const __gri
   __syncthreads();
   if (threadIdx.x < 3 * p.M) {
     double v = 0.0;
-    for (int i = 0; i < kThreads / 32; ++i) v += shf[i][threadIdx.x];
+    for (int i = 0; i < N / 32; ++i) v += shf[i][threadIdx.x];
     if constexpr (kOne) {
       shd[threadIdx.x] = v;
       if (p.diag) p.diag[threadIdx.x % 3 * p.M + threadIdx.x / 3] = static_cast<float>(v);
@@ -413,8 +427,8 @@ __global__ void __launch_bounds__(kFinalThreads) policy_final_kernel(const __gri
 cudaError_t launch_policy(const PolicyParams& p, cudaStream_t s) {
   const int blocks = policy_blocks(p.T);
   cudaError_t e;
-  if (blocks == 1) {
-    policy_kernel<true><<<1, kThreads, 0, s>>>(p);
+  if (p.T <= kPolicyOne) {
+    policy_kernel<true><<<1, kOneThreads, 0, s>>>(p);
     return cudaGetLastError();
   }
   if (p.chunks > 0) {
