@@ -99,10 +99,13 @@ __device__ __forceinline__ int count_some(const PolicyParams& p, long long lo, l
   return n;
 }
 
-// Tokens of [lo, hi) that count; every thread of the block calls it with the same range.
-__device__ int count_range(const PolicyParams& p, long long lo, long long hi, int* sh) {
+// Counted tokens of sequence b if it crosses the block's ends, else 0: this thread's share.
+__device__ __forceinline__ int count_crossing(const PolicyParams& p, int b, long long t0, long long t1) {
+  long long lo = seq_at(p, b);
+  const long long hi = seq_at(p, b + 1);
+  if ((lo >= t0 && hi <= t1) || lo >= hi) return 0;
   int n = 0;
-  if (p.chunks > 0 && lo < hi) {
+  if (p.chunks > 0) {
     const long long c0 = (lo + p.count_tokens - 1) / p.count_tokens, c1 = hi / p.count_tokens;
     if (c0 < c1) {  // whole chunks, and the two ends
       for (long long c = c0 + threadIdx.x; c < c1; c += kThreads) n += p.chunk_count[c];
@@ -110,7 +113,7 @@ __device__ int count_range(const PolicyParams& p, long long lo, long long hi, in
       lo = c1 * p.count_tokens;
     }
   }
-  return block_sum_int<kThreads>(n + count_some(p, lo, hi), sh);
+  return n + count_some(p, lo, hi);
 }
 
 // Counts of the chunks of tokens, and zeros up to a whole vector of four.
@@ -183,11 +186,13 @@ __device__ __forceinline__ Token policy_token(const PolicyParams& p, float logp,
 }
 
 // v[3 m]: sum of weight P, v[3 m + 1]: of weight K.
-__device__ __forceinline__ float total_loss(const PolicyParams& p, const double* v) {
+template <typename F>
+__device__ __forceinline__ float total_loss(const PolicyParams& p, const F* v) {
   double loss = 0.0;
   for (int m = 0; m < p.M; ++m)
     loss += static_cast<double>(p.w[m]) *
-            (p.beta != 0.f ? v[3 * m] + static_cast<double>(p.beta) * v[3 * m + 1] : v[3 * m]);
+            (p.beta != 0.f ? static_cast<double>(v[3 * m]) + static_cast<double>(p.beta) * v[3 * m + 1]
+                           : static_cast<double>(v[3 * m]));
   return static_cast<float>(loss);
 }
 
@@ -235,12 +240,13 @@ __device__ __forceinline__ void policy_row(const PolicyParams& p, const Inputs& 
 template <bool kOne>
 __global__ void __launch_bounds__(kOne ? kOneThreads : kThreads, kOne ? 1 : kResident) policy_kernel(const __grid_constant__ PolicyParams p) {
   constexpr int N = kOne ? kOneThreads : kThreads, kTokens = N * kPer;
-  __shared__ int sh[N / 32];
+  __shared__ int sh[N / 32], sh1[N / 32];
   __shared__ int inside[kTokens];  // counted tokens of the sequence that starts here
   __shared__ int ends[2];
   __shared__ int starts[kFewSeqs];
+  __shared__ float advs[kFewSeqs];
   __shared__ float shf[N / 32][3 * kMaxModels];
-  __shared__ double shd[3 * kMaxModels];
+  __shared__ float shq[3 * kMaxModels];
   const long long t0 = static_cast<long long>(blockIdx.x) * kTokens;
   const long long t1 = t0 + kTokens < p.T ? t0 + kTokens : p.T;
   const int B = p.B, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -253,13 +259,27 @@ __global__ void __launch_bounds__(kOne ? kOneThreads : kThreads, kOne ? 1 : kRes
   Inputs in;
   load_inputs<N>(p, first, left, in);
   bool on[kPer];
+  float adv[kPer];
 #pragma unroll
-  for (int j = 0; j < kPer; ++j) on[j] = j * N < left && counts(p, first + j * N);
+  for (int j = 0; j < kPer; ++j) {
+    on[j] = j * N < left && counts(p, first + j * N);
+    adv[j] = !p.adv_per_seq && j * N < left ? p.adv[first + j * N] : 0.f;
+  }
   if (p.agg == kAggSeq)
     for (int i = threadIdx.x; i < kTokens; i += N) inside[i] = 0;
-  if (p.seq_start && warp < 2) {
-    const int b = seq_of_warp(p, warp ? t1 - 1 : t0, B - 1, lane);
-    if (lane == 0) ends[warp] = b;
+  // The block's sequences [b0, b1], from all starts where they are few, else by search.
+  const bool all = B <= kFewSeqs;
+  int begin = 0, end = 0;
+  if (p.seq_start) {
+    begin = p.seq_start[0];
+    end = p.seq_start[B];
+    if (all) {
+      if (threadIdx.x < kFewSeqs && threadIdx.x + 1 < B) starts[threadIdx.x] = p.seq_start[threadIdx.x + 1];
+      if (threadIdx.x < kFewSeqs && threadIdx.x < B && p.adv_per_seq) advs[threadIdx.x] = p.adv[threadIdx.x];
+    } else if (warp < 2) {
+      const int b = seq_of_warp(p, warp ? t1 - 1 : t0, B - 1, lane);
+      if (lane == 0) ends[warp] = b;
+    }
   }
   // The offsets have to be sorted and within [0, T].
   if (p.seq_start && blockIdx.x == 0)
@@ -268,18 +288,29 @@ __global__ void __launch_bounds__(kOne ? kOneThreads : kThreads, kOne ? 1 : kRes
       if (v < 0 || v > p.T || (b > 0 && v < p.seq_start[b - 1])) atomicOr(p.status, kStatusBadSeq);
     }
   __syncthreads();
-  const int b0 = p.seq_start ? ends[0] : 0, b1 = p.seq_start ? ends[1] : 0;
+  int b0 = 0, b1 = 0;
+  if (p.seq_start && all) {
+    for (int i = 0; i + 1 < B; ++i) {
+      b0 += starts[i] <= t0;
+      b1 += starts[i] < t1;
+    }
+  } else if (p.seq_start) {
+    b0 = ends[0];
+    b1 = ends[1];
+  }
   int seq[kPer];
   float A[kPer], weight[kPer];
 #pragma unroll
   for (int j = 0; j < kPer; ++j) seq[j] = b0;
   if (p.seq_start) {
-    const int begin = p.seq_start[0], end = p.seq_start[B], few = b1 - b0;
+    const int few = b1 - b0;
     if (few > 0 && few <= kFewSeqs) {  // each start of a sequence within the block, past b0's
-      if (threadIdx.x < few) starts[threadIdx.x] = p.seq_start[b0 + 1 + threadIdx.x];
-      __syncthreads();
+      if (!all) {
+        if (threadIdx.x < few) starts[threadIdx.x] = p.seq_start[b0 + 1 + threadIdx.x];
+        __syncthreads();
+      }
       for (int i = 0; i < few; ++i) {
-        const int s = starts[i];
+        const int s = starts[all ? b0 + i : i];
 #pragma unroll
         for (int j = 0; j < kPer; ++j) seq[j] += s <= first + j * N;
       }
@@ -296,7 +327,7 @@ __global__ void __launch_bounds__(kOne ? kOneThreads : kThreads, kOne ? 1 : kRes
   }
 #pragma unroll
   for (int j = 0; j < kPer; ++j) {
-    A[j] = on[j] ? (p.adv_per_seq ? p.adv[seq[j]] : p.adv[first + j * N]) : 0.f;
+    A[j] = on[j] ? (!p.adv_per_seq ? adv[j] : all ? advs[seq[j]] : p.adv[seq[j]]) : 0.f;
     weight[j] = on[j] ? 1.f : 0.f;
   }
   if (!kOne) chain_wait();  // the counts
@@ -331,14 +362,22 @@ __global__ void __launch_bounds__(kOne ? kOneThreads : kThreads, kOne ? 1 : kRes
     // the sequences that cross the block's ends
     int cross0 = 0, cross1 = 0;
     if constexpr (!kOne) {
-      long long lo = seq_at(p, b0), hi = seq_at(p, b0 + 1);
-      if (lo < t0 || hi > t1) cross0 = count_range(p, lo, hi, sh);
-      cross1 = cross0;
-      if (b1 != b0) {
-        lo = seq_at(p, b1);
-        hi = seq_at(p, b1 + 1);
-        if (lo < t0 || hi > t1) cross1 = count_range(p, lo, hi, sh);
+      cross0 = count_crossing(p, b0, t0, t1);
+      if (b1 != b0) cross1 = count_crossing(p, b1, t0, t1);
+      cross0 = __reduce_add_sync(0xffffffffu, cross0);
+      cross1 = __reduce_add_sync(0xffffffffu, cross1);
+      if (lane == 0) {
+        sh[warp] = cross0;
+        sh1[warp] = cross1;
       }
+      __syncthreads();
+      cross0 = cross1 = 0;
+#pragma unroll
+      for (int i = 0; i < N / 32; ++i) {
+        cross0 += sh[i];
+        cross1 += sh1[i];
+      }
+      if (b1 == b0) cross1 = cross0;
     }
     __syncthreads();
 #pragma unroll
@@ -367,19 +406,19 @@ __global__ void __launch_bounds__(kOne ? kOneThreads : kThreads, kOne ? 1 : kRes
     }
   }
   __syncthreads();
-  if (threadIdx.x < 3 * p.M) {
-    double v = 0.0;
-    for (int i = 0; i < N / 32; ++i) v += shf[i][threadIdx.x];
+  for (int q = warp; q < 3 * p.M; q += N / 32) {  // a warp a quantity
+    const float v = warp_sum(lane < N / 32 ? shf[lane][q] : 0.f);
+    if (lane > 0) continue;
     if constexpr (kOne) {
-      shd[threadIdx.x] = v;
-      if (p.diag) p.diag[threadIdx.x % 3 * p.M + threadIdx.x / 3] = static_cast<float>(v);
+      shq[q] = v;
+      if (p.diag) p.diag[q % 3 * p.M + q / 3] = v;
     } else {
-      p.part[static_cast<long long>(threadIdx.x) * gridDim.x + blockIdx.x] = static_cast<float>(v);
+      p.part[static_cast<long long>(q) * gridDim.x + blockIdx.x] = v;
     }
   }
   if constexpr (kOne) {
     __syncthreads();
-    if (threadIdx.x == 0) *p.loss = total_loss(p, shd);
+    if (threadIdx.x == 0) *p.loss = total_loss(p, shq);
   }
 }
 
@@ -413,8 +452,9 @@ __global__ void __launch_bounds__(kFinalThreads) policy_final_kernel(const __gri
   if (lane == 0) sh[warp] = a;
   __syncthreads();
   if (threadIdx.x < nq) {
-    double v = 0.0;
-    for (int i = 0; i < per; ++i) v += pair_value(sh[i * nq + threadIdx.x]);
+    Pair b = sh[threadIdx.x];
+    for (int i = 1; i < per; ++i) pair_add(b, sh[i * nq + threadIdx.x].hi, sh[i * nq + threadIdx.x].lo);
+    const double v = pair_value(b);
     shd[threadIdx.x] = v;
     if (p.diag) p.diag[threadIdx.x % 3 * p.M + threadIdx.x / 3] = static_cast<float>(v);
   }
