@@ -24,8 +24,10 @@
  *     16-byte aligned and d_m * sizeof(element) a multiple of 16 bytes.
  *   - Calls are asynchronous on `stream`; nothing is allocated and the host
  *     never synchronises.  The caller provides a workspace of at least
- *     mls_workspace_size() bytes (256-byte aligned); its contents need not be
- *     preserved between calls.
+ *     mls_workspace_size() bytes (256-byte aligned; the operators that have a size
+ *     function of their own name it); its contents need not be preserved between
+ *     calls.  Calls that may overlap on the GPU (other streams, graphs captured with
+ *     the same buffers) need workspaces and outputs of their own.
  *   - Return value: 0 on success or a negative MLS_ERR_* code, in which case
  *     nothing was launched.  Conditions only the device can see (a target >= V,
  *     an internal wait that timed out) are recorded in a status word read by
@@ -262,8 +264,9 @@ int mls_head_logp_bwd(const mls_problem* p, const void* const* H, const void* co
  *                                          each may be NULL
  *   ws          device workspace of mls_layer_norm_workspace_size(T, d) bytes, 256-byte
  *               aligned; not used, and may be NULL, when dgain and dbias are NULL
- * Sums are fp32.  Outputs overlap inputs only where said.  Asynchronous on `stream`;
- * returns 0 or a negative MLS_ERR_* code (nothing launched).  T = 0 reads no row.
+ * Sums are fp32.  Outputs overlap inputs only where said.  d <= 2^28 (MLS_ERR_UNSUPPORTED
+ * beyond).  eps >= 0; with eps = 0 a row of equal values gives NaN (0 / 0).  Asynchronous
+ * on `stream`; returns 0 or a negative MLS_ERR_* code (nothing launched).  T = 0 reads no row.
  */
 int mls_layer_norm_fwd(int64_t T, int32_t d, int32_t in_dtype, float eps, const void* x,
                        const void* gain, const void* bias, void* y, float* mean, float* rstd,

@@ -524,6 +524,8 @@ def mls_profile_read() -> dict:
 
 # ----------------------------------------------------------------------------------------
 # Convenience layer: allocates outputs and workspace with torch, then calls the entry points.
+# An object's results stay in its buffers until its next call, and its calls must not
+# overlap on the GPU: for work on several streams at once make an object for each.
 class HeadLoss:
     """Fused suite head + CE + distillation loss over device tensors.
 

@@ -986,7 +986,7 @@ extern "C" const char* mls_strerror(int code) {
     case MLS_OK: return "success";
     case MLS_ERR_ARG: return "invalid argument";
     case MLS_ERR_ALIGN: return "device pointer not 16-byte aligned";
-    case MLS_ERR_UNSUPPORTED: return "unsupported shape (row of H/W not a multiple of 16 bytes)";
+    case MLS_ERR_UNSUPPORTED: return "unsupported shape or type (a row not a multiple of 16 bytes, or a limit that mls.h states)";
     case MLS_ERR_WORKSPACE: return "workspace missing, misaligned or too small";
     case MLS_ERR_CUDA: return "CUDA runtime or launch failure";
     case MLS_ERR_DEVICE: return "current device is not compute capability 10.3";
@@ -1252,10 +1252,11 @@ extern "C" int mls_junction_bwd(int64_t T, int32_t d_prev, int32_t d_next, int32
 
 // ------------------------------------------------------------------ layer norm
 namespace {
+constexpr int kNormMostWidth = 1 << 28;  // columns of both sums are counted in 32 bits
 int norm_check(long long T, int d, int dtype, const void* const* ptrs, int n) {
   if (T < 0 || T > INT_MAX || d < 1) return MLS_ERR_ARG;
   if (dtype != MLS_BF16 && dtype != MLS_FP32) return MLS_ERR_ARG;
-  if ((static_cast<long long>(d) * (dtype == MLS_BF16 ? 2 : 4)) % 16) return MLS_ERR_UNSUPPORTED;
+  if (d > kNormMostWidth || (static_cast<long long>(d) * (dtype == MLS_BF16 ? 2 : 4)) % 16) return MLS_ERR_UNSUPPORTED;
   for (int i = 0; i < n; ++i) {
     if (T > 0 && !ptrs[i]) return MLS_ERR_ARG;
     if (!aligned16(ptrs[i])) return MLS_ERR_ALIGN;
@@ -1297,7 +1298,7 @@ extern "C" int mls_layer_norm_fwd(int64_t T, int32_t d, int32_t in_dtype, float 
 }
 
 extern "C" size_t mls_layer_norm_workspace_size(int64_t T, int32_t d) {
-  if (T < 0 || T > INT_MAX || d < 1) return 0;
+  if (T < 0 || T > INT_MAX || d < 1 || d > kNormMostWidth) return 0;
   // fp32 rows take more warps each, so at least as many blocks as bf16 ones
   return align_up(sizeof(float) * 2 * static_cast<size_t>(d) * norm_splits(T, d, true, current_sms()));
 }

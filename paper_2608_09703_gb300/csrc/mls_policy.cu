@@ -432,7 +432,6 @@ __global__ void __launch_bounds__(kFinalThreads) policy_final_kernel(const __gri
   __shared__ double shd[3 * kMaxModels];
   const int nq = 3 * p.M, per = (kFinalThreads / 32) / nq, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int q = warp % nq, k = warp / nq;
-  chain_trigger();
   chain_wait();
   Pair a = {0.f, 0.f};
   if (k < per) {

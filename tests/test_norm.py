@@ -125,7 +125,7 @@ def test_rows_with_infinities_or_nan_stay_alone():
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("T,d", [(50, 264), (50, 9000), (600, 2048)])
+@pytest.mark.parametrize("T,d", [(50, 264), (50, 9000), (600, 2048), (40, 16640)])
 def test_in_place(T, d):
     """y may be x and dx may be dy."""
     x, g, b, dy = inputs(T, d, torch.bfloat16, True, True)
@@ -212,6 +212,8 @@ def test_refusals_of_the_library():
                dict(eps=float("inf")), dict(x=None), dict(y=None), dict(mean=None), dict(rstd=None)):
         assert fwd(**kw) == B.MLS_ERR_ARG, kw
     assert fwd(d=60) == B.MLS_ERR_UNSUPPORTED and fwd(d=6, dt=1) == B.MLS_ERR_UNSUPPORTED
+    assert fwd(d=(1 << 28) + 8) == B.MLS_ERR_UNSUPPORTED and fwd(d=(1 << 31) - 8) == B.MLS_ERR_UNSUPPORTED
+    assert B.mls_layer_norm_workspace_size(1, (1 << 28) + 8) == 0
     for kw in (dict(x=p + 8), dict(gain=p + 8), dict(bias=p + 2), dict(y=q + 4), dict(mean=m + 2)):
         assert fwd(**kw) == B.MLS_ERR_ALIGN, kw
 
