@@ -238,7 +238,8 @@ int mls_spec_verify(const mls_spec_problem* p, const void* H_draft, const void* 
  *   logp, lse  device, fp32 [M, T]; the backward needs lse
  *   dlogp      device, fp32 [M, T]
  *   dH[m], dW[m]  device, bf16 [T, d_m] and [V, d_m], 16-byte aligned, overwritten (dW zeros
- *              when T = 0); sums are fp32, rounded once
+ *              when T = 0); sums are fp32, rounded once.  They overlap neither each other
+ *              nor an input (a buffer given twice: MLS_ERR_ARG).
  *   ws         device workspace of mls_logp_workspace_size(p) bytes
  */
 size_t mls_logp_workspace_size(const mls_problem* p);
@@ -290,8 +291,8 @@ int mls_layer_norm_bwd(int64_t T, int32_t d, int32_t in_dtype, const void* x, co
  *             MLS_AGG_SEQ_MEAN 1 / (B n_b), n_b those of t's sequence (a sequence with
  *             none adds 0 and stays in the mean); MLS_AGG_SUM 1
  * A token counts when its target lies in [0, V) and it belongs to a sequence.
- * Nothing but the target and the sequence of one that does not is read, so the
- * other inputs may hold anything there.
+ * Of one that does not, nothing but its target and its sequence matters: the other
+ * inputs may hold anything there.
  *   logp, old_logp  device, fp32 [M, T]
  *   ref_logp        device, fp32 [M, T]; NULL only when beta = 0 (with beta = 0 it only
  *                   serves the reported K)

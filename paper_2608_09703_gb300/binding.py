@@ -289,8 +289,11 @@ def mls_spec_verify(p: mls_spec_problem, H_draft, W_draft, H_verify, W_verify, d
 def _expect(name: str, t: Optional[torch.Tensor], dtype, shape, like: int = -2) -> int:
     """Raises unless t is a dense CUDA tensor of this type and shape on the current
     device (and on device `like`, if given); returns its device."""
-    if like >= 0 and t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == like:
+    if like >= 0 and t is not None and t.dtype is dtype and t.shape == shape and t.is_contiguous() \
+            and t.get_device() == like:
         return like
+    if t is None:
+        raise TypeError(f"{name}: None")
     if t.dtype is not dtype:
         raise TypeError(f"{name}: {t.dtype}, expected {dtype}")
     if t.shape != shape:
@@ -308,10 +311,22 @@ def _expect(name: str, t: Optional[torch.Tensor], dtype, shape, like: int = -2) 
     return dev
 
 
-def _own(dev: int, buffer: torch.Tensor) -> None:
-    """The inputs' device has to be the one that an object's buffers were made on."""
-    if buffer.get_device() != dev:
-        raise ValueError(f"inputs on cuda:{dev}, outputs and workspace on {buffer.device}")
+class _Home:
+    """The device of an object's buffers.  Its calls run there only while that device is
+    the current one."""
+
+    __slots__ = ("index",)
+
+    def __init__(self, buffer: torch.Tensor):
+        self.index = buffer.get_device()
+        if self.index < 0:
+            raise ValueError(f"device {buffer.device}: expected a CUDA device")
+
+    def __call__(self) -> int:
+        now = _get_device() if _get_device is not None else torch.cuda.current_device()
+        if now != self.index:
+            raise ValueError(f"made on cuda:{self.index}, but cuda:{now} is the current device")
+        return now
 
 
 def _ws_args(ws: Optional[torch.Tensor], like: int):
@@ -322,11 +337,11 @@ def _ws_args(ws: Optional[torch.Tensor], like: int):
     return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
-def _expect_heads(prob: "Problem", H, W, targets) -> int:
+def _expect_heads(prob: "Problem", H, W, targets, dev: int = -2) -> int:
     d, T, V = prob.sizes
     if len(H) != len(d) or len(W) != len(d):
         raise ValueError(f"{len(H)} hidden states and {len(W)} heads for {len(d)} sub-models")
-    dev = _expect("targets", targets, torch.int32, (T,))
+    dev = _expect("targets", targets, torch.int32, (T,), dev)
     dt = torch.bfloat16 if prob.c.in_dtype == MLS_BF16 else torch.float32
     for h, w, dm in zip(H, W, d):
         _expect("H", h, dt, (T, dm), dev)
@@ -611,11 +626,12 @@ class HeadLogp:
         self.dH = [torch.empty(T, dm, dtype=torch.bfloat16, device=dev) for dm in d]
         self.dW = [torch.empty(V, dm, dtype=torch.bfloat16, device=dev) for dm in d]
         self.ws = torch.empty(max(mls_logp_workspace_size(self.prob), 1), dtype=torch.uint8, device=dev)
+        self.home = _Home(self.ws)
 
     # The object's own buffers need no check at every call (some 4 us of a forward and
     # backward of two sub-models).
     def forward(self, H, W, targets, stream=None):
-        _own(_expect_heads(self.prob, H, W, targets), self.ws)
+        _expect_heads(self.prob, H, W, targets, self.home())
         rc = lib().mls_head_logp_fwd(self.prob.ref(), _ptrs(H), _ptrs(W), targets.data_ptr(),
                                      self.logp.data_ptr(), self.lse.data_ptr(), self.ws.data_ptr(),
                                      self.ws.numel(), _stream(stream))
@@ -624,8 +640,7 @@ class HeadLogp:
 
     def backward(self, H, W, targets, dlogp, stream=None):
         """Gradients for the tokens of the last forward; returns (dH, dW)."""
-        dev = _expect_heads(self.prob, H, W, targets)
-        _own(dev, self.ws)
+        dev = _expect_heads(self.prob, H, W, targets, self.home())
         _expect("dlogp", dlogp, torch.float32, self.rows, dev)
         rc = lib().mls_head_logp_bwd(self.prob.ref(), _ptrs(H), _ptrs(W), targets.data_ptr(),
                                      self.lse.data_ptr(), dlogp.data_ptr(), _ptrs(self.dH),
@@ -648,6 +663,7 @@ class LayerNorm:
             raise TypeError(dtype)
         dev = torch.device(device)
         self.y = torch.empty(T, d, dtype=dtype, device=dev)
+        self.home = _Home(self.y)
         self.mean = self.rstd = self.dx = self.dgain = self.dbias = self.ws = None
         if backward:
             self.mean = torch.empty(T, dtype=torch.float32, device=dev)
@@ -666,8 +682,7 @@ class LayerNorm:
     def forward(self, x, gain=None, bias=None, stream=None):
         self._gain("gain", gain, self.gain)
         self._gain("bias", bias, self.bias)
-        dev = _expect("x", x, self.dtype, self.shape)
-        _own(dev, self.y)
+        dev = _expect("x", x, self.dtype, self.shape, self.home())
         T, d = self.shape
         if gain is not None:
             _expect("gain", gain, self.dtype, (d,), dev)
@@ -683,8 +698,7 @@ class LayerNorm:
         self._gain("gain", gain, self.gain)
         if self.dx is None:
             raise ValueError("made with backward=False")
-        dev = _expect("x", x, self.dtype, self.shape)
-        _own(dev, self.y)
+        dev = _expect("x", x, self.dtype, self.shape, self.home())
         _expect("dy", dy, self.dtype, self.shape, dev)
         T, d = self.shape
         if gain is not None:
@@ -714,12 +728,12 @@ class PolicyLoss:
         self.diag = torch.empty(3, M, dtype=torch.float32, device=dev)
         self.dlogp = torch.empty(M, T, dtype=torch.float32, device=dev)
         self.ws = torch.empty(max(mls_policy_workspace_size(self.prob), 1), dtype=torch.uint8, device=dev)
+        self.home = _Home(self.ws)
 
     def __call__(self, logp, old_logp, adv, targets, ref_logp=None, seq_start=None, grad_scale=1.0,
                  stream=None):
         f32, i32, rows, (adv_s, tok_s, seq_s) = torch.float32, torch.int32, self.rows, self.shapes
-        dev = _expect("logp", logp, f32, rows)
-        _own(dev, self.ws)
+        dev = _expect("logp", logp, f32, rows, self.home())
         _expect("old_logp", old_logp, f32, rows, dev)
         _expect("adv", adv, f32, adv_s, dev)
         _expect("targets", targets, i32, tok_s, dev)
@@ -748,7 +762,12 @@ class GradClip:
         dev = self.grads[0].device
         self.stats = torch.empty(2, dtype=torch.float32, device=dev)
         self.ws = torch.empty(mls_grad_clip_workspace_size(len(self.grads)), dtype=torch.uint8, device=dev)
+        self.home = _Home(self.ws)
 
     def __call__(self, max_norm, stream=None):
-        mls_grad_clip(self.table, max_norm, self.stats, self.ws, stream)
+        self.home()
+        t, ws = self.table, self.ws
+        rc = lib().mls_grad_clip(t.n, t.g, t.numel, t.dtype, max_norm, self.stats.data_ptr(), ws.data_ptr(),
+                                 ws.numel(), _stream(stream))
+        _check(rc, "mls_grad_clip")
         return self.stats

@@ -939,6 +939,11 @@ extern "C" int mls_head_logp_bwd(const mls_problem* p, const void* const* H, con
       return MLS_ERR_ALIGN;
   }
   if (!aligned4(targets) || !aligned4(lse) || !aligned4(dlogp)) return MLS_ERR_ALIGN;
+  for (int m = 0; m < p->M; ++m)  // one buffer for two gradients, or for a gradient and an input
+    for (int k = 0; k < p->M; ++k) {
+      if ((k != m && (dW[m] == dW[k] || (p->T > 0 && dH[m] == dH[k]))) || dW[m] == W[k]) return MLS_ERR_ARG;
+      if (p->T > 0 && (dH[m] == H[k] || dH[m] == W[k] || dW[m] == H[k] || dH[m] == dW[k])) return MLS_ERR_ARG;
+    }
   DeviceState* dev = nullptr;
   if ((rc = device_state(&dev))) return rc;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
@@ -1400,7 +1405,7 @@ extern "C" int mls_policy_loss(const mls_policy_problem* p, const float* logp, c
                                mls_stream_t stream) {
   int rc = policy_validate(p);
   if (rc) return rc;
-  if (!loss || !std::isfinite(grad_scale)) return MLS_ERR_ARG;
+  if (!loss || !std::isfinite(grad_scale) || (tok_loss && tok_loss == dlogp)) return MLS_ERR_ARG;
   if (p->T > 0) {
     if (!logp || !old_logp || !adv || !targets || (p->beta > 0.f && !ref_logp)) return MLS_ERR_ARG;
     if (!seq_start && (p->B > 0 || p->agg == MLS_AGG_SEQ_MEAN || p->adv_per_seq)) return MLS_ERR_ARG;

@@ -265,6 +265,11 @@ def test_refusals_of_the_library():
         for kw in (dict(h=p + 8), dict(w=p + 4), dict(y=p + 2), dict(lse=p + 1)):
             assert call(bwd=bwd, **kw) == B.MLS_ERR_ALIGN, kw
     assert call(dh=None) == B.MLS_ERR_ARG and call(dw=p + 8) == B.MLS_ERR_ALIGN
+    # one buffer for both sub-models' gradients, or for a gradient and an input
+    q = 0x100000
+    assert call(dh=q, dw=2 * q) == B.MLS_ERR_ARG
+    for kw in (dict(dh=p, dw=q), dict(dh=q, dw=p), dict(dh=q, dw=q), dict(dh=q, dw=2 * q, h=q)):
+        assert call(d=(64,), **kw) == B.MLS_ERR_ARG, kw
     assert L.mls_head_logp_fwd(None, None, None, None, None, None, None, 0, None) == B.MLS_ERR_ARG
     assert B.mls_logp_workspace_size(mls.Problem((64,), 10, 100, in_dtype=B.MLS_FP32)) == 0
     assert B.mls_logp_workspace_size(mls.Problem((64,), 10, 100)) > 0

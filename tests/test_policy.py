@@ -353,14 +353,15 @@ def test_refusals_of_the_library():
     L = B.lib()
     p = 0x1000
 
-    def call(logp=p, old=p, ref=p, adv=p, y=p, start=p, scale=1.0, loss=p, ws=0x10000, size=1 << 30, **kw):
+    def call(logp=p, old=p, ref=p, adv=p, y=p, start=p, scale=1.0, loss=p, tok=p, dl=0x2000, ws=0x10000,
+             size=1 << 30, **kw):
         prob = mls.PolicyProblem(**{**config(100, B=3), **kw})
-        return L.mls_policy_loss(prob.ref(), logp, old, ref, adv, y, start, scale, loss, p, p, p, ws, size, None)
+        return L.mls_policy_loss(prob.ref(), logp, old, ref, adv, y, start, scale, loss, tok, p, dl, ws, size, None)
 
     for kw in (dict(M=0), dict(M=5), dict(T=-1), dict(T=1 << 31), dict(V=0), dict(V=1 << 31), dict(B=-1),
                dict(clip_low=-0.1), dict(clip_high=float("nan")), dict(beta=-1.0), dict(beta=float("inf")),
                dict(w=[float("nan")]), dict(logp=None), dict(old=None), dict(adv=None), dict(y=None),
-               dict(loss=None), dict(scale=float("inf")), dict(beta=0.1, ref=None), dict(start=None),
+               dict(loss=None), dict(dl=p), dict(scale=float("inf")), dict(beta=0.1, ref=None), dict(start=None),
                dict(B=0), dict(B=0, start=None, agg="seq"), dict(B=0, start=None, adv_per_seq=True)):
         assert call(**kw) == B.MLS_ERR_ARG, kw
     for kw in (dict(logp=p + 2), dict(y=p + 1), dict(start=p + 2)):
