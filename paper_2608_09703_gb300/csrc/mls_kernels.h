@@ -484,7 +484,8 @@ struct PolicyParams {
   int M, B, agg, adv_per_seq;
   float beta, grad_scale;
   float w[kMaxModels];
-  float high[2], low[2];         // log(1 + clip_high), log(1 - clip_low) as two fp32 words
+  float high[3], low[3];         // log(1 + clip_high), log(1 - clip_low) as two fp32 words, and
+                                 //   how near an fp32 difference needs the second
   float ratio_high, ratio_low;   // 1 + clip_high, 1 - clip_low
   const float *logp, *old_logp, *ref_logp;  // [M][T], ref_logp may be null
   const float* adv;              // [B] or [T]

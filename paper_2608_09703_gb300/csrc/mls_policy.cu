@@ -6,9 +6,10 @@
 //   dL/dlogp = (0 where the clamp decides the minimum, else -r A) - beta (e^x - 1)
 // each times the token's weight: 1/N, 1/(B n_b) or 1 (N tokens count, n_b of them in
 // sequence b).  Which side of a clipping bound a token is on decides between a
-// gradient and none, so the comparison is made on D itself, with what rounding the
-// subtraction lost (its exact value is D + e) and the bound, log(1 + clip_high) or
-// log(1 - clip_low), in two fp32 words: as exact as in 64 bits.  K of a small x
+// gradient and none, so the comparison is made on D itself, and where D is near the
+// bound with what rounding the subtraction lost (its exact value is D + e) and the
+// bound, log(1 + clip_high) or log(1 - clip_low), in two fp32 words: as exact as in 64
+// bits.  K of a small x
 // comes from its series, not from a difference of numbers near 1.
 //
 // A block owns 1024 consecutive tokens: it finds each one's sequence,
@@ -31,10 +32,10 @@ constexpr int kPer = kPolicyTokens / kThreads;  // tokens of a thread
 // The kernel of one block for all tokens has as many threads as a block can have: 2000
 // tokens of 8 sequences took 8.9 us in three launches.
 constexpr int kOneThreads = kPolicyOne / kPer;
-// Blocks an SM holds of the main kernel, which its instructions bound (some 140 a token
-// and sub-model, 3.1 a cycle): with 4 (63 registers), 5 and 6 (spills) it takes 85, 85 and
-// 99 us for 4000001 tokens of 4 sub-models; 2048 tokens a block were slower by a tenth.
-constexpr int kResident = 4;
+// Blocks an SM holds of the main kernel, which its instructions bound (some 110 a token
+// and sub-model): 4, 5 and 6 take 95, 90 and 106 us (spills) for 4000001 tokens of 4
+// sub-models; 2048 tokens a block, 103 us.
+constexpr int kResident = 5;
 
 __device__ __forceinline__ bool counts(const PolicyParams& p, long long t) {
   const int y = p.y[t];
@@ -134,19 +135,21 @@ __global__ void __launch_bounds__(kThreads) policy_count_kernel(const __grid_con
 
 // e^x - 1 - x and e^x - 1.  Below 1/2 the Taylor series (remainder under 2^-29 of it).
 __device__ __forceinline__ void exp_excess(float x, float& excess, float& minus_one) {
-  float s = 1.f / 362880.f;
-  s = fmaf(s, x, 1.f / 40320.f);
-  s = fmaf(s, x, 1.f / 5040.f);
-  s = fmaf(s, x, 1.f / 720.f);
-  s = fmaf(s, x, 1.f / 120.f);
-  s = fmaf(s, x, 1.f / 24.f);
-  s = fmaf(s, x, 1.f / 6.f);
-  s = fmaf(s, x, 0.5f);
-  s *= x * x;
-  const float e1 = expf(x) - 1.f;
-  const bool small = fabsf(x) < 0.5f;
-  excess = small ? s : e1 - x;
-  minus_one = small ? x + s : e1;
+  if (fabsf(x) < 0.5f) {
+    float s = 1.f / 362880.f;
+    s = fmaf(s, x, 1.f / 40320.f);
+    s = fmaf(s, x, 1.f / 5040.f);
+    s = fmaf(s, x, 1.f / 720.f);
+    s = fmaf(s, x, 1.f / 120.f);
+    s = fmaf(s, x, 1.f / 24.f);
+    s = fmaf(s, x, 1.f / 6.f);
+    s = fmaf(s, x, 0.5f);
+    excess = x * x * s;
+    minus_one = x + excess;
+  } else {
+    minus_one = expf(x) - 1.f;
+    excess = minus_one - x;
+  }
 }
 
 struct Token {
@@ -154,17 +157,20 @@ struct Token {
   bool clipped;
 };
 
-// Without branches, so that a thread's tokens run side by side: branches around what a
-// token may not need made 4000001 tokens of 4 sub-models 86 us.  `ref` only where kRef.
+// `ref` only where kRef.
 template <bool kRef>
 __device__ __forceinline__ Token policy_token(const PolicyParams& p, float logp, float old, float ref, float A) {
   const float d = logp - old;
-  // the part of the exact difference that rounding d lost (Knuth's two-sum); none if d is infinite
-  const float back = d - logp;
-  const float lost = (logp - (d - back)) - (old + back), e = fabsf(d) < INFINITY ? lost : 0.f;
   // The bound that this advantage meets: above for a gain, below for a loss.
   const bool up = A > 0.f;
-  const float past = (d - (up ? p.high[0] : p.low[0])) + (e - (up ? p.high[1] : p.low[1]));
+  const float hi = up ? p.high[0] : p.low[0];
+  float past = d - hi;
+  if (fabsf(past) <= (up ? p.high[2] : p.low[2])) {  // as near as rounding can matter
+    // the part of the exact difference that rounding d lost (Knuth's two-sum), and the bound's second word
+    const float back = d - logp;
+    const float e = (logp - (d - back)) - (old + back);
+    past += (isfinite(d) ? e : 0.f) - (up ? p.high[1] : p.low[1]);
+  }
   Token k;
   k.clipped = up ? past > 0.f : A < 0.f && past < 0.f;
   const float ratio = k.clipped ? (up ? p.ratio_high : p.ratio_low) : expf(d);
@@ -214,13 +220,15 @@ __device__ __forceinline__ void policy_row(const PolicyParams& p, const Inputs& 
   float *tok = p.tok_loss + i, *grad = p.dlogp + i;
 #pragma unroll
   for (int j = 0; j < kPer; ++j) {
-    // what does not count may be anything, NaN too: chosen away, not multiplied
-    const Token k = policy_token<kRef>(p, in.logp[j], in.old[j], in.ref[j], A[j]);
-    const float all = kRef && p.beta != 0.f ? fmaf(p.beta, k.kl, k.policy) : k.policy;  // beta 0: K is only reported
-    const float L = on[j] ? all : 0.f, g = on[j] ? k.grad * (weight[j] * gw) : 0.f;
-    s[0] = fmaf(on[j] ? k.policy : 0.f, weight[j], s[0]);
-    if (kRef) s[1] = fmaf(on[j] ? k.kl : 0.f, weight[j], s[1]);
-    s[2] += k.clipped ? weight[j] : 0.f;  // the weight is 0 where the token does not count
+    float L = 0.f, g = 0.f;
+    if (on[j]) {
+      const Token k = policy_token<kRef>(p, in.logp[j], in.old[j], in.ref[j], A[j]);
+      L = kRef && p.beta != 0.f ? fmaf(p.beta, k.kl, k.policy) : k.policy;  // beta 0: K is only reported
+      g = k.grad * (weight[j] * gw);
+      s[0] = fmaf(k.policy, weight[j], s[0]);
+      s[1] = fmaf(k.kl, weight[j], s[1]);
+      s[2] += k.clipped ? weight[j] : 0.f;
+    }
     if (j * N < left) {
       if (p.tok_loss) tok[j * N] = L;
       if (p.dlogp) grad[j * N] = g;
