@@ -3,10 +3,11 @@
 // A call's tensors come as a table in the kernels' parameters (kClipTable of them
 // a launch), cut into chunks of kClipChunk values that persistent blocks take in
 // turn.  Squares are summed in fp32 over the 32 values that a thread holds of a
-// chunk, in two fp32 words (Pair) over its chunks, and in 64 bits from there on.  Where such a sum leaves the range in which
-// fp32 squares are exact to rounding (a square that overflowed, or squares so
-// small that some were flushed) those 32 values are summed again in 64 bits, so
-// the norm is right from the smallest to the largest representable gradient.
+// chunk, in two fp32 words (Pair) over its chunks, and in 64 bits from there on.  Where
+// such a sum leaves the range in which fp32 squares are exact to rounding (a square
+// that overflowed, or squares so small that some vanished) those 32 values are taken
+// times a power of two, into sums of their own (Blue's method), so the norm is right
+// from the smallest to the largest representable gradient at about the same speed.
 // The blocks' shares are added in a fixed order: results do not depend on timing.
 #include "mls_device.cuh"
 #include "mls_kernels.h"
@@ -29,31 +30,30 @@ __device__ __forceinline__ int tensor_of(const ClipParams<kCap>& p, int c) {
   return lo;
 }
 
-// What a thread has summed: squares in two fp32 words, and what does not fit them.
+// What a thread has summed: squares as they are, of values times 2^90, of values times 2^-80.
 struct Squares {
-  Pair small;
-  double rest;
+  Pair plain, tiny, huge;
 };
+constexpr float kUp = 0x1p90f, kDown = 0x1p-80f;
+
+template <int n>
+__device__ __forceinline__ float scaled_squares(const float (&f)[n], float scale) {
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < n; ++i) s[i & 3] = fmaf(f[i] * scale, f[i] * scale, s[i & 3]);
+  return (s[0] + s[1]) + (s[2] + s[3]);
+}
 
 // Adds the squares of a thread's values of a chunk, see above.
 template <int n>
 __device__ __forceinline__ void add_squares(Squares& acc, const float (&f)[n]) {
-  float s[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int i = 0; i < n; ++i) s[i & 3] = fmaf(f[i], f[i], s[i & 3]);
-  const float a = (s[0] + s[1]) + (s[2] + s[3]);
-  if (a >= 0x1p-80f && a <= 0x1p90f) {
-    pair_add(acc.small, a, 0.f);
-    return;
-  }
-  float most = 0.f;
-#pragma unroll
-  for (int i = 0; i < n; ++i) most = fmaxf(most, fabsf(f[i]));
-  if (a == 0.f && most == 0.f) return;  // zeros: a frozen tensor, rows of unused tokens
-  double d = 0.0;
-#pragma unroll
-  for (int i = 0; i < n; ++i) d = fma(static_cast<double>(f[i]), static_cast<double>(f[i]), d);
-  acc.rest += d;
+  const float a = scaled_squares(f, 1.f);
+  if (a >= 0x1p-80f && a <= 0x1p90f)
+    pair_add(acc.plain, a, 0.f);
+  else if (a < 0x1p-80f)
+    pair_add(acc.tiny, scaled_squares(f, kUp), 0.f);  // at most 2^100 each
+  else
+    pair_add(acc.huge, scaled_squares(f, kDown), 0.f);  // at most 2^101 each; infinite or NaN stays
 }
 
 // Chunk `local` of a tensor: whole vectors of 16 bytes where there are any, single
@@ -105,7 +105,7 @@ __global__ void __launch_bounds__(kThreads, kClipNormBlocks) clip_norm_kernel(co
   chain_trigger();
   __shared__ Pair sh[kThreads / 32];
   __shared__ double shr[kThreads / 32];
-  Squares acc = {{0.f, 0.f}, 0.0};
+  Squares acc = {};
   for (int c = blockIdx.x; c < p.chunks; c += gridDim.x) {
     const ClipTensor& t = p.t[tensor_of(p, c)];
     if (t.fp32)
@@ -113,9 +113,11 @@ __global__ void __launch_bounds__(kThreads, kClipNormBlocks) clip_norm_kernel(co
     else
       chunk_squares(static_cast<const __nv_bfloat16*>(t.g), t, c - t.chunk0, acc);
   }
-  const Pair s = warp_sum_pair(acc.small);
-  double r = acc.rest;
-  if (__any_sync(0xffffffffu, r != 0.0))  // also where it is NaN
+  const Pair s = warp_sum_pair(acc.plain);
+  double r = 0.0;  // what the other two hold, rarely anything
+  if (acc.tiny.hi != 0.f || acc.huge.hi != 0.f)  // also where one is NaN
+    r = pair_value(acc.tiny) * 0x1p-180 + pair_value(acc.huge) * 0x1p160;
+  if (__any_sync(0xffffffffu, r != 0.0))
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) r += __shfl_down_sync(0xffffffffu, r, o);
   if ((threadIdx.x & 31) == 0) {

@@ -13,8 +13,8 @@
 //   backward  persistent blocks of 16 warps, W of them to a row, which copy rows ahead
 //             into shared memory and keep their columns' sums of g xh and g in
 //             registers over all rows of the block (the widest rows: one row ahead in
-//             registers, the sums in shared memory).  The blocks' sums are added in order by a second kernel,
-//             so results do not depend on timing;
+//             registers, the sums in shared memory).  The blocks' sums are added in
+//             order by a second kernel, so results do not depend on timing;
 //   wider rows are read again from L2 instead, one warp a row.
 #include "mls_device.cuh"
 #include "mls_kernels.h"
@@ -29,12 +29,20 @@ __device__ __forceinline__ void group_sync(int id, int threads) {
 
 // ------------------------------------------------------------------ forward
 // V vectors a lane, W warps a row: vector j of warp w's lane l is number (j W + w) 32 + l.
+// Rows of at most 8 or 16 vectors (V = W = 1) take L lanes each, 32 / L of them a warp.
 template <int W>
-constexpr int kFwdRows = W < 4 ? 4 / W : 1;
+constexpr int kFwdGroups = W < 4 ? 4 / W : 1;  // groups of W warps a block
 
-template <int W>
+template <int L>
+__device__ __forceinline__ float lane_sum(float v) {
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+template <int W, int L>
 __device__ __forceinline__ float row_sum(float v, float* sh, int id, int w) {
-  v = warp_sum(v);
+  v = lane_sum<L>(v);
   if constexpr (W > 1) {
     if ((threadIdx.x & 31) == 0) sh[w] = v;
     group_sync(id, 32 * W);
@@ -45,20 +53,22 @@ __device__ __forceinline__ float row_sum(float v, float* sh, int id, int w) {
   return v;
 }
 
-template <typename E, int V, int W>
-__global__ void __launch_bounds__(32 * W * kFwdRows<W>) norm_fwd_kernel(const NormParams p) {
-  constexpr int N = Vec<E>::N, N2 = Vec2<E>::N;
-  __shared__ float sh[kFwdRows<W>][2][W];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = warp / W, w = warp % W;
-  const long long t = static_cast<long long>(blockIdx.x) * kFwdRows<W> + group;
-  if (t >= p.T) return;  // whole groups
+template <typename E, int V, int W, int L>
+__global__ void __launch_bounds__(32 * W * kFwdGroups<W>) norm_fwd_kernel(const NormParams p) {
+  constexpr int N = Vec<E>::N, N2 = Vec2<E>::N, kRows = 32 / L;
+  __shared__ float sh[kFwdGroups<W>][2][W];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & (L - 1), group = warp / W, w = warp % W;
+  const long long t0 = (static_cast<long long>(blockIdx.x) * kFwdGroups<W> + group) * kRows;
+  if (t0 >= p.T) return;  // whole groups
+  const long long t = t0 + (threadIdx.x & 31) / L;
+  const int d = kRows == 1 || t < p.T ? p.d : 0;  // a row past the last one has no values
   const E* x = static_cast<const E*>(p.x) + t * p.d;
   E* y = static_cast<E*>(p.y) + t * p.d;
   uint4 u[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    const int k = ((j * W + w) * 32 + lane) * N;
-    u[j] = k < p.d ? ld16(x + k) : make_uint4(0u, 0u, 0u, 0u);
+    const int k = ((j * W + w) * L + lane) * N;
+    u[j] = k < d ? ld16(x + k) : make_uint4(0u, 0u, 0u, 0u);
   }
   const float inv_d = 1.0f / static_cast<float>(p.d);
   F2 f[V][N2];
@@ -69,21 +79,21 @@ __global__ void __launch_bounds__(32 * W * kFwdRows<W>) norm_fwd_kernel(const No
 #pragma unroll
     for (int i = 0; i < N2; ++i) s = f2_add(s, f[j][i]);
   }
-  const float mu = row_sum<W>(f2_sum(s), sh[group][0], 1 + group, w) * inv_d;
+  const float mu = row_sum<W, L>(f2_sum(s), sh[group][0], 1 + group, w) * inv_d;
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    const bool in = ((j * W + w) * 32 + lane) * N < p.d;
+    const bool in = ((j * W + w) * L + lane) * N < d;
 #pragma unroll
     for (int i = 0; i < N2; ++i) {
       f[j][i] = f2_add(f[j][i], f2(in ? -mu : 0.f));
       q = f2_fma(f[j][i], f[j][i], q);
     }
   }
-  const float r = 1.0f / sqrtf(row_sum<W>(f2_sum(q), sh[group][1], 1 + group, w) * inv_d + p.eps);
+  const float r = 1.0f / sqrtf(row_sum<W, L>(f2_sum(q), sh[group][1], 1 + group, w) * inv_d + p.eps);
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    const int k = ((j * W + w) * 32 + lane) * N;
-    if (k < p.d) {
+    const int k = ((j * W + w) * L + lane) * N;
+    if (k < d) {
       // no gain: ones, no bias: zeros
       const uint32_t one = Vec2<E>::kOne;
       F2 g[N2], b[N2];
@@ -94,7 +104,7 @@ __global__ void __launch_bounds__(32 * W * kFwdRows<W>) norm_fwd_kernel(const No
       st16(y + k, Vec2<E>::pack(f[j]));
     }
   }
-  if (w == 0 && lane == 0 && p.mean) {
+  if (w == 0 && lane == 0 && d > 0 && p.mean) {
     p.mean[t] = mu;
     p.rstd[t] = r;
   }
@@ -118,12 +128,14 @@ __device__ __forceinline__ void copy_wait() {
 // (cp.async: a lane waits for and reads its own copies only, so no barrier is needed):
 // with a row ahead in registers alone, 32 KB were in flight on an SM, and 65536 x
 // 4096 bf16 values took 372 us.
-template <typename E, int V, int W, int S>
+template <typename E, int V, int W, int S, int L>
 __global__ void __launch_bounds__(32 * kBwdWarps, 1) norm_bwd_kernel(const NormParams p) {
   constexpr int N = Vec<E>::N, N2 = Vec2<E>::N, kGroups = kBwdWarps / W, kThreads = 32 * kBwdWarps;
+  constexpr int kRows = 32 / L;
   extern __shared__ __align__(16) uint4 ring[];  // [S][x, g][V][kThreads], after the loop the sums [2][d]
   __shared__ float2 sh[2][kBwdWarps];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = warp / W, w = warp % W;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & (L - 1), part = (threadIdx.x & 31) / L;
+  const int group = warp / W, w = warp % W;
   const E* gain = static_cast<const E*>(p.gain);
   const float inv_d = 1.0f / static_cast<float>(p.d);
   const uint32_t one = Vec2<E>::kOne;
@@ -131,13 +143,14 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 1) norm_bwd_kernel(const NormP
   F2 dg[V][N2], db[V][N2];
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    const int k = ((j * W + w) * 32 + lane) * N;
+    const int k = ((j * W + w) * L + lane) * N;
     gv[j] = gain && k < p.d ? ld16(gain + k) : make_uint4(one, one, one, one);
 #pragma unroll
     for (int i = 0; i < N2; ++i) dg[j][i] = db[j][i] = 0;
   }
-  const long long step = static_cast<long long>(gridDim.x) * kGroups;
-  long long t = static_cast<long long>(blockIdx.x) * kGroups + group;
+  const long long step = static_cast<long long>(gridDim.x) * kGroups * kRows;
+  long long t0 = (static_cast<long long>(blockIdx.x) * kGroups + group) * kRows;  // the warp's first row
+  long long t = t0 + part;
   const uint32_t mine = smem_u32(ring) + threadIdx.x * 16;
   auto fetch = [&](long long row, int slot) {
     if (row < p.T) {
@@ -145,7 +158,7 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 1) norm_bwd_kernel(const NormP
       const E* g = static_cast<const E*>(p.dy) + row * p.d;
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const int k = ((j * W + w) * 32 + lane) * N;
+        const int k = ((j * W + w) * L + lane) * N;
         if (k < p.d) {
           copy16_async(mine + (slot * 2 * V + j) * kThreads * 16, x + k);
           copy16_async(mine + (slot * 2 * V + V + j) * kThreads * 16, g + k);
@@ -162,7 +175,8 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 1) norm_bwd_kernel(const NormP
     r = p.rstd[t];
   }
   int slot = 0;
-  for (int it = 0; t < p.T; t += step, it ^= 1) {
+  for (int it = 0; t0 < p.T; t0 += step, t += step, it ^= 1) {
+    const int d = kRows == 1 || t < p.T ? p.d : 0;  // a row past the last one has no values
     fetch(t + (S - 1) * step, slot == 0 ? S - 1 : slot - 1);  // the slot read in the round before
     copy_wait<S - 1>();
     const F2 nmu = f2(-mu), r2 = f2(r);
@@ -173,8 +187,8 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 1) norm_bwd_kernel(const NormP
     F2 a2 = 0, b2 = 0, xh[V][N2], h[V][N2];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      const int k = ((j * W + w) * 32 + lane) * N;
-      if (k < p.d) {
+      const int k = ((j * W + w) * L + lane) * N;
+      if (k < d) {
         F2 g[N2], gn[N2];
         Vec2<E>::unpack(ring[(slot * 2 * V + j) * kThreads + threadIdx.x], xh[j]);
         Vec2<E>::unpack(ring[(slot * 2 * V + V + j) * kThreads + threadIdx.x], g);
@@ -191,7 +205,7 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 1) norm_bwd_kernel(const NormP
       }
     }
     slot = slot + 1 == S ? 0 : slot + 1;
-    float a = warp_sum(f2_sum(a2)), b = warp_sum(f2_sum(b2));
+    float a = lane_sum<L>(f2_sum(a2)), b = lane_sum<L>(f2_sum(b2));
     if constexpr (W > 1) {
       // One barrier a row: the next row's words are the other half, and a warp comes back
       // to this one only past that row's barrier, when all have read it.
@@ -209,8 +223,8 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 1) norm_bwd_kernel(const NormP
     E* dx = static_cast<E*>(p.dx) + t * p.d;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      const int k = ((j * W + w) * 32 + lane) * N;
-      if (k < p.d) {
+      const int k = ((j * W + w) * L + lane) * N;
+      if (k < d) {
 #pragma unroll
         for (int i = 0; i < N2; ++i)
           h[j][i] = f2_mul(f2_fma(xh[j][i], nb, f2_add(h[j][i], na)), r2);
@@ -221,16 +235,26 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 1) norm_bwd_kernel(const NormP
   copy_wait<0>();
   chain_trigger();  // the second kernel's launch, under the last rows
   if (!p.part) return;
+  if constexpr (kRows > 1) {  // the warp's rows into its first lanes
+    static_assert(V == 1, "one vector a lane");
+#pragma unroll
+    for (int i = 0; i < N2; ++i)
+#pragma unroll
+      for (int o = L; o < 32; o <<= 1) {
+        dg[0][i] = f2_add(dg[0][i], __shfl_xor_sync(0xffffffffu, dg[0][i], o));
+        db[0][i] = f2_add(db[0][i], __shfl_xor_sync(0xffffffffu, db[0][i], o));
+      }
+  }
 
   // ---- the block's sums: its groups' one after the other
   float* out = p.part + 2ll * p.d * blockIdx.x;
   float* sums = reinterpret_cast<float*>(ring);
   __syncthreads();
   for (int q = 0; q < kGroups; ++q) {
-    if (group == q) {
+    if (group == q && part == 0) {
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const int k = ((j * W + w) * 32 + lane) * N;
+        const int k = ((j * W + w) * L + lane) * N;
         if (k < p.d) {
           float* s = q + 1 < kGroups ? sums : out;  // the last group writes the block's share
 #pragma unroll
@@ -512,14 +536,16 @@ unsigned blocks_of(long long n, int per) { return static_cast<unsigned>((n + per
 
 // Widest rows of the cached backward: 128 KB of sums in shared memory.
 constexpr int kBwdSharedMost = 16384;
-template <typename E, int V, int W>
+template <typename E, int V, int W, int L = 32>
 cudaError_t fwd(const NormParams& p, cudaStream_t s) {
-  norm_fwd_kernel<E, V, W><<<blocks_of(p.T, kFwdRows<W>), 32 * W * kFwdRows<W>, 0, s>>>(p);
+  norm_fwd_kernel<E, V, W, L><<<blocks_of(p.T, kFwdGroups<W> * (32 / L)), 32 * W * kFwdGroups<W>, 0, s>>>(p);
   return cudaGetLastError();
 }
 
 template <typename E>
 cudaError_t fwd_any(const NormParams& p, cudaStream_t s) {
+  if (p.d <= 8 * Vec<E>::N) return fwd<E, 1, 1, 8>(p, s);
+  if (p.d <= 16 * Vec<E>::N) return fwd<E, 1, 1, 16>(p, s);
   const int v = (p.d + 32 * Vec<E>::N - 1) / (32 * Vec<E>::N);  // vectors a lane of one warp
   if (v <= 1) return fwd<E, 1, 1>(p, s);
   if (v <= 2) return fwd<E, 2, 1>(p, s);
@@ -541,10 +567,10 @@ constexpr int kRows = V >= 4 ? 3 : V == 2 ? 5 : 8;
 template <int V>
 constexpr size_t kRingBytes = sizeof(uint4) * 2 * V * 32 * kBwdWarps * kRows<V>;
 
-template <typename E, int V, int W>
+template <typename E, int V, int W, int L = 32>
 cudaError_t bwd(const NormParams& p, cudaStream_t s) {
   static_assert(sizeof(float) * 2 * V * W * 32 * Vec<E>::N <= kRingBytes<V>, "the sums fit in the ring's memory");
-  norm_bwd_kernel<E, V, W, kRows<V>><<<p.splits, 32 * kBwdWarps, kRingBytes<V>, s>>>(p);
+  norm_bwd_kernel<E, V, W, kRows<V>, L><<<p.splits, 32 * kBwdWarps, kRingBytes<V>, s>>>(p);
   return cudaGetLastError();
 }
 template <typename E, int V>
@@ -555,6 +581,8 @@ cudaError_t bwd_shared(const NormParams& p, cudaStream_t s) {
 
 template <typename E>
 cudaError_t bwd_any(const NormParams& p, cudaStream_t s) {
+  if (p.d <= 8 * Vec<E>::N) return bwd<E, 1, 1, 8>(p, s);
+  if (p.d <= 16 * Vec<E>::N) return bwd<E, 1, 1, 16>(p, s);
   const int v = (p.d + 32 * Vec<E>::N - 1) / (32 * Vec<E>::N);
   if (v <= 1) return bwd<E, 1, 1>(p, s);
   if (v <= 2) return bwd<E, 2, 1>(p, s);
@@ -577,9 +605,10 @@ bool bwd_cached(int d) { return d <= kBwdSharedMost; }
 // warps need for one row each and at most one an SM.
 int norm_splits(long long T, int d, bool fp32, int sms) {
   if (bwd_cached(d)) {
-    const int v = (d + 32 * (fp32 ? 4 : 8) - 1) / (32 * (fp32 ? 4 : 8));
-    const int groups = kBwdWarps / (v <= 2 ? 1 : v <= 4 ? 2 : v <= 8 ? 4 : v <= 16 ? 8 : 16);
-    const long long blocks = (T + groups - 1) / groups;
+    const int n = fp32 ? 4 : 8, v = (d + 32 * n - 1) / (32 * n);
+    const int rows = d <= 8 * n ? 4 * kBwdWarps : d <= 16 * n ? 2 * kBwdWarps  // of a block at a time
+                     : kBwdWarps / (v <= 2 ? 1 : v <= 4 ? 2 : v <= 8 ? 4 : v <= 16 ? 8 : 16);
+    const long long blocks = (T + rows - 1) / rows;
     return blocks < 1 ? 1 : blocks < sms ? static_cast<int>(blocks) : sms;
   }
   const long long cols = (d + kColThreads - 1) / kColThreads;
@@ -625,15 +654,17 @@ cudaError_t setup_norm_kernels() {
 #define MLS_SET(K, BYTES)                                                                     \
   e = cudaFuncSetAttribute(K, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(BYTES)); \
   if (e != cudaSuccess) return e;
-#define MLS_SET_RING(E, V, W) MLS_SET((norm_bwd_kernel<E, V, W, kRows<V>>), kRingBytes<V>)
-#define MLS_SET_BOTH(V, W) MLS_SET_RING(float, V, W) MLS_SET_RING(__nv_bfloat16, V, W)
-  MLS_SET_BOTH(1, 1)
-  MLS_SET_BOTH(2, 1)
-  MLS_SET_BOTH(2, 2)
-  MLS_SET_BOTH(2, 4)
-  MLS_SET_BOTH(2, 8)
-  MLS_SET_BOTH(2, 16)
-  MLS_SET_RING(float, 4, 16)
+#define MLS_SET_RING(E, V, W, L) MLS_SET((norm_bwd_kernel<E, V, W, kRows<V>, L>), kRingBytes<V>)
+#define MLS_SET_BOTH(V, W, L) MLS_SET_RING(float, V, W, L) MLS_SET_RING(__nv_bfloat16, V, W, L)
+  MLS_SET_BOTH(1, 1, 8)
+  MLS_SET_BOTH(1, 1, 16)
+  MLS_SET_BOTH(1, 1, 32)
+  MLS_SET_BOTH(2, 1, 32)
+  MLS_SET_BOTH(2, 2, 32)
+  MLS_SET_BOTH(2, 4, 32)
+  MLS_SET_BOTH(2, 8, 32)
+  MLS_SET_BOTH(2, 16, 32)
+  MLS_SET_RING(float, 4, 16, 32)
   MLS_SET((norm_bwd_shared_kernel<float, 8>), sizeof(float) * 2 * kBwdSharedMost)
   MLS_SET((norm_bwd_shared_kernel<__nv_bfloat16, 4>), sizeof(float) * 2 * kBwdSharedMost)
 #undef MLS_SET_BOTH

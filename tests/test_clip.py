@@ -41,7 +41,7 @@ def check(grads, max_norm):
     if want > torch.finfo(torch.float32).max:  # reported in 32 bits, which end at 3.4e38; c is not affected
         assert norm == math.inf
     else:
-        assert abs(norm - want) <= 8 * U * want
+        assert abs(norm - want) <= 8 * U * want + 2.0 ** -150  # half a step of the smallest fp32 values
     c = min(1.0, max_norm / (want + 1e-6)) if math.isfinite(max_norm) else 1.0
     assert abs(coef - c) <= 10 * U * c
     for g, b in zip(grads, before):
@@ -88,6 +88,16 @@ def test_squares_beyond_fp32(scale, dtype):
     """Norms whose squares overflow or vanish in 32 bits."""
     norm, _ = check(tensors([5000, 300], seed=1, dtypes=(dtype,), scale=scale), scale)
     assert norm > 0 and math.isfinite(norm) == (scale < 3e37)  # 72 x 3e37 is past fp32's largest value
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("scale", [1e-44, 1e-41, 1e-38, 1e-34, 1e-13, 1e-12])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_smallest_gradients(scale, dtype):
+    """Down to the smallest values of either type (bf16 has none at 1e-44), and across the
+    border at which squares are taken of scaled values."""
+    norm, _ = check(tensors([50000, 300, 8192], seed=1, dtypes=(dtype,), scale=scale), math.inf)
+    assert (norm > 0) == (dtype is torch.float32 or scale > 1e-43)
 
 
 @pytest.mark.gpu
