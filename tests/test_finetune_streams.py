@@ -73,6 +73,18 @@ def test_two_streams_at_once():
     assert mls.mls_get_status() == 0
 
 
+def test_another_current_device_is_refused(monkeypatch):
+    """An object's calls run on the device that it was made on, or not at all."""
+    x = torch.zeros(4, 64, dtype=torch.bfloat16, device="cuda")
+    norm, clip = mls.LayerNorm(4, 64, gain=False, bias=False), mls.GradClip([x])
+    index = torch.cuda.current_device()
+    monkeypatch.setattr(B, "_get_device", lambda: index + 1)
+    for call in (lambda: norm.forward(x), lambda: norm.backward(x, x), lambda: clip(1.0),
+                 lambda: mls.mls_layer_norm_fwd(x, None, None, 1e-5, x)):
+        with pytest.raises(ValueError, match="current device"):
+            call()
+
+
 CAPTURE = r"""
 import sys
 sys.path.insert(0, {root!r}); sys.path.insert(0, {root!r} + "/tests")
