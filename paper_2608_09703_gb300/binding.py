@@ -381,9 +381,15 @@ def mls_head_logp_bwd(prob: "Problem", H, W, targets, lse, dlogp, dH, dW, ws, st
     _check(rc, "mls_head_logp_bwd")
 
 
+def _width(d: int) -> int:
+    if d >> 31:  # ctypes would cut it
+        raise ValueError(f"d = {d}: past 32 bits")
+    return d
+
+
 def mls_layer_norm_fwd(x, gain, bias, eps: float, y, mean=None, rstd=None, stream=None) -> None:
     """y = (x - mean) rstd gain + bias per row of x [T, d] (see include/mls.h)."""
-    T, d = x.shape
+    T, d = x.shape[0], _width(x.shape[1])
     code = _dtype_code(x)
     dev = _expect("x", x, x.dtype, (T, d))
     _expect("y", y, x.dtype, (T, d), dev)
@@ -403,7 +409,7 @@ def mls_layer_norm_workspace_size(T: int, d: int) -> int:
 
 
 def mls_layer_norm_bwd(x, gain, dy, mean, rstd, dx, dgain, dbias, ws, stream=None) -> None:
-    T, d = x.shape
+    T, d = x.shape[0], _width(x.shape[1])
     code = _dtype_code(x)
     dev = _expect("x", x, x.dtype, (T, d))
     _expect("dy", dy, x.dtype, (T, d), dev)
@@ -433,6 +439,8 @@ class PolicyProblem:
                  adv_per_seq: bool = False, w: Optional[Sequence[float]] = None):
         if w is not None and len(w) != M:
             raise ValueError(f"w: {len(w)} weights for {M} sub-models")
+        if max(M, B) >> 31:  # ctypes would cut it
+            raise ValueError(f"M = {M}, B = {B}: past 32 bits")
         self.w = None if w is None else (ctypes.c_float * M)(*[float(x) for x in w])
         self.c = mls_policy_problem(int(M), int(T), int(V), int(B), float(clip_low), float(clip_high),
                                     float(beta), _AGG[agg], int(bool(adv_per_seq)), self.w)
@@ -657,7 +665,7 @@ class LayerNorm:
     def __init__(self, T, d, eps=1e-5, gain=True, bias=True, dtype=torch.bfloat16, device="cuda",
                  backward=True):
         self.eps, self.gain, self.bias = float(eps), gain, bias
-        self.shape, self.dtype = (T, d), dtype
+        self.shape, self.dtype = (T, _width(d)), dtype
         self.code = MLS_BF16 if dtype is torch.bfloat16 else MLS_FP32
         if dtype not in (torch.bfloat16, torch.float32):
             raise TypeError(dtype)

@@ -1304,8 +1304,9 @@ extern "C" int mls_layer_norm_fwd(int64_t T, int32_t d, int32_t in_dtype, float 
 
 extern "C" size_t mls_layer_norm_workspace_size(int64_t T, int32_t d) {
   if (T < 0 || T > INT_MAX || d < 1 || d > kNormMostWidth) return 0;
-  // fp32 rows take more warps each, so at least as many blocks as bf16 ones
-  return align_up(sizeof(float) * 2 * static_cast<size_t>(d) * norm_splits(T, d, true, current_sms()));
+  // of the two types, whichever takes more blocks
+  const int sms = current_sms(), a = norm_splits(T, d, true, sms), b = norm_splits(T, d, false, sms);
+  return align_up(sizeof(float) * 2 * static_cast<size_t>(d) * (a > b ? a : b));
 }
 
 extern "C" int mls_layer_norm_bwd(int64_t T, int32_t d, int32_t in_dtype, const void* x,

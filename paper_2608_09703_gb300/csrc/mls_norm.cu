@@ -12,9 +12,9 @@
 //             vectors a lane;
 //   backward  persistent blocks of 16 warps, W of them to a row, which copy rows ahead
 //             into shared memory and keep their columns' sums of g xh and g in
-//             registers over all rows of the block (the widest rows: one row ahead in
-//             registers, the sums in shared memory).  The blocks' sums are added in
-//             order by a second kernel, so results do not depend on timing;
+//             registers over all rows of the block (the widest fp32 rows: split over a
+//             cluster of two CTAs).  The blocks' sums are added in order by a second
+//             kernel, so results do not depend on timing;
 //   wider rows are read again from L2 instead, one warp a row.
 #include "mls_device.cuh"
 #include "mls_kernels.h"
@@ -124,16 +124,28 @@ __device__ __forceinline__ void copy_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
+__device__ __forceinline__ void store_remote(uint32_t cluster_addr, float a, float b) {
+  asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(cluster_addr), "f"(a), "f"(b) : "memory");
+}
+
 // S rows of every lane's own vectors in shared memory, S - 1 of them being copied there
 // (cp.async: a lane waits for and reads its own copies only, so no barrier is needed):
 // with a row ahead in registers alone, 32 KB were in flight on an SM, and 65536 x
 // 4096 bf16 values took 372 us.
-template <typename E, int V, int W, int S, int L>
+// C = 2: the widest fp32 rows are split over a cluster of two CTAs, half the columns each, which
+// exchange their sums of each row through shared memory.
+template <typename E, int V, int W, int S, int L, int C>
 __global__ void __launch_bounds__(32 * kBwdWarps, 1) norm_bwd_kernel(const NormParams p) {
   constexpr int N = Vec<E>::N, N2 = Vec2<E>::N, kGroups = kBwdWarps / W, kThreads = 32 * kBwdWarps;
   constexpr int kRows = 32 / L;
+  static_assert(C == 1 || (W == kBwdWarps && L == 32), "a split row takes all warps of both CTAs");
+  const int rank = C == 1 ? 0 : static_cast<int>(cluster_ctarank());
+  // the CTA's columns [from, to): halves of whole vectors of all lanes of a warp
+  const int half = C == 1 ? 0 : (p.d / 2 + 32 * N - 1) / (32 * N) * (32 * N);
+  const int from = rank * half, to = C == 1 || rank == 1 ? p.d : half;
+  const unsigned block = blockIdx.x / C, blocks = gridDim.x / C;
   extern __shared__ __align__(16) uint4 ring[];  // [S][x, g][V][kThreads], after the loop the sums [2][d]
-  __shared__ float2 sh[2][kBwdWarps];
+  __shared__ float2 sh[2][C * kBwdWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & (L - 1), part = (threadIdx.x & 31) / L;
   const int group = warp / W, w = warp % W;
   const E* gain = static_cast<const E*>(p.gain);
@@ -143,13 +155,13 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 1) norm_bwd_kernel(const NormP
   F2 dg[V][N2], db[V][N2];
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    const int k = ((j * W + w) * L + lane) * N;
-    gv[j] = gain && k < p.d ? ld16(gain + k) : make_uint4(one, one, one, one);
+    const int k = from + ((j * W + w) * L + lane) * N;
+    gv[j] = gain && k < to ? ld16(gain + k) : make_uint4(one, one, one, one);
 #pragma unroll
     for (int i = 0; i < N2; ++i) dg[j][i] = db[j][i] = 0;
   }
-  const long long step = static_cast<long long>(gridDim.x) * kGroups * kRows;
-  long long t0 = (static_cast<long long>(blockIdx.x) * kGroups + group) * kRows;  // the warp's first row
+  const long long step = static_cast<long long>(blocks) * kGroups * kRows;
+  long long t0 = (static_cast<long long>(block) * kGroups + group) * kRows;  // the warp's first row
   long long t = t0 + part;
   const uint32_t mine = smem_u32(ring) + threadIdx.x * 16;
   auto fetch = [&](long long row, int slot) {
@@ -158,8 +170,8 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 1) norm_bwd_kernel(const NormP
       const E* g = static_cast<const E*>(p.dy) + row * p.d;
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const int k = ((j * W + w) * L + lane) * N;
-        if (k < p.d) {
+        const int k = from + ((j * W + w) * L + lane) * N;
+        if (k < to) {
           copy16_async(mine + (slot * 2 * V + j) * kThreads * 16, x + k);
           copy16_async(mine + (slot * 2 * V + V + j) * kThreads * 16, g + k);
         }
@@ -169,6 +181,7 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 1) norm_bwd_kernel(const NormP
   };
 #pragma unroll
   for (int q = 0; q < S - 1; ++q) fetch(t + q * step, q);
+  if constexpr (C > 1) cluster_sync();  // both CTAs run before either writes to the other
   float mu = 0.f, r = 0.f;
   if (t < p.T) {
     mu = p.mean[t];
@@ -176,7 +189,7 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 1) norm_bwd_kernel(const NormP
   }
   int slot = 0;
   for (int it = 0; t0 < p.T; t0 += step, t += step, it ^= 1) {
-    const int d = kRows == 1 || t < p.T ? p.d : 0;  // a row past the last one has no values
+    const int d = kRows == 1 || t < p.T ? to : 0;  // a row past the last one has no values
     fetch(t + (S - 1) * step, slot == 0 ? S - 1 : slot - 1);  // the slot read in the round before
     copy_wait<S - 1>();
     const F2 nmu = f2(-mu), r2 = f2(r);
@@ -184,29 +197,52 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 1) norm_bwd_kernel(const NormP
       mu = p.mean[t + step];
       r = p.rstd[t + step];
     }
-    F2 a2 = 0, b2 = 0, xh[V][N2], h[V][N2];
+    // xh and h stay in registers; where those hold 64 sums they are formed again from the ring
+    constexpr bool kAgain = V * N2 > 8;
+    F2 a2 = 0, b2 = 0, xh[kAgain ? 1 : V][N2], h[kAgain ? 1 : V][N2];
+    auto form = [&](int j, F2 (&x)[N2], F2 (&hh)[N2], F2 (&g)[N2]) {
+      F2 gn[N2];
+      Vec2<E>::unpack(ring[(slot * 2 * V + j) * kThreads + threadIdx.x], x);
+      Vec2<E>::unpack(ring[(slot * 2 * V + V + j) * kThreads + threadIdx.x], g);
+      Vec2<E>::unpack(gv[j], gn);
+#pragma unroll
+      for (int i = 0; i < N2; ++i) {
+        x[i] = f2_mul(f2_add(x[i], nmu), r2);
+        hh[i] = f2_mul(g[i], gn[i]);
+      }
+    };
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      const int k = ((j * W + w) * L + lane) * N;
+      const int k = from + ((j * W + w) * L + lane) * N;
       if (k < d) {
-        F2 g[N2], gn[N2];
-        Vec2<E>::unpack(ring[(slot * 2 * V + j) * kThreads + threadIdx.x], xh[j]);
-        Vec2<E>::unpack(ring[(slot * 2 * V + V + j) * kThreads + threadIdx.x], g);
-        Vec2<E>::unpack(gv[j], gn);
+        F2 g[N2];
+        constexpr int kKeep = kAgain ? 0 : 1;
+        form(j, xh[kKeep * j], h[kKeep * j], g);
 #pragma unroll
         for (int i = 0; i < N2; ++i) {
-          xh[j][i] = f2_mul(f2_add(xh[j][i], nmu), r2);
-          h[j][i] = f2_mul(g[i], gn[i]);
-          a2 = f2_add(a2, h[j][i]);
-          b2 = f2_fma(h[j][i], xh[j][i], b2);
-          dg[j][i] = f2_fma(g[i], xh[j][i], dg[j][i]);
+          a2 = f2_add(a2, h[kKeep * j][i]);
+          b2 = f2_fma(h[kKeep * j][i], xh[kKeep * j][i], b2);
+          dg[j][i] = f2_fma(g[i], xh[kKeep * j][i], dg[j][i]);
           db[j][i] = f2_add(db[j][i], g[i]);
         }
       }
     }
-    slot = slot + 1 == S ? 0 : slot + 1;
     float a = lane_sum<L>(f2_sum(a2)), b = lane_sum<L>(f2_sum(b2));
-    if constexpr (W > 1) {
+    if constexpr (C > 1) {
+      // as below, with the other CTA's sums: every warp writes its own to both
+      if (lane == 0) {
+        sh[it][rank * W + w] = make_float2(a, b);
+        store_remote(map_to_rank(smem_u32(&sh[it][rank * W + w]), rank ^ 1), a, b);
+      }
+      cluster_sync();
+      a = b = 0.f;
+#pragma unroll
+      for (int i = 0; i < C * W; ++i) {
+        const float2 v = sh[it][i];
+        a += v.x;
+        b += v.y;
+      }
+    } else if constexpr (W > 1) {
       // One barrier a row: the next row's words are the other half, and a warp comes back
       // to this one only past that row's barrier, when all have read it.
       if (lane == 0) sh[it][warp] = make_float2(a, b);
@@ -223,16 +259,23 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 1) norm_bwd_kernel(const NormP
     E* dx = static_cast<E*>(p.dx) + t * p.d;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      const int k = ((j * W + w) * L + lane) * N;
+      const int k = from + ((j * W + w) * L + lane) * N;
       if (k < d) {
+        constexpr int kKeep = kAgain ? 0 : 1;
+        if constexpr (kAgain) {
+          F2 g[N2];
+          form(j, xh[0], h[0], g);
+        }
 #pragma unroll
         for (int i = 0; i < N2; ++i)
-          h[j][i] = f2_mul(f2_fma(xh[j][i], nb, f2_add(h[j][i], na)), r2);
-        st16(dx + k, Vec2<E>::pack(h[j]));
+          h[kKeep * j][i] = f2_mul(f2_fma(xh[kKeep * j][i], nb, f2_add(h[kKeep * j][i], na)), r2);
+        st16(dx + k, Vec2<E>::pack(h[kKeep * j]));
       }
     }
+    slot = slot + 1 == S ? 0 : slot + 1;
   }
   copy_wait<0>();
+  if constexpr (C > 1) cluster_sync();  // the other CTA's last words have arrived here
   chain_trigger();  // the second kernel's launch, under the last rows
   if (!p.part) return;
   if constexpr (kRows > 1) {  // the warp's rows into its first lanes
@@ -247,15 +290,15 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 1) norm_bwd_kernel(const NormP
   }
 
   // ---- the block's sums: its groups' one after the other
-  float* out = p.part + 2ll * p.d * blockIdx.x;
+  float* out = p.part + 2ll * p.d * block;
   float* sums = reinterpret_cast<float*>(ring);
   __syncthreads();
   for (int q = 0; q < kGroups; ++q) {
     if (group == q && part == 0) {
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const int k = ((j * W + w) * L + lane) * N;
-        if (k < p.d) {
+        const int k = from + ((j * W + w) * L + lane) * N;
+        if (k < to) {
           float* s = q + 1 < kGroups ? sums : out;  // the last group writes the block's share
 #pragma unroll
           for (int i = 0; i < N; i += 4) {
@@ -278,115 +321,6 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 1) norm_bwd_kernel(const NormP
     }
     __syncthreads();
   }
-}
-
-// One row's vectors of a lane, and the row's statistics.
-template <int V>
-struct BwdRow {
-  uint4 x[V], g[V];
-  float mu, r;
-};
-
-template <typename E, int V, int W>
-__device__ __forceinline__ void load_row(const NormParams& p, long long t, int w, int lane, BwdRow<V>& b) {
-  constexpr int N = Vec<E>::N;
-  if (t >= p.T) return;
-  const E* x = static_cast<const E*>(p.x) + t * p.d;
-  const E* g = static_cast<const E*>(p.dy) + t * p.d;
-#pragma unroll
-  for (int j = 0; j < V; ++j) {
-    const int k = ((j * W + w) * 32 + lane) * N;
-    if (k < p.d) {
-      b.x[j] = ld16(x + k);
-      b.g[j] = ld16(g + k);
-    }
-  }
-  b.mu = p.mean[t];
-  b.r = p.rstd[t];
-}
-
-// The widest rows: the columns' sums lie in shared memory and the gain is read at each
-// row, from L1 or L2.
-template <typename E, int V>
-__global__ void __launch_bounds__(32 * kBwdWarps, 1) norm_bwd_shared_kernel(const NormParams p) {
-  constexpr int N = Vec<E>::N, N2 = Vec2<E>::N, W = kBwdWarps;
-  extern __shared__ __align__(16) float sums[];  // [2][d]
-  __shared__ float2 sh[2][kBwdWarps];
-  const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const E* gain = static_cast<const E*>(p.gain);
-  const float inv_d = 1.0f / static_cast<float>(p.d);
-  const uint32_t one = Vec2<E>::kOne;
-  for (int c = threadIdx.x; c < 2 * p.d; c += 32 * kBwdWarps) sums[c] = 0.f;
-  __syncthreads();
-
-  const long long step = gridDim.x;
-  long long t = blockIdx.x;
-  BwdRow<V> next;
-  load_row<E, V, W>(p, t, w, lane, next);
-  for (int it = 0; t < p.T; t += step, it ^= 1) {
-    BwdRow<V> cur = next;
-    load_row<E, V, W>(p, t + step, w, lane, next);
-    const F2 nmu = f2(-cur.mu), r2 = f2(cur.r);
-    F2 a2 = 0, b2 = 0, xh[V][N2], h[V][N2];
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const int k = ((j * W + w) * 32 + lane) * N;
-      if (k < p.d) {
-        F2 g[N2], gn[N2];
-        Vec2<E>::unpack(cur.x[j], xh[j]);
-        Vec2<E>::unpack(cur.g[j], g);
-        Vec2<E>::unpack(gain ? ld16(gain + k) : make_uint4(one, one, one, one), gn);
-        float sg[N], sb[N];
-#pragma unroll
-        for (int i = 0; i < N; i += 4) {
-          *reinterpret_cast<float4*>(sg + i) = *reinterpret_cast<const float4*>(sums + k + i);
-          *reinterpret_cast<float4*>(sb + i) = *reinterpret_cast<const float4*>(sums + p.d + k + i);
-        }
-#pragma unroll
-        for (int i = 0; i < N2; ++i) {
-          xh[j][i] = f2_mul(f2_add(xh[j][i], nmu), r2);
-          h[j][i] = f2_mul(g[i], gn[i]);
-          a2 = f2_add(a2, h[j][i]);
-          b2 = f2_fma(h[j][i], xh[j][i], b2);
-          f2_split(f2_fma(g[i], xh[j][i], f2(sg[2 * i], sg[2 * i + 1])), sg[2 * i], sg[2 * i + 1]);
-          f2_split(f2_add(g[i], f2(sb[2 * i], sb[2 * i + 1])), sb[2 * i], sb[2 * i + 1]);
-        }
-#pragma unroll
-        for (int i = 0; i < N; i += 4) {
-          *reinterpret_cast<float4*>(sums + k + i) = *reinterpret_cast<const float4*>(sg + i);
-          *reinterpret_cast<float4*>(sums + p.d + k + i) = *reinterpret_cast<const float4*>(sb + i);
-        }
-      }
-    }
-    float a = f2_sum(a2), b = f2_sum(b2);
-    a = warp_sum(a);
-    b = warp_sum(b);
-    if (lane == 0) sh[it][w] = make_float2(a, b);
-    __syncthreads();  // one a row, as above
-    a = b = 0.f;
-#pragma unroll
-    for (int i = 0; i < W; ++i) {
-      const float2 v = sh[it][i];
-      a += v.x;
-      b += v.y;
-    }
-    const F2 na = f2(-a * inv_d), nb = f2(-b * inv_d);
-    E* dx = static_cast<E*>(p.dx) + t * p.d;
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const int k = ((j * W + w) * 32 + lane) * N;
-      if (k < p.d) {
-#pragma unroll
-        for (int i = 0; i < N2; ++i)
-          h[j][i] = f2_mul(f2_fma(xh[j][i], nb, f2_add(h[j][i], na)), r2);
-        st16(dx + k, Vec2<E>::pack(h[j]));
-      }
-    }
-  }
-  if (!p.part) return;
-  float* out = p.part + 2ll * p.d * blockIdx.x;
-  __syncthreads();
-  for (int c = threadIdx.x; c < 2 * p.d; c += 32 * kBwdWarps) out[c] = sums[c];
 }
 
 // Blocks' shares [splits][2][d] -> dgain, dbias.  A block owns 32 vectors of four columns;
@@ -534,8 +468,6 @@ __global__ void __launch_bounds__(kColThreads) norm_cols_wide_kernel(const NormP
 
 unsigned blocks_of(long long n, int per) { return static_cast<unsigned>((n + per - 1) / per); }
 
-// Widest rows of the cached backward: 128 KB of sums in shared memory.
-constexpr int kBwdSharedMost = 16384;
 template <typename E, int V, int W, int L = 32>
 cudaError_t fwd(const NormParams& p, cudaStream_t s) {
   norm_fwd_kernel<E, V, W, L><<<blocks_of(p.T, kFwdGroups<W> * (32 / L)), 32 * W * kFwdGroups<W>, 0, s>>>(p);
@@ -567,17 +499,33 @@ constexpr int kRows = V >= 4 ? 3 : V == 2 ? 5 : 8;
 template <int V>
 constexpr size_t kRingBytes = sizeof(uint4) * 2 * V * 32 * kBwdWarps * kRows<V>;
 
-template <typename E, int V, int W, int L = 32>
+template <typename E, int V, int W, int L = 32, int C = 1>
 cudaError_t bwd(const NormParams& p, cudaStream_t s) {
   static_assert(sizeof(float) * 2 * V * W * 32 * Vec<E>::N <= kRingBytes<V>, "the sums fit in the ring's memory");
-  norm_bwd_kernel<E, V, W, kRows<V>, L><<<p.splits, 32 * kBwdWarps, kRingBytes<V>, s>>>(p);
-  return cudaGetLastError();
+  if constexpr (C == 1) {
+    norm_bwd_kernel<E, V, W, kRows<V>, L, 1><<<p.splits, 32 * kBwdWarps, kRingBytes<V>, s>>>(p);
+    return cudaGetLastError();
+  } else {
+    cudaLaunchAttribute attr = {};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = C;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(C * p.splits);
+    cfg.blockDim = dim3(32 * kBwdWarps);
+    cfg.dynamicSmemBytes = kRingBytes<V>;
+    cfg.stream = s;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, norm_bwd_kernel<E, V, W, kRows<V>, L, C>, p);
+    if (e != cudaSuccess) cudaGetLastError();
+    return e;
+  }
 }
-template <typename E, int V>
-cudaError_t bwd_shared(const NormParams& p, cudaStream_t s) {
-  norm_bwd_shared_kernel<E, V><<<p.splits, 32 * kBwdWarps, sizeof(float) * 2 * p.d, s>>>(p);
-  return cudaGetLastError();
-}
+
+// Widest rows of the cached backward: 16 warps of 4 vectors a lane, for fp32 in two CTAs.
+constexpr int kBwdWidest = 16384;
+bool bwd_cached(int d) { return d <= kBwdWidest; }
 
 template <typename E>
 cudaError_t bwd_any(const NormParams& p, cudaStream_t s) {
@@ -590,26 +538,25 @@ cudaError_t bwd_any(const NormParams& p, cudaStream_t s) {
   if (v <= 8) return bwd<E, 2, 4>(p, s);
   if (v <= 16) return bwd<E, 2, 8>(p, s);
   if (v <= 32) return bwd<E, 2, 16>(p, s);
-  if constexpr (Vec<E>::N == 8) {
-    return bwd_shared<E, 4>(p, s);  // 16384 values
-  } else {
-    return v <= 64 ? bwd<E, 4, 16>(p, s) : bwd_shared<E, 8>(p, s);
-  }
+  // bf16 values end here: split over two CTAs too, 16384 x 16384 took 426 us, a row's
+  // exchange through the cluster being 0.6 of the 2 us that the row takes
+  if (v <= 64) return bwd<E, 4, 16>(p, s);
+  if constexpr (Vec<E>::N == 4) return bwd<E, 4, 16, 32, 2>(p, s);
+  return cudaErrorInvalidValue;  // not reached: bwd_cached
 }
-
-bool bwd_cached(int d) { return d <= kBwdSharedMost; }
 
 }  // namespace
 
-// Shares of the column sums: the cached backward's blocks, as many as its groups of
-// warps need for one row each and at most one an SM.
+// Shares of the column sums: the cached backward's blocks (clusters, where rows are split),
+// as many as its groups of warps need for one row each and at most what the SMs hold.
 int norm_splits(long long T, int d, bool fp32, int sms) {
   if (bwd_cached(d)) {
     const int n = fp32 ? 4 : 8, v = (d + 32 * n - 1) / (32 * n);
     const int rows = d <= 8 * n ? 4 * kBwdWarps : d <= 16 * n ? 2 * kBwdWarps  // of a block at a time
                      : kBwdWarps / (v <= 2 ? 1 : v <= 4 ? 2 : v <= 8 ? 4 : v <= 16 ? 8 : 16);
     const long long blocks = (T + rows - 1) / rows;
-    return blocks < 1 ? 1 : blocks < sms ? static_cast<int>(blocks) : sms;
+    const int most = d > 64 * 32 * n ? (sms + 1) / 2 : sms;
+    return blocks < 1 ? 1 : blocks < most ? static_cast<int>(blocks) : most;
   }
   const long long cols = (d + kColThreads - 1) / kColThreads;
   long long s = (8ll * sms + cols - 1) / cols;
@@ -654,8 +601,8 @@ cudaError_t setup_norm_kernels() {
 #define MLS_SET(K, BYTES)                                                                     \
   e = cudaFuncSetAttribute(K, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(BYTES)); \
   if (e != cudaSuccess) return e;
-#define MLS_SET_RING(E, V, W, L) MLS_SET((norm_bwd_kernel<E, V, W, kRows<V>, L>), kRingBytes<V>)
-#define MLS_SET_BOTH(V, W, L) MLS_SET_RING(float, V, W, L) MLS_SET_RING(__nv_bfloat16, V, W, L)
+#define MLS_SET_RING(E, V, W, L, C) MLS_SET((norm_bwd_kernel<E, V, W, kRows<V>, L, C>), kRingBytes<V>)
+#define MLS_SET_BOTH(V, W, L) MLS_SET_RING(float, V, W, L, 1) MLS_SET_RING(__nv_bfloat16, V, W, L, 1)
   MLS_SET_BOTH(1, 1, 8)
   MLS_SET_BOTH(1, 1, 16)
   MLS_SET_BOTH(1, 1, 32)
@@ -664,9 +611,8 @@ cudaError_t setup_norm_kernels() {
   MLS_SET_BOTH(2, 4, 32)
   MLS_SET_BOTH(2, 8, 32)
   MLS_SET_BOTH(2, 16, 32)
-  MLS_SET_RING(float, 4, 16, 32)
-  MLS_SET((norm_bwd_shared_kernel<float, 8>), sizeof(float) * 2 * kBwdSharedMost)
-  MLS_SET((norm_bwd_shared_kernel<__nv_bfloat16, 4>), sizeof(float) * 2 * kBwdSharedMost)
+  MLS_SET_BOTH(4, 16, 32)
+  MLS_SET_RING(float, 4, 16, 32, 2)
 #undef MLS_SET_BOTH
 #undef MLS_SET_RING
 #undef MLS_SET

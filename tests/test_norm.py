@@ -80,6 +80,7 @@ def check(x, gain, bias, dy, eps=1e-5, op=None):
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("T,d", [(1, 8), (1, 16384), (2, 64), (1, 32), (5, 72), (67, 56), (130, 128), (1001, 104), (3001, 40), (3, 520), (5, 4104), (7, 1024), (33, 256),
                                  (130, 2056), (257, 1000), (300, 8192), (1531, 328), (2500, 64), (70, 16392),
+                                 (1, 8200), (153, 8200), (400, 12296), (76, 16384), (77, 16000),
                                  (9, 40000)])
 def test_against_the_definition(T, d, dtype):
     check(*inputs(T, d, dtype, True, True, seed=T + d))
