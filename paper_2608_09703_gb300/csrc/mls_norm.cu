@@ -12,8 +12,8 @@
 //             vectors a lane;
 //   backward  persistent blocks of 16 warps, W of them to a row, which copy rows ahead
 //             into shared memory and keep their columns' sums of g xh and g in
-//             registers over all rows of the block (the widest fp32 rows: split over a
-//             cluster of two CTAs).  The blocks' sums are added in order by a second
+//             registers over all rows of the block (the widest rows: split over a cluster of
+//             two CTAs).  The blocks' sums are added in order by a second
 //             kernel, so results do not depend on timing;
 //   wider rows are read again from L2 instead, one warp a row.
 #include "mls_device.cuh"
@@ -132,7 +132,7 @@ __device__ __forceinline__ void store_remote(uint32_t cluster_addr, float a, flo
 // (cp.async: a lane waits for and reads its own copies only, so no barrier is needed):
 // with a row ahead in registers alone, 32 KB were in flight on an SM, and 65536 x
 // 4096 bf16 values took 372 us.
-// C = 2: the widest fp32 rows are split over a cluster of two CTAs, half the columns each, which
+// C = 2: the widest rows are split over a cluster of two CTAs, half the columns each, which
 // exchange their sums of each row through shared memory.
 template <typename E, int V, int W, int S, int L, int C>
 __global__ void __launch_bounds__(32 * kBwdWarps, 1) norm_bwd_kernel(const NormParams p) {
@@ -478,16 +478,28 @@ template <typename E>
 cudaError_t fwd_any(const NormParams& p, cudaStream_t s) {
   if (p.d <= 8 * Vec<E>::N) return fwd<E, 1, 1, 8>(p, s);
   if (p.d <= 16 * Vec<E>::N) return fwd<E, 1, 1, 16>(p, s);
+  // As few vectors a lane as the row needs, in as few warps as hold them: registers bound
+  // the rows in flight, and a row's second warp costs two barriers.  16384 bf16 rows of 1032
+  // values: 5 vectors in 1 warp 15 us, 8 in 1 18, 2 in 4 20, 3 in 2 26; of 2056: 3 in 4 28, 4
+  // in 4 31; of 4104: 5 in 4 45, 4 in 8 67; of 8200: 5 in 8 105, 4 in 16 155; of 12288: 6 in
+  // 8 126, 8 in 8 164.  32768 of 2048: 8 in 1 and 2 in 4 45, 4 in 2 60.
   const int v = (p.d + 32 * Vec<E>::N - 1) / (32 * Vec<E>::N);  // vectors a lane of one warp
   if (v <= 1) return fwd<E, 1, 1>(p, s);
   if (v <= 2) return fwd<E, 2, 1>(p, s);
+  if (v <= 3) return fwd<E, 3, 1>(p, s);
   if (v <= 4) return fwd<E, 4, 1>(p, s);
-  // eight rows' vectors in one block: two warps a row (4 vectors each) took 59 us for
-  // 32768 x 2048 bf16 values, four 44
+  if (v <= 5) return fwd<E, 5, 1>(p, s);
+  if (v <= 6) return fwd<E, 6, 1>(p, s);
   if (v <= 8) return fwd<E, 2, 4>(p, s);
+  if (v <= 12) return fwd<E, 3, 4>(p, s);
   if (v <= 16) return fwd<E, 4, 4>(p, s);
-  if (v <= 32) return fwd<E, 4, 8>(p, s);
-  if (v <= 64) return fwd<E, 4, 16>(p, s);
+  if (v <= 20) return fwd<E, 5, 4>(p, s);
+  if (v <= 24) return fwd<E, 6, 4>(p, s);
+  if (v <= 32) return fwd<E, 8, 4>(p, s);
+  if (v <= 40) return fwd<E, 5, 8>(p, s);
+  if (v <= 48) return fwd<E, 6, 8>(p, s);
+  if (v <= 64) return fwd<E, 8, 8>(p, s);
+  if (v <= 96) return fwd<E, 6, 16>(p, s);
   if (v <= 128) return fwd<E, 8, 16>(p, s);
   norm_fwd_wide_kernel<E><<<blocks_of(p.T, kWarps), 32 * kWarps, 0, s>>>(p);
   return cudaGetLastError();
@@ -495,7 +507,7 @@ cudaError_t fwd_any(const NormParams& p, cudaStream_t s) {
 
 // Rows of a lane's vectors in the ring: as many as 160 KB hold, at most 8.
 template <int V>
-constexpr int kRows = V >= 4 ? 3 : V == 2 ? 5 : 8;
+constexpr int kRows = V >= 4 ? 3 : V == 3 ? 4 : V == 2 ? 5 : 8;
 template <int V>
 constexpr size_t kRingBytes = sizeof(uint4) * 2 * V * 32 * kBwdWarps * kRows<V>;
 
@@ -523,26 +535,33 @@ cudaError_t bwd(const NormParams& p, cudaStream_t s) {
   }
 }
 
-// Widest rows of the cached backward: 16 warps of 4 vectors a lane, for fp32 in two CTAs.
-constexpr int kBwdWidest = 16384;
-bool bwd_cached(int d) { return d <= kBwdWidest; }
+// The cached backward's rows: at most 16 warps of 4 vectors a lane in each of two CTAs.
+int lane_vectors(int d, bool fp32) { return (d + 32 * (fp32 ? 4 : 8) - 1) / (32 * (fp32 ? 4 : 8)); }
+bool bwd_cached(int d, bool fp32) { return lane_vectors(d, fp32) <= 2 * 64; }
 
 template <typename E>
 cudaError_t bwd_any(const NormParams& p, cudaStream_t s) {
   if (p.d <= 8 * Vec<E>::N) return bwd<E, 1, 1, 8>(p, s);
   if (p.d <= 16 * Vec<E>::N) return bwd<E, 1, 1, 16>(p, s);
-  const int v = (p.d + 32 * Vec<E>::N - 1) / (32 * Vec<E>::N);
+  // 2 or 3 vectors a lane: 16384 bf16 rows of 2056 values 54 -> 47 us against 2 in twice the
+  // warps, of 6000 118 -> 98, of 12288 282 (4 in 16 warps) -> 186; but one warp with 3 takes
+  // 26 us for 768, two with 2 take 22.
+  const int v = lane_vectors(p.d, Vec<E>::N == 4);
   if (v <= 1) return bwd<E, 1, 1>(p, s);
   if (v <= 2) return bwd<E, 2, 1>(p, s);
   if (v <= 4) return bwd<E, 2, 2>(p, s);
+  if (v <= 6) return bwd<E, 3, 2>(p, s);
   if (v <= 8) return bwd<E, 2, 4>(p, s);
+  if (v <= 12) return bwd<E, 3, 4>(p, s);
   if (v <= 16) return bwd<E, 2, 8>(p, s);
+  if (v <= 24) return bwd<E, 3, 8>(p, s);
   if (v <= 32) return bwd<E, 2, 16>(p, s);
-  // bf16 values end here: split over two CTAs too, 16384 x 16384 took 426 us, a row's
-  // exchange through the cluster being 0.6 of the 2 us that the row takes
+  if (v <= 48) return bwd<E, 3, 16>(p, s);
+  // bf16 rows of up to 16384 values split over two CTAs too: 16384 x 16384 took 426 us, a
+  // row's exchange through the cluster being 0.6 of the 2 us that the row takes
   if (v <= 64) return bwd<E, 4, 16>(p, s);
-  if constexpr (Vec<E>::N == 4) return bwd<E, 4, 16, 32, 2>(p, s);
-  return cudaErrorInvalidValue;  // not reached: bwd_cached
+  if (v <= 96) return bwd<E, 3, 16, 32, 2>(p, s);
+  return bwd<E, 4, 16, 32, 2>(p, s);
 }
 
 }  // namespace
@@ -550,12 +569,12 @@ cudaError_t bwd_any(const NormParams& p, cudaStream_t s) {
 // Shares of the column sums: the cached backward's blocks (clusters, where rows are split),
 // as many as its groups of warps need for one row each and at most what the SMs hold.
 int norm_splits(long long T, int d, bool fp32, int sms) {
-  if (bwd_cached(d)) {
-    const int n = fp32 ? 4 : 8, v = (d + 32 * n - 1) / (32 * n);
+  if (bwd_cached(d, fp32)) {
+    const int n = fp32 ? 4 : 8, v = lane_vectors(d, fp32);
     const int rows = d <= 8 * n ? 4 * kBwdWarps : d <= 16 * n ? 2 * kBwdWarps  // of a block at a time
-                     : kBwdWarps / (v <= 2 ? 1 : v <= 4 ? 2 : v <= 8 ? 4 : v <= 16 ? 8 : 16);
+                     : kBwdWarps / (v <= 2 ? 1 : v <= 6 ? 2 : v <= 12 ? 4 : v <= 24 ? 8 : 16);
     const long long blocks = (T + rows - 1) / rows;
-    const int most = d > 64 * 32 * n ? (sms + 1) / 2 : sms;
+    const int most = v > 64 ? (sms + 1) / 2 : sms;
     return blocks < 1 ? 1 : blocks < most ? static_cast<int>(blocks) : most;
   }
   const long long cols = (d + kColThreads - 1) / kColThreads;
@@ -573,7 +592,7 @@ cudaError_t launch_norm_bwd(const NormParams& p, bool fp32, cudaStream_t s) {
   if (p.T <= 0) return cudaSuccess;
   const bool sums = p.dgain || p.dbias;
   cudaError_t e;
-  if (bwd_cached(p.d)) {
+  if (bwd_cached(p.d, fp32)) {
     e = fp32 ? bwd_any<float>(p, s) : bwd_any<__nv_bfloat16>(p, s);
     if (e != cudaSuccess || !sums) return e;
   } else if (sums) {  // before dx, which may take dy's place
@@ -586,7 +605,7 @@ cudaError_t launch_norm_bwd(const NormParams& p, bool fp32, cudaStream_t s) {
   }
   if (sums && (e = launch_chained(norm_cols_sum_kernel, dim3(blocks_of(2 * p.d, 128)), dim3(32 * kColWarps), 0, s, p)) != cudaSuccess)
     return e;
-  if (bwd_cached(p.d)) return cudaSuccess;
+  if (bwd_cached(p.d, fp32)) return cudaSuccess;
   const unsigned grid = blocks_of(p.T, kWarps);
   if (fp32)
     norm_bwd_wide_kernel<float><<<grid, 32 * kWarps, 0, s>>>(p);
@@ -602,17 +621,22 @@ cudaError_t setup_norm_kernels() {
   e = cudaFuncSetAttribute(K, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(BYTES)); \
   if (e != cudaSuccess) return e;
 #define MLS_SET_RING(E, V, W, L, C) MLS_SET((norm_bwd_kernel<E, V, W, kRows<V>, L, C>), kRingBytes<V>)
-#define MLS_SET_BOTH(V, W, L) MLS_SET_RING(float, V, W, L, 1) MLS_SET_RING(__nv_bfloat16, V, W, L, 1)
-  MLS_SET_BOTH(1, 1, 8)
-  MLS_SET_BOTH(1, 1, 16)
-  MLS_SET_BOTH(1, 1, 32)
-  MLS_SET_BOTH(2, 1, 32)
-  MLS_SET_BOTH(2, 2, 32)
-  MLS_SET_BOTH(2, 4, 32)
-  MLS_SET_BOTH(2, 8, 32)
-  MLS_SET_BOTH(2, 16, 32)
-  MLS_SET_BOTH(4, 16, 32)
-  MLS_SET_RING(float, 4, 16, 32, 2)
+#define MLS_SET_BOTH(V, W, L, C) MLS_SET_RING(float, V, W, L, C) MLS_SET_RING(__nv_bfloat16, V, W, L, C)
+  MLS_SET_BOTH(1, 1, 8, 1)
+  MLS_SET_BOTH(1, 1, 16, 1)
+  MLS_SET_BOTH(1, 1, 32, 1)
+  MLS_SET_BOTH(2, 1, 32, 1)
+  MLS_SET_BOTH(2, 2, 32, 1)
+  MLS_SET_BOTH(3, 2, 32, 1)
+  MLS_SET_BOTH(2, 4, 32, 1)
+  MLS_SET_BOTH(3, 4, 32, 1)
+  MLS_SET_BOTH(2, 8, 32, 1)
+  MLS_SET_BOTH(3, 8, 32, 1)
+  MLS_SET_BOTH(2, 16, 32, 1)
+  MLS_SET_BOTH(3, 16, 32, 1)
+  MLS_SET_BOTH(4, 16, 32, 1)
+  MLS_SET_BOTH(3, 16, 32, 2)
+  MLS_SET_BOTH(4, 16, 32, 2)
 #undef MLS_SET_BOTH
 #undef MLS_SET_RING
 #undef MLS_SET

@@ -87,6 +87,15 @@ def test_against_the_definition(T, d, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d", [384, 392, 640, 648, 768, 776, 1280, 1288, 1536, 1544, 2560, 2568, 4096, 5120, 5128, 6144, 6152, 10240, 10248,
+                               12288, 16400, 24576, 24584, 32768, 32776])
+def test_either_side_of_each_split(d, dtype):
+    """The last width of each number of warps and vectors a lane, and the first of the next."""
+    check(*inputs(11, d, dtype, True, True, seed=d))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("gain,bias", [(False, False), (True, False), (False, True)])
 def test_optional_parameters(gain, bias):
     x, g, b, dy = inputs(77, 392, torch.bfloat16, gain, bias)
