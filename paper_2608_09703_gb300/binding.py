@@ -476,6 +476,10 @@ def mls_policy_loss(prob: PolicyProblem, logp, old_logp, ref_logp, adv, targets,
     _check(rc, "mls_policy_loss")
 
 
+def _places(grads):
+    return list(map(torch.Tensor.data_ptr, grads)), list(map(torch.Tensor.numel, grads))
+
+
 class _ClipTable:
     """The host arrays that describe a list of tensors to mls_grad_clip."""
 
@@ -484,8 +488,9 @@ class _ClipTable:
         for i, g in enumerate(grads):
             dev = _expect(f"grads[{i}]", g, g.dtype, g.shape, -2 if self.device is None else self.device)
             self.device = dev
-        self.g = (ctypes.c_void_p * self.n)(*[g.data_ptr() for g in grads])
-        self.numel = (ctypes.c_int64 * self.n)(*[g.numel() for g in grads])
+        self.places = _places(grads)
+        self.g = (ctypes.c_void_p * self.n)(*self.places[0])
+        self.numel = (ctypes.c_int64 * self.n)(*self.places[1])
         self.dtype = (ctypes.c_int32 * self.n)(*[_dtype_code(g) for g in grads])
 
 
@@ -758,9 +763,10 @@ class PolicyLoss:
 
 
 class GradClip:
-    """Global norm of a fixed list of gradient buffers (bf16 or fp32, as HeadLoss
+    """Global norm of a fixed list of gradient tensors (bf16 or fp32, as HeadLoss
     and the others keep them from step to step) and clipping in place.  Returns
-    fp32 [2]: the norm and the factor applied."""
+    fp32 [2]: the norm and the factor applied.  A tensor given other memory since
+    (`t.data = ...`) is followed."""
 
     def __init__(self, grads: Sequence[torch.Tensor]):
         self.grads = list(grads)  # keeps the buffers alive
@@ -773,7 +779,11 @@ class GradClip:
         self.home = _Home(self.ws)
 
     def __call__(self, max_norm, stream=None):
-        self.home()
+        dev = self.home()
+        if _places(self.grads) != self.table.places:
+            self.table = _ClipTable(self.grads)
+            if self.table.device != dev:
+                raise ValueError("grads: not with the object's buffers")
         t, ws = self.table, self.ws
         rc = lib().mls_grad_clip(t.n, t.g, t.numel, t.dtype, max_norm, self.stats.data_ptr(), ws.data_ptr(),
                                  ws.numel(), _stream(stream))

@@ -201,3 +201,23 @@ def test_refusals_of_the_binding_on_the_gpu():
     assert bool((g[0] == 1).all())
     with pytest.raises(mls.MLSError):
         mls.GradClip(g)(0.0)
+
+
+@pytest.mark.gpu
+def test_tensors_given_other_memory():
+    """An object's list follows its tensors, not the memory they had when it was made."""
+    g = tensors([5000, 70], seed=9)
+    op = mls.GradClip(g)
+    op(1.0)
+    old = g[0].data
+    keep = old.clone()
+    g[0].data = torch.full((600,), 3.0, dtype=g[0].dtype, device="cuda")
+    g[1].data = g[1].data[:9]
+    g[1].fill_(2.0)
+    norm, coef = op(1.0).tolist()
+    want = math.sqrt(600 * 9.0 + 9 * 4.0)
+    assert abs(norm - want) <= 8 * U * want and abs(coef - 1 / (want + 1e-6)) <= 10 * U * coef
+    assert torch.equal(old, keep)  # the memory left behind
+    g[1].data = torch.zeros(4, 4, dtype=g[1].dtype, device="cuda").t()[:2]
+    with pytest.raises(ValueError):
+        op(1.0)
