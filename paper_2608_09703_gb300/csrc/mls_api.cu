@@ -1458,6 +1458,7 @@ extern "C" int mls_policy_loss(const mls_policy_problem* p, const float* logp, c
   pp.chunk_count = static_cast<int*>(ws);
   pp.part = reinterpret_cast<float*>(static_cast<char*>(ws) + pl.off_part);
   pp.status = dev->status;
+  pp.sms = dev->sms;
   return timed("policy", s, [&] { return launch_policy(pp, s); });
 }
 

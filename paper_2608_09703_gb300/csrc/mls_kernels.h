@@ -476,7 +476,7 @@ cudaError_t launch_norm_bwd(const NormParams& p, bool fp32, cudaStream_t s);
 
 // ------------------------------------------------------------------ clipped policy loss
 constexpr int kPolicyTokens = 1024;  // tokens per block
-constexpr int kPolicyOne = 4096;     // at most so many take one block, and one launch
+constexpr int kPolicyOne = 4096;     // at most so many take one block a sub-model, and one launch
 constexpr int kPolicyDirect = 16384; // at most so many are counted by each block itself
 enum PolicyAgg { kAggToken = 0, kAggSeq = 1, kAggSum = 2 };
 struct PolicyParams {
@@ -498,6 +498,7 @@ struct PolicyParams {
   long long count_tokens;
   float* part;                   // [M][3][blocks]
   int* status;
+  int sms;
 };
 inline int policy_blocks(long long T) { return static_cast<int>((T + kPolicyTokens - 1) / kPolicyTokens); }
 cudaError_t launch_policy(const PolicyParams& p, cudaStream_t s);

@@ -124,10 +124,6 @@ __device__ __forceinline__ void copy_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
-__device__ __forceinline__ void store_remote(uint32_t cluster_addr, float a, float b) {
-  asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(cluster_addr), "f"(a), "f"(b) : "memory");
-}
-
 // S rows of every lane's own vectors in shared memory, S - 1 of them being copied there
 // (cp.async: a lane waits for and reads its own copies only, so no barrier is needed):
 // with a row ahead in registers alone, 32 KB were in flight on an SM, and 65536 x

@@ -156,6 +156,11 @@ __device__ __forceinline__ Pair warp_sum_pair(Pair a) {  // valid in lane 0
     pair_add(a, __shfl_down_sync(0xffffffffu, a.hi, o), __shfl_down_sync(0xffffffffu, a.lo, o));
   return a;
 }
+__device__ __forceinline__ Pair pair_scaled(const Pair& a, float c) {
+  const float hi = a.hi * c;
+  return {hi, isfinite(hi) ? fmaf(a.hi, c, -hi) + a.lo * c : 0.f};
+}
+__device__ __forceinline__ float pair_float(const Pair& a) { return isfinite(a.hi) ? a.hi + a.lo : a.hi; }
 __device__ __forceinline__ double pair_value(const Pair& a) {
   return isfinite(a.hi) ? static_cast<double>(a.hi) + static_cast<double>(a.lo) : static_cast<double>(a.hi);
 }

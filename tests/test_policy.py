@@ -394,3 +394,26 @@ def test_refusals_of_the_binding():
             op(a["logp"], a["old"], a["adv"], a["y"], ref_logp=a["ref"], seq_start=a["start"])
     with pytest.raises(mls.MLSError):
         mls.mls_policy_loss(op.prob, logp, old, None, adv, y, start, 1.0, op.loss, None, None, None, op.ws[:8])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,M", [(1, 4), (1024, 2), (3000, 3), (4096, 4), (4097, 4), (200001, 3), (320000, 2)])
+def test_models_together_alone_and_in_place(T, M):
+    """Every sub-model as by itself, whatever the launch makes of M; dlogp in logp's place; outputs left out."""
+    c = config(T, B=3, agg="seq", beta=0.07, M=M, adv_per_seq=True)
+    logp, old, ref, adv, y, start = inputs(c, seed=T + M)
+    op = run(c, logp, old, ref, adv, y, start)
+    total, size = 0.0, 0.0
+    for m in range(M):
+        one = run(dict(c, M=1), logp[m:m + 1], old[m:m + 1], ref[m:m + 1], adv, y, start)
+        assert torch.equal(one.tok_loss[0], op.tok_loss[m]) and torch.equal(one.dlogp[0], op.dlogp[m])
+        assert torch.equal(one.diag[:, 0], op.diag[:, m])
+        total, size = total + one.loss.item(), size + abs(one.loss.item())
+    assert abs(op.loss.item() - total) <= 4 * U * size
+    prob = B.PolicyProblem(**c)
+    same, loss = logp.clone(), torch.empty(1, device="cuda")
+    B.mls_policy_loss(prob, same, old, ref, adv, y, start, 1.0, loss, None, None, same, op.ws)
+    assert torch.equal(same, op.dlogp) and torch.equal(loss, op.loss)
+    tok = torch.empty_like(logp)
+    B.mls_policy_loss(prob, logp, old, ref, adv, y, start, 1.0, loss, tok, None, None, op.ws)
+    assert torch.equal(tok, op.tok_loss) and torch.equal(loss, op.loss)
