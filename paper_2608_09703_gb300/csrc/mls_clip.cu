@@ -105,6 +105,7 @@ __global__ void __launch_bounds__(kThreads, kClipNormBlocks) clip_norm_kernel(co
   chain_trigger();
   __shared__ Pair sh[kThreads / 32];
   __shared__ double shr[kThreads / 32];
+  __shared__ bool has[kThreads / 32];
   Squares acc = {};
   for (int c = blockIdx.x; c < p.chunks; c += gridDim.x) {
     const ClipTensor& t = p.t[tensor_of(p, c)];
@@ -114,20 +115,27 @@ __global__ void __launch_bounds__(kThreads, kClipNormBlocks) clip_norm_kernel(co
       chunk_squares(static_cast<const __nv_bfloat16*>(t.g), t, c - t.chunk0, acc);
   }
   const Pair s = warp_sum_pair(acc.plain);
-  double r = 0.0;  // what the other two hold, rarely anything
-  if (acc.tiny.hi != 0.f || acc.huge.hi != 0.f)  // also where one is NaN
-    r = pair_value(acc.tiny) * 0x1p-180 + pair_value(acc.huge) * 0x1p160;
-  if (__any_sync(0xffffffffu, r != 0.0))
+  // what the other two hold, rarely anything; also where one is NaN
+  const bool some = acc.tiny.hi != 0.f || acc.huge.hi != 0.f;
+  const bool warp_has = __any_sync(0xffffffffu, some);
+  double r = 0.0;
+  if (warp_has) {
+    if (some) r = pair_value(acc.tiny) * 0x1p-180 + pair_value(acc.huge) * 0x1p160;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) r += __shfl_down_sync(0xffffffffu, r, o);
+  }
   if ((threadIdx.x & 31) == 0) {
     sh[threadIdx.x >> 5] = s;
     shr[threadIdx.x >> 5] = r;
+    has[threadIdx.x >> 5] = warp_has;
   }
   __syncthreads();
   if (threadIdx.x == 0) {
-    double total = 0.0;
-    for (int i = 0; i < kThreads / 32; ++i) total += pair_value(sh[i]) + shr[i];
+    Pair a = sh[0];
+    for (int i = 1; i < kThreads / 32; ++i) pair_add(a, sh[i].hi, sh[i].lo);
+    double total = pair_value(a);
+    for (int i = 0; i < kThreads / 32; ++i)
+      if (has[i]) total += shr[i];
     p.part[p.part0 + blockIdx.x] = total;
   }
 }
@@ -161,6 +169,25 @@ __device__ __forceinline__ void chunk_scale(E* g, const ClipTensor& t, int local
     g[threadIdx.x] = static_cast<E>(static_cast<float>(g[threadIdx.x]) * coef);
 }
 
+// The norm of a sum of squares a and the factor for it.  The root and the quotient are
+// fp32's, of a times a power of 4 in [1, 4): in 64 bits they took half a microsecond.
+__device__ __forceinline__ float norm_of(double a, float max_norm, float& coef) {
+  const int e = ((__double2hiint(a) >> 20) & 0x7ff) - 1023;
+  if (e == 1024 || a == 0.0) {
+    // NaN stays (every gradient becomes NaN); an infinite norm gives 0, as the formula says
+    const float n = static_cast<float>(a);
+    coef = isinf(max_norm) ? 1.f : a == 0.0 ? fminf(1.f, max_norm / 1e-6f) : isinf(n) ? 0.f : n;
+    return n;
+  }
+  const int h = e >> 1;  // a = m 4^h
+  const float m = static_cast<float>(__hiloint2double(__double2hiint(a) - 2 * h * (1 << 20), __double2loint(a)));
+  const float root = sqrtf(m), norm = ldexpf(root, h);
+  // a norm past fp32's largest value still has its factor
+  const float ratio = h > 64 ? ldexpf(max_norm / root, -h) : max_norm / (norm + 1e-6f);
+  coef = isinf(max_norm) || ratio >= 1.f ? 1.f : ratio;
+  return norm;
+}
+
 // Every block adds all shares of the norm itself, in the same order: its first warp,
 // since 64-bit additions of all warps would only queue for the SM's two units.
 template <int kCap>
@@ -175,12 +202,11 @@ __global__ void __launch_bounds__(kThreads, kClipScaleBlocks) clip_scale_kernel(
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) a += __shfl_down_sync(0xffffffffu, a, o);
     if (threadIdx.x == 0) {
-      const double norm = sqrt(a), ratio = static_cast<double>(p.max_norm) / (norm + 1e-6);
-      // NaN stays (every gradient becomes NaN); an infinite norm gives 0, as the formula says
-      const float c = isinf(p.max_norm) || ratio >= 1.0 ? 1.f : static_cast<float>(ratio);
+      float c;
+      const float norm = norm_of(a, p.max_norm, c);
       sh_coef = c;
       if (p.stats && blockIdx.x == 0) {
-        p.stats[0] = static_cast<float>(norm);
+        p.stats[0] = norm;
         p.stats[1] = c;
       }
     }
