@@ -1367,8 +1367,7 @@ int policy_validate(const mls_policy_problem* p) {
 }
 
 struct PolicyPlan {
-  int chunks = 0;
-  long long count_tokens = 0;
+  int chunks = 0, count_shift = 0;
   size_t off_part = 0, total = 0;
 };
 // Counts per chunk of tokens: few enough for a block to add all.  The mean over
@@ -1377,8 +1376,8 @@ struct PolicyPlan {
 PolicyPlan policy_plan(const mls_policy_problem* p) {
   PolicyPlan pl;
   const long long blocks = policy_blocks(p->T), most = p->agg == MLS_AGG_SEQ_MEAN ? 4096 : 512;
-  pl.count_tokens = kPolicyTokens * ceil_div(p->T, kPolicyTokens * most);
-  if (p->T > kPolicyDirect && p->agg != MLS_AGG_SUM) pl.chunks = static_cast<int>(ceil_div(p->T, pl.count_tokens));
+  while (ceil_div(p->T, 1ll << pl.count_shift) > most || (kPolicyTokens >> pl.count_shift) > 1) ++pl.count_shift;
+  if (p->T > kPolicyDirect && p->agg != MLS_AGG_SUM) pl.chunks = static_cast<int>(ceil_div(p->T, 1ll << pl.count_shift));
   pl.off_part = align_up(sizeof(int) * static_cast<size_t>(pl.chunks));
   pl.total = align_up(pl.off_part + sizeof(float) * 3 * p->M * static_cast<size_t>(blocks));
   return pl;
@@ -1454,7 +1453,7 @@ extern "C" int mls_policy_loss(const mls_policy_problem* p, const float* logp, c
   pp.diag = diag;
   pp.dlogp = dlogp;
   pp.chunks = pl.chunks;
-  pp.count_tokens = pl.count_tokens;
+  pp.count_shift = pl.count_shift;
   pp.chunk_count = static_cast<int*>(ws);
   pp.part = reinterpret_cast<float*>(static_cast<char*>(ws) + pl.off_part);
   pp.status = dev->status;

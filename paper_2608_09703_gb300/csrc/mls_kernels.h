@@ -493,9 +493,9 @@ struct PolicyParams {
   const int* seq_start;          // [B + 1] or null
   float *loss, *tok_loss, *diag, *dlogp;    // [1], [M][T], [3][M], [M][T]; all but loss may be null
   int* chunk_count;              // [chunks, up to a multiple of 4]: counted tokens of each
-                                 //   count_tokens tokens
+                                 //   2^count_shift tokens
   int chunks;                    // 0: no counts needed, or so few tokens that blocks count them
-  long long count_tokens;
+  int count_shift;
   float* part;                   // [M][3][blocks]
   int* status;
   int sms;

@@ -109,11 +109,12 @@ __device__ __forceinline__ int count_crossing(const PolicyParams& p, int b, long
   if ((lo >= t0 && hi <= t1) || lo >= hi) return 0;
   int n = 0;
   if (p.chunks > 0) {
-    const long long c0 = (lo + p.count_tokens - 1) / p.count_tokens, c1 = hi / p.count_tokens;
+    const int sh = p.count_shift;
+    const long long c0 = (lo + (1ll << sh) - 1) >> sh, c1 = hi >> sh;
     if (c0 < c1) {  // whole chunks, and the two ends
       for (long long c = c0 + threadIdx.x; c < c1; c += kThreads) n += p.chunk_count[c];
-      n += count_some(p, lo, c0 * p.count_tokens);
-      lo = c1 * p.count_tokens;
+      n += count_some(p, lo, c0 << sh);
+      lo = c1 << sh;
     }
   }
   return n + count_some(p, lo, hi);
@@ -123,8 +124,8 @@ __device__ __forceinline__ int count_crossing(const PolicyParams& p, int b, long
 __global__ void __launch_bounds__(kThreads) policy_count_kernel(const __grid_constant__ PolicyParams p) {
   __shared__ int sh[kThreads / 32];
   chain_trigger();
-  const long long t0 = static_cast<long long>(blockIdx.x) * p.count_tokens;
-  const long long t1 = t0 + p.count_tokens < p.T ? t0 + p.count_tokens : p.T;
+  const long long t0 = static_cast<long long>(blockIdx.x) << p.count_shift, next = t0 + (1ll << p.count_shift);
+  const long long t1 = next < p.T ? next : p.T;
   // tokens outside every sequence do not count
   const long long lo = p.seq_start ? seq_at(p, 0) : 0, hi = p.seq_start ? seq_at(p, p.B) : p.T;
   int n = 0;
