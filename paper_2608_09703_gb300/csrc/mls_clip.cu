@@ -3,7 +3,7 @@
 // A call's tensors come as a table in the kernels' parameters (kClipTable of them
 // a launch), cut into chunks of kClipChunk values that persistent blocks take in
 // turn.  Squares are summed in fp32 over the 32 values that a thread holds of a
-// chunk, in two fp32 words (Pair) over its chunks, and in 64 bits from there on.  Where
+// chunk, in two fp32 words (Pair) over a block, and in 64 bits from there on.  Where
 // such a sum leaves the range in which fp32 squares are exact to rounding (a square
 // that overflowed, or squares so small that some vanished) those 32 values are taken
 // times a power of two, into sums of their own (Blue's method), so the norm is right

@@ -506,7 +506,21 @@ __global__ void __launch_bounds__(kOne ? kOneThreads : kThreads, kOne ? 1 : kRes
 // Block shares -> diag and the loss.  Each of the 3 M quantities has 32 / (3 M) warps;
 // a lane adds its shares in two fp32 words (Pair): 64-bit additions by every thread
 // took 25 us a sub-model, whatever the number of blocks.
-constexpr int kFinalThreads = 1024, kFinalBatch = 16;
+constexpr int kFinalThreads = 1024, kFinalBatch = 16, kFinalFew = 2;
+
+// Shares first, first + step, ... of `blocks`: kBatch loads at once, one latency for all.  An
+// addition costs 30 cycles, of zeros behind the last share too (16 of them in place of 2 for
+// 131072 tokens: 0.5 us).
+template <int kBatch>
+__device__ __forceinline__ void add_shares(Pair& a, const float* part, int first, int step, int blocks) {
+  for (int i0 = first; i0 < blocks; i0 += kBatch * step) {
+    float v[kBatch];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) v[u] = i0 + u * step < blocks ? part[i0 + u * step] : 0.f;
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) pair_add(a, v[u], 0.f);
+  }
+}
 
 __global__ void __launch_bounds__(kFinalThreads) policy_final_kernel(const __grid_constant__ PolicyParams p, int blocks) {
   __shared__ Pair sh[kFinalThreads / 32];
@@ -517,16 +531,10 @@ __global__ void __launch_bounds__(kFinalThreads) policy_final_kernel(const __gri
   Pair a = {0.f, 0.f};
   if (k < per) {
     const float* part = p.part + static_cast<long long>(q) * blocks;
-    for (int i0 = k * 32 + lane; i0 < blocks; i0 += kFinalBatch * per * 32) {  // a batch's loads at once
-      float v[kFinalBatch];
-#pragma unroll
-      for (int u = 0; u < kFinalBatch; ++u) {
-        const int i = i0 + u * per * 32;
-        v[u] = i < blocks ? part[i] : 0.f;
-      }
-#pragma unroll
-      for (int u = 0; u < kFinalBatch; ++u) pair_add(a, v[u], 0.f);
-    }
+    if (blocks <= kFinalFew * per * 32)
+      add_shares<kFinalFew>(a, part, k * 32 + lane, per * 32, blocks);
+    else
+      add_shares<kFinalBatch>(a, part, k * 32 + lane, per * 32, blocks);
   }
   a = warp_sum_pair(a);
   if (lane == 0) sh[warp] = a;
