@@ -9,13 +9,12 @@
 // gradient and none, so the comparison is made on D itself, and where D is near the
 // bound with what rounding the subtraction lost (its exact value is D + e) and the
 // bound, log(1 + clip_high) or log(1 - clip_low), in two fp32 words: as exact as in 64
-// bits.  K of a small x
-// comes from its series, not from a difference of numbers near 1.
+// bits.  K of a small x comes from its series, not from a difference of numbers near 1.
 //
-// A block owns 1024 consecutive tokens: it finds each one's sequence,
-// computes the weights once and goes through the sub-models (or its one, see below).  How many tokens of
-// a sequence count is known inside the block where the whole sequence is; for the
-// (at most two) that cross the block's ends it comes from counts per chunk of
+// A block owns 1024 consecutive tokens: it finds each one's sequence, computes the
+// weights once and goes through the sub-models (or has one, see below).  How many
+// tokens of a sequence count is known inside the block where the whole sequence is;
+// for the (at most two) that cross the block's ends it comes from counts per chunk of
 // tokens that a kernel before this one made.  Counts are integers and sums are
 // added in a fixed order, so results do not depend on timing.
 #include <climits>
