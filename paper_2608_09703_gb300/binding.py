@@ -477,7 +477,10 @@ def mls_policy_loss(prob: PolicyProblem, logp, old_logp, ref_logp, adv, targets,
 
 
 def _places(grads):
-    return list(map(torch.Tensor.data_ptr, grads)), list(map(torch.Tensor.numel, grads))
+    """What tells whether a list's table still describes it: a tensor given other memory may keep
+    its address and count and be of another type, or no longer be dense."""
+    return (list(map(torch.Tensor.data_ptr, grads)), list(map(torch.Tensor.numel, grads)),
+            [g.dtype for g in grads], all(map(torch.Tensor.is_contiguous, grads)))
 
 
 class _ClipTable:
@@ -766,7 +769,8 @@ class GradClip:
     """Global norm of a fixed list of gradient tensors (bf16 or fp32, as HeadLoss
     and the others keep them from step to step) and clipping in place.  Returns
     fp32 [2]: the norm and the factor applied.  A tensor given other memory since
-    (`t.data = ...`) is followed."""
+    (`t.data = ...`) is followed, of another type or size too; what a new object would
+    refuse is refused."""
 
     def __init__(self, grads: Sequence[torch.Tensor]):
         self.grads = list(grads)  # keeps the buffers alive
@@ -779,11 +783,9 @@ class GradClip:
         self.home = _Home(self.ws)
 
     def __call__(self, max_norm, stream=None):
-        dev = self.home()
+        self.home()
         if _places(self.grads) != self.table.places:
-            self.table = _ClipTable(self.grads)
-            if self.table.device != dev:
-                raise ValueError("grads: not with the object's buffers")
+            self.table = _ClipTable(self.grads)  # refuses what it cannot describe
         t, ws = self.table, self.ws
         rc = lib().mls_grad_clip(t.n, t.g, t.numel, t.dtype, max_norm, self.stats.data_ptr(), ws.data_ptr(),
                                  ws.numel(), _stream(stream))
