@@ -316,12 +316,14 @@ int mls_layer_norm_bwd(int64_t T, int32_t d, int32_t in_dtype, const void* x, co
  * one exactly on a bound is not stopped.
  * Asynchronous; returns 0 or a negative MLS_ERR_* code (nothing launched).
  */
+#define MLS_POLICY_MAX_SEQS (1 << 30)
 enum { MLS_AGG_TOKEN_MEAN = 0, MLS_AGG_SEQ_MEAN = 1, MLS_AGG_SUM = 2 };
 typedef struct {
   int32_t M;            /* sub-models, 1..MLS_MAX_MODELS */
   int64_t T;            /* tokens, 0 .. 2^31 - 1 */
   int64_t V;            /* vocabulary, 1 .. 2^31 - 1 */
-  int32_t B;            /* sequences, >= 0; >= 1 for MLS_AGG_SEQ_MEAN or adv_per_seq when T > 0 */
+  int32_t B;            /* sequences, >= 0; >= 1 for MLS_AGG_SEQ_MEAN or adv_per_seq when T > 0; at
+                           most MLS_POLICY_MAX_SEQS (MLS_ERR_UNSUPPORTED beyond) */
   float clip_low;       /* >= 0; from 1 on the ratio has no lower bound */
   float clip_high;      /* >= 0; infinite: no upper bound */
   float beta;           /* weight of the KL term, >= 0 */

@@ -27,6 +27,7 @@ MLS_STATUS_BAD_TARGET, MLS_STATUS_TIMEOUT, MLS_STATUS_CHECK, MLS_STATUS_DRAIN = 
 MLS_STATUS_BAD_SEQ = 16
 MLS_AGG_TOKEN_MEAN, MLS_AGG_SEQ_MEAN, MLS_AGG_SUM = 0, 1, 2
 MLS_CLIP_MAX_TENSORS = 16384
+MLS_POLICY_MAX_SEQS = 1 << 30
 MLS_MAX_MODELS = 4
 
 

@@ -1354,8 +1354,9 @@ extern "C" int mls_layer_norm_bwd(int64_t T, int32_t d, int32_t in_dtype, const 
 namespace {
 int policy_validate(const mls_policy_problem* p) {
   if (!p || p->M < 1 || p->M > MLS_MAX_MODELS || p->T < 0 || p->T > INT_MAX || p->V < 1 || p->V > INT_MAX ||
-      p->B < 0 || p->B == INT_MAX)
+      p->B < 0)
     return MLS_ERR_ARG;
+  if (p->B > MLS_POLICY_MAX_SEQS) return MLS_ERR_UNSUPPORTED;  // the kernels count sequences in 32 bits, with room for a step
   if (p->agg != MLS_AGG_TOKEN_MEAN && p->agg != MLS_AGG_SEQ_MEAN && p->agg != MLS_AGG_SUM) return MLS_ERR_ARG;
   if (!(p->clip_low >= 0.f) || !(p->clip_high >= 0.f)) return MLS_ERR_ARG;
   if (!(p->beta >= 0.f) || !std::isfinite(p->beta)) return MLS_ERR_ARG;

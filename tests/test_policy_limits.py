@@ -1,0 +1,45 @@
+"""The number of sequences that a policy loss takes, refused by the host beyond."""
+import ctypes
+
+import pytest
+
+import paper_2608_09703_gb300 as mls
+from paper_2608_09703_gb300 import binding as B
+from paper_2608_09703_gb300 import build as mbuild
+
+
+@pytest.mark.parametrize("agg", ["token", "seq", "sum"])
+def test_more_sequences_than_32_bits_can_step_through(agg):
+    mbuild.build()
+    p = 0x1000
+
+    def call(n, size=1 << 40):
+        prob = mls.PolicyProblem(100, 1000, B=n, agg=agg)
+        return B.mls_policy_workspace_size(prob), B.lib().mls_policy_loss(
+            prob.ref(), p, p, p, p, p, p, 1.0, p, p, p, 0x2000, 0x10000, size, None)
+
+    for n in (B.MLS_POLICY_MAX_SEQS + 1, (1 << 31) - 256, (1 << 31) - 30, (1 << 31) - 2, (1 << 31) - 1):
+        assert call(n) == (0, B.MLS_ERR_UNSUPPORTED)
+    # the last one accepted gets as far as its pointers
+    prob = mls.PolicyProblem(100, 1000, B=B.MLS_POLICY_MAX_SEQS, agg=agg)
+    assert B.mls_policy_workspace_size(prob) > 0
+    assert B.lib().mls_policy_loss(prob.ref(), ctypes.c_void_p(p + 2), p, p, p, p, p, 1.0, p, p, p, 0x2000, 0x10000,
+                                   1 << 40, None) == B.MLS_ERR_ALIGN
+
+
+def step_32(lo, hi):
+    """The search's step over [lo, hi] as the kernel forms it, in wrapping 32 bits."""
+    v = (hi - lo + 31 + (1 << 31)) % (1 << 32) - (1 << 31)
+    return int(v / 32)
+
+
+def test_steps_stay_positive_up_to_the_limit():
+    assert step_32(0, (1 << 31) - 30) < 0  # what the limit keeps away
+    for n in (1, 2, 33, 1 << 20, B.MLS_POLICY_MAX_SEQS):
+        lo, hi = 0, n - 1
+        while lo < hi:  # the path that moves furthest up: every candidate starts at or before the token
+            step = step_32(lo, hi)
+            assert step > 0 and lo + 32 * step + step < 1 << 31
+            k = min(32, (hi - lo) // step)
+            lo, hi = lo + k * step, min(hi, lo + k * step + step - 1)
+        assert n + 1024 < 1 << 31  # the check of the offsets, a block's threads a step
