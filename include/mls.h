@@ -234,7 +234,8 @@ int mls_spec_verify(const mls_spec_problem* p, const void* H_draft, const void* 
  * in_dtype is MLS_BF16 (MLS_ERR_UNSUPPORTED otherwise: products of fp32 storage would
  * go through tf32, whose errors a ratio exp(logp - old_logp) turns into gradients).
  * H and W are finite: an infinity or NaN in a row of H, of a token left out too, would
- * reach dW (0 times it is NaN).
+ * reach dW (0 times it is NaN).  Logits that overflow make that token's outputs infinite or
+ * NaN; of one left out, or whose dlogp is 0, they reach no gradient.
  *   targets    device, int32 [T]; outside [0, V): logp 0, no gradient (>= V also
  *              raises MLS_STATUS_BAD_TARGET), and its dlogp is not used
  *   logp, lse  device, fp32 [M, T]; the backward needs lse

@@ -801,6 +801,11 @@ __device__ __forceinline__ void logp_grad_tile(const float (&v)[128], int nvalid
       for (int i = 0; i < 32; ++i)
         if (i == r) g[i] -= c;
     }
+    // A token without a gradient: nothing, also where its logits overflowed (0 times a NaN).
+    if (c == 0.f) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) g[i] = 0.f;
+    }
     put_chunk<false>(o, gcol, ch, g, lane);
   }
 }
@@ -825,8 +830,6 @@ __device__ __forceinline__ void logp_bwd_epilogue(const HeadParams& p, uint32_t 
     const long long i = static_cast<long long>(j) * p.T + row;
     c[j] = on ? p.neg_inv_tau * p.dlogp[i] : 0.f;
     b[j] = j < p.M && row_ok ? -__ldg(p.stats + i) * p.L1 : 0.f;
-    // A token without a gradient adds nothing, whatever its logits: 2^-inf = 0.
-    if (c[j] == 0.f) b[j] = -INFINITY;
   }
   uint32_t acc = 0, acc_par = 0;
   bool aborted = false;
