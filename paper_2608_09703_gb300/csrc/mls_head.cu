@@ -673,9 +673,13 @@ __device__ __forceinline__ void logp_release(uint32_t base, uint32_t& acc, uint3
 // before they compute: 32 columns at a time, read as they were needed, a tile took 6360
 // cycles of which the MMAs of d = 512 filled 4096.
 
-// One sub-model's tile: running maximum m of z, s = sum of 2^((z - m) Lt).
+// One sub-model's tile: running maximum m of z, s = sum of 2^((z - m) Lt).  The maximum is
+// taken off before the product, so that its own term is 1 exactly and a token with nearly all
+// of the mass is left with what the others add to that; z Lt - (m Lt rounded) gave all terms a
+// factor of up to 2^(m Lt 2^-24), 1e-6 of log-probabilities of 1e-7.  The tiles' sums go into two
+// words for the same reason.
 template <bool kMasked>
-__device__ __forceinline__ void logp_tile(float (&v)[128], int nvalid, int yl, float Lt, float& m, float& s,
+__device__ __forceinline__ void logp_tile(float (&v)[128], int nvalid, int yl, float Lt, float& m, Pair& s,
                                           float& zy) {
   if (kMasked) {
 #pragma unroll
@@ -692,18 +696,20 @@ __device__ __forceinline__ void logp_tile(float (&v)[128], int nvalid, int yl, f
 #pragma unroll
     for (int i = 0; i < w; ++i) mx[i] = fmaxf(mx[i], mx[i + w]);
   if (mx[0] > m) {
-    s *= fast_exp2((m - mx[0]) * Lt);
+    const float scale = fast_exp2((m - mx[0]) * Lt);
+    s.hi *= scale;
+    s.lo *= scale;
     m = mx[0];
   }
-  const F2 L2 = f2(Lt), b2 = f2(-m * Lt);
+  const F2 L2 = f2(Lt), nm = f2(-m);
   F2 acc[4] = {0, 0, 0, 0};
 #pragma unroll
   for (int i = 0; i < 64; ++i) {
     float lo, hi;
-    f2_split(f2_fma(f2(v[2 * i], v[2 * i + 1]), L2, b2), lo, hi);
+    f2_split(f2_mul(f2_add(f2(v[2 * i], v[2 * i + 1]), nm), L2), lo, hi);
     acc[i & 3] = f2_add(acc[i & 3], f2(fast_exp2(lo), fast_exp2(hi)));
   }
-  s += f2_sum(f2_add(f2_add(acc[0], acc[1]), f2_add(acc[2], acc[3])));
+  pair_add(s, f2_sum(f2_add(f2_add(acc[0], acc[1]), f2_add(acc[2], acc[3]))), 0.f);
   if (static_cast<unsigned>(yl) < 128u) {
 #pragma unroll
     for (int i = 0; i < 128; ++i)
@@ -719,11 +725,13 @@ __device__ __forceinline__ void logp_fwd_epilogue(const HeadParams& p, uint32_t 
   const bool row_ok = row < p.T;
   const int y = row_ok ? __ldg(p.y + row) : -1;
   const uint32_t tl = tmem + (static_cast<uint32_t>(quad * 32) << 16) + static_cast<uint32_t>(half * 128);
-  float m[kMaxModels], s[kMaxModels], zy[kMaxModels];
+  float m[kMaxModels], zy[kMaxModels];
+  Pair s[kMaxModels];
 #pragma unroll
   for (int j = 0; j < kMaxModels; ++j) {
     m[j] = -INFINITY;
-    s[j] = zy[j] = 0.f;
+    s[j] = {0.f, 0.f};
+    zy[j] = 0.f;
   }
   uint32_t acc = 0, acc_par = 0;
   bool aborted = false;
@@ -755,7 +763,8 @@ __device__ __forceinline__ void logp_fwd_epilogue(const HeadParams& p, uint32_t 
 #pragma unroll
     for (int j = 0; j < kMaxModels; ++j) {
       X(kLogpMax, j) = m[j];
-      X(kLogpSum, j) = s[j];
+      X(kLogpSum, j) = s[j].hi;
+      X(kLogpSumLow, j) = s[j].lo;
       X(kLogpTarget, j) = zy[j];
     }
   }
@@ -769,8 +778,12 @@ __device__ __forceinline__ void logp_fwd_epilogue(const HeadParams& p, uint32_t 
     if (j < p.M) {
       const float m1 = X(kLogpMax, j), mm = fmaxf(m[j], m1);
       float* Pj = P + static_cast<long long>(j) * p.T;
+      const float own = scale_from(m[j], mm, p.Ltau), other = scale_from(m1, mm, p.Ltau);
+      Pair sum = {s[j].hi * own, s[j].lo * own};
+      pair_add(sum, X(kLogpSum, j) * other, X(kLogpSumLow, j) * other);
       Pj[kLogpMax * MT] = mm;
-      Pj[kLogpSum * MT] = s[j] * scale_from(m[j], mm, p.Ltau) + X(kLogpSum, j) * scale_from(m1, mm, p.Ltau);
+      Pj[kLogpSum * MT] = sum.hi;
+      Pj[kLogpSumLow * MT] = sum.lo;
       Pj[kLogpTarget * MT] = zy[j] + X(kLogpTarget, j);
     }
   }

@@ -144,7 +144,7 @@ struct HeadParams {
   const float* dlogp;            // [M][T]
   float neg_inv_tau;             // -1 / tau
 };
-enum LogpField { kLogpMax = 0, kLogpSum, kLogpTarget, kLogpFields };
+enum LogpField { kLogpMax = 0, kLogpSum, kLogpSumLow, kLogpTarget, kLogpFields };  // the sum in two words
 
 // ------------------------------------------------------------------ GEMM kernels
 // CTA pairs: a pair owns a 256 x kGemmBN output tile; each CTA of the pair

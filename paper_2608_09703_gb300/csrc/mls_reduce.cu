@@ -17,6 +17,7 @@
 
 #include "mls_device.cuh"
 #include "mls_kernels.h"
+#include "mls_vec.cuh"
 
 namespace mls {
 namespace {
@@ -317,42 +318,54 @@ constexpr int kLogpMergeWarps = 8;
 
 __global__ void __launch_bounds__(32 * kLogpMergeWarps)
     logp_merge_kernel(const __grid_constant__ LogpMergeParams p) {
-  __shared__ float sh[3][kLogpMergeWarps][32];
+  __shared__ float sh[kLogpFields][kLogpMergeWarps][32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const long long MT = static_cast<long long>(p.M) * p.T, PS = kLogpFields * MT;
   const long long i = static_cast<long long>(blockIdx.x) * 32 + lane;
   chain_wait();
-  float m = -INFINITY, s = 0.f, zy = 0.f;
+  float m = -INFINITY, zy = 0.f;
+  Pair s = {0.f, 0.f};
   if (i < MT) {
     const float* P = p.part + i;
 #pragma unroll 4
     for (int k = warp; k < p.nparts; k += kLogpMergeWarps) {
-      const float mk = P[k * PS + kLogpMax * MT], sk = P[k * PS + kLogpSum * MT];
+      const float mk = P[k * PS + kLogpMax * MT], hi = P[k * PS + kLogpSum * MT], lo = P[k * PS + kLogpSumLow * MT];
       zy += P[k * PS + kLogpTarget * MT];
       const float mn = fmaxf(m, mk);
-      if (mn != -INFINITY) s = s * exp2f((m - mn) * p.Ltau) + sk * exp2f((mk - mn) * p.Ltau);
+      if (mn != -INFINITY) {
+        const float own = exp2f((m - mn) * p.Ltau), other = exp2f((mk - mn) * p.Ltau);
+        s = {s.hi * own, s.lo * own};
+        pair_add(s, hi * other, lo * other);
+      }
       m = mn;
     }
   }
-  sh[0][warp][lane] = m;
-  sh[1][warp][lane] = s;
-  sh[2][warp][lane] = zy;
+  sh[kLogpMax][warp][lane] = m;
+  sh[kLogpSum][warp][lane] = s.hi;
+  sh[kLogpSumLow][warp][lane] = s.lo;
+  sh[kLogpTarget][warp][lane] = zy;
   __syncthreads();
   if (warp > 0 || i >= MT) return;
 #pragma unroll
-  for (int q = 1; q < kLogpMergeWarps; ++q) m = fmaxf(m, sh[0][q][lane]);
-  s = zy = 0.f;
+  for (int q = 1; q < kLogpMergeWarps; ++q) m = fmaxf(m, sh[kLogpMax][q][lane]);
+  s = {0.f, 0.f};
+  zy = 0.f;
 #pragma unroll
   for (int q = 0; q < kLogpMergeWarps; ++q) {
-    const float mq = sh[0][q][lane];
-    if (mq != -INFINITY) s += sh[1][q][lane] * exp2f((mq - m) * p.Ltau);
-    zy += sh[2][q][lane];
+    const float mq = sh[kLogpMax][q][lane];
+    if (mq != -INFINITY) {
+      const float scale = exp2f((mq - m) * p.Ltau);
+      pair_add(s, sh[kLogpSum][q][lane] * scale, sh[kLogpSumLow][q][lane] * scale);
+    }
+    zy += sh[kLogpTarget][q][lane];
   }
   const int y = p.y[i % p.T];
   if (y >= p.V) atomicOr(p.status, kStatusBadTarget);
-  const float ls = logf(s);
+  // The maximum's own term is 1 in every sum above, so what the others add to it is known to
+  // its own size; relative to the maximum nothing cancels where the token has nearly all the mass.
+  const float others = (s.hi - 1.f) + s.lo;
+  const float ls = log1pf(others < 0.f ? 0.f : others);
   p.lse[i] = fmaf(m, p.inv_tau, ls);
-  // relative to the maximum: nothing cancels where the token has nearly all the mass
   p.logp[i] = y >= 0 && y < p.V ? (zy - m) * p.inv_tau - ls : 0.f;
 }
 
