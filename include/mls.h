@@ -243,6 +243,11 @@ int mls_spec_verify(const mls_spec_problem* p, const void* H_draft, const void* 
  *   dH[m], dW[m]  device, bf16 [T, d_m] and [V, d_m], 16-byte aligned, overwritten (dW zeros
  *              when T = 0); sums are fp32, rounded once.  They overlap neither each other
  *              nor an input (a buffer given twice: MLS_ERR_ARG).
+ *   peak       device, fp32 [2, M, T]: the largest logit of the row, and the sum over all other
+ *              tokens of exp((z - largest) / tau).  The _peak forms write and read it, the backward
+ *              beside lse, whatever its targets; the plain ones have none, and their 1 - p of the
+ *              target is off by the rounding of lse, up to |lse| 2^-23 (with it, by 2^-22 and 1e-5 of
+ *              itself: what counts for tokens with nearly all of the mass).
  *   ws         device workspace of mls_logp_workspace_size(p) bytes
  */
 size_t mls_logp_workspace_size(const mls_problem* p);
@@ -253,6 +258,13 @@ int mls_head_logp_bwd(const mls_problem* p, const void* const* H, const void* co
                       const int32_t* targets, const float* lse, const float* dlogp,
                       void* const* dH, void* const* dW, void* ws, size_t ws_bytes,
                       mls_stream_t stream);
+int mls_head_logp_fwd_peak(const mls_problem* p, const void* const* H, const void* const* W,
+                           const int32_t* targets, float* logp, float* lse, float* peak, void* ws,
+                           size_t ws_bytes, mls_stream_t stream);
+int mls_head_logp_bwd_peak(const mls_problem* p, const void* const* H, const void* const* W,
+                           const int32_t* targets, const float* lse, const float* peak,
+                           const float* dlogp, void* const* dH, void* const* dW, void* ws,
+                           size_t ws_bytes, mls_stream_t stream);
 
 /*
  * Layer norm of T rows of d values, the norm in front of a head:

@@ -133,6 +133,10 @@ def lib():
         L.mls_head_logp_fwd.restype = ctypes.c_int
         L.mls_head_logp_bwd.argtypes = [P, vpp, vpp, vp, vp, vp, vpp, vpp, vp, sz, vp]
         L.mls_head_logp_bwd.restype = ctypes.c_int
+        L.mls_head_logp_fwd_peak.argtypes = [P, vpp, vpp, vp, vp, vp, vp, vp, sz, vp]
+        L.mls_head_logp_fwd_peak.restype = ctypes.c_int
+        L.mls_head_logp_bwd_peak.argtypes = [P, vpp, vpp, vp, vp, vp, vp, vpp, vpp, vp, sz, vp]
+        L.mls_head_logp_bwd_peak.restype = ctypes.c_int
         L.mls_layer_norm_fwd.argtypes = [i64, i32, i32, f32, vp, vp, vp, vp, vp, vp, vp]
         L.mls_layer_norm_fwd.restype = ctypes.c_int
         L.mls_layer_norm_workspace_size.argtypes = [i64, i32]
@@ -354,19 +358,25 @@ def mls_logp_workspace_size(prob: "Problem") -> int:
     return int(lib().mls_logp_workspace_size(prob.ref()))
 
 
-def mls_head_logp_fwd(prob: "Problem", H, W, targets, logp, lse, ws, stream=None) -> None:
-    """Log-probabilities of the targets through every head (see include/mls.h)."""
+def mls_head_logp_fwd(prob: "Problem", H, W, targets, logp, lse, ws, stream=None, peak=None) -> None:
+    """Log-probabilities of the targets through every head (see include/mls.h); with peak
+    the backward keeps the digits of tokens with nearly all of the mass."""
     dev = _expect_heads(prob, H, W, targets)
     rows = (prob.c.M, prob.c.T)
     _expect("logp", logp, torch.float32, rows, dev)
     _expect("lse", lse, torch.float32, rows, dev)
     wsp, wsn = _ws_args(ws, dev)
-    rc = lib().mls_head_logp_fwd(prob.ref(), _ptrs(H), _ptrs(W), _ptr(targets), _ptr(logp), _ptr(lse),
-                                 wsp, wsn, _stream(stream))
+    if peak is None:
+        rc = lib().mls_head_logp_fwd(prob.ref(), _ptrs(H), _ptrs(W), _ptr(targets), _ptr(logp), _ptr(lse),
+                                     wsp, wsn, _stream(stream))
+    else:
+        _expect("peak", peak, torch.float32, (2,) + rows, dev)
+        rc = lib().mls_head_logp_fwd_peak(prob.ref(), _ptrs(H), _ptrs(W), _ptr(targets), _ptr(logp), _ptr(lse),
+                                          _ptr(peak), wsp, wsn, _stream(stream))
     _check(rc, "mls_head_logp_fwd")
 
 
-def mls_head_logp_bwd(prob: "Problem", H, W, targets, lse, dlogp, dH, dW, ws, stream=None) -> None:
+def mls_head_logp_bwd(prob: "Problem", H, W, targets, lse, dlogp, dH, dW, ws, stream=None, peak=None) -> None:
     dev = _expect_heads(prob, H, W, targets)
     d, T, V = prob.sizes
     _expect("lse", lse, torch.float32, (len(d), T), dev)
@@ -377,8 +387,13 @@ def mls_head_logp_bwd(prob: "Problem", H, W, targets, lse, dlogp, dH, dW, ws, st
         _expect("dH", h, H[0].dtype, (T, dm), dev)
         _expect("dW", w, H[0].dtype, (V, dm), dev)
     wsp, wsn = _ws_args(ws, dev)
-    rc = lib().mls_head_logp_bwd(prob.ref(), _ptrs(H), _ptrs(W), _ptr(targets), _ptr(lse), _ptr(dlogp),
-                                 _ptrs(dH), _ptrs(dW), wsp, wsn, _stream(stream))
+    if peak is None:
+        rc = lib().mls_head_logp_bwd(prob.ref(), _ptrs(H), _ptrs(W), _ptr(targets), _ptr(lse), _ptr(dlogp),
+                                     _ptrs(dH), _ptrs(dW), wsp, wsn, _stream(stream))
+    else:
+        _expect("peak", peak, torch.float32, (2, len(d), T), dev)
+        rc = lib().mls_head_logp_bwd_peak(prob.ref(), _ptrs(H), _ptrs(W), _ptr(targets), _ptr(lse), _ptr(peak),
+                                          _ptr(dlogp), _ptrs(dH), _ptrs(dW), wsp, wsn, _stream(stream))
     _check(rc, "mls_head_logp_bwd")
 
 
@@ -640,6 +655,7 @@ class HeadLogp:
         self.rows = (M, T)
         self.logp = torch.empty(M, T, dtype=torch.float32, device=dev)
         self.lse = torch.empty(M, T, dtype=torch.float32, device=dev)
+        self.peak = torch.empty(2, M, T, dtype=torch.float32, device=dev)  # handed on to the backward
         self.dH = [torch.empty(T, dm, dtype=torch.bfloat16, device=dev) for dm in d]
         self.dW = [torch.empty(V, dm, dtype=torch.bfloat16, device=dev) for dm in d]
         self.ws = torch.empty(max(mls_logp_workspace_size(self.prob), 1), dtype=torch.uint8, device=dev)
@@ -649,9 +665,9 @@ class HeadLogp:
     # backward of two sub-models).
     def forward(self, H, W, targets, stream=None):
         _expect_heads(self.prob, H, W, targets, self.home())
-        rc = lib().mls_head_logp_fwd(self.prob.ref(), _ptrs(H), _ptrs(W), targets.data_ptr(),
-                                     self.logp.data_ptr(), self.lse.data_ptr(), self.ws.data_ptr(),
-                                     self.ws.numel(), _stream(stream))
+        rc = lib().mls_head_logp_fwd_peak(self.prob.ref(), _ptrs(H), _ptrs(W), targets.data_ptr(),
+                                          self.logp.data_ptr(), self.lse.data_ptr(), self.peak.data_ptr(),
+                                          self.ws.data_ptr(), self.ws.numel(), _stream(stream))
         _check(rc, "mls_head_logp_fwd")
         return self.logp
 
@@ -659,9 +675,10 @@ class HeadLogp:
         """Gradients for the tokens of the last forward; returns (dH, dW)."""
         dev = _expect_heads(self.prob, H, W, targets, self.home())
         _expect("dlogp", dlogp, torch.float32, self.rows, dev)
-        rc = lib().mls_head_logp_bwd(self.prob.ref(), _ptrs(H), _ptrs(W), targets.data_ptr(),
-                                     self.lse.data_ptr(), dlogp.data_ptr(), _ptrs(self.dH),
-                                     _ptrs(self.dW), self.ws.data_ptr(), self.ws.numel(), _stream(stream))
+        rc = lib().mls_head_logp_bwd_peak(self.prob.ref(), _ptrs(H), _ptrs(W), targets.data_ptr(),
+                                          self.lse.data_ptr(), self.peak.data_ptr(), dlogp.data_ptr(),
+                                          _ptrs(self.dH), _ptrs(self.dW), self.ws.data_ptr(), self.ws.numel(),
+                                          _stream(stream))
         _check(rc, "mls_head_logp_bwd")
         return self.dH, self.dW
 

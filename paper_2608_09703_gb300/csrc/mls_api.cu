@@ -884,9 +884,9 @@ extern "C" size_t mls_logp_workspace_size(const mls_problem* p) {
   return logp_plan(p, head, gemm).total;
 }
 
-extern "C" int mls_head_logp_fwd(const mls_problem* p, const void* const* H, const void* const* W,
-                                 const int32_t* targets, float* logp, float* lse, void* ws,
-                                 size_t ws_bytes, mls_stream_t stream) {
+namespace {
+int logp_fwd(const mls_problem* p, const void* const* H, const void* const* W, const int32_t* targets,
+             float* logp, float* lse, float* peak, void* ws, size_t ws_bytes, mls_stream_t stream) {
   int rc = logp_validate(p);
   if (rc) return rc;
   if (!H || !W || (p->T > 0 && (!targets || !logp || !lse))) return MLS_ERR_ARG;
@@ -894,7 +894,7 @@ extern "C" int mls_head_logp_fwd(const mls_problem* p, const void* const* H, con
     if ((p->T > 0 && !H[m]) || !W[m]) return MLS_ERR_ARG;
     if (!aligned16(H[m]) || !aligned16(W[m])) return MLS_ERR_ALIGN;
   }
-  if (!aligned4(targets) || !aligned4(logp) || !aligned4(lse)) return MLS_ERR_ALIGN;
+  if (!aligned4(targets) || !aligned4(logp) || !aligned4(lse) || !aligned4(peak)) return MLS_ERR_ALIGN;
   DeviceState* dev = nullptr;
   if ((rc = device_state(&dev))) return rc;
   if (p->T == 0) return MLS_OK;
@@ -922,14 +922,14 @@ extern "C" int mls_head_logp_fwd(const mls_problem* p, const void* const* H, con
   mp.y = targets;
   mp.logp = logp;
   mp.lse = lse;
+  mp.peak = peak;
   mp.status = dev->status;
   return timed("logp_merge", s, [&] { return launch_logp_merge(mp, s); });
 }
 
-extern "C" int mls_head_logp_bwd(const mls_problem* p, const void* const* H, const void* const* W,
-                                 const int32_t* targets, const float* lse, const float* dlogp,
-                                 void* const* dH, void* const* dW, void* ws, size_t ws_bytes,
-                                 mls_stream_t stream) {
+int logp_bwd(const mls_problem* p, const void* const* H, const void* const* W, const int32_t* targets,
+             const float* lse, const float* peak, const float* dlogp, void* const* dH, void* const* dW,
+             void* ws, size_t ws_bytes, mls_stream_t stream) {
   int rc = logp_validate(p);
   if (rc) return rc;
   if (!H || !W || !dH || !dW || (p->T > 0 && (!targets || !lse || !dlogp))) return MLS_ERR_ARG;
@@ -938,7 +938,7 @@ extern "C" int mls_head_logp_bwd(const mls_problem* p, const void* const* H, con
     if (!aligned16(H[m]) || !aligned16(W[m]) || !aligned16(dW[m]) || !aligned16(dH[m]))
       return MLS_ERR_ALIGN;
   }
-  if (!aligned4(targets) || !aligned4(lse) || !aligned4(dlogp)) return MLS_ERR_ALIGN;
+  if (!aligned4(targets) || !aligned4(lse) || !aligned4(dlogp) || !aligned4(peak)) return MLS_ERR_ALIGN;
   for (int m = 0; m < p->M; ++m)  // one buffer for two gradients, or for a gradient and an input
     for (int k = 0; k < p->M; ++k) {
       if ((k != m && (dW[m] == dW[k] || (p->T > 0 && dH[m] == dH[k]))) || dW[m] == W[k]) return MLS_ERR_ARG;
@@ -963,12 +963,42 @@ extern "C" int mls_head_logp_bwd(const mls_problem* p, const void* const* H, con
   if ((rc = encode_head_maps(hp, p, pl, H, W))) return rc;
   hp.stats = lse;
   hp.dlogp = dlogp;
+  hp.peak = peak;
   hp.neg_inv_tau = static_cast<float>(-1.0 / static_cast<double>(p->tau));
   return backward_groups(p, pl, *dev, H, W, hp, wsb + pl.off_G, dH, dW, true,
                          reinterpret_cast<float*>(wsb + lp.off_acc),
                          reinterpret_cast<float*>(wsb + pl.off_split), s, [&](long long g) {
                            return timed("logp_bwd", s, [&] { return launch_logp_bwd(hp, g > 0, s); });
                          });
+}
+}  // namespace
+
+extern "C" int mls_head_logp_fwd(const mls_problem* p, const void* const* H, const void* const* W,
+                                 const int32_t* targets, float* logp, float* lse, void* ws,
+                                 size_t ws_bytes, mls_stream_t stream) {
+  return logp_fwd(p, H, W, targets, logp, lse, nullptr, ws, ws_bytes, stream);
+}
+
+extern "C" int mls_head_logp_fwd_peak(const mls_problem* p, const void* const* H, const void* const* W,
+                                      const int32_t* targets, float* logp, float* lse, float* peak,
+                                      void* ws, size_t ws_bytes, mls_stream_t stream) {
+  if (p && p->T > 0 && !peak) return MLS_ERR_ARG;
+  return logp_fwd(p, H, W, targets, logp, lse, peak, ws, ws_bytes, stream);
+}
+
+extern "C" int mls_head_logp_bwd(const mls_problem* p, const void* const* H, const void* const* W,
+                                 const int32_t* targets, const float* lse, const float* dlogp,
+                                 void* const* dH, void* const* dW, void* ws, size_t ws_bytes,
+                                 mls_stream_t stream) {
+  return logp_bwd(p, H, W, targets, lse, nullptr, dlogp, dH, dW, ws, ws_bytes, stream);
+}
+
+extern "C" int mls_head_logp_bwd_peak(const mls_problem* p, const void* const* H, const void* const* W,
+                                      const int32_t* targets, const float* lse, const float* peak,
+                                      const float* dlogp, void* const* dH, void* const* dW, void* ws,
+                                      size_t ws_bytes, mls_stream_t stream) {
+  if (p && p->T > 0 && !peak) return MLS_ERR_ARG;
+  return logp_bwd(p, H, W, targets, lse, peak, dlogp, dH, dW, ws, ws_bytes, stream);
 }
 
 extern "C" int mls_get_status(mls_stream_t stream) {

@@ -790,9 +790,14 @@ __device__ __forceinline__ void logp_fwd_epilogue(const HeadParams& p, uint32_t 
 }
 
 // dL/dz of one tile: c (softmax(z / tau) - e_y), c = -dL/dlogp / tau, b = -logsumexp(z / tau) log2(e).
+// With `peak`, 1 - p of the target comes from the largest logit, top, and what the other tokens add
+// to its 1: e^-lse has the error of lse's one word, up to |lse| 2^-24 (1e-6), which is all of 1 - p
+// where the token has nearly all of the mass.  Relative to themselves that error is nothing to
+// the other tokens' shares.
 template <bool kMasked>
 __device__ __forceinline__ void logp_grad_tile(const float (&v)[128], int nvalid, int yl, float Lt, float b,
-                                               float c, const GOut& o, int gcol, int lane) {
+                                               float c, bool peak, float top, float others, const GOut& o,
+                                               int gcol, int lane) {
   const F2 L2 = f2(Lt), b2 = f2(b), c2 = f2(c);
 #pragma unroll
   for (int ch = 0; ch < 4; ++ch) {
@@ -810,9 +815,17 @@ __device__ __forceinline__ void logp_grad_tile(const float (&v)[128], int nvalid
     }
     const int r = yl - ch * 32;
     if (static_cast<unsigned>(r) < 32u) {
+      float zy = 0.f, gy = 0.f;
 #pragma unroll
       for (int i = 0; i < 32; ++i)
-        if (i == r) g[i] -= c;
+        if (i == r) {
+          zy = v[ch * 32 + i];
+          gy = g[i] - c;
+        }
+      if (peak) gy = -c * fmaxf(others + (1.f - exp2f((zy - top) * Lt)), 0.f) / (1.f + others);
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (i == r) g[i] = gy;
     }
     // A token without a gradient: nothing, also where its logits overflowed (0 times a NaN).
     if (c == 0.f) {
@@ -836,12 +849,16 @@ __device__ __forceinline__ void logp_bwd_epilogue(const HeadParams& p, uint32_t 
   uint32_t nchunks = 0;
   const uint32_t stage = base + HeadSmem::kStage + static_cast<uint32_t>(warp) * 2 * kHeadStageChunk;
   const int row0 = row_base + quad * 32;
-  float c[kMaxModels], b[kMaxModels];
+  const bool peak = p.peak != nullptr;
+  const float* others_at = peak ? p.peak + static_cast<long long>(p.M) * p.T : nullptr;
+  float c[kMaxModels], b[kMaxModels], top[kMaxModels], others[kMaxModels];
 #pragma unroll
   for (int j = 0; j < kMaxModels; ++j) {
     const bool on = j < p.M && valid;
     const long long i = static_cast<long long>(j) * p.T + row;
     c[j] = on ? p.neg_inv_tau * p.dlogp[i] : 0.f;
+    top[j] = on && peak ? p.peak[i] : 0.f;
+    others[j] = on && peak ? others_at[i] : 0.f;
     b[j] = j < p.M && row_ok ? -__ldg(p.stats + i) * p.L1 : 0.f;
   }
   uint32_t acc = 0, acc_par = 0;
@@ -863,9 +880,9 @@ __device__ __forceinline__ void logp_bwd_epilogue(const HeadParams& p, uint32_t 
         tmem_ld128(tl + acc * kHeadBN, v);
         logp_release(base, acc, acc_par, lane);
         if (nvalid == 128)
-          logp_grad_tile<false>(v, 128, yl, p.Ltau, b[j], c[j], o, gcol, lane);
+          logp_grad_tile<false>(v, 128, yl, p.Ltau, b[j], c[j], peak, top[j], others[j], o, gcol, lane);
         else
-          logp_grad_tile<true>(v, nvalid, yl, p.Ltau, b[j], c[j], o, gcol, lane);
+          logp_grad_tile<true>(v, nvalid, yl, p.Ltau, b[j], c[j], peak, top[j], others[j], o, gcol, lane);
       }
     }
   }

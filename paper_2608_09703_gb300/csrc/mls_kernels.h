@@ -142,6 +142,7 @@ struct HeadParams {
   long long g_col0;              // vocabulary column of the group's first column
   // log-probabilities: `part` holds [S + extra][kLogpFields][M][T], `stats` [M][T]: logsumexp(z/tau)
   const float* dlogp;            // [M][T]
+  const float* peak;             // [2][M][T] or null: see LogpMergeParams
   float neg_inv_tau;             // -1 / tau
 };
 enum LogpField { kLogpMax = 0, kLogpSum, kLogpSumLow, kLogpTarget, kLogpFields };  // the sum in two words
@@ -442,6 +443,8 @@ struct LogpMergeParams {
   float Ltau, inv_tau;
   const int* y;
   float *logp, *lse;             // [M][T]
+  float* peak;                   // [2][M][T] or null: the largest logit, and what all tokens but
+                                 //   that one add to its e^0
   int* status;
 };
 cudaError_t launch_logp_merge(const LogpMergeParams& p, cudaStream_t s);

@@ -363,8 +363,12 @@ __global__ void __launch_bounds__(32 * kLogpMergeWarps)
   if (y >= p.V) atomicOr(p.status, kStatusBadTarget);
   // The maximum's own term is 1 in every sum above, so what the others add to it is known to
   // its own size; relative to the maximum nothing cancels where the token has nearly all the mass.
-  const float others = (s.hi - 1.f) + s.lo;
-  const float ls = log1pf(others < 0.f ? 0.f : others);
+  const float more = (s.hi - 1.f) + s.lo, others = more < 0.f ? 0.f : more;
+  const float ls = log1pf(others);
+  if (p.peak) {
+    p.peak[i] = m;
+    p.peak[MT + i] = others;
+  }
   p.lse[i] = fmaf(m, p.inv_tau, ls);
   p.logp[i] = y >= 0 && y < p.V ? (zy - m) * p.inv_tau - ls : 0.f;
 }

@@ -9,11 +9,14 @@ and two products), the sums 32 u; the largest logit's own term is 1.  Its column
 of a tile's 128, are added to that 1: there an addition is off by at most u, and by no more than what is
 added, which the next words never see again: 24 u, or twice those columns' terms if that is less.
 """
+import ctypes
+
 import pytest
 import torch
 
 import paper_2608_09703_gb300 as mls
 from paper_2608_09703_gb300 import binding as B
+from paper_2608_09703_gb300 import build as mbuild
 
 U = 2.0 ** -24
 D = 64
@@ -72,3 +75,132 @@ def test_log_probabilities(T, V, scale, gap, tau, alone):
         bad = ~(err <= tol / (1 + others) + 6 * U * want.abs())
         assert not bad.any(), (int(bad.sum()), float(err.max()), float(others.median()))
     assert mls.mls_get_status() == 0
+
+
+def grads(op, H, W, y, scale, plain=False):
+    """dL/dz [M][T, V] for dlogp = scale: with T different unit vectors dW is its transpose."""
+    T = len(y)
+    dl = torch.full((len(H), T), scale, device="cuda")
+    if plain:
+        B.mls_head_logp_bwd(op.prob, H, W, y, op.lse, dl, op.dH, op.dW, op.ws)
+    else:
+        op.backward(H, W, y, dl)
+    return [w.double().t() for w in op.dW]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("alone", [False, True])
+@pytest.mark.parametrize("V,scale,gap,tau,group", [(5000, 12.0, 20.0, 1.0, 0), (5000, 29.75, 27.0, 1.0, 1024),
+                                                   (50304, 41.5, 24.0, 1.0, 0), (300, 30.25, 14.0, 0.7, 0),
+                                                   (20000, 100.5, 34.0, 1.0, 0), (9000, -57.5, 26.0, 1.3, 2048)])
+def test_gradient_at_the_target_and_elsewhere(V, scale, gap, tau, group, alone):
+    """1 - p of the target to its own digits (rounded to bf16 in dL/dz, dW is of one token's), the
+    other tokens' p within the rounding of lse's one word, 2 u |lse|, and of the exponent, and bf16."""
+    H, W, y, k = inputs(D, V, scale, gap, alone, seed=V + 1, models=2)
+    op = mls.HeadLogp((D, D), D, V, tau=tau, vocab_group=group)
+    op.forward(H, W, y)
+    t32 = float(torch.tensor(tau))
+    for m, G in enumerate(grads(op, H, W, y, 3.0)):
+        others, tol = shares(W[m], y, k, tau, V)
+        c = 3.0 / t32
+        want = c * others / (1 + others)
+        got = G.gather(1, y.long()[:, None])[:, 0]
+        assert bool(((got - want).abs() <= c * tol + (2.0 ** -8 + 8 * U) * want).all()), \
+            float(((got - want).abs() / want).max())
+        z = W[m].double().t() / t32
+        p = torch.softmax(z, 1)
+        lse = torch.logsumexp(z, 1, keepdim=True)
+        off = U * (4 * lse.abs() + 4 * z.abs() + 64) + (tol / (1 + others))[:, None]
+        err = (G + c * p).scatter(1, y.long()[:, None], 0.0).abs()
+        assert bool((err <= c * p * (off + 2.0 ** -8) + 1e-37).all())
+    assert mls.mls_get_status() == 0
+
+
+@pytest.mark.gpu
+def test_other_targets_in_the_backward():
+    """What the forward hands on does not depend on its targets."""
+    V = 3000
+    H, W, y, k = inputs(D, V, 30.0, 22.0, seed=5)
+    op = mls.HeadLogp((D,), D, V)
+    op.forward(H, W, y)
+    want = [g.clone() for g in grads(op, H, W, y, 1.0)]
+    other = torch.where(torch.arange(D, device="cuda") % 2 == 0, (y + 1) % V, -1).int()
+    op.forward(H, W, other)
+    got = grads(op, H, W, y, 1.0)
+    assert torch.equal(got[0], want[0])
+    op.forward(H, W, y)
+    G = grads(op, H, W, other, 1.0)[0]
+    assert not G[other < 0].any()
+    on = other >= 0
+    z = W[0].double().t()
+    p = torch.softmax(z, 1).gather(1, other.clamp(min=0).long()[:, None])[:, 0]
+    at = G.gather(1, other.clamp(min=0).long()[:, None])[:, 0]
+    assert bool(((at - (1 - p)).abs() <= (2.0 ** -8 + 64 * U))[on].all())
+
+
+@pytest.mark.gpu
+def test_without_what_the_forward_hands_on():
+    """The plain calls: 1 - p within the rounding of lse."""
+    V, scale = 5000, 29.75
+    H, W, y, k = inputs(D, V, scale, 27.0, seed=2)
+    op = mls.HeadLogp((D,), D, V)
+    B.mls_head_logp_fwd(op.prob, H, W, y, op.logp, op.lse, op.ws)
+    got = grads(op, H, W, y, 1.0, plain=True)[0].gather(1, y.long()[:, None])[:, 0]
+    others, tol = shares(W[0], y, k, 1.0, V)
+    want = others / (1 + others)
+    assert bool(((got - want).abs() <= tol + 2 * U * scale + 16 * U + 2.0 ** -8 * got.abs()).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,V,tau", [(136, 20000, 1.0), (520, 1031, 0.8), (2048, 33000, 1.0)])
+def test_recomputed_logits_are_the_same(d, V, tau):
+    """Any hidden state: one token's dW is dL/dz times its row, so dL/dz at the target is read off dW
+    and is 1 - exp of the forward's log-probability, whatever that is."""
+    for seed in range(4):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        H = [torch.randn(1, d, generator=g, device="cuda").bfloat16()]
+        W = [(torch.randn(V, d, generator=g, device="cuda") * (4.0 / d ** 0.5)).bfloat16()]
+        best = int((H[0].float() @ W[0].float().t()).argmax())
+        W[0][best] = (H[0][0].float() * (24.0 + 2 * seed) / float((H[0].float() ** 2).sum())).bfloat16()
+        y = torch.tensor([best], dtype=torch.int32, device="cuda")
+        op = mls.HeadLogp((d,), 1, V, tau=tau)
+        logp = float(op.forward(H, W, y))
+        op.backward(H, W, y, torch.ones(1, 1, device="cuda"))
+        h = H[0][0].double()
+        got = float((op.dW[0][best].double() * h).sum() / (h * h).sum()) * float(torch.tensor(tau))
+        want = -torch.expm1(torch.tensor(logp, dtype=torch.float64)).item()
+        assert 0 < want < 0.9 and abs(got - want) <= 2 * 2.0 ** -8 * want, (got, want)
+
+
+# ------------------------------------------------------------------ refusals
+def test_refusals_of_the_library():
+    mbuild.build()
+    L, prob, p = B.lib(), mls.Problem((64,), 10, 100), 0x1000
+
+    def arr(v):
+        return (ctypes.c_void_p * 1)(v)
+
+    def fwd(peak, prob=prob):
+        return L.mls_head_logp_fwd_peak(prob.ref(), arr(p), arr(p), p, p, p, peak, 0x10000, 1 << 40, None)
+
+    def bwd(peak, prob=prob):
+        return L.mls_head_logp_bwd_peak(prob.ref(), arr(p), arr(p), p, p, peak, p, arr(2 * p), arr(3 * p), 0x10000,
+                                        1 << 40, None)
+
+    for call in (fwd, bwd):
+        assert call(None) == B.MLS_ERR_ARG and call(p + 2) == B.MLS_ERR_ALIGN
+        assert call(p, mls.Problem((64,), 10, 100, in_dtype=B.MLS_FP32)) == B.MLS_ERR_UNSUPPORTED
+    assert L.mls_head_logp_fwd_peak(*[None] * 8, 0, None) == B.MLS_ERR_ARG
+    assert L.mls_head_logp_bwd_peak(*[None] * 10, 0, None) == B.MLS_ERR_ARG
+
+
+@pytest.mark.gpu
+def test_refusals_of_the_binding():
+    H, W, y, _ = inputs(D, 500, 10.0, 12.0)
+    op = mls.HeadLogp((D,), D, 500)
+    dl = torch.ones(1, D, device="cuda")
+    for peak in (op.peak[0], op.peak.double(), op.peak.cpu(), op.peak.transpose(0, 1)[:, :, 1:]):
+        with pytest.raises((TypeError, ValueError)):
+            B.mls_head_logp_fwd(op.prob, H, W, y, op.logp, op.lse, op.ws, peak=peak)
+        with pytest.raises((TypeError, ValueError)):
+            B.mls_head_logp_bwd(op.prob, H, W, y, op.lse, dl, op.dH, op.dW, op.ws, peak=peak)
