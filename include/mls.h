@@ -243,11 +243,12 @@ int mls_spec_verify(const mls_spec_problem* p, const void* H_draft, const void* 
  *   dH[m], dW[m]  device, bf16 [T, d_m] and [V, d_m], 16-byte aligned, overwritten (dW zeros
  *              when T = 0); sums are fp32, rounded once.  They overlap neither each other
  *              nor an input (a buffer given twice: MLS_ERR_ARG).
- *   peak       device, fp32 [2, M, T]: the largest logit of the row, and the sum over all other
- *              tokens of exp((z - largest) / tau).  The _peak forms write and read it, the backward
- *              beside lse, whatever its targets; the plain ones have none, and their 1 - p of the
- *              target is off by the rounding of lse, up to |lse| 2^-23 (with it, by 2^-22 and 1e-5 of
- *              itself: what counts for tokens with nearly all of the mass).
+ *   peak       device, fp32 [2, M, T]: per row the sum over all tokens but one with the largest
+ *              logit of exp((z - largest) / tau), and as the bits of an int32 the target if it
+ *              has the largest logit, else -1.  The _peak forms write it and read it beside lse.
+ *              With it 1 - p of such a target keeps its own digits in the backward (to 1e-5 of
+ *              it, and 2^-20 at most); the plain forms, and other targets than the forward's,
+ *              have the rounding of lse in it, up to |lse| 2^-23.
  *   ws         device workspace of mls_logp_workspace_size(p) bytes
  */
 size_t mls_logp_workspace_size(const mls_problem* p);

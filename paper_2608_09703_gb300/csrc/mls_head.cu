@@ -790,14 +790,12 @@ __device__ __forceinline__ void logp_fwd_epilogue(const HeadParams& p, uint32_t 
 }
 
 // dL/dz of one tile: c (softmax(z / tau) - e_y), c = -dL/dlogp / tau, b = -logsumexp(z / tau) log2(e).
-// With `peak`, 1 - p of the target comes from the largest logit, top, and what the other tokens add
-// to its 1: e^-lse has the error of lse's one word, up to |lse| 2^-24 (1e-6), which is all of 1 - p
-// where the token has nearly all of the mass.  Relative to themselves that error is nothing to
-// the other tokens' shares.
+// The target's own is at.x times c p plus at.y: (1, -c), or (0, -c (1 - p)) where 1 - p is known better
+// than p is here.  e^-lse has the error of lse's one word, up to |lse| 2^-24 (1e-6): nothing to a
+// token's share relative to itself, but all of 1 - p where the target has nearly all of the mass.
 template <bool kMasked>
 __device__ __forceinline__ void logp_grad_tile(const float (&v)[128], int nvalid, int yl, float Lt, float b,
-                                               float c, bool peak, float top, float others, const GOut& o,
-                                               int gcol, int lane) {
+                                               float c, float2 at, const GOut& o, int gcol, int lane) {
   const F2 L2 = f2(Lt), b2 = f2(b), c2 = f2(c);
 #pragma unroll
   for (int ch = 0; ch < 4; ++ch) {
@@ -815,17 +813,9 @@ __device__ __forceinline__ void logp_grad_tile(const float (&v)[128], int nvalid
     }
     const int r = yl - ch * 32;
     if (static_cast<unsigned>(r) < 32u) {
-      float zy = 0.f, gy = 0.f;
 #pragma unroll
       for (int i = 0; i < 32; ++i)
-        if (i == r) {
-          zy = v[ch * 32 + i];
-          gy = g[i] - c;
-        }
-      if (peak) gy = -c * fmaxf(others + (1.f - exp2f((zy - top) * Lt)), 0.f) / (1.f + others);
-#pragma unroll
-      for (int i = 0; i < 32; ++i)
-        if (i == r) g[i] = gy;
+        if (i == r) g[i] = fmaf(g[i], at.x, at.y);
     }
     // A token without a gradient: nothing, also where its logits overflowed (0 times a NaN).
     if (c == 0.f) {
@@ -849,16 +839,19 @@ __device__ __forceinline__ void logp_bwd_epilogue(const HeadParams& p, uint32_t 
   uint32_t nchunks = 0;
   const uint32_t stage = base + HeadSmem::kStage + static_cast<uint32_t>(warp) * 2 * kHeadStageChunk;
   const int row0 = row_base + quad * 32;
-  const bool peak = p.peak != nullptr;
-  const float* others_at = peak ? p.peak + static_cast<long long>(p.M) * p.T : nullptr;
-  float c[kMaxModels], b[kMaxModels], top[kMaxModels], others[kMaxModels];
+  const long long MT = static_cast<long long>(p.M) * p.T;
+  float c[kMaxModels], b[kMaxModels];
+  float2 at[kMaxModels];
 #pragma unroll
   for (int j = 0; j < kMaxModels; ++j) {
     const bool on = j < p.M && valid;
     const long long i = static_cast<long long>(j) * p.T + row;
     c[j] = on ? p.neg_inv_tau * p.dlogp[i] : 0.f;
-    top[j] = on && peak ? p.peak[i] : 0.f;
-    others[j] = on && peak ? others_at[i] : 0.f;
+    at[j] = make_float2(1.f, -c[j]);
+    if (on && p.peak && __float_as_int(p.peak[MT + i]) == y) {
+      const float others = p.peak[i];
+      at[j] = make_float2(0.f, -c[j] * (others / (1.f + others)));
+    }
     b[j] = j < p.M && row_ok ? -__ldg(p.stats + i) * p.L1 : 0.f;
   }
   uint32_t acc = 0, acc_par = 0;
@@ -880,9 +873,9 @@ __device__ __forceinline__ void logp_bwd_epilogue(const HeadParams& p, uint32_t 
         tmem_ld128(tl + acc * kHeadBN, v);
         logp_release(base, acc, acc_par, lane);
         if (nvalid == 128)
-          logp_grad_tile<false>(v, 128, yl, p.Ltau, b[j], c[j], peak, top[j], others[j], o, gcol, lane);
+          logp_grad_tile<false>(v, 128, yl, p.Ltau, b[j], c[j], at[j], o, gcol, lane);
         else
-          logp_grad_tile<true>(v, nvalid, yl, p.Ltau, b[j], c[j], peak, top[j], others[j], o, gcol, lane);
+          logp_grad_tile<true>(v, nvalid, yl, p.Ltau, b[j], c[j], at[j], o, gcol, lane);
       }
     }
   }

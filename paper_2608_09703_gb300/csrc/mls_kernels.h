@@ -443,8 +443,8 @@ struct LogpMergeParams {
   float Ltau, inv_tau;
   const int* y;
   float *logp, *lse;             // [M][T]
-  float* peak;                   // [2][M][T] or null: the largest logit, and what all tokens but
-                                 //   that one add to its e^0
+  float* peak;                   // [2][M][T] or null: what all tokens but one with the largest logit
+                                 //   add to its e^0, and (an int) the target if that is it, else -1
   int* status;
 };
 cudaError_t launch_logp_merge(const LogpMergeParams& p, cudaStream_t s);

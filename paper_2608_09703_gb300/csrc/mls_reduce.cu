@@ -325,19 +325,24 @@ __global__ void __launch_bounds__(32 * kLogpMergeWarps)
   chain_wait();
   float m = -INFINITY, zy = 0.f;
   Pair s = {0.f, 0.f};
-  if (i < MT) {
-    const float* P = p.part + i;
+  if (i < MT && warp < p.nparts) {
+    // The maximum first, so that the sums' factors do not wait for one another; the warp's first
+    // partial is kept meanwhile, often its only one.
+    const float* P = p.part + i + warp * PS;
+    const float m0 = P[kLogpMax * MT], hi0 = P[kLogpSum * MT], lo0 = P[kLogpSumLow * MT];
+    zy = P[kLogpTarget * MT];
+    m = m0;
+    const long long step = kLogpMergeWarps * PS, end = (p.nparts - warp) * PS;
 #pragma unroll 4
-    for (int k = warp; k < p.nparts; k += kLogpMergeWarps) {
-      const float mk = P[k * PS + kLogpMax * MT], hi = P[k * PS + kLogpSum * MT], lo = P[k * PS + kLogpSumLow * MT];
-      zy += P[k * PS + kLogpTarget * MT];
-      const float mn = fmaxf(m, mk);
-      if (mn != -INFINITY) {
-        const float own = exp2f((m - mn) * p.Ltau), other = exp2f((mk - mn) * p.Ltau);
-        s = {s.hi * own, s.lo * own};
-        pair_add(s, hi * other, lo * other);
-      }
-      m = mn;
+    for (long long k = step; k < end; k += step) m = fmaxf(m, P[k + kLogpMax * MT]);
+    const float scale0 = m0 == -INFINITY ? 0.f : exp2f((m0 - m) * p.Ltau);
+    s = {hi0 * scale0, lo0 * scale0};
+#pragma unroll 4
+    for (long long k = step; k < end; k += step) {
+      const float mk = P[k + kLogpMax * MT], hi = P[k + kLogpSum * MT], lo = P[k + kLogpSumLow * MT];
+      zy += P[k + kLogpTarget * MT];
+      const float scale = mk == -INFINITY ? 0.f : exp2f((mk - m) * p.Ltau);
+      pair_add(s, hi * scale, lo * scale);
     }
   }
   sh[kLogpMax][warp][lane] = m;
@@ -366,8 +371,8 @@ __global__ void __launch_bounds__(32 * kLogpMergeWarps)
   const float more = (s.hi - 1.f) + s.lo, others = more < 0.f ? 0.f : more;
   const float ls = log1pf(others);
   if (p.peak) {
-    p.peak[i] = m;
-    p.peak[MT + i] = others;
+    p.peak[i] = others;
+    p.peak[MT + i] = __int_as_float(y >= 0 && y < p.V && zy == m ? y : -1);
   }
   p.lse[i] = fmaf(m, p.inv_tau, ls);
   p.logp[i] = y >= 0 && y < p.V ? (zy - m) * p.inv_tau - ls : 0.f;
