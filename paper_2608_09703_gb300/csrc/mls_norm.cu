@@ -360,7 +360,13 @@ __global__ void __launch_bounds__(32 * kColWarps) norm_cols_sum_kernel(const Nor
 }
 
 // ------------------------------------------------------------------ wide rows
+// A lane adds d / 32 values, a thread of the column sums T / splits rows, with no bound on either but
+// 32 bits: a few at a time in fp32, and those in two words (one fp32 chain of 2^17 equal squares was
+// off by 6e-4).
 constexpr int kWarps = 4;
+
+// A row's sum from the lanes', in every lane.
+__device__ __forceinline__ float wide_sum(Pair v) { return __shfl_sync(0xffffffffu, pair_float(warp_sum_pair(v)), 0); }
 
 template <typename E>
 __global__ void __launch_bounds__(32 * kWarps) norm_fwd_wide_kernel(const NormParams p) {
@@ -373,19 +379,24 @@ __global__ void __launch_bounds__(32 * kWarps) norm_fwd_wide_kernel(const NormPa
   const E* bias = static_cast<const E*>(p.bias);
   E* y = static_cast<E*>(p.y) + t * p.d;
   const float inv_d = 1.0f / static_cast<float>(p.d);
-  float s = 0.f, q = 0.f, f[N];
+  float f[N];
+  Pair s = {0.f, 0.f}, q = {0.f, 0.f};
   for (int k = lane * N; k < p.d; k += 32 * N) {
     Vec<E>::unpack(ld16(x + k), f);
+    float some = 0.f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) s += f[i];
+    for (int i = 0; i < N; ++i) some += f[i];
+    pair_add(s, some, 0.f);
   }
-  const float mu = warp_sum(s) * inv_d;
+  const float mu = wide_sum(s) * inv_d;
   for (int k = lane * N; k < p.d; k += 32 * N) {
     Vec<E>::unpack(ld16(x + k), f);
+    float some = 0.f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) q = fmaf(f[i] - mu, f[i] - mu, q);
+    for (int i = 0; i < N; ++i) some = fmaf(f[i] - mu, f[i] - mu, some);
+    pair_add(q, some, 0.f);
   }
-  const float r = 1.0f / sqrtf(warp_sum(q) * inv_d + p.eps);
+  const float r = 1.0f / sqrtf(wide_sum(q) * inv_d + p.eps);
   for (int k = lane * N; k < p.d; k += 32 * N) {
     float g[N], b[N];
     Vec<E>::unpack(ld16(x + k), f);
@@ -415,20 +426,23 @@ __global__ void __launch_bounds__(32 * kWarps) norm_bwd_wide_kernel(const NormPa
   const E* gain = static_cast<const E*>(p.gain);
   E* dx = static_cast<E*>(p.dx) + t * p.d;
   const float inv_d = 1.0f / static_cast<float>(p.d), mu = p.mean[t], r = p.rstd[t];
-  float a = 0.f, b = 0.f, f[N], h[N], g[N];
+  float f[N], h[N], g[N];
+  Pair sa = {0.f, 0.f}, sb = {0.f, 0.f};
   for (int k = lane * N; k < p.d; k += 32 * N) {
     Vec<E>::unpack(ld16(x + k), f);
     Vec<E>::unpack(ld16(dy + k), h);
     if (gain) Vec<E>::unpack(ld16(gain + k), g);
+    float some_a = 0.f, some_b = 0.f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const float hg = gain ? h[i] * g[i] : h[i];
-      a += hg;
-      b = fmaf(hg, (f[i] - mu) * r, b);
+      some_a += hg;
+      some_b = fmaf(hg, (f[i] - mu) * r, some_b);
     }
+    pair_add(sa, some_a, 0.f);
+    pair_add(sb, some_b, 0.f);
   }
-  a = warp_sum(a) * inv_d;
-  b = warp_sum(b) * inv_d;
+  const float a = wide_sum(sa) * inv_d, b = wide_sum(sb) * inv_d;
   for (int k = lane * N; k < p.d; k += 32 * N) {
     Vec<E>::unpack(ld16(x + k), f);
     Vec<E>::unpack(ld16(dy + k), h);
@@ -442,8 +456,8 @@ __global__ void __launch_bounds__(32 * kWarps) norm_bwd_wide_kernel(const NormPa
   }
 }
 
-// Column sums: a thread owns a column (x), a block every splits-th row (y).
-constexpr int kColThreads = 128;
+// Column sums: a thread owns a column (x), a block every splits-th row (y), kColRows of them at a time.
+constexpr int kColThreads = 128, kColRows = 8;
 
 template <typename E>
 __global__ void __launch_bounds__(kColThreads) norm_cols_wide_kernel(const NormParams p) {
@@ -451,15 +465,36 @@ __global__ void __launch_bounds__(kColThreads) norm_cols_wide_kernel(const NormP
   if (c >= p.d) return;
   const E* x = static_cast<const E*>(p.x);
   const E* dy = static_cast<const E*>(p.dy);
-  float dg = 0.f, db = 0.f;
-  for (long long t = blockIdx.y; t < p.T; t += p.splits) {
+  Pair dg = {0.f, 0.f}, db = {0.f, 0.f};
+  long long t = blockIdx.y;
+  const long long step = p.splits;
+  for (; t + (kColRows - 1) * step < p.T; t += kColRows * step) {
+    float g[kColRows], v[kColRows], mu[kColRows], r[kColRows];
+#pragma unroll
+    for (int i = 0; i < kColRows; ++i) {  // every load before the first is used
+      const long long row = t + i * step;
+      g[i] = static_cast<float>(dy[row * p.d + c]);
+      v[i] = static_cast<float>(x[row * p.d + c]);
+      mu[i] = p.mean[row];
+      r[i] = p.rstd[row];
+    }
+    float some_g = 0.f, some_b = 0.f;
+#pragma unroll
+    for (int i = 0; i < kColRows; ++i) {
+      some_g = fmaf(g[i], (v[i] - mu[i]) * r[i], some_g);
+      some_b += g[i];
+    }
+    pair_add(dg, some_g, 0.f);
+    pair_add(db, some_b, 0.f);
+  }
+  for (; t < p.T; t += step) {
     const float g = static_cast<float>(dy[t * p.d + c]);
-    dg = fmaf(g, (static_cast<float>(x[t * p.d + c]) - p.mean[t]) * p.rstd[t], dg);
-    db += g;
+    pair_add(dg, g * ((static_cast<float>(x[t * p.d + c]) - p.mean[t]) * p.rstd[t]), 0.f);
+    pair_add(db, g, 0.f);
   }
   float* out = p.part + 2ll * p.d * blockIdx.y + c;
-  out[0] = dg;
-  out[p.d] = db;
+  out[0] = pair_float(dg);
+  out[p.d] = pair_float(db);
 }
 
 unsigned blocks_of(long long n, int per) { return static_cast<unsigned>((n + per - 1) / per); }
