@@ -230,7 +230,7 @@ int mls_spec_verify(const mls_spec_problem* p, const void* H_draft, const void* 
  * Backward, with dlogp = dL/dlogp:
  *   dL/dz = (dlogp / tau) (e_y - softmax(z / tau)),  dH_m = dL/dz W_m,  dW_m = dL/dz^T H_m
  * The [T, V] logits are recomputed, never stored; dL/dz is rounded to bf16 before the
- * last products, as in mls_head_loss_bwd.  teacher, alpha and w of `p` are not used,
+ * last products, as in mls_head_loss_bwd.  teacher, alpha and w of `p` are not read,
  * in_dtype is MLS_BF16 (MLS_ERR_UNSUPPORTED otherwise: products of fp32 storage would
  * go through tf32, whose errors a ratio exp(logp - old_logp) turns into gradients).
  * H and W are finite: an infinity or NaN in a row of H, of a token left out too, would

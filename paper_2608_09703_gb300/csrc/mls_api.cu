@@ -870,25 +870,34 @@ LogpPlan logp_plan(const mls_problem* p, int pairs, int gemm_pairs) {
   if (fwd > lp.total) lp.total = align_up(fwd);
   return lp;
 }
-int logp_validate(const mls_problem* p) {
-  const int rc = validate(p);
+// Sets q to the problem without the loss's fields, which may hold anything here.
+int logp_validate(const mls_problem* p, mls_problem& q) {
+  if (!p) return MLS_ERR_ARG;
+  q = *p;
+  q.teacher = 0;
+  q.alpha = 0.f;
+  q.w = nullptr;
+  const int rc = validate(&q);
   if (rc) return rc;
-  return p->in_dtype == MLS_BF16 ? MLS_OK : MLS_ERR_UNSUPPORTED;
+  return q.in_dtype == MLS_BF16 ? MLS_OK : MLS_ERR_UNSUPPORTED;
 }
 }  // namespace
 
 extern "C" size_t mls_logp_workspace_size(const mls_problem* p) {
-  if (logp_validate(p) != MLS_OK) return 0;
+  mls_problem q;
+  if (logp_validate(p, q) != MLS_OK) return 0;
   int head = 0, gemm = 0;
   current_pairs(head, gemm);
-  return logp_plan(p, head, gemm).total;
+  return logp_plan(&q, head, gemm).total;
 }
 
 namespace {
-int logp_fwd(const mls_problem* p, const void* const* H, const void* const* W, const int32_t* targets,
+int logp_fwd(const mls_problem* problem, const void* const* H, const void* const* W, const int32_t* targets,
              float* logp, float* lse, float* peak, void* ws, size_t ws_bytes, mls_stream_t stream) {
-  int rc = logp_validate(p);
+  mls_problem q;
+  int rc = logp_validate(problem, q);
   if (rc) return rc;
+  const mls_problem* p = &q;
   if (!H || !W || (p->T > 0 && (!targets || !logp || !lse))) return MLS_ERR_ARG;
   for (int m = 0; m < p->M; ++m) {
     if ((p->T > 0 && !H[m]) || !W[m]) return MLS_ERR_ARG;
@@ -927,11 +936,13 @@ int logp_fwd(const mls_problem* p, const void* const* H, const void* const* W, c
   return timed("logp_merge", s, [&] { return launch_logp_merge(mp, s); });
 }
 
-int logp_bwd(const mls_problem* p, const void* const* H, const void* const* W, const int32_t* targets,
+int logp_bwd(const mls_problem* problem, const void* const* H, const void* const* W, const int32_t* targets,
              const float* lse, const float* peak, const float* dlogp, void* const* dH, void* const* dW,
              void* ws, size_t ws_bytes, mls_stream_t stream) {
-  int rc = logp_validate(p);
+  mls_problem q;
+  int rc = logp_validate(problem, q);
   if (rc) return rc;
+  const mls_problem* p = &q;
   if (!H || !W || !dH || !dW || (p->T > 0 && (!targets || !lse || !dlogp))) return MLS_ERR_ARG;
   for (int m = 0; m < p->M; ++m) {
     if ((p->T > 0 && (!H[m] || !dH[m])) || !W[m] || !dW[m]) return MLS_ERR_ARG;
