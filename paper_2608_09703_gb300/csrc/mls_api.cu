@@ -1338,7 +1338,6 @@ extern "C" int mls_layer_norm_fwd(int64_t T, int32_t d, int32_t in_dtype, float 
   np.y = y;
   np.mean = mean;
   np.rstd = rstd;
-  np.sms = dev->sms;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   return timed("norm_fwd", s, [&] { return launch_norm_fwd(np, in_dtype == MLS_FP32, s); });
 }
@@ -1380,7 +1379,6 @@ extern "C" int mls_layer_norm_bwd(int64_t T, int32_t d, int32_t in_dtype, const 
   np.dx = dx;
   np.dgain = dgain;
   np.dbias = dbias;
-  np.sms = dev->sms;
   np.splits = norm_splits(T, d, in_dtype == MLS_FP32, dev->sms);
   if (dgain || dbias) {
     if (!ws || (reinterpret_cast<uintptr_t>(ws) % kAlign) != 0 ||

@@ -470,7 +470,6 @@ struct NormParams {
   float *dgain, *dbias;          // [d] or null
   float* part;                   // [splits][2][d]: shares of dgain and dbias
   int splits;
-  int sms;
 };
 int norm_splits(long long T, int d, bool fp32, int sms);  // shares of the column sums
 cudaError_t setup_norm_kernels();
