@@ -199,6 +199,26 @@ __device__ __forceinline__ float warp_sum3(const float (&s)[3], int lane) {
   return v;
 }
 
+// The same in two words: all tokens' sums of a short batch, which no further sum evens out.
+__device__ __forceinline__ Pair shfl_xor_pair(const Pair& a, int o) {
+  return {__shfl_xor_sync(0xffffffffu, a.hi, o), __shfl_xor_sync(0xffffffffu, a.lo, o)};
+}
+__device__ __forceinline__ Pair warp_sum3_pair(const float (&s)[3], int lane) {
+  const bool up = lane & 16, odd = lane & 8;
+  Pair a = {up ? s[2] : s[0], 0.f}, b = {up ? 0.f : s[1], 0.f};
+  pair_add(a, __shfl_xor_sync(0xffffffffu, up ? s[0] : s[2], 16), 0.f);
+  pair_add(b, __shfl_xor_sync(0xffffffffu, up ? s[1] : 0.f, 16), 0.f);
+  Pair v = odd ? b : a;
+  const Pair other = shfl_xor_pair(odd ? a : b, 8);
+  pair_add(v, other.hi, other.lo);
+#pragma unroll
+  for (int o = 4; o > 0; o >>= 1) {
+    const Pair w = shfl_xor_pair(v, o);
+    pair_add(v, w.hi, w.lo);
+  }
+  return v;
+}
+
 // A sub-model's loss and gradient of a thread's tokens kFrom to kTo - 1: adds to the sums s and writes.  The
 // tokens side by side, without a branch but for what is rare; the ones that do not count
 // are chosen away (a branch for each token and each of its cases: 92 in place of 79 us).
@@ -277,7 +297,8 @@ __global__ void __launch_bounds__(kOne ? kOneThreads : kThreads, kOne ? 1 : kRes
   __shared__ int ends[2];
   __shared__ int starts[kFewSeqs];
   __shared__ float advs[kFewSeqs];
-  __shared__ float shf[N / 32][3 * kMaxModels];
+  using Sum = std::conditional_t<kOne, Pair, float>;
+  __shared__ Sum shf[N / 32][3 * kMaxModels];
   __shared__ __align__(8) Pair shq[3 * kMaxModels];
   // The block's sub-models [m0, m1): one where the grid has a row for each.
   const bool split = gridDim.y > 1;
@@ -475,22 +496,29 @@ __global__ void __launch_bounds__(kOne ? kOneThreads : kThreads, kOne ? 1 : kRes
       }
     }
     in = next;
-    const float sum = some ? warp_sum3(s, lane) : 0.f;
+    Sum sum = {};
+    if constexpr (kOne) {
+      if (some) sum = warp_sum3_pair(s, lane);
+    } else {
+      if (some) sum = warp_sum3(s, lane);
+    }
     if (lane % 8 == 0 && lane < 24) shf[warp][3 * m + lane / 8] = sum;
   }
   __syncthreads();
   if (kOne && split) cluster_wait();  // the first block runs
   for (int q = 3 * m0 + warp; q < 3 * m1; q += N / 32) {  // a warp a quantity
-    const float v = warp_sum(lane < N / 32 ? shf[lane][q] : 0.f);
-    if (lane > 0) continue;
     if constexpr (kOne) {
+      static_assert(N == 32 * 32, "a lane for each warp");
+      const Pair v = warp_sum_pair(shf[lane][q]);
+      if (lane > 0) continue;
       if (split)
-        store_remote(map_to_rank(smem_u32(&shq[q]), 0), v, 0.f);
+        store_remote(map_to_rank(smem_u32(&shq[q]), 0), v.hi, v.lo);
       else
-        shq[q] = {v, 0.f};
-      if (p.diag) p.diag[q % 3 * p.M + q / 3] = v;
+        shq[q] = v;
+      if (p.diag) p.diag[q % 3 * p.M + q / 3] = pair_float(v);
     } else {
-      p.part[static_cast<long long>(q) * gridDim.x + blockIdx.x] = v;
+      const float v = warp_sum(lane < N / 32 ? shf[lane][q] : 0.f);
+      if (lane == 0) p.part[static_cast<long long>(q) * gridDim.x + blockIdx.x] = v;
     }
   }
   if constexpr (kOne) {
