@@ -342,12 +342,19 @@ __global__ void __launch_bounds__(kOne ? kOneThreads : kThreads, kOne ? 1 : kRes
       if (lane == 0) ends[warp] = b;
     }
   }
-  // The offsets have to be sorted and within [0, T].
-  if (p.seq_start && blockIdx.x == 0 && blockIdx.y == 0)
-    for (int b = threadIdx.x; b <= B; b += N) {
+  // The offsets have to be sorted and within [0, T].  Every block looks at some: by one alone 200000
+  // of them took 150 us.
+  if (p.seq_start && blockIdx.y == 0) {
+    auto look = [&](auto b) {
       const int v = p.seq_start[b];
       if (v < 0 || v > p.T || (b > 0 && v < p.seq_start[b - 1])) atomicOr(p.status, kStatusBadSeq);
+    };
+    if constexpr (kOne) {
+      for (int b = threadIdx.x; b <= B; b += N) look(b);
+    } else {  // 32 bits here: 82 us in place of 73 for 4000001 tokens
+      for (long long b = static_cast<long long>(blockIdx.x) * N + threadIdx.x; b <= B; b += static_cast<long long>(gridDim.x) * N) look(b);
     }
+  }
   __syncthreads();
   int b0 = 0, b1 = 0;
   if (p.seq_start && all) {

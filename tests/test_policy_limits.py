@@ -2,6 +2,7 @@
 import ctypes
 
 import pytest
+import torch
 
 import paper_2608_09703_gb300 as mls
 from paper_2608_09703_gb300 import binding as B
@@ -43,3 +44,28 @@ def test_steps_stay_positive_up_to_the_limit():
             k = min(32, (hi - lo) // step)
             lo, hi = lo + k * step, min(hi, lo + k * step + step - 1)
         assert n + 1024 < 1 << 31  # the check of the offsets, a block's threads a step
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,n", [(3, 7), (3, 5000), (4096, 4096), (5000, 3), (5000, 70000), (70001, 1024), (70001, 300000)])
+def test_any_bad_offset_is_reported(T, n):
+    """Every offset is looked at, by whichever block: one alone that is out of order or range."""
+    g = torch.Generator(device="cuda").manual_seed(n)
+    start = torch.randint(0, T + 1, (n + 1,), generator=g, device="cuda").sort().values.int()
+    logp, adv = torch.zeros(1, T, device="cuda"), torch.ones(T, device="cuda")
+    y = torch.zeros(T, dtype=torch.int32, device="cuda")
+    op = mls.PolicyLoss(T, 10, B=n)
+    op(logp, logp, adv, y, seq_start=start)
+    assert mls.mls_get_status() == 0
+    for b in sorted({0, 1, n // 3, n // 2, n - 1, n, min(n, 1023), min(n, 1024), min(n, 4095), min(n, 4096)}):
+        for v in (-1, T + 1):
+            bad = start.clone()
+            bad[b] = v
+            op(logp, logp, adv, y, seq_start=bad)
+            assert mls.mls_get_status() == B.MLS_STATUS_BAD_SEQ, (b, v)
+    if n > 1:
+        bad = torch.arange(n + 1, device="cuda").clamp(max=T).int()
+        bad[n // 2], bad[n // 2 - 1] = 0, max(1, min(T, n // 2 - 1))
+        if n // 2 > 1:
+            op(logp, logp, adv, y, seq_start=bad)
+            assert mls.mls_get_status() == B.MLS_STATUS_BAD_SEQ
