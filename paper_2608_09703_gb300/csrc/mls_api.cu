@@ -1425,11 +1425,13 @@ PolicyPlan policy_plan(const mls_policy_problem* p) {
 
 // A bound as the sum of two floats; out[2]: an fp32 difference d with |d - out[0]| over
 // this is on the side that those two say.  Beyond it, |d| < 2 |out[0]| or d is further off
-// than its own rounding, so 2^-21 |out[0]| covers that (2^-24 |d|) and out[1].
+// than its own rounding, so 2^-21 |out[0]| covers that (2^-24 |d|) and out[1].  No difference is near
+// an infinite bound.
 void two_words(double v, float (&out)[3]) {
   out[0] = static_cast<float>(v);
-  out[1] = std::isfinite(v) ? static_cast<float>(v - static_cast<double>(out[0])) : 0.f;
-  out[2] = std::fabs(out[0]) * 0x1p-21f + 0x1p-126f;
+  const bool finite = std::isfinite(v);
+  out[1] = finite ? static_cast<float>(v - static_cast<double>(out[0])) : 0.f;
+  out[2] = finite ? std::fabs(out[0]) * 0x1p-21f + 0x1p-126f : -1.f;
 }
 }  // namespace
 

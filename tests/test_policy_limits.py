@@ -69,3 +69,29 @@ def test_any_bad_offset_is_reported(T, n):
         if n // 2 > 1:
             op(logp, logp, adv, y, seq_start=bad)
             assert mls.mls_get_status() == B.MLS_STATUS_BAD_SEQ
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [700, 70001])
+@pytest.mark.parametrize("low,high", [(1.0, float("inf")), (0.2, float("inf")), (3.0, 0.28)])
+def test_bounds_that_are_none(T, low, high):
+    """No ratio is past an infinite bound, an infinite ratio neither."""
+    g = torch.Generator(device="cuda").manual_seed(T)
+    old = torch.randn(1, T, generator=g, device="cuda")
+    logp = old + 2 * torch.randn(1, T, generator=g, device="cuda")
+    logp[0, :3], old[0, :3] = torch.tensor([3e38, -3e38, 100.0]), torch.tensor([-3e38, 3e38, 0.0])
+    adv = torch.randn(T, generator=g, device="cuda")
+    adv[:3] = torch.tensor([1.0, -1.0, 1.0])
+    y = torch.zeros(T, dtype=torch.int32, device="cuda")
+    op = mls.PolicyLoss(T, 10, clip_low=low, clip_high=high, agg="sum")
+    op(logp, old, adv, y)
+    r = torch.exp(logp.double() - old.double())[0]
+    hi, lo = 1 + float(torch.tensor(high)), max(0.0, 1 - float(torch.tensor(low)))
+    stop = ((adv > 0) & (r > hi)) | ((adv < 0) & (r < lo))
+    assert torch.equal(op.dlogp[0] == 0, stop | (r.float() == 0))
+    assert float(op.diag[2, 0]) == float(stop.sum())
+    on = ~stop & torch.isfinite(r.float()) & (r > 1e-30)
+    want = -r * adv.double()
+    tol = 2.0 ** -24 * ((logp - old).abs()[0].double() + 16)
+    assert bool(((op.dlogp[0].double() - want).abs() <= tol * want.abs())[on].all())
+    assert mls.mls_get_status() == 0
