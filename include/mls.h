@@ -281,7 +281,9 @@ int mls_head_logp_bwd_peak(const mls_problem* p, const void* const* H, const voi
  *                                          each may be NULL
  *   ws          device workspace of mls_layer_norm_workspace_size(T, d) bytes, 256-byte
  *               aligned; not used, and may be NULL, when dgain and dbias are NULL
- * Sums are fp32.  Outputs overlap inputs only where said.  d <= 2^28 (MLS_ERR_UNSUPPORTED
+ * Sums are fp32 (past 32768 bf16 or 16384 fp32 values a row, and of such rows' columns, in two
+ * fp32 words); a column's over the rows of a block, one after the other.  Outputs overlap inputs
+ * only where said.  d <= 2^28 (MLS_ERR_UNSUPPORTED
  * beyond).  eps >= 0; with eps = 0 a row of equal values gives NaN (0 / 0).  Asynchronous
  * on `stream`; returns 0 or a negative MLS_ERR_* code (nothing launched).  T = 0 reads no row.
  */
@@ -325,9 +327,9 @@ int mls_layer_norm_bwd(int64_t T, int32_t d, int32_t in_dtype, const void* x, co
  *   dlogp           device, fp32 [M, T] or NULL: grad_scale dloss/dlogp, every entry
  *                   written (0 for a token that does not count).  May be the buffer logp.
  *   ws              device workspace of mls_policy_workspace_size(p) bytes, 256-byte aligned
- * A ratio is compared with its bound as if in 64 bits (the fp32 inputs taken as
- * exact, the bounds 1 - clip_low and 1 + clip_high as their fp32 parameters say);
- * one exactly on a bound is not stopped.
+ * A ratio is compared with its bound through its logarithm, the fp32 inputs taken as exact and
+ * the bounds 1 - clip_low and 1 + clip_high as their fp32 parameters say: logp - old_logp against
+ * the bound's logarithm to 2^-47 of it.  One exactly on a bound is not stopped.
  * Asynchronous; returns 0 or a negative MLS_ERR_* code (nothing launched).
  */
 #define MLS_POLICY_MAX_SEQS (1 << 30)
@@ -362,10 +364,11 @@ int mls_policy_loss(const mls_policy_problem* p, const float* logp, const float*
  *   max_norm  > 0; infinite: only the norm is computed
  *   stats  device, fp32 [2]: norm and c
  *   ws     device workspace of mls_grad_clip_workspace_size(n) bytes, 256-byte aligned
- * The sum is taken in 64 bits (fp32 over 32 values at a time where that loses
- * nothing): no square overflows or vanishes, and c and g are right even where norm
- * itself is past the largest fp32 value and reads as infinite.  A NaN among the gradients makes norm,
- * c and so every gradient NaN; an infinity among them makes norm infinite, c 0, and itself NaN.
+ * The sum is taken in fp32 over 32 values at a time, in two fp32 words over a block's and in
+ * 64 bits over all; norm and c are rounded once.  No square overflows or vanishes, and c and g
+ * are right even where norm itself is past the largest fp32 value and reads as infinite.  A NaN
+ * among the gradients makes norm, c and so every gradient NaN; an infinity among them makes norm
+ * infinite, c 0, and itself NaN.
  * The arrays g, numel and dtype are read during the call only.  At most
  * MLS_CLIP_MAX_TENSORS tensors (MLS_ERR_UNSUPPORTED).
  * Asynchronous; returns 0 or a negative MLS_ERR_* code (nothing launched).

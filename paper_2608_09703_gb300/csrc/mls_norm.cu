@@ -7,7 +7,7 @@
 //   dL/dgain = sum over tokens of g xh,  dL/dbias = sum over tokens of g
 // Bound by HBM: forward x and y, backward x, g and dx, each moved once.  The variance
 // is the mean of the squared deviations from the mean itself, so that a mean far
-// from 0 costs no digits.
+// from 0 costs the digits of its own rounding only, not those of its square.
 //   forward   a row stays in the registers of its 1 to 16 warps, at most 8 16-byte
 //             vectors a lane;
 //   backward  persistent blocks of 16 warps, W of them to a row, which copy rows ahead
@@ -15,7 +15,7 @@
 //             registers over all rows of the block (the widest rows: split over a cluster of
 //             two CTAs).  The blocks' sums are added in order by a second
 //             kernel, so results do not depend on timing;
-//   wider rows are read again from L2 instead, one warp a row.
+//   wider rows are read again from L2 instead, one warp a row, their sums in two words.
 #include "mls_device.cuh"
 #include "mls_kernels.h"
 #include "mls_vec.cuh"

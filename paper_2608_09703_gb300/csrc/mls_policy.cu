@@ -8,8 +8,9 @@
 // sequence b).  Which side of a clipping bound a token is on decides between a
 // gradient and none, so the comparison is made on D itself, and where D is near the
 // bound with what rounding the subtraction lost (its exact value is D + e) and the
-// bound, log(1 + clip_high) or log(1 - clip_low), in two fp32 words: as exact as in 64
-// bits.  K of a small x comes from its series, not from a difference of numbers near 1.
+// bound, log(1 + clip_high) or log(1 - clip_low), in two fp32 words: right for every D that is
+// not within 2^-47 of the bound.  K of a small x comes from its series, not from a difference
+// of numbers near 1.
 //
 // A block owns 1024 consecutive tokens: it finds each one's sequence, computes the
 // weights once and goes through the sub-models (or has one, see below).  How many
@@ -136,7 +137,7 @@ __global__ void __launch_bounds__(kThreads) policy_count_kernel(const __grid_con
     p.chunk_count[p.chunks + threadIdx.x] = 0;
 }
 
-// e^x - 1 - x and e^x - 1 for |x| < 1: with h = x / 2, whose series' remainder is under 2^-29 of
+// e^x - 1 - x and e^x - 1 for |x| < 1: with h = x / 2, whose series' remainder is under 2^-28.5 of
 // it, e^x - 1 - x = 2 (e^h - 1 - h) + (e^h - 1)^2, of terms that are never negative.
 constexpr float kSeries = 1.f;
 __device__ __forceinline__ void exp_excess(float x, float& excess, float& minus_one) {
