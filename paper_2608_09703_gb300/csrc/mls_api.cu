@@ -870,6 +870,15 @@ LogpPlan logp_plan(const mls_problem* p, int pairs, int gemm_pairs) {
   if (fwd > lp.total) lp.total = align_up(fwd);
   return lp;
 }
+// Every sub-model alike, in order; its reduction in parts as even as whole stages allow.
+void logp_parts(HeadParams& hp, int M) {
+  for (int m = 0; m < M; ++m) {
+    hp.order[m] = m;
+    const int n = static_cast<int>(ceil_div(hp.nk[m], kLogpPartStages));
+    hp.part_kb[m] = static_cast<int>(ceil_div(hp.nk[m], n));
+    hp.parts[m] = static_cast<int>(ceil_div(hp.nk[m], hp.part_kb[m]));
+  }
+}
 // Sets q to the problem without the loss's fields, which may hold anything here.
 int logp_validate(const mls_problem* p, mls_problem& q) {
   if (!p) return MLS_ERR_ARG;
@@ -914,7 +923,7 @@ int logp_fwd(const mls_problem* problem, const void* const* H, const void* const
   HeadParams hp;
   std::memset(&hp, 0, sizeof hp);
   fill_head_common(hp, p, pl, targets, dev->status);
-  for (int m = 0; m < p->M; ++m) hp.order[m] = m;
+  logp_parts(hp, p->M);
   if ((rc = encode_head_maps(hp, p, pl, H, W))) return rc;
   hp.split = pl.split;
   hp.part = static_cast<float*>(ws);
@@ -970,7 +979,7 @@ int logp_bwd(const mls_problem* problem, const void* const* H, const void* const
   HeadParams hp;
   std::memset(&hp, 0, sizeof hp);
   fill_head_common(hp, p, pl, targets, dev->status);
-  for (int m = 0; m < p->M; ++m) hp.order[m] = m;
+  logp_parts(hp, p->M);
   if ((rc = encode_head_maps(hp, p, pl, H, W))) return rc;
   hp.stats = lse;
   hp.dlogp = dlogp;

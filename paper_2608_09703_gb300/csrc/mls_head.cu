@@ -43,7 +43,8 @@ namespace {
 constexpr int kModeFwd = 0;
 constexpr int kModeBwd = 1;
 constexpr int kModeLogpFwd = 2;
-constexpr int kModeLogpBwd = 3;
+constexpr int kModeLogpBwd = 3;       // no reduction in parts
+constexpr int kModeLogpBwdParts = 4;
 constexpr int kStud = kMaxModels - 1;
 
 // Shared-memory map, offsets from the 1024-byte-aligned base.
@@ -135,7 +136,9 @@ __device__ __forceinline__ void head_producer(const HeadParams& p, uint32_t base
 }
 
 // ------------------------------------------------------------------ MMA issuer
-template <bool kTF32>
+// kParts: a tile's reduction in parts of p.part_kb[m] stages, each an accumulator of its own
+// that the epilogue adds up (see take_logits).
+template <bool kTF32, bool kParts>
 __device__ __forceinline__ void head_mma(const HeadParams& p, uint32_t base, uint32_t tmem,
                                          const volatile int* tiles, volatile int* abort_flag) {
   constexpr uint32_t kIdesc = make_idesc(2 * kHeadBM, kHeadBN, kTF32, false, false);
@@ -143,36 +146,39 @@ __device__ __forceinline__ void head_mma(const HeadParams& p, uint32_t base, uin
   int stage = 0;
   uint32_t phase = 0, acc = 0, acc_par = 0;
   bool ok = true;
+  // Stages [first, end) of a tile into the next accumulator.
+  auto reduce = [&](int first, int end) {
+    if (!mbar_wait(HeadSmem::acce(base, acc), acc_par ^ 1u, abort_flag, p.status)) return false;
+    tc_fence_after();
+    const uint32_t d = tmem + acc * kHeadBN;
+    for (int kb = first; kb < end; ++kb) {
+      if (!mbar_wait(HeadSmem::full(base, stage), phase, abort_flag, p.status)) return false;
+      tc_fence_after();
+      const uint64_t ad = make_sdesc(base + HeadSmem::kA + stage * kHeadABytes, 16);
+      const uint64_t bd = make_sdesc(base + HeadSmem::kB + stage * kHeadBBytes, 16);
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk)  // 4 x 32 bytes of K per stage
+        mma_issue_pair<kTF32>(d, ad + 2u * kk, bd + 2u * kk, kIdesc, kb != first || kk != 0);
+      mma_commit_pair(HeadSmem::empty(base, stage), kBoth);
+      if (++stage == kHeadStages) {
+        stage = 0;
+        phase ^= 1u;
+      }
+    }
+    mma_commit_pair(HeadSmem::accf(base, acc), kBoth);
+    acc ^= 1u;
+    if (acc == 0) acc_par ^= 1u;
+    return true;
+  };
   for (int vt = tiles[0]; ok && vt < tiles[1]; vt += tiles[2]) {
     for (int u = 0; ok && u < p.M; ++u) {
-      const int m = p.order[u];
-      if (!mbar_wait(HeadSmem::acce(base, acc), acc_par ^ 1u, abort_flag, p.status)) {
-        ok = false;
-        break;
+      const int m = p.order[u], nk = p.nk[m];
+      if constexpr (kParts) {
+        const int per = p.part_kb[m];
+        for (int kb = 0; ok && kb < nk; kb += per) ok = reduce(kb, kb + per < nk ? kb + per : nk);
+      } else {
+        ok = reduce(0, nk);
       }
-      tc_fence_after();
-      const uint32_t d = tmem + acc * kHeadBN;
-      for (int kb = 0; kb < p.nk[m]; ++kb) {
-        if (!mbar_wait(HeadSmem::full(base, stage), phase, abort_flag, p.status)) {
-          ok = false;
-          break;
-        }
-        tc_fence_after();
-        const uint64_t ad = make_sdesc(base + HeadSmem::kA + stage * kHeadABytes, 16);
-        const uint64_t bd = make_sdesc(base + HeadSmem::kB + stage * kHeadBBytes, 16);
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk)  // 4 x 32 bytes of K per stage
-          mma_issue_pair<kTF32>(d, ad + 2u * kk, bd + 2u * kk, kIdesc, (kb | kk) != 0);
-        mma_commit_pair(HeadSmem::empty(base, stage), kBoth);
-        if (++stage == kHeadStages) {
-          stage = 0;
-          phase ^= 1u;
-        }
-      }
-      if (!ok) break;
-      mma_commit_pair(HeadSmem::accf(base, acc), kBoth);
-      acc ^= 1u;
-      if (acc == 0) acc_par ^= 1u;
     }
   }
   // Every MMA this thread issued has finished before TMEM is released.
@@ -673,6 +679,31 @@ __device__ __forceinline__ void logp_release(uint32_t base, uint32_t& acc, uint3
 // before they compute: 32 columns at a time, read as they were needed, a tile took 6360
 // cycles of which the MMAs of d = 512 filled 4096.
 
+// A thread's 128 logits of a tile, from the accumulators of its `parts` parts of the reduction: the
+// tensor cores' additions truncate, which leans a sum to 0 by some 6e-10 of its terms' sizes for
+// each value of d (a logsumexp of 14 by 5e-5 at d = 8192).  These additions round, so what is left
+// is that of a part.  False if a wait ran out.
+__device__ __forceinline__ bool take_logits(const HeadParams& p, uint32_t base, uint32_t tl, int parts,
+                                            uint32_t& acc, uint32_t& acc_par, int lane,
+                                            volatile int* abort_flag, float (&v)[128]) {
+  if (!epi_acquire(p, base, acc, acc_par, abort_flag)) return false;
+  tmem_ld128(tl + acc * kHeadBN, v);
+  logp_release(base, acc, acc_par, lane);
+#pragma unroll 1
+  for (int part = 1; part < parts; ++part) {
+    if (!epi_acquire(p, base, acc, acc_par, abort_flag)) return false;
+#pragma unroll
+    for (int ch = 0; ch < 16; ++ch) {
+      float w[8];
+      tmem_ld8(tl + acc * kHeadBN + ch * 8, w);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[ch * 8 + i] += w[i];
+    }
+    logp_release(base, acc, acc_par, lane);
+  }
+  return true;
+}
+
 // One sub-model's tile: running maximum m of z, s = sum of 2^((z - m) Lt).  The maximum is
 // taken off before the product, so that its own term is 1 exactly and a token with nearly all
 // of the mass is left with what the others add to that; z Lt - (m Lt rounded) gave all terms a
@@ -742,13 +773,11 @@ __device__ __forceinline__ void logp_fwd_epilogue(const HeadParams& p, uint32_t 
 #pragma unroll
     for (int j = 0; j < kMaxModels; ++j) {
       if (j < p.M && !aborted) {
-        if (!epi_acquire(p, base, acc, acc_par, abort_flag)) {
+        float v[128];
+        if (!take_logits(p, base, tl, p.parts[j], acc, acc_par, lane, abort_flag, v)) {
           aborted = true;
           break;
         }
-        float v[128];
-        tmem_ld128(tl + acc * kHeadBN, v);
-        logp_release(base, acc, acc_par, lane);
         if (nvalid == 128)
           logp_tile<false>(v, 128, yl, p.Ltau, m[j], s[j], zy[j]);
         else if (nvalid > 0)
@@ -790,12 +819,12 @@ __device__ __forceinline__ void logp_fwd_epilogue(const HeadParams& p, uint32_t 
 }
 
 // dL/dz of one tile: c (softmax(z / tau) - e_y), c = -dL/dlogp / tau, b = -logsumexp(z / tau) log2(e).
-// The target's own is at.x times c p plus at.y: (1, -c), or (0, -c (1 - p)) where 1 - p is known better
-// than p is here.  e^-lse has the error of lse's one word, up to |lse| 2^-24 (1e-6): nothing to a
+// The target's own is c p - c, or `at`, -c (1 - p), where 1 - p is known better than p is here (at is NaN
+// where it is not).  e^-lse has the error of lse's one word, up to |lse| 2^-24 (1e-6): nothing to a
 // token's share relative to itself, but all of 1 - p where the target has nearly all of the mass.
 template <bool kMasked>
 __device__ __forceinline__ void logp_grad_tile(const float (&v)[128], int nvalid, int yl, float Lt, float b,
-                                               float c, float2 at, const GOut& o, int gcol, int lane) {
+                                               float c, float at, const GOut& o, int gcol, int lane) {
   const F2 L2 = f2(Lt), b2 = f2(b), c2 = f2(c);
 #pragma unroll
   for (int ch = 0; ch < 4; ++ch) {
@@ -815,7 +844,7 @@ __device__ __forceinline__ void logp_grad_tile(const float (&v)[128], int nvalid
     if (static_cast<unsigned>(r) < 32u) {
 #pragma unroll
       for (int i = 0; i < 32; ++i)
-        if (i == r) g[i] = fmaf(g[i], at.x, at.y);
+        if (i == r) g[i] = isnan(at) ? g[i] - c : at;
     }
     // A token without a gradient: nothing, also where its logits overflowed (0 times a NaN).
     if (c == 0.f) {
@@ -826,6 +855,7 @@ __device__ __forceinline__ void logp_grad_tile(const float (&v)[128], int nvalid
   }
 }
 
+template <bool kParts>
 __device__ __forceinline__ void logp_bwd_epilogue(const HeadParams& p, uint32_t base, uint32_t tmem,
                                                   int row_base, const volatile int* tiles, int warp, int lane,
                                                   volatile int* abort_flag) {
@@ -840,17 +870,16 @@ __device__ __forceinline__ void logp_bwd_epilogue(const HeadParams& p, uint32_t 
   const uint32_t stage = base + HeadSmem::kStage + static_cast<uint32_t>(warp) * 2 * kHeadStageChunk;
   const int row0 = row_base + quad * 32;
   const long long MT = static_cast<long long>(p.M) * p.T;
-  float c[kMaxModels], b[kMaxModels];
-  float2 at[kMaxModels];
+  float c[kMaxModels], b[kMaxModels], at[kMaxModels];
 #pragma unroll
   for (int j = 0; j < kMaxModels; ++j) {
     const bool on = j < p.M && valid;
     const long long i = static_cast<long long>(j) * p.T + row;
     c[j] = on ? p.neg_inv_tau * p.dlogp[i] : 0.f;
-    at[j] = make_float2(1.f, -c[j]);
+    at[j] = NAN;
     if (on && p.peak && __float_as_int(p.peak[MT + i]) == y) {
       const float others = p.peak[i];
-      at[j] = make_float2(0.f, -c[j] * (others / (1.f + others)));
+      at[j] = -c[j] * (others / (1.f + others));
     }
     b[j] = j < p.M && row_ok ? -__ldg(p.stats + i) * p.L1 : 0.f;
   }
@@ -864,14 +893,12 @@ __device__ __forceinline__ void logp_bwd_epilogue(const HeadParams& p, uint32_t 
 #pragma unroll
     for (int j = 0; j < kMaxModels; ++j) {
       if (j < p.M && !aborted) {
-        if (!epi_acquire(p, base, acc, acc_par, abort_flag)) {
+        float v[128];
+        if (!take_logits(p, base, tl, kParts ? p.parts[j] : 1, acc, acc_par, lane, abort_flag, v)) {
           aborted = true;
           break;
         }
         const GOut o{&p.mapG[j], stage, &nchunks, row0};
-        float v[128];
-        tmem_ld128(tl + acc * kHeadBN, v);
-        logp_release(base, acc, acc_par, lane);
         if (nvalid == 128)
           logp_grad_tile<false>(v, 128, yl, p.Ltau, b[j], c[j], at[j], o, gcol, lane);
         else
@@ -948,7 +975,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHeadThreads, 1)
         chain_trigger();
       }
     } else if (warp == kHeadEpiWarps + 1) {
-      if (lane == 0 && rank == 0) head_mma<kTF32>(p, base, tmem, tiles, abort_flag);
+      if (lane == 0 && rank == 0)
+        head_mma<kTF32, kMode == kModeLogpFwd || kMode == kModeLogpBwdParts>(p, base, tmem, tiles, abort_flag);
       __syncwarp();
     }
   } else {
@@ -959,8 +987,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHeadThreads, 1)
     else if constexpr (kMode == kModeLogpFwd)
       logp_fwd_epilogue(p, base, tmem, reinterpret_cast<float*>(gbase + HeadSmem::kStage), row_base, tiles,
                         warp, lane, abort_flag);
-    else if constexpr (kMode == kModeLogpBwd)
-      logp_bwd_epilogue(p, base, tmem, row_base, tiles, warp, lane, abort_flag);
+    else if constexpr (kMode == kModeLogpBwd || kMode == kModeLogpBwdParts)
+      logp_bwd_epilogue<kMode == kModeLogpBwdParts>(p, base, tmem, row_base, tiles, warp, lane, abort_flag);
     else
       bwd_epilogue<kTauOne, kTF32>(p, base, tmem, row_base, tiles, warp, lane, abort_flag);
   }
@@ -1048,12 +1076,16 @@ cudaError_t launch_logp_fwd(const HeadParams& p, cudaStream_t s) {
   head_kernel<kModeLogpFwd, false, true><<<grid, kHeadThreads, kHeadSmem, s>>>(p);
   return cudaGetLastError();
 }
+// Where no reduction has parts the backward has a kernel without the code for them: 256 tokens,
+// d = (128, 256), 16.9 -> 16.5 us.  The forward is as fast with it.
 cudaError_t launch_logp_bwd(const HeadParams& p, bool chained, cudaStream_t s) {
   const int grid = 2 * p.split.pairs();
   if (grid <= 0) return cudaSuccess;
-  if (chained)
-    return launch_chained(head_kernel<kModeLogpBwd, false, true>, dim3(grid), dim3(kHeadThreads), kHeadSmem, s, p);
-  head_kernel<kModeLogpBwd, false, true><<<grid, kHeadThreads, kHeadSmem, s>>>(p);
+  bool parts = false;
+  for (int m = 0; m < p.M; ++m) parts |= p.parts[m] > 1;
+  auto* kernel = parts ? head_kernel<kModeLogpBwdParts, false, true> : head_kernel<kModeLogpBwd, false, true>;
+  if (chained) return launch_chained(kernel, dim3(grid), dim3(kHeadThreads), kHeadSmem, s, p);
+  kernel<<<grid, kHeadThreads, kHeadSmem, s>>>(p);
   return cudaGetLastError();
 }
 cudaError_t setup_head_kernels() {
@@ -1061,7 +1093,8 @@ cudaError_t setup_head_kernels() {
   if (e != cudaSuccess) return e;
   if ((e = setup_mode<kModeBwd>()) != cudaSuccess) return e;
   if ((e = setup_logp_mode<kModeLogpFwd>()) != cudaSuccess) return e;
-  return setup_logp_mode<kModeLogpBwd>();
+  if ((e = setup_logp_mode<kModeLogpBwd>()) != cudaSuccess) return e;
+  return setup_logp_mode<kModeLogpBwdParts>();
 }
 
 }  // namespace mls

@@ -141,10 +141,14 @@ struct HeadParams {
   CUtensorMap mapG[kMaxModels];  // G_m [T, group] bf16 (fp32), box {64 bytes, 32}, 64B swizzle (TMA store)
   long long g_col0;              // vocabulary column of the group's first column
   // log-probabilities: `part` holds [S + extra][kLogpFields][M][T], `stats` [M][T]: logsumexp(z/tau)
+  int part_kb[kMaxModels];       // stages of a part of sub-model m's reduction
+  int parts[kMaxModels];         // parts of them: ceil(nk / part_kb)
   const float* dlogp;            // [M][T]
   const float* peak;             // [2][M][T] or null: see LogpMergeParams
   float neg_inv_tau;             // -1 / tau
 };
+// Stages of such a part at most: 1024 values of d, whose sums' truncation is 5e-7 of a log-probability.
+constexpr int kLogpPartStages = 16;
 enum LogpField { kLogpMax = 0, kLogpSum, kLogpSumLow, kLogpTarget, kLogpFields };  // the sum in two words
 
 // ------------------------------------------------------------------ GEMM kernels
