@@ -235,7 +235,8 @@ int mls_spec_verify(const mls_spec_problem* p, const void* H_draft, const void* 
  * go through tf32, whose errors a ratio exp(logp - old_logp) turns into gradients).
  * H and W are finite: an infinity or NaN in a row of H, of a token left out too, would
  * reach dW (0 times it is NaN).  Logits that overflow make that token's outputs infinite or
- * NaN; of one left out, or whose dlogp is 0, they reach no gradient.
+ * NaN; of one left out, or whose dlogp is 0, they reach no gradient.  Sums over d are the
+ * tensor cores' over up to 1280 values, which truncate, and rounded ones of those.
  *   targets    device, int32 [T]; outside [0, V): logp 0, no gradient (>= V also
  *              raises MLS_STATUS_BAD_TARGET), and its dlogp is not used
  *   logp, lse  device, fp32 [M, T]; the backward needs lse
@@ -246,8 +247,8 @@ int mls_spec_verify(const mls_spec_problem* p, const void* H_draft, const void* 
  *   peak       device, fp32 [2, M, T]: per row the sum over all tokens but one with the largest
  *              logit of exp((z - largest) / tau), and as the bits of an int32 the target if it
  *              has the largest logit, else -1.  The _peak forms write it and read it beside lse.
- *              With it 1 - p of such a target keeps its own digits in the backward (to 1e-5 of
- *              it, and 2^-20 at most); the plain forms, and other targets than the forward's,
+ *              With it 1 - p of such a target keeps its own digits in the backward (to some 1e-5
+ *              of it, and 2^-19 at most); the plain forms, and other targets than the forward's,
  *              have the rounding of lse in it, up to |lse| 2^-23.
  *   ws         device workspace of mls_logp_workspace_size(p) bytes
  */

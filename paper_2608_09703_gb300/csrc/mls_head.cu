@@ -43,8 +43,9 @@ namespace {
 constexpr int kModeFwd = 0;
 constexpr int kModeBwd = 1;
 constexpr int kModeLogpFwd = 2;
-constexpr int kModeLogpBwd = 3;       // no reduction in parts
-constexpr int kModeLogpBwdParts = 4;
+constexpr int kModeLogpBwd = 3;
+constexpr int kModeLogpFwdParts = 4;  // the same with reductions in parts (take_logits)
+constexpr int kModeLogpBwdParts = 5;
 constexpr int kStud = kMaxModels - 1;
 
 // Shared-memory map, offsets from the 1024-byte-aligned base.
@@ -681,7 +682,7 @@ __device__ __forceinline__ void logp_release(uint32_t base, uint32_t& acc, uint3
 
 // A thread's 128 logits of a tile, from the accumulators of its `parts` parts of the reduction: the
 // tensor cores' additions truncate, which leans a sum to 0 by some 6e-10 of its terms' sizes for
-// each value of d (a logsumexp of 14 by 5e-5 at d = 8192).  These additions round, so what is left
+// each value of d (a logsumexp of 11 by 5e-5 at d = 8192).  These additions round, so what is left
 // is that of a part.  False if a wait ran out.
 __device__ __forceinline__ bool take_logits(const HeadParams& p, uint32_t base, uint32_t tl, int parts,
                                             uint32_t& acc, uint32_t& acc_par, int lane,
@@ -748,6 +749,7 @@ __device__ __forceinline__ void logp_tile(float (&v)[128], int nvalid, int yl, f
   }
 }
 
+template <bool kParts>
 __device__ __forceinline__ void logp_fwd_epilogue(const HeadParams& p, uint32_t base, uint32_t tmem,
                                                   float* xchg, int row_base, const volatile int* tiles,
                                                   int warp, int lane, volatile int* abort_flag) {
@@ -774,7 +776,7 @@ __device__ __forceinline__ void logp_fwd_epilogue(const HeadParams& p, uint32_t 
     for (int j = 0; j < kMaxModels; ++j) {
       if (j < p.M && !aborted) {
         float v[128];
-        if (!take_logits(p, base, tl, p.parts[j], acc, acc_par, lane, abort_flag, v)) {
+        if (!take_logits(p, base, tl, kParts ? p.parts[j] : 1, acc, acc_par, lane, abort_flag, v)) {
           aborted = true;
           break;
         }
@@ -872,16 +874,15 @@ __device__ __forceinline__ void logp_bwd_epilogue(const HeadParams& p, uint32_t 
   const long long MT = static_cast<long long>(p.M) * p.T;
   float c[kMaxModels], b[kMaxModels], at[kMaxModels];
 #pragma unroll
-  for (int j = 0; j < kMaxModels; ++j) {
+  for (int j = 0; j < kMaxModels; ++j) {  // every load before the first is used
     const bool on = j < p.M && valid;
     const long long i = static_cast<long long>(j) * p.T + row;
-    c[j] = on ? p.neg_inv_tau * p.dlogp[i] : 0.f;
-    at[j] = NAN;
-    if (on && p.peak && __float_as_int(p.peak[MT + i]) == y) {
-      const float others = p.peak[i];
-      at[j] = -c[j] * (others / (1.f + others));
-    }
-    b[j] = j < p.M && row_ok ? -__ldg(p.stats + i) * p.L1 : 0.f;
+    const float dlogp = on ? p.dlogp[i] : 0.f, lse = on ? __ldg(p.stats + i) : 0.f;
+    const float others = on && p.peak ? p.peak[i] : 0.f;
+    const int top = on && p.peak ? __float_as_int(p.peak[MT + i]) : -1;
+    c[j] = p.neg_inv_tau * dlogp;
+    b[j] = -lse * p.L1;
+    at[j] = top == y ? -c[j] * (others / (1.f + others)) : NAN;
   }
   uint32_t acc = 0, acc_par = 0;
   bool aborted = false;
@@ -976,7 +977,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHeadThreads, 1)
       }
     } else if (warp == kHeadEpiWarps + 1) {
       if (lane == 0 && rank == 0)
-        head_mma<kTF32, kMode == kModeLogpFwd || kMode == kModeLogpBwdParts>(p, base, tmem, tiles, abort_flag);
+        head_mma<kTF32, kMode == kModeLogpFwdParts || kMode == kModeLogpBwdParts>(p, base, tmem, tiles, abort_flag);
       __syncwarp();
     }
   } else {
@@ -984,9 +985,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHeadThreads, 1)
     if constexpr (kMode == kModeFwd)
       fwd_epilogue<kTauOne>(p, base, tmem, reinterpret_cast<float*>(gbase + HeadSmem::kStage),
                             row_base, tiles, warp, lane, abort_flag);
-    else if constexpr (kMode == kModeLogpFwd)
-      logp_fwd_epilogue(p, base, tmem, reinterpret_cast<float*>(gbase + HeadSmem::kStage), row_base, tiles,
-                        warp, lane, abort_flag);
+    else if constexpr (kMode == kModeLogpFwd || kMode == kModeLogpFwdParts)
+      logp_fwd_epilogue<kMode == kModeLogpFwdParts>(p, base, tmem, reinterpret_cast<float*>(gbase + HeadSmem::kStage),
+                                                    row_base, tiles, warp, lane, abort_flag);
     else if constexpr (kMode == kModeLogpBwd || kMode == kModeLogpBwdParts)
       logp_bwd_epilogue<kMode == kModeLogpBwdParts>(p, base, tmem, row_base, tiles, warp, lane, abort_flag);
     else
@@ -1068,31 +1069,32 @@ cudaError_t launch_head_fwd(const HeadParams& p, bool tf32, bool tau_one, cudaSt
 cudaError_t launch_head_bwd(const HeadParams& p, bool tf32, bool tau_one, cudaStream_t s) {
   return launch_head<kModeBwd>(p, tf32, tau_one, s);
 }
-// The log-probability kernels serve every temperature with one exponential, so there is
-// one of each; `chained`: not the call's first kernel.
-cudaError_t launch_logp_fwd(const HeadParams& p, cudaStream_t s) {
-  const int grid = 2 * p.split.pairs();
-  if (grid <= 0) return cudaSuccess;
-  head_kernel<kModeLogpFwd, false, true><<<grid, kHeadThreads, kHeadSmem, s>>>(p);
-  return cudaGetLastError();
-}
-// Where no reduction has parts the backward has a kernel without the code for them: 256 tokens,
-// d = (128, 256), 16.9 -> 16.5 us.  The forward is as fast with it.
-cudaError_t launch_logp_bwd(const HeadParams& p, bool chained, cudaStream_t s) {
+// The log-probability kernels serve every temperature with one exponential.  Where no reduction has
+// parts they are ones without the code for them, which a short call would fetch: 256 tokens,
+// d = (128, 256), forward and backward 28.0 in place of 28.6 us.
+template <int kMode, int kModeParts>
+cudaError_t launch_logp(const HeadParams& p, bool chained, cudaStream_t s) {
   const int grid = 2 * p.split.pairs();
   if (grid <= 0) return cudaSuccess;
   bool parts = false;
   for (int m = 0; m < p.M; ++m) parts |= p.parts[m] > 1;
-  auto* kernel = parts ? head_kernel<kModeLogpBwdParts, false, true> : head_kernel<kModeLogpBwd, false, true>;
+  auto* kernel = parts ? head_kernel<kModeParts, false, true> : head_kernel<kMode, false, true>;
   if (chained) return launch_chained(kernel, dim3(grid), dim3(kHeadThreads), kHeadSmem, s, p);
   kernel<<<grid, kHeadThreads, kHeadSmem, s>>>(p);
   return cudaGetLastError();
+}
+cudaError_t launch_logp_fwd(const HeadParams& p, cudaStream_t s) {
+  return launch_logp<kModeLogpFwd, kModeLogpFwdParts>(p, false, s);
+}
+cudaError_t launch_logp_bwd(const HeadParams& p, bool chained, cudaStream_t s) {
+  return launch_logp<kModeLogpBwd, kModeLogpBwdParts>(p, chained, s);
 }
 cudaError_t setup_head_kernels() {
   cudaError_t e = setup_mode<kModeFwd>();
   if (e != cudaSuccess) return e;
   if ((e = setup_mode<kModeBwd>()) != cudaSuccess) return e;
   if ((e = setup_logp_mode<kModeLogpFwd>()) != cudaSuccess) return e;
+  if ((e = setup_logp_mode<kModeLogpFwdParts>()) != cudaSuccess) return e;
   if ((e = setup_logp_mode<kModeLogpBwd>()) != cudaSuccess) return e;
   return setup_logp_mode<kModeLogpBwdParts>();
 }

@@ -147,8 +147,8 @@ struct HeadParams {
   const float* peak;             // [2][M][T] or null: see LogpMergeParams
   float neg_inv_tau;             // -1 / tau
 };
-// Stages of such a part at most: 1024 values of d, whose sums' truncation is 5e-7 of a log-probability.
-constexpr int kLogpPartStages = 16;
+// Stages of such a part at most: 1280 values of d, whose sums' truncation is 7e-7 of a log-probability.
+constexpr int kLogpPartStages = 20;
 enum LogpField { kLogpMax = 0, kLogpSum, kLogpSumLow, kLogpTarget, kLogpFields };  // the sum in two words
 
 // ------------------------------------------------------------------ GEMM kernels
