@@ -647,7 +647,7 @@ class HeadLogp:
     """Log-probabilities of given tokens through a suite's heads, and the backward
     of a gradient per token, with outputs and workspace allocated once.  H[m]:
     [T, d_m], W[m]: [V, d_m] bf16; targets int32 [T]; dlogp fp32 [M, T]; dH and dW
-    bf16."""
+    bf16.  lse and peak go from the forward to the backward."""
 
     def __init__(self, d, T, V, tau=1.0, device="cuda", vocab_group=0):
         self.prob = Problem(d, T, V, tau=tau, vocab_group=vocab_group)
