@@ -6,9 +6,11 @@ of a part lose at most n / 2 2^-23 of it, half of that on average, whatever the 
 of all loses that for n = d / 16.)  The parts are added with rounding, 8 u for up to 8 of them."""
 import pytest
 import torch
+from test_finetune_streams import STALL, _child
 from test_logp import check, inputs
 
 import paper_2608_09703_gb300 as mls
+from paper_2608_09703_gb300 import binding as B
 
 U = 2.0 ** -24
 STEPS = 1280 // 16
@@ -70,3 +72,13 @@ def test_captured():
         assert all(torch.equal(a.view(torch.int32) if a.dtype == torch.float32 else a,
                                b.view(torch.int32) if b.dtype == torch.float32 else b) for a, b in zip(got, want))
     assert mls.mls_get_status() == 0
+
+
+@pytest.mark.gpu
+def test_a_stalled_stage_is_reported_and_the_context_survives():
+    """A wait that runs out between the parts of a reduction ends the kernel with its status."""
+    lines = [line.split() for line in _child(STALL.replace("64", "1352")).splitlines()]
+    stalled = [line for line in lines if line[:1] == ["STALLED"]]
+    assert [line[1] for line in stalled] == ["fwd", "bwd"]
+    assert all(int(line[2]) & B.MLS_STATUS_TIMEOUT for line in stalled)
+    assert ["CLEAN", "0", "True"] in lines
