@@ -64,8 +64,12 @@ enum {
   MLS_STATUS_DRAIN = 8,      /* after a timeout, a kernel's bounded shutdown wait for its own
                                 copies or MMAs also ran out: some may still have been in flight
                                 when it exited, so the CUDA context should not be trusted */
-  MLS_STATUS_BAD_SEQ = 16    /* mls_policy_loss: seq_start is not sorted or leaves [0, T]; the
-                                outputs of the tokens concerned mean nothing */
+  MLS_STATUS_BAD_SEQ = 16,   /* mls_policy_loss: seq_start is not sorted or leaves [0, T]; the
+                                outputs of the tokens concerned mean nothing.  The cache and tree
+                                calls: an entry that breaks their rules (see each), left out */
+  MLS_STATUS_NO_PAGES = 32   /* mls_cache_reserve, mls_cache_fork: not enough free pages, or a row of
+                                the table too short: the entries concerned got none.
+                                mls_cache_append: a token past its sequence's pages, not written */
 };
 
 /* Maximum number of sub-models per call. */
@@ -378,6 +382,144 @@ int mls_policy_loss(const mls_policy_problem* p, const float* logp, const float*
 size_t mls_grad_clip_workspace_size(int32_t n);
 int mls_grad_clip(int32_t n, void* const* g, const int64_t* numel, const int32_t* dtype,
                   float max_norm, float* stats, void* ws, size_t ws_bytes, mls_stream_t stream);
+
+/*
+ * Paged key/value cache of a suite's layers, for decoding with a nested draft and verifier
+ * (Sec. 2, "Speculative Decoding": they share it).  All memory is the caller's (device):
+ *   k, v       [layers, pages, kv_heads, page_size, head_dim] dtype, 16-byte aligned; a head's row
+ *              a multiple of 16 bytes
+ *   table      int32 [seqs, max_pages]: the pages of a sequence in order, -1 behind them
+ *   len, held  int32 [seqs]: tokens that a sequence holds, and its pages
+ *   refs       int32 [pages]: how many sequences a page belongs to; 0: it is free
+ *   free_bits  uint32 [ceil(pages / 32)]: bit page % 32 of word page / 32 set for a free page
+ * Position t of a sequence is slot t % page_size of page table[t / page_size].  The calls keep these
+ * arrays; a caller may read them, and write k, v and (all six together) the others between calls.
+ *
+ * A call works on n entries.  `seqs` (device, int32 [n], strictly increasing) says which sequences;
+ * NULL: sequences 0 .. n-1.  An entry that is not greater than all before it, or is no sequence of
+ * the cache, raises MLS_STATUS_BAD_SEQ and is left out; so is one whose other arguments break the
+ * rules below.  n <= seqs of the cache, and n <= MLS_CACHE_MAX_ENTRIES (MLS_ERR_UNSUPPORTED beyond).
+ * All calls are asynchronous on `stream`; calls on one cache must not overlap on the GPU.  Return 0
+ * or a negative MLS_ERR_* code (nothing launched).  n = 0 is a no-op.
+ *
+ *   mls_cache_reset    every page free, every sequence empty.  A new cache's first call.
+ *   mls_cache_reserve  pages for count[i] more tokens (device, int32 [n], >= 0) behind the len of
+ *       each entry, as far as it does not hold them: the lowest-numbered free pages, in the order of the
+ *       entries.  An entry gets its pages if they and those of all entries before it are there.
+ *   mls_cache_append   writes new tokens' keys and values behind len (which stays as it is).  start
+ *       (device, int32 [n + 1], not decreasing, within [0, N]): entry i has tokens start[i] .. start[i+1]-1
+ *       of k_new and v_new, which go to positions len, len + 1, ...; other tokens go nowhere.  layer >= 0:
+ *       k_new and v_new are [N, kv_heads, head_dim] of that layer; layer = -1: [layers, N, ...] of all.
+ *       token_ld, layer_ld: values between tokens and between layers (multiples of 16 bytes;
+ *       layer_ld not read for one layer).
+ *   mls_cache_compact  keeps tokens that were appended: keep[i] (device, int32 [n], >= 0) of them, those
+ *       at positions len + path[i][k], k < keep[i], which move together behind len; len grows by keep[i]
+ *       and pages past it are given back.  path (device, int32 [n, path_ld]): path[i][0] < path[i][1] < ...;
+ *       NULL: the first keep[i] as they lie.
+ *   mls_cache_fork     makes empty sequences dst[i] (strictly increasing; NULL: 0 .. n-1) copies of src[i]
+ *       (any; device, int32 [n]) as they were before the call: whole pages are shared, a partly filled
+ *       last one is copied into a page taken as above.  Tokens behind len are not copied.
+ *       ws: mls_cache_workspace_size() bytes.
+ *   mls_cache_free     gives back the pages of each entry (free where no other sequence has them) and empties it.
+ *   mls_cache_copy     copies page src[i] of `from` to page dst[i] of `to` (device, int32 [n]; any n), for caches of
+ *       the same layers, heads, page size and type; tables and counts are not touched.  dst holds no page
+ *       twice, and none that src holds if the caches share memory.
+ */
+#define MLS_CACHE_MAX_ENTRIES 8192
+typedef struct {
+  int32_t layers, pages;     /* >= 1; pages at most 2^26 */
+  int32_t page_size;         /* a power of two, 8 .. 256 */
+  int32_t kv_heads, head_dim;
+  int32_t dtype;             /* MLS_BF16 or MLS_FP32 */
+  int32_t seqs, max_pages;   /* >= 1; max_pages at most 2^20 */
+  void *k, *v;
+  int32_t *table, *len, *held, *refs;
+  uint32_t* free_bits;
+} mls_cache;
+
+size_t mls_cache_workspace_size(const mls_cache* c);
+int mls_cache_reset(const mls_cache* c, mls_stream_t stream);
+int mls_cache_reserve(const mls_cache* c, int32_t n, const int32_t* seqs, const int32_t* count, mls_stream_t stream);
+int mls_cache_append(const mls_cache* c, int32_t layer, int32_t n, const int32_t* seqs, const int32_t* start,
+                     int64_t N, const void* k_new, const void* v_new, int64_t token_ld, int64_t layer_ld,
+                     mls_stream_t stream);
+int mls_cache_compact(const mls_cache* c, int32_t n, const int32_t* seqs, const int32_t* keep, const int32_t* path,
+                      int32_t path_ld, mls_stream_t stream);
+int mls_cache_fork(const mls_cache* c, int32_t n, const int32_t* src, const int32_t* dst, void* ws, size_t ws_bytes,
+                   mls_stream_t stream);
+int mls_cache_free(const mls_cache* c, int32_t n, const int32_t* seqs, mls_stream_t stream);
+int mls_cache_copy(const mls_cache* from, const mls_cache* to, int32_t n, const int32_t* src, const int32_t* dst,
+                   mls_stream_t stream);
+
+/*
+ * Attention of new tokens over one layer of a paged cache that already holds their own keys and values
+ * (mls_cache_append).  Entry i's nodes are the tokens start[i] .. start[i+1]-1 of q; its node j lies at
+ * position len + j.  For node t and query head h, with key/value head h / (q_heads / kv_heads):
+ *   z_j = scale q . k_j,   lse = log sum_j exp(z_j),   out = sum_j exp(z_j - lse) v_j
+ * over the positions 0 .. len-1 and the nodes on the path from t up to its root, t included.
+ *   parents    device, int32 [N] or NULL: the parent's number within the entry, smaller than the node's
+ *              own; -1: a root; -2: the node takes no part (its out is 0, its lse -infinity, and it is
+ *              no part of another's path).  Others raise MLS_STATUS_BAD_SEQ and count as -2.  At most
+ *              MLS_TREE_MAX_NODES nodes an entry (MLS_STATUS_BAD_SEQ beyond: none takes part).
+ *              NULL: each node hangs below the one before it (a prompt, a chain of drafts, with one
+ *              node a decoding step); any number of nodes.
+ *   seqs       device, int32 [n], in any order, or NULL: sequences 0 .. n-1.  A sequence that is none of
+ *              the cache's, or whose len and nodes the table cannot hold, raises MLS_STATUS_BAD_SEQ
+ *              and its nodes take no part; a page that is none counts as zeros and raises it too.
+ *   start      device, int32 [n + 1], not decreasing, within [0, N].  Tokens in no entry keep their
+ *              out and lse.
+ *   q          device, [N, q_heads, head_dim] of the cache's type, q_ld values between tokens;
+ *              16-byte aligned, q_ld a multiple of 16 bytes
+ *   out        device, [N, q_heads, head_dim], dense, 16-byte aligned; lse: device, fp32 [N, q_heads]
+ *   ws         device workspace of mls_tree_attention_workspace_size() bytes, 256-byte aligned
+ * What a row does not attend to may hold anything, NaN and infinities included.  Sums are fp32; with a bf16
+ * cache exp(z_j - m), m a running maximum, is rounded to bf16 before it meets v_j.  head_dim <= 128
+ * (MLS_ERR_UNSUPPORTED beyond).  Asynchronous; 0 or a negative MLS_ERR_* code (nothing launched).
+ */
+#define MLS_TREE_MAX_NODES 256
+size_t mls_tree_attention_workspace_size(const mls_cache* c, int32_t n, int64_t N, int32_t q_heads);
+int mls_tree_attention(const mls_cache* c, int32_t layer, int32_t n, const int32_t* seqs, const int32_t* start,
+                       const int32_t* parents, int64_t N, int32_t q_heads, const void* q, int64_t q_ld, float scale,
+                       void* out, float* lse, void* ws, size_t ws_bytes, mls_stream_t stream);
+
+/*
+ * Acceptance of drafted trees against the target's probabilities from given random numbers:
+ * mls_spec_verify's rule for trees, and for probabilities that the caller has.  Entry i's nodes are the
+ * tokens start[i] .. start[i+1]-1; its node 0 is the token whose successors were drafted (accepted already),
+ * every other node's token was drafted to follow its parent's.  Row j of target and draft is the
+ * distribution of what follows node j.  At a node with rows p and q its children are tried in order:
+ *   r = p;  a child with token x is accepted iff  q(x) > 0  and  u[child][0] q(x) < r(x)
+ *   after each refusal r becomes max(0, r - q) over its sum (stays as it is where that is 0 everywhere)
+ * and the walk goes on at the child that is accepted; where none is, the next token is the smallest v with
+ * sum_{w <= v} r_w > u[node][1] sum_w r_w.
+ *   replace = 0: siblings were drawn without repetition: after each refusal x is taken out of q, which
+ *              is divided by the sum of what is left (q is 0 from then on where that is 0)
+ *   draft NULL: the children are given, not drawn: q(x) = 1, and a refusal takes x out of r (replace
+ *              not read)
+ * p and q are taken as they are for the first comparison at a node.  A token outside [0, V) is refused.
+ *   target, draft  device, fp32 [N, V], ld_target and ld_draft values between rows, values >= 0
+ *   tokens, parents  device, int32 [N]; parents as for mls_tree_attention, that of node 0 is -1; other
+ *              nodes with -1, and nodes with -2, are never reached
+ *   start      device, int32 [n + 1], not decreasing, within [0, N]
+ *   uniforms   device, fp32 [N, 2] in [0, 1): acceptance draw of the node, sampling draw if the walk ends there
+ *   n_path     device, int32 [n]: nodes on the accepted path, node 0 included
+ *   path       device, int32 [n, max_path]: their numbers in order, -1 behind them (what mls_cache_compact takes)
+ *   next_token device, int32 [n]; -1 where the row that is drawn from sums to 0
+ * An entry without nodes gets 0 and -1; so does one with more than max_path or MLS_TREE_MAX_NODES
+ * nodes or offsets that break the rule (MLS_STATUS_BAD_SEQ).  Sums of a row are kept in two fp32 words
+ * (some 45 bits), comparisons in 64 bits.  Asynchronous; 0 or a negative MLS_ERR_* code (nothing launched).
+ */
+typedef struct {
+  int32_t n;                 /* entries, >= 0 */
+  int64_t N, V;              /* nodes, >= 0; vocabulary, 1 .. 2^31 - 1 */
+  int64_t ld_target, ld_draft;
+  int32_t replace;
+  int32_t max_path;          /* 1 .. MLS_TREE_MAX_NODES */
+} mls_tree_problem;
+
+int mls_tree_verify(const mls_tree_problem* p, const float* target, const float* draft, const int32_t* tokens,
+                    const int32_t* parents, const int32_t* start, const float* uniforms, int32_t* n_path,
+                    int32_t* path, int32_t* next_token, mls_stream_t stream);
 
 /*
  * Synchronises `stream`, then returns the status bits (MLS_STATUS_*) recorded by

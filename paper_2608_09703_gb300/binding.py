@@ -24,11 +24,13 @@ MLS_OK = 0
 MLS_ERR_ARG, MLS_ERR_ALIGN, MLS_ERR_UNSUPPORTED = -1, -2, -3
 MLS_ERR_WORKSPACE, MLS_ERR_CUDA, MLS_ERR_DEVICE = -4, -5, -6
 MLS_STATUS_BAD_TARGET, MLS_STATUS_TIMEOUT, MLS_STATUS_CHECK, MLS_STATUS_DRAIN = 1, 2, 4, 8
-MLS_STATUS_BAD_SEQ = 16
+MLS_STATUS_BAD_SEQ, MLS_STATUS_NO_PAGES = 16, 32
 MLS_AGG_TOKEN_MEAN, MLS_AGG_SEQ_MEAN, MLS_AGG_SUM = 0, 1, 2
 MLS_CLIP_MAX_TENSORS = 16384
 MLS_POLICY_MAX_SEQS = 1 << 30
 MLS_MAX_MODELS = 4
+MLS_CACHE_MAX_ENTRIES = 8192
+MLS_TREE_MAX_NODES = 256
 
 
 class MLSError(RuntimeError):
@@ -78,6 +80,24 @@ class mls_policy_problem(ctypes.Structure):
         ("agg", ctypes.c_int32),
         ("adv_per_seq", ctypes.c_int32),
         ("w", ctypes.POINTER(ctypes.c_float)),
+    ]
+
+
+class mls_cache(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int32) for f in ("layers", "pages", "page_size", "kv_heads", "head_dim", "dtype",
+                                              "seqs", "max_pages")] + \
+               [(f, ctypes.c_void_p) for f in ("k", "v", "table", "len", "held", "refs", "free_bits")]
+
+
+class mls_tree_problem(ctypes.Structure):
+    _fields_ = [
+        ("n", ctypes.c_int32),
+        ("N", ctypes.c_int64),
+        ("V", ctypes.c_int64),
+        ("ld_target", ctypes.c_int64),
+        ("ld_draft", ctypes.c_int64),
+        ("replace", ctypes.c_int32),
+        ("max_path", ctypes.c_int32),
     ]
 
 
@@ -152,6 +172,24 @@ def lib():
         L.mls_grad_clip_workspace_size.restype = sz
         L.mls_grad_clip.argtypes = [i32, vp, vp, vp, f32, vp, vp, sz, vp]
         L.mls_grad_clip.restype = ctypes.c_int
+        CP = ctypes.POINTER(mls_cache)
+        L.mls_cache_workspace_size.argtypes = [CP]
+        L.mls_cache_workspace_size.restype = sz
+        L.mls_cache_reset.argtypes = [CP, vp]
+        L.mls_cache_reserve.argtypes = [CP, i32, vp, vp, vp]
+        L.mls_cache_append.argtypes = [CP, i32, i32, vp, vp, i64, vp, vp, i64, i64, vp]
+        L.mls_cache_compact.argtypes = [CP, i32, vp, vp, vp, i32, vp]
+        L.mls_cache_fork.argtypes = [CP, i32, vp, vp, vp, sz, vp]
+        L.mls_cache_free.argtypes = [CP, i32, vp, vp]
+        L.mls_cache_copy.argtypes = [CP, CP, i32, vp, vp, vp]
+        for name in ("reset", "reserve", "append", "compact", "fork", "free", "copy"):
+            getattr(L, "mls_cache_" + name).restype = ctypes.c_int
+        L.mls_tree_attention_workspace_size.argtypes = [CP, i32, i64, i32]
+        L.mls_tree_attention_workspace_size.restype = sz
+        L.mls_tree_attention.argtypes = [CP, i32, i32, vp, vp, vp, i64, i32, vp, i64, f32, vp, vp, vp, sz, vp]
+        L.mls_tree_attention.restype = ctypes.c_int
+        L.mls_tree_verify.argtypes = [ctypes.POINTER(mls_tree_problem), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.mls_tree_verify.restype = ctypes.c_int
         L.mls_profile_enable.argtypes = [ctypes.c_int]
         L.mls_profile_enable.restype = ctypes.c_int
         L.mls_profile_read.argtypes = [ctypes.POINTER(mls_kernel_time), ctypes.c_int]
@@ -529,6 +567,143 @@ def mls_grad_clip(grads, max_norm: float, stats, ws, stream=None) -> None:
     _check(rc, "mls_grad_clip")
 
 
+def _expect_strided(name: str, t: Optional[torch.Tensor], dtype, shape, inner, like: int = -2) -> int:
+    """As _expect, for a tensor whose last dimensions have the strides `inner` and whose first ones
+    may have any that do not go back."""
+    if t is not None and t.dtype is dtype and t.shape == shape and t.numel():
+        st = t.stride()
+        if any(n > 1 and a != b for n, a, b in zip(shape[-len(inner):], st[-len(inner):], inner)):
+            raise ValueError(f"{name}: strides {st}, the last ones expected {tuple(inner)}")
+        if min(st[:-len(inner)], default=0) < 0:
+            raise ValueError(f"{name}: strides {st}")
+        dev = t.get_device()
+        if dev >= 0 and (dev == like or like == -2 and dev == torch.cuda.current_device()):
+            return dev
+        raise ValueError(f"{name}: on {t.device}, expected the current device, where the others are")
+    return _expect(name, t, dtype, shape, like)
+
+
+def _entries(c: mls_cache, seqs, n: int, dev: int) -> int:
+    if seqs is not None:
+        _expect("seqs", seqs, torch.int32, (n,), dev)
+    return _ptr(seqs)
+
+
+def mls_cache_workspace_size(c: mls_cache) -> int:
+    return int(lib().mls_cache_workspace_size(ctypes.byref(c)))
+
+
+def mls_cache_reset(c: mls_cache, stream=None) -> None:
+    """Every page free, every sequence empty (see include/mls.h, for all calls on a cache)."""
+    _check(lib().mls_cache_reset(ctypes.byref(c), _stream(stream)), "mls_cache_reset")
+
+
+def mls_cache_reserve(c: mls_cache, seqs, count, stream=None) -> None:
+    n = count.shape[0]
+    dev = _expect("count", count, torch.int32, (n,))
+    rc = lib().mls_cache_reserve(ctypes.byref(c), n, _entries(c, seqs, n, dev), _ptr(count), _stream(stream))
+    _check(rc, "mls_cache_reserve")
+
+
+def _token_stride(name: str, t: torch.Tensor) -> int:
+    """Values between tokens of t [..., N, heads, dim]."""
+    return t.stride(-3) if t.shape[-3] > 1 else t.shape[-2] * t.shape[-1]
+
+
+def mls_cache_append(c: mls_cache, layer: int, seqs, start, k_new, v_new, stream=None) -> None:
+    n, N = start.shape[0] - 1, k_new.shape[-3]
+    dt = torch.bfloat16 if c.dtype == MLS_BF16 else torch.float32
+    shape = (N, c.kv_heads, c.head_dim) if layer >= 0 else (c.layers, N, c.kv_heads, c.head_dim)
+    inner = (c.head_dim, 1)
+    dev = _expect_strided("k_new", k_new, dt, shape, inner)
+    _expect_strided("v_new", v_new, dt, shape, inner, dev)
+    _expect("start", start, torch.int32, (n + 1,), dev)
+    if k_new.numel() and k_new.stride() != v_new.stride():
+        raise ValueError(f"k_new, v_new: strides {k_new.stride()} and {v_new.stride()}")
+    rc = lib().mls_cache_append(ctypes.byref(c), layer, n, _entries(c, seqs, n, dev), _ptr(start), N, _ptr(k_new),
+                                _ptr(v_new), _token_stride("k_new", k_new),
+                                0 if layer >= 0 or c.layers == 1 else k_new.stride(0), _stream(stream))
+    _check(rc, "mls_cache_append")
+
+
+def mls_cache_compact(c: mls_cache, seqs, keep, path=None, stream=None) -> None:
+    n = keep.shape[0]
+    dev = _expect("keep", keep, torch.int32, (n,))
+    if path is not None:
+        _expect("path", path, torch.int32, (n, path.shape[1]), dev)
+    rc = lib().mls_cache_compact(ctypes.byref(c), n, _entries(c, seqs, n, dev), _ptr(keep), _ptr(path),
+                                 0 if path is None else path.shape[1], _stream(stream))
+    _check(rc, "mls_cache_compact")
+
+
+def mls_cache_fork(c: mls_cache, src, dst, ws, stream=None) -> None:
+    n = src.shape[0]
+    dev = _expect("src", src, torch.int32, (n,))
+    wsp, wsn = _ws_args(ws, dev)
+    rc = lib().mls_cache_fork(ctypes.byref(c), n, _ptr(src), _entries(c, dst, n, dev), wsp, wsn, _stream(stream))
+    _check(rc, "mls_cache_fork")
+
+
+def mls_cache_free(c: mls_cache, n: int, seqs, stream=None) -> None:
+    if seqs is not None:
+        _expect("seqs", seqs, torch.int32, (n,))
+    _check(lib().mls_cache_free(ctypes.byref(c), n, _ptr(seqs), _stream(stream)), "mls_cache_free")
+
+
+def mls_cache_copy(c: mls_cache, to: mls_cache, src, dst, stream=None) -> None:
+    n = src.shape[0]
+    dev = _expect("src", src, torch.int32, (n,))
+    _expect("dst", dst, torch.int32, (n,), dev)
+    rc = lib().mls_cache_copy(ctypes.byref(c), ctypes.byref(to), n, _ptr(src), _ptr(dst), _stream(stream))
+    _check(rc, "mls_cache_copy")
+
+
+def mls_tree_attention_workspace_size(c: mls_cache, n: int, N: int, q_heads: int) -> int:
+    return int(lib().mls_tree_attention_workspace_size(ctypes.byref(c), int(n), int(N), int(q_heads)))
+
+
+def mls_tree_attention(c: mls_cache, layer: int, seqs, start, parents, q, scale: float, out, lse, ws,
+                       stream=None) -> None:
+    """Attention of new tokens over a paged cache that holds their keys and values (see include/mls.h)."""
+    n, (N, heads, dim) = start.shape[0] - 1, q.shape
+    dt = torch.bfloat16 if c.dtype == MLS_BF16 else torch.float32
+    dev = _expect_strided("q", q, dt, (N, heads, c.head_dim), (dim, 1))
+    _expect("start", start, torch.int32, (n + 1,), dev)
+    if parents is not None:
+        _expect("parents", parents, torch.int32, (N,), dev)
+    _expect("out", out, dt, (N, heads, dim), dev)
+    _expect("lse", lse, torch.float32, (N, heads), dev)
+    wsp, wsn = _ws_args(ws, dev)
+    rc = lib().mls_tree_attention(ctypes.byref(c), layer, n, _entries(c, seqs, n, dev), _ptr(start), _ptr(parents),
+                                  N, heads, _ptr(q), _token_stride("q", q), float(scale), _ptr(out), _ptr(lse), wsp,
+                                  wsn, _stream(stream))
+    _check(rc, "mls_tree_attention")
+
+
+def _row_stride(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def mls_tree_verify(target, draft, tokens, parents, start, uniforms, n_path, path, next_token, replace: bool = True,
+                    stream=None) -> None:
+    """Acceptance of drafted trees from probabilities and given random numbers (see include/mls.h)."""
+    n, (N, V) = start.shape[0] - 1, target.shape
+    f32, i32 = torch.float32, torch.int32
+    dev = _expect_strided("target", target, f32, (N, V), (1,))
+    if draft is not None:
+        _expect_strided("draft", draft, f32, (N, V), (1,), dev)
+    for name, t, dt, shape in (("tokens", tokens, i32, (N,)), ("parents", parents, i32, (N,)),
+                               ("start", start, i32, (n + 1,)), ("uniforms", uniforms, f32, (N, 2)),
+                               ("n_path", n_path, i32, (n,)), ("path", path, i32, (n, path.shape[1])),
+                               ("next_token", next_token, i32, (n,))):
+        _expect(name, t, dt, shape, dev)
+    p = mls_tree_problem(n, N, V, _row_stride(target), V if draft is None else _row_stride(draft), int(bool(replace)),
+                         path.shape[1])
+    rc = lib().mls_tree_verify(ctypes.byref(p), _ptr(target), _ptr(draft), _ptr(tokens), _ptr(parents), _ptr(start),
+                               _ptr(uniforms), _ptr(n_path), _ptr(path), _ptr(next_token), _stream(stream))
+    _check(rc, "mls_tree_verify")
+
+
 def mls_head_loss_fwd_noalloc(prob: Problem, H, W, targets, loss, tok_loss, tok_diag, argmax,
                               stats, stream=None) -> None:
     """Forward with the library's built-in scratch instead of a workspace, for
@@ -809,3 +984,162 @@ class GradClip:
                                  ws.numel(), _stream(stream))
         _check(rc, "mls_grad_clip")
         return self.stats
+
+
+class PagedCache:
+    """Paged key/value cache of a suite's layers: k and v [layers, pages, kv_heads, page_size, head_dim]
+    (bf16 or fp32), the table of pages [seqs, max_pages], len and held [seqs], refs [pages], as include/mls.h
+    has them.  Entries are all sequences from the first on, or those of `seqs` (int32, strictly increasing,
+    on the device); what only the device can see goes to mls_get_status()."""
+
+    def __init__(self, layers, pages, page_size, kv_heads, head_dim, seqs, max_pages, dtype=torch.bfloat16,
+                 device="cuda", stream=None):
+        if dtype not in (torch.bfloat16, torch.float32):
+            raise TypeError(dtype)
+        sizes = [int(x) for x in (layers, pages, page_size, kv_heads, head_dim)] + \
+            [MLS_BF16 if dtype is torch.bfloat16 else MLS_FP32, int(seqs), int(max_pages)]
+        if max(sizes) >> 31:  # ctypes would cut it
+            raise ValueError(f"{sizes}: past 32 bits")
+        if min(sizes[:5] + sizes[6:]) < 1:
+            raise ValueError(f"{sizes}: sizes are at least 1")
+        dev, self.dtype = torch.device(device), dtype
+        self.k = torch.empty(layers, pages, kv_heads, page_size, head_dim, dtype=dtype, device=dev)
+        self.v = torch.empty_like(self.k)
+        self.home = _Home(self.k)
+        self.table = torch.empty(seqs, max_pages, dtype=torch.int32, device=dev)
+        self.len = torch.empty(seqs, dtype=torch.int32, device=dev)
+        self.held = torch.empty(seqs, dtype=torch.int32, device=dev)
+        self.refs = torch.empty(pages, dtype=torch.int32, device=dev)
+        self.free_bits = torch.empty((pages + 31) // 32, dtype=torch.int32, device=dev)
+        buffers = (self.k, self.v, self.table, self.len, self.held, self.refs, self.free_bits)
+        self.c = mls_cache(*sizes, *[t.data_ptr() for t in buffers])
+        self.ref = ctypes.byref(self.c)
+        self.seqs, self.layers = int(seqs), int(layers)
+        self.reset(stream)
+        self.ws = torch.empty(mls_cache_workspace_size(self.c), dtype=torch.uint8, device=dev)
+
+    def _seqs(self, seqs, n, dev):
+        if seqs is None:
+            return None
+        _expect("seqs", seqs, torch.int32, (n,), dev)
+        return seqs.data_ptr()
+
+    def reset(self, stream=None):
+        """Every page free, every sequence empty."""
+        self.home()
+        mls_cache_reset(self.c, stream)
+
+    def reserve(self, count, seqs=None, stream=None):
+        """Pages for count[i] more tokens of each entry."""
+        dev, n = self.home(), count.shape[0]
+        _expect("count", count, torch.int32, (n,), dev)
+        rc = lib().mls_cache_reserve(self.ref, n, self._seqs(seqs, n, dev), count.data_ptr(), _stream(stream))
+        _check(rc, "mls_cache_reserve")
+
+    def append(self, k, v, start, layer=None, seqs=None, stream=None):
+        """Writes new keys and values [layers, N, kv_heads, head_dim] (of one layer: [N, ...]) behind what the
+        entries hold; entry i has the tokens start[i] .. start[i + 1] - 1."""
+        self.home()
+        if layer is not None and not 0 <= layer < self.layers:
+            raise ValueError(f"layer {layer} of {self.layers}")
+        mls_cache_append(self.c, -1 if layer is None else layer, seqs, start, k, v, stream)
+
+    def compact(self, keep, path=None, seqs=None, stream=None):
+        """Keeps keep[i] appended tokens of each entry (those of path[i], or the first ones) and gives back
+        the pages behind them."""
+        dev, n = self.home(), keep.shape[0]
+        _expect("keep", keep, torch.int32, (n,), dev)
+        if path is not None:
+            _expect("path", path, torch.int32, (n, path.shape[1]), dev)
+        rc = lib().mls_cache_compact(self.ref, n, self._seqs(seqs, n, dev), keep.data_ptr(), _ptr(path),
+                                     0 if path is None else path.shape[1], _stream(stream))
+        _check(rc, "mls_cache_compact")
+
+    def fork(self, src, dst, stream=None):
+        """Makes the empty sequences dst copies of src, sharing whole pages."""
+        dev, n = self.home(), src.shape[0]
+        _expect("src", src, torch.int32, (n,), dev)
+        _expect("dst", dst, torch.int32, (n,), dev)
+        rc = lib().mls_cache_fork(self.ref, n, src.data_ptr(), dst.data_ptr(), self.ws.data_ptr(), self.ws.numel(),
+                                  _stream(stream))
+        _check(rc, "mls_cache_fork")
+
+    def free(self, seqs=None, stream=None):
+        """Gives back the pages of the entries (all sequences', if None) and empties them."""
+        dev = self.home()
+        n = self.seqs if seqs is None else seqs.shape[0]
+        _check(lib().mls_cache_free(self.ref, n, self._seqs(seqs, n, dev), _stream(stream)), "mls_cache_free")
+
+    def copy(self, src, dst, to=None, stream=None):
+        """Copies pages src to pages dst (of another cache of this geometry, if given)."""
+        self.home()
+        mls_cache_copy(self.c, self.c if to is None else to.c, src, dst, stream)
+
+
+class TreeAttention:
+    """Attention of N new tokens of S sequences over a PagedCache that holds their keys and values already:
+    q [N, q_heads, head_dim], start int32 [S + 1], parents int32 [N] (None: a chain), seqs int32 [S] (None:
+    sequences 0 .. S-1).  out and lse are allocated once; tokens behind start[S] keep theirs."""
+
+    def __init__(self, cache: PagedCache, S, N, q_heads, scale=None):
+        c, dev = cache.c, cache.k.device
+        self.cache, self.S, self.N = cache, int(S), int(N)
+        self.shape = (self.N, int(q_heads), c.head_dim)
+        self.scale = c.head_dim ** -0.5 if scale is None else float(scale)
+        if q_heads < 1 or q_heads % c.kv_heads:
+            raise ValueError(f"{q_heads} query heads for {c.kv_heads} key/value heads")
+        self.out = torch.zeros(self.shape, dtype=cache.dtype, device=dev)
+        self.lse = torch.zeros(self.shape[:2], dtype=torch.float32, device=dev)
+        size = mls_tree_attention_workspace_size(c, S, N, q_heads)
+        self.ws = torch.empty(max(size, 1), dtype=torch.uint8, device=dev)
+
+    def __call__(self, q, start, parents=None, layer=0, seqs=None, stream=None):
+        cache, i32 = self.cache, torch.int32
+        dev = cache.home()
+        _expect_strided("q", q, cache.dtype, self.shape, (self.shape[2], 1), dev)
+        _expect("start", start, i32, (self.S + 1,), dev)
+        if parents is not None:
+            _expect("parents", parents, i32, (self.N,), dev)
+        if seqs is not None:
+            _expect("seqs", seqs, i32, (self.S,), dev)
+        rc = lib().mls_tree_attention(cache.ref, layer, self.S, _ptr(seqs), start.data_ptr(), _ptr(parents), self.N,
+                                      self.shape[1], q.data_ptr(), _token_stride("q", q), self.scale,
+                                      self.out.data_ptr(), self.lse.data_ptr(), self.ws.data_ptr(), self.ws.numel(),
+                                      _stream(stream))
+        _check(rc, "mls_tree_attention")
+        return self.out, self.lse
+
+
+class TreeVerify:
+    """Acceptance of the drafted trees of S sequences, N nodes in all, from the target's (and the draft's)
+    probabilities [N, V] and given random numbers: tokens and parents int32 [N], start int32 [S + 1], uniforms
+    fp32 [N, 2].  Returns n_path [S], path [S, max_path] (as PagedCache.compact takes them) and next_token [S],
+    allocated once."""
+
+    def __init__(self, S, N, V, max_path=MLS_TREE_MAX_NODES, replace=True, device="cuda"):
+        dev = torch.device(device)
+        self.p = mls_tree_problem(int(S), int(N), int(V), int(V), int(V), int(bool(replace)), int(max_path))
+        if max(int(S), int(max_path)) >> 31:  # ctypes would cut it
+            raise ValueError(f"S = {S}, max_path = {max_path}: past 32 bits")
+        self.n_path = torch.empty(S, dtype=torch.int32, device=dev)
+        self.path = torch.empty(S, max_path, dtype=torch.int32, device=dev)
+        self.next_token = torch.empty(S, dtype=torch.int32, device=dev)
+        self.home = _Home(self.n_path)
+
+    def __call__(self, target, tokens, parents, start, uniforms, draft=None, stream=None):
+        p, i32, f32 = self.p, torch.int32, torch.float32
+        dev = self.home()
+        _expect_strided("target", target, f32, (p.N, p.V), (1,), dev)
+        if draft is not None:
+            _expect_strided("draft", draft, f32, (p.N, p.V), (1,), dev)
+            p.ld_draft = _row_stride(draft)
+        p.ld_target = _row_stride(target)
+        _expect("tokens", tokens, i32, (p.N,), dev)
+        _expect("parents", parents, i32, (p.N,), dev)
+        _expect("start", start, i32, (p.n + 1,), dev)
+        _expect("uniforms", uniforms, f32, (p.N, 2), dev)
+        rc = lib().mls_tree_verify(ctypes.byref(p), target.data_ptr(), _ptr(draft), tokens.data_ptr(),
+                                   parents.data_ptr(), start.data_ptr(), uniforms.data_ptr(), self.n_path.data_ptr(),
+                                   self.path.data_ptr(), self.next_token.data_ptr(), _stream(stream))
+        _check(rc, "mls_tree_verify")
+        return self.n_path, self.path, self.next_token

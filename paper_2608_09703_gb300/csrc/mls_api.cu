@@ -77,6 +77,8 @@ int device_state(DeviceState** out) {
       s.err = fail(MLS_ERR_CUDA, "junction kernel attributes", e);
     } else if ((e = setup_norm_kernels()) != cudaSuccess) {
       s.err = fail(MLS_ERR_CUDA, "norm kernel attributes", e);
+    } else if ((e = setup_cache_kernels()) != cudaSuccess) {
+      s.err = fail(MLS_ERR_CUDA, "cache kernel attributes", e);
     } else if ((s.gemm_pairs = gemm_max_active_pairs()) <= 0) {
       s.err = fail(MLS_ERR_CUDA, "gemm cluster occupancy");
     } else if ((s.head_pairs = head_max_active_pairs()) <= 0) {
@@ -1049,12 +1051,13 @@ extern "C" const char* mls_strerror(int code) {
     case MLS_STATUS_TIMEOUT: return "a pipeline wait timed out; outputs are invalid";
     case MLS_STATUS_BAD_TARGET | MLS_STATUS_TIMEOUT: return "target >= V and a pipeline timeout";
     case MLS_STATUS_CHECK: return "an internal invariant failed (checked build)";
-    case MLS_STATUS_BAD_SEQ: return "sequence offsets not sorted or outside the tokens";
+    case MLS_STATUS_BAD_SEQ: return "sequence offsets not sorted or outside the tokens, or an entry that breaks a call's rules";
+    case MLS_STATUS_NO_PAGES: return "not enough pages in the cache";
     case MLS_STATUS_DRAIN:
     case MLS_STATUS_TIMEOUT | MLS_STATUS_DRAIN:
       return "a pipeline timeout, and a shutdown wait ran out: the CUDA context is unreliable";
     default:
-      return code > 0 && code < 32 ? "several status bits are set (MLS_STATUS_* in mls.h)" : "unknown code";
+      return code > 0 && code < 64 ? "several status bits are set (MLS_STATUS_* in mls.h)" : "unknown code";
   }
 }
 
@@ -1803,4 +1806,287 @@ extern "C" int mls_spec_verify(const mls_spec_problem* p, const void* H_draft, c
   if (!p->greedy && (rc = timed("spec_rows", s, [&] { return launch_spec_rows(sp, s); })))
     return rc;
   return timed("spec_sample", s, [&] { return launch_spec_sample(sp, s); });
+}
+
+// ------------------------------------------------------------------ paged cache, tree attention, tree verify
+namespace {
+
+int cache_validate(const mls_cache* c) {
+  if (!c || c->layers < 1 || c->pages < 1 || c->kv_heads < 1 || c->head_dim < 1 || c->seqs < 1 || c->max_pages < 1)
+    return MLS_ERR_ARG;
+  if (c->dtype != MLS_BF16 && c->dtype != MLS_FP32) return MLS_ERR_ARG;
+  const long long row = static_cast<long long>(c->head_dim) * (c->dtype == MLS_BF16 ? 2 : 4);
+  const int ps = c->page_size;
+  if (ps < 8 || ps > 256 || (ps & (ps - 1)) || row % 16 || c->pages > (1 << 26) || c->max_pages > (1 << 20))
+    return MLS_ERR_UNSUPPORTED;
+  // A token's pieces over all layers, and a page's of one layer, are counted in 32 bits.
+  const long long token = 2 * (row / 16);
+  if (c->kv_heads > INT_MAX / token / c->layers || c->kv_heads > INT_MAX / token / ps) return MLS_ERR_UNSUPPORTED;
+  if (!c->k || !c->v || !c->table || !c->len || !c->held || !c->refs || !c->free_bits) return MLS_ERR_ARG;
+  if (!aligned16(c->k) || !aligned16(c->v) || !aligned4(c->table) || !aligned4(c->len) || !aligned4(c->held) ||
+      !aligned4(c->refs) || !aligned4(c->free_bits))
+    return MLS_ERR_ALIGN;
+  return MLS_OK;
+}
+
+CacheView cache_view(const mls_cache* c, const DeviceState* dev) {
+  CacheView v;
+  v.layers = c->layers;
+  v.pages = c->pages;
+  v.heads = c->kv_heads;
+  v.row = c->head_dim * (c->dtype == MLS_BF16 ? 2 : 4) / 16;
+  v.page_shift = 0;
+  while ((1 << v.page_shift) < c->page_size) ++v.page_shift;
+  v.seqs = c->seqs;
+  v.max_pages = c->max_pages;
+  v.k = static_cast<uint4*>(c->k);
+  v.v = static_cast<uint4*>(c->v);
+  v.table = c->table;
+  v.len = c->len;
+  v.held = c->held;
+  v.refs = c->refs;
+  v.free_bits = c->free_bits;
+  v.status = dev->status;
+  return v;
+}
+
+// The checks that the calls on entries share.
+int cache_entries(const mls_cache* c, int n, const int32_t* seqs) {
+  if (const int rc = cache_validate(c)) return rc;
+  if (n < 0 || n > c->seqs) return MLS_ERR_ARG;
+  if (n > MLS_CACHE_MAX_ENTRIES) return MLS_ERR_UNSUPPORTED;
+  if (!aligned4(seqs)) return MLS_ERR_ALIGN;
+  return MLS_OK;
+}
+static_assert(kCacheMaxEntries == MLS_CACHE_MAX_ENTRIES && kTreeMaxNodes == MLS_TREE_MAX_NODES, "as mls.h says");
+}  // namespace
+
+extern "C" size_t mls_cache_workspace_size(const mls_cache* c) {
+  if (cache_validate(c)) return 0;
+  const int n = c->seqs < kCacheMaxEntries ? c->seqs : kCacheMaxEntries;
+  return align_up(sizeof(int) * n) * 2;
+}
+
+extern "C" int mls_cache_reset(const mls_cache* c, mls_stream_t stream) {
+  int rc = cache_validate(c);
+  if (rc) return rc;
+  DeviceState* dev = nullptr;
+  if ((rc = device_state(&dev))) return rc;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  return timed("cache_reset", s, [&] { return launch_cache_reset(cache_view(c, dev), s); });
+}
+
+extern "C" int mls_cache_reserve(const mls_cache* c, int32_t n, const int32_t* seqs, const int32_t* count,
+                                 mls_stream_t stream) {
+  int rc = cache_entries(c, n, seqs);
+  if (rc) return rc;
+  if (n == 0) return MLS_OK;
+  if (!count) return MLS_ERR_ARG;
+  if (!aligned4(count)) return MLS_ERR_ALIGN;
+  DeviceState* dev = nullptr;
+  if ((rc = device_state(&dev))) return rc;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  return timed("cache_reserve", s, [&] { return launch_cache_reserve(cache_view(c, dev), n, seqs, count, s); });
+}
+
+extern "C" int mls_cache_append(const mls_cache* c, int32_t layer, int32_t n, const int32_t* seqs, const int32_t* start,
+                                int64_t N, const void* k_new, const void* v_new, int64_t token_ld, int64_t layer_ld,
+                                mls_stream_t stream) {
+  int rc = cache_entries(c, n, seqs);
+  if (rc) return rc;
+  if (layer < -1 || layer >= c->layers || N < 0 || N > INT_MAX) return MLS_ERR_ARG;
+  if (n == 0 || N == 0) return MLS_OK;
+  if (!start || !k_new || !v_new) return MLS_ERR_ARG;
+  const int width = c->dtype == MLS_BF16 ? 8 : 4;
+  const int64_t dense = static_cast<int64_t>(c->kv_heads) * c->head_dim;
+  // Strides so large that an address would pass 64 bits are no strides.
+  constexpr int64_t kMost = int64_t{1} << 40;
+  if (token_ld < dense || token_ld > kMost || (layer < 0 && (layer_ld < 0 || layer_ld > kMost))) return MLS_ERR_ARG;
+  if (token_ld % width || (layer < 0 && layer_ld % width) || !aligned16(k_new) || !aligned16(v_new) || !aligned4(start))
+    return MLS_ERR_ALIGN;
+  DeviceState* dev = nullptr;
+  if ((rc = device_state(&dev))) return rc;
+  CacheAppend a;
+  a.layer0 = layer < 0 ? 0 : layer;
+  a.layers = layer < 0 ? c->layers : 1;
+  a.n = n;
+  a.seqs = seqs;
+  a.start = start;
+  a.N = N;
+  a.k = static_cast<const uint4*>(k_new);
+  a.v = static_cast<const uint4*>(v_new);
+  a.token_ld = token_ld / width;
+  a.layer_ld = layer < 0 ? layer_ld / width : 0;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  return timed("cache_append", s, [&] { return launch_cache_append(cache_view(c, dev), a, s); });
+}
+
+extern "C" int mls_cache_compact(const mls_cache* c, int32_t n, const int32_t* seqs, const int32_t* keep,
+                                 const int32_t* path, int32_t path_ld, mls_stream_t stream) {
+  int rc = cache_entries(c, n, seqs);
+  if (rc) return rc;
+  if (path && path_ld < 1) return MLS_ERR_ARG;
+  if (n == 0) return MLS_OK;
+  if (!keep) return MLS_ERR_ARG;
+  if (!aligned4(keep) || !aligned4(path)) return MLS_ERR_ALIGN;
+  DeviceState* dev = nullptr;
+  if ((rc = device_state(&dev))) return rc;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  return timed("cache_compact", s, [&] {
+    return launch_cache_compact(cache_view(c, dev), n, seqs, keep, path, path_ld, dev->sms, s);
+  });
+}
+
+extern "C" int mls_cache_fork(const mls_cache* c, int32_t n, const int32_t* src, const int32_t* dst, void* ws,
+                              size_t ws_bytes, mls_stream_t stream) {
+  int rc = cache_entries(c, n, dst);
+  if (rc) return rc;
+  if (n == 0) return MLS_OK;
+  if (!src) return MLS_ERR_ARG;
+  if (!aligned4(src)) return MLS_ERR_ALIGN;
+  if (!ws || (reinterpret_cast<uintptr_t>(ws) % kAlign) != 0 || ws_bytes < mls_cache_workspace_size(c))
+    return MLS_ERR_WORKSPACE;
+  DeviceState* dev = nullptr;
+  if ((rc = device_state(&dev))) return rc;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  int* const fresh = static_cast<int*>(ws);
+  int* const length = fresh + align_up(sizeof(int) * n) / sizeof(int);
+  return timed("cache_fork", s, [&] {
+    return launch_cache_fork(cache_view(c, dev), n, src, dst, fresh, length, dev->sms, s);
+  });
+}
+
+extern "C" int mls_cache_free(const mls_cache* c, int32_t n, const int32_t* seqs, mls_stream_t stream) {
+  int rc = cache_entries(c, n, seqs);
+  if (rc) return rc;
+  if (n == 0) return MLS_OK;
+  DeviceState* dev = nullptr;
+  if ((rc = device_state(&dev))) return rc;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  return timed("cache_free", s, [&] { return launch_cache_free(cache_view(c, dev), n, seqs, s); });
+}
+
+extern "C" int mls_cache_copy(const mls_cache* from, const mls_cache* to, int32_t n, const int32_t* src,
+                              const int32_t* dst, mls_stream_t stream) {
+  int rc;
+  if ((rc = cache_validate(from)) || (rc = cache_validate(to))) return rc;
+  if (from->layers != to->layers || from->kv_heads != to->kv_heads || from->page_size != to->page_size ||
+      from->head_dim != to->head_dim || from->dtype != to->dtype || n < 0)
+    return MLS_ERR_ARG;
+  if (n == 0) return MLS_OK;
+  if (!src || !dst) return MLS_ERR_ARG;
+  if (!aligned4(src) || !aligned4(dst)) return MLS_ERR_ALIGN;
+  DeviceState* dev = nullptr;
+  if ((rc = device_state(&dev))) return rc;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  return timed("cache_copy", s, [&] {
+    return launch_cache_copy(cache_view(from, dev), cache_view(to, dev), n, src, dst, dev->sms, s);
+  });
+}
+
+namespace {
+
+int tree_validate(const mls_cache* c, int n, int64_t N, int q_heads) {
+  if (const int rc = cache_validate(c)) return rc;
+  if (n < 0 || N < 0 || N > INT_MAX || q_heads < 1 || q_heads % c->kv_heads) return MLS_ERR_ARG;
+  if (c->head_dim > 128) return MLS_ERR_UNSUPPORTED;
+  // Boxes of the tensor maps are numbered, and warps counted, in 32 bits.
+  if (static_cast<long long>(c->layers) * c->pages > INT_MAX / c->kv_heads || N * q_heads > INT_MAX / 64)
+    return MLS_ERR_UNSUPPORTED;
+  return MLS_OK;
+}
+}  // namespace
+
+extern "C" size_t mls_tree_attention_workspace_size(const mls_cache* c, int32_t n, int64_t N, int32_t q_heads) {
+  if (tree_validate(c, n, N, q_heads)) return 0;
+  const int splits = tree_fp32_splits(N, q_heads, current_sms());
+  return align_up(sizeof(float) * N * q_heads * splits * (c->head_dim + 4));
+}
+
+extern "C" int mls_tree_attention(const mls_cache* c, int32_t layer, int32_t n, const int32_t* seqs,
+                                  const int32_t* start, const int32_t* parents, int64_t N, int32_t q_heads,
+                                  const void* q, int64_t q_ld, float scale, void* out, float* lse, void* ws,
+                                  size_t ws_bytes, mls_stream_t stream) {
+  int rc = tree_validate(c, n, N, q_heads);
+  if (rc) return rc;
+  if (layer < 0 || layer >= c->layers || !std::isfinite(scale) || (!seqs && n > c->seqs)) return MLS_ERR_ARG;
+  if (n == 0 || N == 0) return MLS_OK;
+  if (!start || !q || !out || !lse) return MLS_ERR_ARG;
+  const int64_t dense = static_cast<int64_t>(q_heads) * c->head_dim;
+  if (q_ld < dense || q_ld > (int64_t{1} << 40)) return MLS_ERR_ARG;
+  if (q_ld % (c->dtype == MLS_BF16 ? 8 : 4) || !aligned16(q) || !aligned16(out) || !aligned4(lse) || !aligned4(seqs) ||
+      !aligned4(start) || !aligned4(parents))
+    return MLS_ERR_ALIGN;
+  if (!ws || (reinterpret_cast<uintptr_t>(ws) % kAlign) != 0 ||
+      ws_bytes < mls_tree_attention_workspace_size(c, n, N, q_heads))
+    return MLS_ERR_WORKSPACE;
+  DeviceState* dev = nullptr;
+  if ((rc = device_state(&dev))) return rc;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  TreeParams p;
+  std::memset(&p, 0, sizeof p);
+  p.c = cache_view(c, dev);
+  p.layer = layer;
+  p.n = n;
+  p.N = N;
+  p.q_heads = q_heads;
+  p.group = q_heads / c->kv_heads;
+  p.dim = c->head_dim;
+  p.seqs = seqs;
+  p.start = start;
+  p.parents = parents;
+  p.q = q;
+  p.q_ld = q_ld;
+  p.scale = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634);
+  p.out = out;
+  p.lse = lse;
+  p.part = static_cast<float*>(ws);
+  p.splits = tree_fp32_splits(N, q_heads, dev->sms);
+  p.status = dev->status;
+  p.sms = dev->sms;
+  return timed("tree_attention", s,
+               [&] { return c->dtype == MLS_FP32 ? launch_tree_fp32(p, s) : launch_tree_bf16(p, s); });
+}
+
+extern "C" int mls_tree_verify(const mls_tree_problem* p, const float* target, const float* draft,
+                               const int32_t* tokens, const int32_t* parents, const int32_t* start,
+                               const float* uniforms, int32_t* n_path, int32_t* path, int32_t* next_token,
+                               mls_stream_t stream) {
+  if (!p || p->n < 0 || p->N < 0 || p->N > INT_MAX || p->V < 1 || p->V > INT_MAX || p->max_path < 1 ||
+      p->max_path > MLS_TREE_MAX_NODES)
+    return MLS_ERR_ARG;
+  constexpr int64_t kMost = int64_t{1} << 31;
+  if (p->ld_target < p->V || p->ld_target > kMost || (draft && (p->ld_draft < p->V || p->ld_draft > kMost)))
+    return MLS_ERR_ARG;
+  if (p->n > INT_MAX / 8) return MLS_ERR_UNSUPPORTED;
+  if (p->n == 0) return MLS_OK;
+  if (!start || !n_path || !path || !next_token || (p->N > 0 && (!target || !tokens || !parents || !uniforms)))
+    return MLS_ERR_ARG;
+  const void* const ptrs[] = {target, draft, tokens, parents, start, uniforms, n_path, path, next_token};
+  for (const void* x : ptrs)
+    if (!aligned4(x)) return MLS_ERR_ALIGN;
+  DeviceState* dev = nullptr;
+  if (const int rc = device_state(&dev)) return rc;
+  AcceptParams a;
+  std::memset(&a, 0, sizeof a);
+  a.n = p->n;
+  a.N = p->N;
+  a.V = p->V;
+  a.target = target;
+  a.draft = draft;
+  a.ld_target = p->ld_target;
+  a.ld_draft = p->ld_draft;
+  a.tokens = tokens;
+  a.parents = parents;
+  a.start = start;
+  a.u = uniforms;
+  a.replace = p->replace;
+  a.max_path = p->max_path;
+  a.n_path = n_path;
+  a.path = path;
+  a.next = next_token;
+  a.cluster = accept_cluster(p->n, p->V, dev->sms);
+  a.status = dev->status;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  return timed("tree_verify", s, [&] { return launch_accept(a, s); });
 }

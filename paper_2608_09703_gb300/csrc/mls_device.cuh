@@ -17,6 +17,7 @@ constexpr int kStatusTimeout = 2;
 constexpr int kStatusCheck = 4;
 constexpr int kStatusDrain = 8;
 constexpr int kStatusBadSeq = 16;
+constexpr int kStatusNoPages = 32;
 
 // Invariant checks of the checked build (-DMLS_CHECKED, libmls_checked.so):
 // a failed condition raises kStatusCheck in the status word and execution

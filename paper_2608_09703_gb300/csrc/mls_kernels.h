@@ -536,6 +536,86 @@ cudaError_t launch_clip_norm(const ClipParams<kCap>& p, int grid, cudaStream_t s
 template <int kCap>
 cudaError_t launch_clip_scale(const ClipParams<kCap>& p, int grid, cudaStream_t s);
 
+// ------------------------------------------------------------------ paged key/value cache
+// The kernels' view of an mls_cache.  A token's values of one head and layer are `row`
+// pieces of 16 bytes; k and v are [layers][pages][heads][page_size][row].
+struct CacheView {
+  int layers, pages, heads, row;
+  int page_shift;                // page_size = 1 << page_shift
+  int seqs, max_pages;
+  uint4 *k, *v;
+  int *table, *len, *held, *refs;
+  unsigned* free_bits;
+  int* status;
+};
+// Where a token of a page begins, in pieces.
+__host__ __device__ inline long long cache_at(const CacheView& c, int layer, int page, int head, int slot) {
+  return ((((static_cast<long long>(layer) * c.pages + page) * c.heads + head) << c.page_shift) + slot) * c.row;
+}
+constexpr int kCacheMaxEntries = 8192;  // entries of one call: a prefix over them stays in shared memory
+constexpr int kCachePath = 256;         // path tokens whose places a block keeps at a time
+cudaError_t launch_cache_reset(const CacheView& c, cudaStream_t s);
+cudaError_t launch_cache_free(const CacheView& c, int n, const int* seqs, cudaStream_t s);
+cudaError_t launch_cache_reserve(const CacheView& c, int n, const int* seqs, const int* count, cudaStream_t s);
+// fresh, length: [n] each, handed from the first kernel to the second
+cudaError_t launch_cache_fork(const CacheView& c, int n, const int* src, const int* dst, int* fresh, int* length,
+                              int sms, cudaStream_t s);
+struct CacheAppend {
+  int layer0, layers;            // layers written; k and v begin with the first of them
+  int n;
+  const int *seqs, *start;
+  long long N;
+  const uint4 *k, *v;
+  long long token_ld, layer_ld;  // pieces between tokens and between layers of k and of v
+};
+cudaError_t launch_cache_append(const CacheView& c, const CacheAppend& a, cudaStream_t s);
+cudaError_t launch_cache_compact(const CacheView& c, int n, const int* seqs, const int* keep, const int* path,
+                                 int path_ld, int sms, cudaStream_t s);
+cudaError_t launch_cache_copy(const CacheView& from, const CacheView& to, int n, const int* src, const int* dst,
+                              int sms, cudaStream_t s);
+cudaError_t setup_cache_kernels();
+
+// ------------------------------------------------------------------ tree attention
+struct TreeParams {
+  CacheView c;
+  CUtensorMap map_k, map_v;      // bf16: boxes of 64 values of one head and page
+  int layer, n;
+  long long N;
+  int q_heads, group;            // group = query heads of a key/value head
+  int dim;
+  const int *seqs, *start, *parents;
+  const void* q;
+  long long q_ld;                // values between tokens of q
+  float scale;                   // times log2(e)
+  void* out;
+  float* lse;
+  int splits;                    // fp32: pieces of the keys
+  float* part;                   // workspace
+  int* status;
+  int sms;
+};
+constexpr int kTreeMaxNodes = 256;
+cudaError_t launch_tree_fp32(const TreeParams& p, cudaStream_t s);
+cudaError_t launch_tree_bf16(const TreeParams& p, cudaStream_t s);
+int tree_fp32_splits(long long N, int q_heads, int sms);
+
+// ------------------------------------------------------------------ acceptance of drafted trees
+struct AcceptParams {
+  int n;
+  long long N, V;
+  const float *target, *draft;   // rows of ld values; draft may be null
+  long long ld_target, ld_draft;
+  const int *tokens, *parents, *start;
+  const float* u;                // [N][2]
+  int replace;
+  int max_path;
+  int *n_path, *path, *next;
+  int cluster;                   // CTAs of a sequence
+  int* status;
+};
+int accept_cluster(int n, long long V, int sms);
+cudaError_t launch_accept(const AcceptParams& p, cudaStream_t s);
+
 // One-time per-device kernel attribute setup (dynamic shared memory limits).
 cudaError_t setup_head_kernels();
 cudaError_t setup_gemm_kernels();
