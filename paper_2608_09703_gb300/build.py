@@ -26,8 +26,9 @@ BUILD_CHECKED = os.path.join(PKG, "_build_checked")
 LIB_CHECKED = os.path.join(PKG, "libmls_checked.so")
 SOURCES = ["mls_api.cu", "mls_head.cu", "mls_gemm.cu", "mls_reduce.cu", "mls_eval.cu",
            "mls_junction.cu", "mls_spec.cu", "mls_logits.cu", "mls_norm.cu", "mls_policy.cu",
-           "mls_clip.cu", "mls_cache.cu", "mls_tree.cu", "mls_accept.cu"]
-HEADERS = ["mls_device.cuh", "mls_vec.cuh", "mls_kernels.h"]
+           "mls_clip.cu", "mls_cache.cu", "mls_tree.cu",
+           "mls_tree_mma.cu", "mls_accept.cu"]
+HEADERS = ["mls_device.cuh", "mls_vec.cuh", "mls_kernels.h", "mls_tree.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

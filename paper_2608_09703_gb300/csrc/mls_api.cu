@@ -9,6 +9,7 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <limits>
 #include <mutex>
 #include <vector>
 
@@ -79,6 +80,8 @@ int device_state(DeviceState** out) {
       s.err = fail(MLS_ERR_CUDA, "norm kernel attributes", e);
     } else if ((e = setup_cache_kernels()) != cudaSuccess) {
       s.err = fail(MLS_ERR_CUDA, "cache kernel attributes", e);
+    } else if ((e = setup_tree_kernels()) != cudaSuccess) {
+      s.err = fail(MLS_ERR_CUDA, "tree attention kernel attributes", e);
     } else if ((s.gemm_pairs = gemm_max_active_pairs()) <= 0) {
       s.err = fail(MLS_ERR_CUDA, "gemm cluster occupancy");
     } else if ((s.head_pairs = head_max_active_pairs()) <= 0) {
@@ -1995,12 +1998,43 @@ int tree_validate(const mls_cache* c, int n, int64_t N, int q_heads) {
     return MLS_ERR_UNSUPPORTED;
   return MLS_OK;
 }
+
+struct TreePlan {
+  int splits, part_rows;
+  size_t off_part, total;
+};
+TreePlan tree_plan(const mls_cache* c, int n, int64_t N, int q_heads, int sms) {
+  TreePlan pl;
+  const size_t row = sizeof(float) * (c->head_dim + 4);
+  pl.splits = tree_fp32_splits(N, q_heads, sms);
+  pl.part_rows = tree_part_rows(N, q_heads / c->kv_heads);
+  if (c->dtype == MLS_FP32) {
+    pl.off_part = 0;
+    pl.total = align_up(pl.splits > 1 ? row * N * q_heads * pl.splits : 1);
+  } else {
+    pl.off_part = align_up(sizeof(long long) * (static_cast<size_t>(n) + 1));
+    pl.total = pl.off_part + align_up(row * 2 * sms * pl.part_rows);
+  }
+  return pl;
+}
+
+// The cache's k or v as [layers * pages * heads][page_size][head_dim], in boxes of 64 values (128 bytes,
+// swizzled) of the tokens of one page, or of as many as a tile has.
+int encode_pages(CUtensorMap* map, const mls_cache* c, const void* ptr) {
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(c->head_dim), static_cast<cuuint64_t>(c->page_size),
+                              static_cast<cuuint64_t>(c->layers) * c->pages * c->kv_heads};
+  const cuuint64_t strides[2] = {dims[0] * 2, dims[0] * dims[1] * 2};
+  const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(c->page_size < 128 ? c->page_size : 128), 1}, estr[3] = {1, 1, 1};
+  const CUresult r = g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), dims, strides, box, estr,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? MLS_OK : fail(MLS_ERR_CUDA, "cuTensorMapEncodeTiled (cache)");
+}
 }  // namespace
 
 extern "C" size_t mls_tree_attention_workspace_size(const mls_cache* c, int32_t n, int64_t N, int32_t q_heads) {
   if (tree_validate(c, n, N, q_heads)) return 0;
-  const int splits = tree_fp32_splits(N, q_heads, current_sms());
-  return align_up(sizeof(float) * N * q_heads * splits * (c->head_dim + 4));
+  return tree_plan(c, n, N, q_heads, current_sms()).total;
 }
 
 extern "C" int mls_tree_attention(const mls_cache* c, int32_t layer, int32_t n, const int32_t* seqs,
@@ -2017,9 +2051,8 @@ extern "C" int mls_tree_attention(const mls_cache* c, int32_t layer, int32_t n, 
   if (q_ld % (c->dtype == MLS_BF16 ? 8 : 4) || !aligned16(q) || !aligned16(out) || !aligned4(lse) || !aligned4(seqs) ||
       !aligned4(start) || !aligned4(parents))
     return MLS_ERR_ALIGN;
-  if (!ws || (reinterpret_cast<uintptr_t>(ws) % kAlign) != 0 ||
-      ws_bytes < mls_tree_attention_workspace_size(c, n, N, q_heads))
-    return MLS_ERR_WORKSPACE;
+  const TreePlan pl = tree_plan(c, n, N, q_heads, current_sms());
+  if (!ws || (reinterpret_cast<uintptr_t>(ws) % kAlign) != 0 || ws_bytes < pl.total) return MLS_ERR_WORKSPACE;
   DeviceState* dev = nullptr;
   if ((rc = device_state(&dev))) return rc;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
@@ -2037,13 +2070,19 @@ extern "C" int mls_tree_attention(const mls_cache* c, int32_t layer, int32_t n, 
   p.parents = parents;
   p.q = q;
   p.q_ld = q_ld;
-  p.scale = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634);
+  // Positive, so that a masked score's -infinity times it is one too (the smallest for a scale of 0).
+  p.scale = std::max(static_cast<float>(std::fabs(static_cast<double>(scale)) * 1.4426950408889634),
+                     std::numeric_limits<float>::denorm_min());
+  p.negate = scale < 0.f;
   p.out = out;
   p.lse = lse;
-  p.part = static_cast<float*>(ws);
-  p.splits = tree_fp32_splits(N, q_heads, dev->sms);
+  p.part = reinterpret_cast<float*>(static_cast<char*>(ws) + pl.off_part);
+  p.part_rows = pl.part_rows;
+  p.unit_base = static_cast<long long*>(ws);
+  p.splits = pl.splits;
   p.status = dev->status;
   p.sms = dev->sms;
+  if (c->dtype == MLS_BF16 && (encode_pages(&p.map_k, c, c->k) || encode_pages(&p.map_v, c, c->v))) return MLS_ERR_CUDA;
   return timed("tree_attention", s,
                [&] { return c->dtype == MLS_FP32 ? launch_tree_fp32(p, s) : launch_tree_bf16(p, s); });
 }

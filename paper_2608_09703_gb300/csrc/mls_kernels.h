@@ -586,11 +586,16 @@ struct TreeParams {
   const int *seqs, *start, *parents;
   const void* q;
   long long q_ld;                // values between tokens of q
-  float scale;                   // times log2(e)
+  float scale;                   // times log2(e), made positive (zero); negate: q is to change its sign
+  int negate;
   void* out;
   float* lse;
   int splits;                    // fp32: pieces of the keys
-  float* part;                   // workspace
+  // Workspace: of rows whose keys are split their maximum, sum and product, dim + 4 words each.
+  // fp32: [N][q_heads][splits] of them.  bf16: [CTAs][2][part_rows], a CTA's first and its last item.
+  float* part;
+  int part_rows;
+  long long* unit_base;          // bf16: [n + 1] the first key tile of each entry, in one numbering
   int* status;
   int sms;
 };
@@ -598,6 +603,8 @@ constexpr int kTreeMaxNodes = 256;
 cudaError_t launch_tree_fp32(const TreeParams& p, cudaStream_t s);
 cudaError_t launch_tree_bf16(const TreeParams& p, cudaStream_t s);
 int tree_fp32_splits(long long N, int q_heads, int sms);
+int tree_part_rows(long long N, int group);
+cudaError_t setup_tree_kernels();
 
 // ------------------------------------------------------------------ acceptance of drafted trees
 struct AcceptParams {

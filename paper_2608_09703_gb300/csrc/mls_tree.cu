@@ -7,43 +7,11 @@
 
 #include "mls_device.cuh"
 #include "mls_kernels.h"
+#include "mls_tree.cuh"
 #include "mls_vec.cuh"
 
 namespace mls {
 namespace {
-
-constexpr float kLn2 = 0.6931471805599453f;
-
-// What an entry of a call is: its nodes [first, first + nodes) of the packed ones, its row of the
-// table and the tokens cached there.  What does not fit the cache is an entry of unused nodes.
-struct Entry {
-  int nodes, row, len;
-  long long first;
-};
-__device__ __forceinline__ Entry tree_entry(const TreeParams& p, int i, int* status) {
-  Entry e;
-  const long long a = p.start[i], b = p.start[i + 1];
-  bool bad = a < 0 || b < a || b > p.N;
-  e.first = a;
-  e.nodes = bad ? 0 : static_cast<int>(b - a);
-  e.row = p.seqs ? p.seqs[i] : i;
-  e.len = 0;
-  if (e.nodes) {
-    if (e.row < 0 || e.row >= p.c.seqs || (p.parents && e.nodes > kTreeMaxNodes)) {
-      bad = true;
-      e.row = -1;
-    } else {
-      e.len = p.c.len[e.row];
-      if (e.len < 0 || static_cast<long long>(e.len) + e.nodes > (static_cast<long long>(p.c.max_pages) << p.c.page_shift)) {
-        bad = true;
-        e.row = -1;
-        e.len = 0;
-      }
-    }
-  }
-  if (bad) atomicOr(status, kStatusBadSeq);
-  return e;
-}
 
 // ------------------------------------------------------------------ one warp a node
 // A warp takes one node and up to kHeads query heads of one key/value head, a piece of the keys, 32
@@ -116,7 +84,8 @@ __global__ void __launch_bounds__(32 * kWarps) node_kernel(TreeParams p) {
   }
   for (int x = lane; x < nh * p.dim; x += 32) {
     const int h = x / p.dim, d = x - h * p.dim;
-    qs[warp][h][d] = static_cast<float>(static_cast<const E*>(p.q)[t * p.q_ld + static_cast<long long>(h0 + h) * p.dim + d]);
+    const float f = static_cast<float>(static_cast<const E*>(p.q)[t * p.q_ld + static_cast<long long>(h0 + h) * p.dim + d]);
+    qs[warp][h][d] = p.negate ? -f : f;
   }
   __syncwarp();
   float m[kHeads], l[kHeads], o[kHeads][4];
@@ -255,6 +224,5 @@ int tree_fp32_splits(long long N, int q_heads, int sms) {
 }
 
 cudaError_t launch_tree_fp32(const TreeParams& p, cudaStream_t s) { return run_nodes<float>(p, s); }
-cudaError_t launch_tree_bf16(const TreeParams& p, cudaStream_t s) { return run_nodes<__nv_bfloat16>(p, s); }
 
 }  // namespace mls

@@ -1,0 +1,724 @@
+// Tree attention over a bf16 cache on the tensor cores (the operator: mls_tree.cu).
+//
+// The rows of a product are an entry's nodes times the query heads of one key/value head (node-major), 128 a
+// tile.  S = Q K^T and O += P V run as tcgen05 MMAs of 128 rows and 128 keys; K and V come by TMA, a box a page
+// (V in place as an MN-major operand), P goes back to TMEM as the A operand, over S.
+// A CTA has two streams of a warpgroup, an S and an O accumulator each (512 columns of TMEM): the tensor cores
+// work for one while the other takes its exponentials.  With more than 128 rows the streams have a row
+// tile each and share the keys; with fewer they have the same rows, and every other key tile: what they
+// hold is joined at the end, each warp reading the other stream's O in its own lanes.
+//
+// Lengths are known on the device only, so CTAs cut the work there: all key tiles of all items (entry, pair of
+// row tiles, key/value head) are numbered, and CTA c of G takes the c-th of G equal ranges, which may begin and
+// end inside an item.  Pieces of an item that lies in several ranges go to the workspace, and a second kernel joins
+// them.  Work is even over the card whatever the lengths are, and a captured graph follows them.
+//
+// Softmax in one pass: a running maximum per row, which moves only when it grows by more than 2^8 (P stays
+// below 256, exact enough in bf16), so that O is rarely rescaled.  Only tiles past the cached tokens look at
+// masks.  Masked weights are 0, and so that 0 times what lies there is 0 too, values behind the item's last
+// node are cleared, and infinities and NaN among the nodes' values taken out of the product and added to the
+// rows that do see them.
+#include <climits>
+#include <cmath>
+
+#include "mls_device.cuh"
+#include "mls_kernels.h"
+#include "mls_tree.cuh"
+#include "mls_vec.cuh"
+
+namespace mls {
+namespace {
+
+constexpr int kRows = 128, kKeys = 128;           // of a tile
+constexpr int kThreads = 384;
+constexpr int kCtlRegs = 72, kSoftmaxRegs = 216, kLaunchRegs = 168;  // 72 + 2 x 216 = 3 x 168
+constexpr uint64_t kDrainNs = 100000000ull;
+constexpr uint32_t kTmemCols = 512, kAccO = 256;  // S of stream w at 128 w, O at 256 + 128 w
+constexpr float kGrow = 8.f;
+constexpr int kMaxStages = 12;
+constexpr uint32_t kSmem = 227 * 1024;
+
+// Past the operands.  A warpgroup's `up` and `ml` share memory: parents are read before any sum is.
+struct Tail {
+  uint64_t full[kMaxStages], empty[kMaxStages], q_ready[2], s_full[2], p_ready[2], o_full[2], drain;
+  union {
+    short up[kTreeMaxNodes];
+    float2 ml[kRows];
+  } row[2];
+  long long scan[kThreads / 32], base0;
+  int e0, fix[2], abort;
+  uint32_t tmem_slot;
+};
+template <int DC>
+struct Layout {                                   // DC: pieces of 64 values of a row
+  static constexpr uint32_t kTile = DC * kKeys * 128u;
+  static constexpr int kStages = DC == 2 ? 5 : 12;
+  static constexpr uint32_t kRing = 2 * kTile, kTail = kRing + kStages * kTile;
+  static_assert(kTail + sizeof(Tail) <= kSmem, "shared memory");
+};
+
+// A piece of an item: rows [r0, r0 + nrows) of an entry and head, key tiles [t0, t1) of nt.
+struct Seg {
+  Entry en;
+  int e, head, r0, nrows, t0, t1, nt;
+  int total;                                      // keys of the item: cached tokens and nodes up to its last
+  int all;                                        // keys that every row sees
+  bool first;                                     // of this CTA
+};
+// Key tiles of rows [r0, r0 + 256) of an entry.
+__device__ __forceinline__ int item_total(const TreeParams& p, const Entry& en, int r0) {
+  const int rows = min(en.nodes * p.group - r0, 2 * kRows);
+  return en.len + (r0 + rows - 1) / p.group + 1;
+}
+__device__ __forceinline__ int tiles_of(int total) { return (total + kKeys - 1) / kKeys; }
+__device__ long long entry_units(const TreeParams& p, const Entry& en) {
+  long long sum = 0;
+  for (int r0 = 0; r0 < en.nodes * p.group; r0 += 2 * kRows) sum += tiles_of(item_total(p, en, r0));
+  return sum * p.c.heads;
+}
+
+// Walks the segments of units [at, hi); entry e begins at unit `base`.
+struct Walker {
+  long long at, hi, base;
+  int e;
+  Entry en;
+  long long units;
+  bool first;
+  __device__ Walker(const TreeParams& p, long long lo, long long hi_, int e0, long long base0)
+      : at(lo), hi(hi_), base(base0), e(e0), first(true) {
+    units = 0;
+    if (at < hi) {
+      en = tree_entry(p, e, p.status);
+      units = entry_units(p, en);
+    }
+  }
+  __device__ bool next(const TreeParams& p, Seg& g) {
+    if (at >= hi) return false;
+    while (at - base >= units) {
+      base += units;
+      en = tree_entry(p, ++e, p.status);
+      units = entry_units(p, en);
+    }
+    long long v = at - base;
+    g.r0 = 0;
+    while (true) {
+      g.total = item_total(p, en, g.r0);
+      g.nt = tiles_of(g.total);
+      const long long here = static_cast<long long>(g.nt) * p.c.heads;
+      if (v < here) break;
+      v -= here;
+      g.r0 += 2 * kRows;
+    }
+    g.head = static_cast<int>(v / g.nt);
+    g.t0 = static_cast<int>(v - static_cast<long long>(g.head) * g.nt);
+    g.t1 = static_cast<int>(min(static_cast<long long>(g.nt), g.t0 + (hi - at)));
+    g.nrows = min(en.nodes * p.group - g.r0, 2 * kRows);
+    g.all = en.row < 0 ? 0 : p.parents ? en.len : en.len + g.r0 / p.group + 1;
+    g.en = en;
+    g.e = e;
+    g.first = first;
+    first = false;
+    at += g.t1 - g.t0;
+    return true;
+  }
+};
+
+// Where the K and V tiles of step j lie in the order in which a segment of n tiles is loaded: K0 V0 K1 V1 ...
+// for two row tiles, K0 K1 V0 K2 V1 K3 ... for two streams of key tiles, as the MMAs take them.
+__device__ __forceinline__ uint32_t place_k(int j, bool pair) { return pair ? 2 * j : j < 2 ? j : 2 * j - 1; }
+__device__ __forceinline__ uint32_t place_v(int j, int n, bool pair) { return pair ? 2 * j + 1 : min(2 * j + 2, 2 * n - 1); }
+
+template <int DC>
+__device__ void load_role(const TreeParams& p, Tail* sh, uint32_t base, Walker it) {
+  using L = Layout<DC>;
+  const int lane = threadIdx.x & 31;
+  const int size = 1 << p.c.page_shift, box = min(size, kKeys), boxes = kKeys / box;
+  const int mine = lane / DC, half = lane - mine * DC;        // this lane's box of a tile: boxes * DC <= 32
+  const bool active = mine < boxes;
+  const int none = p.c.layers * p.c.pages * p.c.heads;        // a box there is filled with zeros
+  const uint32_t dst = half * (kKeys * 128u) + mine * box * 128u;
+  uint32_t ring = 0;
+  bool ok = true;
+  Seg g;
+  while (ok && it.next(p, g)) {
+    const int n = g.t1 - g.t0;
+    const bool pair = g.nrows > kRows;
+    const int* const table = g.en.row < 0 ? nullptr : p.c.table + static_cast<long long>(g.en.row) * p.c.max_pages;
+    for (int i = 0; i < 2 * n; ++i, ++ring) {
+      // The i-th load of the segment: K of step kj, or V of step vj.
+      int j;
+      bool is_v;
+      if (pair) {
+        j = i >> 1;
+        is_v = i & 1;
+      } else if (i < 2) {
+        is_v = i == 1 && n == 1;
+        j = is_v ? 0 : i;
+      } else if (i == 2 * n - 1) {
+        is_v = true;
+        j = n - 1;
+      } else {
+        is_v = !(i & 1);
+        j = is_v ? (i - 2) >> 1 : (i + 1) >> 1;
+      }
+      const int pos = (g.t0 + j) * kKeys + mine * box;
+      int at = none;
+      if (active && table && pos < g.total) {
+        const int page = table[pos >> p.c.page_shift];
+        if (page >= 0 && page < p.c.pages) at = (p.layer * p.c.pages + page) * p.c.heads + g.head;
+        else atomicOr(p.status, kStatusBadSeq);
+      }
+      const uint32_t stage = ring % L::kStages, phase = (ring / L::kStages) & 1u;
+      ok = mbar_wait(smem_u32(&sh->empty[stage]), phase ^ 1u, &sh->abort, p.status);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      const uint32_t bar = smem_u32(&sh->full[stage]);
+      if (lane == 0) mbar_arrive_expect_tx(bar, L::kTile);
+      __syncwarp();
+      if (active)
+        tma_load_3d(base + L::kRing + stage * L::kTile + dst, is_v ? &p.map_v : &p.map_k, bar, half * 64,
+                    pos & (size - 1), at);
+    }
+  }
+  if (!ok && lane == 0)  // what was asked for lands before the shared memory goes away
+    for (uint32_t b = ring > L::kStages ? ring - L::kStages : 0; b < ring; ++b)
+      mbar_wait_drain(smem_u32(&sh->full[b % L::kStages]), (b / L::kStages) & 1u, kDrainNs, p.status);
+  __syncwarp();
+}
+
+template <int DC>
+__device__ void mma_role(const TreeParams& p, Tail* sh, uint32_t base, uint32_t tmem, Walker it) {
+  using L = Layout<DC>;
+  const uint32_t idesc_s = make_idesc(kRows, kKeys, false, false, false);
+  const int dn = (p.dim + 15) & ~15;
+  const uint32_t idesc_o = make_idesc(kRows, dn, false, false, true);
+  const int ks = dn / 16;
+  uint32_t ring = 0, q_par = 0, p_par = 0;  // a bit a stream
+  bool ok = true;
+  auto wait = [&](uint64_t* bar, uint32_t parity) {
+    ok = ok && mbar_wait(smem_u32(bar), parity, &sh->abort, p.status);
+    tc_fence_after();
+    return ok;
+  };
+  Seg g;
+  while (ok && it.next(p, g)) {
+    const int n = g.t1 - g.t0;
+    const bool pair = g.nrows > kRows;
+    const int steps[2] = {pair ? n : (n + 1) / 2, pair ? n : n / 2};
+    auto scores = [&](int w, int i) {
+      const uint32_t at = ring + place_k(pair ? i : 2 * i + w, pair), stage = at % L::kStages;
+      if (!wait(&sh->full[stage], (at / L::kStages) & 1u)) return;
+      const uint64_t a = make_sdesc(base + w * L::kTile, 16), b = make_sdesc(base + L::kRing + stage * L::kTile, 16);
+      for (int k = 0; k < ks; ++k) {
+        const uint64_t step = (k >> 2) * (kKeys * 128 / 16) + (k & 3) * 2;
+        mma_issue<false>(tmem + w * kKeys, a + step, b + step, idesc_s, k > 0);
+      }
+      if (!pair || w == 1) mma_commit(smem_u32(&sh->empty[stage]));
+      mma_commit(smem_u32(&sh->s_full[w]));
+    };
+    for (int w = 0; w < 2; ++w)
+      if (steps[w] > 0 && wait(&sh->q_ready[w], (q_par >> w) & 1u)) {
+        q_par ^= 1u << w;
+        scores(w, 0);
+      }
+    for (int i = 0; ok && i < steps[0]; ++i)
+      for (int w = 0; ok && w < 2; ++w) {
+        if (i >= steps[w] || !wait(&sh->p_ready[w], (p_par >> w) & 1u)) continue;
+        p_par ^= 1u << w;
+        const uint32_t at = ring + place_v(pair ? i : 2 * i + w, n, pair), stage = at % L::kStages;
+        if (!wait(&sh->full[stage], (at / L::kStages) & 1u)) break;
+        const uint64_t b = make_sdesc(base + L::kRing + stage * L::kTile, kKeys * 128);
+        for (int k = 0; k < kKeys / 16; ++k)
+          mma_issue_ts(tmem + kAccO + w * 128, tmem + w * kKeys + k * 8, b + k * (16 * 128 / 16), idesc_o, i > 0 || k > 0);
+        if (!pair || w == 1) mma_commit(smem_u32(&sh->empty[stage]));
+        if (i + 1 < steps[w]) scores(w, i + 1);
+        else mma_commit(smem_u32(&sh->o_full[w]));
+      }
+    ring += 2 * n;
+  }
+  // Every MMA that this thread issued has finished before TMEM is released.
+  mma_commit(smem_u32(&sh->drain));
+  mbar_wait_drain(smem_u32(&sh->drain), 0, kDrainNs, p.status);
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// Halves of a word that are infinite or NaN.
+__device__ __forceinline__ bool odd_lo(uint32_t w) { return (w & 0x7f80u) == 0x7f80u; }
+__device__ __forceinline__ bool odd_hi(uint32_t w) { return (w & 0x7f800000u) == 0x7f800000u; }
+__device__ __forceinline__ bool odd_any(const uint4& v) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) odd |= odd_lo(w[i]) || odd_hi(w[i]);
+  return odd;
+}
+
+// What a row sees past the cached tokens: the nodes up to its own, or those on its path.
+struct Sight {
+  unsigned path[kTreeMaxNodes / 32];
+  int len, upto;                                  // keys before `upto` where there is no path
+  bool tree, used;
+  // Truth of keys [k, k + 32), a bit each.
+  __device__ __forceinline__ unsigned bits(int k) const {
+    if (!used) return 0u;
+    if (!tree) {
+      const int n = upto - k;
+      return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u;
+    }
+    const int j = k - len;                        // node of the first
+    if (j <= -32) return 0xffffffffu;
+    const int word = j >> 5, shift = j & 31;      // rounds down
+    unsigned lo = word < 0 ? 0xffffffffu : 0u, hi = 0u;
+#pragma unroll
+    for (int i = 0; i < kTreeMaxNodes / 32; ++i) {
+      if (i == word) lo = path[i];
+      if (i == word + 1) hi = path[i];
+    }
+    return __funnelshift_r(lo, hi, shift);
+  }
+};
+
+template <int DC>
+__device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint32_t tmem, int w, Walker it) {
+  using L = Layout<DC>;
+  const int tid = threadIdx.x & 127, quad = tid >> 5;
+  const uint32_t lanes = static_cast<uint32_t>(quad * 32) << 16;
+  const uint32_t ts = tmem + lanes + w * kKeys, to = tmem + lanes + kAccO + w * 128;
+  const int width = p.dim >> 3;                   // pieces of a row
+  const __nv_bfloat16* const V = reinterpret_cast<const __nv_bfloat16*>(p.c.v);
+  const int mask = (1 << p.c.page_shift) - 1;
+  uint32_t ring = 0, s_par = 0, o_par = 0;
+  Seg g;
+  while (it.next(p, g)) {
+    const int n = g.t1 - g.t0;
+    const bool pair = g.nrows > kRows;
+    const int steps = pair ? n : (n + 1 - w) / 2;
+    const int rl = (pair ? w * kRows : 0) + tid;  // this thread's row of the item
+    const bool inside = rl < g.nrows;
+    const int r = g.r0 + rl, node = inside ? r / p.group : 0;
+    const int* const table = p.c.table + static_cast<long long>(max(g.en.row, 0)) * p.c.max_pages;
+    Sight see;
+    see.tree = p.parents != nullptr;
+    see.len = g.en.len;
+    see.upto = g.en.len + node + 1;
+    see.used = inside && g.en.row >= 0;
+    if (see.tree) {
+      short* const up = sh->row[w].up;
+      const int nodes = g.en.row < 0 ? 0 : g.en.nodes;
+      for (int j = tid; j < nodes; j += kRows) {
+        const int u = p.parents[g.en.first + j];
+        const bool odd = u < -2 || u >= j;
+        if (odd) atomicOr(p.status, kStatusBadSeq);
+        up[j] = static_cast<short>(odd ? -2 : u);
+      }
+      named_bar_sync(1 + w, kRows);
+#pragma unroll
+      for (int i = 0; i < kTreeMaxNodes / 32; ++i) see.path[i] = 0u;
+      if (see.used) {
+        see.used = up[node] >= -1;
+        for (int j = node; j >= 0 && up[j] >= -1; j = up[j])
+#pragma unroll
+          for (int i = 0; i < kTreeMaxNodes / 32; ++i)
+            if (i == j >> 5) see.path[i] |= 1u << (j & 31);
+      }
+      named_bar_sync(1 + w, kRows);
+    }
+    if (steps > 0) {
+      // Queries of this stream's rows, swizzled as TMA would, zeros where there is no row or value.
+      const uint32_t flip = p.negate ? 0x80008000u : 0u;
+      const int row0 = g.r0 + (pair ? w * kRows : 0);
+      const __nv_bfloat16* const q = static_cast<const __nv_bfloat16*>(p.q) + g.en.first * p.q_ld +
+                                     static_cast<long long>(g.head) * p.group * p.dim;
+#pragma unroll 4
+      for (int x = tid; x < kRows * DC * 8; x += kRows) {
+        const int row = x / (DC * 8), c = x - row * (DC * 8);
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (row0 + row < g.r0 + g.nrows && c < width) {
+          const int t = (row0 + row) / p.group, h = row0 + row - t * p.group;
+          v = ld16(q + t * p.q_ld + static_cast<long long>(h) * p.dim + c * 8);
+          v.x ^= flip, v.y ^= flip, v.z ^= flip, v.w ^= flip;
+        }
+        st_shared_v4(base + w * L::kTile + (c >> 3) * (kRows * 128u) + row * 128u + (((c & 7) ^ (row & 7)) << 4), v.x, v.y,
+                     v.z, v.w);
+      }
+      fence_proxy_async_smem();
+      mbar_arrive(smem_u32(&sh->q_ready[w]));
+    }
+    const bool busy = (pair ? w * kRows : 0) + quad * 32 < g.nrows;  // rows of this warp
+    float m = -INFINITY, l = 0.f;
+    bool fix = false;
+    for (int i = 0; i < steps; ++i) {
+      const int j = pair ? i : 2 * i + w, k0 = (g.t0 + j) * kKeys;
+      const bool masked = k0 + kKeys > g.all;
+      bool odd = false;
+      if (masked && g.en.row >= 0) {              // infinities and NaN among values that not every row sees
+        const int a = max(g.all, k0), b = min(g.total, k0 + kKeys);
+        for (int x = tid; x < (b - a) * width; x += kRows) {
+          const int k = a + x / width, c = x % width;
+          const int page = table[k >> p.c.page_shift];
+          if (page >= 0 && page < p.c.pages)
+            odd |= odd_any(ld16(V + cache_at(p.c, p.layer, page, g.head, k & mask) * 8 + c * 8));
+        }
+        odd = !named_bar_and(1 + w, kRows, !odd);
+        fix |= odd;
+      }
+      mbar_wait(smem_u32(&sh->s_full[w]), s_par, &sh->abort, p.status);
+      s_par ^= 1u;
+      tc_fence_after();
+      if (busy) {
+        float z[kKeys];
+        tmem_ld128(ts, z);
+        if (masked) {
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const unsigned b = see.bits(k0 + 32 * x);
+#pragma unroll
+            for (int y = 0; y < 32; ++y) z[32 * x + y] = (b >> y) & 1u ? z[32 * x + y] : -INFINITY;
+          }
+        }
+        float top[4] = {z[0], z[1], z[2], z[3]};
+#pragma unroll
+        for (int x = 4; x < kKeys; x += 8) {
+          top[0] = fmaxf(top[0], fmaxf(z[x], z[(x + 4) % kKeys]));
+          top[1] = fmaxf(top[1], fmaxf(z[x + 1], z[(x + 5) % kKeys]));
+          top[2] = fmaxf(top[2], fmaxf(z[x + 2], z[(x + 6) % kKeys]));
+          top[3] = fmaxf(top[3], fmaxf(z[x + 3], z[(x + 7) % kKeys]));
+        }
+        const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+        // The maximum moves only where it must; where it does, what is summed so far is brought down.
+        const bool move = (now - m) * p.scale > kGrow || (m == -INFINITY && now > m);
+        if (__any_sync(0xffffffffu, move)) {
+          const float c = !move ? 1.f : m == -INFINITY ? 0.f : fast_exp2((m - now) * p.scale);
+          if (move) m = now;
+          l *= c;
+          if (i > 0) {
+#pragma unroll 1
+            for (int x = 0; x < p.dim; x += 32) {
+              float o[32];
+              tmem_ld32(to + x, o);
+              uint32_t u[32];
+#pragma unroll
+              for (int y = 0; y < 32; ++y) u[y] = __float_as_uint(o[y] * c);
+              tmem_st32(to + x, u);
+            }
+          }
+        }
+        const float off = m == -INFINITY ? 0.f : m * p.scale;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        uint32_t u[kKeys / 2];
+#pragma unroll
+        for (int x = 0; x < kKeys; x += 2) {
+          const float a = fast_exp2(fmaf(z[x], p.scale, -off)), b = fast_exp2(fmaf(z[x + 1], p.scale, -off));
+          sum[x & 2] += a;
+          sum[(x & 2) + 1] += b;
+          u[x / 2] = pack_bf16(a, b);
+        }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        tmem_st32(ts, u);
+        tmem_st32(ts + 32, u + 32);
+        tmem_st_wait();
+      }
+      if (masked) {
+        const uint32_t at = ring + place_v(j, n, pair), stage = at % L::kStages;
+        const uint32_t tile = base + L::kRing + stage * L::kTile;
+        // Values behind the last key, up to the end of its page: the pages behind it came as zeros.
+        const int a = min(max(g.total - k0, 0), kKeys);
+        const int b = min((g.total + mask & ~mask) - k0, kKeys);
+        if (b > a || odd) {
+          mbar_wait(smem_u32(&sh->full[stage]), (at / L::kStages) & 1u, &sh->abort, p.status);
+          for (int x = tid; x < (b - a) * DC * 8; x += kRows) {
+            const int row = a + x / (DC * 8), c = x % (DC * 8);
+            st_shared_v4(tile + (c >> 3) * (kKeys * 128u) + row * 128u + ((c & 7) << 4), 0u, 0u, 0u, 0u);
+          }
+          if (odd)
+            for (int x = tid; x < kKeys * DC * 8; x += kRows) {
+              const int row = x / (DC * 8), c = x % (DC * 8);
+              if (k0 + row < g.all) continue;
+              const uint32_t addr = tile + (c >> 3) * (kKeys * 128u) + row * 128u + ((c & 7) << 4);
+              uint32_t v[4];
+              asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                           : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
+                           : "r"(addr)
+                           : "memory");
+#pragma unroll
+              for (int y = 0; y < 4; ++y) {
+                if (odd_lo(v[y])) v[y] &= 0xffff0000u;
+                if (odd_hi(v[y])) v[y] &= 0x0000ffffu;
+              }
+              st_shared_v4(addr, v[0], v[1], v[2], v[3]);
+            }
+          fence_proxy_async_smem();
+        }
+      }
+      tc_fence_before();
+      mbar_arrive(smem_u32(&sh->p_ready[w]));
+    }
+    ring += 2 * n;
+
+    // The end of a segment.  Streams of one row tile meet here: both read both accumulators, half of the columns
+    // each, which is why neither goes on before the other has read.
+    if (steps > 0) {
+      mbar_wait(smem_u32(&sh->o_full[w]), o_par, &sh->abort, p.status);
+      o_par ^= 1u;
+    }
+    float c_own = 1.f, c_other = 0.f, M = m, Lsum = l;
+    if (!pair) {
+      sh->row[w].ml[tid] = make_float2(m, l);
+      if (tid == 0) sh->fix[w] = fix;
+      tc_fence_before();
+      named_bar_sync(3, 2 * kRows);
+      const float2 o = sh->row[1 - w].ml[tid];
+      fix = sh->fix[0] || sh->fix[1];
+      M = fmaxf(m, o.x);
+      const float off = M == -INFINITY ? 0.f : M;
+      c_own = l == 0.f ? 0.f : m == -INFINITY ? 1.f : fast_exp2((m - off) * p.scale);
+      c_other = o.y == 0.f ? 0.f : o.x == -INFINITY ? 1.f : fast_exp2((o.x - off) * p.scale);
+      // (A sum without a maximum is NaN and stays so.)
+      Lsum = (l == 0.f ? 0.f : l * c_own) + (o.y == 0.f ? 0.f : o.y * c_other);
+    }
+    tc_fence_after();
+    const bool whole = g.t0 == 0 && g.t1 == g.nt;
+    const float inv = whole ? (Lsum == 0.f || !see.used ? 0.f : 1.f / Lsum) : 1.f;
+    const int chunks = (p.dim + 31) / 32;
+    const int x0 = pair || w == 0 ? 0 : (chunks + 1) / 2, x1 = pair || w == 1 ? chunks : (chunks + 1) / 2;
+    const long long t = g.en.first + node;
+    const long long out_row = t * p.q_heads + g.head * p.group + (r - node * p.group);
+    float* const part = p.part + ((static_cast<long long>(blockIdx.x) * 2 + (g.first ? 0 : 1)) * p.part_rows + rl) * (p.dim + 4);
+    const uint32_t other = tmem + lanes + kAccO + (1 - w) * 128;
+    const bool reads = (pair ? w * kRows : 0) + quad * 32 < g.nrows;
+    if (reads) {
+#pragma unroll 1
+      for (int x = x0; x < x1; ++x) {
+        float o[32];
+#pragma unroll
+        for (int y = 0; y < 32; ++y) o[y] = 0.f;
+        if (steps > 0) {
+          float v[32];
+          tmem_ld32(to + 32 * x, v);
+#pragma unroll
+          for (int y = 0; y < 32; ++y) o[y] = c_own == 0.f ? 0.f : v[y] * c_own;
+        }
+        if (!pair && n > 1 - w) {                  // the other stream had a tile too
+          float v[32];
+          tmem_ld32(other + 32 * x, v);
+#pragma unroll
+          for (int y = 0; y < 32; ++y) o[y] += c_other == 0.f ? 0.f : v[y] * c_other;
+        }
+        if (fix) {
+          const int b = min(g.total, g.t1 * kKeys);
+          for (int k = max(g.all, g.t0 * kKeys); k < b; ++k) {
+            const int page = table[k >> p.c.page_shift];
+            if (!(see.bits(k) & 1u) || page < 0 || page >= p.c.pages) continue;
+            const __nv_bfloat16* const v = V + cache_at(p.c, p.layer, page, g.head, k & mask) * 8 + 32 * x;
+#pragma unroll
+            for (int y = 0; y < 32; ++y)
+              if (32 * x + y < p.dim) {
+                const float f = __bfloat162float(v[y]);
+                if (!isfinite(f)) o[y] += f;
+              }
+          }
+        }
+        if (!inside) continue;
+        if (whole) {
+          __nv_bfloat16* const out = static_cast<__nv_bfloat16*>(p.out) + out_row * p.dim + 32 * x;
+#pragma unroll
+          for (int y = 0; y < 32; y += 8)
+            if (32 * x + y < p.dim) {
+              uint32_t u[4];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const float a = see.used ? o[y + 2 * k] * inv : 0.f, b = see.used ? o[y + 2 * k + 1] * inv : 0.f;
+                u[k] = pack_bf16(a, b);
+              }
+              st16(out + y, make_uint4(u[0], u[1], u[2], u[3]));
+            }
+        } else {
+#pragma unroll
+          for (int y = 0; y < 32; y += 4)
+            if (32 * x + y < p.dim)
+              *reinterpret_cast<float4*>(part + 4 + 32 * x + y) = make_float4(o[y], o[y + 1], o[y + 2], o[y + 3]);
+        }
+      }
+    }
+    if (inside && (pair || w == 0)) {
+      const float sum = see.used ? Lsum : 0.f;
+      if (whole) p.lse[out_row] = sum == 0.f ? -INFINITY : fmaf(M, p.scale, log2f(sum)) * kLn2;
+      else part[0] = M, part[1] = sum;
+    }
+    tc_fence_before();
+    if (!pair) named_bar_sync(3, 2 * kRows);
+  }
+}
+
+template <int DC>
+__global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant__ TreeParams p) {
+  using L = Layout<DC>;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const uint32_t base = smem_u32(smem);
+  Tail* const sh = reinterpret_cast<Tail*>(smem + L::kTail);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    sh->abort = 0;
+    for (int s = 0; s < L::kStages; ++s) {
+      mbar_init(smem_u32(&sh->full[s]), 1);
+      mbar_init(smem_u32(&sh->empty[s]), 1);
+    }
+    for (int w = 0; w < 2; ++w) {
+      mbar_init(smem_u32(&sh->q_ready[w]), kRows);
+      mbar_init(smem_u32(&sh->s_full[w]), 1);
+      mbar_init(smem_u32(&sh->p_ready[w]), kRows);
+      mbar_init(smem_u32(&sh->o_full[w]), 1);
+    }
+    mbar_init(smem_u32(&sh->drain), 1);
+    fence_barrier_init();
+  }
+  if (warp == 1) {
+    tmem_alloc(smem_u32(&sh->tmem_slot), kTmemCols);
+    tmem_relinquish();
+  }
+  // The work: every thread adds up a run of entries.
+  const int chunk = (p.n + kThreads - 1) / kThreads;
+  const int i0 = min(tid * chunk, p.n), i1 = min(i0 + chunk, p.n);
+  long long mine = 0;
+  for (int i = i0; i < i1; ++i) mine += entry_units(p, tree_entry(p, i, p.status));
+  long long upto = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long v = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += v;
+  }
+  if (lane == 31) sh->scan[warp] = upto;
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = sh->tmem_slot;
+  long long before = upto - mine, units = 0;
+  for (int x = 0; x < kThreads / 32; ++x) {
+    if (x < warp) before += sh->scan[x];
+    units += sh->scan[x];
+  }
+  const long long each = (units + gridDim.x - 1) / gridDim.x;
+  const long long lo = min(blockIdx.x * each, units), hi = min(lo + each, units);
+  if (blockIdx.x == 0 && tid == 0) p.unit_base[p.n] = units;
+  if (blockIdx.x == 0 || (lo < hi && before <= lo && lo < before + mine)) {
+    long long at = before;
+    for (int i = i0; i < i1; ++i) {
+      const long long u = entry_units(p, tree_entry(p, i, p.status));
+      if (blockIdx.x == 0) p.unit_base[i] = at;
+      if (at <= lo && lo < at + u) {
+        sh->e0 = i;
+        sh->base0 = at;
+      }
+      at += u;
+    }
+  }
+  __syncthreads();
+  const Walker it(p, lo, hi, sh->e0, sh->base0);
+
+  if (warp < 4) {
+    regs_decrease<kCtlRegs>();
+    if (warp == 0) {
+      load_role<DC>(p, sh, base, it);
+    } else if (warp == 1) {
+      if (lane == 0) mma_role<DC>(p, sh, base, tmem, it);
+      __syncwarp();
+    }
+  } else {
+    regs_increase<kSoftmaxRegs>();
+    softmax_role<DC>(p, sh, base, tmem, (warp - 4) >> 2, it);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, kTmemCols);
+  }
+}
+
+// Joins the pieces of rows whose keys lie in several CTAs' ranges, in order.  A warp a node and head.
+constexpr int kJoinWarps = 4;
+__global__ void __launch_bounds__(32 * kJoinWarps) tree_join_kernel(TreeParams p, int grid) {
+  chain_wait();
+  const int lane = threadIdx.x & 31;
+  const long long task = static_cast<long long>(blockIdx.x) * kJoinWarps + (threadIdx.x >> 5);
+  const long long t = task / p.q_heads;
+  const int h = static_cast<int>(task - t * p.q_heads);
+  if (t >= p.N) return;
+  int mine = -1;
+  for (int i0 = 0; i0 < p.n && mine < 0; i0 += 32) {
+    const int i = i0 + lane;
+    const unsigned b = __ballot_sync(0xffffffffu, i < p.n && p.start[i] <= t && t < p.start[i + 1]);
+    if (b) mine = i0 + __ffs(b) - 1;
+  }
+  if (mine < 0) return;
+  const Entry en = tree_entry(p, mine, p.status);
+  if (en.nodes == 0) return;
+  const int head = h / p.group, r = static_cast<int>(t - en.first) * p.group + (h - head * p.group);
+  const int r0 = r & ~(2 * kRows - 1);
+  long long u0 = p.unit_base[mine];
+  for (int x = 0; x < r0; x += 2 * kRows) u0 += static_cast<long long>(tiles_of(item_total(p, en, x))) * p.c.heads;
+  const int nt = tiles_of(item_total(p, en, r0));
+  u0 += static_cast<long long>(head) * nt;
+  const long long each = (p.unit_base[p.n] + grid - 1) / grid;
+  const int c0 = static_cast<int>(u0 / each), c1 = static_cast<int>((u0 + nt - 1) / each);
+  if (c0 == c1) return;  // written by the one CTA that had it all
+  const int stride = p.dim + 4;
+  auto piece = [&](int c) {
+    return p.part + ((static_cast<long long>(c) * 2 + (c * each >= u0 ? 0 : 1)) * p.part_rows + (r - r0)) * stride;
+  };
+  float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int c = c0 + lane; c <= c1; c += 32) m = fmaxf(m, piece(c)[0]);
+#pragma unroll
+  for (int x = 16; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+  const float off = m == -INFINITY ? 0.f : m;
+  for (int c = c0; c <= c1; ++c) {
+    const float* const x = piece(c);
+    const float pm = x[0], pl = x[1];
+    if (pl == 0.f) continue;
+    const float k = pm == -INFINITY ? 1.f : fast_exp2((pm - off) * p.scale);  // a sum without a maximum is NaN
+    l = fmaf(pl, k, l);
+    if (lane * 4 < p.dim) {
+      const float4 f = *reinterpret_cast<const float4*>(x + 4 + lane * 4);
+      o[0] = fmaf(f.x, k, o[0]), o[1] = fmaf(f.y, k, o[1]), o[2] = fmaf(f.z, k, o[2]), o[3] = fmaf(f.w, k, o[3]);
+    }
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const long long row = t * p.q_heads + h;
+  if (lane * 4 < p.dim)
+    *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + row * p.dim + lane * 4) =
+        make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
+  if (lane == 0) p.lse[row] = l == 0.f ? -INFINITY : fmaf(m, p.scale, log2f(l)) * kLn2;
+}
+
+}  // namespace
+
+int tree_part_rows(long long N, int group) {
+  return static_cast<int>(N * group < 2 * kRows ? N * group : 2 * kRows);
+}
+
+cudaError_t launch_tree_bf16(const TreeParams& p, cudaStream_t s) {
+  const int grid = p.sms;
+  if (p.dim > 64) tree_kernel<2><<<grid, kThreads, kSmem, s>>>(p);
+  else tree_kernel<1><<<grid, kThreads, kSmem, s>>>(p);
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  return launch_chained(tree_join_kernel, dim3(static_cast<unsigned>((p.N * p.q_heads + kJoinWarps - 1) / kJoinWarps)),
+                        dim3(32 * kJoinWarps), 0, s, p, grid);
+}
+
+cudaError_t setup_tree_kernels() {
+  for (void (*kernel)(TreeParams) : {tree_kernel<1>, tree_kernel<2>}) {
+    cudaFuncAttributes fa;
+    cudaError_t e = cudaFuncGetAttributes(&fa, kernel);
+    if (e != cudaSuccess) return e;
+    // The split of registers between the roles waits forever unless the launch has just that many.
+    if (fa.numRegs != kLaunchRegs || fa.maxThreadsPerBlock < kThreads) return cudaErrorInvalidConfiguration;
+    if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem)) != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
+}  // namespace mls
