@@ -2018,14 +2018,18 @@ TreePlan tree_plan(const mls_cache* c, int n, int64_t N, int q_heads, int sms) {
   return pl;
 }
 
-// The cache's k or v as [layers * pages * heads][page_size][head_dim], in boxes of 64 values (128 bytes,
-// swizzled) of the tokens of one page, or of as many as a tile has.
-int encode_pages(CUtensorMap* map, const mls_cache* c, const void* ptr) {
-  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(c->head_dim), static_cast<cuuint64_t>(c->page_size),
-                              static_cast<cuuint64_t>(c->layers) * c->pages * c->kv_heads};
-  const cuuint64_t strides[2] = {dims[0] * 2, dims[0] * dims[1] * 2};
-  const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(c->page_size < 128 ? c->page_size : 128), 1}, estr[3] = {1, 1, 1};
-  const CUresult r = g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), dims, strides, box, estr,
+// The cache's k or v as [layers * pages * heads][page_size][head_dim], in boxes (128 bytes wide, swizzled) of
+// the tokens of one page, or of as many as a tile has: 64 values of each, or, where a token has 128, all of them,
+// the two halves of 8 tokens behind one another.
+int encode_pages(CUtensorMap* map, const mls_cache* c, const void* ptr, bool joint) {
+  const cuuint64_t dim = c->head_dim, size = c->page_size, all = static_cast<cuuint64_t>(c->layers) * c->pages * c->kv_heads;
+  const cuuint32_t tokens = static_cast<cuuint32_t>(c->page_size < 128 ? c->page_size : 128);
+  const cuuint64_t dims[5] = {64, 8, 2, size / 8, all}, strides[4] = {dim * 2, 128, dim * 16, dim * size * 2};
+  const cuuint32_t box[5] = {64, 8, 2, tokens / 8, 1}, estr[5] = {1, 1, 1, 1, 1};
+  const cuuint64_t dims3[3] = {dim, size, all}, strides3[2] = {dim * 2, dim * size * 2};
+  const cuuint32_t box3[3] = {64, tokens, 1};
+  const CUresult r = g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, joint ? 5 : 3, const_cast<void*>(ptr),
+                              joint ? dims : dims3, joint ? strides : strides3, joint ? box : box3, estr,
                               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? MLS_OK : fail(MLS_ERR_CUDA, "cuTensorMapEncodeTiled (cache)");
@@ -2082,7 +2086,9 @@ extern "C" int mls_tree_attention(const mls_cache* c, int32_t layer, int32_t n, 
   p.splits = pl.splits;
   p.status = dev->status;
   p.sms = dev->sms;
-  if (c->dtype == MLS_BF16 && (encode_pages(&p.map_k, c, c->k) || encode_pages(&p.map_v, c, c->v))) return MLS_ERR_CUDA;
+  p.joint = c->dtype == MLS_BF16 && c->head_dim == 128;
+  if (c->dtype == MLS_BF16 && (encode_pages(&p.map_k, c, c->k, p.joint) || encode_pages(&p.map_v, c, c->v, p.joint)))
+    return MLS_ERR_CUDA;
   return timed("tree_attention", s,
                [&] { return c->dtype == MLS_FP32 ? launch_tree_fp32(p, s) : launch_tree_bf16(p, s); });
 }

@@ -578,7 +578,8 @@ cudaError_t setup_cache_kernels();
 // ------------------------------------------------------------------ tree attention
 struct TreeParams {
   CacheView c;
-  CUtensorMap map_k, map_v;      // bf16: boxes of 64 values of one head and page
+  CUtensorMap map_k, map_v;      // bf16: boxes of one head and page, of 64 values a token or (joint) 128
+  int joint;
   int layer, n;
   long long N;
   int q_heads, group;            // group = query heads of a key/value head

@@ -38,114 +38,157 @@ constexpr float kGrow = 8.f;
 constexpr int kMaxStages = 12;
 constexpr uint32_t kSmem = 227 * 1024;
 
+// A piece of an item, for every role: rows [r0, r0 + nrows) of an entry and head, key tiles [t0, t1) of nt.
+struct Seg {
+  long long first;                                // of the entry's nodes
+  int nodes, row, len;                            // its nodes, row of the table (-1: none takes part) and cached tokens
+  int head, r0, nrows, t0, t1, nt;                // t0 = t1: the end
+  int total;                                      // keys of the item: cached tokens and nodes up to its last
+  int all;                                        // keys that every row sees
+  int slot;                                       // of the CTA's two in the workspace
+};
+constexpr int kSegs = 4;
+constexpr int kSegReaders = 3 + 8;                // load, MMA and query warp, eight of softmax
 // Past the operands.  A warpgroup's `up` and `ml` share memory: parents are read before any sum is.
 struct Tail {
-  uint64_t full[kMaxStages], empty[kMaxStages], q_ready[2], s_full[2], p_ready[2], o_full[2], drain;
+  uint64_t full[kMaxStages], empty[kMaxStages], q_ready[2], q_free[2], s_full[2], p_ready[2], o_full[2], met, drain;
+  uint64_t seg_full[kSegs], seg_empty[kSegs];
+  Seg seg[kSegs];
   union {
     short up[kTreeMaxNodes];
     float2 ml[kRows];
   } row[2];
   long long scan[kThreads / 32], base0;
-  int e0, fix[2], abort;
+  int e0, abort;
+  int fix[2];                                     // by a segment's parity: the last one with values taken out
   uint32_t tmem_slot;
 };
-template <int DC>
-struct Layout {                                   // DC: pieces of 64 values of a row
+// DC: pieces of 64 values (128 bytes) of a row.  K and V tiles lie in atoms of 8 rows of 128 bytes; of rows of
+// 128 values (kJoint) the two pieces' atoms alternate, so that one TMA box brings a page.
+template <int DC, bool kJoint>
+struct Layout {
   static constexpr uint32_t kTile = DC * kKeys * 128u;
   static constexpr int kStages = DC == 2 ? 5 : 12;
   static constexpr uint32_t kRing = 2 * kTile, kTail = kRing + kStages * kTile;
+  static constexpr uint32_t kAtom = kJoint ? 2048u : 1024u;         // between atoms of rows
+  static constexpr uint32_t kPiece = kJoint ? 1024u : kKeys * 128u; // between pieces
   static_assert(kTail + sizeof(Tail) <= kSmem, "shared memory");
+  static_assert(!kJoint || DC == 2, "two pieces");
+  // Where 16 bytes of a tile lie: row, and which of the row's (not swizzled).
+  static __device__ __forceinline__ uint32_t at(int row, int c) {
+    return (row >> 3) * kAtom + (row & 7) * 128u + (c >> 3) * kPiece + ((c & 7) << 4);
+  }
 };
 
-// A piece of an item: rows [r0, r0 + nrows) of an entry and head, key tiles [t0, t1) of nt.
-struct Seg {
-  Entry en;
-  int e, head, r0, nrows, t0, t1, nt;
-  int total;                                      // keys of the item: cached tokens and nodes up to its last
-  int all;                                        // keys that every row sees
-  bool first;                                     // of this CTA
-};
 // Key tiles of rows [r0, r0 + 256) of an entry.
 __device__ __forceinline__ int item_total(const TreeParams& p, const Entry& en, int r0) {
   const int rows = min(en.nodes * p.group - r0, 2 * kRows);
   return en.len + (r0 + rows - 1) / p.group + 1;
 }
 __device__ __forceinline__ int tiles_of(int total) { return (total + kKeys - 1) / kKeys; }
+// Units of work: an item's tiles, and kOver more for its beginning and end.
+constexpr int kOver = 1;
 __device__ long long entry_units(const TreeParams& p, const Entry& en) {
   long long sum = 0;
-  for (int r0 = 0; r0 < en.nodes * p.group; r0 += 2 * kRows) sum += tiles_of(item_total(p, en, r0));
+  for (int r0 = 0; r0 < en.nodes * p.group; r0 += 2 * kRows) sum += kOver + tiles_of(item_total(p, en, r0));
   return sum * p.c.heads;
 }
 
-// Walks the segments of units [at, hi); entry e begins at unit `base`.
-struct Walker {
-  long long at, hi, base;
-  int e;
+__device__ __forceinline__ bool wait(const TreeParams& p, Tail* sh, uint64_t* bar, uint32_t parity) {
+  return mbar_wait(smem_u32(bar), parity, &sh->abort, p.status);
+}
+
+// One thread: writes down the segments of units [at, hi), entry e beginning at unit `base`.
+__device__ void plan_role(const TreeParams& p, Tail* sh, long long at, long long hi, int e, long long base) {
+  uint32_t k = 0;
+  bool first = true;
+  auto slot = [&]() -> Seg* {
+    return wait(p, sh, &sh->seg_empty[k % kSegs], ((k / kSegs) & 1u) ^ 1u) ? &sh->seg[k % kSegs] : nullptr;
+  };
   Entry en;
-  long long units;
-  bool first;
-  __device__ Walker(const TreeParams& p, long long lo, long long hi_, int e0, long long base0)
-      : at(lo), hi(hi_), base(base0), e(e0), first(true) {
-    units = 0;
-    if (at < hi) {
-      en = tree_entry(p, e, p.status);
-      units = entry_units(p, en);
-    }
+  long long units = 0;
+  if (at < hi) {
+    en = tree_entry(p, e, p.status);
+    units = entry_units(p, en);
   }
-  __device__ bool next(const TreeParams& p, Seg& g) {
-    if (at >= hi) return false;
+  while (at < hi) {
     while (at - base >= units) {
       base += units;
       en = tree_entry(p, ++e, p.status);
       units = entry_units(p, en);
     }
     long long v = at - base;
-    g.r0 = 0;
+    int r0 = 0, total, nt;
     while (true) {
-      g.total = item_total(p, en, g.r0);
-      g.nt = tiles_of(g.total);
-      const long long here = static_cast<long long>(g.nt) * p.c.heads;
+      total = item_total(p, en, r0);
+      nt = tiles_of(total);
+      const long long here = static_cast<long long>(nt + kOver) * p.c.heads;
       if (v < here) break;
       v -= here;
-      g.r0 += 2 * kRows;
+      r0 += 2 * kRows;
     }
-    g.head = static_cast<int>(v / g.nt);
-    g.t0 = static_cast<int>(v - static_cast<long long>(g.head) * g.nt);
-    g.t1 = static_cast<int>(min(static_cast<long long>(g.nt), g.t0 + (hi - at)));
-    g.nrows = min(en.nodes * p.group - g.r0, 2 * kRows);
-    g.all = en.row < 0 ? 0 : p.parents ? en.len : en.len + g.r0 / p.group + 1;
-    g.en = en;
-    g.e = e;
-    g.first = first;
+    const int head = static_cast<int>(v / (nt + kOver)), in = static_cast<int>(v - static_cast<long long>(head) * (nt + kOver));
+    const int end = static_cast<int>(min(static_cast<long long>(nt + kOver), in + (hi - at)));
+    at += end - in;
+    const int t0 = max(in - kOver, 0), t1 = end - kOver;
+    if (t1 <= t0) continue;                       // the range ends before the item's first tile
+    Seg* const g = slot();
+    if (!g) return;
+    g->first = en.first;
+    g->nodes = en.nodes;
+    g->row = en.row;
+    g->len = en.len;
+    g->head = head;
+    g->r0 = r0;
+    g->nrows = min(en.nodes * p.group - r0, 2 * kRows);
+    g->t0 = t0;
+    g->t1 = t1;
+    g->nt = nt;
+    g->total = total;
+    g->all = en.row < 0 ? 0 : p.parents ? en.len : en.len + r0 / p.group + 1;
+    g->slot = first ? 0 : 1;
     first = false;
-    at += g.t1 - g.t0;
-    return true;
+    mbar_arrive(smem_u32(&sh->seg_full[k++ % kSegs]));
   }
-};
+  if (Seg* const g = slot()) {
+    g->t0 = g->t1 = 0;
+    mbar_arrive(smem_u32(&sh->seg_full[k % kSegs]));
+  }
+}
+// The k-th segment for one of its readers (false: there is none, or a wait ran out).
+__device__ __forceinline__ bool read_seg(const TreeParams& p, Tail* sh, uint32_t k, Seg& g) {
+  if (!wait(p, sh, &sh->seg_full[k % kSegs], (k / kSegs) & 1u)) return false;
+  g = sh->seg[k % kSegs];
+  return g.t1 > g.t0;
+}
+__device__ __forceinline__ void free_seg(Tail* sh, uint32_t k) { mbar_arrive(smem_u32(&sh->seg_empty[k % kSegs])); }
 
 // Where the K and V tiles of step j lie in the order in which a segment of n tiles is loaded: K0 V0 K1 V1 ...
 // for two row tiles, K0 K1 V0 K2 V1 K3 ... for two streams of key tiles, as the MMAs take them.
 __device__ __forceinline__ uint32_t place_k(int j, bool pair) { return pair ? 2 * j : j < 2 ? j : 2 * j - 1; }
 __device__ __forceinline__ uint32_t place_v(int j, int n, bool pair) { return pair ? 2 * j + 1 : min(2 * j + 2, 2 * n - 1); }
 
-template <int DC>
-__device__ void load_role(const TreeParams& p, Tail* sh, uint32_t base, Walker it) {
-  using L = Layout<DC>;
+template <int DC, bool kJoint>
+__device__ void load_role(const TreeParams& p, Tail* sh, uint32_t base) {
+  using L = Layout<DC, kJoint>;
   const int lane = threadIdx.x & 31;
   const int size = 1 << p.c.page_shift, box = min(size, kKeys), boxes = kKeys / box;
-  const int mine = lane / DC, half = lane - mine * DC;        // this lane's box of a tile: boxes * DC <= 32
+  constexpr int kParts = kJoint ? 1 : DC;                     // boxes of a page
+  const int mine = lane / kParts, part = lane - mine * kParts;  // this lane's box of a tile: boxes * kParts <= 32
   const bool active = mine < boxes;
   const int none = p.c.layers * p.c.pages * p.c.heads;        // a box there is filled with zeros
-  const uint32_t dst = half * (kKeys * 128u) + mine * box * 128u;
+  const uint32_t dst = part * L::kPiece + mine * (box >> 3) * L::kAtom;
   uint32_t ring = 0;
   bool ok = true;
   Seg g;
-  while (ok && it.next(p, g)) {
+  for (uint32_t k = 0; ok && (ok = __all_sync(0xffffffffu, read_seg(p, sh, k, g))); ++k) {
+    __syncwarp();
+    if (lane == 0) free_seg(sh, k);
     const int n = g.t1 - g.t0;
     const bool pair = g.nrows > kRows;
-    const int* const table = g.en.row < 0 ? nullptr : p.c.table + static_cast<long long>(g.en.row) * p.c.max_pages;
+    const int* const table = g.row < 0 ? nullptr : p.c.table + static_cast<long long>(g.row) * p.c.max_pages;
     for (int i = 0; i < 2 * n; ++i, ++ring) {
-      // The i-th load of the segment: K of step kj, or V of step vj.
+      // The i-th load of the segment: the K or the V tile of step j.
       int j;
       bool is_v;
       if (pair) {
@@ -161,7 +204,7 @@ __device__ void load_role(const TreeParams& p, Tail* sh, uint32_t base, Walker i
         is_v = !(i & 1);
         j = is_v ? (i - 2) >> 1 : (i + 1) >> 1;
       }
-      const int pos = (g.t0 + j) * kKeys + mine * box;
+      const int pos = (g.t0 + j) * kKeys + mine * box, slot = pos & (size - 1);
       int at = none;
       if (active && table && pos < g.total) {
         const int page = table[pos >> p.c.page_shift];
@@ -169,67 +212,111 @@ __device__ void load_role(const TreeParams& p, Tail* sh, uint32_t base, Walker i
         else atomicOr(p.status, kStatusBadSeq);
       }
       const uint32_t stage = ring % L::kStages, phase = (ring / L::kStages) & 1u;
-      ok = mbar_wait(smem_u32(&sh->empty[stage]), phase ^ 1u, &sh->abort, p.status);
-      ok = __all_sync(0xffffffffu, ok);
+      ok = __all_sync(0xffffffffu, wait(p, sh, &sh->empty[stage], phase ^ 1u));
       if (!ok) break;
-      const uint32_t bar = smem_u32(&sh->full[stage]);
+      const uint32_t bar = smem_u32(&sh->full[stage]), to = base + L::kRing + stage * L::kTile + dst;
       if (lane == 0) mbar_arrive_expect_tx(bar, L::kTile);
       __syncwarp();
-      if (active)
-        tma_load_3d(base + L::kRing + stage * L::kTile + dst, is_v ? &p.map_v : &p.map_k, bar, half * 64,
-                    pos & (size - 1), at);
+      const CUtensorMap* const map = is_v ? &p.map_v : &p.map_k;
+      if (active) {
+        if (kJoint) tma_load_5d(to, map, bar, 0, 0, 0, slot >> 3, at);
+        else tma_load_3d(to, map, bar, part * 64, slot, at);
+      }
     }
   }
-  if (!ok && lane == 0)  // what was asked for lands before the shared memory goes away
+  if (lane == 0)  // what was asked for lands before the shared memory goes away
     for (uint32_t b = ring > L::kStages ? ring - L::kStages : 0; b < ring; ++b)
       mbar_wait_drain(smem_u32(&sh->full[b % L::kStages]), (b / L::kStages) & 1u, kDrainNs, p.status);
   __syncwarp();
 }
 
+// One warp: queries of each stream's rows, swizzled as TMA would, zeros where there is no row or value.
 template <int DC>
-__device__ void mma_role(const TreeParams& p, Tail* sh, uint32_t base, uint32_t tmem, Walker it) {
-  using L = Layout<DC>;
-  const uint32_t idesc_s = make_idesc(kRows, kKeys, false, false, false);
+__device__ void query_role(const TreeParams& p, Tail* sh, uint32_t base) {
+  constexpr int kWide = DC * 8, kStep = 32 / kWide;           // pieces of 16 bytes of a row, rows at a time
+  const int lane = threadIdx.x & 31, c = lane % kWide;
+  uint32_t free_par = 0;                                      // a bit a stream
+  Seg g;
+  for (uint32_t k = 0; __all_sync(0xffffffffu, read_seg(p, sh, k, g)); ++k) {
+    __syncwarp();
+    if (lane == 0) free_seg(sh, k);
+    const int n = g.t1 - g.t0;
+    const bool pair = g.nrows > kRows;
+    for (int w = 0; w < 2; ++w) {
+      if (!pair && w == 1 && n < 2) continue;
+      wait(p, sh, &sh->q_free[w], ((free_par >> w) & 1u) ^ 1u);
+      free_par ^= 1u << w;
+      const int row0 = pair ? w * kRows : 0, last = g.r0 + g.nrows;
+      int r = g.r0 + row0 + lane / kWide, t = r / p.group, h = r - t * p.group;
+      const __nv_bfloat16* const q = static_cast<const __nv_bfloat16*>(p.q) + g.first * p.q_ld +
+                                     static_cast<long long>(g.head) * p.group * p.dim + c * 8;
+      uint32_t to = base + w * DC * kRows * 128u + (c >> 3) * (kRows * 128u) + (lane / kWide) * 128u;
+#pragma unroll 4
+      for (int i = lane / kWide; i < kRows; i += kStep) {
+        const bool in = r < last && c * 8 < p.dim;
+        cp_async_16(to + (((c & 7) ^ (i & 7)) << 4), in ? q + t * p.q_ld + static_cast<long long>(h) * p.dim : p.q, in);
+        to += kStep * 128u;
+        r += kStep;
+        h += kStep;
+        while (h >= p.group) {
+          h -= p.group;
+          ++t;
+        }
+      }
+      cp_async_wait_all();
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&sh->q_ready[w]));
+    }
+  }
+}
+
+template <int DC, bool kJoint>
+__device__ void mma_role(const TreeParams& p, Tail* sh, uint32_t base, uint32_t tmem) {
+  using L = Layout<DC, kJoint>;
+  constexpr uint32_t kNegateA = 1u << 13;
+  const uint32_t idesc_s = make_idesc(kRows, kKeys, false, false, false) | (p.negate ? kNegateA : 0u);
   const int dn = (p.dim + 15) & ~15;
   const uint32_t idesc_o = make_idesc(kRows, dn, false, false, true);
   const int ks = dn / 16;
   uint32_t ring = 0, q_par = 0, p_par = 0;  // a bit a stream
   bool ok = true;
-  auto wait = [&](uint64_t* bar, uint32_t parity) {
-    ok = ok && mbar_wait(smem_u32(bar), parity, &sh->abort, p.status);
+  auto ready = [&](uint64_t* bar, uint32_t parity) {
+    ok = ok && wait(p, sh, bar, parity);
     tc_fence_after();
     return ok;
   };
   Seg g;
-  while (ok && it.next(p, g)) {
+  for (uint32_t k = 0; ok && read_seg(p, sh, k, g); ++k) {
+    free_seg(sh, k);
     const int n = g.t1 - g.t0;
     const bool pair = g.nrows > kRows;
     const int steps[2] = {pair ? n : (n + 1) / 2, pair ? n : n / 2};
     auto scores = [&](int w, int i) {
       const uint32_t at = ring + place_k(pair ? i : 2 * i + w, pair), stage = at % L::kStages;
-      if (!wait(&sh->full[stage], (at / L::kStages) & 1u)) return;
-      const uint64_t a = make_sdesc(base + w * L::kTile, 16), b = make_sdesc(base + L::kRing + stage * L::kTile, 16);
-      for (int k = 0; k < ks; ++k) {
-        const uint64_t step = (k >> 2) * (kKeys * 128 / 16) + (k & 3) * 2;
-        mma_issue<false>(tmem + w * kKeys, a + step, b + step, idesc_s, k > 0);
-      }
+      if (!ready(&sh->full[stage], (at / L::kStages) & 1u)) return;
+      const uint64_t a = make_sdesc(base + w * L::kTile, 16), b = make_sdesc(base + L::kRing + stage * L::kTile, 16, L::kAtom);
+      for (int x = 0; x < ks; ++x)
+        mma_issue<false>(tmem + w * kKeys, a + (x >> 2) * (kRows * 128 / 16) + (x & 3) * 2,
+                         b + (x >> 2) * (L::kPiece / 16) + (x & 3) * 2, idesc_s, x > 0);
       if (!pair || w == 1) mma_commit(smem_u32(&sh->empty[stage]));
       mma_commit(smem_u32(&sh->s_full[w]));
+      if (i + 1 == steps[w]) mma_commit(smem_u32(&sh->q_free[w]));
     };
     for (int w = 0; w < 2; ++w)
-      if (steps[w] > 0 && wait(&sh->q_ready[w], (q_par >> w) & 1u)) {
+      if (steps[w] > 0 && ready(&sh->q_ready[w], (q_par >> w) & 1u)) {
         q_par ^= 1u << w;
         scores(w, 0);
       }
     for (int i = 0; ok && i < steps[0]; ++i)
       for (int w = 0; ok && w < 2; ++w) {
-        if (i >= steps[w] || !wait(&sh->p_ready[w], (p_par >> w) & 1u)) continue;
+        if (i >= steps[w] || !ready(&sh->p_ready[w], (p_par >> w) & 1u)) continue;
         p_par ^= 1u << w;
         const uint32_t at = ring + place_v(pair ? i : 2 * i + w, n, pair), stage = at % L::kStages;
-        if (!wait(&sh->full[stage], (at / L::kStages) & 1u)) break;
-        const uint64_t b = make_sdesc(base + L::kRing + stage * L::kTile, kKeys * 128);
-        for (int k = 0; k < kKeys / 16; ++k)
-          mma_issue_ts(tmem + kAccO + w * 128, tmem + w * kKeys + k * 8, b + k * (16 * 128 / 16), idesc_o, i > 0 || k > 0);
+        if (!ready(&sh->full[stage], (at / L::kStages) & 1u)) break;
+        const uint64_t b = make_sdesc(base + L::kRing + stage * L::kTile, L::kPiece, L::kAtom);
+        for (int x = 0; x < kKeys / 16; ++x)
+          mma_issue_ts(tmem + kAccO + w * 128, tmem + w * kKeys + x * 8, b + x * (2 * L::kAtom / 16), idesc_o, i > 0 || x > 0);
         if (!pair || w == 1) mma_commit(smem_u32(&sh->empty[stage]));
         if (i + 1 < steps[w]) scores(w, i + 1);
         else mma_commit(smem_u32(&sh->o_full[w]));
@@ -281,91 +368,73 @@ struct Sight {
   }
 };
 
-template <int DC>
-__device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint32_t tmem, int w, Walker it) {
-  using L = Layout<DC>;
-  const int tid = threadIdx.x & 127, quad = tid >> 5;
+template <int DC, bool kJoint>
+__device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint32_t tmem, int w) {
+  using L = Layout<DC, kJoint>;
+  const int tid = threadIdx.x & 127, quad = tid >> 5, lane = tid & 31;
   const uint32_t lanes = static_cast<uint32_t>(quad * 32) << 16;
   const uint32_t ts = tmem + lanes + w * kKeys, to = tmem + lanes + kAccO + w * 128;
-  const int width = p.dim >> 3;                   // pieces of a row
   const __nv_bfloat16* const V = reinterpret_cast<const __nv_bfloat16*>(p.c.v);
   const int mask = (1 << p.c.page_shift) - 1;
-  uint32_t ring = 0, s_par = 0, o_par = 0;
+  uint32_t ring = 0, s_par = 0, o_par = 0, met = 0;
+  auto meet = [&] {                               // both streams (a wait with a limit, unlike a barrier)
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_u32(&sh->met));
+    wait(p, sh, &sh->met, met);
+    met ^= 1u;
+  };
+  Sight see;
+  long long had_first = -1;                       // whose `see` this is
+  int had_row = -1, had_r0 = -1;
   Seg g;
-  while (it.next(p, g)) {
+  for (uint32_t k = 0;; ++k) {
+    const int seg = static_cast<int>(k) + 1;
+    // All of a warpgroup go on or leave together: the barriers below need all of them.
+    if (!named_bar_and(1 + w, kRows, read_seg(p, sh, k, g))) break;
+    if (lane == 0) free_seg(sh, k);
     const int n = g.t1 - g.t0;
     const bool pair = g.nrows > kRows;
     const int steps = pair ? n : (n + 1 - w) / 2;
     const int rl = (pair ? w * kRows : 0) + tid;  // this thread's row of the item
     const bool inside = rl < g.nrows;
     const int r = g.r0 + rl, node = inside ? r / p.group : 0;
-    const int* const table = p.c.table + static_cast<long long>(max(g.en.row, 0)) * p.c.max_pages;
-    Sight see;
-    see.tree = p.parents != nullptr;
-    see.len = g.en.len;
-    see.upto = g.en.len + node + 1;
-    see.used = inside && g.en.row >= 0;
-    if (see.tree) {
-      short* const up = sh->row[w].up;
-      const int nodes = g.en.row < 0 ? 0 : g.en.nodes;
-      for (int j = tid; j < nodes; j += kRows) {
-        const int u = p.parents[g.en.first + j];
-        const bool odd = u < -2 || u >= j;
-        if (odd) atomicOr(p.status, kStatusBadSeq);
-        up[j] = static_cast<short>(odd ? -2 : u);
-      }
-      named_bar_sync(1 + w, kRows);
-#pragma unroll
-      for (int i = 0; i < kTreeMaxNodes / 32; ++i) see.path[i] = 0u;
-      if (see.used) {
-        see.used = up[node] >= -1;
-        for (int j = node; j >= 0 && up[j] >= -1; j = up[j])
-#pragma unroll
-          for (int i = 0; i < kTreeMaxNodes / 32; ++i)
-            if (i == j >> 5) see.path[i] |= 1u << (j & 31);
-      }
-      named_bar_sync(1 + w, kRows);
-    }
-    if (steps > 0) {
-      // Queries of this stream's rows, swizzled as TMA would, zeros where there is no row or value.
-      const uint32_t flip = p.negate ? 0x80008000u : 0u;
-      const int row0 = g.r0 + (pair ? w * kRows : 0);
-      const __nv_bfloat16* const q = static_cast<const __nv_bfloat16*>(p.q) + g.en.first * p.q_ld +
-                                     static_cast<long long>(g.head) * p.group * p.dim;
-#pragma unroll 4
-      for (int x = tid; x < kRows * DC * 8; x += kRows) {
-        const int row = x / (DC * 8), c = x - row * (DC * 8);
-        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if (row0 + row < g.r0 + g.nrows && c < width) {
-          const int t = (row0 + row) / p.group, h = row0 + row - t * p.group;
-          v = ld16(q + t * p.q_ld + static_cast<long long>(h) * p.dim + c * 8);
-          v.x ^= flip, v.y ^= flip, v.z ^= flip, v.w ^= flip;
+    const int* const table = p.c.table + static_cast<long long>(max(g.row, 0)) * p.c.max_pages;
+    if (g.first != had_first || g.row != had_row || g.r0 != had_r0) {  // other heads of the same rows see the same
+      had_first = g.first;
+      had_row = g.row;
+      had_r0 = g.r0;
+      see.tree = p.parents != nullptr;
+      see.len = g.len;
+      see.upto = g.len + node + 1;
+      see.used = inside && g.row >= 0;
+      if (see.tree) {
+        short* const up = sh->row[w].up;
+        const int nodes = g.row < 0 ? 0 : g.nodes;
+        for (int j = tid; j < nodes; j += kRows) {
+          const int u = p.parents[g.first + j];
+          const bool odd = u < -2 || u >= j;
+          if (odd) atomicOr(p.status, kStatusBadSeq);
+          up[j] = static_cast<short>(odd ? -2 : u);
         }
-        st_shared_v4(base + w * L::kTile + (c >> 3) * (kRows * 128u) + row * 128u + (((c & 7) ^ (row & 7)) << 4), v.x, v.y,
-                     v.z, v.w);
+        named_bar_sync(1 + w, kRows);
+#pragma unroll
+        for (int i = 0; i < kTreeMaxNodes / 32; ++i) see.path[i] = 0u;
+        if (see.used) {
+          see.used = up[node] >= -1;
+          for (int j = node; j >= 0 && up[j] >= -1; j = up[j])
+#pragma unroll
+            for (int i = 0; i < kTreeMaxNodes / 32; ++i)
+              if (i == j >> 5) see.path[i] |= 1u << (j & 31);
+        }
+        named_bar_sync(1 + w, kRows);
       }
-      fence_proxy_async_smem();
-      mbar_arrive(smem_u32(&sh->q_ready[w]));
     }
     const bool busy = (pair ? w * kRows : 0) + quad * 32 < g.nrows;  // rows of this warp
     float m = -INFINITY, l = 0.f;
-    bool fix = false;
     for (int i = 0; i < steps; ++i) {
       const int j = pair ? i : 2 * i + w, k0 = (g.t0 + j) * kKeys;
       const bool masked = k0 + kKeys > g.all;
-      bool odd = false;
-      if (masked && g.en.row >= 0) {              // infinities and NaN among values that not every row sees
-        const int a = max(g.all, k0), b = min(g.total, k0 + kKeys);
-        for (int x = tid; x < (b - a) * width; x += kRows) {
-          const int k = a + x / width, c = x % width;
-          const int page = table[k >> p.c.page_shift];
-          if (page >= 0 && page < p.c.pages)
-            odd |= odd_any(ld16(V + cache_at(p.c, p.layer, page, g.head, k & mask) * 8 + c * 8));
-        }
-        odd = !named_bar_and(1 + w, kRows, !odd);
-        fix |= odd;
-      }
-      mbar_wait(smem_u32(&sh->s_full[w]), s_par, &sh->abort, p.status);
+      wait(p, sh, &sh->s_full[w], s_par);
       s_par ^= 1u;
       tc_fence_after();
       if (busy) {
@@ -422,56 +491,54 @@ __device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint3
         tmem_st_wait();
       }
       if (masked) {
+        // Values that not every row sees: infinities and NaN become 0, to be added to the rows that see them at
+        // the end.  Those behind the last key, up to the end of its page, become 0 (the pages behind it came as
+        // zeros).  Where the other stream has the same tile, one of the two finds what there is: it says so before
+        // it clears anything, and the other, which looks at `fix` when both are through, has seen either.
         const uint32_t at = ring + place_v(j, n, pair), stage = at % L::kStages;
         const uint32_t tile = base + L::kRing + stage * L::kTile;
-        // Values behind the last key, up to the end of its page: the pages behind it came as zeros.
-        const int a = min(max(g.total - k0, 0), kKeys);
-        const int b = min((g.total + mask & ~mask) - k0, kKeys);
-        if (b > a || odd) {
-          mbar_wait(smem_u32(&sh->full[stage]), (at / L::kStages) & 1u, &sh->abort, p.status);
-          for (int x = tid; x < (b - a) * DC * 8; x += kRows) {
-            const int row = a + x / (DC * 8), c = x % (DC * 8);
-            st_shared_v4(tile + (c >> 3) * (kKeys * 128u) + row * 128u + ((c & 7) << 4), 0u, 0u, 0u, 0u);
-          }
-          if (odd)
-            for (int x = tid; x < kKeys * DC * 8; x += kRows) {
-              const int row = x / (DC * 8), c = x % (DC * 8);
-              if (k0 + row < g.all) continue;
-              const uint32_t addr = tile + (c >> 3) * (kKeys * 128u) + row * 128u + ((c & 7) << 4);
-              uint32_t v[4];
-              asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                           : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
-                           : "r"(addr)
-                           : "memory");
+        const int a = max(g.all - k0, 0), b = min((g.total + mask & ~mask) - k0, kKeys), last = g.total - k0;
+        wait(p, sh, &sh->full[stage], (at / L::kStages) & 1u);
+        for (int x = a * DC * 8 + tid; x < b * DC * 8; x += kRows) {
+          const int row = x / (DC * 8), c = x % (DC * 8);
+          const uint32_t addr = tile + L::at(row, c);
+          uint4 v = make_uint4(0u, 0u, 0u, 0u);
+          if (row < last) {
+            v = ld_shared_v4(addr);
+            if (!odd_any(v)) continue;
+            *static_cast<volatile int*>(&sh->fix[seg & 1]) = seg;
+            __threadfence_block();
+            uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-              for (int y = 0; y < 4; ++y) {
-                if (odd_lo(v[y])) v[y] &= 0xffff0000u;
-                if (odd_hi(v[y])) v[y] &= 0x0000ffffu;
-              }
-              st_shared_v4(addr, v[0], v[1], v[2], v[3]);
+            for (int y = 0; y < 4; ++y) {
+              if (odd_lo(u[y])) u[y] &= 0xffff0000u;
+              if (odd_hi(u[y])) u[y] &= 0x0000ffffu;
             }
-          fence_proxy_async_smem();
+            v = make_uint4(u[0], u[1], u[2], u[3]);
+          }
+          st_shared_v4(addr, v.x, v.y, v.z, v.w);
         }
+        fence_proxy_async_smem();
+        __threadfence_block();
       }
       tc_fence_before();
-      mbar_arrive(smem_u32(&sh->p_ready[w]));
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&sh->p_ready[w]));
     }
     ring += 2 * n;
 
     // The end of a segment.  Streams of one row tile meet here: both read both accumulators, half of the columns
     // each, which is why neither goes on before the other has read.
     if (steps > 0) {
-      mbar_wait(smem_u32(&sh->o_full[w]), o_par, &sh->abort, p.status);
+      wait(p, sh, &sh->o_full[w], o_par);
       o_par ^= 1u;
     }
     float c_own = 1.f, c_other = 0.f, M = m, Lsum = l;
     if (!pair) {
       sh->row[w].ml[tid] = make_float2(m, l);
-      if (tid == 0) sh->fix[w] = fix;
       tc_fence_before();
-      named_bar_sync(3, 2 * kRows);
+      meet();
       const float2 o = sh->row[1 - w].ml[tid];
-      fix = sh->fix[0] || sh->fix[1];
       M = fmaxf(m, o.x);
       const float off = M == -INFINITY ? 0.f : M;
       c_own = l == 0.f ? 0.f : m == -INFINITY ? 1.f : fast_exp2((m - off) * p.scale);
@@ -480,13 +547,14 @@ __device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint3
       Lsum = (l == 0.f ? 0.f : l * c_own) + (o.y == 0.f ? 0.f : o.y * c_other);
     }
     tc_fence_after();
+    const bool fix = *static_cast<volatile int*>(&sh->fix[seg & 1]) == seg;
     const bool whole = g.t0 == 0 && g.t1 == g.nt;
     const float inv = whole ? (Lsum == 0.f || !see.used ? 0.f : 1.f / Lsum) : 1.f;
     const int chunks = (p.dim + 31) / 32;
     const int x0 = pair || w == 0 ? 0 : (chunks + 1) / 2, x1 = pair || w == 1 ? chunks : (chunks + 1) / 2;
-    const long long t = g.en.first + node;
+    const long long t = g.first + node;
     const long long out_row = t * p.q_heads + g.head * p.group + (r - node * p.group);
-    float* const part = p.part + ((static_cast<long long>(blockIdx.x) * 2 + (g.first ? 0 : 1)) * p.part_rows + rl) * (p.dim + 4);
+    float* const part = p.part + ((static_cast<long long>(blockIdx.x) * 2 + g.slot) * p.part_rows + rl) * (p.dim + 4);
     const uint32_t other = tmem + lanes + kAccO + (1 - w) * 128;
     const bool reads = (pair ? w * kRows : 0) + quad * 32 < g.nrows;
     if (reads) {
@@ -549,29 +617,35 @@ __device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint3
       else part[0] = M, part[1] = sum;
     }
     tc_fence_before();
-    if (!pair) named_bar_sync(3, 2 * kRows);
+    if (!pair) meet();
   }
 }
 
-template <int DC>
+template <int DC, bool kJoint>
 __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant__ TreeParams p) {
-  using L = Layout<DC>;
+  using L = Layout<DC, kJoint>;
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t base = smem_u32(smem);
   Tail* const sh = reinterpret_cast<Tail*>(smem + L::kTail);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
-    sh->abort = 0;
+    sh->abort = sh->fix[0] = sh->fix[1] = 0;
     for (int s = 0; s < L::kStages; ++s) {
       mbar_init(smem_u32(&sh->full[s]), 1);
       mbar_init(smem_u32(&sh->empty[s]), 1);
     }
     for (int w = 0; w < 2; ++w) {
-      mbar_init(smem_u32(&sh->q_ready[w]), kRows);
+      mbar_init(smem_u32(&sh->q_ready[w]), 1);
+      mbar_init(smem_u32(&sh->q_free[w]), 1);
       mbar_init(smem_u32(&sh->s_full[w]), 1);
-      mbar_init(smem_u32(&sh->p_ready[w]), kRows);
+      mbar_init(smem_u32(&sh->p_ready[w]), kRows / 32);
       mbar_init(smem_u32(&sh->o_full[w]), 1);
     }
+    for (int k = 0; k < kSegs; ++k) {
+      mbar_init(smem_u32(&sh->seg_full[k]), 1);
+      mbar_init(smem_u32(&sh->seg_empty[k]), kSegReaders);
+    }
+    mbar_init(smem_u32(&sh->met), 8);
     mbar_init(smem_u32(&sh->drain), 1);
     fence_barrier_init();
   }
@@ -606,7 +680,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
   if (blockIdx.x == 0 || (lo < hi && before <= lo && lo < before + mine)) {
     long long at = before;
     for (int i = i0; i < i1; ++i) {
-      const long long u = entry_units(p, tree_entry(p, i, p.status));
+      const long long u = i1 - i0 == 1 ? mine : entry_units(p, tree_entry(p, i, p.status));
       if (blockIdx.x == 0) p.unit_base[i] = at;
       if (at <= lo && lo < at + u) {
         sh->e0 = i;
@@ -616,19 +690,23 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
     }
   }
   __syncthreads();
-  const Walker it(p, lo, hi, sh->e0, sh->base0);
+  chain_trigger();  // every CTA of this launch is resident: the next kernel's cannot take their place
 
   if (warp < 4) {
     regs_decrease<kCtlRegs>();
     if (warp == 0) {
-      load_role<DC>(p, sh, base, it);
+      load_role<DC, kJoint>(p, sh, base);
     } else if (warp == 1) {
-      if (lane == 0) mma_role<DC>(p, sh, base, tmem, it);
-      __syncwarp();
+      if (lane == 0) mma_role<DC, kJoint>(p, sh, base, tmem);
+    } else if (warp == 2) {
+      if (lane == 0) plan_role(p, sh, lo, hi, sh->e0, sh->base0);
+    } else {
+      query_role<DC>(p, sh, base);
     }
+    __syncwarp();
   } else {
     regs_increase<kSoftmaxRegs>();
-    softmax_role<DC>(p, sh, base, tmem, (warp - 4) >> 2, it);
+    softmax_role<DC, kJoint>(p, sh, base, tmem, (warp - 4) >> 2);
   }
   tc_fence_before();
   __syncthreads();
@@ -638,59 +716,65 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
   }
 }
 
-// Joins the pieces of rows whose keys lie in several CTAs' ranges, in order.  A warp a node and head.
-constexpr int kJoinWarps = 4;
+// Joins the pieces of the items that lie in several CTAs' ranges, in order.  Every such item has a CTA whose
+// range begins inside it after none other does: blocks (CTA, part of its rows) of those have work.  A warp a row.
+constexpr int kJoinWarps = 8, kJoinParts = 8;
 __global__ void __launch_bounds__(32 * kJoinWarps) tree_join_kernel(TreeParams p, int grid) {
+  __shared__ int s_entry;
   chain_wait();
-  const int lane = threadIdx.x & 31;
-  const long long task = static_cast<long long>(blockIdx.x) * kJoinWarps + (threadIdx.x >> 5);
-  const long long t = task / p.q_heads;
-  const int h = static_cast<int>(task - t * p.q_heads);
-  if (t >= p.N) return;
-  int mine = -1;
-  for (int i0 = 0; i0 < p.n && mine < 0; i0 += 32) {
-    const int i = i0 + lane;
-    const unsigned b = __ballot_sync(0xffffffffu, i < p.n && p.start[i] <= t && t < p.start[i + 1]);
-    if (b) mine = i0 + __ffs(b) - 1;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const long long units = p.unit_base[p.n], each = (units + grid - 1) / grid;
+  const long long b = (blockIdx.x + 1) * each;    // where the range begins
+  if (b >= units) return;
+  if (threadIdx.x == 0) s_entry = -1;
+  __syncthreads();
+  for (int i = threadIdx.x; i < p.n; i += blockDim.x)
+    if (p.unit_base[i] <= b && b < p.unit_base[i + 1]) s_entry = i;  // one does
+  __syncthreads();
+  const Entry en = tree_entry(p, s_entry, p.status);
+  long long v = b - p.unit_base[s_entry];
+  int r0 = 0, nt;
+  while (true) {
+    nt = tiles_of(item_total(p, en, r0));
+    const long long here = static_cast<long long>(nt + kOver) * p.c.heads;
+    if (v < here) break;
+    v -= here;
+    r0 += 2 * kRows;
   }
-  if (mine < 0) return;
-  const Entry en = tree_entry(p, mine, p.status);
-  if (en.nodes == 0) return;
-  const int head = h / p.group, r = static_cast<int>(t - en.first) * p.group + (h - head * p.group);
-  const int r0 = r & ~(2 * kRows - 1);
-  long long u0 = p.unit_base[mine];
-  for (int x = 0; x < r0; x += 2 * kRows) u0 += static_cast<long long>(tiles_of(item_total(p, en, x))) * p.c.heads;
-  const int nt = tiles_of(item_total(p, en, r0));
-  u0 += static_cast<long long>(head) * nt;
-  const long long each = (p.unit_base[p.n] + grid - 1) / grid;
-  const int c0 = static_cast<int>(u0 / each), c1 = static_cast<int>((u0 + nt - 1) / each);
-  if (c0 == c1) return;  // written by the one CTA that had it all
-  const int stride = p.dim + 4;
-  auto piece = [&](int c) {
-    return p.part + ((static_cast<long long>(c) * 2 + (c * each >= u0 ? 0 : 1)) * p.part_rows + (r - r0)) * stride;
-  };
-  float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int c = c0 + lane; c <= c1; c += 32) m = fmaxf(m, piece(c)[0]);
+  const int head = static_cast<int>(v / (nt + kOver)), in = static_cast<int>(v - static_cast<long long>(head) * (nt + kOver));
+  if (in <= kOver) return;                        // it begins with the item's first tile
+  const long long first = b - in + kOver, last = first + nt - 1;  // units of the item's tiles
+  if (b - each > first) return;                   // another range begins inside the item before
+  const int c0 = blockIdx.x, c1 = static_cast<int>(last / each);
+  const int rows = min(en.nodes * p.group - r0, 2 * kRows), stride = p.dim + 4;
+  for (int r = blockIdx.y * kJoinWarps + warp; r < rows; r += kJoinWarps * gridDim.y) {
+    auto piece = [&](int c) {  // the item is the CTA's first if its range begins with or inside it
+      return p.part + ((static_cast<long long>(c) * 2 + (c * each >= first - kOver ? 0 : 1)) * p.part_rows + r) * stride;
+    };
+    float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int c = c0 + lane; c <= c1; c += 32) m = fmaxf(m, piece(c)[0]);
 #pragma unroll
-  for (int x = 16; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-  const float off = m == -INFINITY ? 0.f : m;
-  for (int c = c0; c <= c1; ++c) {
-    const float* const x = piece(c);
-    const float pm = x[0], pl = x[1];
-    if (pl == 0.f) continue;
-    const float k = pm == -INFINITY ? 1.f : fast_exp2((pm - off) * p.scale);  // a sum without a maximum is NaN
-    l = fmaf(pl, k, l);
-    if (lane * 4 < p.dim) {
-      const float4 f = *reinterpret_cast<const float4*>(x + 4 + lane * 4);
+    for (int x = 16; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+    const float off = m == -INFINITY ? 0.f : m;
+#pragma unroll 4
+    for (int c = c0; c <= c1; ++c) {
+      const float* const x = piece(c);
+      const float pm = x[0], pl = x[1];
+      float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (lane * 4 < p.dim) f = *reinterpret_cast<const float4*>(x + 4 + lane * 4);
+      if (pl == 0.f) continue;
+      const float k = pm == -INFINITY ? 1.f : fast_exp2((pm - off) * p.scale);  // a sum without a maximum is NaN
+      l = fmaf(pl, k, l);
       o[0] = fmaf(f.x, k, o[0]), o[1] = fmaf(f.y, k, o[1]), o[2] = fmaf(f.z, k, o[2]), o[3] = fmaf(f.w, k, o[3]);
     }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int node = (r0 + r) / p.group;
+    const long long row = (en.first + node) * p.q_heads + head * p.group + (r0 + r - node * p.group);
+    if (lane * 4 < p.dim)
+      *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + row * p.dim + lane * 4) =
+          make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
+    if (lane == 0) p.lse[row] = l == 0.f ? -INFINITY : fmaf(m, p.scale, log2f(l)) * kLn2;
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  const long long row = t * p.q_heads + h;
-  if (lane * 4 < p.dim)
-    *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + row * p.dim + lane * 4) =
-        make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
-  if (lane == 0) p.lse[row] = l == 0.f ? -INFINITY : fmaf(m, p.scale, log2f(l)) * kLn2;
 }
 
 }  // namespace
@@ -701,16 +785,18 @@ int tree_part_rows(long long N, int group) {
 
 cudaError_t launch_tree_bf16(const TreeParams& p, cudaStream_t s) {
   const int grid = p.sms;
-  if (p.dim > 64) tree_kernel<2><<<grid, kThreads, kSmem, s>>>(p);
-  else tree_kernel<1><<<grid, kThreads, kSmem, s>>>(p);
+  if (p.joint) tree_kernel<2, true><<<grid, kThreads, kSmem, s>>>(p);
+  else if (p.dim > 64) tree_kernel<2, false><<<grid, kThreads, kSmem, s>>>(p);
+  else tree_kernel<1, false><<<grid, kThreads, kSmem, s>>>(p);
   const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  return launch_chained(tree_join_kernel, dim3(static_cast<unsigned>((p.N * p.q_heads + kJoinWarps - 1) / kJoinWarps)),
-                        dim3(32 * kJoinWarps), 0, s, p, grid);
+  const int parts = (p.part_rows + kJoinWarps - 1) / kJoinWarps;
+  return launch_chained(tree_join_kernel, dim3(grid - 1, parts < kJoinParts ? parts : kJoinParts), dim3(32 * kJoinWarps),
+                        0, s, p, grid);
 }
 
 cudaError_t setup_tree_kernels() {
-  for (void (*kernel)(TreeParams) : {tree_kernel<1>, tree_kernel<2>}) {
+  for (void (*kernel)(TreeParams) : {tree_kernel<1, false>, tree_kernel<2, false>, tree_kernel<2, true>}) {
     cudaFuncAttributes fa;
     cudaError_t e = cudaFuncGetAttributes(&fa, kernel);
     if (e != cudaSuccess) return e;
