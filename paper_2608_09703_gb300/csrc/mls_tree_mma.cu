@@ -271,6 +271,7 @@ __device__ void query_role(const TreeParams& p, Tail* sh, uint32_t base) {
   }
 }
 
+// One warp, which runs as one (all of its lanes wait) down to the elected lane that issues.
 template <int DC, bool kJoint>
 __device__ void mma_role(const TreeParams& p, Tail* sh, uint32_t base, uint32_t tmem) {
   using L = Layout<DC, kJoint>;
@@ -278,30 +279,36 @@ __device__ void mma_role(const TreeParams& p, Tail* sh, uint32_t base, uint32_t 
   const uint32_t idesc_s = make_idesc(kRows, kKeys, false, false, false) | (p.negate ? kNegateA : 0u);
   const int dn = (p.dim + 15) & ~15;
   const uint32_t idesc_o = make_idesc(kRows, dn, false, false, true);
-  const int ks = dn / 16;
+  const int ks = dn / 16, lane = threadIdx.x & 31;
   uint32_t ring = 0, q_par = 0, p_par = 0;  // a bit a stream
   bool ok = true;
   auto ready = [&](uint64_t* bar, uint32_t parity) {
-    ok = ok && wait(p, sh, bar, parity);
+    ok = ok && __all_sync(0xffffffffu, wait(p, sh, bar, parity));
     tc_fence_after();
     return ok;
   };
   Seg g;
-  for (uint32_t k = 0; ok && read_seg(p, sh, k, g); ++k) {
-    free_seg(sh, k);
-    const int n = g.t1 - g.t0;
-    const bool pair = g.nrows > kRows;
+  for (uint32_t k = 0; ok && __all_sync(0xffffffffu, read_seg(p, sh, k, g)); ++k) {
+    __syncwarp();
+    if (lane == 0) free_seg(sh, k);
+    const int n = __shfl_sync(0xffffffffu, g.t1 - g.t0, 0);
+    const bool pair = __shfl_sync(0xffffffffu, g.nrows, 0) > kRows;
     const int steps[2] = {pair ? n : (n + 1) / 2, pair ? n : n / 2};
     auto scores = [&](int w, int i) {
       const uint32_t at = ring + place_k(pair ? i : 2 * i + w, pair), stage = at % L::kStages;
       if (!ready(&sh->full[stage], (at / L::kStages) & 1u)) return;
       const uint64_t a = make_sdesc(base + w * L::kTile, 16), b = make_sdesc(base + L::kRing + stage * L::kTile, 16, L::kAtom);
-      for (int x = 0; x < ks; ++x)
-        mma_issue<false>(tmem + w * kKeys, a + (x >> 2) * (kRows * 128 / 16) + (x & 3) * 2,
-                         b + (x >> 2) * (L::kPiece / 16) + (x & 3) * 2, idesc_s, x > 0);
-      if (!pair || w == 1) mma_commit(smem_u32(&sh->empty[stage]));
-      mma_commit(smem_u32(&sh->s_full[w]));
-      if (i + 1 == steps[w]) mma_commit(smem_u32(&sh->q_free[w]));
+      if (elect_one()) {
+#pragma unroll
+        for (int x = 0; x < DC * 4; ++x)
+          if (x < ks)
+            mma_issue<false>(tmem + w * kKeys, a + (x >> 2) * (kRows * 128 / 16) + (x & 3) * 2,
+                             b + (x >> 2) * (L::kPiece / 16) + (x & 3) * 2, idesc_s, x > 0);
+        if (!pair || w == 1) mma_commit(smem_u32(&sh->empty[stage]));
+        mma_commit(smem_u32(&sh->s_full[w]));
+        if (i + 1 == steps[w]) mma_commit(smem_u32(&sh->q_free[w]));
+      }
+      __syncwarp();
     };
     for (int w = 0; w < 2; ++w)
       if (steps[w] > 0 && ready(&sh->q_ready[w], (q_par >> w) & 1u)) {
@@ -315,16 +322,22 @@ __device__ void mma_role(const TreeParams& p, Tail* sh, uint32_t base, uint32_t 
         const uint32_t at = ring + place_v(pair ? i : 2 * i + w, n, pair), stage = at % L::kStages;
         if (!ready(&sh->full[stage], (at / L::kStages) & 1u)) break;
         const uint64_t b = make_sdesc(base + L::kRing + stage * L::kTile, L::kPiece, L::kAtom);
-        for (int x = 0; x < kKeys / 16; ++x)
-          mma_issue_ts(tmem + kAccO + w * 128, tmem + w * kKeys + x * 8, b + x * (2 * L::kAtom / 16), idesc_o, i > 0 || x > 0);
-        if (!pair || w == 1) mma_commit(smem_u32(&sh->empty[stage]));
+        if (elect_one()) {
+#pragma unroll
+          for (int x = 0; x < kKeys / 16; ++x)
+            mma_issue_ts(tmem + kAccO + w * 128, tmem + w * kKeys + x * 8, b + x * (2 * L::kAtom / 16), idesc_o,
+                         i > 0 || x > 0);
+          if (!pair || w == 1) mma_commit(smem_u32(&sh->empty[stage]));
+          if (i + 1 == steps[w]) mma_commit(smem_u32(&sh->o_full[w]));
+        }
+        __syncwarp();
         if (i + 1 < steps[w]) scores(w, i + 1);
-        else mma_commit(smem_u32(&sh->o_full[w]));
       }
     ring += 2 * n;
   }
-  // Every MMA that this thread issued has finished before TMEM is released.
-  mma_commit(smem_u32(&sh->drain));
+  // Every MMA that the elected lane issued has finished before TMEM is released.
+  if (elect_one()) mma_commit(smem_u32(&sh->drain));
+  __syncwarp();
   mbar_wait_drain(smem_u32(&sh->drain), 0, kDrainNs, p.status);
 }
 
@@ -697,7 +710,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
     if (warp == 0) {
       load_role<DC, kJoint>(p, sh, base);
     } else if (warp == 1) {
-      if (lane == 0) mma_role<DC, kJoint>(p, sh, base, tmem);
+      mma_role<DC, kJoint>(p, sh, base, tmem);
     } else if (warp == 2) {
       if (lane == 0) plan_role(p, sh, lo, hi, sh->e0, sh->base0);
     } else {
