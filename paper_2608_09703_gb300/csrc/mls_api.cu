@@ -2034,6 +2034,17 @@ int encode_pages(CUtensorMap* map, const mls_cache* c, const void* ptr, bool joi
                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? MLS_OK : fail(MLS_ERR_CUDA, "cuTensorMapEncodeTiled (cache)");
 }
+// The queries as [N][q_heads][head_dim], in boxes of 64 values of a group's heads of some nodes.
+int encode_queries(TreeParams* p) {
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(p->dim), static_cast<cuuint64_t>(p->q_heads), static_cast<cuuint64_t>(p->N)};
+  const cuuint64_t strides[2] = {dims[0] * 2, static_cast<cuuint64_t>(p->q_ld) * 2};
+  const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(p->group), static_cast<cuuint32_t>(p->q_rows / p->group)};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  const CUresult r = g_encode(&p->map_q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(p->q), dims, strides, box, estr,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? MLS_OK : fail(MLS_ERR_CUDA, "cuTensorMapEncodeTiled (queries)");
+}
 }  // namespace
 
 extern "C" size_t mls_tree_attention_workspace_size(const mls_cache* c, int32_t n, int64_t N, int32_t q_heads) {
@@ -2051,7 +2062,7 @@ extern "C" int mls_tree_attention(const mls_cache* c, int32_t layer, int32_t n, 
   if (n == 0 || N == 0) return MLS_OK;
   if (!start || !q || !out || !lse) return MLS_ERR_ARG;
   const int64_t dense = static_cast<int64_t>(q_heads) * c->head_dim;
-  if (q_ld < dense || q_ld > (int64_t{1} << 40)) return MLS_ERR_ARG;
+  if (q_ld < dense || q_ld > (int64_t{1} << 38)) return MLS_ERR_ARG;  // strides of a tensor map are below 2^40 bytes
   if (q_ld % (c->dtype == MLS_BF16 ? 8 : 4) || !aligned16(q) || !aligned16(out) || !aligned4(lse) || !aligned4(seqs) ||
       !aligned4(start) || !aligned4(parents))
     return MLS_ERR_ALIGN;
@@ -2086,9 +2097,14 @@ extern "C" int mls_tree_attention(const mls_cache* c, int32_t layer, int32_t n, 
   p.splits = pl.splits;
   p.status = dev->status;
   p.sms = dev->sms;
-  p.joint = c->dtype == MLS_BF16 && c->head_dim == 128;
-  if (c->dtype == MLS_BF16 && (encode_pages(&p.map_k, c, c->k, p.joint) || encode_pages(&p.map_v, c, c->v, p.joint)))
-    return MLS_ERR_CUDA;
+  if (c->dtype == MLS_BF16) {
+    p.joint = c->head_dim == 128;
+    p.tile_rows = tree_tile_rows(p.group);
+    p.q_rows = tree_query_rows(p.group);
+    if (encode_pages(&p.map_k, c, c->k, p.joint) || encode_pages(&p.map_v, c, c->v, p.joint) ||
+        (p.q_rows && encode_queries(&p)))
+      return MLS_ERR_CUDA;
+  }
   return timed("tree_attention", s,
                [&] { return c->dtype == MLS_FP32 ? launch_tree_fp32(p, s) : launch_tree_bf16(p, s); });
 }

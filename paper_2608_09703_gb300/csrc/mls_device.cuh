@@ -664,6 +664,32 @@ __device__ __forceinline__ float fast_exp2(float x) {
   return y;
 }
 
+// Largest of three, in one instruction (NaN where all are).
+__device__ __forceinline__ float fmax3(float a, float b, float c) {
+  float y;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
+// Two fp32 operations in one instruction: v * s + t, and a + b.
+__device__ __forceinline__ float2 fma2(const float2& v, float s, float t) {
+  float2 y;
+  asm("{\n\t.reg .b64 v, s, t, y;\n\t"
+      "mov.b64 v, {%2, %3};\n\tmov.b64 s, {%4, %4};\n\tmov.b64 t, {%5, %5};\n\t"
+      "fma.rn.f32x2 y, v, s, t;\n\tmov.b64 {%0, %1}, y;\n\t}"
+      : "=f"(y.x), "=f"(y.y)
+      : "f"(v.x), "f"(v.y), "f"(s), "f"(t));
+  return y;
+}
+__device__ __forceinline__ float2 add2(const float2& a, const float2& b) {
+  float2 y;
+  asm("{\n\t.reg .b64 a, b, y;\n\t"
+      "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+      "add.rn.f32x2 y, a, b;\n\tmov.b64 {%0, %1}, y;\n\t}"
+      : "=f"(y.x), "=f"(y.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return y;
+}
+
 // Register reallocation between warpgroups (all four warps of a warpgroup
 // execute it).  The sum over warpgroups must equal the launch allocation.
 template <uint32_t kRegs>

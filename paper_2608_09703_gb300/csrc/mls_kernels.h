@@ -579,6 +579,8 @@ cudaError_t setup_cache_kernels();
 struct TreeParams {
   CacheView c;
   CUtensorMap map_k, map_v;      // bf16: boxes of one head and page, of 64 values a token or (joint) 128
+  CUtensorMap map_q;             // boxes of a group's heads and some nodes, q_rows rows (0: no map) of 64 values
+  int q_rows, tile_rows;         // tile_rows of a row tile's 128 are used
   int joint;
   int layer, n;
   long long N;
@@ -593,7 +595,8 @@ struct TreeParams {
   float* lse;
   int splits;                    // fp32: pieces of the keys
   // Workspace: of rows whose keys are split their maximum, sum and product, dim + 4 words each.
-  // fp32: [N][q_heads][splits] of them.  bf16: [CTAs][2][part_rows], a CTA's first and its last item.
+  // fp32: [N][q_heads][splits] of them.  bf16: [CTAs][2] times part_rows rows, a CTA's first and its last item:
+  // float2 [rows] of maximum and sum in the first 4 part_rows words, then float4 [dim / 4][part_rows].
   float* part;
   int part_rows;
   long long* unit_base;          // bf16: [n + 1] the first key tile of each entry, in one numbering
@@ -605,6 +608,8 @@ cudaError_t launch_tree_fp32(const TreeParams& p, cudaStream_t s);
 cudaError_t launch_tree_bf16(const TreeParams& p, cudaStream_t s);
 int tree_fp32_splits(long long N, int q_heads, int sms);
 int tree_part_rows(long long N, int group);
+int tree_tile_rows(int group);
+int tree_query_rows(int group);
 cudaError_t setup_tree_kernels();
 
 // ------------------------------------------------------------------ acceptance of drafted trees

@@ -51,7 +51,7 @@ constexpr int kSegs = 4;
 constexpr int kSegReaders = 3 + 8;                // load, MMA and query warp, eight of softmax
 // Past the operands.  A warpgroup's `up` and `ml` share memory: parents are read before any sum is.
 struct Tail {
-  uint64_t full[kMaxStages], empty[kMaxStages], q_ready[2], q_free[2], s_full[2], p_ready[2], o_full[2], met, drain;
+  uint64_t full[kMaxStages], empty[kMaxStages], q_ready[2], q_free[2], s_full[2], p_ready[2][2], o_full[2], met, drain;
   uint64_t seg_full[kSegs], seg_empty[kSegs];
   Seg seg[kSegs];
   union {
@@ -80,9 +80,9 @@ struct Layout {
   }
 };
 
-// Key tiles of rows [r0, r0 + 256) of an entry.
+// Key tiles of rows [r0, r0 + two tiles) of an entry.
 __device__ __forceinline__ int item_total(const TreeParams& p, const Entry& en, int r0) {
-  const int rows = min(en.nodes * p.group - r0, 2 * kRows);
+  const int rows = min(en.nodes * p.group - r0, 2 * p.tile_rows);
   return en.len + (r0 + rows - 1) / p.group + 1;
 }
 __device__ __forceinline__ int tiles_of(int total) { return (total + kKeys - 1) / kKeys; }
@@ -90,7 +90,7 @@ __device__ __forceinline__ int tiles_of(int total) { return (total + kKeys - 1) 
 constexpr int kOver = 1;
 __device__ long long entry_units(const TreeParams& p, const Entry& en) {
   long long sum = 0;
-  for (int r0 = 0; r0 < en.nodes * p.group; r0 += 2 * kRows) sum += kOver + tiles_of(item_total(p, en, r0));
+  for (int r0 = 0; r0 < en.nodes * p.group; r0 += 2 * p.tile_rows) sum += kOver + tiles_of(item_total(p, en, r0));
   return sum * p.c.heads;
 }
 
@@ -125,7 +125,7 @@ __device__ void plan_role(const TreeParams& p, Tail* sh, long long at, long long
       const long long here = static_cast<long long>(nt + kOver) * p.c.heads;
       if (v < here) break;
       v -= here;
-      r0 += 2 * kRows;
+      r0 += 2 * p.tile_rows;
     }
     const int head = static_cast<int>(v / (nt + kOver)), in = static_cast<int>(v - static_cast<long long>(head) * (nt + kOver));
     const int end = static_cast<int>(min(static_cast<long long>(nt + kOver), in + (hi - at)));
@@ -140,7 +140,7 @@ __device__ void plan_role(const TreeParams& p, Tail* sh, long long at, long long
     g->len = en.len;
     g->head = head;
     g->r0 = r0;
-    g->nrows = min(en.nodes * p.group - r0, 2 * kRows);
+    g->nrows = min(en.nodes * p.group - r0, 2 * p.tile_rows);
     g->t0 = t0;
     g->t1 = t1;
     g->nt = nt;
@@ -185,7 +185,7 @@ __device__ void load_role(const TreeParams& p, Tail* sh, uint32_t base) {
     __syncwarp();
     if (lane == 0) free_seg(sh, k);
     const int n = g.t1 - g.t0;
-    const bool pair = g.nrows > kRows;
+    const bool pair = g.nrows > p.tile_rows;
     const int* const table = g.row < 0 ? nullptr : p.c.table + static_cast<long long>(g.row) * p.c.max_pages;
     for (int i = 0; i < 2 * n; ++i, ++ring) {
       // The i-th load of the segment: the K or the V tile of step j.
@@ -230,27 +230,42 @@ __device__ void load_role(const TreeParams& p, Tail* sh, uint32_t base) {
   __syncwarp();
 }
 
-// One warp: queries of each stream's rows, swizzled as TMA would, zeros where there is no row or value.
+// One warp: queries of each stream's rows.  A TMA box has the heads of some nodes, in the order of the rows; nodes
+// behind the entry's may come with it: their rows are nobody's.  Groups of more than a tile's rows are
+// gathered, swizzled as TMA would.
 template <int DC>
 __device__ void query_role(const TreeParams& p, Tail* sh, uint32_t base) {
   constexpr int kWide = DC * 8, kStep = 32 / kWide;           // pieces of 16 bytes of a row, rows at a time
   const int lane = threadIdx.x & 31, c = lane % kWide;
-  uint32_t free_par = 0;                                      // a bit a stream
+  const int part = lane % DC, mine = lane / DC;               // this lane's box: at most 16 of DC pieces
+  uint32_t loads[2] = {0, 0};
+  bool ok = true;
   Seg g;
-  for (uint32_t k = 0; __all_sync(0xffffffffu, read_seg(p, sh, k, g)); ++k) {
+  for (uint32_t k = 0; ok && __all_sync(0xffffffffu, read_seg(p, sh, k, g)); ++k) {
     __syncwarp();
     if (lane == 0) free_seg(sh, k);
     const int n = g.t1 - g.t0;
-    const bool pair = g.nrows > kRows;
+    const bool pair = g.nrows > p.tile_rows;
     for (int w = 0; w < 2; ++w) {
       if (!pair && w == 1 && n < 2) continue;
-      wait(p, sh, &sh->q_free[w], ((free_par >> w) & 1u) ^ 1u);
-      free_par ^= 1u << w;
-      const int row0 = pair ? w * kRows : 0, last = g.r0 + g.nrows;
-      int r = g.r0 + row0 + lane / kWide, t = r / p.group, h = r - t * p.group;
+      ok = __all_sync(0xffffffffu, wait(p, sh, &sh->q_free[w], (loads[w] & 1u) ^ 1u));
+      if (!ok) break;
+      ++loads[w];
+      const int row0 = g.r0 + (pair ? w * p.tile_rows : 0), last = g.r0 + g.nrows;
+      const uint32_t bar = smem_u32(&sh->q_ready[w]), tile = base + w * DC * kRows * 128u;
+      if (p.q_rows) {
+        const int boxes = (min(last - row0, p.tile_rows) + p.q_rows - 1) / p.q_rows;
+        if (lane == 0) mbar_arrive_expect_tx(bar, boxes * DC * p.q_rows * 128u);
+        __syncwarp();
+        if (mine < boxes)
+          tma_load_3d(tile + part * (kRows * 128u) + mine * p.q_rows * 128u, &p.map_q, bar, part * 64, g.head * p.group,
+                      static_cast<int>(g.first) + (row0 + mine * p.q_rows) / p.group);
+        continue;
+      }
+      int r = row0 + lane / kWide, t = r / p.group, h = r - t * p.group;
       const __nv_bfloat16* const q = static_cast<const __nv_bfloat16*>(p.q) + g.first * p.q_ld +
                                      static_cast<long long>(g.head) * p.group * p.dim + c * 8;
-      uint32_t to = base + w * DC * kRows * 128u + (c >> 3) * (kRows * 128u) + (lane / kWide) * 128u;
+      uint32_t to = tile + (c >> 3) * (kRows * 128u) + (lane / kWide) * 128u;
 #pragma unroll 4
       for (int i = lane / kWide; i < kRows; i += kStep) {
         const bool in = r < last && c * 8 < p.dim;
@@ -266,9 +281,13 @@ __device__ void query_role(const TreeParams& p, Tail* sh, uint32_t base) {
       cp_async_wait_all();
       fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&sh->q_ready[w]));
+      if (lane == 0) mbar_arrive(bar);
     }
   }
+  if (lane == 0)
+    for (int w = 0; w < 2; ++w)
+      if (loads[w]) mbar_wait_drain(smem_u32(&sh->q_ready[w]), (loads[w] - 1) & 1u, kDrainNs, p.status);
+  __syncwarp();
 }
 
 // One warp, which runs as one (all of its lanes wait) down to the elected lane that issues.
@@ -280,7 +299,15 @@ __device__ void mma_role(const TreeParams& p, Tail* sh, uint32_t base, uint32_t 
   const int dn = (p.dim + 15) & ~15;
   const uint32_t idesc_o = make_idesc(kRows, dn, false, false, true);
   const int ks = dn / 16, lane = threadIdx.x & 31;
-  uint32_t ring = 0, q_par = 0, p_par = 0;  // a bit a stream
+  // A place in the ring, and which round.
+  struct Place {
+    uint32_t stage, phase;
+    __device__ __forceinline__ Place next() const {
+      return stage + 1 == L::kStages ? Place{0, phase ^ 1u} : Place{stage + 1, phase};
+    }
+  };
+  Place at = {0, 0};
+  uint32_t q_par = 0, p_par = 0;  // a bit a stream
   bool ok = true;
   auto ready = [&](uint64_t* bar, uint32_t parity) {
     ok = ok && __all_sync(0xffffffffu, wait(p, sh, bar, parity));
@@ -292,48 +319,75 @@ __device__ void mma_role(const TreeParams& p, Tail* sh, uint32_t base, uint32_t 
     __syncwarp();
     if (lane == 0) free_seg(sh, k);
     const int n = __shfl_sync(0xffffffffu, g.t1 - g.t0, 0);
-    const bool pair = __shfl_sync(0xffffffffu, g.nrows, 0) > kRows;
-    const int steps[2] = {pair ? n : (n + 1) / 2, pair ? n : n / 2};
-    auto scores = [&](int w, int i) {
-      const uint32_t at = ring + place_k(pair ? i : 2 * i + w, pair), stage = at % L::kStages;
-      if (!ready(&sh->full[stage], (at / L::kStages) & 1u)) return;
-      const uint64_t a = make_sdesc(base + w * L::kTile, 16), b = make_sdesc(base + L::kRing + stage * L::kTile, 16, L::kAtom);
+    const bool pair = __shfl_sync(0xffffffffu, g.nrows, 0) > p.tile_rows;
+    // S of stream w from the K tile at `from`, which it is the last to read or not.
+    auto scores = [&](int w, const Place& from, bool last, bool done) {
+      const uint64_t a = make_sdesc(base + w * L::kTile, 16), b = make_sdesc(base + L::kRing + from.stage * L::kTile, 16, L::kAtom);
       if (elect_one()) {
 #pragma unroll
         for (int x = 0; x < DC * 4; ++x)
           if (x < ks)
             mma_issue<false>(tmem + w * kKeys, a + (x >> 2) * (kRows * 128 / 16) + (x & 3) * 2,
                              b + (x >> 2) * (L::kPiece / 16) + (x & 3) * 2, idesc_s, x > 0);
-        if (!pair || w == 1) mma_commit(smem_u32(&sh->empty[stage]));
         mma_commit(smem_u32(&sh->s_full[w]));
-        if (i + 1 == steps[w]) mma_commit(smem_u32(&sh->q_free[w]));
+        if (done) mma_commit(smem_u32(&sh->empty[from.stage]));
+        if (last) mma_commit(smem_u32(&sh->q_free[w]));
       }
       __syncwarp();
     };
-    for (int w = 0; w < 2; ++w)
-      if (steps[w] > 0 && ready(&sh->q_ready[w], (q_par >> w) & 1u)) {
-        q_par ^= 1u << w;
-        scores(w, 0);
-      }
-    for (int i = 0; ok && i < steps[0]; ++i)
-      for (int w = 0; ok && w < 2; ++w) {
-        if (i >= steps[w] || !ready(&sh->p_ready[w], (p_par >> w) & 1u)) continue;
-        p_par ^= 1u << w;
-        const uint32_t at = ring + place_v(pair ? i : 2 * i + w, n, pair), stage = at % L::kStages;
-        if (!ready(&sh->full[stage], (at / L::kStages) & 1u)) break;
-        const uint64_t b = make_sdesc(base + L::kRing + stage * L::kTile, L::kPiece, L::kAtom);
+    // O of stream w from the V tile at `from`, its P in two halves.
+    auto values = [&](int w, const Place& from, bool first, bool last, bool done) {
+      const uint64_t b = make_sdesc(base + L::kRing + from.stage * L::kTile, L::kPiece, L::kAtom);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (!ready(&sh->p_ready[w][h], (p_par >> w) & 1u)) return;
         if (elect_one()) {
 #pragma unroll
-          for (int x = 0; x < kKeys / 16; ++x)
+          for (int x = 4 * h; x < 4 * h + 4; ++x)
             mma_issue_ts(tmem + kAccO + w * 128, tmem + w * kKeys + x * 8, b + x * (2 * L::kAtom / 16), idesc_o,
-                         i > 0 || x > 0);
-          if (!pair || w == 1) mma_commit(smem_u32(&sh->empty[stage]));
-          if (i + 1 == steps[w]) mma_commit(smem_u32(&sh->o_full[w]));
+                         !first || x > 0);
+          if (h == 1) {
+            if (done) mma_commit(smem_u32(&sh->empty[from.stage]));
+            if (last) mma_commit(smem_u32(&sh->o_full[w]));
+          }
         }
         __syncwarp();
-        if (i + 1 < steps[w]) scores(w, i + 1);
       }
-    ring += 2 * n;
+      p_par ^= 1u << w;
+    };
+    const int streams = pair || n > 1 ? 2 : 1;
+    for (int w = 0; ok && w < streams; ++w) {
+      if (!ready(&sh->q_ready[w], (q_par >> w) & 1u)) break;
+      q_par ^= 1u << w;
+      if ((!pair || w == 0) && !ready(&sh->full[at.stage], at.phase)) break;
+      scores(w, at, pair ? n == 1 : w + 2 >= n, !pair || w == 1);
+      if (!pair || w == 1) at = at.next();
+    }
+    if (pair) {  // K0 | V0 K1 | V1 K2 ... each for both
+      for (int i = 0; ok && i < n; ++i) {
+        const Place v = at, key = at.next();
+        const bool more = i + 1 < n;
+        if (!ready(&sh->full[v.stage], v.phase)) break;
+        for (int w = 0; ok && w < 2; ++w) {
+          values(w, v, i == 0, !more, w == 1);
+          if (!more) continue;
+          if (w == 0 && !ready(&sh->full[key.stage], key.phase)) break;
+          if (ok) scores(w, key, i + 2 == n, w == 1);
+        }
+        at = more ? key.next() : key;
+      }
+    } else {     // K0 K1 | V0 K2 | V1 K3 ... one for each in turn
+      for (int j = 0; ok && j < n; ++j) {
+        const int w = j & 1;
+        if (!ready(&sh->full[at.stage], at.phase)) break;
+        values(w, at, j < 2, j + 2 >= n, true);
+        at = at.next();
+        if (!ok || j + 2 >= n) continue;
+        if (!ready(&sh->full[at.stage], at.phase)) break;
+        scores(w, at, j + 4 >= n, true);
+        at = at.next();
+      }
+    }
   }
   // Every MMA that the elected lane issued has finished before TMEM is released.
   if (elect_one()) mma_commit(smem_u32(&sh->drain));
@@ -406,10 +460,10 @@ __device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint3
     if (!named_bar_and(1 + w, kRows, read_seg(p, sh, k, g))) break;
     if (lane == 0) free_seg(sh, k);
     const int n = g.t1 - g.t0;
-    const bool pair = g.nrows > kRows;
+    const bool pair = g.nrows > p.tile_rows;
     const int steps = pair ? n : (n + 1 - w) / 2;
-    const int rl = (pair ? w * kRows : 0) + tid;  // this thread's row of the item
-    const bool inside = rl < g.nrows;
+    const int rl = (pair ? w * p.tile_rows : 0) + tid;  // this thread's row of the item
+    const bool inside = tid < p.tile_rows && rl < g.nrows;
     const int r = g.r0 + rl, node = inside ? r / p.group : 0;
     const int* const table = p.c.table + static_cast<long long>(max(g.row, 0)) * p.c.max_pages;
     if (g.first != had_first || g.row != had_row || g.r0 != had_r0) {  // other heads of the same rows see the same
@@ -442,67 +496,11 @@ __device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint3
         named_bar_sync(1 + w, kRows);
       }
     }
-    const bool busy = (pair ? w * kRows : 0) + quad * 32 < g.nrows;  // rows of this warp
+    const bool busy = __any_sync(0xffffffffu, inside);  // rows of this warp
     float m = -INFINITY, l = 0.f;
     for (int i = 0; i < steps; ++i) {
       const int j = pair ? i : 2 * i + w, k0 = (g.t0 + j) * kKeys;
       const bool masked = k0 + kKeys > g.all;
-      wait(p, sh, &sh->s_full[w], s_par);
-      s_par ^= 1u;
-      tc_fence_after();
-      if (busy) {
-        float z[kKeys];
-        tmem_ld128(ts, z);
-        if (masked) {
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const unsigned b = see.bits(k0 + 32 * x);
-#pragma unroll
-            for (int y = 0; y < 32; ++y) z[32 * x + y] = (b >> y) & 1u ? z[32 * x + y] : -INFINITY;
-          }
-        }
-        float top[4] = {z[0], z[1], z[2], z[3]};
-#pragma unroll
-        for (int x = 4; x < kKeys; x += 8) {
-          top[0] = fmaxf(top[0], fmaxf(z[x], z[(x + 4) % kKeys]));
-          top[1] = fmaxf(top[1], fmaxf(z[x + 1], z[(x + 5) % kKeys]));
-          top[2] = fmaxf(top[2], fmaxf(z[x + 2], z[(x + 6) % kKeys]));
-          top[3] = fmaxf(top[3], fmaxf(z[x + 3], z[(x + 7) % kKeys]));
-        }
-        const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-        // The maximum moves only where it must; where it does, what is summed so far is brought down.
-        const bool move = (now - m) * p.scale > kGrow || (m == -INFINITY && now > m);
-        if (__any_sync(0xffffffffu, move)) {
-          const float c = !move ? 1.f : m == -INFINITY ? 0.f : fast_exp2((m - now) * p.scale);
-          if (move) m = now;
-          l *= c;
-          if (i > 0) {
-#pragma unroll 1
-            for (int x = 0; x < p.dim; x += 32) {
-              float o[32];
-              tmem_ld32(to + x, o);
-              uint32_t u[32];
-#pragma unroll
-              for (int y = 0; y < 32; ++y) u[y] = __float_as_uint(o[y] * c);
-              tmem_st32(to + x, u);
-            }
-          }
-        }
-        const float off = m == -INFINITY ? 0.f : m * p.scale;
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
-        uint32_t u[kKeys / 2];
-#pragma unroll
-        for (int x = 0; x < kKeys; x += 2) {
-          const float a = fast_exp2(fmaf(z[x], p.scale, -off)), b = fast_exp2(fmaf(z[x + 1], p.scale, -off));
-          sum[x & 2] += a;
-          sum[(x & 2) + 1] += b;
-          u[x / 2] = pack_bf16(a, b);
-        }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        tmem_st32(ts, u);
-        tmem_st32(ts + 32, u + 32);
-        tmem_st_wait();
-      }
       if (masked) {
         // Values that not every row sees: infinities and NaN become 0, to be added to the rows that see them at
         // the end.  Those behind the last key, up to the end of its page, become 0 (the pages behind it came as
@@ -512,6 +510,7 @@ __device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint3
         const uint32_t tile = base + L::kRing + stage * L::kTile;
         const int a = max(g.all - k0, 0), b = min((g.total + mask & ~mask) - k0, kKeys), last = g.total - k0;
         wait(p, sh, &sh->full[stage], (at / L::kStages) & 1u);
+#pragma unroll 4
         for (int x = a * DC * 8 + tid; x < b * DC * 8; x += kRows) {
           const int row = x / (DC * 8), c = x % (DC * 8);
           const uint32_t addr = tile + L::at(row, c);
@@ -534,9 +533,70 @@ __device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint3
         fence_proxy_async_smem();
         __threadfence_block();
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&sh->p_ready[w]));
+      wait(p, sh, &sh->s_full[w], s_par);
+      s_par ^= 1u;
+      tc_fence_after();
+      if (busy) {
+        float z[kKeys];
+        tmem_ld128(ts, z);
+        if (masked) {
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const unsigned b = see.bits(k0 + 32 * x);
+#pragma unroll
+            for (int y = 0; y < 32; ++y) z[32 * x + y] = (b >> y) & 1u ? z[32 * x + y] : -INFINITY;
+          }
+        }
+        float top[4] = {z[0], z[1], z[2], z[3]};
+#pragma unroll
+        for (int x = 4; x + 8 <= kKeys; x += 8)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) top[y] = fmax3(top[y], z[x + y], z[x + 4 + y]);
+        const float now = fmax3(fmaxf(top[0], z[kKeys - 4]), fmax3(top[1], z[kKeys - 3], top[2]),
+                                fmax3(top[3], z[kKeys - 2], z[kKeys - 1]));
+        // The maximum moves only where it must; where it does, what is summed so far is brought down.
+        const bool move = (now - m) * p.scale > kGrow || (m == -INFINITY && now > m);
+        if (__any_sync(0xffffffffu, move)) {
+          const float c = !move ? 1.f : m == -INFINITY ? 0.f : fast_exp2((m - now) * p.scale);
+          if (move) m = now;
+          l *= c;
+          if (i > 0) {
+#pragma unroll 1
+            for (int x = 0; x < p.dim; x += 32) {
+              float o[32];
+              tmem_ld32(to + x, o);
+              uint32_t u[32];
+#pragma unroll
+              for (int y = 0; y < 32; ++y) u[y] = __float_as_uint(o[y] * c);
+              tmem_st32(to + x, u);
+            }
+          }
+        }
+        const float off = m == -INFINITY ? 0.f : -m * p.scale;
+        float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+        // The MMAs of the first half of the keys begin while the second half's exponentials are taken.
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t u[kKeys / 4];
+#pragma unroll
+          for (int x = 0; x < kKeys / 2; x += 2) {
+            const float2 e = fma2(make_float2(z[64 * h + x], z[64 * h + x + 1]), p.scale, off);
+            const float2 f = make_float2(fast_exp2(e.x), fast_exp2(e.y));
+            sum[(x >> 1) & 1] = add2(sum[(x >> 1) & 1], f);
+            u[x / 2] = pack_bf16(f.x, f.y);
+          }
+          tmem_st32(ts + 32 * h, u);
+          tmem_st_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&sh->p_ready[w][h]));
+        }
+        l += (sum[0].x + sum[1].x) + (sum[0].y + sum[1].y);
+      } else {
+        __syncwarp();
+        if (lane == 0)
+          for (int h = 0; h < 2; ++h) mbar_arrive(smem_u32(&sh->p_ready[w][h]));
+      }
     }
     ring += 2 * n;
 
@@ -565,12 +625,17 @@ __device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint3
     const float inv = whole ? (Lsum == 0.f || !see.used ? 0.f : 1.f / Lsum) : 1.f;
     const int chunks = (p.dim + 31) / 32;
     const int x0 = pair || w == 0 ? 0 : (chunks + 1) / 2, x1 = pair || w == 1 ? chunks : (chunks + 1) / 2;
-    const long long t = g.first + node;
-    const long long out_row = t * p.q_heads + g.head * p.group + (r - node * p.group);
-    float* const part = p.part + ((static_cast<long long>(blockIdx.x) * 2 + g.slot) * p.part_rows + rl) * (p.dim + 4);
+    const int out_row = (static_cast<int>(g.first) + node) * p.q_heads + g.head * p.group + (r - node * p.group);
+    // A piece's rows lie side by side, four values each, so that the lanes' stores do.
+    const int rows = p.part_rows;
+    float* const part = p.part + (static_cast<long long>(blockIdx.x) * 2 + g.slot) * rows * (p.dim + 4);
     const uint32_t other = tmem + lanes + kAccO + (1 - w) * 128;
-    const bool reads = (pair ? w * kRows : 0) + quad * 32 < g.nrows;
-    if (reads) {
+    if (busy) {
+      // For stores of 64 bytes of a row, four lanes exchange their 16 bytes of each other's rows.
+      const int four = lane & 3;
+      int row4[4];
+#pragma unroll
+      for (int y = 0; y < 4; ++y) row4[y] = __shfl_sync(0xffffffffu, inside ? out_row : -1, (lane & ~3) + y);
 #pragma unroll 1
       for (int x = x0; x < x1; ++x) {
         float o[32];
@@ -602,32 +667,41 @@ __device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint3
               }
           }
         }
-        if (!inside) continue;
+        __syncwarp();
         if (whole) {
-          __nv_bfloat16* const out = static_cast<__nv_bfloat16*>(p.out) + out_row * p.dim + 32 * x;
+          uint32_t u[4][4];
 #pragma unroll
-          for (int y = 0; y < 32; y += 8)
-            if (32 * x + y < p.dim) {
-              uint32_t u[4];
+          for (int y = 0; y < 16; ++y)
+            u[y >> 2][y & 3] = see.used ? pack_bf16(o[2 * y] * inv, o[2 * y + 1] * inv) : 0u;
 #pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                const float a = see.used ? o[y + 2 * k] * inv : 0.f, b = see.used ? o[y + 2 * k + 1] * inv : 0.f;
-                u[k] = pack_bf16(a, b);
-              }
-              st16(out + y, make_uint4(u[0], u[1], u[2], u[3]));
-            }
-        } else {
+          for (int d = 1; d < 4; d <<= 1)
 #pragma unroll
-          for (int y = 0; y < 32; y += 4)
-            if (32 * x + y < p.dim)
-              *reinterpret_cast<float4*>(part + 4 + 32 * x + y) = make_float4(o[y], o[y + 1], o[y + 2], o[y + 3]);
+            for (int a = 0; a < 4; ++a)
+              if (!(a & d))
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                  const bool up = four & d;
+                  const uint32_t give = __shfl_xor_sync(0xffffffffu, up ? u[a][y] : u[a + d][y], d);
+                  if (up) u[a][y] = give;
+                  else u[a + d][y] = give;
+                }
+          __nv_bfloat16* const out = static_cast<__nv_bfloat16*>(p.out) + 32 * x + 8 * four;
+#pragma unroll
+          for (int y = 0; y < 4; ++y)
+            if (row4[y] >= 0 && 32 * x + 8 * four < p.dim)
+              st16(out + static_cast<long long>(row4[y]) * p.dim, make_uint4(u[y][0], u[y][1], u[y][2], u[y][3]));
+        } else if (inside) {
+          float4* const at = reinterpret_cast<float4*>(part + 4 * rows) + static_cast<long long>(8 * x) * rows + rl;
+#pragma unroll
+          for (int y = 0; y < 8; ++y)
+            if (32 * x + 4 * y < p.dim) at[y * rows] = make_float4(o[4 * y], o[4 * y + 1], o[4 * y + 2], o[4 * y + 3]);
         }
       }
     }
     if (inside && (pair || w == 0)) {
       const float sum = see.used ? Lsum : 0.f;
       if (whole) p.lse[out_row] = sum == 0.f ? -INFINITY : fmaf(M, p.scale, log2f(sum)) * kLn2;
-      else part[0] = M, part[1] = sum;
+      else reinterpret_cast<float2*>(part)[rl] = make_float2(M, sum);
     }
     tc_fence_before();
     if (!pair) meet();
@@ -651,7 +725,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
       mbar_init(smem_u32(&sh->q_ready[w]), 1);
       mbar_init(smem_u32(&sh->q_free[w]), 1);
       mbar_init(smem_u32(&sh->s_full[w]), 1);
-      mbar_init(smem_u32(&sh->p_ready[w]), kRows / 32);
+      for (int h = 0; h < 2; ++h) mbar_init(smem_u32(&sh->p_ready[w][h]), kRows / 32);
       mbar_init(smem_u32(&sh->o_full[w]), 1);
     }
     for (int k = 0; k < kSegs; ++k) {
@@ -730,10 +804,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
 }
 
 // Joins the pieces of the items that lie in several CTAs' ranges, in order.  Every such item has a CTA whose
-// range begins inside it after none other does: blocks (CTA, part of its rows) of those have work.  A warp a row.
-constexpr int kJoinWarps = 8, kJoinParts = 8;
-__global__ void __launch_bounds__(32 * kJoinWarps) tree_join_kernel(TreeParams p, int grid) {
+// range begins inside it after none other does: blocks (CTA, part of its rows) of those have work.  32 threads
+// have four values of a row each, whose pieces the eight warps share.
+constexpr int kJoinWarps = 8, kJoinParts = 16;
+__global__ void __launch_bounds__(32 * kJoinWarps) tree_join_kernel(const __grid_constant__ TreeParams p, int grid) {
   __shared__ int s_entry;
+  __shared__ float s_top[kJoinWarps][32], s_sum[kJoinWarps][32];
+  __shared__ float4 s_o[kJoinWarps][32];
   chain_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long units = p.unit_base[p.n], each = (units + grid - 1) / grid;
@@ -752,48 +829,70 @@ __global__ void __launch_bounds__(32 * kJoinWarps) tree_join_kernel(TreeParams p
     const long long here = static_cast<long long>(nt + kOver) * p.c.heads;
     if (v < here) break;
     v -= here;
-    r0 += 2 * kRows;
+    r0 += 2 * p.tile_rows;
   }
   const int head = static_cast<int>(v / (nt + kOver)), in = static_cast<int>(v - static_cast<long long>(head) * (nt + kOver));
   if (in <= kOver) return;                        // it begins with the item's first tile
   const long long first = b - in + kOver, last = first + nt - 1;  // units of the item's tiles
   if (b - each > first) return;                   // another range begins inside the item before
   const int c0 = blockIdx.x, c1 = static_cast<int>(last / each);
-  const int rows = min(en.nodes * p.group - r0, 2 * kRows), stride = p.dim + 4;
-  for (int r = blockIdx.y * kJoinWarps + warp; r < rows; r += kJoinWarps * gridDim.y) {
+  const int rows = min(en.nodes * p.group - r0, 2 * p.tile_rows), stride = p.part_rows, all = rows * (p.dim / 4);
+  for (int i0 = blockIdx.y * 32; i0 < all; i0 += 32 * gridDim.y) {
+    const int i = min(i0 + lane, all - 1), x = i / rows, r = i - x * rows;  // lanes side by side have rows that are
     auto piece = [&](int c) {  // the item is the CTA's first if its range begins with or inside it
-      return p.part + ((static_cast<long long>(c) * 2 + (c * each >= first - kOver ? 0 : 1)) * p.part_rows + r) * stride;
+      return p.part + (static_cast<long long>(c) * 2 + (c * each >= first - kOver ? 0 : 1)) * stride * (p.dim + 4);
     };
-    float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int c = c0 + lane; c <= c1; c += 32) m = fmaxf(m, piece(c)[0]);
-#pragma unroll
-    for (int x = 16; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-    const float off = m == -INFINITY ? 0.f : m;
+    float m = -INFINITY;
 #pragma unroll 4
-    for (int c = c0; c <= c1; ++c) {
-      const float* const x = piece(c);
-      const float pm = x[0], pl = x[1];
-      float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (lane * 4 < p.dim) f = *reinterpret_cast<const float4*>(x + 4 + lane * 4);
-      if (pl == 0.f) continue;
-      const float k = pm == -INFINITY ? 1.f : fast_exp2((pm - off) * p.scale);  // a sum without a maximum is NaN
-      l = fmaf(pl, k, l);
-      o[0] = fmaf(f.x, k, o[0]), o[1] = fmaf(f.y, k, o[1]), o[2] = fmaf(f.z, k, o[2]), o[3] = fmaf(f.w, k, o[3]);
+    for (int c = c0 + warp; c <= c1; c += kJoinWarps) m = fmaxf(m, piece(c)[2 * r]);
+    s_top[warp][lane] = m;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kJoinWarps; ++w) m = fmaxf(m, s_top[w][lane]);
+    const float off = m == -INFINITY ? 0.f : m;
+    float l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int c = c0 + warp; c <= c1; c += kJoinWarps) {
+      const float* const at = piece(c);
+      const float2 ml = *reinterpret_cast<const float2*>(at + 2 * r);
+      const float4 f = *reinterpret_cast<const float4*>(at + (static_cast<long long>(x + 1) * stride + r) * 4);
+      if (ml.y == 0.f) continue;
+      const float k = ml.x == -INFINITY ? 1.f : fast_exp2((ml.x - off) * p.scale);  // a sum without a maximum is NaN
+      l = fmaf(ml.y, k, l);
+      o = make_float4(fmaf(f.x, k, o.x), fmaf(f.y, k, o.y), fmaf(f.z, k, o.z), fmaf(f.w, k, o.w));
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    const int node = (r0 + r) / p.group;
-    const long long row = (en.first + node) * p.q_heads + head * p.group + (r0 + r - node * p.group);
-    if (lane * 4 < p.dim)
-      *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + row * p.dim + lane * 4) =
-          make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
-    if (lane == 0) p.lse[row] = l == 0.f ? -INFINITY : fmaf(m, p.scale, log2f(l)) * kLn2;
+    s_sum[warp][lane] = l;
+    s_o[warp][lane] = o;
+    __syncthreads();
+    if (warp == 0 && i0 + lane < all) {
+      for (int w = 1; w < kJoinWarps; ++w) {
+        const float4 f = s_o[w][lane];
+        l += s_sum[w][lane];
+        o = make_float4(o.x + f.x, o.y + f.y, o.z + f.z, o.w + f.w);
+      }
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const int node = (r0 + r) / p.group;
+      const long long row = (en.first + node) * p.q_heads + head * p.group + (r0 + r - node * p.group);
+      *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + row * p.dim + x * 4) =
+          make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+      if (x == 0) p.lse[row] = l == 0.f ? -INFINITY : fmaf(m, p.scale, log2f(l)) * kLn2;
+    }
   }
 }
 
 }  // namespace
 
+// Rows of a tile: whole nodes, as many as it holds, or any of a larger group.
+int tree_tile_rows(int group) { return group <= kRows ? kRows / group * group : kRows; }
+// Rows of a box of queries (0: none takes them): where tiles are full, as few nodes as make whole atoms of 8 rows,
+// so that few nodes bring few; else the tile's, as boxes have to begin with an atom.
+int tree_query_rows(int group) {
+  return group > kRows ? 0 : kRows % group ? kRows / group * group : group < 8 ? 8 : group;
+}
 int tree_part_rows(long long N, int group) {
-  return static_cast<int>(N * group < 2 * kRows ? N * group : 2 * kRows);
+  const long long most = 2 * tree_tile_rows(group);
+  return static_cast<int>(N * group < most ? N * group : most);
 }
 
 cudaError_t launch_tree_bf16(const TreeParams& p, cudaStream_t s) {
@@ -803,7 +902,7 @@ cudaError_t launch_tree_bf16(const TreeParams& p, cudaStream_t s) {
   else tree_kernel<1, false><<<grid, kThreads, kSmem, s>>>(p);
   const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  const int parts = (p.part_rows + kJoinWarps - 1) / kJoinWarps;
+  const int parts = (p.part_rows * (p.dim / 4) + 31) / 32;
   return launch_chained(tree_join_kernel, dim3(grid - 1, parts < kJoinParts ? parts : kJoinParts), dim3(32 * kJoinWarps),
                         0, s, p, grid);
 }
