@@ -2003,7 +2003,7 @@ struct TreePlan {
   int splits, part_rows;
   size_t off_part, total;
 };
-TreePlan tree_plan(const mls_cache* c, int n, int64_t N, int q_heads, int sms) {
+TreePlan tree_plan(const mls_cache* c, int64_t N, int q_heads, int sms) {
   TreePlan pl;
   const size_t row = sizeof(float) * (c->head_dim + 4);
   pl.splits = tree_fp32_splits(N, q_heads, sms);
@@ -2012,7 +2012,7 @@ TreePlan tree_plan(const mls_cache* c, int n, int64_t N, int q_heads, int sms) {
     pl.off_part = 0;
     pl.total = align_up(pl.splits > 1 ? row * N * q_heads * pl.splits : 1);
   } else {
-    pl.off_part = align_up(sizeof(long long) * (static_cast<size_t>(n) + 1));
+    pl.off_part = align_up(sizeof(TreeJoin) * sms);
     pl.total = pl.off_part + align_up(row * 2 * sms * pl.part_rows);
   }
   return pl;
@@ -2049,7 +2049,7 @@ int encode_queries(TreeParams* p) {
 
 extern "C" size_t mls_tree_attention_workspace_size(const mls_cache* c, int32_t n, int64_t N, int32_t q_heads) {
   if (tree_validate(c, n, N, q_heads)) return 0;
-  return tree_plan(c, n, N, q_heads, current_sms()).total;
+  return tree_plan(c, N, q_heads, current_sms()).total;
 }
 
 extern "C" int mls_tree_attention(const mls_cache* c, int32_t layer, int32_t n, const int32_t* seqs,
@@ -2066,7 +2066,7 @@ extern "C" int mls_tree_attention(const mls_cache* c, int32_t layer, int32_t n, 
   if (q_ld % (c->dtype == MLS_BF16 ? 8 : 4) || !aligned16(q) || !aligned16(out) || !aligned4(lse) || !aligned4(seqs) ||
       !aligned4(start) || !aligned4(parents))
     return MLS_ERR_ALIGN;
-  const TreePlan pl = tree_plan(c, n, N, q_heads, current_sms());
+  const TreePlan pl = tree_plan(c, N, q_heads, current_sms());
   if (!ws || (reinterpret_cast<uintptr_t>(ws) % kAlign) != 0 || ws_bytes < pl.total) return MLS_ERR_WORKSPACE;
   DeviceState* dev = nullptr;
   if ((rc = device_state(&dev))) return rc;
@@ -2093,7 +2093,7 @@ extern "C" int mls_tree_attention(const mls_cache* c, int32_t layer, int32_t n, 
   p.lse = lse;
   p.part = reinterpret_cast<float*>(static_cast<char*>(ws) + pl.off_part);
   p.part_rows = pl.part_rows;
-  p.unit_base = static_cast<long long*>(ws);
+  p.joins = static_cast<TreeJoin*>(ws);
   p.splits = pl.splits;
   p.status = dev->status;
   p.sms = dev->sms;

@@ -576,6 +576,11 @@ cudaError_t launch_cache_copy(const CacheView& from, const CacheView& to, int n,
 cudaError_t setup_cache_kernels();
 
 // ------------------------------------------------------------------ tree attention
+// The item that a CTA begins and does not end: `pieces` (0: there is none) CTAs have parts of its `rows` rows, which
+// begin with row r0 of an entry whose first node is `first`; the first piece is in `slot` of the CTA's two.
+struct TreeJoin {
+  int pieces, slot, rows, first, r0, head;
+};
 struct TreeParams {
   CacheView c;
   CUtensorMap map_k, map_v;      // bf16: boxes of one head and page, of 64 values a token or (joint) 128
@@ -599,7 +604,7 @@ struct TreeParams {
   // float2 [rows] of maximum and sum in the first 4 part_rows words, then float4 [dim / 4][part_rows].
   float* part;
   int part_rows;
-  long long* unit_base;          // bf16: [n + 1] the first key tile of each entry, in one numbering
+  TreeJoin* joins;               // bf16: [CTAs]
   int* status;
   int sms;
 };

@@ -86,8 +86,9 @@ __device__ __forceinline__ int item_total(const TreeParams& p, const Entry& en, 
   return en.len + (r0 + rows - 1) / p.group + 1;
 }
 __device__ __forceinline__ int tiles_of(int total) { return (total + kKeys - 1) / kKeys; }
-// Units of work: an item's tiles, and kOver more for its beginning and end.
-constexpr int kOver = 1;
+// Units of work: an item's tiles, and kOver more for its beginning and end (1, 3, 5, 8 and 12 more: 32 trees 90, 70,
+// 71, 71 and 73 us, prompts 403, 369, 370, 376 and 383).
+constexpr int kOver = 4;
 __device__ long long entry_units(const TreeParams& p, const Entry& en) {
   long long sum = 0;
   for (int r0 = 0; r0 < en.nodes * p.group; r0 += 2 * p.tile_rows) sum += kOver + tiles_of(item_total(p, en, r0));
@@ -98,10 +99,12 @@ __device__ __forceinline__ bool wait(const TreeParams& p, Tail* sh, uint64_t* ba
   return mbar_wait(smem_u32(bar), parity, &sh->abort, p.status);
 }
 
-// One thread: writes down the segments of units [at, hi), entry e beginning at unit `base`.
-__device__ void plan_role(const TreeParams& p, Tail* sh, long long at, long long hi, int e, long long base) {
+// One thread: writes down the segments of units [at, hi), entry e beginning at unit `base`, and what begins
+// there and goes on in other CTAs' ranges (of `each` units).
+__device__ void plan_role(const TreeParams& p, Tail* sh, long long at, long long hi, long long each, int e, long long base) {
   uint32_t k = 0;
   bool first = true;
+  TreeJoin join = {};
   auto slot = [&]() -> Seg* {
     return wait(p, sh, &sh->seg_empty[k % kSegs], ((k / kSegs) & 1u) ^ 1u) ? &sh->seg[k % kSegs] : nullptr;
   };
@@ -133,7 +136,7 @@ __device__ void plan_role(const TreeParams& p, Tail* sh, long long at, long long
     const int t0 = max(in - kOver, 0), t1 = end - kOver;
     if (t1 <= t0) continue;                       // the range ends before the item's first tile
     Seg* const g = slot();
-    if (!g) return;
+    if (!g) break;
     g->first = en.first;
     g->nodes = en.nodes;
     g->row = en.row;
@@ -148,8 +151,17 @@ __device__ void plan_role(const TreeParams& p, Tail* sh, long long at, long long
     g->all = en.row < 0 ? 0 : p.parents ? en.len : en.len + r0 / p.group + 1;
     g->slot = first ? 0 : 1;
     first = false;
+    if (t0 == 0 && t1 < nt) {  // at = hi: the range ends after tile t1 of the item
+      join.pieces = 1 + static_cast<int>((nt - t1 + each - 1) / each);
+      join.slot = g->slot;
+      join.rows = g->nrows;
+      join.first = static_cast<int>(en.first);
+      join.r0 = r0;
+      join.head = head;
+    }
     mbar_arrive(smem_u32(&sh->seg_full[k++ % kSegs]));
   }
+  p.joins[blockIdx.x] = join;
   if (Seg* const g = slot()) {
     g->t0 = g->t1 = 0;
     mbar_arrive(smem_u32(&sh->seg_full[k % kSegs]));
@@ -484,14 +496,17 @@ __device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint3
           up[j] = static_cast<short>(odd ? -2 : u);
         }
         named_bar_sync(1 + w, kRows);
+        see.used = see.used && up[node] >= -1;
+        int j = see.used ? node : -1;
 #pragma unroll
-        for (int i = 0; i < kTreeMaxNodes / 32; ++i) see.path[i] = 0u;
-        if (see.used) {
-          see.used = up[node] >= -1;
-          for (int j = node; j >= 0 && up[j] >= -1; j = up[j])
-#pragma unroll
-            for (int i = 0; i < kTreeMaxNodes / 32; ++i)
-              if (i == j >> 5) see.path[i] |= 1u << (j & 31);
+        for (int i = kTreeMaxNodes / 32 - 1; i >= 0; --i) {  // parents come before their children
+          unsigned on = 0u;
+          while (j >= 32 * i) {
+            const int above = up[j];
+            if (above >= -1) on |= 1u << (j & 31);
+            j = above;
+          }
+          see.path[i] = on;
         }
         named_bar_sync(1 + w, kRows);
       }
@@ -763,12 +778,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
   }
   const long long each = (units + gridDim.x - 1) / gridDim.x;
   const long long lo = min(blockIdx.x * each, units), hi = min(lo + each, units);
-  if (blockIdx.x == 0 && tid == 0) p.unit_base[p.n] = units;
-  if (blockIdx.x == 0 || (lo < hi && before <= lo && lo < before + mine)) {
+  if (lo < hi && before <= lo && lo < before + mine) {
     long long at = before;
     for (int i = i0; i < i1; ++i) {
       const long long u = i1 - i0 == 1 ? mine : entry_units(p, tree_entry(p, i, p.status));
-      if (blockIdx.x == 0) p.unit_base[i] = at;
       if (at <= lo && lo < at + u) {
         sh->e0 = i;
         sh->base0 = at;
@@ -786,7 +799,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
     } else if (warp == 1) {
       mma_role<DC, kJoint>(p, sh, base, tmem);
     } else if (warp == 2) {
-      if (lane == 0) plan_role(p, sh, lo, hi, sh->e0, sh->base0);
+      if (lane == 0) plan_role(p, sh, lo, hi, each, sh->e0, sh->base0);
     } else {
       query_role<DC>(p, sh, base);
     }
@@ -803,57 +816,36 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
   }
 }
 
-// Joins the pieces of the items that lie in several CTAs' ranges, in order.  Every such item has a CTA whose
-// range begins inside it after none other does: blocks (CTA, part of its rows) of those have work.  32 threads
-// have four values of a row each, whose pieces the eight warps share.
-constexpr int kJoinWarps = 8, kJoinParts = 16;
-__global__ void __launch_bounds__(32 * kJoinWarps) tree_join_kernel(const __grid_constant__ TreeParams p, int grid) {
-  __shared__ int s_entry;
-  __shared__ float s_top[kJoinWarps][32], s_sum[kJoinWarps][32];
-  __shared__ float4 s_o[kJoinWarps][32];
+// Joins the pieces of the items that lie in several CTAs' ranges, in order: blocks x have those of the item that
+// CTA x began.  A thread has four values of a row; where there are many pieces, several threads share them.
+// (Where a block of 32 threads' work each looked for the item itself, 16 trees of 64 nodes took 178 us instead of 130.)
+constexpr int kJoinThreads = 256, kJoinParts = 32;
+__global__ void __launch_bounds__(kJoinThreads) tree_join_kernel(const __grid_constant__ TreeParams p) {
+  __shared__ float s_top[kJoinThreads], s_sum[kJoinThreads];
+  __shared__ float4 s_o[kJoinThreads];
   chain_wait();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const long long units = p.unit_base[p.n], each = (units + grid - 1) / grid;
-  const long long b = (blockIdx.x + 1) * each;    // where the range begins
-  if (b >= units) return;
-  if (threadIdx.x == 0) s_entry = -1;
-  __syncthreads();
-  for (int i = threadIdx.x; i < p.n; i += blockDim.x)
-    if (p.unit_base[i] <= b && b < p.unit_base[i + 1]) s_entry = i;  // one does
-  __syncthreads();
-  const Entry en = tree_entry(p, s_entry, p.status);
-  long long v = b - p.unit_base[s_entry];
-  int r0 = 0, nt;
-  while (true) {
-    nt = tiles_of(item_total(p, en, r0));
-    const long long here = static_cast<long long>(nt + kOver) * p.c.heads;
-    if (v < here) break;
-    v -= here;
-    r0 += 2 * p.tile_rows;
-  }
-  const int head = static_cast<int>(v / (nt + kOver)), in = static_cast<int>(v - static_cast<long long>(head) * (nt + kOver));
-  if (in <= kOver) return;                        // it begins with the item's first tile
-  const long long first = b - in + kOver, last = first + nt - 1;  // units of the item's tiles
-  if (b - each > first) return;                   // another range begins inside the item before
-  const int c0 = blockIdx.x, c1 = static_cast<int>(last / each);
-  const int rows = min(en.nodes * p.group - r0, 2 * p.tile_rows), stride = p.part_rows, all = rows * (p.dim / 4);
-  for (int i0 = blockIdx.y * 32; i0 < all; i0 += 32 * gridDim.y) {
-    const int i = min(i0 + lane, all - 1), x = i / rows, r = i - x * rows;  // lanes side by side have rows that are
-    auto piece = [&](int c) {  // the item is the CTA's first if its range begins with or inside it
-      return p.part + (static_cast<long long>(c) * 2 + (c * each >= first - kOver ? 0 : 1)) * stride * (p.dim + 4);
-    };
+  const TreeJoin it = p.joins[blockIdx.x];
+  const int all = it.rows * (p.dim / 4), stride = p.part_rows;
+  const int shift = it.pieces <= 4 ? 0 : it.pieces <= 8 ? 1 : it.pieces <= 16 ? 2 : 3;  // 2^shift threads share
+  const int width = kJoinThreads >> shift, mine = threadIdx.x / width, own = threadIdx.x % width;
+  auto piece = [&](int c) {  // in the CTAs behind the first it is the first of their items
+    return p.part + (static_cast<long long>(blockIdx.x + c) * 2 + (c == 0 ? it.slot : 0)) * stride * (p.dim + 4);
+  };
+  for (int i0 = blockIdx.y * width; i0 < all; i0 += width * gridDim.y) {
+    const int i = min(i0 + own, all - 1), x = i / it.rows, r = i - x * it.rows;  // lanes side by side have rows that are
     float m = -INFINITY;
 #pragma unroll 4
-    for (int c = c0 + warp; c <= c1; c += kJoinWarps) m = fmaxf(m, piece(c)[2 * r]);
-    s_top[warp][lane] = m;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kJoinWarps; ++w) m = fmaxf(m, s_top[w][lane]);
+    for (int c = mine; c < it.pieces; c += 1 << shift) m = fmaxf(m, piece(c)[2 * r]);
+    if (shift) {
+      s_top[threadIdx.x] = m;
+      __syncthreads();
+      for (int w = 0; w < 1 << shift; ++w) m = fmaxf(m, s_top[w * width + own]);
+    }
     const float off = m == -INFINITY ? 0.f : m;
     float l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-    for (int c = c0 + warp; c <= c1; c += kJoinWarps) {
+    for (int c = mine; c < it.pieces; c += 1 << shift) {
       const float* const at = piece(c);
       const float2 ml = *reinterpret_cast<const float2*>(at + 2 * r);
       const float4 f = *reinterpret_cast<const float4*>(at + (static_cast<long long>(x + 1) * stride + r) * 4);
@@ -862,18 +854,21 @@ __global__ void __launch_bounds__(32 * kJoinWarps) tree_join_kernel(const __grid
       l = fmaf(ml.y, k, l);
       o = make_float4(fmaf(f.x, k, o.x), fmaf(f.y, k, o.y), fmaf(f.z, k, o.z), fmaf(f.w, k, o.w));
     }
-    s_sum[warp][lane] = l;
-    s_o[warp][lane] = o;
-    __syncthreads();
-    if (warp == 0 && i0 + lane < all) {
-      for (int w = 1; w < kJoinWarps; ++w) {
-        const float4 f = s_o[w][lane];
-        l += s_sum[w][lane];
-        o = make_float4(o.x + f.x, o.y + f.y, o.z + f.z, o.w + f.w);
-      }
+    if (shift) {
+      s_sum[threadIdx.x] = l;
+      s_o[threadIdx.x] = o;
+      __syncthreads();
+      if (mine == 0)
+        for (int w = 1; w < 1 << shift; ++w) {
+          const float4 f = s_o[w * width + own];
+          l += s_sum[w * width + own];
+          o = make_float4(o.x + f.x, o.y + f.y, o.z + f.z, o.w + f.w);
+        }
+    }
+    if (mine == 0 && i0 + own < all) {
       const float inv = l == 0.f ? 0.f : 1.f / l;
-      const int node = (r0 + r) / p.group;
-      const long long row = (en.first + node) * p.q_heads + head * p.group + (r0 + r - node * p.group);
+      const int node = (it.r0 + r) / p.group;
+      const long long row = static_cast<long long>(it.first + node) * p.q_heads + it.head * p.group + (it.r0 + r - node * p.group);
       *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + row * p.dim + x * 4) =
           make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
       if (x == 0) p.lse[row] = l == 0.f ? -INFINITY : fmaf(m, p.scale, log2f(l)) * kLn2;
@@ -902,9 +897,8 @@ cudaError_t launch_tree_bf16(const TreeParams& p, cudaStream_t s) {
   else tree_kernel<1, false><<<grid, kThreads, kSmem, s>>>(p);
   const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  const int parts = (p.part_rows * (p.dim / 4) + 31) / 32;
-  return launch_chained(tree_join_kernel, dim3(grid - 1, parts < kJoinParts ? parts : kJoinParts), dim3(32 * kJoinWarps),
-                        0, s, p, grid);
+  const int parts = (p.part_rows * (p.dim / 4) + kJoinThreads - 1) / kJoinThreads;
+  return launch_chained(tree_join_kernel, dim3(grid - 1, parts < kJoinParts ? parts : kJoinParts), dim3(kJoinThreads), 0, s, p);
 }
 
 cudaError_t setup_tree_kernels() {
