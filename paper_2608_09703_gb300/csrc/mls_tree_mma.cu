@@ -817,60 +817,87 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
 }
 
 // Joins the pieces of the items that lie in several CTAs' ranges, in order: blocks x have those of the item that
-// CTA x began.  A thread has four values of a row; where there are many pieces, several threads share them.
+// CTA x began.  A thread has 16 values of a row; where there are many pieces, several threads share them.
 // (Where a block of 32 threads' work each looked for the item itself, 16 trees of 64 nodes took 178 us instead of 130.)
-constexpr int kJoinThreads = 256, kJoinParts = 32;
+constexpr int kJoinThreads = 256, kJoinParts = 8, kJoinWide = 4;  // pieces of four values a thread
 __global__ void __launch_bounds__(kJoinThreads) tree_join_kernel(const __grid_constant__ TreeParams p) {
   __shared__ float s_top[kJoinThreads], s_sum[kJoinThreads];
-  __shared__ float4 s_o[kJoinThreads];
+  __shared__ float4 s_o[kJoinWide][kJoinThreads];
   chain_wait();
   const TreeJoin it = p.joins[blockIdx.x];
-  const int all = it.rows * (p.dim / 4), stride = p.part_rows;
+  const int units = p.dim / 4, all = it.rows * ((units + kJoinWide - 1) / kJoinWide), stride = p.part_rows;
   const int shift = it.pieces <= 4 ? 0 : it.pieces <= 8 ? 1 : it.pieces <= 16 ? 2 : 3;  // 2^shift threads share
-  const int width = kJoinThreads >> shift, mine = threadIdx.x / width, own = threadIdx.x % width;
+  const int width = kJoinThreads >> shift, mine = threadIdx.x / width, own = threadIdx.x % width, step = 1 << shift;
   auto piece = [&](int c) {  // in the CTAs behind the first it is the first of their items
     return p.part + (static_cast<long long>(blockIdx.x + c) * 2 + (c == 0 ? it.slot : 0)) * stride * (p.dim + 4);
   };
   for (int i0 = blockIdx.y * width; i0 < all; i0 += width * gridDim.y) {
-    const int i = min(i0 + own, all - 1), x = i / it.rows, r = i - x * it.rows;  // lanes side by side have rows that are
-    float m = -INFINITY;
-#pragma unroll 4
-    for (int c = mine; c < it.pieces; c += 1 << shift) m = fmaxf(m, piece(c)[2 * r]);
+    const int i = min(i0 + own, all - 1), x = i / it.rows * kJoinWide, r = i % it.rows;  // lanes side by side: rows that are
+    float m = -INFINITY, l = 0.f;
+    float4 o[kJoinWide];
+#pragma unroll
+    for (int y = 0; y < kJoinWide; ++y) o[y] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int c = mine; c < it.pieces; c += 4 * step) {
+      float top[4];
+#pragma unroll
+      for (int y = 0; y < 4; ++y) top[y] = c + y * step < it.pieces ? piece(c + y * step)[2 * r] : -INFINITY;
+#pragma unroll
+      for (int y = 0; y < 4; ++y) m = fmaxf(m, top[y]);
+    }
     if (shift) {
       s_top[threadIdx.x] = m;
       __syncthreads();
-      for (int w = 0; w < 1 << shift; ++w) m = fmaxf(m, s_top[w * width + own]);
+      for (int w = 0; w < step; ++w) m = fmaxf(m, s_top[w * width + own]);
     }
     const float off = m == -INFINITY ? 0.f : m;
-    float l = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int c = mine; c < it.pieces; c += 1 << shift) {
-      const float* const at = piece(c);
-      const float2 ml = *reinterpret_cast<const float2*>(at + 2 * r);
-      const float4 f = *reinterpret_cast<const float4*>(at + (static_cast<long long>(x + 1) * stride + r) * 4);
-      if (ml.y == 0.f) continue;
-      const float k = ml.x == -INFINITY ? 1.f : fast_exp2((ml.x - off) * p.scale);  // a sum without a maximum is NaN
-      l = fmaf(ml.y, k, l);
-      o = make_float4(fmaf(f.x, k, o.x), fmaf(f.y, k, o.y), fmaf(f.z, k, o.z), fmaf(f.w, k, o.w));
+    for (int c = mine; c < it.pieces; c += 2 * step) {
+      float2 ml[2];
+      float4 f[2][kJoinWide];
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        const bool in = c + z * step < it.pieces;
+        const float* const at = piece(in ? c + z * step : c);
+        ml[z] = in ? *reinterpret_cast<const float2*>(at + 2 * r) : make_float2(-INFINITY, 0.f);
+#pragma unroll
+        for (int y = 0; y < kJoinWide; ++y)
+          if (x + y < units) f[z][y] = *reinterpret_cast<const float4*>(at + (static_cast<long long>(x + y + 1) * stride + r) * 4);
+      }
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        if (ml[z].y == 0.f) continue;
+        const float k = ml[z].x == -INFINITY ? 1.f : fast_exp2((ml[z].x - off) * p.scale);  // a sum without a maximum is NaN
+        l = fmaf(ml[z].y, k, l);
+#pragma unroll
+        for (int y = 0; y < kJoinWide; ++y)
+          o[y] = make_float4(fmaf(f[z][y].x, k, o[y].x), fmaf(f[z][y].y, k, o[y].y), fmaf(f[z][y].z, k, o[y].z),
+                             fmaf(f[z][y].w, k, o[y].w));
+      }
     }
     if (shift) {
       s_sum[threadIdx.x] = l;
-      s_o[threadIdx.x] = o;
+#pragma unroll
+      for (int y = 0; y < kJoinWide; ++y) s_o[y][threadIdx.x] = o[y];
       __syncthreads();
       if (mine == 0)
-        for (int w = 1; w < 1 << shift; ++w) {
-          const float4 f = s_o[w * width + own];
+        for (int w = 1; w < step; ++w) {
           l += s_sum[w * width + own];
-          o = make_float4(o.x + f.x, o.y + f.y, o.z + f.z, o.w + f.w);
+#pragma unroll
+          for (int y = 0; y < kJoinWide; ++y) {
+            const float4 f = s_o[y][w * width + own];
+            o[y] = make_float4(o[y].x + f.x, o[y].y + f.y, o[y].z + f.z, o[y].w + f.w);
+          }
         }
     }
     if (mine == 0 && i0 + own < all) {
       const float inv = l == 0.f ? 0.f : 1.f / l;
       const int node = (it.r0 + r) / p.group;
       const long long row = static_cast<long long>(it.first + node) * p.q_heads + it.head * p.group + (it.r0 + r - node * p.group);
-      *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + row * p.dim + x * 4) =
-          make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+      __nv_bfloat16* const out = static_cast<__nv_bfloat16*>(p.out) + row * p.dim + x * 4;
+#pragma unroll
+      for (int y = 0; y < kJoinWide; y += 2)  // values come in eights
+        if (x + y < units)
+          st16(out + 4 * y, make_uint4(pack_bf16(o[y].x * inv, o[y].y * inv), pack_bf16(o[y].z * inv, o[y].w * inv),
+                                       pack_bf16(o[y + 1].x * inv, o[y + 1].y * inv), pack_bf16(o[y + 1].z * inv, o[y + 1].w * inv)));
       if (x == 0) p.lse[row] = l == 0.f ? -INFINITY : fmaf(m, p.scale, log2f(l)) * kLn2;
     }
   }
@@ -897,7 +924,7 @@ cudaError_t launch_tree_bf16(const TreeParams& p, cudaStream_t s) {
   else tree_kernel<1, false><<<grid, kThreads, kSmem, s>>>(p);
   const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  const int parts = (p.part_rows * (p.dim / 4) + kJoinThreads - 1) / kJoinThreads;
+  const int parts = (p.part_rows * ((p.dim + 4 * kJoinWide - 1) / (4 * kJoinWide)) + kJoinThreads - 1) / kJoinThreads;
   return launch_chained(tree_join_kernel, dim3(grid - 1, parts < kJoinParts ? parts : kJoinParts), dim3(kJoinThreads), 0, s, p);
 }
 
