@@ -14,7 +14,7 @@
 //
 // Which token an inverse CDF finds depends on where its sums' edges lie, so the sums are taken in two
 // fp32 words, p - c q too, and decisions are made in 64 bits: a handful per node.  (64-bit sums of a
-// row of 50304 would take an SM's two units 12 us; these take 2.)
+// row of 50304 would take an SM's two units 12 us.)
 // A sequence has a cluster of CTAs, each with a part of the vocabulary, whose warps' sums meet in
 // shared memory; all walk alike.
 #include <climits>
@@ -27,7 +27,7 @@
 namespace mls {
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
 constexpr int kSpan = 128;  // values that a warp reads at a time
 
@@ -48,7 +48,6 @@ struct Walk {
   // next pass while another still reads the sums of this one.
   alignas(8) Pair sums[2][kMaxCluster * kWarps];               // written from other CTAs, two words at a time
   alignas(8) Pair mass[2][kMaxCluster * kWarps];
-  double base[kWarps];
   Pair warp_sums[kWarps];
   double before, goal;           // of the part that holds the token drawn: the sum before it, u times the whole
   int part, found, last;
@@ -91,16 +90,38 @@ __device__ __forceinline__ Pair value(const Walk& s, const Pass& a, float p, flo
   return w;
 }
 
-// The sums of a pass over this warp's part [v0, v1) of the row, to every CTA of the cluster.
+// pair_add and residual of two values at a time.
+struct Pair2 {
+  float2 hi, lo;
+};
+__device__ __forceinline__ void pair2_add(Pair2& a, const float2& hi, const float2& lo) {
+  const float2 s = add2(a.hi, hi), b = sub2(s, a.hi);
+  a.lo = add2(a.lo, add2(add2(sub2(a.hi, sub2(s, b)), sub2(hi, b)), lo));
+  a.hi = s;
+}
+__device__ __forceinline__ Pair2 residual2(const float2& p, const float2& q, float c_hi, float c_lo) {
+  const float2 hi = make_float2(c_hi, c_hi);
+  const float2 na = mul2(make_float2(-c_hi, -c_hi), q), b = fma2(make_float2(c_lo, c_lo), q, fma2(hi, q, na));
+  const float2 d = add2(p, na), e = sub2(d, p);
+  const float2 rest = sub2(sub2(sub2(p, sub2(d, e)), sub2(e, na)), b), all = add2(d, rest);
+  const bool x = all.x > 0.f, y = all.y > 0.f;
+  return {make_float2(x ? d.x : 0.f, y ? d.y : 0.f), make_float2(x ? rest.x : 0.f, y ? rest.y : 0.f)};
+}
+
+// The sums of a pass over this warp's part [v0, v1) of the row, to every CTA of the cluster.  Arithmetic bounds it
+// (some 16 operations a value), so it is done on two values an instruction, and only stretches with a refused
+// token look at which it is.
 template <bool kDraft, bool kMass>
 __device__ void row_pass(const AcceptParams& p, Walk& s, const Pass& a, long long row, long long v0, long long v1,
                          int buffer, int slot) {
   const int lane = threadIdx.x & 31;
   const float* const P = p.target + row * p.ld_target;
   const float* const Q = kDraft ? p.draft + row * p.ld_draft : nullptr;
-  Pair sum = two(0.f), mass = two(0.f);
+  const float2 zero = make_float2(0.f, 0.f);
+  Pair2 sum = {zero, zero}, mass = {zero, zero};
   constexpr int kDeep = 8;
-  for (long long b = v0 + lane; b < v1; b += 32 * kDeep) {
+  for (long long b0 = v0; b0 < v1; b0 += 32 * kDeep) {
+    const long long b = b0 + lane;
     float x[kDeep], y[kDeep];
 #pragma unroll
     for (int j = 0; j < kDeep; ++j) {
@@ -108,51 +129,72 @@ __device__ void row_pass(const AcceptParams& p, Walk& s, const Pass& a, long lon
       x[j] = in ? P[b + 32 * j] : 0.f;
       y[j] = in && kDraft ? Q[b + 32 * j] : 0.f;
     }
+    bool some = false;
+    for (int j = 0; j < a.refused; ++j) some |= s.refused[j] >= b0 && s.refused[j] < b0 + 32 * kDeep;
 #pragma unroll
-    for (int j = 0; j < kDeep; ++j) {
-      const Pair w = value<kDraft>(s, a, x[j], y[j], static_cast<int>(b + 32 * j));
-      pair_add(sum, w.hi, w.lo);
-      if (kMass) pair_add(mass, y[j], 0.f);
+    for (int j = 0; j < kDeep; j += 2) {
+      Pair2 w = {make_float2(x[j], x[j + 1]), zero};
+      if (some) {
+        const Pair w0 = value<kDraft>(s, a, x[j], y[j], static_cast<int>(b + 32 * j));
+        const Pair w1 = value<kDraft>(s, a, x[j + 1], y[j + 1], static_cast<int>(b + 32 * j + 32));
+        w = {make_float2(w0.hi, w1.hi), make_float2(w0.lo, w1.lo)};
+      } else if (kDraft) {
+        w = residual2(w.hi, make_float2(y[j], y[j + 1]), a.c_hi, a.c_lo);
+      }
+      pair2_add(sum, w.hi, w.lo);
+      if (kMass) pair2_add(mass, make_float2(y[j], y[j + 1]), zero);
     }
   }
-  sum = warp_sum_pair(sum);
-  if (kMass) mass = warp_sum_pair(mass);
+  auto total = [](const Pair2& t) {
+    Pair one = {t.hi.x, t.lo.x};
+    pair_add(one, t.hi.y, t.lo.y);
+    return warp_sum_pair(one);
+  };
+  const Pair one = total(sum), left = kMass ? total(mass) : two(0.f);
   if (lane == 0)
     for (int r = 0; r < p.cluster; ++r) {
-      store_remote(map_to_rank(smem_u32(&s.sums[buffer][slot]), r), sum.hi, sum.lo);
-      if (kMass) store_remote(map_to_rank(smem_u32(&s.mass[buffer][slot]), r), mass.hi, mass.lo);
+      store_remote(map_to_rank(smem_u32(&s.sums[buffer][slot]), r), one.hi, one.lo);
+      if (kMass) store_remote(map_to_rank(smem_u32(&s.mass[buffer][slot]), r), left.hi, left.lo);
     }
 }
 
-__device__ __forceinline__ double warp_total(const Pair* x, int n) {
-  double sum = 0.0;
-  for (int j = threadIdx.x & 31; j < n; j += 32) sum += pair_value(x[j]);
+// Inclusive sums over the lanes.
+__device__ __forceinline__ Pair warp_scan_pair(Pair a) {
+  const int lane = threadIdx.x & 31;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  return sum;
+  for (int o = 1; o < 32; o <<= 1) {
+    const float hi = __shfl_up_sync(0xffffffffu, a.hi, o), lo = __shfl_up_sync(0xffffffffu, a.lo, o);
+    if (lane >= o) pair_add(a, hi, lo);
+  }
+  return a;
 }
+constexpr int kEach = kMaxCluster * kWarps / 32;  // warps' sums that a lane has
+static_assert(kMaxCluster * kWarps % 32 == 0, "a lane's share");
+// A lane's share of the warps' sums of a pass, and those up to it.
+struct Sums {
+  Pair mine, upto;
+  __device__ __forceinline__ Sums(const Pair* x, int warps) : mine(two(0.f)) {
+    const int at = (threadIdx.x & 31) * kEach;
+    for (int j = 0; j < kEach; ++j)
+      if (at + j < warps) pair_add(mine, x[at + j].hi, x[at + j].lo);
+    upto = warp_scan_pair(mine);
+  }
+  __device__ __forceinline__ double total() const {
+    return pair_value({__shfl_sync(0xffffffffu, upto.hi, 31), __shfl_sync(0xffffffffu, upto.lo, 31)});
+  }
+};
 
 // Which warp's part holds the token that u draws from the sums.  Warp 0 calls it.
 __device__ void choose_part(Walk& s, const Pair* sums, int warps, float u) {
-  constexpr int kEach = kMaxCluster * kWarps / 32;
   const int lane = threadIdx.x & 31;
-  double mine = 0.0;
-  for (int j = 0; j < kEach; ++j)
-    if (lane * kEach + j < warps) mine += pair_value(sums[lane * kEach + j]);
-  double upto = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const double w = __shfl_up_sync(0xffffffffu, upto, o);
-    if (lane >= o) upto += w;
-  }
-  const double goal = static_cast<double>(u) * __shfl_sync(0xffffffffu, upto, 31);
-  const double before = upto - mine;
-  // The first lane whose sum passes the goal; of rounding, another's `before` may be past it by a little.
-  const unsigned past = __ballot_sync(0xffffffffu, upto > goal && mine > 0.0);
+  const Sums own(sums, warps);
+  const double goal = static_cast<double>(u) * own.total(), end = pair_value(own.upto), mine = pair_value(own.mine);
+  // The first lane whose sum passes the goal; of rounding, another's begin may be past it by a little.
+  const unsigned past = __ballot_sync(0xffffffffu, end > goal && mine > 0.0);
   if (lane == 0) s.part = -1;
   __syncwarp();
   if (past && lane == __ffs(past) - 1) {
-    double at = before;
+    double at = end - mine;
     int part = -1;
     for (int j = 0; j < kEach && lane * kEach + j < warps; ++j) {
       const double v = pair_value(sums[lane * kEach + j]);
@@ -177,46 +219,39 @@ __device__ void draw(const AcceptParams& p, Walk& s, const Pass& a, long long ro
   const long long each = (v1 - v0 + kThreads - 1) / kThreads;
   const long long a0 = min(v0 + tid * each, v1), a1 = min(a0 + each, v1);
   Pair sum = two(0.f);
-  int last = -1;
+  int first = -1, last = -1;
+#pragma unroll 4
   for (long long v = a0; v < a1; ++v) {
     float q = kDraft ? Q[v] : 0.f;
     const Pair w = value<kDraft>(s, a, P[v], q, static_cast<int>(v));
-    if (w.hi + w.lo > 0.f) last = static_cast<int>(v);
+    if (w.hi + w.lo > 0.f) {
+      last = static_cast<int>(v);
+      if (first < 0) first = last;
+    }
     pair_add(sum, w.hi, w.lo);
   }
   if (tid == 0) s.found = INT_MAX, s.last = -1;
-  Pair upto = sum;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const float hi = __shfl_up_sync(0xffffffffu, upto.hi, o), lo = __shfl_up_sync(0xffffffffu, upto.lo, o);
-    if (lane >= o) pair_add(upto, hi, lo);
-  }
+  const Pair upto = warp_scan_pair(sum);
   if (lane == 31) s.warp_sums[warp] = upto;
   __syncthreads();
-  if (warp == 0) {
-    const double mine = lane < kWarps ? pair_value(s.warp_sums[lane]) : 0.0;
-    double w = mine;
-#pragma unroll
-    for (int o = 1; o < kWarps; o <<= 1) {
-      const double x = __shfl_up_sync(0xffffffffu, w, o);
-      if (lane >= o) w += x;
-    }
-    if (lane < kWarps) s.base[lane] = s.before + (w - mine);
-  }
+  Pair base = two(0.f);
+  for (int w = 0; w < warp; ++w) pair_add(base, s.warp_sums[w].hi, s.warp_sums[w].lo);
   if (last >= 0) atomicMax(&s.last, last);
-  __syncthreads();
-  const double goal = s.goal, end = s.base[warp] + pair_value(upto);
+  const double goal = s.goal, end = s.before + pair_value(base) + pair_value(upto), begin = end - pair_value(sum);
   if (end > goal && last >= 0) {
-    Pair cum = two(0.f);
-    const double begin = end - pair_value(sum);
-    for (long long v = a0; v < a1; ++v) {
-      float q = kDraft ? Q[v] : 0.f;
-      const Pair w = value<kDraft>(s, a, P[v], q, static_cast<int>(v));
-      if (!(w.hi + w.lo > 0.f)) continue;
-      pair_add(cum, w.hi, w.lo);
-      if (begin + pair_value(cum) > goal) {
-        atomicMin(&s.found, static_cast<int>(v));
-        break;
+    if (begin > goal) {
+      atomicMin(&s.found, first);
+    } else {
+      Pair cum = two(0.f);
+      for (long long v = a0; v < a1; ++v) {
+        float q = kDraft ? Q[v] : 0.f;
+        const Pair w = value<kDraft>(s, a, P[v], q, static_cast<int>(v));
+        if (!(w.hi + w.lo > 0.f)) continue;
+        pair_add(cum, w.hi, w.lo);
+        if (begin + pair_value(cum) > goal) {
+          atomicMin(&s.found, static_cast<int>(v));
+          break;
+        }
       }
     }
   }
@@ -224,7 +259,7 @@ __device__ void draw(const AcceptParams& p, Walk& s, const Pass& a, long long ro
   if (tid == 0) *next = s.found != INT_MAX ? s.found : s.last;  // the goal within rounding of the part's end
 }
 
-__global__ void __launch_bounds__(kThreads) accept_kernel(AcceptParams p) {
+__global__ void __launch_bounds__(kThreads, 4) accept_kernel(AcceptParams p) {
   __shared__ Walk s;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = p.cluster > 1 ? static_cast<int>(cluster_ctarank()) : 0;
@@ -269,7 +304,7 @@ __global__ void __launch_bounds__(kThreads) accept_kernel(AcceptParams p) {
   while (true) {
     if (warp == 0) {
       if (pending) {
-        const double sum = warp_total(s.sums[buffer], warps);
+        const double sum = Sums(s.sums[buffer], warps).total();
         fresh = sum > 0.0;
         if (fresh) {
           Z = sum;
@@ -279,7 +314,7 @@ __global__ void __launch_bounds__(kThreads) accept_kernel(AcceptParams p) {
           if (listed && drafted && lane == 0) split(c_old, s.c_hi[refused - 1], s.c_lo[refused - 1]);
         }
         if (distinct) {
-          const double left = warp_total(s.mass[buffer], warps);
+          const double left = Sums(s.mass[buffer], warps).total();
           share = left > 0.0 ? 1.0 / left : 0.0;
         }
         pending = false;
@@ -380,10 +415,12 @@ cudaError_t launch_accept(const AcceptParams& p, cudaStream_t s) {
   return e;
 }
 
-// Enough CTAs of a sequence that few sequences fill the card too.
+// Enough CTAs of a sequence that few sequences fill the card too, four an SM, but no fewer than 16 values a thread.
+// (CTAs of 512 threads, one an SM: 102 chains at V = 50304 28.7 us, 64 trees at V = 128256 54 after the pass was packed;
+// of 256, two an SM: 28.6 and 72; four: 22.5 and 50.)
 int accept_cluster(int n, long long V, int sms) {
   int c = 1;
-  while (c < kMaxCluster && static_cast<long long>(n) * 2 * c <= sms && V / (2 * c) >= 4096) c *= 2;
+  while (c < kMaxCluster && static_cast<long long>(n) * 2 * c <= 4 * sms && V / (2 * c) >= 4096) c *= 2;
   return c;
 }
 

@@ -670,14 +670,14 @@ __device__ __forceinline__ float fmax3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
   return y;
 }
-// Two fp32 operations in one instruction: v * s + t, and a + b.
-__device__ __forceinline__ float2 fma2(const float2& v, float s, float t) {
+// Two fp32 operations in one instruction: a * b + c, a + b, a - b.
+__device__ __forceinline__ float2 fma2(const float2& a, const float2& b, const float2& c) {
   float2 y;
-  asm("{\n\t.reg .b64 v, s, t, y;\n\t"
-      "mov.b64 v, {%2, %3};\n\tmov.b64 s, {%4, %4};\n\tmov.b64 t, {%5, %5};\n\t"
-      "fma.rn.f32x2 y, v, s, t;\n\tmov.b64 {%0, %1}, y;\n\t}"
+  asm("{\n\t.reg .b64 a, b, c, y;\n\t"
+      "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+      "fma.rn.f32x2 y, a, b, c;\n\tmov.b64 {%0, %1}, y;\n\t}"
       : "=f"(y.x), "=f"(y.y)
-      : "f"(v.x), "f"(v.y), "f"(s), "f"(t));
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
   return y;
 }
 __device__ __forceinline__ float2 add2(const float2& a, const float2& b) {
@@ -688,6 +688,18 @@ __device__ __forceinline__ float2 add2(const float2& a, const float2& b) {
       : "=f"(y.x), "=f"(y.y)
       : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
   return y;
+}
+__device__ __forceinline__ float2 mul2(const float2& a, const float2& b) {
+  float2 y;
+  asm("{\n\t.reg .b64 a, b, y;\n\t"
+      "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+      "mul.rn.f32x2 y, a, b;\n\tmov.b64 {%0, %1}, y;\n\t}"
+      : "=f"(y.x), "=f"(y.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return y;
+}
+__device__ __forceinline__ float2 sub2(const float2& a, const float2& b) {
+  return fma2(b, make_float2(-1.f, -1.f), a);
 }
 
 // Register reallocation between warpgroups (all four warps of a warpgroup

@@ -59,6 +59,7 @@ struct Tail {
     float2 ml[kRows];
   } row[2];
   long long scan[kThreads / 32], base0;
+  Entry en0;                                      // the range's first entry, its number and first unit
   int e0, abort;
   int fix[2];                                     // by a segment's parity: the last one with values taken out
   uint32_t tmem_slot;
@@ -111,7 +112,7 @@ __device__ void plan_role(const TreeParams& p, Tail* sh, long long at, long long
   Entry en;
   long long units = 0;
   if (at < hi) {
-    en = tree_entry(p, e, p.status);
+    en = sh->en0;
     units = entry_units(p, en);
   }
   while (at < hi) {
@@ -588,6 +589,7 @@ __device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint3
           }
         }
         const float off = m == -INFINITY ? 0.f : -m * p.scale;
+        const float2 scale2 = make_float2(p.scale, p.scale), off2 = make_float2(off, off);
         float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
         // The MMAs of the first half of the keys begin while the second half's exponentials are taken.
 #pragma unroll
@@ -595,7 +597,7 @@ __device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint3
           uint32_t u[kKeys / 4];
 #pragma unroll
           for (int x = 0; x < kKeys / 2; x += 2) {
-            const float2 e = fma2(make_float2(z[64 * h + x], z[64 * h + x + 1]), p.scale, off);
+            const float2 e = fma2(make_float2(z[64 * h + x], z[64 * h + x + 1]), scale2, off2);
             const float2 f = make_float2(fast_exp2(e.x), fast_exp2(e.y));
             sum[(x >> 1) & 1] = add2(sum[(x >> 1) & 1], f);
             u[x / 2] = pack_bf16(f.x, f.y);
@@ -783,6 +785,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
     for (int i = i0; i < i1; ++i) {
       const long long u = i1 - i0 == 1 ? mine : entry_units(p, tree_entry(p, i, p.status));
       if (at <= lo && lo < at + u) {
+        sh->en0 = tree_entry(p, i, p.status);
         sh->e0 = i;
         sh->base0 = at;
       }
