@@ -1999,41 +1999,39 @@ int tree_validate(const mls_cache* c, int n, int64_t N, int q_heads) {
   return MLS_OK;
 }
 
-struct TreePlan {
-  int splits, part_rows;
-  size_t off_part, total;
-};
-TreePlan tree_plan(const mls_cache* c, int64_t N, int q_heads, int sms) {
-  TreePlan pl;
-  const size_t row = sizeof(float) * (c->head_dim + 4);
-  pl.splits = tree_fp32_splits(N, q_heads, sms);
-  pl.part_rows = tree_part_rows(N, q_heads / c->kv_heads);
-  if (c->dtype == MLS_FP32) {
-    pl.off_part = 0;
-    pl.total = align_up(pl.splits > 1 ? row * N * q_heads * pl.splits : 1);
-  } else {
-    pl.off_part = align_up(sizeof(TreeJoin) * sms);
-    pl.total = pl.off_part + align_up(row * 2 * sms * pl.part_rows);
-  }
-  return pl;
+// Sizes of a call, and its workspace: what CTAs leave for the join, then the pieces.
+size_t tree_plan(TreeParams* p, const mls_cache* c, int n, int64_t N, int q_heads, int sms) {
+  std::memset(p, 0, sizeof *p);
+  p->bf16 = c->dtype == MLS_BF16;
+  p->joint = p->bf16 && c->head_dim == 128;
+  p->n = n;
+  p->N = N;
+  p->q_heads = q_heads;
+  p->group = q_heads / c->kv_heads;
+  p->dim = c->head_dim;
+  p->sms = sms;
+  tree_sizes(p);
+  return align_up(sizeof(TreeJoin) * sms) + align_up(sizeof(float) * (p->dim + 4) * 2 * sms * p->part_rows);
 }
 
 // The cache's k or v as [layers * pages * heads][page_size][head_dim], in boxes (128 bytes wide, swizzled) of
-// the tokens of one page, or of as many as a tile has: 64 values of each, or, where a token has 128, all of them,
-// the two halves of 8 tokens behind one another.
-int encode_pages(CUtensorMap* map, const mls_cache* c, const void* ptr, bool joint) {
+// the tokens of one page, or of as many as a tile has: 128 bytes of each, or, where a token has 256 (bf16), all of
+// them, the two halves of 8 tokens behind one another.
+int encode_pages(CUtensorMap* map, const mls_cache* c, const void* ptr, const TreeParams& p) {
+  const cuuint64_t elt = p.bf16 ? 2 : 4, wide = 128 / elt;
   const cuuint64_t dim = c->head_dim, size = c->page_size, all = static_cast<cuuint64_t>(c->layers) * c->pages * c->kv_heads;
-  const cuuint32_t tokens = static_cast<cuuint32_t>(c->page_size < 128 ? c->page_size : 128);
+  const cuuint32_t most = 1u << p.key_shift, tokens = static_cast<cuuint32_t>(size) < most ? static_cast<cuuint32_t>(size) : most;
   const cuuint64_t dims[5] = {64, 8, 2, size / 8, all}, strides[4] = {dim * 2, 128, dim * 16, dim * size * 2};
   const cuuint32_t box[5] = {64, 8, 2, tokens / 8, 1}, estr[5] = {1, 1, 1, 1, 1};
-  const cuuint64_t dims3[3] = {dim, size, all}, strides3[2] = {dim * 2, dim * size * 2};
-  const cuuint32_t box3[3] = {64, tokens, 1};
-  const CUresult r = g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, joint ? 5 : 3, const_cast<void*>(ptr),
-                              joint ? dims : dims3, joint ? strides : strides3, joint ? box : box3, estr,
-                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+  const cuuint64_t dims3[3] = {dim, size, all}, strides3[2] = {dim * elt, dim * size * elt};
+  const cuuint32_t box3[3] = {static_cast<cuuint32_t>(wide), tokens, 1};
+  const CUresult r = g_encode(map, p.bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, p.joint ? 5 : 3,
+                              const_cast<void*>(ptr), p.joint ? dims : dims3, p.joint ? strides : strides3, p.joint ? box : box3,
+                              estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? MLS_OK : fail(MLS_ERR_CUDA, "cuTensorMapEncodeTiled (cache)");
 }
+
 // The queries as [N][q_heads][head_dim], in boxes of 64 values of a group's heads of some nodes.
 int encode_queries(TreeParams* p) {
   const cuuint64_t dims[3] = {static_cast<cuuint64_t>(p->dim), static_cast<cuuint64_t>(p->q_heads), static_cast<cuuint64_t>(p->N)};
@@ -2049,7 +2047,8 @@ int encode_queries(TreeParams* p) {
 
 extern "C" size_t mls_tree_attention_workspace_size(const mls_cache* c, int32_t n, int64_t N, int32_t q_heads) {
   if (tree_validate(c, n, N, q_heads)) return 0;
-  return tree_plan(c, N, q_heads, current_sms()).total;
+  TreeParams p;
+  return tree_plan(&p, c, n, N, q_heads, current_sms());
 }
 
 extern "C" int mls_tree_attention(const mls_cache* c, int32_t layer, int32_t n, const int32_t* seqs,
@@ -2066,20 +2065,14 @@ extern "C" int mls_tree_attention(const mls_cache* c, int32_t layer, int32_t n, 
   if (q_ld % (c->dtype == MLS_BF16 ? 8 : 4) || !aligned16(q) || !aligned16(out) || !aligned4(lse) || !aligned4(seqs) ||
       !aligned4(start) || !aligned4(parents))
     return MLS_ERR_ALIGN;
-  const TreePlan pl = tree_plan(c, N, q_heads, current_sms());
-  if (!ws || (reinterpret_cast<uintptr_t>(ws) % kAlign) != 0 || ws_bytes < pl.total) return MLS_ERR_WORKSPACE;
+  TreeParams p;
+  const size_t need = tree_plan(&p, c, n, N, q_heads, current_sms());
+  if (!ws || (reinterpret_cast<uintptr_t>(ws) % kAlign) != 0 || ws_bytes < need) return MLS_ERR_WORKSPACE;
   DeviceState* dev = nullptr;
   if ((rc = device_state(&dev))) return rc;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  TreeParams p;
-  std::memset(&p, 0, sizeof p);
   p.c = cache_view(c, dev);
   p.layer = layer;
-  p.n = n;
-  p.N = N;
-  p.q_heads = q_heads;
-  p.group = q_heads / c->kv_heads;
-  p.dim = c->head_dim;
   p.seqs = seqs;
   p.start = start;
   p.parents = parents;
@@ -2091,22 +2084,12 @@ extern "C" int mls_tree_attention(const mls_cache* c, int32_t layer, int32_t n, 
   p.negate = scale < 0.f;
   p.out = out;
   p.lse = lse;
-  p.part = reinterpret_cast<float*>(static_cast<char*>(ws) + pl.off_part);
-  p.part_rows = pl.part_rows;
   p.joins = static_cast<TreeJoin*>(ws);
-  p.splits = pl.splits;
+  p.part = reinterpret_cast<float*>(static_cast<char*>(ws) + align_up(sizeof(TreeJoin) * p.sms));
   p.status = dev->status;
-  p.sms = dev->sms;
-  if (c->dtype == MLS_BF16) {
-    p.joint = c->head_dim == 128;
-    p.tile_rows = tree_tile_rows(p.group);
-    p.q_rows = tree_query_rows(p.group);
-    if (encode_pages(&p.map_k, c, c->k, p.joint) || encode_pages(&p.map_v, c, c->v, p.joint) ||
-        (p.q_rows && encode_queries(&p)))
-      return MLS_ERR_CUDA;
-  }
-  return timed("tree_attention", s,
-               [&] { return c->dtype == MLS_FP32 ? launch_tree_fp32(p, s) : launch_tree_bf16(p, s); });
+  if (encode_pages(&p.map_k, c, c->k, p) || encode_pages(&p.map_v, c, c->v, p) || (p.q_rows && encode_queries(&p)))
+    return MLS_ERR_CUDA;
+  return timed("tree_attention", s, [&] { return p.bf16 ? launch_tree_bf16(p, s) : launch_tree_fp32(p, s); });
 }
 
 extern "C" int mls_tree_verify(const mls_tree_problem* p, const float* target, const float* draft,

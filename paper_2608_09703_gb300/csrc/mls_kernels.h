@@ -583,10 +583,12 @@ struct TreeJoin {
 };
 struct TreeParams {
   CacheView c;
-  CUtensorMap map_k, map_v;      // bf16: boxes of one head and page, of 64 values a token or (joint) 128
-  CUtensorMap map_q;             // boxes of a group's heads and some nodes, q_rows rows (0: no map) of 64 values
-  int q_rows, tile_rows;         // tile_rows of a row tile's 128 are used
-  int joint;
+  // Boxes of one head and page, 128 bytes of each token's row (joint: both halves of 256).
+  CUtensorMap map_k, map_v;
+  CUtensorMap map_q;             // bf16: boxes of a group's heads and some nodes, q_rows rows (0: no map) of 128 bytes
+  int bf16, joint;
+  int q_rows, tile_rows;         // bf16: tile_rows of a row tile's 128 are used
+  int item_rows, key_shift, over;  // rows and keys (2^key_shift) of a tile of work; units that an item costs beside its tiles
   int layer, n;
   long long N;
   int q_heads, group;            // group = query heads of a key/value head
@@ -598,24 +600,23 @@ struct TreeParams {
   int negate;
   void* out;
   float* lse;
-  int splits;                    // fp32: pieces of the keys
-  // Workspace: of rows whose keys are split their maximum, sum and product, dim + 4 words each.
-  // fp32: [N][q_heads][splits] of them.  bf16: [CTAs][2] times part_rows rows, a CTA's first and its last item:
-  // float2 [rows] of maximum and sum in the first 4 part_rows words, then float4 [dim / 4][part_rows].
+  // Workspace.  Of items whose keys are split, CTA c's first in [c][0] and its last in [c][1], part_rows rows each:
+  // float2 [part_rows] of maximum and sum in the first 4 part_rows words, then float4 [dim / 4][part_rows].
   float* part;
   int part_rows;
-  TreeJoin* joins;               // bf16: [CTAs]
+  TreeJoin* joins;               // [CTAs]
   int* status;
   int sms;
 };
 constexpr int kTreeMaxNodes = 256;
-cudaError_t launch_tree_fp32(const TreeParams& p, cudaStream_t s);
-cudaError_t launch_tree_bf16(const TreeParams& p, cudaStream_t s);
-int tree_fp32_splits(long long N, int q_heads, int sms);
-int tree_part_rows(long long N, int group);
+void tree_sizes(TreeParams* p);  // those that follow from bf16, group, n and N
 int tree_tile_rows(int group);
 int tree_query_rows(int group);
+cudaError_t launch_tree_fp32(const TreeParams& p, cudaStream_t s);
+cudaError_t launch_tree_bf16(const TreeParams& p, cudaStream_t s);
+cudaError_t launch_tree_join(const TreeParams& p, cudaStream_t s);
 cudaError_t setup_tree_kernels();
+cudaError_t setup_tree_mma_kernels();
 
 // ------------------------------------------------------------------ acceptance of drafted trees
 struct AcceptParams {

@@ -2,7 +2,13 @@
 // key/value cache.  For node t of an entry, query head h and its key/value head:
 //   out = sum_j softmax_j(scale q . k_j) v_j,   lse = log sum_j exp(scale q . k_j)
 // over the entry's cached tokens and the nodes on the path from t to its root, t included.
-#include <climits>
+// Here: the kernel of an fp32 cache, and the one that joins pieces (a bf16 cache's: mls_tree_mma.cu).
+//
+// fp32: products of full precision are the vector units' work.  An item has 16 rows (4, where entries have no more:
+// decoding) and tiles of 64 keys, of which each of eight warps has 8: a lane has a key and every fourth row of the
+// scores, then 16 columns and the same rows of the product, whose weights come by shuffles.  Warps keep a
+// maximum, sum and product of their own to the end of a segment.  K and V come by TMA, swizzled, so that eight keys'
+// same 16 bytes lie in different banks.  Arithmetic bounds long trees and prompts, HBM single tokens.
 #include <cmath>
 
 #include "mls_device.cuh"
@@ -13,216 +19,412 @@
 namespace mls {
 namespace {
 
-// ------------------------------------------------------------------ one warp a node
-// A warp takes one node and up to kHeads query heads of one key/value head, a piece of the keys, 32
-// of them at a time: each lane has a key, the products with the queries of the heads come from
-// shared memory; then each lane has four columns of the values.  All heads of a node see the same keys,
-// so what the mask leaves out is not even read.
-constexpr int kHeads = 4, kWarps = 4;
+constexpr int kWarps = 8, kKeys = 64, kThreads = 32 * (kWarps + 2);
+constexpr int kPieces = 4;                        // of 32 values, 128 bytes, a row
+constexpr uint32_t kPiece = kKeys * 128u, kTile = kPieces * kPiece;
+constexpr int kStages = 4;
+constexpr uint64_t kDrainNs = 100000000ull;
 
-template <typename E>
-__device__ __forceinline__ void load4(const E* p, float (&f)[4]);
-template <>
-__device__ __forceinline__ void load4<float>(const float* p, float (&f)[4]) {
-  const float4 v = *reinterpret_cast<const float4*>(p);
-  f[0] = v.x, f[1] = v.y, f[2] = v.z, f[3] = v.w;
-}
-template <>
-__device__ __forceinline__ void load4<__nv_bfloat16>(const __nv_bfloat16* p, float (&f)[4]) {
-  const uint2 v = *reinterpret_cast<const uint2*>(p);
-  f[0] = __uint_as_float(v.x << 16), f[1] = __uint_as_float(v.x & 0xffff0000u);
-  f[2] = __uint_as_float(v.y << 16), f[3] = __uint_as_float(v.y & 0xffff0000u);
-}
-__device__ __forceinline__ void store4(float* p, const float (&f)[4]) {
-  *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
-}
-__device__ __forceinline__ void store4(__nv_bfloat16* p, const float (&f)[4]) {
-  const __nv_bfloat162 a = __floats2bfloat162_rn(f[0], f[1]), b = __floats2bfloat162_rn(f[2], f[3]);
-  *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
-}
+template <int RW>
+struct Shared {
+  uint8_t ring[kStages][kTile];
+  float o[kWarps][RW][128];
+  float q[RW][132];                               // a row's end shifts the next one's banks
+  float2 ml[kWarps][RW];
+  unsigned path[RW][kTreeMaxNodes / 32];          // the nodes that a row sees, a bit each
+  int used[RW], upto[RW];                         // upto: chains, keys that a row sees
+  short up[kTreeMaxNodes];
+  struct : Plan {
+    uint64_t full[kStages], empty[kStages];
+  } tail;
+};
 
-template <typename E>
-__global__ void __launch_bounds__(32 * kWarps) node_kernel(TreeParams p) {
-  __shared__ float qs[kWarps][kHeads][128];
-  __shared__ short up[kWarps][kTreeMaxNodes];
-  __shared__ unsigned see[kWarps][kTreeMaxNodes / 32];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int chunks = (p.group + kHeads - 1) / kHeads;
-  const long long per_node = static_cast<long long>(p.c.heads) * chunks * p.splits;
-  const long long task = static_cast<long long>(blockIdx.x) * kWarps + warp;
-  if (task >= p.N * per_node) return;
-  const long long t = task / per_node;
-  int rest = static_cast<int>(task - t * per_node);
-  const int split = rest % p.splits;
-  rest /= p.splits;
-  const int chunk = rest % chunks, kvh = rest / chunks;
-  const int h0 = kvh * p.group + chunk * kHeads, nh = min(kHeads, p.group - chunk * kHeads);
-  int mine = -1;
-  for (int i0 = 0; i0 < p.n && mine < 0; i0 += 32) {
-    const int i = i0 + lane;
-    const bool here = i < p.n && p.start[i] <= t && t < p.start[i + 1];
-    const unsigned b = __ballot_sync(0xffffffffu, here);
-    if (b) mine = i0 + __ffs(b) - 1;
-  }
-  if (mine < 0) return;  // behind the last entry: left as it was
-  const Entry e = tree_entry(p, mine, p.status);
-  const int node = static_cast<int>(t - e.first);
-  bool used = e.row >= 0 && e.nodes > 0;
-  if (used && p.parents) {
-    for (int j = lane; j < e.nodes; j += 32) {
-      const int u = p.parents[e.first + j];
-      const bool odd = u < -2 || u >= j;
-      if (odd) atomicOr(p.status, kStatusBadSeq);
-      up[warp][j] = static_cast<short>(odd ? -2 : u);
+__device__ void load_role(const TreeParams& p, Plan* sh, uint64_t* full, uint64_t* empty, uint32_t ring0) {
+  const int lane = threadIdx.x & 31;
+  const int size = 1 << p.c.page_shift, box = min(size, kKeys), boxes = kKeys / box;
+  const int parts = (p.dim + 31) / 32, mine = lane / parts, part = lane - mine * parts;  // boxes * parts <= 32
+  const bool active = mine < boxes;
+  const int none = p.c.layers * p.c.pages * p.c.heads;  // a box there is filled with zeros
+  uint32_t ring = 0;
+  bool ok = true;
+  Seg g;
+  for (uint32_t k = 0; ok && (ok = __all_sync(0xffffffffu, read_seg(p, sh, k, g))); ++k) {
+    __syncwarp();
+    if (lane == 0) free_seg(sh, k);
+    const int* const table = g.row < 0 ? nullptr : p.c.table + static_cast<long long>(g.row) * p.c.max_pages;
+    for (int j = g.t0; ok && j < g.t1; ++j) {
+      const int pos = j * kKeys + mine * box, slot = pos & (size - 1);
+      int at = none;
+      if (active && table && pos < g.total) {
+        const int page = table[pos >> p.c.page_shift];
+        if (page >= 0 && page < p.c.pages) at = (p.layer * p.c.pages + page) * p.c.heads + g.head;
+        else atomicOr(p.status, kStatusBadSeq);
+      }
+      for (int v = 0; v < 2; ++v, ++ring) {
+        const uint32_t stage = ring % kStages;
+        ok = __all_sync(0xffffffffu, wait(p, sh, &empty[stage], ((ring / kStages) & 1u) ^ 1u));
+        if (!ok) break;
+        const uint32_t bar = smem_u32(&full[stage]);
+        if (lane == 0) mbar_arrive_expect_tx(bar, parts * kPiece);
+        __syncwarp();
+        if (active)
+          tma_load_3d(ring0 + stage * kTile + part * kPiece + mine * box * 128u, v ? &p.map_v : &p.map_k, bar, part * 32, slot, at);
+      }
     }
-    if (lane < kTreeMaxNodes / 32) see[warp][lane] = 0u;
-    __syncwarp();
-    if (lane == 0)
-      for (int j = node; j >= 0 && up[warp][j] >= -1; j = up[warp][j]) see[warp][j >> 5] |= 1u << (j & 31);
-    used = up[warp][node] >= -1;
-    __syncwarp();
   }
-  for (int x = lane; x < nh * p.dim; x += 32) {
-    const int h = x / p.dim, d = x - h * p.dim;
-    const float f = static_cast<float>(static_cast<const E*>(p.q)[t * p.q_ld + static_cast<long long>(h0 + h) * p.dim + d]);
-    qs[warp][h][d] = p.negate ? -f : f;
-  }
+  if (lane == 0)  // what was asked for lands before the shared memory goes away
+    for (uint32_t b = ring > kStages ? ring - kStages : 0; b < ring; ++b)
+      mbar_wait_drain(smem_u32(&full[b % kStages]), (b / kStages) & 1u, kDrainNs, p.status);
   __syncwarp();
-  float m[kHeads], l[kHeads], o[kHeads][4];
-#pragma unroll
-  for (int h = 0; h < kHeads; ++h) {
-    m[h] = -INFINITY;
-    l[h] = 0.f;
-    o[h][0] = o[h][1] = o[h][2] = o[h][3] = 0.f;
-  }
-  const int total = used ? e.len + node + 1 : 0;
-  const int each = (total + 32 * p.splits - 1) / (32 * p.splits) * 32;
-  const int k0 = static_cast<int>(min(static_cast<long long>(split) * each, static_cast<long long>(total)));
-  const int k1 = static_cast<int>(min(static_cast<long long>(k0) + each, static_cast<long long>(total)));
-  const int mask = (1 << p.c.page_shift) - 1;
-  const E* const K = reinterpret_cast<const E*>(p.c.k);
-  const E* const V = reinterpret_cast<const E*>(p.c.v);
-  const int width = 16 / static_cast<int>(sizeof(E));  // values of a piece
-  for (int b = k0; b < k1; b += 32) {
-    const int pos = b + lane;
-    bool seen = pos < k1;
-    if (seen && pos >= e.len && p.parents) seen = see[warp][(pos - e.len) >> 5] >> ((pos - e.len) & 31) & 1u;
-    long long at = -1;
-    if (seen) {
-      const int page = p.c.table[static_cast<long long>(e.row) * p.c.max_pages + (pos >> p.c.page_shift)];
-      if (page >= 0 && page < p.c.pages) at = cache_at(p.c, p.layer, page, kvh, pos & mask) * width;
-      else atomicOr(p.status, kStatusBadSeq);  // its keys and values count as 0
+}
+
+template <int RW>
+__device__ void row_role(const TreeParams& p, Shared<RW>& s) {
+  constexpr int RL = RW / 4, kCols = 4;           // a lane's rows (lr + 4 i), and its columns, four times four
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, lr = lane >> 3, lk = lane & 7;
+  const int key = warp * 8 + lk, units = p.dim / 4;
+  uint32_t ring = 0;
+  long long had_first = -1;                       // whose paths are in shared memory
+  int had_row = -1, had_r0 = -1;
+  Seg g;
+  for (uint32_t k = 0;; ++k) {
+    // All warps go on or leave together: the barriers below need all of them.  This one also says that all have
+    // read what the last segment left in shared memory.
+    if (!named_bar_and(1, kWarps * 32, read_seg(p, &s.tail, k, g))) break;
+    if (lane == 0) free_seg(&s.tail, k);
+    for (int x = tid; x < RW * units; x += kWarps * 32) {
+      const int row = x / units, c = x - row * units, r = g.r0 + row, node = r / p.group;
+      float4 q = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (row < g.nrows)
+        q = *reinterpret_cast<const float4*>(static_cast<const float*>(p.q) + (g.first + node) * p.q_ld +
+                                             static_cast<long long>(g.head * p.group + r - node * p.group) * p.dim + c * 4);
+      if (p.negate) q = make_float4(-q.x, -q.y, -q.z, -q.w);
+      *reinterpret_cast<float4*>(&s.q[row][c * 4]) = q;
     }
-    float s[kHeads] = {0.f, 0.f, 0.f, 0.f};
-    if (at >= 0)
-      for (int d = 0; d < p.dim; d += 4) {
-        float f[4];
-        load4(K + at + d, f);
+    if (g.first != had_first || g.row != had_row || g.r0 != had_r0) {  // other heads of the same rows see the same
+      had_first = g.first;
+      had_row = g.row;
+      had_r0 = g.r0;
+      if (p.parents) {
+        for (int j = tid; j < (g.row < 0 ? 0 : g.nodes); j += kWarps * 32) {
+          const int u = p.parents[g.first + j];
+          const bool odd = u < -2 || u >= j;
+          if (odd) atomicOr(p.status, kStatusBadSeq);
+          s.up[j] = static_cast<short>(odd ? -2 : u);
+        }
+        named_bar_sync(1, kWarps * 32);
+      }
+      if (tid < RW) {
+        const int node = (g.r0 + tid) / p.group;
+        bool used = g.row >= 0 && tid < g.nrows;
+        s.upto[tid] = g.len + node + 1;
+        if (p.parents) {
+          used = used && s.up[node] >= -1;
+          int j = used ? node : -1;
+          for (int i = kTreeMaxNodes / 32 - 1; i >= 0; --i) {  // parents come before their children
+            unsigned on = 0u;
+            while (j >= 32 * i) {
+              const int above = s.up[j];
+              if (above >= -1) on |= 1u << (j & 31);
+              j = above;
+            }
+            s.path[tid][i] = on;
+          }
+        }
+        s.used[tid] = used;
+      }
+    }
+    named_bar_sync(1, kWarps * 32);
+    float m[RL], l[RL];
+    float4 o[RL][kCols];
 #pragma unroll
-        for (int h = 0; h < kHeads; ++h) {
-          const float4 q = *reinterpret_cast<const float4*>(&qs[warp][h][d]);
-          s[h] = fmaf(f[3], q.w, fmaf(f[2], q.z, fmaf(f[1], q.y, fmaf(f[0], q.x, s[h]))));
+    for (int i = 0; i < RL; ++i) {
+      m[i] = -INFINITY;
+      l[i] = 0.f;
+#pragma unroll
+      for (int c = 0; c < kCols; ++c) o[i][c] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    for (int t = g.t0; t < g.t1; ++t, ring += 2) {
+      const int pos = t * kKeys + key;
+      const bool masked = (t + 1) * kKeys > g.all;
+      uint32_t stage = ring % kStages;
+      wait(p, &s.tail, &s.tail.full[stage], (ring / kStages) & 1u);
+      float2 z2[RL][2];
+#pragma unroll
+      for (int i = 0; i < RL; ++i) z2[i][0] = z2[i][1] = make_float2(0.f, 0.f);
+      for (int x = 0; x < units; x += 8) {
+        const uint8_t* const at = s.ring[stage] + (x >> 3) * kPiece + key * 128;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          if (x + c >= units) break;
+          const float4 f = *reinterpret_cast<const float4*>(at + ((c ^ lk) << 4));
+#pragma unroll
+          for (int i = 0; i < RL; ++i) {
+            const float4 q = *reinterpret_cast<const float4*>(&s.q[lr + 4 * i][(x + c) * 4]);
+            z2[i][0] = fma2(make_float2(f.x, f.y), make_float2(q.x, q.y), z2[i][0]);
+            z2[i][1] = fma2(make_float2(f.z, f.w), make_float2(q.z, q.w), z2[i][1]);
+          }
         }
       }
-    float w[kHeads];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&s.tail.empty[stage]));
+      float w[RL];
+      unsigned seen = 0xffffffffu;                // a bit a row of this lane's
 #pragma unroll
-    for (int h = 0; h < kHeads; ++h) {
-      const float z = seen ? s[h] : -INFINITY;
-      float top = z;
+      for (int i = 0; i < RL; ++i) {
+        float z = (z2[i][0].x + z2[i][0].y) + (z2[i][1].x + z2[i][1].y);
+        if (masked) {
+          const int row = lr + 4 * i, j = pos - g.len;
+          bool on = s.used[row] && pos < g.total;
+          if (on && j >= 0) on = p.parents ? s.path[row][j >> 5] >> (j & 31) & 1u : pos < s.upto[row];
+          if (!on) {
+            z = -INFINITY;
+            seen &= ~(1u << i);
+          }
+        }
+        float top = z;
 #pragma unroll
-      for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-      const float now = fmaxf(m[h], top);
-      const float base = now == -INFINITY ? 0.f : now * p.scale;
-      const float c = exp2f(fmaf(m[h], p.scale, -base));
-      w[h] = seen ? exp2f(fmaf(z, p.scale, -base)) : 0.f;
-      l[h] = fmaf(l[h], m[h] == -INFINITY ? 0.f : c, warp_sum(w[h]));
+        for (int x = 1; x < 8; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+        const float now = fmaxf(m[i], top), base = tree_base(p, now);
+        if (__any_sync(0xffffffffu, now > m[i])) {
+          const float c = m[i] == -INFINITY ? 0.f : exp2f(tree_base(p, m[i]) - base);
+          l[i] *= c;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) o[h][j] *= m[h] == -INFINITY ? 0.f : c;
-      m[h] = now;
+          for (int y = 0; y < kCols; ++y) o[i][y] = make_float4(o[i][y].x * c, o[i][y].y * c, o[i][y].z * c, o[i][y].w * c);
+          m[i] = now;
+        }
+        w[i] = seen >> i & 1u ? exp2f(fmaf(z, p.scale, -base)) : 0.f;
+        l[i] += w[i];
+      }
+      stage = (ring + 1) % kStages;
+      wait(p, &s.tail, &s.tail.full[stage], ((ring + 1) / kStages) & 1u);
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk) {
+        const int from = (lane & 24) | kk;
+        float wk[RL];
+#pragma unroll
+        for (int i = 0; i < RL; ++i) wk[i] = __shfl_sync(0xffffffffu, w[i], from);
+        const unsigned on = masked ? __shfl_sync(0xffffffffu, seen, from) : 0xffffffffu;
+        const uint8_t* const at = s.ring[stage] + (warp * 8 + kk) * 128 + ((lk ^ kk) << 4);
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) {
+          if (32 * c >= p.dim) break;
+          const float4 f = *reinterpret_cast<const float4*>(at + c * kPiece);
+#pragma unroll
+          for (int i = 0; i < RL; ++i)
+            if (on >> i & 1u) {                   // what a row does not see may be anything
+              const float2 w2 = make_float2(wk[i], wk[i]);
+              const float2 lo = fma2(make_float2(f.x, f.y), w2, make_float2(o[i][c].x, o[i][c].y));
+              const float2 hi = fma2(make_float2(f.z, f.w), w2, make_float2(o[i][c].z, o[i][c].w));
+              o[i][c] = make_float4(lo.x, lo.y, hi.x, hi.y);
+            }
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&s.tail.empty[stage]));
     }
-    unsigned live = __ballot_sync(0xffffffffu, at >= 0);
-    while (live) {
-      const int k = __ffs(live) - 1;
-      live &= live - 1u;
-      const long long va = __shfl_sync(0xffffffffu, at, k);
-      float f[4] = {0.f, 0.f, 0.f, 0.f};
-      if (lane * 4 < p.dim) load4(V + va + lane * 4, f);
+    // The warps' parts of the keys meet.
 #pragma unroll
-      for (int h = 0; h < kHeads; ++h) {
-        const float wk = __shfl_sync(0xffffffffu, w[h], k);
+    for (int i = 0; i < RL; ++i) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) o[h][j] = fmaf(wk, f[j], o[h][j]);
+      for (int x = 1; x < 8; x <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
+      if (lk == 0) s.ml[warp][lr + 4 * i] = make_float2(m[i], l[i]);
+#pragma unroll
+      for (int c = 0; c < kCols; ++c) *reinterpret_cast<float4*>(&s.o[warp][lr + 4 * i][32 * c + 4 * lk]) = o[i][c];
+    }
+    named_bar_sync(1, kWarps * 32);
+    const bool whole = g.t0 == 0 && g.t1 == g.nt;
+    for (int x = tid; x < g.nrows * units; x += kWarps * 32) {
+      // Lanes side by side: a row's columns, or of pieces a column's rows, as each lies in memory.
+      const int row = whole ? x / units : x % g.nrows, c = whole ? x - row * units : x / g.nrows;
+      float M = -INFINITY, sum = 0.f;
+      float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) M = fmaxf(M, s.ml[w][row].x);
+      const float base = tree_base(p, M);
+      for (int w = 0; w < kWarps; ++w) {
+        const float2 ml = s.ml[w][row];
+        if (ml.y == 0.f) continue;                // nothing seen
+        const float f = ml.x == -INFINITY ? 1.f : exp2f(tree_base(p, ml.x) - base);  // a sum without a maximum is NaN
+        const float4 b = *reinterpret_cast<const float4*>(&s.o[w][row][c * 4]);
+        sum = fmaf(ml.y, f, sum);
+        a = make_float4(fmaf(b.x, f, a.x), fmaf(b.y, f, a.y), fmaf(b.z, f, a.z), fmaf(b.w, f, a.w));
+      }
+      if (!s.used[row]) {
+        sum = 0.f;
+        a = make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+      if (whole) {
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        const long long to = tree_out_row(p, g.first, g.head, g.r0 + row);
+        *reinterpret_cast<float4*>(static_cast<float*>(p.out) + to * p.dim + c * 4) =
+            make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv);
+        if (c == 0) p.lse[to] = tree_lse(p, M, sum);
+      } else {
+        float* const part = tree_part(p, blockIdx.x, g.slot);
+        reinterpret_cast<float4*>(part)[static_cast<long long>(c + 1) * p.part_rows + row] = a;
+        if (c == 0) reinterpret_cast<float2*>(part)[row] = make_float2(M, sum);
       }
     }
   }
-  for (int h = 0; h < nh; ++h) {
-    const long long row = t * p.q_heads + h0 + h;
-    if (p.splits > 1) {
-      float* const part = p.part + (row * p.splits + split) * (p.dim + 4);
-      if (lane * 4 < p.dim) store4(part + 4 + lane * 4, o[h]);
-      if (lane == 0) part[0] = m[h], part[1] = l[h];
-      continue;
-    }
-    const float inv = l[h] == 0.f ? 0.f : 1.f / l[h];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) o[h][j] *= inv;
-    if (lane * 4 < p.dim) store4(static_cast<E*>(p.out) + row * p.dim + lane * 4, o[h]);
-    if (lane == 0) p.lse[row] = l[h] == 0.f ? -INFINITY : fmaf(m[h], p.scale, log2f(l[h])) * kLn2;
-  }
 }
 
-// Joins the pieces of a node's keys, in order.  A warp a node and head.
-template <typename E>
-__global__ void __launch_bounds__(32 * kWarps) join_kernel(TreeParams p) {
+template <int RW>
+__global__ void __launch_bounds__(kThreads, 1) tree_fp32_kernel(const __grid_constant__ TreeParams p) {
+  extern __shared__ __align__(1024) uint8_t smem[];
+  Shared<RW>& s = *reinterpret_cast<Shared<RW>*>(smem);
+  const int warp = threadIdx.x >> 5;
+  if (threadIdx.x == 0) {
+    plan_init(&s.tail, 1 + kWarps);
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(smem_u32(&s.tail.full[i]), 1);
+      mbar_init(smem_u32(&s.tail.empty[i]), kWarps);
+    }
+    fence_barrier_init();
+  }
+  const Range range = plan_cut<kThreads>(p, &s.tail);  // has barriers
+  chain_trigger();  // every CTA of this launch is resident: the next kernel's cannot take their place
+  if (warp < kWarps) row_role<RW>(p, s);
+  else if (warp == kWarps) load_role(p, &s.tail, s.tail.full, s.tail.empty, smem_u32(s.ring));
+  else if ((threadIdx.x & 31) == 0) plan_role(p, &s.tail, range);
+  __syncwarp();
+  __syncthreads();
+}
+
+// Joins the pieces of the items that lie in several CTAs' ranges, in order: blocks x have those of the item that
+// CTA x began.  A thread has 16 values of a row; where there are many pieces, several threads share them.
+// (Where a block of 32 threads' work each looked for the item itself, 16 trees of 64 nodes took 178 us instead of 130.)
+constexpr int kJoinThreads = 256, kJoinParts = 8, kJoinWide = 4;  // pieces of four values a thread
+__device__ __forceinline__ uint32_t pack(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <bool kBf16>
+__global__ void __launch_bounds__(kJoinThreads) tree_join_kernel(const __grid_constant__ TreeParams p) {
+  __shared__ float s_top[kJoinThreads], s_sum[kJoinThreads];
+  __shared__ float4 s_o[kJoinWide][kJoinThreads];
   chain_wait();
-  const int lane = threadIdx.x & 31;
-  const long long row = static_cast<long long>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
-  if (row >= p.N * p.q_heads || row / p.q_heads >= p.start[p.n] || row / p.q_heads < p.start[0]) return;
-  const int stride = p.dim + 4;
-  const float* const part = p.part + row * p.splits * stride;
-  float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int s = lane; s < p.splits; s += 32) m = fmaxf(m, part[s * stride]);
+  const TreeJoin it = p.joins[blockIdx.x];
+  const int units = p.dim / 4, all = it.rows * ((units + kJoinWide - 1) / kJoinWide), stride = p.part_rows;
+  const int shift = it.pieces <= 4 ? 0 : it.pieces <= 8 ? 1 : it.pieces <= 16 ? 2 : 3;  // 2^shift threads share
+  const int width = kJoinThreads >> shift, mine = threadIdx.x / width, own = threadIdx.x % width, step = 1 << shift;
+  auto piece = [&](int c) { return tree_part(p, blockIdx.x + c, c == 0 ? it.slot : 0); };  // the first item of those behind
+  for (int i0 = blockIdx.y * width; i0 < all; i0 += width * gridDim.y) {
+    const int i = min(i0 + own, all - 1), x = i / it.rows * kJoinWide, r = i % it.rows;  // lanes side by side: rows that are
+    float m = -INFINITY, l = 0.f;
+    float4 o[kJoinWide];
 #pragma unroll
-  for (int x = 16; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-  const float base = m == -INFINITY ? 0.f : m * p.scale;
-  for (int s = 0; s < p.splits; ++s) {
-    const float* const x = part + s * stride;
-    if (x[1] == 0.f) continue;  // nothing seen
-    const float c = x[0] == -INFINITY ? 1.f : exp2f(fmaf(x[0], p.scale, -base));  // a sum without a maximum is NaN
-    l = fmaf(x[1], c, l);
-    if (lane * 4 < p.dim) {
-      float f[4];
-      load4(x + 4 + lane * 4, f);
+    for (int y = 0; y < kJoinWide; ++y) o[y] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int c = mine; c < it.pieces; c += 4 * step) {
+      float top[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) o[j] = fmaf(f[j], c, o[j]);
+      for (int y = 0; y < 4; ++y) top[y] = c + y * step < it.pieces ? piece(c + y * step)[2 * r] : -INFINITY;
+#pragma unroll
+      for (int y = 0; y < 4; ++y) m = fmaxf(m, top[y]);
+    }
+    if (shift) {
+      s_top[threadIdx.x] = m;
+      __syncthreads();
+      for (int w = 0; w < step; ++w) m = fmaxf(m, s_top[w * width + own]);
+    }
+    const float base = tree_base(p, m);
+    for (int c = mine; c < it.pieces; c += 2 * step) {
+      float2 ml[2];
+      float4 f[2][kJoinWide];
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        const bool in = c + z * step < it.pieces;
+        const float* const at = piece(in ? c + z * step : c);
+        ml[z] = in ? *reinterpret_cast<const float2*>(at + 2 * r) : make_float2(-INFINITY, 0.f);
+#pragma unroll
+        for (int y = 0; y < kJoinWide; ++y)
+          if (x + y < units) f[z][y] = *reinterpret_cast<const float4*>(at + (static_cast<long long>(x + y + 1) * stride + r) * 4);
+      }
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        if (ml[z].y == 0.f) continue;
+        const float k = ml[z].x == -INFINITY ? 1.f : exp2f(tree_base(p, ml[z].x) - base);  // a sum without a maximum is NaN
+        l = fmaf(ml[z].y, k, l);
+#pragma unroll
+        for (int y = 0; y < kJoinWide; ++y)
+          o[y] = make_float4(fmaf(f[z][y].x, k, o[y].x), fmaf(f[z][y].y, k, o[y].y), fmaf(f[z][y].z, k, o[y].z),
+                             fmaf(f[z][y].w, k, o[y].w));
+      }
+    }
+    if (shift) {
+      s_sum[threadIdx.x] = l;
+#pragma unroll
+      for (int y = 0; y < kJoinWide; ++y) s_o[y][threadIdx.x] = o[y];
+      __syncthreads();
+      if (mine == 0)
+        for (int w = 1; w < step; ++w) {
+          l += s_sum[w * width + own];
+#pragma unroll
+          for (int y = 0; y < kJoinWide; ++y) {
+            const float4 f = s_o[y][w * width + own];
+            o[y] = make_float4(o[y].x + f.x, o[y].y + f.y, o[y].z + f.z, o[y].w + f.w);
+          }
+        }
+    }
+    if (mine == 0 && i0 + own < all) {
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const long long row = tree_out_row(p, it.first, it.head, it.r0 + r), to = row * p.dim + x * 4;
+#pragma unroll
+      for (int y = 0; y < kJoinWide; ++y) o[y] = make_float4(o[y].x * inv, o[y].y * inv, o[y].z * inv, o[y].w * inv);
+      if (kBf16) {
+#pragma unroll
+        for (int y = 0; y < kJoinWide; y += 2)  // values come in eights
+          if (x + y < units)
+            st16(static_cast<__nv_bfloat16*>(p.out) + to + 4 * y,
+                 make_uint4(pack(o[y].x, o[y].y), pack(o[y].z, o[y].w), pack(o[y + 1].x, o[y + 1].y), pack(o[y + 1].z, o[y + 1].w)));
+      } else {
+#pragma unroll
+        for (int y = 0; y < kJoinWide; ++y)
+          if (x + y < units) *reinterpret_cast<float4*>(static_cast<float*>(p.out) + to + 4 * y) = o[y];
+      }
+      if (x == 0) p.lse[row] = tree_lse(p, m, l);
     }
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) o[j] *= inv;
-  if (lane * 4 < p.dim) store4(static_cast<E*>(p.out) + row * p.dim + lane * 4, o);
-  if (lane == 0) p.lse[row] = l == 0.f ? -INFINITY : fmaf(m, p.scale, log2f(l)) * kLn2;
-}
-
-template <typename E>
-cudaError_t run_nodes(const TreeParams& p, cudaStream_t s) {
-  const long long tasks = p.N * p.c.heads * ((p.group + kHeads - 1) / kHeads) * p.splits;
-  node_kernel<E><<<static_cast<unsigned>((tasks + kWarps - 1) / kWarps), 32 * kWarps, 0, s>>>(p);
-  const cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess || p.splits == 1) return e;
-  return launch_chained(join_kernel<E>, dim3(static_cast<unsigned>((p.N * p.q_heads + kWarps - 1) / kWarps)),
-                        dim3(32 * kWarps), 0, s, p);
 }
 
 }  // namespace
 
-// Pieces of the keys: as many warps as the card holds sixteen an SM of, where the nodes are few.
-int tree_fp32_splits(long long N, int q_heads, int sms) {
-  const long long rows = N * ((q_heads + kHeads - 1) / kHeads);
-  const long long want = rows > 0 ? (16LL * sms) / rows : 1;
-  return static_cast<int>(want < 1 ? 1 : want > 64 ? 64 : want);
+cudaError_t launch_tree_join(const TreeParams& p, cudaStream_t s) {
+  const int parts = (p.part_rows * ((p.dim + 4 * kJoinWide - 1) / (4 * kJoinWide)) + kJoinThreads - 1) / kJoinThreads;
+  return launch_chained(p.bf16 ? tree_join_kernel<true> : tree_join_kernel<false>,
+                        dim3(p.sms - 1, parts < kJoinParts ? parts : kJoinParts), dim3(kJoinThreads), 0, s, p);
 }
 
-cudaError_t launch_tree_fp32(const TreeParams& p, cudaStream_t s) { return run_nodes<float>(p, s); }
+cudaError_t launch_tree_fp32(const TreeParams& p, cudaStream_t s) {
+  if (p.item_rows == 4) tree_fp32_kernel<4><<<p.sms, kThreads, sizeof(Shared<4>), s>>>(p);
+  else tree_fp32_kernel<16><<<p.sms, kThreads, sizeof(Shared<16>), s>>>(p);
+  const cudaError_t e = cudaGetLastError();
+  return e != cudaSuccess ? e : launch_tree_join(p, s);
+}
+
+void tree_sizes(TreeParams* p) {
+  if (p->bf16) {
+    p->tile_rows = tree_tile_rows(p->group);
+    p->q_rows = tree_query_rows(p->group);
+    p->item_rows = 2 * p->tile_rows;
+    p->key_shift = 7;
+    // (1, 3, 5, 8 and 12: 32 trees 90, 70, 71, 71 and 73 us, prompts 403, 369, 370, 376 and 383.)
+    p->over = 4;
+  } else {
+    // Rows of an entry on average: where they are few, less is computed for nobody.
+    p->item_rows = p->N * p->group <= 4LL * p->n ? 4 : 16;
+    p->key_shift = 6;
+    p->over = p->item_rows == 4 ? 6 : 2;
+  }
+  p->part_rows = static_cast<int>(p->N * p->group < p->item_rows ? p->N * p->group : p->item_rows);
+}
+
+cudaError_t setup_tree_kernels() {
+  static_assert(sizeof(Shared<16>) <= 227 * 1024, "shared memory");
+  cudaError_t e = cudaFuncSetAttribute(tree_fp32_kernel<4>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Shared<4>));
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(tree_fp32_kernel<16>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Shared<16>));
+  return e == cudaSuccess ? setup_tree_mma_kernels() : e;
+}
 
 }  // namespace mls

@@ -1,4 +1,11 @@
-// What the tree-attention kernels share: the entries of a call.
+// What the tree-attention kernels share: the entries of a call, and how its work is cut into equal ranges.
+//
+// Items are (entry, item_rows of its rows, key/value head); the rows of an entry are its nodes times the query
+// heads of one key/value head (node-major).  Lengths are known on the device only, so CTAs cut the work there: the
+// key tiles of all items, and `over` units more for each item's beginning and end, are numbered, and CTA c of G takes
+// the c-th of G equal ranges, which may begin and end inside an item.  Pieces of an item that lies in several
+// ranges go to the workspace, and a second kernel joins them, as the first of the CTAs wrote it down.  Work is
+// even over the card whatever the lengths are, and a captured graph follows them.
 #pragma once
 
 #include "mls_device.cuh"
@@ -7,6 +14,13 @@
 namespace mls {
 
 constexpr float kLn2 = 0.6931471805599453f;
+
+// Weights are 2^(scale z - base) with base = scale m rounded, m a maximum: what they are brought to, and what lse
+// adds, is that same number.
+__device__ __forceinline__ float tree_base(const TreeParams& p, float m) { return m == -INFINITY ? 0.f : __fmul_rn(m, p.scale); }
+__device__ __forceinline__ float tree_lse(const TreeParams& p, float m, float sum) {
+  return sum == 0.f ? -INFINITY : (tree_base(p, m) + log2f(sum)) * kLn2;
+}
 
 // What an entry of a call is: its nodes [first, first + nodes) of the packed ones, its row of the
 // table and the tokens cached there.  What does not fit the cache is an entry of unused nodes.
@@ -37,6 +51,198 @@ __device__ __forceinline__ Entry tree_entry(const TreeParams& p, int i, int* sta
   }
   if (bad) atomicOr(status, kStatusBadSeq);
   return e;
+}
+
+// A run of items of an entry that have as many key tiles each: those of rows r0, r0 + item_rows, ...
+struct Run {
+  int r0, rows, count, total, nt;                 // rows and keys of the first
+};
+__device__ __forceinline__ Run tree_run(const TreeParams& p, const Entry& en, int r0) {
+  Run u;
+  const int all = en.nodes * p.group;
+  u.r0 = r0;
+  u.rows = min(all - r0, p.item_rows);
+  u.total = en.len + (r0 + u.rows - 1) / p.group + 1;
+  u.nt = ((u.total - 1) >> p.key_shift) + 1;
+  // An item of nt tiles has its last row below `most`.
+  const long long most = ((static_cast<long long>(u.nt) << p.key_shift) - en.len) * p.group;
+  u.count = most >= all ? (all - r0 + p.item_rows - 1) / p.item_rows : static_cast<int>(most - r0) / p.item_rows;
+  return u;
+}
+__device__ inline long long entry_units(const TreeParams& p, const Entry& en) {
+  long long sum = 0;
+  for (int r0 = 0; r0 < en.nodes * p.group;) {
+    const Run u = tree_run(p, en, r0);
+    sum += static_cast<long long>(u.count) * (p.over + u.nt);
+    r0 += u.count * p.item_rows;
+  }
+  return sum * p.c.heads;
+}
+
+// A piece of an item, for every role: rows [r0, r0 + nrows) of an entry and head, key tiles [t0, t1) of nt.
+struct Seg {
+  long long first;                                // of the entry's nodes
+  int nodes, row, len;                            // its nodes, row of the table (-1: none takes part) and cached tokens
+  int head, r0, nrows, t0, t1, nt;                // t0 = t1: the end
+  int total;                                      // keys of the item: cached tokens and nodes up to its last
+  int all;                                        // keys that every row sees
+  int slot;                                       // of the CTA's two in the workspace
+};
+constexpr int kSegs = 4;
+// In shared memory.
+struct Plan {
+  uint64_t seg_full[kSegs], seg_empty[kSegs];
+  Seg seg[kSegs];
+  Entry en0;                                      // the range's first entry, its number and first unit
+  long long scan[32], base0;
+  int e0, abort;
+};
+
+__device__ __forceinline__ bool wait(const TreeParams& p, Plan* sh, uint64_t* bar, uint32_t parity) {
+  return mbar_wait(smem_u32(bar), parity, &sh->abort, p.status);
+}
+__device__ inline void plan_init(Plan* sh, int readers) {
+  sh->abort = 0;
+  for (int k = 0; k < kSegs; ++k) {
+    mbar_init(smem_u32(&sh->seg_full[k]), 1);
+    mbar_init(smem_u32(&sh->seg_empty[k]), readers);
+  }
+}
+
+// The CTA's range [lo, hi) of units, of `each` a CTA.  All threads: each adds up a run of entries.  Two barriers.
+struct Range {
+  long long lo, hi, each;
+};
+template <int kThreads>
+__device__ Range plan_cut(const TreeParams& p, Plan* sh) {
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int chunk = (p.n + kThreads - 1) / kThreads;
+  const int i0 = min(tid * chunk, p.n), i1 = min(i0 + chunk, p.n);
+  long long mine = 0;
+  for (int i = i0; i < i1; ++i) mine += entry_units(p, tree_entry(p, i, p.status));
+  long long upto = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long v = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += v;
+  }
+  if (lane == 31) sh->scan[warp] = upto;
+  __syncthreads();
+  long long before = upto - mine, units = 0;
+  for (int x = 0; x < kThreads / 32; ++x) {
+    if (x < warp) before += sh->scan[x];
+    units += sh->scan[x];
+  }
+  Range r;
+  r.each = (units + gridDim.x - 1) / gridDim.x;
+  r.lo = min(blockIdx.x * r.each, units);
+  r.hi = min(r.lo + r.each, units);
+  if (r.lo < r.hi && before <= r.lo && r.lo < before + mine) {
+    long long at = before;
+    for (int i = i0; i < i1; ++i) {
+      const Entry en = tree_entry(p, i, p.status);
+      const long long u = entry_units(p, en);
+      if (at <= r.lo && r.lo < at + u) {
+        sh->en0 = en;
+        sh->e0 = i;
+        sh->base0 = at;
+      }
+      at += u;
+    }
+  }
+  __syncthreads();
+  return r;
+}
+
+// One thread: writes down the segments of the range, and what begins there and goes on in other CTAs'.
+__device__ inline void plan_role(const TreeParams& p, Plan* sh, const Range& range) {
+  uint32_t k = 0;
+  bool first = true;
+  TreeJoin join = {};
+  auto slot = [&]() -> Seg* {
+    return wait(p, sh, &sh->seg_empty[k % kSegs], ((k / kSegs) & 1u) ^ 1u) ? &sh->seg[k % kSegs] : nullptr;
+  };
+  long long at = range.lo;
+  if (at < range.hi) {
+    Entry en = sh->en0;
+    int e = sh->e0;
+    long long v = at - sh->base0;                 // units into the run
+    Run u = {};
+    bool some = en.nodes > 0;
+    if (some) u = tree_run(p, en, 0);
+    while (at < range.hi) {
+      while (!some || v >= static_cast<long long>(u.count) * (u.nt + p.over) * p.c.heads) {
+        int r0 = 0;
+        if (some) {
+          v -= static_cast<long long>(u.count) * (u.nt + p.over) * p.c.heads;
+          r0 = u.r0 + u.count * p.item_rows;
+        }
+        if (!some || r0 >= en.nodes * p.group) {
+          en = tree_entry(p, ++e, p.status);
+          some = en.nodes > 0;
+          r0 = 0;
+        }
+        if (some) u = tree_run(p, en, r0);
+      }
+      // The item, and where in it: its rows come after those of all heads before.
+      const int size = u.nt + p.over;
+      const long long item = v / size;
+      const int in = static_cast<int>(v - item * size);
+      const int head = static_cast<int>(item % p.c.heads), r0 = u.r0 + static_cast<int>(item / p.c.heads) * p.item_rows;
+      const int end = static_cast<int>(min(static_cast<long long>(size), in + (range.hi - at)));
+      at += end - in;
+      v += end - in;
+      const int t0 = max(in - p.over, 0), t1 = end - p.over;
+      if (t1 <= t0) continue;                     // the range ends before the item's first tile
+      Seg* const g = slot();
+      if (!g) break;
+      g->first = en.first;
+      g->nodes = en.nodes;
+      g->row = en.row;
+      g->len = en.len;
+      g->head = head;
+      g->r0 = r0;
+      g->nrows = min(en.nodes * p.group - r0, p.item_rows);
+      g->t0 = t0;
+      g->t1 = t1;
+      g->nt = u.nt;
+      g->total = en.len + (r0 + g->nrows - 1) / p.group + 1;
+      g->all = en.row < 0 ? 0 : p.parents ? en.len : en.len + r0 / p.group + 1;
+      g->slot = first ? 0 : 1;
+      first = false;
+      if (t0 == 0 && t1 < u.nt) {                 // at = hi: the range ends after tile t1 of the item
+        join.pieces = 1 + static_cast<int>((u.nt - t1 + range.each - 1) / range.each);
+        join.slot = g->slot;
+        join.rows = g->nrows;
+        join.first = static_cast<int>(en.first);
+        join.r0 = r0;
+        join.head = head;
+      }
+      mbar_arrive(smem_u32(&sh->seg_full[k++ % kSegs]));
+    }
+  }
+  p.joins[blockIdx.x] = join;
+  if (Seg* const g = slot()) {
+    g->t0 = g->t1 = 0;
+    mbar_arrive(smem_u32(&sh->seg_full[k % kSegs]));
+  }
+}
+// The k-th segment for one of its readers (false: there is none, or a wait ran out).
+__device__ __forceinline__ bool read_seg(const TreeParams& p, Plan* sh, uint32_t k, Seg& g) {
+  if (!wait(p, sh, &sh->seg_full[k % kSegs], (k / kSegs) & 1u)) return false;
+  g = sh->seg[k % kSegs];
+  return g.t1 > g.t0;
+}
+__device__ __forceinline__ void free_seg(Plan* sh, uint32_t k) { mbar_arrive(smem_u32(&sh->seg_empty[k % kSegs])); }
+
+// A piece's rows in the workspace: float2 [part_rows] of maximum and sum, float4 [dim / 4][part_rows].
+__device__ __forceinline__ float* tree_part(const TreeParams& p, long long cta, int slot) {
+  return p.part + (cta * 2 + slot) * p.part_rows * (p.dim + 4);
+}
+// Where an item's row goes in out [N * q_heads] and lse.
+__device__ __forceinline__ int tree_out_row(const TreeParams& p, long long first, int head, int r) {
+  const int node = r / p.group;
+  return (static_cast<int>(first) + node) * p.q_heads + head * p.group + (r - node * p.group);
 }
 
 }  // namespace mls

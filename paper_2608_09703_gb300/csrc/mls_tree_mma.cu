@@ -7,18 +7,13 @@
 // work for one while the other takes its exponentials.  With more than 128 rows the streams have a row
 // tile each and share the keys; with fewer they have the same rows, and every other key tile: what they
 // hold is joined at the end, each warp reading the other stream's O in its own lanes.
-//
-// Lengths are known on the device only, so CTAs cut the work there: all key tiles of all items (entry, pair of
-// row tiles, key/value head) are numbered, and CTA c of G takes the c-th of G equal ranges, which may begin and
-// end inside an item.  Pieces of an item that lies in several ranges go to the workspace, and a second kernel joins
-// them.  Work is even over the card whatever the lengths are, and a captured graph follows them.
+// Items are pairs of row tiles of an entry and key/value head, cut into ranges as mls_tree.cuh has it.
 //
 // Softmax in one pass: a running maximum per row, which moves only when it grows by more than 2^8 (P stays
 // below 256, exact enough in bf16), so that O is rarely rescaled.  Only tiles past the cached tokens look at
 // masks.  Masked weights are 0, and so that 0 times what lies there is 0 too, values behind the item's last
 // node are cleared, and infinities and NaN among the nodes' values taken out of the product and added to the
 // rows that do see them.
-#include <climits>
 #include <cmath>
 
 #include "mls_device.cuh"
@@ -38,29 +33,14 @@ constexpr float kGrow = 8.f;
 constexpr int kMaxStages = 12;
 constexpr uint32_t kSmem = 227 * 1024;
 
-// A piece of an item, for every role: rows [r0, r0 + nrows) of an entry and head, key tiles [t0, t1) of nt.
-struct Seg {
-  long long first;                                // of the entry's nodes
-  int nodes, row, len;                            // its nodes, row of the table (-1: none takes part) and cached tokens
-  int head, r0, nrows, t0, t1, nt;                // t0 = t1: the end
-  int total;                                      // keys of the item: cached tokens and nodes up to its last
-  int all;                                        // keys that every row sees
-  int slot;                                       // of the CTA's two in the workspace
-};
-constexpr int kSegs = 4;
 constexpr int kSegReaders = 3 + 8;                // load, MMA and query warp, eight of softmax
 // Past the operands.  A warpgroup's `up` and `ml` share memory: parents are read before any sum is.
-struct Tail {
+struct Tail : Plan {
   uint64_t full[kMaxStages], empty[kMaxStages], q_ready[2], q_free[2], s_full[2], p_ready[2][2], o_full[2], met, drain;
-  uint64_t seg_full[kSegs], seg_empty[kSegs];
-  Seg seg[kSegs];
   union {
     short up[kTreeMaxNodes];
     float2 ml[kRows];
   } row[2];
-  long long scan[kThreads / 32], base0;
-  Entry en0;                                      // the range's first entry, its number and first unit
-  int e0, abort;
   int fix[2];                                     // by a segment's parity: the last one with values taken out
   uint32_t tmem_slot;
 };
@@ -80,101 +60,6 @@ struct Layout {
     return (row >> 3) * kAtom + (row & 7) * 128u + (c >> 3) * kPiece + ((c & 7) << 4);
   }
 };
-
-// Key tiles of rows [r0, r0 + two tiles) of an entry.
-__device__ __forceinline__ int item_total(const TreeParams& p, const Entry& en, int r0) {
-  const int rows = min(en.nodes * p.group - r0, 2 * p.tile_rows);
-  return en.len + (r0 + rows - 1) / p.group + 1;
-}
-__device__ __forceinline__ int tiles_of(int total) { return (total + kKeys - 1) / kKeys; }
-// Units of work: an item's tiles, and kOver more for its beginning and end (1, 3, 5, 8 and 12 more: 32 trees 90, 70,
-// 71, 71 and 73 us, prompts 403, 369, 370, 376 and 383).
-constexpr int kOver = 4;
-__device__ long long entry_units(const TreeParams& p, const Entry& en) {
-  long long sum = 0;
-  for (int r0 = 0; r0 < en.nodes * p.group; r0 += 2 * p.tile_rows) sum += kOver + tiles_of(item_total(p, en, r0));
-  return sum * p.c.heads;
-}
-
-__device__ __forceinline__ bool wait(const TreeParams& p, Tail* sh, uint64_t* bar, uint32_t parity) {
-  return mbar_wait(smem_u32(bar), parity, &sh->abort, p.status);
-}
-
-// One thread: writes down the segments of units [at, hi), entry e beginning at unit `base`, and what begins
-// there and goes on in other CTAs' ranges (of `each` units).
-__device__ void plan_role(const TreeParams& p, Tail* sh, long long at, long long hi, long long each, int e, long long base) {
-  uint32_t k = 0;
-  bool first = true;
-  TreeJoin join = {};
-  auto slot = [&]() -> Seg* {
-    return wait(p, sh, &sh->seg_empty[k % kSegs], ((k / kSegs) & 1u) ^ 1u) ? &sh->seg[k % kSegs] : nullptr;
-  };
-  Entry en;
-  long long units = 0;
-  if (at < hi) {
-    en = sh->en0;
-    units = entry_units(p, en);
-  }
-  while (at < hi) {
-    while (at - base >= units) {
-      base += units;
-      en = tree_entry(p, ++e, p.status);
-      units = entry_units(p, en);
-    }
-    long long v = at - base;
-    int r0 = 0, total, nt;
-    while (true) {
-      total = item_total(p, en, r0);
-      nt = tiles_of(total);
-      const long long here = static_cast<long long>(nt + kOver) * p.c.heads;
-      if (v < here) break;
-      v -= here;
-      r0 += 2 * p.tile_rows;
-    }
-    const int head = static_cast<int>(v / (nt + kOver)), in = static_cast<int>(v - static_cast<long long>(head) * (nt + kOver));
-    const int end = static_cast<int>(min(static_cast<long long>(nt + kOver), in + (hi - at)));
-    at += end - in;
-    const int t0 = max(in - kOver, 0), t1 = end - kOver;
-    if (t1 <= t0) continue;                       // the range ends before the item's first tile
-    Seg* const g = slot();
-    if (!g) break;
-    g->first = en.first;
-    g->nodes = en.nodes;
-    g->row = en.row;
-    g->len = en.len;
-    g->head = head;
-    g->r0 = r0;
-    g->nrows = min(en.nodes * p.group - r0, 2 * p.tile_rows);
-    g->t0 = t0;
-    g->t1 = t1;
-    g->nt = nt;
-    g->total = total;
-    g->all = en.row < 0 ? 0 : p.parents ? en.len : en.len + r0 / p.group + 1;
-    g->slot = first ? 0 : 1;
-    first = false;
-    if (t0 == 0 && t1 < nt) {  // at = hi: the range ends after tile t1 of the item
-      join.pieces = 1 + static_cast<int>((nt - t1 + each - 1) / each);
-      join.slot = g->slot;
-      join.rows = g->nrows;
-      join.first = static_cast<int>(en.first);
-      join.r0 = r0;
-      join.head = head;
-    }
-    mbar_arrive(smem_u32(&sh->seg_full[k++ % kSegs]));
-  }
-  p.joins[blockIdx.x] = join;
-  if (Seg* const g = slot()) {
-    g->t0 = g->t1 = 0;
-    mbar_arrive(smem_u32(&sh->seg_full[k % kSegs]));
-  }
-}
-// The k-th segment for one of its readers (false: there is none, or a wait ran out).
-__device__ __forceinline__ bool read_seg(const TreeParams& p, Tail* sh, uint32_t k, Seg& g) {
-  if (!wait(p, sh, &sh->seg_full[k % kSegs], (k / kSegs) & 1u)) return false;
-  g = sh->seg[k % kSegs];
-  return g.t1 > g.t0;
-}
-__device__ __forceinline__ void free_seg(Tail* sh, uint32_t k) { mbar_arrive(smem_u32(&sh->seg_empty[k % kSegs])); }
 
 // Where the K and V tiles of step j lie in the order in which a segment of n tiles is loaded: K0 V0 K1 V1 ...
 // for two row tiles, K0 K1 V0 K2 V1 K3 ... for two streams of key tiles, as the MMAs take them.
@@ -573,7 +458,7 @@ __device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint3
         // The maximum moves only where it must; where it does, what is summed so far is brought down.
         const bool move = (now - m) * p.scale > kGrow || (m == -INFINITY && now > m);
         if (__any_sync(0xffffffffu, move)) {
-          const float c = !move ? 1.f : m == -INFINITY ? 0.f : fast_exp2((m - now) * p.scale);
+          const float c = !move ? 1.f : m == -INFINITY ? 0.f : fast_exp2(tree_base(p, m) - tree_base(p, now));
           if (move) m = now;
           l *= c;
           if (i > 0) {
@@ -588,7 +473,7 @@ __device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint3
             }
           }
         }
-        const float off = m == -INFINITY ? 0.f : -m * p.scale;
+        const float off = -tree_base(p, m);
         const float2 scale2 = make_float2(p.scale, p.scale), off2 = make_float2(off, off);
         float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
         // The MMAs of the first half of the keys begin while the second half's exponentials are taken.
@@ -630,9 +515,9 @@ __device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint3
       meet();
       const float2 o = sh->row[1 - w].ml[tid];
       M = fmaxf(m, o.x);
-      const float off = M == -INFINITY ? 0.f : M;
-      c_own = l == 0.f ? 0.f : m == -INFINITY ? 1.f : fast_exp2((m - off) * p.scale);
-      c_other = o.y == 0.f ? 0.f : o.x == -INFINITY ? 1.f : fast_exp2((o.x - off) * p.scale);
+      const float off = tree_base(p, M);
+      c_own = l == 0.f ? 0.f : m == -INFINITY ? 1.f : fast_exp2(tree_base(p, m) - off);
+      c_other = o.y == 0.f ? 0.f : o.x == -INFINITY ? 1.f : fast_exp2(tree_base(p, o.x) - off);
       // (A sum without a maximum is NaN and stays so.)
       Lsum = (l == 0.f ? 0.f : l * c_own) + (o.y == 0.f ? 0.f : o.y * c_other);
     }
@@ -642,10 +527,10 @@ __device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint3
     const float inv = whole ? (Lsum == 0.f || !see.used ? 0.f : 1.f / Lsum) : 1.f;
     const int chunks = (p.dim + 31) / 32;
     const int x0 = pair || w == 0 ? 0 : (chunks + 1) / 2, x1 = pair || w == 1 ? chunks : (chunks + 1) / 2;
-    const int out_row = (static_cast<int>(g.first) + node) * p.q_heads + g.head * p.group + (r - node * p.group);
+    const int out_row = tree_out_row(p, g.first, g.head, inside ? r : g.r0);
     // A piece's rows lie side by side, four values each, so that the lanes' stores do.
     const int rows = p.part_rows;
-    float* const part = p.part + (static_cast<long long>(blockIdx.x) * 2 + g.slot) * rows * (p.dim + 4);
+    float* const part = tree_part(p, blockIdx.x, g.slot);
     const uint32_t other = tmem + lanes + kAccO + (1 - w) * 128;
     if (busy) {
       // For stores of 64 bytes of a row, four lanes exchange their 16 bytes of each other's rows.
@@ -717,7 +602,7 @@ __device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint3
     }
     if (inside && (pair || w == 0)) {
       const float sum = see.used ? Lsum : 0.f;
-      if (whole) p.lse[out_row] = sum == 0.f ? -INFINITY : fmaf(M, p.scale, log2f(sum)) * kLn2;
+      if (whole) p.lse[out_row] = tree_lse(p, M, sum);
       else reinterpret_cast<float2*>(part)[rl] = make_float2(M, sum);
     }
     tc_fence_before();
@@ -733,7 +618,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
   Tail* const sh = reinterpret_cast<Tail*>(smem + L::kTail);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
-    sh->abort = sh->fix[0] = sh->fix[1] = 0;
+    plan_init(sh, kSegReaders);
+    sh->fix[0] = sh->fix[1] = 0;
     for (int s = 0; s < L::kStages; ++s) {
       mbar_init(smem_u32(&sh->full[s]), 1);
       mbar_init(smem_u32(&sh->empty[s]), 1);
@@ -745,10 +631,6 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
       for (int h = 0; h < 2; ++h) mbar_init(smem_u32(&sh->p_ready[w][h]), kRows / 32);
       mbar_init(smem_u32(&sh->o_full[w]), 1);
     }
-    for (int k = 0; k < kSegs; ++k) {
-      mbar_init(smem_u32(&sh->seg_full[k]), 1);
-      mbar_init(smem_u32(&sh->seg_empty[k]), kSegReaders);
-    }
     mbar_init(smem_u32(&sh->met), 8);
     mbar_init(smem_u32(&sh->drain), 1);
     fence_barrier_init();
@@ -757,42 +639,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
     tmem_alloc(smem_u32(&sh->tmem_slot), kTmemCols);
     tmem_relinquish();
   }
-  // The work: every thread adds up a run of entries.
-  const int chunk = (p.n + kThreads - 1) / kThreads;
-  const int i0 = min(tid * chunk, p.n), i1 = min(i0 + chunk, p.n);
-  long long mine = 0;
-  for (int i = i0; i < i1; ++i) mine += entry_units(p, tree_entry(p, i, p.status));
-  long long upto = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const long long v = __shfl_up_sync(0xffffffffu, upto, o);
-    if (lane >= o) upto += v;
-  }
-  if (lane == 31) sh->scan[warp] = upto;
   tc_fence_before();
-  __syncthreads();
+  const Range range = plan_cut<kThreads>(p, sh);  // has barriers
   tc_fence_after();
   const uint32_t tmem = sh->tmem_slot;
-  long long before = upto - mine, units = 0;
-  for (int x = 0; x < kThreads / 32; ++x) {
-    if (x < warp) before += sh->scan[x];
-    units += sh->scan[x];
-  }
-  const long long each = (units + gridDim.x - 1) / gridDim.x;
-  const long long lo = min(blockIdx.x * each, units), hi = min(lo + each, units);
-  if (lo < hi && before <= lo && lo < before + mine) {
-    long long at = before;
-    for (int i = i0; i < i1; ++i) {
-      const long long u = i1 - i0 == 1 ? mine : entry_units(p, tree_entry(p, i, p.status));
-      if (at <= lo && lo < at + u) {
-        sh->en0 = tree_entry(p, i, p.status);
-        sh->e0 = i;
-        sh->base0 = at;
-      }
-      at += u;
-    }
-  }
-  __syncthreads();
   chain_trigger();  // every CTA of this launch is resident: the next kernel's cannot take their place
 
   if (warp < 4) {
@@ -802,7 +652,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
     } else if (warp == 1) {
       mma_role<DC, kJoint>(p, sh, base, tmem);
     } else if (warp == 2) {
-      if (lane == 0) plan_role(p, sh, lo, hi, each, sh->e0, sh->base0);
+      if (lane == 0) plan_role(p, sh, range);
     } else {
       query_role<DC>(p, sh, base);
     }
@@ -819,93 +669,6 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
   }
 }
 
-// Joins the pieces of the items that lie in several CTAs' ranges, in order: blocks x have those of the item that
-// CTA x began.  A thread has 16 values of a row; where there are many pieces, several threads share them.
-// (Where a block of 32 threads' work each looked for the item itself, 16 trees of 64 nodes took 178 us instead of 130.)
-constexpr int kJoinThreads = 256, kJoinParts = 8, kJoinWide = 4;  // pieces of four values a thread
-__global__ void __launch_bounds__(kJoinThreads) tree_join_kernel(const __grid_constant__ TreeParams p) {
-  __shared__ float s_top[kJoinThreads], s_sum[kJoinThreads];
-  __shared__ float4 s_o[kJoinWide][kJoinThreads];
-  chain_wait();
-  const TreeJoin it = p.joins[blockIdx.x];
-  const int units = p.dim / 4, all = it.rows * ((units + kJoinWide - 1) / kJoinWide), stride = p.part_rows;
-  const int shift = it.pieces <= 4 ? 0 : it.pieces <= 8 ? 1 : it.pieces <= 16 ? 2 : 3;  // 2^shift threads share
-  const int width = kJoinThreads >> shift, mine = threadIdx.x / width, own = threadIdx.x % width, step = 1 << shift;
-  auto piece = [&](int c) {  // in the CTAs behind the first it is the first of their items
-    return p.part + (static_cast<long long>(blockIdx.x + c) * 2 + (c == 0 ? it.slot : 0)) * stride * (p.dim + 4);
-  };
-  for (int i0 = blockIdx.y * width; i0 < all; i0 += width * gridDim.y) {
-    const int i = min(i0 + own, all - 1), x = i / it.rows * kJoinWide, r = i % it.rows;  // lanes side by side: rows that are
-    float m = -INFINITY, l = 0.f;
-    float4 o[kJoinWide];
-#pragma unroll
-    for (int y = 0; y < kJoinWide; ++y) o[y] = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int c = mine; c < it.pieces; c += 4 * step) {
-      float top[4];
-#pragma unroll
-      for (int y = 0; y < 4; ++y) top[y] = c + y * step < it.pieces ? piece(c + y * step)[2 * r] : -INFINITY;
-#pragma unroll
-      for (int y = 0; y < 4; ++y) m = fmaxf(m, top[y]);
-    }
-    if (shift) {
-      s_top[threadIdx.x] = m;
-      __syncthreads();
-      for (int w = 0; w < step; ++w) m = fmaxf(m, s_top[w * width + own]);
-    }
-    const float off = m == -INFINITY ? 0.f : m;
-    for (int c = mine; c < it.pieces; c += 2 * step) {
-      float2 ml[2];
-      float4 f[2][kJoinWide];
-#pragma unroll
-      for (int z = 0; z < 2; ++z) {
-        const bool in = c + z * step < it.pieces;
-        const float* const at = piece(in ? c + z * step : c);
-        ml[z] = in ? *reinterpret_cast<const float2*>(at + 2 * r) : make_float2(-INFINITY, 0.f);
-#pragma unroll
-        for (int y = 0; y < kJoinWide; ++y)
-          if (x + y < units) f[z][y] = *reinterpret_cast<const float4*>(at + (static_cast<long long>(x + y + 1) * stride + r) * 4);
-      }
-#pragma unroll
-      for (int z = 0; z < 2; ++z) {
-        if (ml[z].y == 0.f) continue;
-        const float k = ml[z].x == -INFINITY ? 1.f : fast_exp2((ml[z].x - off) * p.scale);  // a sum without a maximum is NaN
-        l = fmaf(ml[z].y, k, l);
-#pragma unroll
-        for (int y = 0; y < kJoinWide; ++y)
-          o[y] = make_float4(fmaf(f[z][y].x, k, o[y].x), fmaf(f[z][y].y, k, o[y].y), fmaf(f[z][y].z, k, o[y].z),
-                             fmaf(f[z][y].w, k, o[y].w));
-      }
-    }
-    if (shift) {
-      s_sum[threadIdx.x] = l;
-#pragma unroll
-      for (int y = 0; y < kJoinWide; ++y) s_o[y][threadIdx.x] = o[y];
-      __syncthreads();
-      if (mine == 0)
-        for (int w = 1; w < step; ++w) {
-          l += s_sum[w * width + own];
-#pragma unroll
-          for (int y = 0; y < kJoinWide; ++y) {
-            const float4 f = s_o[y][w * width + own];
-            o[y] = make_float4(o[y].x + f.x, o[y].y + f.y, o[y].z + f.z, o[y].w + f.w);
-          }
-        }
-    }
-    if (mine == 0 && i0 + own < all) {
-      const float inv = l == 0.f ? 0.f : 1.f / l;
-      const int node = (it.r0 + r) / p.group;
-      const long long row = static_cast<long long>(it.first + node) * p.q_heads + it.head * p.group + (it.r0 + r - node * p.group);
-      __nv_bfloat16* const out = static_cast<__nv_bfloat16*>(p.out) + row * p.dim + x * 4;
-#pragma unroll
-      for (int y = 0; y < kJoinWide; y += 2)  // values come in eights
-        if (x + y < units)
-          st16(out + 4 * y, make_uint4(pack_bf16(o[y].x * inv, o[y].y * inv), pack_bf16(o[y].z * inv, o[y].w * inv),
-                                       pack_bf16(o[y + 1].x * inv, o[y + 1].y * inv), pack_bf16(o[y + 1].z * inv, o[y + 1].w * inv)));
-      if (x == 0) p.lse[row] = l == 0.f ? -INFINITY : fmaf(m, p.scale, log2f(l)) * kLn2;
-    }
-  }
-}
-
 }  // namespace
 
 // Rows of a tile: whole nodes, as many as it holds, or any of a larger group.
@@ -915,10 +678,6 @@ int tree_tile_rows(int group) { return group <= kRows ? kRows / group * group : 
 int tree_query_rows(int group) {
   return group > kRows ? 0 : kRows % group ? kRows / group * group : group < 8 ? 8 : group;
 }
-int tree_part_rows(long long N, int group) {
-  const long long most = 2 * tree_tile_rows(group);
-  return static_cast<int>(N * group < most ? N * group : most);
-}
 
 cudaError_t launch_tree_bf16(const TreeParams& p, cudaStream_t s) {
   const int grid = p.sms;
@@ -927,11 +686,10 @@ cudaError_t launch_tree_bf16(const TreeParams& p, cudaStream_t s) {
   else tree_kernel<1, false><<<grid, kThreads, kSmem, s>>>(p);
   const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  const int parts = (p.part_rows * ((p.dim + 4 * kJoinWide - 1) / (4 * kJoinWide)) + kJoinThreads - 1) / kJoinThreads;
-  return launch_chained(tree_join_kernel, dim3(grid - 1, parts < kJoinParts ? parts : kJoinParts), dim3(kJoinThreads), 0, s, p);
+  return launch_tree_join(p, s);
 }
 
-cudaError_t setup_tree_kernels() {
+cudaError_t setup_tree_mma_kernels() {
   for (void (*kernel)(TreeParams) : {tree_kernel<1, false>, tree_kernel<2, false>, tree_kernel<2, true>}) {
     cudaFuncAttributes fa;
     cudaError_t e = cudaFuncGetAttributes(&fa, kernel);
