@@ -5,10 +5,12 @@
 // Here: the kernel of an fp32 cache, and the one that joins pieces (a bf16 cache's: mls_tree_mma.cu).
 //
 // fp32: products of full precision are the vector units' work.  An item has 16 rows (4, where entries have no more:
-// decoding) and tiles of 64 keys, of which each of eight warps has 8: a lane has a key and every fourth row of the
-// scores, then 16 columns and the same rows of the product, whose weights come by shuffles.  Warps keep a
-// maximum, sum and product of their own to the end of a segment.  K and V come by TMA, swizzled, so that eight keys'
-// same 16 bytes lie in different banks.  Arithmetic bounds long trees and prompts, HBM single tokens.
+// decoding) and tiles of 64 keys, of which each of eight warps has 8.  Half a warp has half of the rows, and a lane
+// of it 8 columns, of the queries and of the product, in registers; a key's partial scores are added up by exchanges
+// that leave each lane one row.  That asks shared memory for 8 of the 16 words a key and lane that it does for each of
+// K and V (with rows over four groups of lanes and queries in shared memory 64 single tokens over 10000 took 766 us, now
+// 534: 99% of the copy rate; 8 nodes of 16 heads over 30000 340 us, now 290).  Warps keep a maximum,
+// sum and product of their own to the end of a segment.
 #include <cmath>
 
 #include "mls_device.cuh"
@@ -19,7 +21,8 @@
 namespace mls {
 namespace {
 
-constexpr int kWarps = 8, kKeys = 64, kThreads = 32 * (kWarps + 2);
+constexpr int kWarps = 8, kKeys = 64, kThreads = 32 * (kWarps + 4);  // warps for rows; load, plan and two idle ones
+constexpr int kCtlRegs = 72, kRowRegs = 216, kLaunchRegs = 168;        // 72 + 2 x 216 = 3 x 168
 constexpr int kPieces = 4;                        // of 32 values, 128 bytes, a row
 constexpr uint32_t kPiece = kKeys * 128u, kTile = kPieces * kPiece;
 constexpr int kStages = 4;
@@ -29,7 +32,6 @@ template <int RW>
 struct Shared {
   uint8_t ring[kStages][kTile];
   float o[kWarps][RW][128];
-  float q[RW][132];                               // a row's end shifts the next one's banks
   float2 ml[kWarps][RW];
   unsigned path[RW][kTreeMaxNodes / 32];          // the nodes that a row sees, a bit each
   int used[RW], upto[RW];                         // upto: chains, keys that a row sees
@@ -42,7 +44,8 @@ struct Shared {
 __device__ void load_role(const TreeParams& p, Plan* sh, uint64_t* full, uint64_t* empty, uint32_t ring0) {
   const int lane = threadIdx.x & 31;
   const int size = 1 << p.c.page_shift, box = min(size, kKeys), boxes = kKeys / box;
-  const int parts = (p.dim + 31) / 32, mine = lane / parts, part = lane - mine * parts;  // boxes * parts <= 32
+  // Halves of a row are read as a whole: what lies behind its end is filled with zeros.  boxes * parts <= 32.
+  const int parts = p.dim > 64 ? 4 : 2, mine = lane / parts, part = lane - mine * parts;
   const bool active = mine < boxes;
   const int none = p.c.layers * p.c.pages * p.c.heads;  // a box there is filled with zeros
   uint32_t ring = 0;
@@ -78,11 +81,13 @@ __device__ void load_role(const TreeParams& p, Plan* sh, uint64_t* full, uint64_
   __syncwarp();
 }
 
-template <int RW>
+template <int RW, bool kTwo>  // kTwo: rows of more than 64 values
 __device__ void row_role(const TreeParams& p, Shared<RW>& s) {
-  constexpr int RL = RW / 4, kCols = 4;           // a lane's rows (lr + 4 i), and its columns, four times four
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, lr = lane >> 3, lk = lane & 7;
-  const int key = warp * 8 + lk, units = p.dim / 4;
+  constexpr int RL = RW / 2, kDup = 16 / RL;      // a lane's rows; lanes that are left with the same one
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, half = lane >> 4, ls = lane & 15;
+  const int own = half * RL + ls / kDup, units = p.dim / 4;
+  // A lane's columns: 4 ls and 64 + 4 ls, where there are any.
+  const bool some[2] = {ls < units, 16 + ls < units};
   uint32_t ring = 0;
   long long had_first = -1;                       // whose paths are in shared memory
   int had_row = -1, had_r0 = -1;
@@ -92,14 +97,18 @@ __device__ void row_role(const TreeParams& p, Shared<RW>& s) {
     // read what the last segment left in shared memory.
     if (!named_bar_and(1, kWarps * 32, read_seg(p, &s.tail, k, g))) break;
     if (lane == 0) free_seg(&s.tail, k);
-    for (int x = tid; x < RW * units; x += kWarps * 32) {
-      const int row = x / units, c = x - row * units, r = g.r0 + row, node = r / p.group;
-      float4 q = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (row < g.nrows)
-        q = *reinterpret_cast<const float4*>(static_cast<const float*>(p.q) + (g.first + node) * p.q_ld +
-                                             static_cast<long long>(g.head * p.group + r - node * p.group) * p.dim + c * 4);
-      if (p.negate) q = make_float4(-q.x, -q.y, -q.z, -q.w);
-      *reinterpret_cast<float4*>(&s.q[row][c * 4]) = q;
+    float4 q[RL][2];
+#pragma unroll
+    for (int i = 0; i < RL; ++i) {
+      const int row = half * RL + i, r = g.r0 + row, node = r / p.group;
+      const float* const from = static_cast<const float*>(p.q) + (g.first + node) * p.q_ld +
+                                static_cast<long long>(g.head * p.group + r - node * p.group) * p.dim + 4 * ls;
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        q[i][c] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (row < g.nrows && some[c]) q[i][c] = *reinterpret_cast<const float4*>(from + 64 * c);
+        if (p.negate) q[i][c] = make_float4(-q[i][c].x, -q[i][c].y, -q[i][c].z, -q[i][c].w);
+      }
     }
     if (g.first != had_first || g.row != had_row || g.r0 != had_r0) {  // other heads of the same rows see the same
       had_first = g.first;
@@ -133,105 +142,120 @@ __device__ void row_role(const TreeParams& p, Shared<RW>& s) {
         }
         s.used[tid] = used;
       }
+      named_bar_sync(1, kWarps * 32);
     }
-    named_bar_sync(1, kWarps * 32);
-    float m[RL], l[RL];
-    float4 o[RL][kCols];
+    float m = -INFINITY, l = 0.f;                 // of row `own`
+    float4 o[RL][2];
 #pragma unroll
-    for (int i = 0; i < RL; ++i) {
-      m[i] = -INFINITY;
-      l[i] = 0.f;
-#pragma unroll
-      for (int c = 0; c < kCols; ++c) o[i][c] = make_float4(0.f, 0.f, 0.f, 0.f);
-    }
+    for (int i = 0; i < RL; ++i) o[i][0] = o[i][1] = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int t = g.t0; t < g.t1; ++t, ring += 2) {
-      const int pos = t * kKeys + key;
+      const int pos = t * kKeys + warp * 8;
       const bool masked = (t + 1) * kKeys > g.all;
       uint32_t stage = ring % kStages;
+      const uint32_t chunk = (ls >> 3) * kPiece + warp * 1024u;
       wait(p, &s.tail, &s.tail.full[stage], (ring / kStages) & 1u);
-      float2 z2[RL][2];
+      float z[8];
 #pragma unroll
-      for (int i = 0; i < RL; ++i) z2[i][0] = z2[i][1] = make_float2(0.f, 0.f);
-      for (int x = 0; x < units; x += 8) {
-        const uint8_t* const at = s.ring[stage] + (x >> 3) * kPiece + key * 128;
+      for (int kk = 0; kk < 8; ++kk) {
+        const uint8_t* const at = s.ring[stage] + chunk + kk * 128 + (((ls & 7) ^ kk) << 4);
+        const float4 f0 = *reinterpret_cast<const float4*>(at);
+        float4 f1 = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (kTwo) f1 = *reinterpret_cast<const float4*>(at + 2 * kPiece);
+        float v[RL];
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-          if (x + c >= units) break;
-          const float4 f = *reinterpret_cast<const float4*>(at + ((c ^ lk) << 4));
+        for (int i = 0; i < RL; ++i) {
+          float2 a = mul2(make_float2(f0.x, f0.y), make_float2(q[i][0].x, q[i][0].y));
+          a = fma2(make_float2(f0.z, f0.w), make_float2(q[i][0].z, q[i][0].w), a);
+          if (kTwo) {
+            a = fma2(make_float2(f1.x, f1.y), make_float2(q[i][1].x, q[i][1].y), a);
+            a = fma2(make_float2(f1.z, f1.w), make_float2(q[i][1].z, q[i][1].w), a);
+          }
+          v[i] = a.x + a.y;
+        }
+        // Lanes whose bit is set go on with the upper half of the rows, the others with the lower.
 #pragma unroll
-          for (int i = 0; i < RL; ++i) {
-            const float4 q = *reinterpret_cast<const float4*>(&s.q[lr + 4 * i][(x + c) * 4]);
-            z2[i][0] = fma2(make_float2(f.x, f.y), make_float2(q.x, q.y), z2[i][0]);
-            z2[i][1] = fma2(make_float2(f.z, f.w), make_float2(q.z, q.w), z2[i][1]);
+        for (int n = RL / 2, bit = 8; bit > 0; bit >>= 1, n >>= 1) {
+          const bool up = ls & bit;
+          if (n > 0) {
+#pragma unroll
+            for (int i = 0; i < n; ++i) {
+              const float give = up ? v[i] : v[i + n], keep = up ? v[i + n] : v[i];
+              v[i] = keep + __shfl_xor_sync(0xffffffffu, give, bit);
+            }
+          } else {
+            v[0] += __shfl_xor_sync(0xffffffffu, v[0], bit);
           }
         }
+        z[kk] = v[0];
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&s.tail.empty[stage]));
-      float w[RL];
-      unsigned seen = 0xffffffffu;                // a bit a row of this lane's
+      unsigned seen = 0xffu;                      // a bit a key, of row `own`
+      if (masked) {
 #pragma unroll
-      for (int i = 0; i < RL; ++i) {
-        float z = (z2[i][0].x + z2[i][0].y) + (z2[i][1].x + z2[i][1].y);
-        if (masked) {
-          const int row = lr + 4 * i, j = pos - g.len;
-          bool on = s.used[row] && pos < g.total;
-          if (on && j >= 0) on = p.parents ? s.path[row][j >> 5] >> (j & 31) & 1u : pos < s.upto[row];
+        for (int kk = 0; kk < 8; ++kk) {
+          const int j = pos + kk - g.len;
+          bool on = s.used[own] && pos + kk < g.total;
+          if (on && j >= 0) on = p.parents ? s.path[own][j >> 5] >> (j & 31) & 1u : pos + kk < s.upto[own];
           if (!on) {
-            z = -INFINITY;
-            seen &= ~(1u << i);
+            z[kk] = -INFINITY;
+            seen &= ~(1u << kk);
           }
         }
-        float top = z;
-#pragma unroll
-        for (int x = 1; x < 8; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-        const float now = fmaxf(m[i], top), base = tree_base(p, now);
-        if (__any_sync(0xffffffffu, now > m[i])) {
-          const float c = m[i] == -INFINITY ? 0.f : exp2f(tree_base(p, m[i]) - base);
-          l[i] *= c;
-#pragma unroll
-          for (int y = 0; y < kCols; ++y) o[i][y] = make_float4(o[i][y].x * c, o[i][y].y * c, o[i][y].z * c, o[i][y].w * c);
-          m[i] = now;
-        }
-        w[i] = seen >> i & 1u ? exp2f(fmaf(z, p.scale, -base)) : 0.f;
-        l[i] += w[i];
       }
+      const float now = fmaxf(m, fmax3(fmax3(z[0], z[1], z[2]), fmax3(z[3], z[4], z[5]), fmaxf(z[6], z[7])));
+      const float base = tree_base(p, now);
+      if (__any_sync(0xffffffffu, now > m)) {
+        const float c = m == -INFINITY ? 0.f : exp2f(tree_base(p, m) - base);
+        l *= c;
+        m = now;
+#pragma unroll
+        for (int i = 0; i < RL; ++i) {
+          const float ci = __shfl_sync(0xffffffffu, c, half * 16 + i * kDup);
+          const float2 c2 = make_float2(ci, ci);
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const float2 lo = mul2(make_float2(o[i][y].x, o[i][y].y), c2), hi = mul2(make_float2(o[i][y].z, o[i][y].w), c2);
+            o[i][y] = make_float4(lo.x, lo.y, hi.x, hi.y);
+          }
+        }
+      }
+      float w[8];
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk) w[kk] = seen >> kk & 1u ? exp2f(fmaf(z[kk], p.scale, -base)) : 0.f;
+      l += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
       stage = (ring + 1) % kStages;
       wait(p, &s.tail, &s.tail.full[stage], ((ring + 1) / kStages) & 1u);
 #pragma unroll
       for (int kk = 0; kk < 8; ++kk) {
-        const int from = (lane & 24) | kk;
-        float wk[RL];
+        const uint8_t* const at = s.ring[stage] + chunk + kk * 128 + (((ls & 7) ^ kk) << 4);
+        const float4 f0 = *reinterpret_cast<const float4*>(at);
+        float4 f1 = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (kTwo) f1 = *reinterpret_cast<const float4*>(at + 2 * kPiece);
 #pragma unroll
-        for (int i = 0; i < RL; ++i) wk[i] = __shfl_sync(0xffffffffu, w[i], from);
-        const unsigned on = masked ? __shfl_sync(0xffffffffu, seen, from) : 0xffffffffu;
-        const uint8_t* const at = s.ring[stage] + (warp * 8 + kk) * 128 + ((lk ^ kk) << 4);
-#pragma unroll
-        for (int c = 0; c < kCols; ++c) {
-          if (32 * c >= p.dim) break;
-          const float4 f = *reinterpret_cast<const float4*>(at + c * kPiece);
-#pragma unroll
-          for (int i = 0; i < RL; ++i)
-            if (on >> i & 1u) {                   // what a row does not see may be anything
-              const float2 w2 = make_float2(wk[i], wk[i]);
-              const float2 lo = fma2(make_float2(f.x, f.y), w2, make_float2(o[i][c].x, o[i][c].y));
-              const float2 hi = fma2(make_float2(f.z, f.w), w2, make_float2(o[i][c].z, o[i][c].w));
-              o[i][c] = make_float4(lo.x, lo.y, hi.x, hi.y);
-            }
+        for (int i = 0; i < RL; ++i) {
+          const float wk = __shfl_sync(0xffffffffu, w[kk], half * 16 + i * kDup);
+          if (masked && !(__shfl_sync(0xffffffffu, seen, half * 16 + i * kDup) >> kk & 1u)) continue;  // it may be anything
+          const float2 w2 = make_float2(wk, wk);
+          const float2 a = fma2(make_float2(f0.x, f0.y), w2, make_float2(o[i][0].x, o[i][0].y));
+          const float2 b = fma2(make_float2(f0.z, f0.w), w2, make_float2(o[i][0].z, o[i][0].w));
+          o[i][0] = make_float4(a.x, a.y, b.x, b.y);
+          if (kTwo) {
+            const float2 c = fma2(make_float2(f1.x, f1.y), w2, make_float2(o[i][1].x, o[i][1].y));
+            const float2 d = fma2(make_float2(f1.z, f1.w), w2, make_float2(o[i][1].z, o[i][1].w));
+            o[i][1] = make_float4(c.x, c.y, d.x, d.y);
+          }
         }
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&s.tail.empty[stage]));
     }
     // The warps' parts of the keys meet.
+    if (ls % kDup == 0) s.ml[warp][own] = make_float2(m, l);
 #pragma unroll
-    for (int i = 0; i < RL; ++i) {
+    for (int i = 0; i < RL; ++i)
 #pragma unroll
-      for (int x = 1; x < 8; x <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
-      if (lk == 0) s.ml[warp][lr + 4 * i] = make_float2(m[i], l[i]);
-#pragma unroll
-      for (int c = 0; c < kCols; ++c) *reinterpret_cast<float4*>(&s.o[warp][lr + 4 * i][32 * c + 4 * lk]) = o[i][c];
-    }
+      for (int c = 0; c < 2; ++c) *reinterpret_cast<float4*>(&s.o[warp][half * RL + i][64 * c + 4 * ls]) = o[i][c];
     named_bar_sync(1, kWarps * 32);
     const bool whole = g.t0 == 0 && g.t1 == g.nt;
     for (int x = tid; x < g.nrows * units; x += kWarps * 32) {
@@ -269,7 +293,7 @@ __device__ void row_role(const TreeParams& p, Shared<RW>& s) {
   }
 }
 
-template <int RW>
+template <int RW, bool kTwo>
 __global__ void __launch_bounds__(kThreads, 1) tree_fp32_kernel(const __grid_constant__ TreeParams p) {
   extern __shared__ __align__(1024) uint8_t smem[];
   Shared<RW>& s = *reinterpret_cast<Shared<RW>*>(smem);
@@ -284,10 +308,15 @@ __global__ void __launch_bounds__(kThreads, 1) tree_fp32_kernel(const __grid_con
   }
   const Range range = plan_cut<kThreads>(p, &s.tail);  // has barriers
   chain_trigger();  // every CTA of this launch is resident: the next kernel's cannot take their place
-  if (warp < kWarps) row_role<RW>(p, s);
-  else if (warp == kWarps) load_role(p, &s.tail, s.tail.full, s.tail.empty, smem_u32(s.ring));
-  else if ((threadIdx.x & 31) == 0) plan_role(p, &s.tail, range);
-  __syncwarp();
+  if (warp < kWarps) {
+    if (RW == 16 && kTwo) regs_increase<kRowRegs>();
+    row_role<RW, kTwo>(p, s);
+  } else {
+    if (RW == 16 && kTwo) regs_decrease<kCtlRegs>();
+    if (warp == kWarps) load_role(p, &s.tail, s.tail.full, s.tail.empty, smem_u32(s.ring));
+    else if (warp == kWarps + 1 && (threadIdx.x & 31) == 0) plan_role(p, &s.tail, range);
+    __syncwarp();
+  }
   __syncthreads();
 }
 
@@ -396,8 +425,10 @@ cudaError_t launch_tree_join(const TreeParams& p, cudaStream_t s) {
 }
 
 cudaError_t launch_tree_fp32(const TreeParams& p, cudaStream_t s) {
-  if (p.item_rows == 4) tree_fp32_kernel<4><<<p.sms, kThreads, sizeof(Shared<4>), s>>>(p);
-  else tree_fp32_kernel<16><<<p.sms, kThreads, sizeof(Shared<16>), s>>>(p);
+  if (p.item_rows == 4 && p.dim > 64) tree_fp32_kernel<4, true><<<p.sms, kThreads, sizeof(Shared<4>), s>>>(p);
+  else if (p.item_rows == 4) tree_fp32_kernel<4, false><<<p.sms, kThreads, sizeof(Shared<4>), s>>>(p);
+  else if (p.dim > 64) tree_fp32_kernel<16, true><<<p.sms, kThreads, sizeof(Shared<16>), s>>>(p);
+  else tree_fp32_kernel<16, false><<<p.sms, kThreads, sizeof(Shared<16>), s>>>(p);
   const cudaError_t e = cudaGetLastError();
   return e != cudaSuccess ? e : launch_tree_join(p, s);
 }
@@ -414,17 +445,24 @@ void tree_sizes(TreeParams* p) {
     // Rows of an entry on average: where they are few, less is computed for nobody.
     p->item_rows = p->N * p->group <= 4LL * p->n ? 4 : 16;
     p->key_shift = 6;
-    p->over = p->item_rows == 4 ? 6 : 2;
+    p->over = 2;  // (4 and 8: prompts of 1500 tokens 185 and 208 us instead of 173)
   }
   p->part_rows = static_cast<int>(p->N * p->group < p->item_rows ? p->N * p->group : p->item_rows);
 }
 
 cudaError_t setup_tree_kernels() {
   static_assert(sizeof(Shared<16>) <= 227 * 1024, "shared memory");
-  cudaError_t e = cudaFuncSetAttribute(tree_fp32_kernel<4>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Shared<4>));
-  if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(tree_fp32_kernel<16>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Shared<16>));
-  return e == cudaSuccess ? setup_tree_mma_kernels() : e;
+  cudaError_t e = cudaSuccess;
+  for (void (*kernel)(TreeParams) : {tree_fp32_kernel<4, false>, tree_fp32_kernel<4, true>})
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Shared<4>));
+  for (void (*kernel)(TreeParams) : {tree_fp32_kernel<16, false>, tree_fp32_kernel<16, true>})
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Shared<16>));
+  if (e != cudaSuccess) return e;
+  cudaFuncAttributes fa;
+  if ((e = cudaFuncGetAttributes(&fa, tree_fp32_kernel<16, true>)) != cudaSuccess) return e;
+  // The split of registers between the roles waits forever unless the launch has just that many.
+  if (fa.numRegs != kLaunchRegs || fa.maxThreadsPerBlock < kThreads) return cudaErrorInvalidConfiguration;
+  return setup_tree_mma_kernels();
 }
 
 }  // namespace mls
