@@ -1015,6 +1015,7 @@ class PagedCache:
         self.c = mls_cache(*sizes, *[t.data_ptr() for t in buffers])
         self.ref = ctypes.byref(self.c)
         self.seqs, self.layers = int(seqs), int(layers)
+        self.token = torch.Size((int(kv_heads), int(head_dim)))
         self.reset(stream)
         self.ws = torch.empty(mls_cache_workspace_size(self.c), dtype=torch.uint8, device=dev)
 
@@ -1039,10 +1040,20 @@ class PagedCache:
     def append(self, k, v, start, layer=None, seqs=None, stream=None):
         """Writes new keys and values [layers, N, kv_heads, head_dim] (of one layer: [N, ...]) behind what the
         entries hold; entry i has the tokens start[i] .. start[i + 1] - 1."""
-        self.home()
+        dev = self.home()
         if layer is not None and not 0 <= layer < self.layers:
             raise ValueError(f"layer {layer} of {self.layers}")
-        mls_cache_append(self.c, -1 if layer is None else layer, seqs, start, k, v, stream)
+        at, dense = -1 if layer is None else layer, k.shape[-2:]
+        if not (k.is_contiguous() and v.is_contiguous() and k.shape == v.shape and dense == self.token
+                and k.dim() == (4 if layer is None else 3) and (layer is not None or k.shape[0] == self.layers)
+                and k.dtype is self.dtype and v.dtype is self.dtype and k.get_device() == dev == v.get_device()):
+            mls_cache_append(self.c, at, seqs, start, k, v, stream)  # with strides, or a mistake to name
+            return
+        n, N, size = start.shape[0] - 1, k.shape[-3], dense[0] * dense[1]
+        _expect("start", start, torch.int32, (n + 1,), dev)
+        rc = lib().mls_cache_append(self.ref, at, n, self._seqs(seqs, n, dev), start.data_ptr(), N, k.data_ptr(),
+                                    v.data_ptr(), size, N * size, _stream(stream))
+        _check(rc, "mls_cache_append")
 
     def compact(self, keep, path=None, seqs=None, stream=None):
         """Keeps keep[i] appended tokens of each entry (those of path[i], or the first ones) and gives back

@@ -1822,9 +1822,9 @@ int cache_validate(const mls_cache* c) {
   const int ps = c->page_size;
   if (ps < 8 || ps > 256 || (ps & (ps - 1)) || row % 16 || c->pages > (1 << 26) || c->max_pages > (1 << 20))
     return MLS_ERR_UNSUPPORTED;
-  // A token's pieces over all layers, and a page's of one layer, are counted in 32 bits.
-  const long long token = 2 * (row / 16);
-  if (c->kv_heads > INT_MAX / token / c->layers || c->kv_heads > INT_MAX / token / ps) return MLS_ERR_UNSUPPORTED;
+  // A page's pieces over all layers are counted in 32 bits (with room for a stride of the whole card's threads).
+  const long long token = 2 * (row / 16) * ps;
+  if (token > (1 << 30) || c->kv_heads > (1 << 30) / token / c->layers) return MLS_ERR_UNSUPPORTED;
   if (!c->k || !c->v || !c->table || !c->len || !c->held || !c->refs || !c->free_bits) return MLS_ERR_ARG;
   if (!aligned16(c->k) || !aligned16(c->v) || !aligned4(c->table) || !aligned4(c->len) || !aligned4(c->held) ||
       !aligned4(c->refs) || !aligned4(c->free_bits))

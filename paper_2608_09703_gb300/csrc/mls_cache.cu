@@ -131,12 +131,17 @@ __device__ void block_max_before(int v, int& before, int& all) {
 // Hands out pages to the entries of a reserve (as many as it takes to hold len + count tokens)
 // or of a fork (one, where the source's last page is partly filled).  One block: the entries' needs
 // become a prefix in shared memory, the free pages of the bit map are ranked by their count of
-// bits, and the page of rank r goes to the entry whose range of the prefix holds r.
+// bits, and the page of rank r goes to the entry whose range of the prefix holds r.  A warp takes a word of
+// the map at a time, a lane a page (a thread a word: 12.5 us for 64 entries and some 3500 pages, so 6.3).
 template <bool kFork>
 __global__ void __launch_bounds__(kTake)
     take_kernel(CacheView c, int n, const int* seqs, const int* count, const int* src, int* fresh, int* length) {
   extern __shared__ int pre[];  // [n + 1]
-  const int tid = threadIdx.x;
+  __shared__ unsigned s_bits[kTake];
+  __shared__ int s_rank[kTake];
+  const int tid = threadIdx.x, lane = tid & 31;
+  const int words = (c.pages + 31) >> 5;
+  const unsigned first_bits = tid < words ? c.free_bits[tid] : 0u;  // on its way while the entries are looked at
   int total = 0, top = -1;
   bool wide = false;
   for (int i0 = 0; i0 < n; i0 += kTake) {
@@ -191,9 +196,8 @@ __global__ void __launch_bounds__(kTake)
     wide = total > c.pages;
   }
   if (tid == 0) pre[n] = wide ? INT_MAX : total;
-  const int words = (c.pages + 31) >> 5;
-  int mine = 0;
-  for (int w = tid; w < words; w += kTake) mine += __popc(c.free_bits[w]);
+  int mine = __popc(first_bits);
+  for (int w = tid + kTake; w < words; w += kTake) mine += __popc(c.free_bits[w]);
   int skip, avail;
   block_scan(mine, skip, avail);  // also orders pre[] before its readers
   // Entries are served while their pages and those of all before them are there.
@@ -208,22 +212,25 @@ __global__ void __launch_bounds__(kTake)
   int given = 0;
   for (int w0 = 0; w0 < words && given < limit; w0 += kTake) {
     const int w = w0 + tid;
-    unsigned bits = w < words ? c.free_bits[w] : 0u;
-    int before, all;
-    block_scan(__popc(bits), before, all);
-    int r = given + before;
+    const unsigned bits = w0 == 0 ? first_bits : w < words ? c.free_bits[w] : 0u;
+    int before = skip, all = avail;
+    if (words > kTake) block_scan(__popc(bits), before, all);
+    s_bits[tid] = bits;
+    s_rank[tid] = given + before;
     given += all;
-    if (bits && r < limit) {
-      int e = 0, e1 = served - 1;  // the last entry whose range begins at or before r
-      while (e < e1) {
-        const int mid = (e + e1 + 1) >> 1;
-        if (pre[mid] <= r) e = mid;
-        else e1 = mid - 1;
-      }
-      while (bits && r < limit) {
-        const int page = w * 32 + __ffs(bits) - 1;
-        bits &= bits - 1u;
-        while (pre[e + 1] <= r) ++e;
+    __syncthreads();
+    for (int x = tid >> 5; x < kTake && w0 + x < words && s_rank[x] < limit; x += kTake / 32) {
+      const unsigned b = s_bits[x];
+      const int r = s_rank[x] + __popc(b & ((1u << lane) - 1u));
+      const bool mine_too = (b >> lane & 1u) && r < limit;
+      if (mine_too) {
+        const int page = (w0 + x) * 32 + lane;
+        int e = 0, e1 = served - 1;  // the last entry whose range begins at or before r: it is not empty
+        while (e < e1) {
+          const int mid = (e + e1 + 1) >> 1;
+          if (pre[mid] <= r) e = mid;
+          else e1 = mid - 1;
+        }
         if constexpr (kFork) {
           fresh[e] = page;
         } else {
@@ -231,10 +238,11 @@ __global__ void __launch_bounds__(kTake)
           c.table[static_cast<long long>(row) * c.max_pages + clamp_held(c, row) + (r - pre[e])] = page;
         }
         c.refs[page] = 1;
-        ++r;
       }
-      c.free_bits[w] = bits;
+      const unsigned gone = __ballot_sync(0xffffffffu, mine_too);
+      if (lane == 0 && gone) c.free_bits[w0 + x] = b & ~gone;
     }
+    __syncthreads();
   }
   __syncthreads();
   for (int i = tid; i < n; i += kTake) {
@@ -251,21 +259,20 @@ __global__ void __launch_bounds__(kTake)
 // gridDim.y blocks.  kDeep copies of 16 bytes are in flight per thread.
 constexpr int kDeep = 8;
 __device__ void copy_page(const CacheView& from, const CacheView& to, int src, int dst, int slots) {
-  const long long each = static_cast<long long>(slots) * from.row;  // pieces of a head: they lie side by side
-  const int planes = 2 * from.layers * from.heads;
-  const long long all = each * planes;
-  const long long step = static_cast<long long>(gridDim.y) * blockDim.x;
-  for (long long i = static_cast<long long>(blockIdx.y) * blockDim.x + threadIdx.x; i < all; i += step * kDeep) {
+  // Pieces of a head lie side by side; all of a page's are counted in 32 bits.  (In 64, whose division is slow, forking
+  // 64 prompts of 28 layers took 26 us, so 23.)
+  const unsigned each = static_cast<unsigned>(slots) * from.row, planes = 2u * from.layers * from.heads;
+  const unsigned all = each * planes, step = gridDim.y * blockDim.x;
+  for (unsigned i = blockIdx.y * blockDim.x + threadIdx.x; i < all; i += step * kDeep) {
     uint4 v[kDeep];
     uint4* at[kDeep];
 #pragma unroll
     for (int j = 0; j < kDeep; ++j) {
-      const long long x = i + j * step;
+      const unsigned x = i + j * step;
       at[j] = nullptr;
       if (x >= all) continue;
-      const int plane = static_cast<int>(x / each);
-      const long long piece = x - plane * each;
-      const int head = plane % from.heads, lk = plane / from.heads, layer = lk >> 1;
+      const unsigned plane = x / each, piece = x - plane * each, lk = plane / from.heads;
+      const int head = static_cast<int>(plane - lk * from.heads), layer = static_cast<int>(lk >> 1);
       v[j] = ((lk & 1) ? from.v : from.k)[cache_at(from, layer, src, head, 0) + piece];
       at[j] = ((lk & 1) ? to.v : to.k) + cache_at(to, layer, dst, head, 0) + piece;
     }
@@ -385,9 +392,22 @@ __device__ bool path_ok(const CacheView& c, const int* path, int path_ld, int ke
   return true;
 }
 
+// The lengths that are kept, and the pages behind them given back.
+__device__ void close_entry(const CacheView& c, int row, int n, int len, int held) {
+  const int pages = (len + n + (1 << c.page_shift) - 1) >> c.page_shift;
+  drop_pages(c, row, pages, held);
+  __syncthreads();  // every thread has read len and held
+  if (threadIdx.x == 0) {
+    c.len[row] = len + n;
+    c.held[row] = pages;
+  }
+}
+
 // Moves the kept tokens of an entry together.  A thread has one piece of 16 bytes of a head and
 // layer and walks the path: since path[k] >= k and the path increases, what it writes at k lies
 // before all that it has still to read, so the move is right in place, several tokens at a time.
+// An entry's only block closes it too (kClose).
+template <bool kClose>
 __global__ void __launch_bounds__(kThreads)
     move_kernel(CacheView c, const int* seqs, const int* keep, const int* path, int path_ld) {
   __shared__ int src_page[kCachePath], dst_page[kCachePath];
@@ -395,9 +415,12 @@ __global__ void __launch_bounds__(kThreads)
   const int row = entry_row(c, seqs, blockIdx.x);
   if (row < 0) return;
   const int* const mine = path + static_cast<long long>(blockIdx.x) * path_ld;
-  const int n = keep[blockIdx.x], len = c.len[row];
+  const int n = keep[blockIdx.x], len = c.len[row], held = clamp_held(c, row);
   int first;
-  if (!path_ok(c, mine, path_ld, n, len, clamp_held(c, row), first)) return;  // refused by the next kernel
+  if (!path_ok(c, mine, path_ld, n, len, held, first)) {
+    if (kClose && threadIdx.x == 0) atomicOr(c.status, kStatusBadSeq);  // else the next kernel says so
+    return;
+  }
   const int* const table = c.table + static_cast<long long>(row) * c.max_pages;
   const int mask = (1 << c.page_shift) - 1;
   const int pieces = 2 * c.layers * c.heads * c.row;
@@ -415,7 +438,7 @@ __global__ void __launch_bounds__(kThreads)
     }
     if (__syncthreads_or(bad)) {
       if (threadIdx.x == 0) atomicOr(c.status, kStatusBadSeq);
-      return;
+      break;
     }
     for (int x = blockIdx.y * blockDim.x + threadIdx.x; x < pieces; x += gridDim.y * blockDim.x) {
       const int piece = x % c.row, plane = x / c.row, head = plane % c.heads, lk = plane / c.heads;
@@ -432,9 +455,12 @@ __global__ void __launch_bounds__(kThreads)
       }
     }
   }
+  if (kClose) {
+    __syncthreads();  // the table is read until here
+    close_entry(c, row, n, len, held);
+  }
 }
 
-// The lengths that are kept, and the pages behind them given back.
 __global__ void __launch_bounds__(kThreads)
     close_kernel(CacheView c, const int* seqs, const int* keep, const int* path, int path_ld) {
   chain_wait();
@@ -447,13 +473,7 @@ __global__ void __launch_bounds__(kThreads)
     if (threadIdx.x == 0) atomicOr(c.status, kStatusBadSeq);
     return;
   }
-  const int pages = (len + n + (1 << c.page_shift) - 1) >> c.page_shift;
-  drop_pages(c, row, pages, held);
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    c.len[row] = len + n;
-    c.held[row] = pages;
-  }
+  close_entry(c, row, n, len, held);
 }
 
 // Blocks for each of n entries that share `pieces` pieces of work, `deep` of them a thread: eight
@@ -500,9 +520,14 @@ cudaError_t launch_cache_append(const CacheView& c, const CacheAppend& a, cudaSt
 
 cudaError_t launch_cache_compact(const CacheView& c, int n, const int* seqs, const int* keep, const int* path,
                                  int path_ld, int sms, cudaStream_t s) {
+  const long long pieces = 2LL * c.layers * c.heads * c.row;
+  // Up to two pieces a thread one block moves as fast as two do, and needs no second kernel.
+  if (path && pieces <= 2 * kThreads) {
+    move_kernel<true><<<n, kThreads, 0, s>>>(c, seqs, keep, path, path_ld);
+    return cudaGetLastError();
+  }
   if (path) {
-    move_kernel<<<dim3(n, spread(n, 2LL * c.layers * c.heads * c.row, 1, sms)), kThreads, 0, s>>>(c, seqs, keep, path,
-                                                                                                path_ld);
+    move_kernel<false><<<dim3(n, spread(n, pieces, 1, sms)), kThreads, 0, s>>>(c, seqs, keep, path, path_ld);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     return launch_chained(close_kernel, dim3(n), dim3(kThreads), 0, s, c, seqs, keep, path, path_ld);
