@@ -402,6 +402,11 @@ __device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint3
     for (int i = 0; i < steps; ++i) {
       const int j = pair ? i : 2 * i + w, k0 = (g.t0 + j) * kKeys;
       const bool masked = k0 + kKeys > g.all;
+      // (Before anything else: that S is there says that what the ring held before this step's V has arrived, without
+      // which a wait for V, by parity, could take an earlier round's arrival for it.)
+      wait(p, sh, &sh->s_full[w], s_par);
+      s_par ^= 1u;
+      tc_fence_after();
       if (masked) {
         // Values that not every row sees: infinities and NaN become 0, to be added to the rows that see them at
         // the end.  Those behind the last key, up to the end of its page, become 0 (the pages behind it came as
@@ -434,9 +439,6 @@ __device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint3
         fence_proxy_async_smem();
         __threadfence_block();
       }
-      wait(p, sh, &sh->s_full[w], s_par);
-      s_par ^= 1u;
-      tc_fence_after();
       if (busy) {
         float z[kKeys];
         tmem_ld128(ts, z);

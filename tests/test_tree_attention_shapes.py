@@ -88,3 +88,14 @@ def test_sequences_whose_nodes_all_take_no_part(dtype):
     check(x, out, lse, scale)
     assert (out[5:145] == 0).all() and torch.isinf(lse[5:145]).all()
     assert mls.mls_get_status() == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("n,tree", [(1, False), (16, True), (70, True)])
+def test_many_long_sequences(n, tree, dim):
+    """Ranges of many tiles that end in others' midst, their last tiles masked: a warp that comes early to a tile with a
+    mask must not touch what the ring holds before it."""
+    g = torch.Generator().manual_seed(n + dim)
+    lens = [3000] + [int(3000 * float(torch.rand(1, generator=g))) for _ in range(59)]
+    run_and_check(make(lens, [n] * 60, 8, 2, dim, 32, BF16, seed=n, tree=tree))
