@@ -472,6 +472,7 @@ int mls_cache_copy(const mls_cache* from, const mls_cache* to, int32_t n, const 
  *              16-byte aligned, q_ld a multiple of 16 bytes
  *   out        device, [N, q_heads, head_dim], dense, 16-byte aligned; lse: device, fp32 [N, q_heads]
  *   ws         device workspace of mls_tree_attention_workspace_size() bytes, 256-byte aligned
+ *              (its content does not matter; calls that overlap on the GPU need one each)
  * What a row does not attend to may hold anything, NaN and infinities included.  Sums are fp32; with a bf16
  * cache exp(z_j - m), m a running maximum, is rounded to bf16 before it meets v_j.  head_dim <= 128
  * (MLS_ERR_UNSUPPORTED beyond).  Asynchronous; 0 or a negative MLS_ERR_* code (nothing launched).

@@ -1060,10 +1060,12 @@ class PagedCache:
         the pages behind them."""
         dev, n = self.home(), keep.shape[0]
         _expect("keep", keep, torch.int32, (n,), dev)
+        at, ld = None, 0
         if path is not None:
-            _expect("path", path, torch.int32, (n, path.shape[1]), dev)
-        rc = lib().mls_cache_compact(self.ref, n, self._seqs(seqs, n, dev), keep.data_ptr(), _ptr(path),
-                                     0 if path is None else path.shape[1], _stream(stream))
+            ld = path.shape[1]
+            _expect("path", path, torch.int32, (n, ld), dev)
+            at = path.data_ptr()
+        rc = lib().mls_cache_compact(self.ref, n, self._seqs(seqs, n, dev), keep.data_ptr(), at, ld, _stream(stream))
         _check(rc, "mls_cache_compact")
 
     def fork(self, src, dst, stream=None):

@@ -31,23 +31,19 @@ struct Entry {
 __device__ __forceinline__ Entry tree_entry(const TreeParams& p, int i, int* status) {
   Entry e;
   const long long a = p.start[i], b = p.start[i + 1];
+  e.row = p.seqs ? p.seqs[i] : i;
+  const bool known = e.row >= 0 && e.row < p.c.seqs;
+  e.len = known ? p.c.len[e.row] : 0;             // does not wait for what start says
   bool bad = a < 0 || b < a || b > p.N;
   e.first = a;
   e.nodes = bad ? 0 : static_cast<int>(b - a);
-  e.row = p.seqs ? p.seqs[i] : i;
-  e.len = 0;
-  if (e.nodes) {
-    if (e.row < 0 || e.row >= p.c.seqs || (p.parents && e.nodes > kTreeMaxNodes)) {
-      bad = true;
-      e.row = -1;
-    } else {
-      e.len = p.c.len[e.row];
-      if (e.len < 0 || static_cast<long long>(e.len) + e.nodes > (static_cast<long long>(p.c.max_pages) << p.c.page_shift)) {
-        bad = true;
-        e.row = -1;
-        e.len = 0;
-      }
-    }
+  if (e.nodes == 0) {
+    e.len = 0;
+  } else if (!known || (p.parents && e.nodes > kTreeMaxNodes) || e.len < 0 ||
+             static_cast<long long>(e.len) + e.nodes > (static_cast<long long>(p.c.max_pages) << p.c.page_shift)) {
+    bad = true;
+    e.row = -1;
+    e.len = 0;
   }
   if (bad) atomicOr(status, kStatusBadSeq);
   return e;
@@ -94,7 +90,7 @@ struct Plan {
   uint64_t seg_full[kSegs], seg_empty[kSegs];
   Seg seg[kSegs];
   Entry en0;                                      // the range's first entry, its number and first unit
-  long long scan[32], base0;
+  long long scan[12], base0;                      // of at most 12 warps
   int e0, abort;
 };
 
@@ -115,6 +111,7 @@ struct Range {
 };
 template <int kThreads>
 __device__ Range plan_cut(const TreeParams& p, Plan* sh) {
+  static_assert(kThreads <= 12 * 32, "Plan::scan");
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int chunk = (p.n + kThreads - 1) / kThreads;
   const int i0 = min(tid * chunk, p.n), i1 = min(i0 + chunk, p.n);
@@ -186,9 +183,11 @@ __device__ inline void plan_role(const TreeParams& p, Plan* sh, const Range& ran
       }
       // The item, and where in it: its rows come after those of all heads before.
       const int size = u.nt + p.over;
-      const long long item = v / size;
+      // (In 32 bits where they do: a division of 64 is slow, and this is a thread's latency.)
+      const long long item = v >> 31 ? v / size : static_cast<unsigned>(v) / static_cast<unsigned>(size);
       const int in = static_cast<int>(v - item * size);
-      const int head = static_cast<int>(item % p.c.heads), r0 = u.r0 + static_cast<int>(item / p.c.heads) * p.item_rows;
+      const int up = item >> 31 ? static_cast<int>(item / p.c.heads) : static_cast<int>(static_cast<unsigned>(item) / p.c.heads);
+      const int head = static_cast<int>(item - static_cast<long long>(up) * p.c.heads), r0 = u.r0 + up * p.item_rows;
       const int end = static_cast<int>(min(static_cast<long long>(size), in + (range.hi - at)));
       at += end - in;
       v += end - in;
