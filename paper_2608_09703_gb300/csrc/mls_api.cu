@@ -1993,8 +1993,8 @@ int tree_validate(const mls_cache* c, int n, int64_t N, int q_heads) {
   if (const int rc = cache_validate(c)) return rc;
   if (n < 0 || N < 0 || N > INT_MAX || q_heads < 1 || q_heads % c->kv_heads) return MLS_ERR_ARG;
   if (c->head_dim > 128) return MLS_ERR_UNSUPPORTED;
-  // Boxes of the tensor maps are numbered, and warps counted, in 32 bits.
-  if (static_cast<long long>(c->layers) * c->pages > INT_MAX / c->kv_heads || N * q_heads > INT_MAX / 64)
+  // Boxes of the tensor maps, and the rows of out, are numbered in 32 bits (with room for an item's rows).
+  if (static_cast<long long>(c->layers) * c->pages > INT_MAX / c->kv_heads || N * q_heads > INT_MAX - 1024)
     return MLS_ERR_UNSUPPORTED;
   return MLS_OK;
 }
