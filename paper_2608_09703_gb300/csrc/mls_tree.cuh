@@ -83,8 +83,10 @@ struct Seg {
   int total;                                      // keys of the item: cached tokens and nodes up to its last
   int all;                                        // keys that every row sees
   int slot;                                       // of the CTA's two in the workspace
+  int solo, other;                                // bf16: 1, 2: of a couple, with `other` tiles in the other one
 };
 constexpr int kSegs = 4;
+constexpr int kSoloTiles = 8;                     // at most, of a couple's segments
 // In shared memory.
 struct Plan {
   uint64_t seg_full[kSegs], seg_empty[kSegs];
@@ -151,14 +153,18 @@ __device__ Range plan_cut(const TreeParams& p, Plan* sh) {
   return r;
 }
 
-// One thread: writes down the segments of the range, and what begins there and goes on in other CTAs'.
+// One thread: writes down the segments of the range, and what begins there and goes on in other CTAs'.  Two short
+// ones of about as many tiles that follow one another make a couple, where the kernel works on such side by side
+// (224 trees of 5 nodes, 16 heads: 164 us without, 116 with; 256 single tokens over up to 1000: 362 and 277).
 __device__ inline void plan_role(const TreeParams& p, Plan* sh, const Range& range) {
   uint32_t k = 0;
   bool first = true;
   TreeJoin join = {};
-  auto slot = [&]() -> Seg* {
-    return wait(p, sh, &sh->seg_empty[k % kSegs], ((k / kSegs) & 1u) ^ 1u) ? &sh->seg[k % kSegs] : nullptr;
+  auto slot = [&](uint32_t i) -> Seg* {
+    return wait(p, sh, &sh->seg_empty[i % kSegs], ((i / kSegs) & 1u) ^ 1u) ? &sh->seg[i % kSegs] : nullptr;
   };
+  auto publish = [&] { mbar_arrive(smem_u32(&sh->seg_full[k++ % kSegs])); };
+  int held = 0;                                   // tiles of the k-th, written down, that waits for one to make a couple with
   long long at = range.lo;
   if (at < range.hi) {
     Entry en = sh->en0;
@@ -193,7 +199,7 @@ __device__ inline void plan_role(const TreeParams& p, Plan* sh, const Range& ran
       v += end - in;
       const int t0 = max(in - p.over, 0), t1 = end - p.over;
       if (t1 <= t0) continue;                     // the range ends before the item's first tile
-      Seg* const g = slot();
+      Seg* const g = slot(held ? k + 1 : k);
       if (!g) break;
       g->first = en.first;
       g->nodes = en.nodes;
@@ -208,6 +214,7 @@ __device__ inline void plan_role(const TreeParams& p, Plan* sh, const Range& ran
       g->total = en.len + (r0 + g->nrows - 1) / p.group + 1;
       g->all = en.row < 0 ? 0 : p.parents ? en.len : en.len + r0 / p.group + 1;
       g->slot = first ? 0 : 1;
+      g->solo = g->other = 0;
       first = false;
       if (t0 == 0 && t1 < u.nt) {                 // at = hi: the range ends after tile t1 of the item
         join.pieces = 1 + static_cast<int>((u.nt - t1 + range.each - 1) / range.each);
@@ -217,13 +224,25 @@ __device__ inline void plan_role(const TreeParams& p, Plan* sh, const Range& ran
         join.r0 = r0;
         join.head = head;
       }
-      mbar_arrive(smem_u32(&sh->seg_full[k++ % kSegs]));
+      const int n = t1 - t0;
+      const bool may = p.bf16 && g->nrows <= p.tile_rows && n <= kSoloTiles;
+      const bool couple = held && may && abs(n - held) <= p.over;
+      if (couple) {
+        sh->seg[k % kSegs].solo = 1;
+        sh->seg[k % kSegs].other = n;
+        g->solo = 2;
+        g->other = held;
+      }
+      if (held) publish();
+      held = may && !couple ? n : 0;
+      if (!held) publish();
     }
+    if (held) publish();
   }
   p.joins[blockIdx.x] = join;
-  if (Seg* const g = slot()) {
+  if (Seg* const g = slot(k)) {
     g->t0 = g->t1 = 0;
-    mbar_arrive(smem_u32(&sh->seg_full[k % kSegs]));
+    publish();
   }
 }
 // The k-th segment for one of its readers (false: there is none, or a wait ran out).

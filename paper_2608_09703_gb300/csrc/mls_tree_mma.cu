@@ -6,7 +6,8 @@
 // A CTA has two streams of a warpgroup, an S and an O accumulator each (512 columns of TMEM): the tensor cores
 // work for one while the other takes its exponentials.  With more than 128 rows the streams have a row
 // tile each and share the keys; with fewer they have the same rows, and every other key tile: what they
-// hold is joined at the end, each warp reading the other stream's O in its own lanes.
+// hold is joined at the end, each warp reading the other stream's O in its own lanes.  Two short pieces of work with
+// a row tile each are taken side by side, a stream each: what begins and ends one hides behind the other.
 // Items are pairs of row tiles of an entry and key/value head, cut into ranges as mls_tree.cuh has it.
 //
 // Softmax in one pass: a running maximum per row, which moves only when it grows by more than 2^8 (P stays
@@ -26,7 +27,7 @@ namespace {
 
 constexpr int kRows = 128, kKeys = 128;           // of a tile
 constexpr int kThreads = 384;
-constexpr int kCtlRegs = 72, kSoftmaxRegs = 216, kLaunchRegs = 168;  // 72 + 2 x 216 = 3 x 168
+constexpr int kCtlRegs = 88, kSoftmaxRegs = 208, kLaunchRegs = 168;  // 88 + 2 x 208 = 3 x 168
 constexpr uint64_t kDrainNs = 100000000ull;
 constexpr uint32_t kTmemCols = 512, kAccO = 256;  // S of stream w at 128 w, O at 256 + 128 w
 constexpr float kGrow = 8.f;
@@ -41,7 +42,8 @@ struct Tail : Plan {
     short up[kTreeMaxNodes];
     float2 ml[kRows];
   } row[2];
-  int fix[2];                                     // by a segment's parity: the last one with values taken out
+  // By a segment's last two bits (streams are at most three segments apart): the last one with values taken out.
+  int fix[4];
   uint32_t tmem_slot;
 };
 // DC: pieces of 64 values (128 bytes) of a row.  K and V tiles lie in atoms of 8 rows of 128 bytes; of rows of
@@ -61,10 +63,13 @@ struct Layout {
   }
 };
 
-// Where the K and V tiles of step j lie in the order in which a segment of n tiles is loaded: K0 V0 K1 V1 ...
-// for two row tiles, K0 K1 V0 K2 V1 K3 ... for two streams of key tiles, as the MMAs take them.
-__device__ __forceinline__ uint32_t place_k(int j, bool pair) { return pair ? 2 * j : j < 2 ? j : 2 * j - 1; }
-__device__ __forceinline__ uint32_t place_v(int j, int n, bool pair) { return pair ? 2 * j + 1 : min(2 * j + 2, 2 * n - 1); }
+// The order in which tiles are loaded, as the MMAs take them: for two row tiles K V K V ...; for two streams with n[0]
+// and n[1] steps of their own (a couple's, or every other tile of one segment) K K, then V of a step and K of the
+// next for each stream in turn, as far as there are any.  Where V of step i lies then:
+__device__ __forceinline__ uint32_t place_v(int n0, int n1, int w, int i) {
+  const int a = i + w;                            // steps of the first stream that come before it
+  return min(n1, 1) + 1 + min(a, n0) + min(a, n0 - 1) + min(i, n1) + min(i, max(n1 - 1, 0));
+}
 
 template <int DC, bool kJoint>
 __device__ void load_role(const TreeParams& p, Tail* sh, uint32_t base) {
@@ -84,34 +89,33 @@ __device__ void load_role(const TreeParams& p, Tail* sh, uint32_t base) {
     if (lane == 0) free_seg(sh, k);
     const int n = g.t1 - g.t0;
     const bool pair = g.nrows > p.tile_rows;
-    const int* const table = g.row < 0 ? nullptr : p.c.table + static_cast<long long>(g.row) * p.c.max_pages;
-    for (int i = 0; i < 2 * n; ++i, ++ring) {
-      // The i-th load of the segment: the K or the V tile of step j.
-      int j;
-      bool is_v;
-      if (pair) {
-        j = i >> 1;
-        is_v = i & 1;
-      } else if (i < 2) {
-        is_v = i == 1 && n == 1;
-        j = is_v ? 0 : i;
-      } else if (i == 2 * n - 1) {
-        is_v = true;
-        j = n - 1;
-      } else {
-        is_v = !(i & 1);
-        j = is_v ? (i - 2) >> 1 : (i + 1) >> 1;
-      }
-      const int pos = (g.t0 + j) * kKeys + mine * box, slot = pos & (size - 1);
+    const int each = pair || g.solo ? 1 : 2, n0 = each == 1 ? n : (n + 1) / 2, n1 = pair ? 0 : g.solo ? g.other : n / 2;
+    // What the second stream's tiles are of: the couple's other segment, or the same one, from its second tile on.
+    int row = g.row, head = g.head, t0 = g.t0 + 1, total = g.total;
+    if (g.solo) {
+      Seg b;
+      ok = __all_sync(0xffffffffu, read_seg(p, sh, ++k, b));
+      row = b.row, head = b.head, t0 = b.t0, total = b.total;
+      __syncwarp();
+      if (lane == 0) free_seg(sh, k);
+    }
+#pragma unroll 1
+    for (int x = 1; ok && (x >> 2) <= max(n0, n1); ++x) {  // K K, then V K V K of each step
+      const bool second = x & 2, is_v = !(x & 1);
+      const int i = (x >> 2) - is_v;
+      if (i < 0 || i >= (second ? n1 : n0)) continue;
+      const int pos = ((second ? t0 : g.t0) + i * each) * kKeys + mine * box, slot = pos & (size - 1);
+      const int of = second ? row : g.row;
       int at = none;
-      if (active && table && pos < g.total) {
-        const int page = table[pos >> p.c.page_shift];
-        if (page >= 0 && page < p.c.pages) at = (p.layer * p.c.pages + page) * p.c.heads + g.head;
+      if (active && of >= 0 && pos < (second ? total : g.total)) {
+        const int page = p.c.table[static_cast<long long>(of) * p.c.max_pages + (pos >> p.c.page_shift)];
+        if (page >= 0 && page < p.c.pages) at = (p.layer * p.c.pages + page) * p.c.heads + (second ? head : g.head);
         else atomicOr(p.status, kStatusBadSeq);
       }
       const uint32_t stage = ring % L::kStages, phase = (ring / L::kStages) & 1u;
       ok = __all_sync(0xffffffffu, wait(p, sh, &sh->empty[stage], phase ^ 1u));
       if (!ok) break;
+      ++ring;
       const uint32_t bar = smem_u32(&sh->full[stage]), to = base + L::kRing + stage * L::kTile + dst;
       if (lane == 0) mbar_arrive_expect_tx(bar, L::kTile);
       __syncwarp();
@@ -145,7 +149,7 @@ __device__ void query_role(const TreeParams& p, Tail* sh, uint32_t base) {
     const int n = g.t1 - g.t0;
     const bool pair = g.nrows > p.tile_rows;
     for (int w = 0; w < 2; ++w) {
-      if (!pair && w == 1 && n < 2) continue;
+      if (g.solo ? w != g.solo - 1 : !pair && w == 1 && n < 2) continue;
       ok = __all_sync(0xffffffffu, wait(p, sh, &sh->q_free[w], (loads[w] & 1u) ^ 1u));
       if (!ok) break;
       ++loads[w];
@@ -253,15 +257,14 @@ __device__ void mma_role(const TreeParams& p, Tail* sh, uint32_t base, uint32_t 
       }
       p_par ^= 1u << w;
     };
-    const int streams = pair || n > 1 ? 2 : 1;
-    for (int w = 0; ok && w < streams; ++w) {
-      if (!ready(&sh->q_ready[w], (q_par >> w) & 1u)) break;
-      q_par ^= 1u << w;
-      if ((!pair || w == 0) && !ready(&sh->full[at.stage], at.phase)) break;
-      scores(w, at, pair ? n == 1 : w + 2 >= n, !pair || w == 1);
-      if (!pair || w == 1) at = at.next();
-    }
-    if (pair) {  // K0 | V0 K1 | V1 K2 ... each for both
+    if (pair) {  // K | V K | V K ... each for both
+      for (int w = 0; ok && w < 2; ++w) {
+        if (!ready(&sh->q_ready[w], (q_par >> w) & 1u)) break;
+        if (w == 0 && !ready(&sh->full[at.stage], at.phase)) break;
+        scores(w, at, n == 1, w == 1);
+      }
+      q_par ^= 3u;
+      at = at.next();
       for (int i = 0; ok && i < n; ++i) {
         const Place v = at, key = at.next();
         const bool more = i + 1 < n;
@@ -274,18 +277,33 @@ __device__ void mma_role(const TreeParams& p, Tail* sh, uint32_t base, uint32_t 
         }
         at = more ? key.next() : key;
       }
-    } else {     // K0 K1 | V0 K2 | V1 K3 ... one for each in turn
-      for (int j = 0; ok && j < n; ++j) {
-        const int w = j & 1;
+      continue;
+    }
+    // K K | V K | V K ... of either stream in turn.
+    const bool solo = __shfl_sync(0xffffffffu, g.solo, 0) != 0;
+    const int n0 = solo ? n : (n + 1) / 2, n1 = solo ? __shfl_sync(0xffffffffu, g.other, 0) : n / 2;
+    if (solo) {  // the stream's other segment: all there is to know of it is here
+      if (!(ok = __all_sync(0xffffffffu, wait(p, sh, &sh->seg_full[(k + 1) % kSegs], ((k + 1) / kSegs) & 1u)))) break;
+      ++k;
+      if (lane == 0) free_seg(sh, k);
+    }
+    for (int i = -1; ok && i < max(n0, n1); ++i)
+      for (int w = 0; ok && w < 2; ++w) {
+        const int steps = w ? n1 : n0;
+        if (i >= steps || (i < 0 && steps == 0)) continue;
+        if (i >= 0) {
+          if (!ready(&sh->full[at.stage], at.phase)) break;
+          values(w, at, i == 0, i + 1 == steps, true);
+          at = at.next();
+        } else {
+          if (!ready(&sh->q_ready[w], (q_par >> w) & 1u)) break;
+          q_par ^= 1u << w;
+        }
+        if (!ok || i + 1 >= steps) continue;
         if (!ready(&sh->full[at.stage], at.phase)) break;
-        values(w, at, j < 2, j + 2 >= n, true);
-        at = at.next();
-        if (!ok || j + 2 >= n) continue;
-        if (!ready(&sh->full[at.stage], at.phase)) break;
-        scores(w, at, j + 4 >= n, true);
+        scores(w, at, i + 2 == steps, true);
         at = at.next();
       }
-    }
   }
   // Every MMA that the elected lane issued has finished before TMEM is released.
   if (elect_one()) mma_commit(smem_u32(&sh->drain));
@@ -341,7 +359,7 @@ __device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint3
   const uint32_t ts = tmem + lanes + w * kKeys, to = tmem + lanes + kAccO + w * 128;
   const __nv_bfloat16* const V = reinterpret_cast<const __nv_bfloat16*>(p.c.v);
   const int mask = (1 << p.c.page_shift) - 1;
-  uint32_t ring = 0, s_par = 0, o_par = 0, met = 0;
+  uint32_t ring = 0, couple = 0, s_par = 0, o_par = 0, met = 0;
   auto meet = [&] {                               // both streams (a wait with a limit, unlike a barrier)
     __syncwarp();
     if (lane == 0) mbar_arrive(smem_u32(&sh->met));
@@ -358,8 +376,13 @@ __device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint3
     if (!named_bar_and(1 + w, kRows, read_seg(p, sh, k, g))) break;
     if (lane == 0) free_seg(sh, k);
     const int n = g.t1 - g.t0;
-    const bool pair = g.nrows > p.tile_rows;
-    const int steps = pair ? n : (n + 1 - w) / 2;
+    if (g.solo == 1) {
+      couple = ring;
+      ring += 2 * (n + g.other);
+    }
+    if (g.solo && g.solo - 1 != w) continue;
+    const bool pair = g.nrows > p.tile_rows, alone = pair || g.solo;  // alone: a row tile is this stream's only
+    const int steps = alone ? n : (n + 1 - w) / 2;
     const int rl = (pair ? w * p.tile_rows : 0) + tid;  // this thread's row of the item
     const bool inside = tid < p.tile_rows && rl < g.nrows;
     const int r = g.r0 + rl, node = inside ? r / p.group : 0;
@@ -400,7 +423,7 @@ __device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint3
     const bool busy = __any_sync(0xffffffffu, inside);  // rows of this warp
     float m = -INFINITY, l = 0.f;
     for (int i = 0; i < steps; ++i) {
-      const int j = pair ? i : 2 * i + w, k0 = (g.t0 + j) * kKeys;
+      const int j = alone ? i : 2 * i + w, k0 = (g.t0 + j) * kKeys;
       const bool masked = k0 + kKeys > g.all;
       // (Before anything else: that S is there says that what the ring held before this step's V has arrived, without
       // which a wait for V, by parity, could take an earlier round's arrival for it.)
@@ -412,7 +435,8 @@ __device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint3
         // the end.  Those behind the last key, up to the end of its page, become 0 (the pages behind it came as
         // zeros).  Where the other stream has the same tile, one of the two finds what there is: it says so before
         // it clears anything, and the other, which looks at `fix` when both are through, has seen either.
-        const uint32_t at = ring + place_v(j, n, pair), stage = at % L::kStages;
+        const int n0 = g.solo == 2 ? g.other : g.solo ? n : (n + 1) / 2, n1 = g.solo == 1 ? g.other : g.solo ? n : n / 2;
+        const uint32_t at = pair ? ring + 2 * i + 1 : (g.solo ? couple : ring) + place_v(n0, n1, w, i), stage = at % L::kStages;
         const uint32_t tile = base + L::kRing + stage * L::kTile;
         const int a = max(g.all - k0, 0), b = min((g.total + mask & ~mask) - k0, kKeys), last = g.total - k0;
         wait(p, sh, &sh->full[stage], (at / L::kStages) & 1u);
@@ -424,7 +448,7 @@ __device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint3
           if (row < last) {
             v = ld_shared_v4(addr);
             if (!odd_any(v)) continue;
-            *static_cast<volatile int*>(&sh->fix[seg & 1]) = seg;
+            *static_cast<volatile int*>(&sh->fix[seg & 3]) = seg;
             __threadfence_block();
             uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -502,7 +526,7 @@ __device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint3
           for (int h = 0; h < 2; ++h) mbar_arrive(smem_u32(&sh->p_ready[w][h]));
       }
     }
-    ring += 2 * n;
+    if (!g.solo) ring += 2 * n;
 
     // The end of a segment.  Streams of one row tile meet here: both read both accumulators, half of the columns
     // each, which is why neither goes on before the other has read.
@@ -511,7 +535,7 @@ __device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint3
       o_par ^= 1u;
     }
     float c_own = 1.f, c_other = 0.f, M = m, Lsum = l;
-    if (!pair) {
+    if (!alone) {
       sh->row[w].ml[tid] = make_float2(m, l);
       tc_fence_before();
       meet();
@@ -524,11 +548,11 @@ __device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint3
       Lsum = (l == 0.f ? 0.f : l * c_own) + (o.y == 0.f ? 0.f : o.y * c_other);
     }
     tc_fence_after();
-    const bool fix = *static_cast<volatile int*>(&sh->fix[seg & 1]) == seg;
+    const bool fix = *static_cast<volatile int*>(&sh->fix[seg & 3]) == seg;
     const bool whole = g.t0 == 0 && g.t1 == g.nt;
     const float inv = whole ? (Lsum == 0.f || !see.used ? 0.f : 1.f / Lsum) : 1.f;
     const int chunks = (p.dim + 31) / 32;
-    const int x0 = pair || w == 0 ? 0 : (chunks + 1) / 2, x1 = pair || w == 1 ? chunks : (chunks + 1) / 2;
+    const int x0 = alone || w == 0 ? 0 : (chunks + 1) / 2, x1 = alone || w == 1 ? chunks : (chunks + 1) / 2;
     const int out_row = tree_out_row(p, g.first, g.head, inside ? r : g.r0);
     // A piece's rows lie side by side, four values each, so that the lanes' stores do.
     const int rows = p.part_rows;
@@ -551,7 +575,7 @@ __device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint3
 #pragma unroll
           for (int y = 0; y < 32; ++y) o[y] = c_own == 0.f ? 0.f : v[y] * c_own;
         }
-        if (!pair && n > 1 - w) {                  // the other stream had a tile too
+        if (!alone && n > 1 - w) {                  // the other stream had a tile too
           float v[32];
           tmem_ld32(other + 32 * x, v);
 #pragma unroll
@@ -602,13 +626,13 @@ __device__ void softmax_role(const TreeParams& p, Tail* sh, uint32_t base, uint3
         }
       }
     }
-    if (inside && (pair || w == 0)) {
+    if (inside && (alone || w == 0)) {
       const float sum = see.used ? Lsum : 0.f;
       if (whole) p.lse[out_row] = tree_lse(p, M, sum);
       else reinterpret_cast<float2*>(part)[rl] = make_float2(M, sum);
     }
     tc_fence_before();
-    if (!pair) meet();
+    if (!alone) meet();
   }
 }
 
@@ -621,7 +645,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     plan_init(sh, kSegReaders);
-    sh->fix[0] = sh->fix[1] = 0;
+    for (int& f : sh->fix) f = 0;
     for (int s = 0; s < L::kStages; ++s) {
       mbar_init(smem_u32(&sh->full[s]), 1);
       mbar_init(smem_u32(&sh->empty[s]), 1);

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paper_2608_09703_gb300 as mls
-from test_tree_attention import BF16, F32, cache_of, check, make, run, run_and_check
+from test_tree_attention import BF16, F32, cache_of, check, make, run, run_and_check, visible
 
 # lens, news, q_heads, kv_heads, dim, page
 GROUPS = [
@@ -99,3 +99,35 @@ def test_many_long_sequences(n, tree, dim):
     g = torch.Generator().manual_seed(n + dim)
     lens = [3000] + [int(3000 * float(torch.rand(1, generator=g))) for _ in range(59)]
     run_and_check(make(lens, [n] * 60, 8, 2, dim, 32, BF16, seed=n, tree=tree))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("q_heads", [8, 24])
+def test_many_short_sequences(q_heads, dim):
+    """Many short pieces of work a CTA, some with two row tiles: those that are taken side by side, and their neighbours."""
+    g = torch.Generator().manual_seed(dim + q_heads)
+    lens = [int(700 * float(torch.rand(1, generator=g)) ** 3) for _ in range(200)]
+    news = [int(torch.randint(0, 8, (1,), generator=g)) for _ in range(200)]
+    news[50], news[51], news[120] = 100, 200, 60
+    run_and_check(make(lens, news, q_heads, 4, dim, 16, BF16, seed=dim, unused=0.1))
+
+
+@pytest.mark.gpu
+def test_infinite_values_in_many_short_sequences():
+    """Each sequence's node 2 holds an infinite value: its column is infinite for the nodes that see it, nothing else is."""
+    n, S = 9, 120
+    g = torch.Generator().manual_seed(0)
+    lens = [int(300 * float(torch.rand(1, generator=g))) for _ in range(S)]
+    x = make(lens, [n] * S, 16, 8, 64, 16, BF16, seed=3, forest=0.0)
+    for b in range(S):
+        pos = lens[b] + 2
+        x["v"][0, x["table"][b, pos // 16].long(), :, pos % 16, 3] = float("inf")
+    for _ in range(5):
+        out, lse, _ = run(x)
+        assert mls.mls_get_status() == 0 and torch.isfinite(lse).all()
+        for b in range(S):
+            sees = visible(x, b)[:, lens[b] + 2]
+            mine = out[b * n:(b + 1) * n]
+            assert (mine[sees][..., 3] == float("inf")).all() and torch.isfinite(mine[~sees]).all(), b
+            assert torch.isfinite(mine[..., [d for d in range(64) if d != 3]]).all(), b
