@@ -63,8 +63,8 @@ struct Layout {
   }
 };
 
-// The order in which tiles are loaded, as the MMAs take them: for two row tiles K V K V ...; for two streams with n[0]
-// and n[1] steps of their own (a couple's, or every other tile of one segment) K K, then V of a step and K of the
+// The order in which tiles are loaded, as the MMAs take them: for two row tiles K V K V ...; for two streams with n0
+// and n1 steps of their own (a couple's, or every other tile of one segment) K K, then V of a step and K of the
 // next for each stream in turn, as far as there are any.  Where V of step i lies then:
 __device__ __forceinline__ uint32_t place_v(int n0, int n1, int w, int i) {
   const int a = i + w;                            // steps of the first stream that come before it
