@@ -414,7 +414,8 @@ int mls_grad_clip(int32_t n, void* const* g, const int64_t* numel, const int32_t
  *       layer_ld not read for one layer).
  *   mls_cache_compact  keeps tokens that were appended: keep[i] (device, int32 [n], >= 0) of them, those
  *       at positions len + path[i][k], k < keep[i], which move together behind len; len grows by keep[i]
- *       and pages past it are given back.  path (device, int32 [n, path_ld]): path[i][0] < path[i][1] < ...;
+ *       and pages past it are given back.  What the table holds behind len has to be pages of the cache
+ *       (MLS_STATUS_BAD_SEQ, and the entry is left out).  path (device, int32 [n, path_ld]): path[i][0] < path[i][1] < ...;
  *       NULL: the first keep[i] as they lie.
  *   mls_cache_fork     makes empty sequences dst[i] (strictly increasing; NULL: 0 .. n-1) copies of src[i]
  *       (any; device, int32 [n]) as they were before the call: whole pages are shared, a partly filled

@@ -365,11 +365,16 @@ __global__ void __launch_bounds__(kThreads) append_kernel(CacheView c, CacheAppe
 }
 
 // Whether an entry's path may be kept: 0 <= path[0] < path[1] < ... < what is there behind its
-// len tokens.  Then path[k] >= k.  Also the first k with path[k] != k.  The whole block calls it.
-__device__ bool path_ok(const CacheView& c, const int* path, int path_ld, int keep, int len, int held, int& first) {
+// len tokens, in pages that are all the cache's.  Then path[k] >= k.  Also the first k with path[k] != k.
+// The whole block calls it; all of an entry's blocks find the same, as nothing here changes before its closing.
+__device__ bool path_ok(const CacheView& c, int row, const int* path, int path_ld, int keep, int len, int held,
+                        int& first) {
   const long long room = (static_cast<long long>(held) << c.page_shift) - len;
   int bad = keep < 0 || keep > room || len < 0 || (path && keep > path_ld);
   int moved = 0;
+  if (!bad)
+    for (int col = (len >> c.page_shift) + threadIdx.x; col < held; col += blockDim.x)
+      bad |= !page_ok(c, c.table[static_cast<long long>(row) * c.max_pages + col]);
   if (path && !bad)
     for (int k = threadIdx.x; k < keep; k += blockDim.x) {
       const int at = path[k];
@@ -417,7 +422,7 @@ __global__ void __launch_bounds__(kThreads)
   const int* const mine = path + static_cast<long long>(blockIdx.x) * path_ld;
   const int n = keep[blockIdx.x], len = c.len[row], held = clamp_held(c, row);
   int first;
-  if (!path_ok(c, mine, path_ld, n, len, held, first)) {
+  if (!path_ok(c, row, mine, path_ld, n, len, held, first)) {
     if (kClose && threadIdx.x == 0) atomicOr(c.status, kStatusBadSeq);  // else the next kernel says so
     return;
   }
@@ -427,19 +432,14 @@ __global__ void __launch_bounds__(kThreads)
   for (int k0 = first; k0 < n; k0 += kCachePath) {
     const int m = min(kCachePath, n - k0);
     __syncthreads();
-    int bad = 0;
     for (int k = threadIdx.x; k < m; k += blockDim.x) {
       const long long a = static_cast<long long>(len) + mine[k0 + k], b = static_cast<long long>(len) + k0 + k;
       src_page[k] = table[a >> c.page_shift];
       dst_page[k] = table[b >> c.page_shift];
       src_slot[k] = static_cast<short>(a & mask);
       dst_slot[k] = static_cast<short>(b & mask);
-      bad |= !page_ok(c, src_page[k]) || !page_ok(c, dst_page[k]);
     }
-    if (__syncthreads_or(bad)) {
-      if (threadIdx.x == 0) atomicOr(c.status, kStatusBadSeq);
-      break;
-    }
+    __syncthreads();
     for (int x = blockIdx.y * blockDim.x + threadIdx.x; x < pieces; x += gridDim.y * blockDim.x) {
       const int piece = x % c.row, plane = x / c.row, head = plane % c.heads, lk = plane / c.heads;
       uint4* const pool = ((lk & 1) ? c.v : c.k) + piece;
@@ -469,7 +469,7 @@ __global__ void __launch_bounds__(kThreads)
   const int* const mine = path ? path + static_cast<long long>(blockIdx.x) * path_ld : nullptr;
   const int n = keep[blockIdx.x], len = c.len[row], held = clamp_held(c, row);
   int first;
-  if (!path_ok(c, mine, path_ld, n, len, held, first)) {
+  if (!path_ok(c, row, mine, path_ld, n, len, held, first)) {
     if (threadIdx.x == 0) atomicOr(c.status, kStatusBadSeq);
     return;
   }
