@@ -419,7 +419,8 @@ int mls_grad_clip(int32_t n, void* const* g, const int64_t* numel, const int32_t
  *       NULL: the first keep[i] as they lie.
  *   mls_cache_fork     makes empty sequences dst[i] (strictly increasing; NULL: 0 .. n-1) copies of src[i]
  *       (any; device, int32 [n]) as they were before the call: whole pages are shared, a partly filled
- *       last one is copied into a page taken as above.  Tokens behind len are not copied.
+ *       last one is copied into a page taken as above.  Tokens behind len are not copied.  A src whose table holds
+ *       what is no page raises MLS_STATUS_BAD_SEQ and is left out; a page taken for its copy is free again.
  *       ws: mls_cache_workspace_size() bytes.
  *   mls_cache_free     gives back the pages of each entry (free where no other sequence has them) and empties it.
  *   mls_cache_copy     copies page src[i] of `from` to page dst[i] of `to` (device, int32 [n]; any n), for caches of

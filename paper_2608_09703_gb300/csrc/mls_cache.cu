@@ -290,13 +290,27 @@ __global__ void __launch_bounds__(kThreads)
   const int from = src[i], to = dst ? dst[i] : i, len = length[i];
   const int full = len >> c.page_shift, part = len & ((1 << c.page_shift) - 1);
   const int* const row = c.table + static_cast<long long>(from) * c.max_pages;
+  if (blockIdx.y > 0 && part == 0) return;
+  // A source with a page that is none is left out, and the page taken for the copy is free again.  Each block
+  // looks, so that none writes.
+  int bad = 0;
+  for (int col = threadIdx.x; col < full + (part != 0); col += blockDim.x) bad |= !page_ok(c, row[col]);
+  if (__syncthreads_or(bad)) {
+    if (blockIdx.y == 0 && threadIdx.x == 0) {
+      atomicOr(c.status, kStatusBadSeq);
+      if (part) {
+        c.refs[f] = 0;
+        atomicOr(c.free_bits + (f >> 5), 1u << (f & 31));
+      }
+    }
+    return;
+  }
   if (blockIdx.y == 0) {
     int* const out = c.table + static_cast<long long>(to) * c.max_pages;
     for (int col = threadIdx.x; col < full; col += blockDim.x) {
       const int page = row[col];
       out[col] = page;
-      if (page_ok(c, page)) atomicAdd(c.refs + page, 1);
-      else atomicOr(c.status, kStatusBadSeq);
+      atomicAdd(c.refs + page, 1);
     }
     if (threadIdx.x == 0) {
       if (part) out[full] = f;
@@ -304,11 +318,7 @@ __global__ void __launch_bounds__(kThreads)
       c.len[to] = len;
     }
   }
-  if (part) {
-    const int last = row[full];
-    if (page_ok(c, last)) copy_page(c, c, last, f, part);
-    else if (threadIdx.x == 0 && blockIdx.y == 0) atomicOr(c.status, kStatusBadSeq);
-  }
+  if (part) copy_page(c, c, row[full], f, part);
 }
 
 __global__ void __launch_bounds__(kThreads) copy_kernel(CacheView from, CacheView to, const int* src, const int* dst) {

@@ -1,5 +1,5 @@
-"""A table that holds what is no page of the cache: compact leaves such an entry out, as it was to the last bit,
-and raises the status; the entries beside it are served."""
+"""A table that holds what is no page of the cache: compact and fork leave such an entry out, as it was to the
+last bit, and raise the status; the entries beside it are served."""
 import pytest
 import torch
 
@@ -73,6 +73,30 @@ def test_compact_of_a_path_of_several_turns(sizes):
     m.compact([1], [589], path[1:])
     m.status |= BAD
     c.compact(i32([589, 589]), i32(path))
+    same(c, m)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("sizes", SIZES)
+@pytest.mark.parametrize("page", NO_PAGES)
+def test_fork(sizes, page):
+    """Sources: a good one, one with a bad whole page, one whose partly filled page is bad, one of whole pages with
+    a bad one, a good one."""
+    ps = sizes[2]
+    lens = [ps + 3, 2 * ps + 1, ps + 1, 2 * ps, 2]
+    c, m = filled((sizes[0], sizes[1], ps, sizes[3], sizes[4], 10, 9), lens, [0] * 5)
+    spoil(c, m, 1, 0, page)
+    spoil(c, m, 2, 1, page)
+    spoil(c, m, 3, 1, page)
+    free = [p for p in range(m.pages) if m.refs[p] == 0]
+    # Pages are handed out in the order of the entries; those of the entries left out are free again.
+    m.fork([0], [5])
+    m.refs[free[1]] = m.refs[free[2]] = 1
+    m.fork([4], [9])
+    m.refs[free[1]] = m.refs[free[2]] = 0
+    m.status |= BAD
+    assert m.rows[9] == [free[3]]
+    c.fork(i32([0, 1, 2, 3, 4]), i32([5, 6, 7, 8, 9]))
     same(c, m)
 
 
