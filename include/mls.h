@@ -398,7 +398,8 @@ int mls_grad_clip(int32_t n, void* const* g, const int64_t* numel, const int32_t
  * A call works on n entries.  `seqs` (device, int32 [n], strictly increasing) says which sequences;
  * NULL: sequences 0 .. n-1.  An entry that is not greater than all before it, or is no sequence of
  * the cache, raises MLS_STATUS_BAD_SEQ and is left out; so is one whose other arguments break the
- * rules below.  n <= seqs of the cache, and n <= MLS_CACHE_MAX_ENTRIES (MLS_ERR_UNSUPPORTED beyond).
+ * rules below.  n <= seqs of the cache, and n <= MLS_CACHE_MAX_ENTRIES (MLS_ERR_UNSUPPORTED beyond;
+ * mls_cache_free with seqs NULL takes any n).
  * All calls are asynchronous on `stream`; calls on one cache must not overlap on the GPU.  Return 0
  * or a negative MLS_ERR_* code (nothing launched).  n = 0 is a no-op.
  *
@@ -422,7 +423,8 @@ int mls_grad_clip(int32_t n, void* const* g, const int64_t* numel, const int32_t
  *       last one is copied into a page taken as above.  Tokens behind len are not copied.  A src whose table holds
  *       what is no page raises MLS_STATUS_BAD_SEQ and is left out; a page taken for its copy is free again.
  *       ws: mls_cache_workspace_size() bytes.
- *   mls_cache_free     gives back the pages of each entry (free where no other sequence has them) and empties it.
+ *   mls_cache_free     gives back the pages of each entry (free where no other sequence has them) and empties it;
+ *       what its table holds and is no page is passed over (MLS_STATUS_BAD_SEQ).
  *   mls_cache_copy     copies page src[i] of `from` to page dst[i] of `to` (device, int32 [n]; any n), for caches of
  *       the same layers, heads, page size and type; tables and counts are not touched.  dst holds no page
  *       twice, and none that src holds if the caches share memory.

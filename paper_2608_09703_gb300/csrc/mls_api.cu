@@ -1854,10 +1854,10 @@ CacheView cache_view(const mls_cache* c, const DeviceState* dev) {
 }
 
 // The checks that the calls on entries share.
-int cache_entries(const mls_cache* c, int n, const int32_t* seqs) {
+int cache_entries(const mls_cache* c, int n, const int32_t* seqs, int most = MLS_CACHE_MAX_ENTRIES) {
   if (const int rc = cache_validate(c)) return rc;
   if (n < 0 || n > c->seqs) return MLS_ERR_ARG;
-  if (n > MLS_CACHE_MAX_ENTRIES) return MLS_ERR_UNSUPPORTED;
+  if (n > most) return MLS_ERR_UNSUPPORTED;
   if (!aligned4(seqs)) return MLS_ERR_ALIGN;
   return MLS_OK;
 }
@@ -1960,7 +1960,8 @@ extern "C" int mls_cache_fork(const mls_cache* c, int32_t n, const int32_t* src,
 }
 
 extern "C" int mls_cache_free(const mls_cache* c, int32_t n, const int32_t* seqs, mls_stream_t stream) {
-  int rc = cache_entries(c, n, seqs);
+  // Without a list no entry is looked up among those before it: every sequence of any cache.
+  int rc = cache_entries(c, n, seqs, seqs ? MLS_CACHE_MAX_ENTRIES : INT_MAX);
   if (rc) return rc;
   if (n == 0) return MLS_OK;
   DeviceState* dev = nullptr;
