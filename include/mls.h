@@ -409,7 +409,9 @@ int mls_grad_clip(int32_t n, void* const* g, const int64_t* numel, const int32_t
  *       entries.  An entry gets its pages if they and those of all entries before it are there.
  *   mls_cache_append   writes new tokens' keys and values behind len (which stays as it is).  start
  *       (device, int32 [n + 1], not decreasing, within [0, N]): entry i has tokens start[i] .. start[i+1]-1
- *       of k_new and v_new, which go to positions len, len + 1, ...; other tokens go nowhere.  layer >= 0:
+ *       of k_new and v_new, which go to positions len, len + 1, ...; other tokens go nowhere.  An entry whose
+ *       offsets leave [0, N], go back or begin before those of one in front raises MLS_STATUS_BAD_SEQ and is
+ *       left out.  layer >= 0:
  *       k_new and v_new are [N, kv_heads, head_dim] of that layer; layer = -1: [layers, N, ...] of all.
  *       token_ld, layer_ld: values between tokens and between layers (multiples of 16 bytes;
  *       layer_ld not read for one layer).

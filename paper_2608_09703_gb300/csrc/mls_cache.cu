@@ -334,14 +334,25 @@ __global__ void __launch_bounds__(kThreads) copy_kernel(CacheView from, CacheVie
 __global__ void __launch_bounds__(kThreads) append_kernel(CacheView c, CacheAppend a) {
   __shared__ int entry;
   const long long t = blockIdx.x;
-  if (threadIdx.x == 0) entry = -1;
+  if (threadIdx.x == 0) entry = INT_MAX;
   __syncthreads();
-  // start[] does not decrease, so at most one entry holds the token; of an unsorted one any that does.
-  for (int i = threadIdx.x; i < a.n; i += blockDim.x)
-    if (a.start[i] <= t && t < a.start[i + 1]) atomicMax(&entry, i);
-  __syncthreads();
+  // Each block looks at all offsets.  Of the entries whose own are in order only the first that holds the token can
+  // have it: one behind it that holds it too begins before the end of the first, where the entry after the first begins.
+  int bad = 0;
+  for (int i = threadIdx.x; i < a.n; i += blockDim.x) {
+    const int from = a.start[i], to = a.start[i + 1];
+    if (from < 0 || to < from || to > a.N) bad = 1;
+    else if (from <= t && t < to) atomicMin(&entry, i);
+  }
+  bad = __syncthreads_or(bad);
   const int i = entry;
-  if (i < 0) return;  // behind the last entry
+  if (bad) {
+    if (threadIdx.x == 0) atomicOr(c.status, kStatusBadSeq);
+    int late = 0;  // it begins before one in front of it does
+    for (int j = threadIdx.x; i < a.n && j < i; j += blockDim.x) late |= a.start[j] > a.start[i];
+    if (__syncthreads_or(late)) return;
+  }
+  if (i >= a.n) return;  // a token of no entry
   const int row = entry_row(c, a.seqs, i);
   if (row < 0) return;
   const long long at = c.len[row] + (t - a.start[i]);
