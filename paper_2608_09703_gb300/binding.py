@@ -1085,8 +1085,10 @@ class PagedCache:
 
     def copy(self, src, dst, to=None, stream=None):
         """Copies pages src to pages dst (of another cache of this geometry, if given)."""
+        to = self if to is None else to
         self.home()
-        mls_cache_copy(self.c, self.c if to is None else to.c, src, dst, stream)
+        to.home()
+        mls_cache_copy(self.c, to.c, src, dst, stream)
 
 
 class TreeAttention:
