@@ -2088,6 +2088,7 @@ extern "C" int mls_tree_attention(const mls_cache* c, int32_t layer, int32_t n, 
   p.joins = static_cast<TreeJoin*>(ws);
   p.part = reinterpret_cast<float*>(static_cast<char*>(ws) + align_up(sizeof(TreeJoin) * p.sms));
   p.status = dev->status;
+  p.test_stall = std::getenv("MLS_TEST_STALL_FIRST_STAGE") != nullptr;  // as for the head kernels: a wait that runs out
   if (encode_pages(&p.map_k, c, c->k, p) || encode_pages(&p.map_v, c, c->v, p) || (p.q_rows && encode_queries(&p)))
     return MLS_ERR_CUDA;
   return timed("tree_attention", s, [&] { return p.bf16 ? launch_tree_bf16(p, s) : launch_tree_fp32(p, s); });

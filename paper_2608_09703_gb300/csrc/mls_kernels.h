@@ -607,6 +607,7 @@ struct TreeParams {
   TreeJoin* joins;               // [CTAs]
   int* status;
   int sms;
+  int test_stall;                // test hook: see tree_skipped (0 in normal use)
 };
 constexpr int kTreeMaxNodes = 256;
 void tree_sizes(TreeParams* p);  // those that follow from bf16, group, n and N

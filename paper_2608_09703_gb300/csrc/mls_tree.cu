@@ -48,6 +48,7 @@ __device__ void load_role(const TreeParams& p, Plan* sh, uint64_t* full, uint64_
   const int parts = p.dim > 64 ? 4 : 2, mine = lane / parts, part = lane - mine * parts;
   const bool active = mine < boxes;
   const int none = p.c.layers * p.c.pages * p.c.heads;  // a box there is filled with zeros
+  const uint32_t skipped = tree_skipped(p);
   uint32_t ring = 0;
   bool ok = true;
   Seg g;
@@ -64,8 +65,11 @@ __device__ void load_role(const TreeParams& p, Plan* sh, uint64_t* full, uint64_
         else atomicOr(p.status, kStatusBadSeq);
       }
       for (int v = 0; v < 2; ++v, ++ring) {
+        if (ring < skipped) continue;
         const uint32_t stage = ring % kStages;
-        ok = __all_sync(0xffffffffu, wait(p, sh, &empty[stage], ((ring / kStages) & 1u) ^ 1u));
+        // (Warps whose wait for a stage ran out give it back all the same.  Filling it again would make its phases
+        // other than its rounds, and the wait for copies at the end would miss some.)
+        ok = __all_sync(0xffffffffu, wait_or_stop(p, sh, &empty[stage], ((ring / kStages) & 1u) ^ 1u));
         if (!ok) break;
         const uint32_t bar = smem_u32(&full[stage]);
         if (lane == 0) mbar_arrive_expect_tx(bar, parts * kPiece);
@@ -76,7 +80,7 @@ __device__ void load_role(const TreeParams& p, Plan* sh, uint64_t* full, uint64_
     }
   }
   if (lane == 0)  // what was asked for lands before the shared memory goes away
-    for (uint32_t b = ring > kStages ? ring - kStages : 0; b < ring; ++b)
+    for (uint32_t b = ring > kStages ? ring - kStages : skipped; b < ring; ++b)
       mbar_wait_drain(smem_u32(&full[b % kStages]), (b / kStages) & 1u, kDrainNs, p.status);
   __syncwarp();
 }

@@ -99,6 +99,13 @@ struct Plan {
 __device__ __forceinline__ bool wait(const TreeParams& p, Plan* sh, uint64_t* bar, uint32_t parity) {
   return mbar_wait(smem_u32(bar), parity, &sh->abort, p.status);
 }
+// As `wait`, for one who is to stop where another gave up, even if what it waits for came.
+__device__ __forceinline__ bool wait_or_stop(const TreeParams& p, Plan* sh, uint64_t* bar, uint32_t parity) {
+  return wait(p, sh, bar, parity) && !*static_cast<volatile int*>(&sh->abort);
+}
+// Test hook (off unless the host sets it): stages at the beginning that each CTA brings nothing for, so that the wait for
+// them runs out.  (Each: which CTAs have tiles depends on the lengths.)
+__device__ __forceinline__ uint32_t tree_skipped(const TreeParams& p) { return p.test_stall != 0; }
 __device__ inline void plan_init(Plan* sh, int readers) {
   sh->abort = 0;
   for (int k = 0; k < kSegs; ++k) {

@@ -80,7 +80,7 @@ __device__ void load_role(const TreeParams& p, Tail* sh, uint32_t base) {
   const int mine = lane / kParts, part = lane - mine * kParts;  // this lane's box of a tile: boxes * kParts <= 32
   const bool active = mine < boxes;
   const int none = p.c.layers * p.c.pages * p.c.heads;        // a box there is filled with zeros
-  const uint32_t dst = part * L::kPiece + mine * (box >> 3) * L::kAtom;
+  const uint32_t dst = part * L::kPiece + mine * (box >> 3) * L::kAtom, skipped = tree_skipped(p);
   uint32_t ring = 0;
   bool ok = true;
   Seg g;
@@ -112,6 +112,10 @@ __device__ void load_role(const TreeParams& p, Tail* sh, uint32_t base) {
         if (page >= 0 && page < p.c.pages) at = (p.layer * p.c.pages + page) * p.c.heads + (second ? head : g.head);
         else atomicOr(p.status, kStatusBadSeq);
       }
+      if (ring < skipped) {
+        ++ring;
+        continue;
+      }
       const uint32_t stage = ring % L::kStages, phase = (ring / L::kStages) & 1u;
       ok = __all_sync(0xffffffffu, wait(p, sh, &sh->empty[stage], phase ^ 1u));
       if (!ok) break;
@@ -127,7 +131,7 @@ __device__ void load_role(const TreeParams& p, Tail* sh, uint32_t base) {
     }
   }
   if (lane == 0)  // what was asked for lands before the shared memory goes away
-    for (uint32_t b = ring > L::kStages ? ring - L::kStages : 0; b < ring; ++b)
+    for (uint32_t b = ring > L::kStages ? ring - L::kStages : skipped; b < ring; ++b)
       mbar_wait_drain(smem_u32(&sh->full[b % L::kStages]), (b / L::kStages) & 1u, kDrainNs, p.status);
   __syncwarp();
 }
