@@ -1876,7 +1876,7 @@ extern "C" int mls_cache_reset(const mls_cache* c, mls_stream_t stream) {
   DeviceState* dev = nullptr;
   if ((rc = device_state(&dev))) return rc;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  return timed("cache_reset", s, [&] { return launch_cache_reset(cache_view(c, dev), s); });
+  return timed("cache_reset", s, [&] { return launch_cache_reset(cache_view(c, dev), dev->sms, s); });
 }
 
 extern "C" int mls_cache_reserve(const mls_cache* c, int32_t n, const int32_t* seqs, const int32_t* count,
@@ -1921,7 +1921,7 @@ extern "C" int mls_cache_append(const mls_cache* c, int32_t layer, int32_t n, co
   a.token_ld = token_ld / width;
   a.layer_ld = layer < 0 ? layer_ld / width : 0;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  return timed("cache_append", s, [&] { return launch_cache_append(cache_view(c, dev), a, s); });
+  return timed("cache_append", s, [&] { return launch_cache_append(cache_view(c, dev), a, dev->sms, s); });
 }
 
 extern "C" int mls_cache_compact(const mls_cache* c, int32_t n, const int32_t* seqs, const int32_t* keep,

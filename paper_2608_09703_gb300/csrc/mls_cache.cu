@@ -508,8 +508,8 @@ int spread(long long n, long long pieces, int deep, int sms) {
 
 }  // namespace
 
-cudaError_t launch_cache_reset(const CacheView& c, cudaStream_t s) {
-  reset_kernel<<<152, kThreads, 0, s>>>(c);
+cudaError_t launch_cache_reset(const CacheView& c, int sms, cudaStream_t s) {
+  reset_kernel<<<sms, kThreads, 0, s>>>(c);
   return cudaGetLastError();
 }
 
@@ -533,9 +533,9 @@ cudaError_t launch_cache_fork(const CacheView& c, int n, const int* src, const i
                         static_cast<const int*>(fresh), static_cast<const int*>(length));
 }
 
-cudaError_t launch_cache_append(const CacheView& c, const CacheAppend& a, cudaStream_t s) {
+cudaError_t launch_cache_append(const CacheView& c, const CacheAppend& a, int sms, cudaStream_t s) {
   const long long pieces = 2LL * a.layers * c.heads * c.row;
-  append_kernel<<<dim3(static_cast<unsigned>(a.N), spread(a.N, pieces, 4, 152)), kThreads, 0, s>>>(c, a);
+  append_kernel<<<dim3(static_cast<unsigned>(a.N), spread(a.N, pieces, 4, sms)), kThreads, 0, s>>>(c, a);
   return cudaGetLastError();
 }
 

@@ -554,7 +554,7 @@ __host__ __device__ inline long long cache_at(const CacheView& c, int layer, int
 }
 constexpr int kCacheMaxEntries = 8192;  // entries of one call: a prefix over them stays in shared memory
 constexpr int kCachePath = 256;         // path tokens whose places a block keeps at a time
-cudaError_t launch_cache_reset(const CacheView& c, cudaStream_t s);
+cudaError_t launch_cache_reset(const CacheView& c, int sms, cudaStream_t s);
 cudaError_t launch_cache_free(const CacheView& c, int n, const int* seqs, cudaStream_t s);
 cudaError_t launch_cache_reserve(const CacheView& c, int n, const int* seqs, const int* count, cudaStream_t s);
 // fresh, length: [n] each, handed from the first kernel to the second
@@ -568,7 +568,7 @@ struct CacheAppend {
   const uint4 *k, *v;
   long long token_ld, layer_ld;  // pieces between tokens and between layers of k and of v
 };
-cudaError_t launch_cache_append(const CacheView& c, const CacheAppend& a, cudaStream_t s);
+cudaError_t launch_cache_append(const CacheView& c, const CacheAppend& a, int sms, cudaStream_t s);
 cudaError_t launch_cache_compact(const CacheView& c, int n, const int* seqs, const int* keep, const int* path,
                                  int path_ld, int sms, cudaStream_t s);
 cudaError_t launch_cache_copy(const CacheView& from, const CacheView& to, int n, const int* src, const int* dst,
