@@ -256,6 +256,7 @@ __device__ void draw(const AcceptParams& p, Walk& s, const Pass& a, long long ro
     }
   }
   __syncthreads();
+  MLS_CHECK(p.status, s.found == INT_MAX ? s.last >= v0 && s.last < v1 : s.found >= v0 && s.found < v1);
   if (tid == 0) *next = s.found != INT_MAX ? s.found : s.last;  // the goal within rounding of the part's end
 }
 
@@ -340,6 +341,7 @@ __global__ void __launch_bounds__(kThreads, 4) accept_kernel(AcceptParams p) {
         else if (again) w = 0.0;
         if (q > 0.0 && static_cast<double>(s.u[d]) * q * Z < w) {
           cur = d;
+          MLS_CHECK(p.status, depth < n && d < n);
           if (rank == 0 && lane == 0) path[depth] = d;
           ++depth;
           refused = 0;
@@ -350,6 +352,7 @@ __global__ void __launch_bounds__(kThreads, 4) accept_kernel(AcceptParams p) {
           c_old = c;
           c += share * Z;
           listed = (distinct || !drafted) && x >= 0 && x < p.V && !again;
+          MLS_CHECK(p.status, refused < kTreeMaxNodes);
           if (listed && lane == 0) {
             s.refused[refused] = x;
             split(c, s.c_hi[refused], s.c_lo[refused]);
@@ -389,6 +392,7 @@ __global__ void __launch_bounds__(kThreads, 4) accept_kernel(AcceptParams p) {
     }
     __syncthreads();
     const int part = s.part;
+    MLS_CHECK(p.status, part < warps);
     if (part < 0 || part / kWarps != rank) return;  // -1: a row without mass
     const long long b0 = min(part * each, p.V), b1 = min(b0 + each, p.V);
     if (a.with_draft) draw<true>(p, s, a, row, b0, b1, p.next + b);

@@ -225,6 +225,7 @@ __global__ void __launch_bounds__(kTake)
       const bool mine_too = (b >> lane & 1u) && r < limit;
       if (mine_too) {
         const int page = (w0 + x) * 32 + lane;
+        MLS_CHECK(c.status, page < c.pages && c.refs[page] == 0);
         int e = 0, e1 = served - 1;  // the last entry whose range begins at or before r: it is not empty
         while (e < e1) {
           const int mid = (e + e1 + 1) >> 1;
@@ -235,6 +236,7 @@ __global__ void __launch_bounds__(kTake)
           fresh[e] = page;
         } else {
           const int row = seqs ? seqs[e] : e;
+          MLS_CHECK(c.status, e < served && r >= pre[e] && r < pre[e + 1] && clamp_held(c, row) + (r - pre[e]) < c.max_pages);
           c.table[static_cast<long long>(row) * c.max_pages + clamp_held(c, row) + (r - pre[e])] = page;
         }
         c.refs[page] = 1;
@@ -263,6 +265,7 @@ __device__ void copy_page(const CacheView& from, const CacheView& to, int src, i
   // 64 prompts of 28 layers took 26 us, so 23.)
   const unsigned each = static_cast<unsigned>(slots) * from.row, planes = 2u * from.layers * from.heads;
   const unsigned all = each * planes, step = gridDim.y * blockDim.x;
+  MLS_CHECK(from.status, page_ok(from, src) && page_ok(to, dst) && slots <= 1 << from.page_shift);
   for (unsigned i = blockIdx.y * blockDim.x + threadIdx.x; i < all; i += step * kDeep) {
     uint4 v[kDeep];
     uint4* at[kDeep];
@@ -363,6 +366,7 @@ __global__ void __launch_bounds__(kThreads) append_kernel(CacheView c, CacheAppe
     return;
   }
   const int slot = static_cast<int>(at & ((1 << c.page_shift) - 1));
+  MLS_CHECK(c.status, t >= a.start[i] && t < a.start[i + 1] && t < a.N && a.layer0 + a.layers <= c.layers);
   const int each = c.heads * c.row, all = 2 * a.layers * each;
   const int step = gridDim.y * blockDim.x;
   constexpr int kAhead = 4;
@@ -459,6 +463,7 @@ __global__ void __launch_bounds__(kThreads)
       dst_page[k] = table[b >> c.page_shift];
       src_slot[k] = static_cast<short>(a & mask);
       dst_slot[k] = static_cast<short>(b & mask);
+      MLS_CHECK(c.status, b <= a && (a >> c.page_shift) < held && page_ok(c, src_page[k]) && page_ok(c, dst_page[k]));
     }
     __syncthreads();
     for (int x = blockIdx.y * blockDim.x + threadIdx.x; x < pieces; x += gridDim.y * blockDim.x) {

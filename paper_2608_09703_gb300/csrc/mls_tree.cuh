@@ -223,9 +223,12 @@ __device__ inline void plan_role(const TreeParams& p, Plan* sh, const Range& ran
       g->slot = first ? 0 : 1;
       g->solo = g->other = 0;
       first = false;
+      MLS_CHECK(p.status, head < p.c.heads && g->nrows > 0 && g->nrows <= p.part_rows && t1 <= u.nt && (u.nt - 1) << p.key_shift < g->total &&
+                              g->first + (r0 + g->nrows - 1) / p.group < p.N);
       if (t0 == 0 && t1 < u.nt) {                 // at = hi: the range ends after tile t1 of the item
         join.pieces = 1 + static_cast<int>((u.nt - t1 + range.each - 1) / range.each);
         join.slot = g->slot;
+        MLS_CHECK(p.status, blockIdx.x + join.pieces <= gridDim.x);
         join.rows = g->nrows;
         join.first = static_cast<int>(en.first);
         join.r0 = r0;
