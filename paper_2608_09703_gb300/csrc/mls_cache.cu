@@ -6,8 +6,10 @@
 // change by integer atomics whose order does not matter, and no list remembers an order.
 //
 // What moves data (append, fork, compact, copy) reads each byte once and writes it once, in
-// pieces of 16 bytes, several of them in flight per thread; HBM bounds it.  The rest touches a
-// few words per page and is bound by the latency of its chain of loads.
+// pieces of 16 bytes, several of them in flight per thread; HBM bounds it.  (Not where an append has
+// thousands of entries: each of its blocks looks at all offsets, and 8192 of a token each take 68 us
+// where their bytes take 10.)  The rest touches a few words per page and is bound by the latency of
+// its chain of loads.
 //
 // The calls take entries (rows of the table) in strictly increasing order, which every
 // block can check for its own entry by looking at those before it.
@@ -294,10 +296,11 @@ __global__ void __launch_bounds__(kThreads)
   const int full = len >> c.page_shift, part = len & ((1 << c.page_shift) - 1);
   const int* const row = c.table + static_cast<long long>(from) * c.max_pages;
   if (blockIdx.y > 0 && part == 0) return;
+  const int last = part ? row[full] : 0;
   // A source with a page that is none is left out, and the page taken for the copy is free again.  Each block
-  // looks, so that none writes.
-  int bad = 0;
-  for (int col = threadIdx.x; col < full + (part != 0); col += blockDim.x) bad |= !page_ok(c, row[col]);
+  // looks, so that none writes: 0.6 of 14.3 us for 64 samples of 28 layers.
+  int bad = !page_ok(c, last);
+  for (int col = threadIdx.x; col < full; col += blockDim.x) bad |= !page_ok(c, row[col]);
   if (__syncthreads_or(bad)) {
     if (blockIdx.y == 0 && threadIdx.x == 0) {
       atomicOr(c.status, kStatusBadSeq);
@@ -321,7 +324,7 @@ __global__ void __launch_bounds__(kThreads)
       c.len[to] = len;
     }
   }
-  if (part) copy_page(c, c, row[full], f, part);
+  if (part) copy_page(c, c, last, f, part);
 }
 
 __global__ void __launch_bounds__(kThreads) copy_kernel(CacheView from, CacheView to, const int* src, const int* dst) {
