@@ -605,7 +605,7 @@ def mls_cache_reserve(c: mls_cache, seqs, count, stream=None) -> None:
     _check(rc, "mls_cache_reserve")
 
 
-def _token_stride(name: str, t: torch.Tensor) -> int:
+def _token_stride(t: torch.Tensor) -> int:
     """Values between tokens of t [..., N, heads, dim]."""
     return t.stride(-3) if t.shape[-3] > 1 else t.shape[-2] * t.shape[-1]
 
@@ -621,7 +621,7 @@ def mls_cache_append(c: mls_cache, layer: int, seqs, start, k_new, v_new, stream
     if k_new.numel() and k_new.stride() != v_new.stride():
         raise ValueError(f"k_new, v_new: strides {k_new.stride()} and {v_new.stride()}")
     rc = lib().mls_cache_append(ctypes.byref(c), layer, n, _entries(c, seqs, n, dev), _ptr(start), N, _ptr(k_new),
-                                _ptr(v_new), _token_stride("k_new", k_new),
+                                _ptr(v_new), _token_stride(k_new),
                                 0 if layer >= 0 or c.layers == 1 else k_new.stride(0), _stream(stream))
     _check(rc, "mls_cache_append")
 
@@ -675,7 +675,7 @@ def mls_tree_attention(c: mls_cache, layer: int, seqs, start, parents, q, scale:
     _expect("lse", lse, torch.float32, (N, heads), dev)
     wsp, wsn = _ws_args(ws, dev)
     rc = lib().mls_tree_attention(ctypes.byref(c), layer, n, _entries(c, seqs, n, dev), _ptr(start), _ptr(parents),
-                                  N, heads, _ptr(q), _token_stride("q", q), float(scale), _ptr(out), _ptr(lse), wsp,
+                                  N, heads, _ptr(q), _token_stride(q), float(scale), _ptr(out), _ptr(lse), wsp,
                                   wsn, _stream(stream))
     _check(rc, "mls_tree_attention")
 
@@ -1118,7 +1118,7 @@ class TreeAttention:
         if seqs is not None:
             _expect("seqs", seqs, i32, (self.S,), dev)
         rc = lib().mls_tree_attention(cache.ref, layer, self.S, _ptr(seqs), start.data_ptr(), _ptr(parents), self.N,
-                                      self.shape[1], q.data_ptr(), _token_stride("q", q), self.scale,
+                                      self.shape[1], q.data_ptr(), _token_stride(q), self.scale,
                                       self.out.data_ptr(), self.lse.data_ptr(), self.ws.data_ptr(), self.ws.numel(),
                                       _stream(stream))
         _check(rc, "mls_tree_attention")
