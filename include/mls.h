@@ -472,8 +472,9 @@ int mls_cache_copy(const mls_cache* from, const mls_cache* to, int32_t n, const 
  *   seqs       device, int32 [n], in any order, or NULL: sequences 0 .. n-1.  A sequence that is none of
  *              the cache's, or whose len and nodes the table cannot hold, raises MLS_STATUS_BAD_SEQ
  *              and its nodes take no part; a page that is none counts as zeros and raises it too.
- *   start      device, int32 [n + 1], not decreasing, within [0, N].  Tokens in no entry keep their
- *              out and lse.
+ *   start      device, int32 [n + 1], not decreasing, within [0, N].  An entry whose own two break that
+ *              raises MLS_STATUS_BAD_SEQ and is left out; where others overlap then, the out and lse of
+ *              their tokens mean nothing.  Tokens in no entry keep their out and lse.
  *   q          device, [N, q_heads, head_dim] of the cache's type, q_ld values between tokens;
  *              16-byte aligned, q_ld a multiple of 16 bytes
  *   out        device, [N, q_heads, head_dim], dense, 16-byte aligned; lse: device, fp32 [N, q_heads]

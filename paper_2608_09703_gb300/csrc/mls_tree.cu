@@ -9,7 +9,7 @@
 // of it 8 columns, of the queries and of the product, in registers; a key's partial scores are added up by exchanges
 // that leave each lane one row.  That asks shared memory for 8 of the 16 words a key and lane that it does for each of
 // K and V (with rows over four groups of lanes and queries in shared memory 64 single tokens over 10000 took 766 us, now
-// 534: 99% of the copy rate; 8 nodes of 16 heads over 30000 340 us, now 290).  Warps keep a maximum,
+// 528: 99% of the copy rate; 8 nodes of 16 heads over 30000 340 us, now 281).  Warps keep a maximum,
 // sum and product of their own to the end of a segment.
 #include <cmath>
 

@@ -10,11 +10,13 @@
 // a row tile each are taken side by side, a stream each: what begins and ends one hides behind the other.
 // Items are pairs of row tiles of an entry and key/value head, cut into ranges as mls_tree.cuh has it.
 //
-// Softmax in one pass: a running maximum per row, which moves only when it grows by more than 2^8 (P stays
-// below 256, exact enough in bf16), so that O is rarely rescaled.  Only tiles past the cached tokens look at
-// masks.  Masked weights are 0, and so that 0 times what lies there is 0 too, values behind the item's last
-// node are cleared, and infinities and NaN among the nodes' values taken out of the product and added to the
-// rows that do see them.
+// Softmax in one pass: a running maximum per row, which moves only where weights would pass 2^8, so that O is
+// rarely rescaled (a published technique: rescaling past a threshold only).  Scores, sums, maxima and O are fp32; P
+// is rounded to bf16 for its product, as the tensor cores take operands of one type and V is bf16.  That moves each
+// weight by 2^-9 on average, whatever its size: 1.5e-3 of out's norm, beside the 1.7e-3 of rounding out itself.
+// Only tiles past the cached tokens look at masks.  Masked weights are 0, and so that 0 times what lies there is 0
+// too, values behind the item's last node are cleared, and infinities and NaN among the nodes' values taken out of
+// the product and added to the rows that do see them.
 #include <cmath>
 
 #include "mls_device.cuh"
